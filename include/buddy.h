@@ -73,7 +73,7 @@ enum {
   BUDDY_ERR_STATE = 5     /* call order: e.g. weights not set */
 };
 
-enum { BUDDY_DTYPE_F32 = 0, BUDDY_DTYPE_BF16 = 1 };
+enum { BUDDY_DTYPE_F32 = 0, BUDDY_DTYPE_BF16 = 1, BUDDY_DTYPE_F16 = 2 /* buddy_kv4_read only */ };
 
 /* Planner feature G_t pooled from the context layer's cache (Sec. 4.3; the
  * Sec. 5.4 ablation "Hidden-State Features"): value states (the paper's
@@ -92,7 +92,9 @@ enum {
   BUDDY_DEV_BAD_BUDGET = 1,    /* k_i outside [1, L-2-c] (0 without a Budget Predictor) */
   BUDDY_DEV_BAD_POSITION = 2,  /* len_i + new positions > cap_i or > max_pos */
   BUDDY_DEV_BAD_SEQ = 4,       /* a sequence id outside [0, batch) */
-  BUDDY_DEV_TIMEOUT = 8        /* a bounded wait inside a kernel ran out */
+  BUDDY_DEV_TIMEOUT = 8,       /* a bounded wait inside a kernel ran out */
+  BUDDY_DEV_NO_PAGES = 16,     /* the list of free pages is shorter than what a plan needs */
+  BUDDY_DEV_BAD_PAGE = 32      /* a page id outside [0, n_pages) (a slot's or a table's) */
 };
 
 typedef struct buddy_ctx buddy_ctx;
@@ -366,6 +368,181 @@ BUDDY_API int buddy_device_status(buddy_ctx* ctx, void* stream, int32_t* flags);
  * ties to even), clamped to the action space [1, L-2] (Sec. 4.4).
  * Returns -1 if n_layers < 3 or b is not finite. */
 BUDDY_API int32_t buddy_budget_to_k(float b, int32_t n_layers);
+
+/* ---------------------------------------------------------------------------
+ * Paged KV cache in 4 bits.  The paper has no counterpart; it is the cache of
+ * deployments whose batches are bound by the bytes of keys and values, or whose
+ * sequences (and the blocks that skip them) grow at different rates.  The
+ * entries below need no context and allocate nothing.
+ *
+ * One layer's cache is n_pages pages of page_size positions for the keys and as
+ * many for the values.  A page holds one block per KV head; block (page p, head
+ * g) starts at byte (p * n_kv_heads + g) * page_size * (hd/2 + hd/16) and holds
+ *   codes   [page_size][hd/2]   4 bits per channel,
+ *   scales  [page_size][hd/32]  IEEE half, one per 32 channels.
+ * Channels 8w .. 8w + 7 are the 32-bit little-endian word w of the position's
+ * codes: bits 4j .. 4j + 3 hold channel 8w + 2j (j < 4) or 8w + 2(j - 4) + 1
+ * (j >= 4).  The value of a channel is (code - 8) * scale, code 1 .. 15.
+ *
+ * An entry x of 32 channels is stored with
+ *   scale = max|x| / 7 rounded to 7 significant bits (ties to even), then to
+ *           half, at most 896,
+ *   code  = 8 + x / scale rounded to the nearest integer (ties to even), kept in
+ *           [-7, 7]; 8 where the scale is 0.
+ * A NaN among the 32 makes the scale NaN, and so the 32 values; an infinite
+ * channel takes the largest value of the largest scale (6272).
+ *
+ * Position p of a sequence is at slot table[p / page_size] * page_size +
+ * p % page_size.  Pages belong to one sequence each.  What a cache holds behind
+ * a sequence's last position may be anything.
+ *
+ * `flags` of the entries below: device int32, or NULL.  A kernel that meets a
+ * bad value in device memory sets its BUDDY_DEV_* bit there and leaves out what
+ * the entry says; nothing clears the word. */
+typedef struct {
+  void* k_pages;        /* device, n_pages * n_kv_heads blocks; 16-byte aligned */
+  void* v_pages;        /* device, as k_pages */
+  int32_t n_pages;      /* >= 1 */
+  int32_t page_size;    /* positions of a page: 16, 32, 64 or 128 */
+  int32_t n_kv_heads;   /* 1 .. 1024 */
+  int32_t head_dim;     /* 64 or 128 */
+} buddy_kv4_cache;
+
+/* Block tables and slot maps from request lengths.  Sequence i holds len[i]
+ * positions in the first ceil(len[i] / page_size) pages of its table row and is
+ * to take n_new[i] >= 0 more (len[i] = 0: a request that starts).  The pages it
+ * lacks come from free_pages, in order, from index *free_head on: first those of
+ * sequence 0, then of sequence 1, ...
+ * Written: those table entries (others are left as they are); kv_len[i] = len[i]
+ * + n_new[i]; row_start[i] = new tokens before sequence i, row_start[batch] =
+ * their number; for token t of the call its slot and its position; -1 for both
+ * behind the last token, up to n_tok; *free_head_out = the index after the last
+ * page taken.  No output may overlap an input other than `table`.
+ * Device-checked: lengths >= 0, len[i] + n_new[i] <= max_pages * page_size, at
+ * most n_tok new tokens (BUDDY_DEV_BAD_POSITION); 0 <= *free_head and as many free
+ * pages left as the call needs (BUDDY_DEV_NO_PAGES); on failure nothing is
+ * written. */
+typedef struct {
+  int32_t batch;              /* 1 .. 16384 */
+  int32_t page_size;          /* a power of two, 1 .. 65536 */
+  int32_t max_pages;          /* entries of a table row */
+  int32_t n_free;             /* entries of free_pages */
+  int32_t n_tok;              /* entries of slot and pos */
+  const int32_t* len;         /* device [batch] */
+  const int32_t* n_new;       /* device [batch] */
+  int32_t* table;             /* device [batch, max_pages] page ids */
+  const int32_t* free_pages;  /* device [n_free] page ids (may be NULL when n_free is 0) */
+  const int32_t* free_head;   /* device */
+  int32_t* kv_len;            /* device [batch] */
+  int32_t* row_start;         /* device [batch + 1] */
+  int64_t* slot;              /* device [n_tok] (may be NULL when n_tok is 0) */
+  int32_t* pos;               /* device [n_tok], as slot */
+  int32_t* free_head_out;     /* device */
+} buddy_page_plan_args;
+BUDDY_API int buddy_page_plan(const buddy_page_plan_args* args, int32_t* flags, void* stream);
+
+/* Rotary tables: cos and sin of p * theta^(-2j / head_dim), device [max_pos,
+ * head_dim / 2] each, evaluated in double and stored fp32. */
+BUDDY_API int buddy_rope_table(float* rope_cos, float* rope_sin, int32_t max_pos, int32_t head_dim,
+                               float rope_theta, void* stream);
+
+/* Query and key heads of n_tok tokens.  Head h of token t is head_dim
+ * consecutive elements from element t * stride + h * head_dim on.  All rows
+ * 16-byte aligned: pointers, and strides in bytes. */
+typedef struct {
+  int32_t n_tok;         /* >= 0 */
+  int32_t n_q_heads;     /* >= 0 (0: no queries; q, q_out unused) */
+  int32_t n_kv_heads;    /* >= 1 */
+  int32_t head_dim;      /* 64 or 128 */
+  int32_t dtype;         /* BUDDY_DTYPE_F32 or _BF16: q, k, v and the outputs */
+  int32_t max_pos;       /* rows of the rotary tables */
+  float eps;             /* of the norms, > 0 */
+  const void* q;         /* device */
+  const void* k;         /* device */
+  int64_t q_stride;      /* elements from token to token */
+  int64_t k_stride;
+  const float* q_gain;   /* device [head_dim], or NULL: no norm of the queries */
+  const float* k_gain;   /* device [head_dim], or NULL: no norm of the keys */
+  const int32_t* pos;    /* device [n_tok] positions; negative: the token is left out */
+  const float* rope_cos; /* device [max_pos, head_dim / 2] */
+  const float* rope_sin;
+  void* q_out;           /* device; may be q with q's stride */
+  void* k_out;           /* device; may be k with k's stride */
+  int64_t q_out_stride;
+  int64_t k_out_stride;
+} buddy_qk_rows;
+
+/* The norm of every query and key head and its rotation, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * gain,
+ *   out[j] = y[j] cos_j - y[j + hd/2] sin_j,  out[j + hd/2] = y[j + hd/2] cos_j + y[j] sin_j,
+ * in fp32, rounded once.  The sum of squares is taken in a fixed order (halves
+ * onto each other inside eight neighbours, then over the eights), without fused
+ * multiply-adds, so that equal inputs give equal bits in any batch.
+ * Device-checked: pos[t] < max_pos (BUDDY_DEV_BAD_POSITION; the token's outputs
+ * are left as they were, as for a negative position, which sets no bit). */
+BUDDY_API int buddy_qk_norm_rope(const buddy_qk_rows* rows, int32_t* flags, void* stream);
+
+/* The same for a block that keeps its entries in a 4-bit cache: queries to
+ * q_out; keys, normalised and rotated, and values v (device, rows as k's with
+ * stride v_stride) into the cache at slot[t]; keys also to rows->k_out unless
+ * that is NULL.  Keys are quantised from their fp32 values.  A token with a
+ * negative slot stores no entry (its queries are written).  The slots of a call
+ * must be distinct.  Device-checked: positions as above (the token is left out
+ * as a whole); slot[t] < n_pages * page_size (BUDDY_DEV_BAD_PAGE; no entry is
+ * stored). */
+BUDDY_API int buddy_kv4_append(const buddy_kv4_cache* cache, const buddy_qk_rows* rows, const void* v,
+                               int64_t v_stride, const int64_t* slot, int32_t* flags, void* stream);
+
+/* The values that the cache holds at n slots: k_out, v_out device [n,
+ * n_kv_heads, head_dim] of dtype BUDDY_DTYPE_F32 or _F16 (both exact) or _BF16
+ * (rounded), 16-byte aligned; either may be NULL.  Rows of negative slots are
+ * left as they were, and those of slots past the last page (BUDDY_DEV_BAD_PAGE). */
+BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int64_t* slot, int32_t dtype,
+                             void* k_out, void* v_out, int32_t* flags, void* stream);
+
+/* Causal attention over a 4-bit cache.  Sequence i's query tokens are rows
+ * row_start[i] .. row_start[i + 1] - 1 of q, and the last of them is the
+ * sequence's position kv_len[i] - 1 (the entries of the tokens are in the cache
+ * already: append first).  Query head h reads KV head h / (n_q_heads /
+ * n_kv_heads).  A token's output is
+ *   sum_p softmax_p(scale * q . k_p) v_p   over positions 0 .. its own;
+ * a token without any position (kv_len[i] = 0, or more query tokens than
+ * positions) gets zeros.  Rows of q behind row_start[batch] are not written.
+ * Queries enter the products with 11 significant bits (of their head's largest
+ * element; a bf16 query whole), probabilities with 11, keys and values exactly;
+ * sums and statistics are fp32.
+ * Device-checked: 0 <= kv_len[i] <= max_pages * page_size and row_start
+ * ascending from >= 0 to <= n_tok with at most max_new rows each
+ * (BUDDY_DEV_BAD_POSITION: the sequence's rows are not written); page ids
+ * (BUDDY_DEV_BAD_PAGE: the page's positions count as not there). */
+typedef struct {
+  int32_t batch;              /* 1 .. 16384 */
+  int32_t n_tok;              /* rows of q and out */
+  int32_t max_new;            /* >= 1: most query tokens of one sequence */
+  int32_t n_q_heads;          /* a multiple of n_kv_heads, at most 8 times */
+  int32_t q_dtype;            /* BUDDY_DTYPE_F32 or _BF16 */
+  int32_t out_dtype;          /* BUDDY_DTYPE_F32 or _BF16 */
+  int32_t max_pages;          /* entries of a table row, max_pages * page_size < 2^31 */
+  float scale;                /* of the scores; 0: 1 / sqrt(head_dim) */
+  const void* q;              /* device [n_tok, n_q_heads, head_dim], tokens q_stride elements apart */
+  void* out;                  /* device, as q with out_stride; must not overlap q */
+  int64_t q_stride;           /* rows 16-byte aligned */
+  int64_t out_stride;
+  const int32_t* row_start;   /* device [batch + 1]; NULL: one token per sequence (n_tok == batch) */
+  const int32_t* kv_len;      /* device [batch], the query tokens' own positions among them */
+  const int32_t* table;       /* device [batch, max_pages] */
+  void* workspace;            /* device, 256-byte aligned */
+  int64_t workspace_bytes;    /* at least buddy_kv4_attention_workspace() */
+} buddy_kv4_attention_args;
+BUDDY_API int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* args,
+                                  int32_t* flags, void* stream);
+
+/* Bytes of workspace that any buddy_kv4_attention call with these sizes takes on
+ * the current device; -1 for sizes that it rejects.  The caller zeroes it once;
+ * every call leaves it ready for the next.  Calls that may overlap on the GPU
+ * need workspaces of their own. */
+BUDDY_API int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                int32_t max_new);
 
 BUDDY_API const char* buddy_error_string(int32_t code);
 BUDDY_API int32_t buddy_version(void);

@@ -13,17 +13,19 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbuddy.so")
 
 BUDDY_OK, BUDDY_ERR_ARG, BUDDY_ERR_RANGE, BUDDY_ERR_CUDA, BUDDY_ERR_DEVICE, BUDDY_ERR_STATE = range(6)
-BUDDY_DTYPE_F32, BUDDY_DTYPE_BF16 = 0, 1
+BUDDY_DTYPE_F32, BUDDY_DTYPE_BF16, BUDDY_DTYPE_F16 = 0, 1, 2
 BUDDY_FEATURE = {"v": 0, "k": 1, "kv": 2}
 BUDDY_SKIP = {"zero": 0, "masked": 1}
 BUDDY_DEV_BAD_BUDGET, BUDDY_DEV_BAD_POSITION, BUDDY_DEV_BAD_SEQ, BUDDY_DEV_TIMEOUT = 1, 2, 4, 8
+BUDDY_DEV_NO_PAGES, BUDDY_DEV_BAD_PAGE = 16, 32
 
 EXPORTED = ["buddy_create", "buddy_destroy", "buddy_set_weights", "buddy_kv_append", "buddy_route",
             "buddy_decode_step", "buddy_decode_step_host", "buddy_set_options",
             "buddy_device_status", "buddy_budget_to_k", "buddy_error_string", "buddy_version",
             "buddy_set_profiling", "buddy_profile_read", "buddy_profile_class_name",
             "buddy_route_noalloc", "buddy_set_budget_predictor", "buddy_get_paths", "buddy_prefill",
-            "buddy_set_wait_limit"]
+            "buddy_set_wait_limit", "buddy_page_plan", "buddy_rope_table", "buddy_qk_norm_rope",
+            "buddy_kv4_append", "buddy_kv4_read", "buddy_kv4_attention", "buddy_kv4_attention_workspace"]
 PROF_CLASSES = ["check", "rmsnorm", "gemm_qkv", "qkv_finalize", "attention", "gemm_o", "gemm_gate_up",
                 "gemm_down", "route", "compact", "other", "gemm_fixup",
                 "pf_gemm", "pf_attention", "pf_other"]
@@ -57,6 +59,32 @@ class buddy_predictor_weights(ctypes.Structure):
 class buddy_kv_state(ctypes.Structure):
     _fields_ = [("k_cache", ctypes.POINTER(c_p)), ("v_cache", ctypes.POINTER(c_p)), ("seq_off", c_p),
                 ("cap", c_p), ("len", c_p), ("pool_sum", c_p), ("batch", c_i32), ("layer_len", c_p)]
+
+
+class buddy_kv4_cache(ctypes.Structure):
+    _fields_ = [("k_pages", c_p), ("v_pages", c_p), ("n_pages", c_i32), ("page_size", c_i32),
+                ("n_kv_heads", c_i32), ("head_dim", c_i32)]
+
+
+class buddy_page_plan_args(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("page_size", c_i32), ("max_pages", c_i32), ("n_free", c_i32), ("n_tok", c_i32),
+                ("len", c_p), ("n_new", c_p), ("table", c_p), ("free_pages", c_p), ("free_head", c_p),
+                ("kv_len", c_p), ("row_start", c_p), ("slot", c_p), ("pos", c_p), ("free_head_out", c_p)]
+
+
+class buddy_qk_rows(ctypes.Structure):
+    _fields_ = [("n_tok", c_i32), ("n_q_heads", c_i32), ("n_kv_heads", c_i32), ("head_dim", c_i32),
+                ("dtype", c_i32), ("max_pos", c_i32), ("eps", ctypes.c_float), ("q", c_p), ("k", c_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_gain", c_p), ("k_gain", c_p),
+                ("pos", c_p), ("rope_cos", c_p), ("rope_sin", c_p), ("q_out", c_p), ("k_out", c_p),
+                ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
+
+
+class buddy_kv4_attention_args(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("n_tok", c_i32), ("max_new", c_i32), ("n_q_heads", c_i32), ("q_dtype", c_i32),
+                ("out_dtype", c_i32), ("max_pages", c_i32), ("scale", ctypes.c_float), ("q", c_p), ("out", c_p),
+                ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("row_start", c_p), ("kv_len", c_p),
+                ("table", c_p), ("workspace", c_p), ("workspace_bytes", ctypes.c_int64)]
 
 
 class BuddyError(RuntimeError):
@@ -111,6 +139,18 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.buddy_prefill.restype = ctypes.c_int
     lib.buddy_set_wait_limit.argtypes = [c_p, ctypes.c_int64]
     lib.buddy_set_wait_limit.restype = ctypes.c_int
+    P = ctypes.POINTER
+    lib.buddy_page_plan.argtypes = [P(buddy_page_plan_args), c_p, c_p]
+    lib.buddy_rope_table.argtypes = [c_p, c_p, c_i32, c_i32, ctypes.c_float, c_p]
+    lib.buddy_qk_norm_rope.argtypes = [P(buddy_qk_rows), c_p, c_p]
+    lib.buddy_kv4_append.argtypes = [P(buddy_kv4_cache), P(buddy_qk_rows), c_p, ctypes.c_int64, c_p, c_p, c_p]
+    lib.buddy_kv4_read.argtypes = [P(buddy_kv4_cache), c_i32, c_p, c_i32, c_p, c_p, c_p, c_p]
+    lib.buddy_kv4_attention.argtypes = [P(buddy_kv4_cache), P(buddy_kv4_attention_args), c_p, c_p]
+    lib.buddy_kv4_attention_workspace.argtypes = [c_i32, c_i32, c_i32, c_i32]
+    for name in ("buddy_page_plan", "buddy_rope_table", "buddy_qk_norm_rope", "buddy_kv4_append", "buddy_kv4_read",
+                 "buddy_kv4_attention"):
+        getattr(lib, name).restype = ctypes.c_int
+    lib.buddy_kv4_attention_workspace.restype = ctypes.c_int64
     for name in ("buddy_create", "buddy_set_weights", "buddy_kv_append", "buddy_route", "buddy_decode_step",
                  "buddy_decode_step_host", "buddy_set_options", "buddy_device_status", "buddy_set_profiling",
                  "buddy_profile_read"):
@@ -334,3 +374,165 @@ class Context:
         if rc not in (BUDDY_OK, BUDDY_ERR_DEVICE):
             _check(rc, "buddy_device_status")
         return int(flags.value)
+
+
+# ---------------------------------------------------------------------------
+# Paged 4-bit KV cache (see include/buddy.h).  The library sees addresses only:
+# what a tensor can say about itself (type, device, shape, strides) is checked here.
+# ---------------------------------------------------------------------------
+_DTYPES = {torch.float32: BUDDY_DTYPE_F32, torch.bfloat16: BUDDY_DTYPE_BF16, torch.float16: BUDDY_DTYPE_F16}
+
+
+def _at(t: Optional[torch.Tensor], dtype, n: int, what: str) -> Optional[int]:
+    """Address of a contiguous CUDA tensor of `n` elements or more."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {n} or more {dtype} is wanted")
+    return t.data_ptr()
+
+
+def _heads(t: torch.Tensor, tokens: int, dim: int, what: str) -> int:
+    """Elements from token to token of a [tokens, heads, dim] view with whole heads."""
+    if not t.is_cuda or t.dim() != 3:
+        raise ValueError(f"{what}: a CUDA tensor [tokens, heads, head_dim] is wanted")
+    n, h, d = t.shape
+    s = t.stride()
+    if n != tokens or d != dim or s[2] != 1 or (h > 1 and s[1] != d):
+        raise ValueError(f"{what}: [{tokens}, heads, {dim}] with whole heads one after the other is wanted")
+    return s[0]
+
+
+def buddy_rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None):
+    """(cos, sin) rotary tables, [max_pos, head_dim / 2] fp32 each."""
+    co, si = (torch.empty(max_pos, head_dim // 2, dtype=torch.float32, device=device) for _ in range(2))
+    _check(load_library().buddy_rope_table(_ptr(co), _ptr(si), max_pos, head_dim, theta, _stream(stream)),
+           "buddy_rope_table")
+    return co, si
+
+
+def buddy_page_plan(length: torch.Tensor, n_new: torch.Tensor, page_size: int, table: torch.Tensor,
+                    free_pages: torch.Tensor, free_head: torch.Tensor, kv_len: torch.Tensor, row_start: torch.Tensor,
+                    slot: torch.Tensor, pos: torch.Tensor, free_head_out: torch.Tensor,
+                    flags: Optional[torch.Tensor] = None, stream=None):
+    """Block tables, slots and positions of a call's new tokens from the lengths."""
+    B, i32 = length.numel(), torch.int32
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("table: [batch, max_pages] is wanted")
+    T = slot.numel()
+    a = buddy_page_plan_args(B, page_size, table.shape[1], free_pages.numel(), T, _at(length, i32, B, "length"),
+                             _at(n_new, i32, B, "n_new"), _at(table, i32, 0, "table"),
+                             _at(free_pages, i32, 0, "free_pages"), _at(free_head, i32, 1, "free_head"),
+                             _at(kv_len, i32, B, "kv_len"), _at(row_start, i32, B + 1, "row_start"),
+                             _at(slot, torch.int64, T, "slot"), _at(pos, i32, T, "pos"),
+                             _at(free_head_out, i32, 1, "free_head_out"))
+    _check(load_library().buddy_page_plan(a, _at(flags, i32, 1, "flags"), _stream(stream)), "buddy_page_plan")
+
+
+def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps) -> buddy_qk_rows:
+    T, nkv, hd = k.shape
+    dt, f32 = k.dtype, torch.float32
+    nq = 0 if q is None else q.shape[1]
+    for t in (q, q_out, k_out):
+        if t is not None and t.dtype is not dt:
+            raise ValueError("queries, keys and outputs are of one type")
+    if nq and (q_out is None or q_out.shape[1] != nq) or k_out is not None and k_out.shape[1] != nkv:
+        raise ValueError("outputs have the heads of their inputs")
+    co, si = rope
+    rows = co.shape[0]
+    return buddy_qk_rows(T, nq, nkv, hd, _DTYPES.get(dt, -1), rows, eps, q.data_ptr() if nq else None, k.data_ptr(),
+                         _heads(q, T, hd, "q") if nq else 0, _heads(k, T, hd, "k"), _at(q_gain, f32, hd, "q_gain"),
+                         _at(k_gain, f32, hd, "k_gain"), _at(pos, torch.int32, T, "pos"),
+                         _at(co, f32, rows * hd // 2, "cos"), _at(si, f32, rows * hd // 2, "sin"),
+                         q_out.data_ptr() if nq else None, None if k_out is None else k_out.data_ptr(),
+                         _heads(q_out, T, hd, "q_out") if nq else 0,
+                         0 if k_out is None else _heads(k_out, T, hd, "k_out"))
+
+
+def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Tensor, rope, q_out, k_out,
+                       q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+                       eps: float = 1e-6, flags: Optional[torch.Tensor] = None, stream=None):
+    """Norm of each query and key head (with gains) and rotation, in one pass.
+    q, k, q_out, k_out: [tokens, heads, head_dim], fp32 or bf16; rope: (cos, sin)."""
+    r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps)
+    _check(load_library().buddy_qk_norm_rope(r, _at(flags, torch.int32, 1, "flags"), _stream(stream)),
+           "buddy_qk_norm_rope")
+
+
+class KV4Cache:
+    """One layer's paged 4-bit KV cache: pages of keys and of values, uint8
+    [n_pages, n_kv, page_size * (hd / 2 + hd / 16)], and the workspace of its
+    attention calls.  Layers whose calls do not overlap on the GPU may share one
+    workspace: pass it, a zeroed uint8 tensor of workspace_bytes()."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_size: int,
+                 workspace: Optional[torch.Tensor] = None):
+        if k_pages.dim() != 3 or k_pages.shape != v_pages.shape:
+            raise ValueError("pages: [n_pages, n_kv, bytes of a block] is wanted, alike for keys and values")
+        n_pages, n_kv, blk = k_pages.shape
+        self.head_dim = {36: 64, 72: 128}.get(blk // page_size, 0) if page_size > 0 and blk % page_size == 0 else 0
+        if not self.head_dim:
+            raise ValueError("a block holds page_size * (hd / 2 + hd / 16) bytes, hd 64 or 128")
+        self.k_pages, self.v_pages, self.page_size, self.n_kv = k_pages, v_pages, page_size, n_kv
+        self.state = buddy_kv4_cache(_at(k_pages, torch.uint8, 0, "k_pages"), _at(v_pages, torch.uint8, 0, "v_pages"),
+                                     n_pages, page_size, n_kv, self.head_dim)
+        self.lib = load_library()
+        self.workspace = workspace
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv: int, head_dim: int, device="cuda",
+              workspace: Optional[torch.Tensor] = None) -> "KV4Cache":
+        shape = (n_pages, n_kv, page_size * (head_dim // 2 + head_dim // 16))
+        return cls(*(torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2)), page_size, workspace)
+
+    def workspace_bytes(self, n_q_heads: int, max_new: int = 1) -> int:
+        n = self.lib.buddy_kv4_attention_workspace(n_q_heads, self.n_kv, self.head_dim, max_new)
+        if n < 0:
+            raise BuddyError(BUDDY_ERR_ARG, "buddy_kv4_attention_workspace")
+        return n
+
+    def buddy_kv4_append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+                         slot: torch.Tensor, rope, q_out: Optional[torch.Tensor],
+                         q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+                         eps: float = 1e-6, flags: Optional[torch.Tensor] = None,
+                         k_out: Optional[torch.Tensor] = None, stream=None):
+        """buddy_qk_norm_rope, with the keys and values v stored at `slot`."""
+        r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps)
+        T = k.shape[0]
+        if v.dtype is not k.dtype or v.shape != k.shape:
+            raise ValueError("v: type and shape of k are wanted")
+        _check(self.lib.buddy_kv4_append(self.state, r, _ptr(v), _heads(v, T, k.shape[2], "v"),
+                                         _at(slot, torch.int64, T, "slot"), _at(flags, torch.int32, 1, "flags"),
+                                         _stream(stream)), "buddy_kv4_append")
+
+    def buddy_kv4_read(self, slot: torch.Tensor, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor],
+                       flags: Optional[torch.Tensor] = None, stream=None):
+        """The values stored at `slot`: [n, n_kv, head_dim] of fp32, fp16 or bf16."""
+        n = slot.numel()
+        out = k_out if k_out is not None else v_out
+        if out is None or out.dtype not in _DTYPES:
+            raise ValueError("k_out, v_out: fp32, fp16 or bf16 is wanted")
+        size = n * self.n_kv * self.head_dim
+        _check(self.lib.buddy_kv4_read(self.state, n, _at(slot, torch.int64, n, "slot"), _DTYPES[out.dtype],
+                                       _at(k_out, out.dtype, size, "k_out"), _at(v_out, out.dtype, size, "v_out"),
+                                       _at(flags, torch.int32, 1, "flags"), _stream(stream)), "buddy_kv4_read")
+
+    def buddy_kv4_attention(self, q: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, out: torch.Tensor,
+                            row_start: Optional[torch.Tensor] = None, max_new: int = 1, scale: float = 0.0,
+                            flags: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                            stream=None):
+        """Causal attention of query tokens over the cache; q, out [tokens, n_q, head_dim]."""
+        T, nq, hd = q.shape
+        B, i32 = kv_len.numel(), torch.int32
+        if hd != self.head_dim or out.shape != q.shape or table.dim() != 2 or table.shape[0] != B:
+            raise ValueError("q, out: [tokens, heads, head_dim of the cache], table: [batch, max_pages] are wanted")
+        ws = workspace if workspace is not None else self.workspace
+        if ws is None:
+            ws = self.workspace = torch.zeros(self.workspace_bytes(nq, max_new), dtype=torch.uint8, device=q.device)
+        a = buddy_kv4_attention_args(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1),
+                                     table.shape[1], scale, q.data_ptr(), out.data_ptr(), _heads(q, T, hd, "q"),
+                                     _heads(out, T, hd, "out"), _at(row_start, i32, B + 1, "row_start"),
+                                     _at(kv_len, i32, B, "kv_len"), _at(table, i32, 0, "table"), ws.data_ptr(),
+                                     ws.numel())
+        _check(self.lib.buddy_kv4_attention(self.state, a, _at(flags, i32, 1, "flags"), _stream(stream)),
+               "buddy_kv4_attention")
