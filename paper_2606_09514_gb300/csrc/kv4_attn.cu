@@ -1,109 +1,616 @@
-// Causal attention over the paged 4-bit cache.
+// Causal attention over the paged 4-bit cache: few query rows per KV head (single
+// tokens, proposed tokens checked at once).
 //
-// One CTA per (sequence, place of the query token in it, KV head): its warps take the positions in turn, a lane
-// holding four channels of the group's query heads; running maximum and sum per
-// head, joined over the warps at the end.
+// The rows of a (sequence, KV head) are (query token, head of the group) pairs, row
+// r = token r / G, head r % G; up to 8 NB of them share a walk over the keys and
+// values (a stream; more rows make more streams).  With so few rows the work is
+// reading the cache and turning codes into numbers, which the tensor cores' mma.sync
+// takes from registers: nothing goes back to shared memory.
+//
+//   S^T = K Q^T   m16n8k16, half: 16 positions x 8 rows.  The order of the channels
+//                 in the contraction is free, so a lane takes HD / 4 consecutive
+//                 ones: one wide load of codes is its A operand of all K steps.
+//   softmax       base 2, per row (a column here): running reference m, which follows
+//                 the maximum when that rises by more than 8 (p < 2^8 in half).
+//   O^T += V^T P^T  16 channels x 8 rows; a lane takes HD / 8 consecutive channels of
+//                 four positions, whose code words are put side by side by halves; P^T
+//                 is S^T's accumulator transposed in registers (movmatrix).
+//
+// Codes become halves in one logical and one fused multiply-add instruction per pair
+// (kv4.cuh), exactly.  Queries are scaled by a power of two per row to 1 .. 2 and
+// rounded to half (11 bits; bf16 queries lose nothing), the power goes into the
+// softmax's factor.  Probabilities are rounded to half for the product only (their
+// sum is taken before): 2^-12 of the largest value at most.
+//
+// Work: chunks of 32 positions of all streams, end to end, in equal shares per CTA;
+// in a share, four warps take the chunks of a stream in turn, each with its own ring of
+// cp.async buffers that runs on across streams; rows past the sequence's end and
+// pages that are not there are filled with zeros and masked.  A stream within a share
+// is written out; the CTAs of one that is cut write partials, and the last of them
+// (an arrival counter) joins them in order.
 #include <cuda_runtime.h>
 
+#include <algorithm>
+
+#include "attn_tc.cuh"
 #include "common.cuh"
 #include "internal.h"
 #include "kv4.cuh"
+#include "ptx.cuh"
 
 namespace buddy {
 
 bool kv4_cache_ok(const buddy_kv4_cache* c);
 kv4::Pages kv4_pages(const buddy_kv4_cache* c);
 
-constexpr int kSimpleWarps = 4;
+namespace kv4 {
+
+constexpr int kChunk = 32;
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStages = 3;
+constexpr int kCtasPerSm = 3;
+constexpr int kMaxGrid = 1024;   // CTAs: three on each of at most 341 SMs
 
 template <int HD>
-__global__ void __launch_bounds__(32 * kSimpleWarps) kv4_attn_simple_kernel(const buddy_kv4_attention_args A,
-                                                                            const kv4::Pages P, int32_t* flags) {
-  constexpr int C = HD / 32;
-  const int i = blockIdx.x / A.max_new, j = blockIdx.x % A.max_new;
-  const int g = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int G = A.n_q_heads / P.nkv;
-  const int t0 = A.row_start ? A.row_start[i] : i, t1 = A.row_start ? A.row_start[i + 1] : i + 1;
-  const int n = A.kv_len[i], m = t1 - t0;
-  if (t0 < 0 || t1 < t0 || t1 > A.n_tok || m > A.max_new || n < 0 || n > (int64_t)A.max_pages << P.shift) {
-    if (flags && threadIdx.x == 0) atomicOr(flags, BUDDY_DEV_BAD_POSITION);
-    return;
+__host__ __device__ constexpr int stage_bytes() { return 2 * kChunk * entry_bytes(HD); }
+template <int HD, int NB>
+__host__ __device__ constexpr int smem_bytes() {
+  return kWarps * kStages * stage_bytes<HD>() + kWarps * 8 * NB * (HD + 4 + 2) * 4;
+}
+// Arrival counters, then two partials per CTA: m and l of 8 NB rows, then their outputs.
+template <int HD, int NB>
+__host__ __device__ constexpr int64_t partial_floats() { return 8 * NB * (HD + 2); }
+
+struct AttnArgs4 {
+  buddy_kv4_attention_args a;
+  Pages p;
+  int G, row_limit;           // sequences of at most this many rows are this kernel's
+  int32_t* flags;
+  int32_t* arrive;            // [grid], zero between calls
+  float* part;                // [grid][2]
+};
+
+// What a sequence asks for: query rows t0 .. t0 + m - 1, n positions.
+struct Seq {
+  int t0, m, n, nc, subs;     // nc chunks, subs streams (0: not this kernel's)
+};
+
+template <int NB>
+__device__ __forceinline__ Seq seq_of(const AttnArgs4& A, int i, bool* bad) {
+  Seq s;
+  s.t0 = A.a.row_start ? A.a.row_start[i] : i;
+  const int t1 = A.a.row_start ? A.a.row_start[i + 1] : i + 1;
+  s.n = A.a.kv_len[i];
+  *bad = s.t0 < 0 || t1 < s.t0 || t1 > A.a.n_tok || t1 - s.t0 > A.a.max_new || s.n < 0 ||
+         s.n > (int64_t)A.a.max_pages << A.p.shift;
+  s.m = *bad ? 0 : t1 - s.t0;
+  const int rows = s.m * A.G;
+  s.nc = max(1, (s.n + kChunk - 1) / kChunk);   // (a sequence without positions: one chunk of nothing)
+  s.subs = rows > A.row_limit ? 0 : A.p.nkv * ((rows + 8 * NB - 1) / (8 * NB));
+  return s;
+}
+
+// A walk over the streams of a CTA's share.
+template <int NB>
+struct Walk {
+  Seq q;
+  int i, sub, c, c1;          // sequence, stream of it, chunks [c, c1) of the stream in this share
+  int64_t rem;                // chunks of the share behind this stream
+  // to the next stream; false at the share's end
+  __device__ __forceinline__ bool next(const AttnArgs4& A) {
+    if (rem <= 0) return false;
+    if (++sub >= q.subs) {
+      sub = 0;
+      bool bad;
+      do {
+        q = seq_of<NB>(A, ++i, &bad);   // rem > 0: there is another sequence with streams
+      } while (q.subs == 0);
+    }
+    c = 0;
+    c1 = (int)min((int64_t)q.nc, rem);
+    rem -= c1;
+    return true;
   }
-  if (j >= m) return;
-  const int t = t0 + j;
-  const int seen = min(n, n - m + j + 1);
-  const float scale = A.scale != 0.f ? A.scale : rsqrtf((float)HD);
-  float q[8][C], acc[8][C], mx[8], sum[8];
+};
+
+__device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+__device__ __forceinline__ __half2 as_h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+
+// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.
+__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72) {
+  return h2(__hfma2(as_h2((w & 0x00F000F0u) | 0x54005400u), s, s72));
+}
+// The four pairs (codes j of both halves) of a word.
+__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t* o) {
+  o[0] = dequant(w << 4, s, s72);
+  o[1] = dequant(w, s, s72);
+  o[2] = dequant(w >> 4, s, s72);
+  o[3] = dequant(w >> 8, s, s72);
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes) {   // the rest of 16: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Position (of 16) of row r of S^T: odd and even neighbours, so that neither the key nor the
+// value loads meet in a bank more than they have to.
+__device__ __forceinline__ int place(int r) { return r ^ ((r >> 1) & 1); }
+
+// A warp's copies of one chunk into a stage: K codes, V codes, K scales, V scales.
+// Returns one bit per page of the chunk that is there.
+template <int HD>
+__device__ __forceinline__ uint32_t load_chunk(const Pages& P, uint32_t dst, int64_t page0, int64_t page1, int g, int p0,
+                                               int n, int lane) {
+  constexpr int PPR = code_bytes(HD) / 16;          // 16-byte pieces of a position's codes
+  constexpr int RPS = 16 / scale_bytes(HD);         // positions of a piece of scales
+  const int in_page = (1 << P.shift) - 1;
+  const uint32_t ok = (page0 >= 0 ? 1u : 0u) | (page1 >= 0 ? 2u : 0u);
+  const int64_t b0 = block_at<HD>(P, max(page0, (int64_t)0), g), b1 = block_at<HD>(P, max(page1, (int64_t)0), g);
 #pragma unroll
-  for (int h = 0; h < 8; ++h) {
-    mx[h] = -INFINITY, sum[h] = 0.f;
-    for (int c = 0; c < C; ++c) {
-      acc[h][c] = 0.f;
-      const int64_t at = t * A.q_stride + (int64_t)(g * G + min(h, G - 1)) * HD + lane * C + c;
-      q[h][c] = (A.q_dtype == BUDDY_DTYPE_F32 ? ((const float*)A.q)[at] : to_f(((const bf16*)A.q)[at])) * scale;
-    }
+  for (int x = 0; x < kChunk * PPR / 32; ++x) {
+    const int r = x * (32 / PPR) + lane / PPR;
+    const bool up = r >= 16;
+    const int64_t at = (up ? b1 : b0) + ((p0 + r) & in_page) * code_bytes(HD) + (lane % PPR) * 16;
+    const int real = p0 + r < n && ((ok >> (up ? 1 : 0)) & 1) ? 16 : 0;
+    const uint32_t d = dst + r * code_bytes(HD) + (lane % PPR) * 16;
+    cp_async(d, P.k + (real ? at : 0), real);
+    cp_async(d + kChunk * code_bytes(HD), P.v + (real ? at : 0), real);
   }
-  for (int p = warp; p < seen; p += kSimpleWarps) {
-    const int page = A.table[(int64_t)i * A.max_pages + (p >> P.shift)];
-    if (page < 0 || page >= P.n_pages) {
-      if (flags && lane == 0) atomicOr(flags, BUDDY_DEV_BAD_PAGE);
-      continue;
-    }
-    const int row = p & ((1 << P.shift) - 1);
-    float kv[2][C];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint8_t* b = (x ? P.v : P.k) + kv4::block_at<HD>(P, page, g);
-      const int ch = lane * C;
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(b + row * kv4::code_bytes(HD) + (ch / 8) * 4);
-      const float s = __half2float(*reinterpret_cast<const __half*>(b + ((int64_t)kv4::code_bytes(HD) << P.shift) +
-                                                                    row * kv4::scale_bytes(HD) + ch / 32 * 2));
-      for (int c = 0; c < C; ++c) kv[x][c] = kv4::decode(w, (ch + c) & 7, s);
-    }
-#pragma unroll
-    for (int h = 0; h < 8; ++h) {
-      float d = 0.f;
-      for (int c = 0; c < C; ++c) d += q[h][c] * kv[0][c];
-      d = warp_sum(d);
-      const float m1 = fmaxf(mx[h], d);
-      const float a = expf(mx[h] - m1), e = expf(d - m1);
-      mx[h] = m1;
-      sum[h] = sum[h] * a + e;
-      for (int c = 0; c < C; ++c) acc[h][c] = acc[h][c] * a + e * kv[1][c];
-    }
+  constexpr int PIECES = kChunk / RPS;              // pieces of scales: 16 or 8, keys on the lower half-warp
+  const int x = lane & 15;
+  if (x < PIECES) {
+    const int r = x * RPS;
+    const bool up = r >= 16;
+    const int real = ((ok >> (up ? 1 : 0)) & 1) ? min(max(n - p0 - r, 0), RPS) * scale_bytes(HD) : 0;
+    const int64_t at = (up ? b1 : b0) + ((int64_t)code_bytes(HD) << P.shift) + ((p0 + r) & in_page) * scale_bytes(HD);
+    const uint8_t* src = lane < 16 ? P.k : P.v;
+    cp_async(dst + 2 * kChunk * code_bytes(HD) + (lane < 16 ? 0 : kChunk * scale_bytes(HD)) + x * 16,
+             src + (real ? at : 0), real);
   }
-  __shared__ float s_m[kSimpleWarps][8], s_l[kSimpleWarps][8], s_o[kSimpleWarps][8][HD];
+  return ok;
+}
+
+template <int HD, int NB>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const AttnArgs4 A) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  constexpr int ROWS = 8 * NB, KS = HD / 16, LDO = HD + 4;
+  float* sO = reinterpret_cast<float*>(smem + kWarps * kStages * stage_bytes<HD>());   // [warp][row][LDO]
+  float* sM = sO + kWarps * ROWS * LDO;                                                // [warp][row]
+  float* sL = sM + kWarps * ROWS;
+  __shared__ int64_t s_sum[kWarps], s_at;
+  __shared__ int s_first, s_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
+  const int B = A.a.batch, G = A.G;
+
+  // ---- this CTA's share: chunks [lo, lo + share) of all
+  const int per = (B + kThreads - 1) / kThreads;
+  const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
+  int64_t mine = 0;
+  bool any_bad = false;
+  for (int i = b0; i < b1; ++i) {
+    bool bad;
+    const Seq q = seq_of<NB>(A, i, &bad);
+    any_bad |= bad;
+    mine += (int64_t)q.nc * q.subs;
+  }
+  if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+  int64_t upto = mine;
 #pragma unroll
-  for (int h = 0; h < 8; ++h) {
-    if (lane == 0) s_m[warp][h] = mx[h], s_l[warp][h] = sum[h];
-    for (int c = 0; c < C; ++c) s_o[warp][h][lane * C + c] = acc[h][c];
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) s_sum[warp] = upto;
+  __syncthreads();
+  int64_t total = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w == warp) upto += total;
+    total += s_sum[w];
+  }
+  const int64_t share = max((int64_t)kWarps, (total + gridDim.x - 1) / gridDim.x + kWarps - 1) / kWarps * kWarps;
+  const int64_t lo = blockIdx.x * share;
+  if (lo >= total) return;
+  if (upto - mine <= lo && lo < upto) {
+    int64_t at = upto - mine;
+    for (int i = b0; i < b1; ++i) {
+      bool bad;
+      const Seq q = seq_of<NB>(A, i, &bad);
+      const int64_t n = (int64_t)q.nc * q.subs;
+      if (lo < at + n) {
+        s_first = i;
+        s_at = lo - at;
+        break;
+      }
+      at += n;
+    }
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < G * HD; x += blockDim.x) {
-    const int h = x / HD, c = x % HD;
-    float M = -INFINITY, L = 0.f, O = 0.f;
-    for (int w = 0; w < kSimpleWarps; ++w) M = fmaxf(M, s_m[w][h]);
-    for (int w = 0; w < kSimpleWarps; ++w) {
-      const float a = s_l[w][h] != 0.f ? expf(s_m[w][h] - M) : 0.f;
-      if (a != 0.f) L += a * s_l[w][h], O += a * s_o[w][h][c];
-    }
-    const float o = L != 0.f ? O / L : 0.f;
-    const int64_t at = t * A.out_stride + (int64_t)(g * G + h) * HD + c;
-    if (A.out_dtype == BUDDY_DTYPE_F32) ((float*)A.out)[at] = o;
-    else ((bf16*)A.out)[at] = from_f<bf16>(o);
+  Walk<NB> use;
+  {
+    bool bad;
+    use.i = s_first;
+    use.q = seq_of<NB>(A, use.i, &bad);
+    use.sub = (int)(s_at / use.q.nc);
+    use.c = (int)(s_at - (int64_t)use.sub * use.q.nc);
+    const int64_t all = min(share, total - lo);
+    use.c1 = (int)min((int64_t)use.q.nc, use.c + all);
+    use.rem = all - (use.c1 - use.c);
   }
+  int64_t start = lo - use.c;       // where the stream's first chunk is
+  Walk<NB> ld = use;
+  bool more = true;
+  ld.c += warp;
+  const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * stage_bytes<HD>();
+
+  // The load walk stands on the chunk to copy next; its page ids are read a chunk early.
+  int64_t id0 = -1, id1 = -1;
+  auto fetch_ids = [&]() {
+    while (more && ld.c >= ld.c1) {
+      more = ld.next(A);
+      ld.c += warp;
+    }
+    if (!more) return;
+    const int p0 = ld.c * kChunk;
+    const int32_t* row = A.a.table + (int64_t)ld.i * A.a.max_pages;
+    const int top = max(ld.q.n - 1, 0) >> A.p.shift;   // the last page with positions
+    id0 = ld.q.n > 0 ? row[min(p0 >> A.p.shift, top)] : -1;
+    id1 = A.p.shift == 4 && ld.q.n > 0 ? row[min((p0 + 16) >> A.p.shift, top)] : id0;
+  };
+  uint32_t there = 0;               // two bits per chunk in flight, the oldest lowest
+  int flying = 0, put = 0, take = 0;
+  auto issue = [&]() {
+    uint32_t ok = 0;
+    if (more) {
+      const int p0 = ld.c * kChunk;
+      const bool in0 = id0 >= 0 && id0 < A.p.n_pages, in1 = id1 >= 0 && id1 < A.p.n_pages;
+      if (lane == 0 && A.flags && ld.q.n > 0 && ((!in0 && p0 < ld.q.n) || (!in1 && p0 + 16 < ld.q.n)))
+        atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+      const int subs_g = ld.q.subs / A.p.nkv;
+      ok = load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), in0 ? id0 : -1, in1 ? id1 : -1, ld.sub / subs_g, p0,
+                          ld.q.n, lane);
+      ld.c += kWarps;
+      fetch_ids();
+    }
+    cp_commit();
+    there |= ok << (2 * flying);
+    ++flying;
+    put = put + 1 == kStages ? 0 : put + 1;
+  };
+  fetch_ids();
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) issue();
+
+  for (bool go = true; go;) {
+    // ---- one stream (or the part of it in this share)
+    const int subs_g = use.q.subs / A.p.nkv, g = use.sub / subs_g, r0 = (use.sub - g * subs_g) * ROWS;
+    const int rows = min(use.q.m * G - r0, ROWS), n = use.q.n;
+    const bool whole = use.c == 0 && use.c1 == use.q.nc;
+    // queries: rows lg of each block of eight, this lane's HD / 4 channels
+    uint32_t qf[NB][KS][2];
+    float fac[NB][2];               // of the scores of rows 2 lc and 2 lc + 1
+    int seen[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int r = min(8 * b + lg, rows - 1) + r0;
+      const int64_t at = (use.q.t0 + r / G) * A.a.q_stride + (int64_t)(g * G + r % G) * HD + lc * (HD / 4);
+      float x[HD / 4], top = 0.f;
+#pragma unroll
+      for (int e = 0; e < HD / 4; e += 8) {
+        if (A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + at + e, x + e);
+        else load8((const bf16*)A.a.q + at + e, x + e);
+      }
+#pragma unroll
+      for (int e = 0; e < HD / 4; ++e) top = fmaxf(top, fabsf(x[e]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+      const float down = __uint_as_float((uint32_t)(127 - ex) << 23), up = __uint_as_float((uint32_t)(127 + ex) << 23);
+#pragma unroll
+      for (int e = 0; e < HD / 4; e += 2)
+        qf[b][e / 4][(e / 2) & 1] = h2(__floats2half2_rn(x[e] * down, x[e + 1] * down));
+      // (above zero, so that it takes -inf to -inf)
+      const float f = fmaxf((A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f * up, 1.2e-38f);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        fac[b][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
+        const int rr = 8 * b + 2 * lc + e;
+        seen[b][e] = rr < rows ? n - use.q.m + (r0 + rr) / G + 1 : 0;
+      }
+    }
+    const int all_seen = n - use.q.m + r0 / G + 1;   // positions that every row sees
+    float o[NB][HD / 16][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      m[b][0] = m[b][1] = -INFINITY;
+      l[b][0] = l[b][1] = 0.f;
+#pragma unroll
+      for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[b][t][e] = 0.f;
+    }
+
+    for (int c = use.c + warp; c < use.c1; c += kWarps) {
+      cp_wait<kStages - 2>();
+      __syncwarp();
+      const uint8_t* st = smem + (warp * kStages + take) * stage_bytes<HD>();
+      const uint8_t *kc = st, *vc = st + kChunk * code_bytes(HD), *ks = st + 2 * kChunk * code_bytes(HD);
+      const uint8_t* vs = ks + kChunk * scale_bytes(HD);
+      const uint32_t ok = there & 3u;
+      there >>= 2;
+      --flying;
+      take = take + 1 == kStages ? 0 : take + 1;
+      const int p0 = c * kChunk;
+
+      // ---- S^T
+      float s[NB][2][4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint32_t a[2][HD / 8];                       // halves of the two positions' channels
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int r = 16 * t + place(lg) + 8 * u;
+          const __half sc = *reinterpret_cast<const __half*>(ks + r * scale_bytes(HD) + (lc * (HD / 4) / 32) * 2);
+          const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(kc + r * code_bytes(HD) + lc * (HD / 8));
+          if constexpr (HD == 128) {
+            const uint4 v = *reinterpret_cast<const uint4*>(w);
+            dequant4(v.x, s2, s72, a[u]);
+            dequant4(v.y, s2, s72, a[u] + 4);
+            dequant4(v.z, s2, s72, a[u] + 8);
+            dequant4(v.w, s2, s72, a[u] + 12);
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(w);
+            dequant4(v.x, s2, s72, a[u]);
+            dequant4(v.y, s2, s72, a[u] + 4);
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          s[b][t][0] = s[b][t][1] = s[b][t][2] = s[b][t][3] = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const uint32_t f[4] = {a[0][2 * k], a[1][2 * k], a[0][2 * k + 1], a[1][2 * k + 1]};
+            mma_f16(s[b][t], f, qf[b][k][0], qf[b][k][1]);
+          }
+        }
+      }
+      // ---- mask and softmax
+      uint32_t pt[NB][2][2];
+      const bool cut = p0 + kChunk > all_seen || ok != 3u;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if (cut || rows < ROWS) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int p = p0 + 16 * t + place(lg) + 8 * (e >> 1);
+              if (p >= seen[b][e & 1] || !((ok >> t) & 1)) s[b][t][e] = -INFINITY;
+            }
+        }
+        float mx[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          mx[e] = fmaxf(fmaxf(s[b][0][e], s[b][0][e + 2]), fmaxf(s[b][1][e], s[b][1][e + 2]));
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
+          mx[e] *= fac[b][e];
+        }
+        if (__any_sync(0xffffffffu, mx[0] > m[b][0] + 8.f || mx[1] > m[b][1] + 8.f)) {
+          float al[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float to = fmaxf(m[b][e], mx[e]);
+            al[e] = to == -INFINITY ? 1.f : tca::exp2a(m[b][e] - to);
+            m[b][e] = to;
+            l[b][e] *= al[e];
+          }
+#pragma unroll
+          for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[b][t][e] *= al[e & 1];
+        }
+        const float ref[2] = {m[b][0] == -INFINITY ? 0.f : m[b][0], m[b][1] == -INFINITY ? 0.f : m[b][1]};
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = tca::exp2a(fmaf(s[b][t][e], fac[b][e & 1], -ref[e & 1]));
+            l[b][e & 1] += p[e];
+          }
+          pt[b][t][0] = tca::movt(h2(__floats2half2_rn(p[0], p[1])));
+          pt[b][t][1] = tca::movt(h2(__floats2half2_rn(p[2], p[3])));
+        }
+      }
+      // ---- O^T: this lane's four positions of each 16, channels lg * HD / 8 on
+      int nan_at = INT32_MAX;                         // first position whose values here are NaN
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint32_t w[4][HD / 64];
+        __half sc[4];
+        int pos[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          pos[u] = 16 * t + place(2 * lc + (u & 1)) + 8 * (u >> 1);
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(vc + pos[u] * code_bytes(HD) + lg * (HD / 16));
+          if constexpr (HD == 128) {
+            const uint2 v = *reinterpret_cast<const uint2*>(src);
+            w[u][0] = v.x;
+            w[u][HD / 64 - 1] = v.y;
+          } else {
+            w[u][0] = *src;
+          }
+          sc[u] = *reinterpret_cast<const __half*>(vs + pos[u] * scale_bytes(HD) + (lg * (HD / 8) / 32) * 2);
+        }
+        // A NaN must not meet the zero probabilities of rows that do not see its position:
+        // its values count as zeros here, and the rows that do see it become NaN below.
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (__hisnan(sc[u])) {
+            sc[u] = __ushort_as_half(0);
+            nan_at = min(nan_at, p0 + pos[u]);
+          }
+        const __half2 sa = __halves2half2(sc[0], sc[1]), sb = __halves2half2(sc[2], sc[3]);
+        const __half2 k72 = __float2half2_rn(-72.f), sa72 = __hmul2(sa, k72), sb72 = __hmul2(sb, k72);
+#pragma unroll
+        for (int x = 0; x < HD / 64; ++x) {
+          uint32_t a[4][4];
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, a[0]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, a[1]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, a[2]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, a[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t f[4] = {a[0][j], a[1][j], a[2][j], a[3][j]};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mma_f16(o[b][4 * x + j], f, pt[b][t][0], pt[b][t][1]);
+          }
+        }
+      }
+      if (__any_sync(0xffffffffu, nan_at != INT32_MAX)) {
+        nan_at = min(nan_at, __shfl_xor_sync(0xffffffffu, nan_at, 1));
+        nan_at = min(nan_at, __shfl_xor_sync(0xffffffffu, nan_at, 2));
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (nan_at < seen[b][e & 1]) o[b][t][e] = __uint_as_float(0x7FC00000u);
+      }
+      __syncwarp();
+      issue();
+    }
+
+    // ---- join the warps: a lane has rows 2 lc, 2 lc + 1 of each block, HD / 8 channels from lg * HD / 8 on
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], x);
+        const int r = 8 * b + 2 * lc + e;
+        if (r < rows) {
+          if (lg == 0) sM[warp * ROWS + r] = m[b][e], sL[warp * ROWS + r] = l[b][e];
+          float4* d = reinterpret_cast<float4*>(sO + (warp * ROWS + r) * LDO + lg * (HD / 8));
+#pragma unroll
+          for (int t = 0; t < HD / 16; t += 2)
+            d[t / 2] = make_float4(o[b][t][e], o[b][t][e + 2], o[b][t + 1][e], o[b][t + 1][e + 2]);
+        }
+      }
+    __syncthreads();
+    const int64_t first_cta = whole ? 0 : start / share, last_cta = whole ? 0 : (start + use.q.nc - 1) / share;
+    float* part = A.part + (2 * (int64_t)blockIdx.x + ((int64_t)blockIdx.x == first_cta ? 1 : 0)) * partial_floats<HD, NB>();
+    auto out4 = [&](int r, int ch, float4 v) {
+      const int row = r0 + r;
+      const int64_t at = (use.q.t0 + row / G) * A.a.out_stride + (int64_t)(g * G + row % G) * HD + ch;
+      if (A.a.out_dtype == BUDDY_DTYPE_F32) {
+        *reinterpret_cast<float4*>((float*)A.a.out + at) = v;
+      } else {
+        *reinterpret_cast<uint2*>((bf16*)A.a.out + at) = make_uint2(tca::pack_bf16(v.x, v.y), tca::pack_bf16(v.z, v.w));
+      }
+    };
+    for (int x = tid; x < rows * (HD / 4); x += kThreads) {
+      const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
+      float M = -INFINITY, L = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sM[w * ROWS + r]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float mw = sM[w * ROWS + r], a = mw == -INFINITY ? 0.f : tca::exp2a(mw - M);
+        const float4 y = *reinterpret_cast<const float4*>(sO + (w * ROWS + r) * LDO + ch);
+        L += a * sL[w * ROWS + r];
+        v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
+      }
+      if (whole) {
+        const float inv = M == -INFINITY ? 0.f : 1.f / L;
+        out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+      } else {
+        if (ch == 0) part[r] = M, part[ROWS + r] = L;
+        *reinterpret_cast<float4*>(part + 2 * ROWS + r * HD + ch) = v;
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      __syncthreads();
+      const int spans = (int)(last_cta - first_cta) + 1;
+      if (tid == 0) {
+        s_last = ptx::atom_add_acq_rel(A.arrive + first_cta, 1) == spans - 1;
+        if (s_last) A.arrive[first_cta] = 0;
+      }
+      __syncthreads();
+      if (s_last) {
+        for (int x = tid; x < rows * (HD / 4); x += kThreads) {
+          const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
+          float M = -INFINITY, L = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int64_t k = first_cta; k <= last_cta; ++k) {
+            const float* p = A.part + (2 * k + (k == first_cta ? 1 : 0)) * partial_floats<HD, NB>();
+            const float mk = __ldcg(p + r), lk = __ldcg(p + ROWS + r);
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS + r * HD + ch));
+            const float to = fmaxf(M, mk);
+            const float a = M == -INFINITY ? 0.f : tca::exp2a(M - to), b = mk == -INFINITY ? 0.f : tca::exp2a(mk - to);
+            M = to;
+            L = L * a + lk * b;
+            v.x = v.x * a + y.x * b, v.y = v.y * a + y.y * b, v.z = v.z * a + y.z * b, v.w = v.w * a + y.w * b;
+          }
+          const float inv = M == -INFINITY ? 0.f : 1.f / L;
+          out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        }
+      }
+    }
+    __syncthreads();     // sM, sL, sO are free again
+    start += use.q.nc;
+    go = use.next(A);
+  }
+  cp_wait<0>();
+}
+
+}  // namespace kv4
+
+using namespace kv4;
+
+static int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  return n;
+}
+
+template <int HD, int NB>
+static int launch_decode(const AttnArgs4& A, int grid, cudaStream_t s) {
+  constexpr int smem = smem_bytes<HD, NB>();
+  if (cudaFuncSetAttribute(kv4_decode_kernel<HD, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    return BUDDY_ERR_CUDA;
+  kv4_decode_kernel<HD, NB><<<grid, kThreads, smem, s>>>(A);
+  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 
 }  // namespace buddy
 
 using namespace buddy;
 
+constexpr int64_t kWsCounters = 4096;   // bytes of arrival counters in front of a workspace
+
 extern "C" int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                                  int32_t max_new) {
   if (n_kv_heads < 1 || n_kv_heads > 1024 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads ||
       n_q_heads / n_kv_heads > 8 || (head_dim != 64 && head_dim != 128) || max_new < 1)
     return -1;
-  return 256;
+  return kWsCounters + (int64_t)kMaxGrid * 2 * 16 * (head_dim + 2) * 4;
 }
 
 extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags,
@@ -119,14 +626,21 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   if (!a->row_start && (a->n_tok != a->batch || a->max_new != 1)) return BUDDY_ERR_ARG;
   if (!a->workspace || a->workspace_bytes < need || (reinterpret_cast<uintptr_t>(a->workspace) & 255)) return BUDDY_ERR_ARG;
   if (a->n_tok == 0) return BUDDY_OK;
-  if ((int64_t)a->batch * a->max_new > INT32_MAX) return BUDDY_ERR_RANGE;
+  if ((int64_t)a->n_tok * a->n_q_heads > INT32_MAX) return BUDDY_ERR_RANGE;   // rows are counted in 32 bits
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) ||
       a->q_stride * (a->q_dtype == BUDDY_DTYPE_F32 ? 4 : 2) % 16 || a->out_stride * (a->out_dtype == BUDDY_DTYPE_F32 ? 4 : 2) % 16)
     return BUDDY_ERR_ARG;
-  dim3 grid((unsigned)((int64_t)a->batch * a->max_new), cache->n_kv_heads);
-  if (cache->head_dim == 128)
-    kv4_attn_simple_kernel<128><<<grid, 32 * kSimpleWarps, 0, (cudaStream_t)stream>>>(*a, kv4_pages(cache), flags);
-  else
-    kv4_attn_simple_kernel<64><<<grid, 32 * kSimpleWarps, 0, (cudaStream_t)stream>>>(*a, kv4_pages(cache), flags);
-  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  const int sms = sm_count();
+  if (sms == 0) return BUDDY_ERR_CUDA;
+  AttnArgs4 A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, INT32_MAX, flags, (int32_t*)a->workspace,
+              (float*)((uint8_t*)a->workspace + kWsCounters)};
+  // one CTA for every four chunks there can be, three on each SM at most
+  const bool two = (int64_t)a->max_new * A.G > 8;
+  const int64_t streams = cache->n_kv_heads * (((int64_t)a->max_new * A.G + (two ? 15 : 7)) / (two ? 16 : 8));
+  const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
+  const int64_t most = streams > (1 << 20) || chunks > (1 << 20) ? INT32_MAX : a->batch * streams * chunks / kWarps + 1;
+  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, kCtasPerSm * sms));
+  cudaStream_t s = (cudaStream_t)stream;
+  if (cache->head_dim == 128) return two ? launch_decode<128, 2>(A, grid, s) : launch_decode<128, 1>(A, grid, s);
+  return two ? launch_decode<64, 2>(A, grid, s) : launch_decode<64, 1>(A, grid, s);
 }
