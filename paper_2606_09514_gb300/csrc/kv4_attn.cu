@@ -23,7 +23,8 @@
 // sum is taken before): 2^-12 of the largest value at most.
 //
 // Work: chunks of 32 positions of all streams, end to end, in equal shares per CTA;
-// in a share, four warps take the chunks of a stream in turn, each with its own ring of
+// (a short stream belongs to the share where it begins: what a CTA saves by passing on
+// a part of it, the partials cost again); in a share, four warps take the chunks of a stream in turn, each with its own ring of
 // cp.async buffers that runs on across streams; rows past the sequence's end and
 // pages that are not there are filled with zeros and masked.  A stream within a share
 // is written out; the CTAs of one that is cut write partials, and the last of them
@@ -50,6 +51,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 3;
 constexpr int kCtasPerSm = 3;
+constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
 constexpr int kMaxGrid = 1024;   // CTAs: three on each of at most 341 SMs
 
 template <int HD>
@@ -97,6 +99,7 @@ struct Walk {
   Seq q;
   int i, sub, c, c1;          // sequence, stream of it, chunks [c, c1) of the stream in this share
   int64_t rem;                // chunks of the share behind this stream
+  __device__ __forceinline__ int g(const AttnArgs4& A) const { return q.subs == A.p.nkv ? sub : sub / (q.subs / A.p.nkv); }
   // to the next stream; false at the share's end
   __device__ __forceinline__ bool next(const AttnArgs4& A) {
     if (rem <= 0) return false;
@@ -108,7 +111,7 @@ struct Walk {
       } while (q.subs == 0);
     }
     c = 0;
-    c1 = (int)min((int64_t)q.nc, rem);
+    c1 = q.nc <= kWhole ? q.nc : (int)min((int64_t)q.nc, rem);
     rem -= c1;
     return true;
   }
@@ -147,38 +150,63 @@ __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0
 // value loads meet in a bank more than they have to.
 __device__ __forceinline__ int place(int r) { return r ^ ((r >> 1) & 1); }
 
-// A warp's copies of one chunk into a stage: K codes, V codes, K scales, V scales.
-// Returns one bit per page of the chunk that is there.
+// A warp's copies of one chunk into a stage: K codes, V codes, K scales, V scales.  A
+// position's codes are as many bytes in the stage as in the page, so a lane's pieces lie
+// 512 bytes apart on both sides.  page0, page1: pages of the lower and the upper 16
+// positions, negative where there is none.
 template <int HD>
-__device__ __forceinline__ uint32_t load_chunk(const Pages& P, uint32_t dst, int64_t page0, int64_t page1, int g, int p0,
-                                               int n, int lane) {
-  constexpr int PPR = code_bytes(HD) / 16;          // 16-byte pieces of a position's codes
-  constexpr int RPS = 16 / scale_bytes(HD);         // positions of a piece of scales
-  const int in_page = (1 << P.shift) - 1;
-  const uint32_t ok = (page0 >= 0 ? 1u : 0u) | (page1 >= 0 ? 2u : 0u);
-  const int64_t b0 = block_at<HD>(P, max(page0, (int64_t)0), g), b1 = block_at<HD>(P, max(page1, (int64_t)0), g);
-#pragma unroll
-  for (int x = 0; x < kChunk * PPR / 32; ++x) {
-    const int r = x * (32 / PPR) + lane / PPR;
-    const bool up = r >= 16;
-    const int64_t at = (up ? b1 : b0) + ((p0 + r) & in_page) * code_bytes(HD) + (lane % PPR) * 16;
-    const int real = p0 + r < n && ((ok >> (up ? 1 : 0)) & 1) ? 16 : 0;
-    const uint32_t d = dst + r * code_bytes(HD) + (lane % PPR) * 16;
-    cp_async(d, P.k + (real ? at : 0), real);
-    cp_async(d + kChunk * code_bytes(HD), P.v + (real ? at : 0), real);
-  }
-  constexpr int PIECES = kChunk / RPS;              // pieces of scales: 16 or 8, keys on the lower half-warp
+__device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, int page0, int page1, int g, int p0, int n,
+                                           int lane) {
+  constexpr int CB = code_bytes(HD), SB = scale_bytes(HD);
+  constexpr int HALF = 16 * CB / 512;               // copies of 16 positions' codes
+  constexpr int PIECES = kChunk * SB / 16;          // 16-byte pieces of scales: 16 or 8, keys on the lower half-warp
+  const int in_page = p0 & ((1 << P.shift) - 1);
   const int x = lane & 15;
-  if (x < PIECES) {
-    const int r = x * RPS;
-    const bool up = r >= 16;
-    const int real = ((ok >> (up ? 1 : 0)) & 1) ? min(max(n - p0 - r, 0), RPS) * scale_bytes(HD) : 0;
-    const int64_t at = (up ? b1 : b0) + ((int64_t)code_bytes(HD) << P.shift) + ((p0 + r) & in_page) * scale_bytes(HD);
-    const uint8_t* src = lane < 16 ? P.k : P.v;
-    cp_async(dst + 2 * kChunk * code_bytes(HD) + (lane < 16 ? 0 : kChunk * scale_bytes(HD)) + x * 16,
-             src + (real ? at : 0), real);
+  const uint32_t sdst = dst + 2 * kChunk * CB + (lane < 16 ? 0 : kChunk * SB) + x * 16;
+  const uint8_t* const sbase = lane < 16 ? P.k : P.v;
+  dst += lane * 16;
+  if (page0 >= 0 && page1 >= 0 && p0 + kChunk <= n) {
+    const int64_t b0 = block_at<HD>(P, page0, g);
+    int64_t at = b0 + in_page * CB + lane * 16;
+    int64_t sat = b0 + (CB << P.shift) + in_page * SB + x * 16;
+    const uint8_t *k = P.k + at, *v = P.v + at;
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) {
+      cp_async(dst + 512 * i, k + 512 * i, 16);
+      cp_async(dst + kChunk * CB + 512 * i, v + 512 * i, 16);
+    }
+    if (P.shift == 4) {
+      const int64_t b1 = block_at<HD>(P, page1, g);
+      at = b1 + lane * 16 - 512 * HALF;
+      k = P.k + at, v = P.v + at;
+      if (x >= PIECES / 2) sat = b1 + (CB << 4) + (x - PIECES / 2) * 16;
+    }
+#pragma unroll
+    for (int i = HALF; i < 2 * HALF; ++i) {
+      cp_async(dst + 512 * i, k + 512 * i, 16);
+      cp_async(dst + kChunk * CB + 512 * i, v + 512 * i, 16);
+    }
+    if (x < PIECES) cp_async(sdst, sbase + sat, 16);
+    return;
   }
-  return ok;
+  // at a sequence's end, and where a page is not there: zeros for what is not read
+  const int64_t b0 = block_at<HD>(P, max(page0, 0), g), b1 = block_at<HD>(P, max(page1, 0), g);
+  const int up = P.shift == 4 ? 0 : in_page + 16;   // where the upper 16 positions begin in their page
+#pragma unroll
+  for (int i = 0; i < 2 * HALF; ++i) {
+    const int r = i * (512 / CB) + lane / (CB / 16);
+    const int64_t at = i < HALF ? b0 + in_page * CB + lane * 16 + 512 * i : b1 + up * CB + lane * 16 + 512 * (i - HALF);
+    const int real = p0 + r < n && (i < HALF ? page0 : page1) >= 0 ? 16 : 0;
+    cp_async(dst + 512 * i, P.k + (real ? at : 0), real);
+    cp_async(dst + kChunk * CB + 512 * i, P.v + (real ? at : 0), real);
+  }
+  if (x < PIECES) {
+    constexpr int RPS = 16 / SB;                    // positions of a piece
+    const int r = x * RPS;
+    const int real = (r < 16 ? page0 : page1) >= 0 ? min(max(n - p0 - r, 0), RPS) * SB : 0;
+    const int64_t sat = r < 16 ? b0 + (CB << P.shift) + (in_page + r) * SB : b1 + (CB << P.shift) + (up + r - 16) * SB;
+    cp_async(sdst, sbase + (real ? sat : 0), real);
+  }
 }
 
 template <int HD, int NB>
@@ -244,17 +272,21 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     use.sub = (int)(s_at / use.q.nc);
     use.c = (int)(s_at - (int64_t)use.sub * use.q.nc);
     const int64_t all = min(share, total - lo);
-    use.c1 = (int)min((int64_t)use.q.nc, use.c + all);
+    use.c1 = use.c == 0 && use.q.nc <= kWhole ? use.q.nc : (int)min((int64_t)use.q.nc, use.c + all);
     use.rem = all - (use.c1 - use.c);
   }
   int64_t start = lo - use.c;       // where the stream's first chunk is
+  if (use.c > 0 && use.q.nc <= kWhole) {   // the CTA before has it all
+    start += use.q.nc;
+    if (!use.next(A)) return;
+  }
   Walk<NB> ld = use;
   bool more = true;
   ld.c += warp;
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * stage_bytes<HD>();
 
   // The load walk stands on the chunk to copy next; its page ids are read a chunk early.
-  int64_t id0 = -1, id1 = -1;
+  int id0 = -1, id1 = -1;
   auto fetch_ids = [&]() {
     while (more && ld.c >= ld.c1) {
       more = ld.next(A);
@@ -262,28 +294,30 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     }
     if (!more) return;
     const int p0 = ld.c * kChunk;
-    const int32_t* row = A.a.table + (int64_t)ld.i * A.a.max_pages;
-    const int top = max(ld.q.n - 1, 0) >> A.p.shift;   // the last page with positions
-    id0 = ld.q.n > 0 ? row[min(p0 >> A.p.shift, top)] : -1;
-    id1 = A.p.shift == 4 && ld.q.n > 0 ? row[min((p0 + 16) >> A.p.shift, top)] : id0;
+    id0 = id1 = -1;
+    if (p0 < ld.q.n) {              // (a chunk of nothing has no page)
+      const int32_t* row = A.a.table + (int64_t)ld.i * A.a.max_pages;
+      id0 = id1 = row[p0 >> A.p.shift];
+      if (A.p.shift == 4 && p0 + 16 < ld.q.n) id1 = row[(p0 >> 4) + 1];
+    }
   };
-  uint32_t there = 0;               // two bits per chunk in flight, the oldest lowest
+  uint32_t there = 0;               // two bits per chunk in flight, the oldest lowest: 16 positions whose page is there
   int flying = 0, put = 0, take = 0;
   auto issue = [&]() {
-    uint32_t ok = 0;
     if (more) {
       const int p0 = ld.c * kChunk;
-      const bool in0 = id0 >= 0 && id0 < A.p.n_pages, in1 = id1 >= 0 && id1 < A.p.n_pages;
-      if (lane == 0 && A.flags && ld.q.n > 0 && ((!in0 && p0 < ld.q.n) || (!in1 && p0 + 16 < ld.q.n)))
-        atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
-      const int subs_g = ld.q.subs / A.p.nkv;
-      ok = load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), in0 ? id0 : -1, in1 ? id1 : -1, ld.sub / subs_g, p0,
-                          ld.q.n, lane);
+      uint32_t ok = 3;
+      if ((uint32_t)id0 >= (uint32_t)A.p.n_pages || (uint32_t)id1 >= (uint32_t)A.p.n_pages) {
+        if ((uint32_t)id0 >= (uint32_t)A.p.n_pages) id0 = -1, ok &= 2;
+        if ((uint32_t)id1 >= (uint32_t)A.p.n_pages) id1 = -1, ok &= 1;
+        if (lane == 0 && A.flags && p0 < ld.q.n) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+      }
+      load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), id0, id1, ld.g(A), p0, ld.q.n, lane);
+      there |= ok << (2 * flying);
       ld.c += kWarps;
       fetch_ids();
     }
     cp_commit();
-    there |= ok << (2 * flying);
     ++flying;
     put = put + 1 == kStages ? 0 : put + 1;
   };
@@ -291,9 +325,20 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) issue();
 
+  // where a lane's codes and scales are in a stage: keys of row lg, values of rows 2 lc and 2 lc + 1
+  constexpr int VC = kChunk * code_bytes(HD), KSC = 2 * VC, VSC = KSC + kChunk * scale_bytes(HD);
+  const int k_at = place(lg) * code_bytes(HD) + lc * (HD / 8);
+  const int ks_at = KSC + place(lg) * scale_bytes(HD) + (lc * (HD / 4) / 32) * 2;
+  int v_at[2], vs_at[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    v_at[u] = VC + place(2 * lc + u) * code_bytes(HD) + lg * (HD / 16);
+    vs_at[u] = VSC + place(2 * lc + u) * scale_bytes(HD) + (lg * (HD / 8) / 32) * 2;
+  }
+
   for (bool go = true; go;) {
     // ---- one stream (or the part of it in this share)
-    const int subs_g = use.q.subs / A.p.nkv, g = use.sub / subs_g, r0 = (use.sub - g * subs_g) * ROWS;
+    const int g = use.g(A), r0 = (use.sub - g * (use.q.subs / A.p.nkv)) * ROWS;
     const int rows = min(use.q.m * G - r0, ROWS), n = use.q.n;
     const bool whole = use.c == 0 && use.c1 == use.q.nc;
     // queries: rows lg of each block of eight, this lane's HD / 4 channels
@@ -324,8 +369,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         fac[b][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
-        const int rr = 8 * b + 2 * lc + e;
-        seen[b][e] = rr < rows ? n - use.q.m + (r0 + rr) / G + 1 : 0;
+        // (rows that are not there repeat the last)
+        seen[b][e] = n - use.q.m + (r0 + min(8 * b + 2 * lc + e, rows - 1)) / G + 1;
       }
     }
     const int all_seen = n - use.q.m + r0 / G + 1;   // positions that every row sees
@@ -344,8 +389,6 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       cp_wait<kStages - 2>();
       __syncwarp();
       const uint8_t* st = smem + (warp * kStages + take) * stage_bytes<HD>();
-      const uint8_t *kc = st, *vc = st + kChunk * code_bytes(HD), *ks = st + 2 * kChunk * code_bytes(HD);
-      const uint8_t* vs = ks + kChunk * scale_bytes(HD);
       const uint32_t ok = there & 3u;
       there >>= 2;
       --flying;
@@ -359,10 +402,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
         uint32_t a[2][HD / 8];                       // halves of the two positions' channels
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int r = 16 * t + place(lg) + 8 * u;
-          const __half sc = *reinterpret_cast<const __half*>(ks + r * scale_bytes(HD) + (lc * (HD / 4) / 32) * 2);
+          const __half sc = *reinterpret_cast<const __half*>(st + ks_at + (16 * t + 8 * u) * scale_bytes(HD));
           const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(kc + r * code_bytes(HD) + lc * (HD / 8));
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(st + k_at + (16 * t + 8 * u) * code_bytes(HD));
           if constexpr (HD == 128) {
             const uint4 v = *reinterpret_cast<const uint4*>(w);
             dequant4(v.x, s2, s72, a[u]);
@@ -390,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       const bool cut = p0 + kChunk > all_seen || ok != 3u;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        if (cut || rows < ROWS) {
+        if (cut) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -401,16 +443,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
         }
         float mx[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          mx[e] = fmaxf(fmaxf(s[b][0][e], s[b][0][e + 2]), fmaxf(s[b][1][e], s[b][1][e + 2]));
-#pragma unroll
-          for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
-          mx[e] *= fac[b][e];
-        }
+        for (int e = 0; e < 2; ++e)
+          mx[e] = fmaxf(fmaxf(s[b][0][e], s[b][0][e + 2]), fmaxf(s[b][1][e], s[b][1][e + 2])) * fac[b][e];
         if (__any_sync(0xffffffffu, mx[0] > m[b][0] + 8.f || mx[1] > m[b][1] + 8.f)) {
           float al[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], x));
             const float to = fmaxf(m[b][e], mx[e]);
             al[e] = to == -INFINITY ? 1.f : tca::exp2a(m[b][e] - to);
             m[b][e] = to;
@@ -435,16 +475,40 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
         }
       }
       // ---- O^T: this lane's four positions of each 16, channels lg * HD / 8 on
+      // scales of pairs of positions, [16 positions][pairs 0 1, 8 9 of the contraction]
+      __half2 vsc[2][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          vsc[t][u] = __halves2half2(*reinterpret_cast<const __half*>(st + vs_at[0] + (16 * t + 8 * u) * scale_bytes(HD)),
+                                     *reinterpret_cast<const __half*>(st + vs_at[1] + (16 * t + 8 * u) * scale_bytes(HD)));
+      // A NaN must not meet the zero probabilities of rows that do not see its position:
+      // its values count as zeros, and the rows that do see it become NaN below.
       int nan_at = INT32_MAX;                         // first position whose values here are NaN
+      const __half2 probe = __hadd2(__hadd2(vsc[0][0], vsc[0][1]), __hadd2(vsc[1][0], vsc[1][1]));
+      const bool has_nan = __any_sync(0xffffffffu, !__hbeq2(probe, probe));   // (NaN spreads through sums)
+      if (has_nan) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            __half x = (u & 1) ? __high2half(vsc[t][u >> 1]) : __low2half(vsc[t][u >> 1]);
+            if (!__hisnan(x)) continue;
+            nan_at = min(nan_at, p0 + 16 * t + place(2 * lc + (u & 1)) + 8 * (u >> 1));
+            const __half2 z = vsc[t][u >> 1], o2 = __float2half2_rn(0.f);
+            vsc[t][u >> 1] = (u & 1) ? __lows2half2(z, o2) : __highs2half2(o2, z);
+          }
+      }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
+        const __half2 k72 = __float2half2_rn(-72.f);
+        const __half2 sa = vsc[t][0], sb = vsc[t][1], sa72 = __hmul2(sa, k72), sb72 = __hmul2(sb, k72);
         uint32_t w[4][HD / 64];
-        __half sc[4];
-        int pos[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          pos[u] = 16 * t + place(2 * lc + (u & 1)) + 8 * (u >> 1);
-          const uint32_t* src = reinterpret_cast<const uint32_t*>(vc + pos[u] * code_bytes(HD) + lg * (HD / 16));
+          const uint32_t* src =
+              reinterpret_cast<const uint32_t*>(st + v_at[u & 1] + (16 * t + 8 * (u >> 1)) * code_bytes(HD));
           if constexpr (HD == 128) {
             const uint2 v = *reinterpret_cast<const uint2*>(src);
             w[u][0] = v.x;
@@ -452,18 +516,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
           } else {
             w[u][0] = *src;
           }
-          sc[u] = *reinterpret_cast<const __half*>(vs + pos[u] * scale_bytes(HD) + (lg * (HD / 8) / 32) * 2);
         }
-        // A NaN must not meet the zero probabilities of rows that do not see its position:
-        // its values count as zeros here, and the rows that do see it become NaN below.
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (__hisnan(sc[u])) {
-            sc[u] = __ushort_as_half(0);
-            nan_at = min(nan_at, p0 + pos[u]);
-          }
-        const __half2 sa = __halves2half2(sc[0], sc[1]), sb = __halves2half2(sc[2], sc[3]);
-        const __half2 k72 = __float2half2_rn(-72.f), sa72 = __hmul2(sa, k72), sb72 = __hmul2(sb, k72);
 #pragma unroll
         for (int x = 0; x < HD / 64; ++x) {
           uint32_t a[4][4];
@@ -479,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
           }
         }
       }
-      if (__any_sync(0xffffffffu, nan_at != INT32_MAX)) {
+      if (has_nan) {
         nan_at = min(nan_at, __shfl_xor_sync(0xffffffffu, nan_at, 1));
         nan_at = min(nan_at, __shfl_xor_sync(0xffffffffu, nan_at, 2));
 #pragma unroll
