@@ -120,23 +120,64 @@ struct Walk {
 __device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
 __device__ __forceinline__ __half2 as_h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
 
-// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.
-__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72) {
-  return h2(__hfma2(as_h2((w & 0x00F000F0u) | 0x54005400u), s, s72));
+// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.  `magic`: 64 in
+// both halves, in a register (the instruction takes one constant).
+__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72, uint32_t magic) {
+  uint32_t x;
+  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic));   // (w & mask) | magic
+  return h2(__hfma2(as_h2(x), s, s72));
+}
+#ifndef SHIFTS
+#define SHIFTS 0
+#endif
+__device__ __forceinline__ uint32_t dq_low(uint32_t w, __half2 s, uint32_t magic1024) {   // codes in bits 0 .. 3
+  uint32_t x;
+  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic1024));
+  return h2(__hmul2(__hadd2(as_h2(x), __float2half2_rn(-1032.f)), s));
 }
 // The four pairs (codes j of both halves) of a word.
-__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t* o) {
-  o[0] = dequant(w << 4, s, s72);
-  o[1] = dequant(w, s, s72);
-  o[2] = dequant(w >> 4, s, s72);
-  o[3] = dequant(w >> 8, s, s72);
+__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t m1024, uint32_t* o) {
+#if SHIFTS == 0
+  o[0] = dequant(w << 4, s, s72, magic);
+  o[1] = dequant(w, s, s72, magic);
+  o[2] = dequant(w >> 4, s, s72, magic);
+  o[3] = dequant(w >> 8, s, s72, magic);
+#elif SHIFTS == 1
+  const uint32_t t = w >> 8;
+  o[0] = dq_low(w, s, m1024);
+  o[1] = dequant(w, s, s72, magic);
+  o[2] = dq_low(t, s, m1024);
+  o[3] = dequant(t, s, s72, magic);
+#elif SHIFTS == 2
+  uint32_t t;
+  asm("mul.hi.u32 %0, %1, 0x01000000;" : "=r"(t) : "r"(w));
+  o[0] = dq_low(w, s, m1024);
+  o[1] = dequant(w, s, s72, magic);
+  o[2] = dq_low(t, s, m1024);
+  o[3] = dequant(t, s, s72, magic);
+#elif SHIFTS == 3
+  uint32_t a, b, c;
+  asm("mul.lo.u32 %0, %1, 16;" : "=r"(a) : "r"(w));
+  asm("mul.hi.u32 %0, %1, 0x10000000;" : "=r"(b) : "r"(w));
+  asm("mul.hi.u32 %0, %1, 0x01000000;" : "=r"(c) : "r"(w));
+  o[0] = dequant(a, s, s72, magic);
+  o[1] = dequant(w, s, s72, magic);
+  o[2] = dequant(b, s, s72, magic);
+  o[3] = dequant(c, s, s72, magic);
+#elif SHIFTS == 4
+  const uint32_t t = w >> 8;
+  o[0] = dequant(w << 4, s, s72, magic);
+  o[1] = dequant(w, s, s72, magic);
+  o[2] = dq_low(t, s, m1024);
+  o[3] = dequant(t, s, s72, magic);
+#endif
 }
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes) {   // the rest of 16: zeros
@@ -336,6 +377,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     vs_at[u] = VSC + place(2 * lc + u) * scale_bytes(HD) + (lg * (HD / 8) / 32) * 2;
   }
 
+  uint32_t magic, m1024;            // (opaque: otherwise they are made anew at every use)
+  asm volatile("mov.b32 %0, 0x54005400;" : "=r"(magic));
+  asm volatile("mov.b32 %0, 0x64006400;" : "=r"(m1024));
+
   for (bool go = true; go;) {
     // ---- one stream (or the part of it in this share)
     const int g = use.g(A), r0 = (use.sub - g * (use.q.subs / A.p.nkv)) * ROWS;
@@ -398,34 +443,40 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       // ---- S^T
       float s[NB][2][4];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        uint32_t a[2][HD / 8];                       // halves of the two positions' channels
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const __half sc = *reinterpret_cast<const __half*>(st + ks_at + (16 * t + 8 * u) * scale_bytes(HD));
-          const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(st + k_at + (16 * t + 8 * u) * code_bytes(HD));
-          if constexpr (HD == 128) {
-            const uint4 v = *reinterpret_cast<const uint4*>(w);
-            dequant4(v.x, s2, s72, a[u]);
-            dequant4(v.y, s2, s72, a[u] + 4);
-            dequant4(v.z, s2, s72, a[u] + 8);
-            dequant4(v.w, s2, s72, a[u] + 12);
-          } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(w);
-            dequant4(v.x, s2, s72, a[u]);
-            dequant4(v.y, s2, s72, a[u] + 4);
+        for (int t = 0; t < 2; ++t) s[b][t][0] = s[b][t][1] = s[b][t][2] = s[b][t][3] = 0.f;
+      {
+        uint32_t w[2][2][HD / 32];                   // codes of positions 16 t + 8 u + place(lg)
+        __half2 sc[2][2], s72[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint8_t* src = st + k_at + (16 * t + 8 * u) * code_bytes(HD);
+            if constexpr (HD == 128) {
+              const uint4 v = *reinterpret_cast<const uint4*>(src);
+              w[t][u][0] = v.x, w[t][u][1] = v.y, w[t][u][HD / 32 - 2] = v.z, w[t][u][HD / 32 - 1] = v.w;
+            } else {
+              const uint2 v = *reinterpret_cast<const uint2*>(src);
+              w[t][u][0] = v.x, w[t][u][1] = v.y;
+            }
+            sc[t][u] = __half2half2(*reinterpret_cast<const __half*>(st + ks_at + (16 * t + 8 * u) * scale_bytes(HD)));
+            s72[t][u] = __hmul2(sc[t][u], __float2half2_rn(-72.f));
           }
-        }
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          s[b][t][0] = s[b][t][1] = s[b][t][2] = s[b][t][3] = 0.f;
+        for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            const uint32_t f[4] = {a[0][2 * k], a[1][2 * k], a[0][2 * k + 1], a[1][2 * k + 1]};
-            mma_f16(s[b][t], f, qf[b][k][0], qf[b][k][1]);
+          for (int t = 0; t < 2; ++t) {
+            uint32_t x[4], y[4];
+            dequant4(w[t][0][i], sc[t][0], s72[t][0], magic, m1024, x);
+            dequant4(w[t][1][i], sc[t][1], s72[t][1], magic, m1024, y);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              mma_f16(s[b][t], x[0], y[0], x[1], y[1], qf[b][2 * i][0], qf[b][2 * i][1]);
+              mma_f16(s[b][t], x[2], y[2], x[3], y[3], qf[b][2 * i + 1][0], qf[b][2 * i + 1][1]);
+            }
           }
-        }
       }
       // ---- mask and softmax
       uint32_t pt[NB][2][2];
@@ -520,15 +571,15 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
 #pragma unroll
         for (int x = 0; x < HD / 64; ++x) {
           uint32_t a[4][4];
-          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, a[0]);
-          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, a[1]);
-          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, a[2]);
-          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, a[3]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, magic, m1024, a[0]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, magic, m1024, a[1]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, magic, m1024, a[2]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, magic, m1024, a[3]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t f[4] = {a[0][j], a[1][j], a[2][j], a[3][j]};
 #pragma unroll
-            for (int b = 0; b < NB; ++b) mma_f16(o[b][4 * x + j], f, pt[b][t][0], pt[b][t][1]);
+            for (int b = 0; b < NB; ++b)
+              mma_f16(o[b][4 * x + j], a[0][j], a[1][j], a[2][j], a[3][j], pt[b][t][0], pt[b][t][1]);
           }
         }
       }
@@ -597,8 +648,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       }
     }
     if (!whole) {
-      __threadfence();
-      __syncthreads();
+      __syncthreads();   // the partial's writes come before the arrival, which releases them
       const int spans = (int)(last_cta - first_cta) + 1;
       if (tid == 0) {
         s_last = ptx::atom_add_acq_rel(A.arrive + first_cta, 1) == spans - 1;
@@ -606,22 +656,52 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       }
       __syncthreads();
       if (s_last) {
-        for (int x = tid; x < rows * (HD / 4); x += kThreads) {
-          const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
+        // first every row's M = max m and L = sum 2^(m - M) l over the spans, a warp per row;
+        // then the outputs, eight spans' loads at a time
+        auto span = [&](int k) {
+          return A.part + (2 * (first_cta + k) + (k == 0 ? 1 : 0)) * partial_floats<HD, NB>();
+        };
+        for (int r = warp; r < rows; r += kWarps) {
           float M = -INFINITY, L = 0.f;
+          for (int k = lane; k < spans; k += 32) M = fmaxf(M, __ldcg(span(k) + r));
+          M = warp_max(M);
+          const float at = M == -INFINITY ? 0.f : M;
+          for (int k = lane; k < spans; k += 32)
+            L += __ldcg(span(k) + ROWS + r) * tca::exp2a(__ldcg(span(k) + r) - at);
+          L = warp_sum(L);
+          if (lane == 0) sM[r] = at, sL[r] = M == -INFINITY ? 0.f : 1.f / L;
+        }
+        __syncthreads();
+        const int items = rows * (HD / 4);
+        // few rows: the spans go over as many groups of threads as there are
+        const int groups = max(1, kThreads / items), grp = tid / items;
+        for (int x = items >= kThreads ? tid : tid - grp * items; x < items; x += kThreads) {
+          if (items < kThreads && grp >= groups) break;
+          const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int64_t k = first_cta; k <= last_cta; ++k) {
-            const float* p = A.part + (2 * k + (k == first_cta ? 1 : 0)) * partial_floats<HD, NB>();
-            const float mk = __ldcg(p + r), lk = __ldcg(p + ROWS + r);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS + r * HD + ch));
-            const float to = fmaxf(M, mk);
-            const float a = M == -INFINITY ? 0.f : tca::exp2a(M - to), b = mk == -INFINITY ? 0.f : tca::exp2a(mk - to);
-            M = to;
-            L = L * a + lk * b;
-            v.x = v.x * a + y.x * b, v.y = v.y * a + y.y * b, v.z = v.z * a + y.z * b, v.w = v.w * a + y.w * b;
+#pragma unroll 8
+          for (int k = items < kThreads ? grp : 0; k < spans; k += groups) {
+            const float a = tca::exp2a(__ldcg(span(k) + r) - sM[r]);
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(span(k) + 2 * ROWS + r * HD + ch));
+            v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
           }
-          const float inv = M == -INFINITY ? 0.f : 1.f / L;
-          out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+          if (groups == 1) {
+            out4(r, ch, make_float4(v.x * sL[r], v.y * sL[r], v.z * sL[r], v.w * sL[r]));
+          } else {
+            reinterpret_cast<float4*>(sO)[grp * items + x] = v;
+          }
+        }
+        if (groups > 1) {
+          __syncthreads();
+          if (tid < items) {
+            const int r = tid / (HD / 4), ch = tid % (HD / 4) * 4;
+            float4 v = reinterpret_cast<float4*>(sO)[tid];
+            for (int k = 1; k < groups; ++k) {
+              const float4 y = reinterpret_cast<float4*>(sO)[k * items + tid];
+              v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+            }
+            out4(r, ch, make_float4(v.x * sL[r], v.y * sL[r], v.z * sL[r], v.w * sL[r]));
+          }
         }
       }
     }
