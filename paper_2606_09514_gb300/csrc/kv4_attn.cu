@@ -22,8 +22,11 @@
 // softmax's factor.  Probabilities are rounded to half for the product only (their
 // sum is taken before): 2^-12 of the largest value at most.
 //
-// Work: chunks of 32 positions of all streams, end to end, in equal shares per CTA;
-// (a short stream belongs to the share where it begins: what a CTA saves by passing on
+// Work: all streams end to end, each as its chunks of 32 positions and kOpen chunks'
+// worth for its beginning and end, in equal shares per CTA (31 sequences of 100 to
+// 4,096 positions, 40 KV heads: 174 us with shares of chunks alone, 93, 70, 72 and 77 us
+// with 4, 8, 16 and 24 for an opening; 250 sequences of 512 to 8,192, 4 KV heads: 121, then
+// 110, 104, 106, 113; a short stream belongs to the share where it begins: what a CTA saves by passing on
 // a part of it, the partials cost again); in a share, four warps take the chunks of a stream in turn, each with its own ring of
 // cp.async buffers that runs on across streams; rows past the sequence's end and
 // pages that are not there are filled with zeros and masked.  A stream within a share
@@ -52,6 +55,7 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 3;
 constexpr int kCtasPerSm = 3;
 constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
+constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
 constexpr int kMaxGrid = 1024;   // CTAs: three on each of at most 341 SMs
 
 template <int HD>
@@ -98,16 +102,17 @@ template <int NB>
 struct Walk {
   Seq q;
   int i, sub, c, c1;          // sequence, stream of it, chunks [c, c1) of the stream in this share
-  int64_t rem;                // chunks of the share behind this stream
+  int64_t rem;                // what is left of the share behind this stream
   __device__ __forceinline__ int g(const AttnArgs4& A) const { return q.subs == A.p.nkv ? sub : sub / (q.subs / A.p.nkv); }
   // to the next stream; false at the share's end
   __device__ __forceinline__ bool next(const AttnArgs4& A) {
+    rem -= kOpen;
     if (rem <= 0) return false;
     if (++sub >= q.subs) {
       sub = 0;
       bool bad;
       do {
-        q = seq_of<NB>(A, ++i, &bad);   // rem > 0: there is another sequence with streams
+        q = seq_of<NB>(A, ++i, &bad);   // (with some of the share left there is another stream)
       } while (q.subs == 0);
     }
     c = 0;
@@ -127,50 +132,14 @@ __device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72, 
   asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic));   // (w & mask) | magic
   return h2(__hfma2(as_h2(x), s, s72));
 }
-#ifndef SHIFTS
-#define SHIFTS 0
-#endif
-__device__ __forceinline__ uint32_t dq_low(uint32_t w, __half2 s, uint32_t magic1024) {   // codes in bits 0 .. 3
-  uint32_t x;
-  asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic1024));
-  return h2(__hmul2(__hadd2(as_h2(x), __float2half2_rn(-1032.f)), s));
-}
-// The four pairs (codes j of both halves) of a word.
-__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t m1024, uint32_t* o) {
-#if SHIFTS == 0
+// The four pairs (codes j of both halves) of a word.  (Codes in bits 0 .. 3 can also be
+// taken without a shift, as 1024 + n, one subtraction and one product: as fast.  Shifts as
+// high halves of products, on the other pipe, are 4 to 10% slower.)
+__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t* o) {
   o[0] = dequant(w << 4, s, s72, magic);
   o[1] = dequant(w, s, s72, magic);
   o[2] = dequant(w >> 4, s, s72, magic);
   o[3] = dequant(w >> 8, s, s72, magic);
-#elif SHIFTS == 1
-  const uint32_t t = w >> 8;
-  o[0] = dq_low(w, s, m1024);
-  o[1] = dequant(w, s, s72, magic);
-  o[2] = dq_low(t, s, m1024);
-  o[3] = dequant(t, s, s72, magic);
-#elif SHIFTS == 2
-  uint32_t t;
-  asm("mul.hi.u32 %0, %1, 0x01000000;" : "=r"(t) : "r"(w));
-  o[0] = dq_low(w, s, m1024);
-  o[1] = dequant(w, s, s72, magic);
-  o[2] = dq_low(t, s, m1024);
-  o[3] = dequant(t, s, s72, magic);
-#elif SHIFTS == 3
-  uint32_t a, b, c;
-  asm("mul.lo.u32 %0, %1, 16;" : "=r"(a) : "r"(w));
-  asm("mul.hi.u32 %0, %1, 0x10000000;" : "=r"(b) : "r"(w));
-  asm("mul.hi.u32 %0, %1, 0x01000000;" : "=r"(c) : "r"(w));
-  o[0] = dequant(a, s, s72, magic);
-  o[1] = dequant(w, s, s72, magic);
-  o[2] = dequant(b, s, s72, magic);
-  o[3] = dequant(c, s, s72, magic);
-#elif SHIFTS == 4
-  const uint32_t t = w >> 8;
-  o[0] = dequant(w << 4, s, s72, magic);
-  o[1] = dequant(w, s, s72, magic);
-  o[2] = dq_low(t, s, m1024);
-  o[3] = dequant(t, s, s72, magic);
-#endif
 }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -262,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
   const int B = A.a.batch, G = A.G;
 
-  // ---- this CTA's share: chunks [lo, lo + share) of all
+  // ---- this CTA's share: [lo, lo + share) of all streams' openings and chunks
   const int per = (B + kThreads - 1) / kThreads;
   const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
   int64_t mine = 0;
@@ -271,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     bool bad;
     const Seq q = seq_of<NB>(A, i, &bad);
     any_bad |= bad;
-    mine += (int64_t)q.nc * q.subs;
+    mine += (int64_t)(q.nc + kOpen) * q.subs;
   }
   if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
   int64_t upto = mine;
@@ -295,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     for (int i = b0; i < b1; ++i) {
       bool bad;
       const Seq q = seq_of<NB>(A, i, &bad);
-      const int64_t n = (int64_t)q.nc * q.subs;
+      const int64_t n = (int64_t)(q.nc + kOpen) * q.subs;
       if (lo < at + n) {
         s_first = i;
         s_at = lo - at;
@@ -306,20 +275,25 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
   }
   __syncthreads();
   Walk<NB> use;
+  int64_t start;                    // where the first chunk of the stream is
   {
     bool bad;
     use.i = s_first;
     use.q = seq_of<NB>(A, use.i, &bad);
-    use.sub = (int)(s_at / use.q.nc);
-    use.c = (int)(s_at - (int64_t)use.sub * use.q.nc);
-    const int64_t all = min(share, total - lo);
-    use.c1 = use.c == 0 && use.q.nc <= kWhole ? use.q.nc : (int)min((int64_t)use.q.nc, use.c + all);
-    use.rem = all - (use.c1 - use.c);
-  }
-  int64_t start = lo - use.c;       // where the stream's first chunk is
-  if (use.c > 0 && use.q.nc <= kWhole) {   // the CTA before has it all
-    start += use.q.nc;
-    if (!use.next(A)) return;
+    use.sub = (int)(s_at / (use.q.nc + kOpen));
+    const int64_t x = s_at - (int64_t)use.sub * (use.q.nc + kOpen) - kOpen;   // chunk of the stream; below 0: its opening
+    start = lo - x;
+    use.rem = min(share, total - lo) + min(x, (int64_t)0);
+    use.c = (int)max(x, (int64_t)0);
+    if (use.rem <= 0) return;
+    if (x > 0 && use.q.nc <= kWhole) {   // the CTA before has it all
+      use.rem -= use.q.nc - x;
+      start += use.q.nc + kOpen;
+      if (!use.next(A)) return;
+    } else {
+      use.c1 = use.q.nc <= kWhole ? use.q.nc : (int)min((int64_t)use.q.nc, use.c + use.rem);
+      use.rem -= use.c1 - use.c;
+    }
   }
   Walk<NB> ld = use;
   bool more = true;
@@ -377,9 +351,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     vs_at[u] = VSC + place(2 * lc + u) * scale_bytes(HD) + (lg * (HD / 8) / 32) * 2;
   }
 
-  uint32_t magic, m1024;            // (opaque: otherwise they are made anew at every use)
+  uint32_t magic;                   // (opaque: otherwise it is made anew at every use)
   asm volatile("mov.b32 %0, 0x54005400;" : "=r"(magic));
-  asm volatile("mov.b32 %0, 0x64006400;" : "=r"(m1024));
 
   for (bool go = true; go;) {
     // ---- one stream (or the part of it in this share)
@@ -469,8 +442,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             uint32_t x[4], y[4];
-            dequant4(w[t][0][i], sc[t][0], s72[t][0], magic, m1024, x);
-            dequant4(w[t][1][i], sc[t][1], s72[t][1], magic, m1024, y);
+            dequant4(w[t][0][i], sc[t][0], s72[t][0], magic, x);
+            dequant4(w[t][1][i], sc[t][1], s72[t][1], magic, y);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
               mma_f16(s[b][t], x[0], y[0], x[1], y[1], qf[b][2 * i][0], qf[b][2 * i][1]);
@@ -571,10 +544,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
 #pragma unroll
         for (int x = 0; x < HD / 64; ++x) {
           uint32_t a[4][4];
-          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, magic, m1024, a[0]);
-          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, magic, m1024, a[1]);
-          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, magic, m1024, a[2]);
-          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, magic, m1024, a[3]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, magic, a[0]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, magic, a[1]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, magic, a[2]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, magic, a[3]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -706,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       }
     }
     __syncthreads();     // sM, sL, sO are free again
-    start += use.q.nc;
+    start += use.q.nc + kOpen;
     go = use.next(A);
   }
   cp_wait<0>();
