@@ -478,6 +478,8 @@ class KV4Cache:
                                      n_pages, page_size, n_kv, self.head_dim)
         self.lib = load_library()
         self.workspace = workspace
+        self._made: List = []           # workspaces made here; calls under way may still use an older one
+        self._need: Dict = {}
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv: int, head_dim: int, device="cuda",
@@ -486,9 +488,12 @@ class KV4Cache:
         return cls(*(torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2)), page_size, workspace)
 
     def workspace_bytes(self, n_q_heads: int, max_new: int = 1) -> int:
-        n = self.lib.buddy_kv4_attention_workspace(n_q_heads, self.n_kv, self.head_dim, max_new)
-        if n < 0:
-            raise BuddyError(BUDDY_ERR_ARG, "buddy_kv4_attention_workspace")
+        n = self._need.get((n_q_heads, max_new))
+        if n is None:
+            n = self.lib.buddy_kv4_attention_workspace(n_q_heads, self.n_kv, self.head_dim, max_new)
+            if n < 0:
+                raise BuddyError(BUDDY_ERR_ARG, "buddy_kv4_attention_workspace")
+            self._need[n_q_heads, max_new] = n
         return n
 
     def buddy_kv4_append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
@@ -528,7 +533,10 @@ class KV4Cache:
             raise ValueError("q, out: [tokens, heads, head_dim of the cache], table: [batch, max_pages] are wanted")
         ws = workspace if workspace is not None else self.workspace
         if ws is None:
-            ws = self.workspace = torch.zeros(self.workspace_bytes(nq, max_new), dtype=torch.uint8, device=q.device)
+            need = self.workspace_bytes(nq, max_new)
+            if not self._made or self._made[-1].numel() < need:
+                self._made.append(torch.zeros(need, dtype=torch.uint8, device=q.device))
+            ws = self._made[-1]
         a = buddy_kv4_attention_args(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1),
                                      table.shape[1], scale, q.data_ptr(), out.data_ptr(), _heads(q, T, hd, "q"),
                                      _heads(out, T, hd, "out"), _at(row_start, i32, B + 1, "row_start"),

@@ -36,11 +36,8 @@
 
 #include <algorithm>
 
-#include "attn_tc.cuh"
-#include "common.cuh"
 #include "internal.h"
-#include "kv4.cuh"
-#include "ptx.cuh"
+#include "kv4_attn.cuh"
 
 namespace buddy {
 
@@ -57,6 +54,7 @@ constexpr int kCtasPerSm = 3;
 constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
 constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
 constexpr int kMaxGrid = 1024;   // CTAs: three on each of at most 341 SMs
+constexpr int kFewRows = 32;     // rows of a KV head up to which these kernels take a sequence
 
 template <int HD>
 __host__ __device__ constexpr int stage_bytes() { return 2 * kChunk * entry_bytes(HD); }
@@ -68,29 +66,15 @@ __host__ __device__ constexpr int smem_bytes() {
 template <int HD, int NB>
 __host__ __device__ constexpr int64_t partial_floats() { return 8 * NB * (HD + 2); }
 
-struct AttnArgs4 {
-  buddy_kv4_attention_args a;
-  Pages p;
-  int G, row_limit;           // sequences of at most this many rows are this kernel's
-  int32_t* flags;
-  int32_t* arrive;            // [grid], zero between calls
-  float* part;                // [grid][2]
-};
-
-// What a sequence asks for: query rows t0 .. t0 + m - 1, n positions.
-struct Seq {
-  int t0, m, n, nc, subs;     // nc chunks, subs streams (0: not this kernel's)
+// What a sequence asks for: query rows, positions, and its streams here.
+struct Seq : Rows {
+  int nc, subs;               // nc chunks, subs streams (0: not this kernel's)
 };
 
 template <int NB>
 __device__ __forceinline__ Seq seq_of(const AttnArgs4& A, int i, bool* bad) {
   Seq s;
-  s.t0 = A.a.row_start ? A.a.row_start[i] : i;
-  const int t1 = A.a.row_start ? A.a.row_start[i + 1] : i + 1;
-  s.n = A.a.kv_len[i];
-  *bad = s.t0 < 0 || t1 < s.t0 || t1 > A.a.n_tok || t1 - s.t0 > A.a.max_new || s.n < 0 ||
-         s.n > (int64_t)A.a.max_pages << A.p.shift;
-  s.m = *bad ? 0 : t1 - s.t0;
+  *static_cast<Rows*>(&s) = rows_of(A, i, bad);
   const int rows = s.m * A.G;
   s.nc = max(1, (s.n + kChunk - 1) / kChunk);   // (a sequence without positions: one chunk of nothing)
   s.subs = rows > A.row_limit ? 0 : A.p.nkv * ((rows + 8 * NB - 1) / (8 * NB));
@@ -121,26 +105,6 @@ struct Walk {
     return true;
   }
 };
-
-__device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
-__device__ __forceinline__ __half2 as_h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
-
-// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.  `magic`: 64 in
-// both halves, in a register (the instruction takes one constant).
-__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72, uint32_t magic) {
-  uint32_t x;
-  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic));   // (w & mask) | magic
-  return h2(__hfma2(as_h2(x), s, s72));
-}
-// The four pairs (codes j of both halves) of a word.  (Codes in bits 0 .. 3 can also be
-// taken without a shift, as 1024 + n, one subtraction and one product: as fast.  Shifts as
-// high halves of products, on the other pipe, are 4 to 10% slower.)
-__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t* o) {
-  o[0] = dequant(w << 4, s, s72, magic);
-  o[1] = dequant(w, s, s72, magic);
-  o[2] = dequant(w >> 4, s, s72, magic);
-  o[3] = dequant(w >> 8, s, s72, magic);
-}
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
@@ -377,13 +341,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       for (int e = 0; e < HD / 4; ++e) top = fmaxf(top, fabsf(x[e]));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
-      const float down = __uint_as_float((uint32_t)(127 - ex) << 23), up = __uint_as_float((uint32_t)(127 + ex) << 23);
+      float down, f;
+      row_scale(top, A.a.scale, HD, &down, &f);
 #pragma unroll
       for (int e = 0; e < HD / 4; e += 2)
         qf[b][e / 4][(e / 2) & 1] = h2(__floats2half2_rn(x[e] * down, x[e + 1] * down));
-      // (above zero, so that it takes -inf to -inf)
-      const float f = fmaxf((A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f * up, 1.2e-38f);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         fac[b][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
@@ -710,13 +672,21 @@ static int launch_decode(const AttnArgs4& A, int grid, cudaStream_t s) {
 using namespace buddy;
 
 constexpr int64_t kWsCounters = 4096;   // bytes of arrival counters in front of a workspace
+static int64_t few_bytes(int head_dim) { return kWsCounters + (int64_t)kMaxGrid * 2 * 16 * (head_dim + 2) * 4; }
+
+static bool sizes_ok(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_new) {
+  return n_kv_heads >= 1 && n_kv_heads <= 1024 && n_q_heads >= n_kv_heads && n_q_heads % n_kv_heads == 0 &&
+         n_q_heads / n_kv_heads <= 8 && (head_dim == 64 || head_dim == 128) && max_new >= 1;
+}
+static int64_t workspace_bytes(int group, int head_dim, int max_new, int sms) {
+  return few_bytes(head_dim) + ((int64_t)max_new * group > kFewRows ? prompt_workspace(head_dim, sms) : 0);
+}
 
 extern "C" int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                                  int32_t max_new) {
-  if (n_kv_heads < 1 || n_kv_heads > 1024 || n_q_heads < n_kv_heads || n_q_heads % n_kv_heads ||
-      n_q_heads / n_kv_heads > 8 || (head_dim != 64 && head_dim != 128) || max_new < 1)
-    return -1;
-  return kWsCounters + (int64_t)kMaxGrid * 2 * 16 * (head_dim + 2) * 4;
+  if (!sizes_ok(n_q_heads, n_kv_heads, head_dim, max_new)) return -1;
+  const int sms = sm_count();
+  return sms > 0 ? workspace_bytes(n_q_heads / n_kv_heads, head_dim, max_new, sms) : -1;
 }
 
 extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags,
@@ -724,13 +694,14 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   if (!kv4_cache_ok(cache) || !a || a->batch < 1 || a->batch > 16384 || a->n_tok < 0 || a->max_pages < 1 ||
       (int64_t)a->max_pages * cache->page_size > INT32_MAX || !(a->scale >= 0.f) || a->scale > 3e38f)
     return BUDDY_ERR_ARG;
-  const int64_t need =
-      buddy_kv4_attention_workspace(a->n_q_heads, cache->n_kv_heads, cache->head_dim, a->max_new);
-  if (need < 0 || (a->q_dtype != BUDDY_DTYPE_F32 && a->q_dtype != BUDDY_DTYPE_BF16) ||
+  if (!sizes_ok(a->n_q_heads, cache->n_kv_heads, cache->head_dim, a->max_new) ||
+      (a->q_dtype != BUDDY_DTYPE_F32 && a->q_dtype != BUDDY_DTYPE_BF16) ||
       (a->out_dtype != BUDDY_DTYPE_F32 && a->out_dtype != BUDDY_DTYPE_BF16) || !a->kv_len || !a->table)
     return BUDDY_ERR_ARG;
   if (!a->row_start && (a->n_tok != a->batch || a->max_new != 1)) return BUDDY_ERR_ARG;
-  if (!a->workspace || a->workspace_bytes < need || (reinterpret_cast<uintptr_t>(a->workspace) & 255)) return BUDDY_ERR_ARG;
+  if (!a->workspace || a->workspace_bytes < few_bytes(cache->head_dim) ||
+      (reinterpret_cast<uintptr_t>(a->workspace) & 255))
+    return BUDDY_ERR_ARG;
   if (a->n_tok == 0) return BUDDY_OK;
   if ((int64_t)a->n_tok * a->n_q_heads > INT32_MAX) return BUDDY_ERR_RANGE;   // rows are counted in 32 bits
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) ||
@@ -738,15 +709,20 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
     return BUDDY_ERR_ARG;
   const int sms = sm_count();
   if (sms == 0) return BUDDY_ERR_CUDA;
-  AttnArgs4 A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, INT32_MAX, flags, (int32_t*)a->workspace,
+  if (a->workspace_bytes < workspace_bytes(a->n_q_heads / cache->n_kv_heads, cache->head_dim, a->max_new, sms))
+    return BUDDY_ERR_ARG;
+  AttnArgs4 A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, kFewRows, flags, (int32_t*)a->workspace,
               (float*)((uint8_t*)a->workspace + kWsCounters)};
   // one CTA for every four chunks there can be, three on each SM at most
-  const bool two = (int64_t)a->max_new * A.G > 8;
-  const int64_t streams = cache->n_kv_heads * (((int64_t)a->max_new * A.G + (two ? 15 : 7)) / (two ? 16 : 8));
+  const int64_t most_rows = (int64_t)a->max_new * A.G;
+  const bool two = most_rows > 8;
+  const int64_t streams = cache->n_kv_heads * ((std::min<int64_t>(most_rows, kFewRows) + (two ? 15 : 7)) / (two ? 16 : 8));
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
   const int64_t most = streams > (1 << 20) || chunks > (1 << 20) ? INT32_MAX : a->batch * streams * chunks / kWarps + 1;
   const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, kCtasPerSm * sms));
   cudaStream_t s = (cudaStream_t)stream;
-  if (cache->head_dim == 128) return two ? launch_decode<128, 2>(A, grid, s) : launch_decode<128, 1>(A, grid, s);
-  return two ? launch_decode<64, 2>(A, grid, s) : launch_decode<64, 1>(A, grid, s);
+  const int rc = cache->head_dim == 128 ? (two ? launch_decode<128, 2>(A, grid, s) : launch_decode<128, 1>(A, grid, s))
+                                        : (two ? launch_decode<64, 2>(A, grid, s) : launch_decode<64, 1>(A, grid, s));
+  if (rc != BUDDY_OK || most_rows <= kFewRows) return rc;
+  return launch_prompt(A, cache->head_dim, sms, (uint8_t*)a->workspace + few_bytes(cache->head_dim), s);
 }

@@ -1,0 +1,72 @@
+// What the attention kernels over the 4-bit cache share: arguments, the sequences'
+// checks, and codes to halves.
+#pragma once
+
+#include "attn_tc.cuh"
+#include "common.cuh"
+#include "kv4.cuh"
+#include "ptx.cuh"
+
+namespace buddy {
+namespace kv4 {
+
+struct AttnArgs4 {
+  buddy_kv4_attention_args a;
+  Pages p;
+  int G, row_limit;           // sequences of at most this many rows are the few-row kernel's
+  int32_t* flags;
+  int32_t* arrive;            // few rows: [grid], zero between calls
+  float* part;                // partials of streams or items that are cut
+};
+
+// A sequence's query tokens t0 .. t0 + m - 1 and its n positions; m = 0 where they are bad.
+struct Rows {
+  int t0, m, n;
+};
+__device__ __forceinline__ Rows rows_of(const AttnArgs4& A, int i, bool* bad) {
+  Rows s;
+  s.t0 = A.a.row_start ? A.a.row_start[i] : i;
+  const int t1 = A.a.row_start ? A.a.row_start[i + 1] : i + 1;
+  s.n = A.a.kv_len[i];
+  *bad = s.t0 < 0 || t1 < s.t0 || t1 > A.a.n_tok || t1 - s.t0 > A.a.max_new || s.n < 0 ||
+         s.n > (int64_t)A.a.max_pages << A.p.shift;
+  s.m = *bad ? 0 : t1 - s.t0;
+  return s;
+}
+
+// Query rows enter the products as halves of 1 .. 2 times a power of two per row: the
+// exponent (of the row's largest magnitude), its inverse, and the factor that takes a
+// score of the halves to base 2.  (Above zero, so that it takes -inf to -inf.)
+__device__ __forceinline__ void row_scale(float top, float scale, int hd, float* down, float* fac) {
+  const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+  *down = __uint_as_float((uint32_t)(127 - ex) << 23);
+  const float up = __uint_as_float((uint32_t)(127 + ex) << 23);
+  *fac = fmaxf((scale != 0.f ? scale : rsqrtf((float)hd)) * 1.4426950408889634f * up, 1.2e-38f);
+}
+
+__device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+__device__ __forceinline__ __half2 as_h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+
+// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.  `magic`: 64 in
+// both halves, in a register (the instruction takes one constant).
+__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72, uint32_t magic) {
+  uint32_t x;
+  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic));   // (w & mask) | magic
+  return h2(__hfma2(as_h2(x), s, s72));
+}
+// The four pairs (codes j of both halves) of a word.  (Codes in bits 0 .. 3 can also be
+// taken without a shift, as 1024 + n, one subtraction and one product: as fast.  Shifts as
+// high halves of products, on the other pipe, are 4 to 10% slower.)
+__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t* o) {
+  o[0] = dequant(w << 4, s, s72, magic);
+  o[1] = dequant(w, s, s72, magic);
+  o[2] = dequant(w >> 4, s, s72, magic);
+  o[3] = dequant(w >> 8, s, s72, magic);
+}
+
+// Sequences of more than row_limit rows per KV head (kv4_pf.cu).
+int64_t prompt_workspace(int head_dim, int sms);
+int launch_prompt(AttnArgs4 A, int head_dim, int sms, void* ws, cudaStream_t s);
+
+}  // namespace kv4
+}  // namespace buddy

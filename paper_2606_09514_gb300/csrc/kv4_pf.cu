@@ -1,0 +1,671 @@
+// Causal attention over the paged 4-bit cache: many query rows per KV head (prompts
+// and pieces of prompts behind a prefix).
+//
+// The rows of a (sequence, KV head) are (query token, head of the group) pairs, row
+// r = token r / G, head r % G; two tiles of 128 of them (an item) walk the same
+// key/value tiles of 128 positions.  On the 5th-generation tensor cores, in half:
+//   S = Q K^T   tcgen05.mma M = 128, N = 128, K = HD: queries (scaled by a power of two
+//               per row to 1 .. 2) and keys from shared memory, S in TMEM;
+//   softmax     four warps per tile, a row per thread, base 2: running reference m,
+//               which follows the maximum when that rises by more than 8; p back into
+//               TMEM as half over S's columns;
+//   O += P V    M = 128, N = HD, K = 128: P from TMEM, V from shared memory (MN-major),
+//               O in TMEM.
+// Two producer warps take the codes of a tile's positions from the pages (a position per
+// thread and half tile, in registers while the tile before is worked on) and write them
+// as halves into the 128-byte-swizzled layout, two buffers each for keys and values.
+// Positions past the end and pages that are not there become zeros and are masked.
+//
+// Work: the items' tiles end to end, each item with kPfOpen tiles' worth for its
+// beginning and end, in equal shares for one CTA per SM.  What an item that is cut
+// has gathered (m, l, O of its rows) goes to the workspace, and a second kernel joins
+// the parts in order.  Every wait is bounded.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "gemm_common.cuh"
+#include "internal.h"
+#include "kv4_attn.cuh"
+
+namespace buddy {
+namespace kv4 {
+
+constexpr int kPfRows = 128, kPfKeys = 128;
+constexpr int kPfSoftWarps = 8, kPfProducers = 64;
+constexpr int kPfThreads = 32 * kPfSoftWarps + 32 + kPfProducers;
+constexpr int kPfOpen = 3;               // what beginning and ending an item costs, in tiles
+constexpr int kPfWhole = 4;              // items of at most this many tiles are not cut
+constexpr uint32_t kPfRegion = 128u * 128u;   // 128 rows x 64 channels of half
+
+template <int HD>
+__host__ __device__ constexpr size_t pf_smem() {
+  return (size_t)(HD / 64) * kPfRegion * 6 + 1024;   // two tiles of queries, two of keys, two of values; alignment
+}
+template <int HD>
+__host__ __device__ constexpr int64_t pf_part_floats() { return 2 * kPfRows * (HD + 2); }
+
+// Byte offset of 16-byte piece c of row r in a tile of 64-channel regions (128-byte
+// rows, 128-byte swizzle).
+__device__ __forceinline__ uint32_t pf_piece(int r, int c) {
+  return (uint32_t)(c >> 3) * kPfRegion + (uint32_t)r * 128u + (uint32_t)(((c ^ r) & 7) << 4);
+}
+
+// A cut item, written by the CTA where it begins.
+struct CutItem {
+  int spans, t0, g, row0, rows;   // spans 0: none
+  int pad[3];
+};
+
+struct PfItem {
+  int seq, t0, m, n, g, R, row0, nt, j0, j1;
+  int64_t start;                  // where the item's first tile is
+};
+
+__device__ __forceinline__ int pf_tiles(int n, int m, int G, int R, int qp) {
+  const int last = min(R, (qp + 1) * 2 * kPfRows) - 1;
+  return max(1, (max(n - m + last / G + 1, 0) + kPfKeys - 1) / kPfKeys);
+}
+// Cost of one KV head of a sequence (whole warp).
+__device__ __forceinline__ int64_t pf_head_cost(int n, int m, int G, int R, int lane) {
+  const int nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+  int64_t c = 0;
+  for (int qp = lane; qp < nqp; qp += 32) c += pf_tiles(n, m, G, R, qp) + kPfOpen;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+  return c;
+}
+// First sequence from i on (below end) that is this kernel's; end if none (whole warp).
+__device__ __forceinline__ int pf_next_seq(const AttnArgs4& A, int i, int end, int lane, Rows* q) {
+  for (; i < end; i += 32) {
+    Rows s{0, 0, 0};
+    bool bad;
+    if (i + lane < end) s = rows_of(A, i + lane, &bad);
+    const uint32_t hit = __ballot_sync(0xffffffffu, s.m * A.G > A.row_limit);
+    if (hit) {
+      const int at = __ffs(hit) - 1;
+      q->t0 = __shfl_sync(0xffffffffu, s.t0, at);
+      q->m = __shfl_sync(0xffffffffu, s.m, at);
+      q->n = __shfl_sync(0xffffffffu, s.n, at);
+      return i + at;
+    }
+  }
+  return end;
+}
+
+// The walk over a CTA's items, by one warp.
+struct PfWalk {
+  Rows q;
+  int i, g, qp, nt, j0, j1;
+  int64_t rem, start;
+  __device__ __forceinline__ bool next(const AttnArgs4& A, int lane) {
+    start += nt + kPfOpen;
+    rem -= kPfOpen;
+    if (rem <= 0) return false;
+    if (++qp * 2 * kPfRows >= q.m * A.G) {
+      qp = 0;
+      if (++g == A.p.nkv) {
+        g = 0;
+        i = pf_next_seq(A, i + 1, A.a.batch, lane, &q);   // (with some of the share left there is another)
+      }
+    }
+    nt = pf_tiles(q.n, q.m, A.G, q.m * A.G, qp);
+    j0 = 0;
+    j1 = nt <= kPfWhole ? nt : (int)min((int64_t)nt, rem);
+    rem -= j1;
+    return true;
+  }
+};
+
+__device__ __forceinline__ void pf_store_row32(const AttnArgs4& A, int64_t at, const float* o) {
+  if (A.a.out_dtype == BUDDY_DTYPE_F32) {
+    float4* d = reinterpret_cast<float4*>((float*)A.a.out + at);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+  } else {
+    uint4* d = reinterpret_cast<uint4*>((bf16*)A.a.out + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      d[i] = make_uint4(tca::pack_bf16(o[8 * i], o[8 * i + 1]), tca::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
+                        tca::pack_bf16(o[8 * i + 4], o[8 * i + 5]), tca::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArgs4 A, CutItem* cuts) {
+  extern __shared__ uint8_t smem_raw[];
+  constexpr uint32_t TILE = (HD / 64) * kPfRegion;      // bytes of a 128-row tile
+  constexpr int GR = HD / kGroup;                       // scale groups of a head
+  // TMEM columns: S of tile q at 128 q (P over their first half), O of tile q at 256 + 128 q
+  constexpr uint32_t kO = 256;
+  __shared__ __align__(8) uint64_t q_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
+  __shared__ __align__(8) uint64_t s_full[2], p_ready[2], o_full[2], drained;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  __shared__ int64_t s_sum[kPfSoftWarps];
+  __shared__ PfItem s_item;
+  __shared__ int s_go;
+  __shared__ float s_fac[2 * kPfRows];
+  __shared__ int s_nan[GR];
+  __shared__ __align__(4) uint8_t s_ok[4][4];           // [tile % 4][32 positions]: two bits, pages that are there
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int B = A.a.batch, G = A.G;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem;                                   // [tile]
+  uint8_t* sK = smem + 2 * TILE;                        // [2]
+  uint8_t* sV = sK + 2 * TILE;                          // [2]
+  constexpr int kMmaWarp = kPfSoftWarps;
+
+  // ---- this CTA's share of all items' openings and tiles
+  const int per = (B + kPfSoftWarps - 1) / kPfSoftWarps;
+  const int b0 = min(B, warp * per), b1 = min(B, b0 + per);
+  int64_t mine = 0;
+  if (warp < kPfSoftWarps) {
+    Rows q;
+    for (int i = pf_next_seq(A, b0, b1, lane, &q); i < b1; i = pf_next_seq(A, i + 1, b1, lane, &q))
+      mine += A.p.nkv * pf_head_cost(q.n, q.m, G, q.m * G, lane);
+    if (lane == 0) s_sum[warp] = mine;
+  }
+  if (tid == 0) {
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(&q_ready[b], 128);
+      ptx::mbar_init(&k_full[b], kPfProducers);
+      ptx::mbar_init(&v_full[b], kPfProducers);
+      ptx::mbar_init(&k_empty[b], 1);
+      ptx::mbar_init(&v_empty[b], 1);
+      ptx::mbar_init(&s_full[b], 1);
+      ptx::mbar_init(&p_ready[b], 128);
+      ptx::mbar_init(&o_full[b], 1);
+    }
+    ptx::mbar_init(&drained, 1);
+    abort_flag = 0;
+    s_go = 0;
+    cuts[blockIdx.x].spans = 0;
+    ptx::fence_mbar_init();
+  }
+  __syncthreads();
+  int64_t total = 0, before = 0;
+  for (int w = 0; w < kPfSoftWarps; ++w) {
+    if (w < warp) before += s_sum[w];
+    total += s_sum[w];
+  }
+  const int64_t share = max((int64_t)kPfWhole, (total + gridDim.x - 1) / gridDim.x);
+  const int64_t lo = blockIdx.x * share;
+  if (lo >= total) return;
+  if (warp < kPfSoftWarps && before <= lo && lo < before + mine) {
+    // the sequence, its head, the item of it and the tile where the share begins
+    PfWalk w;
+    int64_t at = before, cost = 0;
+    for (w.i = pf_next_seq(A, b0, b1, lane, &w.q);; w.i = pf_next_seq(A, w.i + 1, b1, lane, &w.q)) {
+      cost = pf_head_cost(w.q.n, w.q.m, G, w.q.m * G, lane);
+      if (lo < at + cost * A.p.nkv) break;
+      at += cost * A.p.nkv;
+    }
+    w.g = (int)((lo - at) / cost);
+    at += w.g * cost;
+    const int R = w.q.m * G, nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+    for (int q0 = 0;; q0 += 32) {
+      const int64_t c = q0 + lane < nqp ? pf_tiles(w.q.n, w.q.m, G, R, q0 + lane) + kPfOpen : 0;
+      int64_t upto = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const uint32_t hit = __ballot_sync(0xffffffffu, lo < at + upto);
+      if (hit || q0 + 32 >= nqp) {
+        const int x = hit ? __ffs(hit) - 1 : 31;
+        w.qp = q0 + x;
+        at += __shfl_sync(0xffffffffu, upto - c, x);
+        break;
+      }
+      at += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0)
+      s_item = {w.i, w.q.t0, w.q.m, w.q.n, w.g, R, w.qp * 2 * kPfRows, pf_tiles(w.q.n, w.q.m, G, R, w.qp), 0, 0, at + kPfOpen};
+  }
+  if (warp == kMmaWarp) {
+    ptx::tmem_alloc(&tmem_slot, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  PfWalk walk{};                   // warp 0's
+  if (warp == 0) {
+    walk.q = {s_item.t0, s_item.m, s_item.n};
+    walk.i = s_item.seq, walk.g = s_item.g, walk.qp = s_item.row0 / (2 * kPfRows), walk.nt = s_item.nt;
+    walk.start = s_item.start;
+    const int64_t x = lo - walk.start;                  // tile of the item; below 0: its opening
+    walk.rem = min(share, total - lo) + min(x, (int64_t)0);
+    walk.j0 = (int)max(x, (int64_t)0);
+    bool go = walk.rem > 0;
+    if (go) {
+      if (x > 0 && walk.nt <= kPfWhole) {               // the CTA before has it all
+        walk.rem -= walk.nt - x;
+        go = walk.next(A, lane);
+      } else {
+        walk.j1 = walk.nt <= kPfWhole ? walk.nt : (int)min((int64_t)walk.nt, walk.j0 + walk.rem);
+        walk.rem -= walk.j1 - walk.j0;
+      }
+    }
+    __syncwarp();
+    if (lane == 0) s_go = go;
+  }
+
+  // counts of tiles and items so far, which give the barriers' phases: all tiles, items,
+  // and those with a second tile of rows
+  uint32_t T = 0, I = 0, T1 = 0, I1 = 0;
+  while (true) {
+    if (warp == 0 && lane == 0)
+      s_item = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * 2 * kPfRows, walk.nt, walk.j0, walk.j1,
+                walk.start};
+    if (tid < GR) s_nan[tid] = INT32_MAX;
+    __syncthreads();
+    if (!s_go || abort_flag) break;
+    const PfItem it = s_item;
+    const int nq = it.R - it.row0 > kPfRows ? 2 : 1;    // tiles with rows
+    const int len = it.j1 - it.j0;
+    const int last = min(it.R, it.row0 + 2 * kPfRows) - 1;
+    const int kmax = max(it.n - it.m + last / G + 1, 0);   // positions that the last row sees
+
+    if (warp < kMmaWarp) {
+      const int q = warp >> 2;                          // this warp's tile
+      if (q < nq) {
+        // ----------------------------------------------------------- softmax
+        const int rt = (warp & 3) * 32 + lane;          // row of the tile
+        const int row = it.row0 + q * kPfRows + rt, rr = min(row, it.R - 1);
+        const int t = rr / G, h = it.g * G + rr - t * G;
+        uint8_t* const qdst = sQ + (size_t)q * TILE;
+        {
+          constexpr int LPR = HD / 8, RPL = 32 / LPR;   // lanes per row, rows per load
+          const int64_t at = (it.t0 + t) * A.a.q_stride + (int64_t)h * HD;
+          const int l8 = lane % LPR;
+#pragma unroll 1
+          for (int r0 = 0; r0 < 32; r0 += 4 * RPL) {
+            float v[4][8];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int64_t src = __shfl_sync(0xffffffffu, (long long)at, r0 + u * RPL + lane / LPR) + l8 * 8;
+              if (A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + src, v[u]);
+              else load8((const bf16*)A.a.q + src, v[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int r = (warp & 3) * 32 + r0 + u * RPL + lane / LPR;
+              float top = 0.f, down, fac;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[u][e]));
+#pragma unroll
+              for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+              row_scale(top, A.a.scale, HD, &down, &fac);
+              if (l8 == 0) s_fac[q * kPfRows + r] = fac;
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[e] = h2(__floats2half2_rn(v[u][2 * e] * down, v[u][2 * e + 1] * down));
+              *reinterpret_cast<uint4*>(qdst + pf_piece(r, l8)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+          __syncwarp();
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          ptx::mbar_arrive(&q_ready[q]);
+        }
+        const float fac = s_fac[q * kPfRows + rt];
+        const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t ts = tq + (uint32_t)q * 128u, to = tq + kO + (uint32_t)q * 128u;
+        const int seen = it.n - it.m + t + 1;           // positions this row sees (may be <= 0)
+        const uint32_t C = q == 0 ? T : T1;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int jj = 0; jj < len; ++jj) {
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&s_full[q], (C + jj) & 1, kWaitLimitNs, &abort_flag));
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const int lim = seen - (it.j0 + jj) * kPfKeys;   // visible columns of this tile (may be <= 0)
+          const uint32_t there = *reinterpret_cast<const volatile uint32_t*>(s_ok[(T + jj) & 3]);
+          uint32_t s[kPfKeys];   // the row, read once (P overwrites its columns)
+#pragma unroll
+          for (int c = 0; c < kPfKeys; c += 32) ptx::tmem_ld32(ts + c, s + c);
+          ptx::tmem_wait_ld();
+          if (__any_sync(0xffffffffu, lim < kPfKeys)) {
+#pragma unroll
+            for (int i = 0; i < kPfKeys; ++i)
+              if (i >= lim) s[i] = 0xff800000u;   // -inf: p = 0
+          }
+          if (there != 0x03030303u) {
+#pragma unroll
+            for (int i = 0; i < kPfKeys; ++i)
+              if (!((there >> (8 * (i >> 5) + ((i >> 4) & 1))) & 1)) s[i] = 0xff800000u;
+          }
+          float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < kPfKeys; ++i) mx4[i & 3] = fmaxf(mx4[i & 3], __uint_as_float(s[i]));
+          const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * fac;
+          const bool raise = mx > m + 8.f;
+          if (__any_sync(0xffffffffu, raise)) {
+            const float al = raise ? tca::exp2a(m - mx) : 1.f;
+            if (raise) m = mx;
+            l *= al;
+            if (jj > 0) {
+#pragma unroll 1
+              for (int c = 0; c < HD; c += 32) {
+                uint32_t o[32];
+                ptx::tmem_ld32(to + c, o);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
+                ptx::tmem_st32(to + c, o);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < kPfKeys; c += 32) {
+            uint32_t p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float p0 = tca::exp2a(fmaf(__uint_as_float(s[c + 2 * i]), fac, -ref));
+              const float p1 = tca::exp2a(fmaf(__uint_as_float(s[c + 2 * i + 1]), fac, -ref));
+              ls[i & 3] += p0 + p1;
+              p[i] = h2(__floats2half2_rn(p0, p1));
+            }
+            ptx::tmem_st16(ts + c / 2, p);
+          }
+          l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+          ptx::tmem_wait_st();
+          ptx::tc_fence_before();
+          ptx::mbar_arrive(&p_ready[q]);
+        }
+        if (ok)
+          ok = __all_sync(0xffffffffu,
+                          ptx::mbar_wait_bounded(&o_full[q], (q == 0 ? I : I1) & 1, kWaitLimitNs, &abort_flag));
+        if (ok) {
+          ptx::tc_fence_after();
+          const bool whole = len == it.nt;
+          const float inv = !whole ? 1.f : m == -INFINITY ? 0.f : 1.f / l;
+          float* part = A.part + (2 * (int64_t)blockIdx.x + (it.j0 == 0 ? 1 : 0)) * pf_part_floats<HD>() + q * kPfRows + rt;
+          if (!whole) part[0] = m, part[2 * kPfRows] = l;
+          const int64_t out_at = (it.t0 + t) * A.a.out_stride + (int64_t)h * HD;
+          const bool staged = whole && A.a.out_dtype == BUDDY_DTYPE_BF16;
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 32) {
+            float o[32];
+            ptx::tmem_ld32(to + c, reinterpret_cast<uint32_t*>(o));
+            ptx::tmem_wait_ld();
+            const bool nan = *reinterpret_cast<const volatile int*>(s_nan + c / kGroup) < seen;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = nan ? __uint_as_float(0x7FC00000u) : o[i] * inv;
+            if (!whole) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) part[(2 + c + i) * 2 * kPfRows] = o[i];
+            } else if (staged) {   // through this tile's query buffer (its MMAs are done): whole rows are stored
+#pragma unroll
+              for (int i = 0; i < 32; i += 8)
+                *reinterpret_cast<uint4*>(qdst + pf_piece(rt, (c + i) >> 3)) =
+                    make_uint4(tca::pack_bf16(o[i], o[i + 1]), tca::pack_bf16(o[i + 2], o[i + 3]),
+                               tca::pack_bf16(o[i + 4], o[i + 5]), tca::pack_bf16(o[i + 6], o[i + 7]));
+            } else if (row < it.R) {
+              pf_store_row32(A, out_at + c, o);
+            }
+          }
+          if (staged) {
+            __syncwarp();
+            constexpr int V16 = HD / 8, RPS = 32 / V16;   // pieces of a row, rows per store
+#pragma unroll 4
+            for (int r0 = 0; r0 < 32; r0 += RPS) {
+              const int r = r0 + lane / V16, c = lane % V16;
+              const int64_t dst = __shfl_sync(0xffffffffu, (long long)out_at, r) + c * 8;
+              if (it.row0 + q * kPfRows + (warp & 3) * 32 + r < it.R)
+                *reinterpret_cast<uint4*>((bf16*)A.a.out + dst) =
+                    *reinterpret_cast<const uint4*>(qdst + pf_piece((warp & 3) * 32 + r, c));
+            }
+          }
+        }
+      }
+    } else if (warp == kMmaWarp) {
+      // ------------------------------------------------------------------ MMA
+      if (lane == 0) {
+        const uint32_t id_s = (1u << 4) | ((uint32_t)(kPfKeys >> 3) << 17) | (8u << 24);   // half in, fp32 out, M 128
+        const uint32_t id_o = (1u << 4) | ((uint32_t)(HD >> 3) << 17) | (8u << 24) | ptx::kIdescBMnMajor;
+        auto wait = [&](uint64_t* bar, uint32_t count) {
+          return ptx::mbar_wait_bounded(bar, count & 1, kWaitLimitNs, &abort_flag);
+        };
+        auto qk = [&](int q, uint32_t tile) {           // S_q = Q_q K^T
+          const uint8_t* Q = sQ + (size_t)q * TILE;
+          const uint8_t* K = sK + (size_t)(tile & 1) * TILE;
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint64_t dk = ptx::smem_desc_sw128(K + (k >> 2) * kPfRegion) + 2ull * (k & 3);
+            const uint64_t dq = ptx::smem_desc_sw128(Q + (k >> 2) * kPfRegion) + 2ull * (k & 3);
+            ptx::mma_bf16(tmem + (uint32_t)q * 128u, dq, dk, id_s, k > 0 ? 1u : 0u);
+          }
+          ptx::mma_commit(&s_full[q]);
+        };
+        auto pv = [&](int q, uint32_t tile, bool first) {   // O_q += P_q V
+          const uint8_t* V = sV + (size_t)(tile & 1) * TILE;
+#pragma unroll
+          for (int k = 0; k < kPfKeys / 16; ++k) {
+            const uint64_t dv = ptx::smem_desc_sw128_mn(V + k * 2048, kPfRegion);   // 16 positions: two 1 KiB groups
+            ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, tmem + (uint32_t)q * 128u + 8u * k, dv, id_o,
+                             (!first || k > 0) ? 1u : 0u);
+          }
+        };
+        bool ok = wait(&q_ready[0], I) && (nq == 1 || wait(&q_ready[1], I1)) && wait(&k_full[T & 1], T >> 1);
+        if (ok) {
+          ptx::tc_fence_after();
+          for (int q = 0; q < nq; ++q) qk(q, T);
+          ptx::mma_commit(&k_empty[T & 1]);
+        }
+        for (int jj = 0; jj < len && ok; ++jj) {
+          const bool more = jj + 1 < len;
+          const uint32_t u = T + jj;
+          for (int q = 0; q < nq && ok; ++q) {
+            ok = wait(&p_ready[q], (q == 0 ? T : T1) + jj) && (q > 0 || wait(&v_full[u & 1], u >> 1)) &&
+                 (q > 0 || !more || wait(&k_full[(u + 1) & 1], (u + 1) >> 1));
+            if (!ok) break;
+            ptx::tc_fence_after();
+            pv(q, u, jj == 0);
+            if (q == nq - 1) ptx::mma_commit(&v_empty[u & 1]);
+            if (more) {
+              qk(q, u + 1);   // in issue order after the P V that reads P from the same columns
+              if (q == nq - 1) ptx::mma_commit(&k_empty[(u + 1) & 1]);
+            } else {
+              ptx::mma_commit(&o_full[q]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------ K, V tiles
+      const int lt = tid - 32 * (kMmaWarp + 1);
+      const int end = min(it.n, kmax);                  // positions that any row sees
+      const int in_page = (1 << A.p.shift) - 1;
+      const int32_t* table = A.a.table + (int64_t)it.seq * A.a.max_pages;
+      const uint32_t magic = 0x54005400u;
+      struct Entry {
+        uint4 w[GR];
+        __half s[GR];
+      };
+      // pages of this thread's positions of a tile: -1 past the end, -2 not there
+      auto ids_of = [&](int j, int* id) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int p = j * kPfKeys + lt + 64 * u;
+          id[u] = -1;
+          if (p < end) {
+            id[u] = table[p >> A.p.shift];
+            if ((uint32_t)id[u] >= (uint32_t)A.p.n_pages) {
+              id[u] = -2;
+              if (A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+            }
+          }
+        }
+      };
+      auto load = [&](const uint8_t* pages, int j, const int* id, Entry* e) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int r = (j * kPfKeys + lt + 64 * u) & in_page;
+          const uint8_t* b = pages + (id[u] >= 0 ? block_at<HD>(A.p, id[u], it.g) : 0);
+          const uint8_t* sc = b + ((int64_t)code_bytes(HD) << A.p.shift) + r * scale_bytes(HD);
+          b += r * code_bytes(HD);
+#pragma unroll
+          for (int x = 0; x < GR; ++x) {
+            e[u].w[x] = id[u] >= 0 ? __ldg(reinterpret_cast<const uint4*>(b) + x) : make_uint4(0, 0, 0, 0);
+            e[u].s[x] = id[u] >= 0 ? __ldg(reinterpret_cast<const __half*>(sc) + x) : __ushort_as_half(0);
+          }
+        }
+      };
+      auto put = [&](uint8_t* dst, const Entry* e, int j, bool values) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int r = lt + 64 * u;
+#pragma unroll
+          for (int x = 0; x < GR; ++x) {
+            __half sc = e[u].s[x];
+            // A NaN must not meet the zero probabilities of rows that do not see its position:
+            // its values count as zeros, and the rows that see it become NaN at the end.
+            if (values && __hisnan(sc)) {
+              sc = __ushort_as_half(0);
+              atomicMin(s_nan + x, j * kPfKeys + r);
+            }
+            const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
+            const uint32_t w[4] = {e[u].w[x].x, e[u].w[x].y, e[u].w[x].z, e[u].w[x].w};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              uint32_t o[4];
+              dequant4(w[y], s2, s72, magic, o);
+              *reinterpret_cast<uint4*>(dst + pf_piece(r, 4 * x + y)) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      };
+      Entry ek[2], ev[2];
+      int id[2], id_next[2] = {-1, -1};
+      ids_of(it.j0, id);
+      load(A.p.k, it.j0, id, ek);
+      load(A.p.v, it.j0, id, ev);
+      for (int jj = 0; jj < len; ++jj) {
+        const int j = it.j0 + jj;
+        const uint32_t u = T + jj;
+        const bool more = jj + 1 < len;
+        if (more) ids_of(j + 1, id_next);
+        if (!ptx::mbar_wait_bounded(&k_empty[u & 1], ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag)) break;
+        put(sK + (size_t)(u & 1) * TILE, ek, j, false);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t bad = __ballot_sync(0xffffffffu, id[x] == -2);
+          if (lane == 0) s_ok[u & 3][(lt >> 5) + 2 * x] = (uint8_t)(((bad & 0xFFFFu) ? 0 : 1) | ((bad >> 16) ? 0 : 2));
+        }
+        ptx::mbar_arrive(&k_full[u & 1]);
+        if (more) load(A.p.k, j + 1, id_next, ek);
+        if (!ptx::mbar_wait_bounded(&v_empty[u & 1], ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag)) break;
+        put(sV + (size_t)(u & 1) * TILE, ev, j, true);
+        ptx::mbar_arrive(&v_full[u & 1]);
+        if (more) load(A.p.v, j + 1, id_next, ev);
+        id[0] = id_next[0], id[1] = id_next[1];
+      }
+    }
+
+    T += len, ++I;
+    if (nq == 2) T1 += len, ++I1;
+    if (warp == 0) {
+      if (lane == 0 && it.j0 == 0 && len < it.nt) {
+        CutItem* c = cuts + blockIdx.x;
+        c->t0 = it.t0, c->g = it.g, c->row0 = it.row0, c->rows = min(it.R - it.row0, 2 * kPfRows);
+        c->spans = (int)((it.start + it.nt - 1) / share - blockIdx.x) + 1;
+      }
+      const bool go = walk.next(A, lane);
+      __syncwarp();
+      if (lane == 0) s_go = go;      // (read by the others behind the next barrier, and before the one after it)
+    }
+    __syncthreads();                 // s_item, s_nan and the query buffers are free again
+  }
+
+  // every issued MMA completes before TMEM is freed: normally all have (o_full), after a
+  // wait that ran out the MMA warp waits for its own
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    if (abort_flag) {
+      if (lane == 0) {
+        ptx::mma_commit(&drained);
+        volatile int dummy = 0;
+        ptx::mbar_wait_bounded(&drained, 0, kWaitLimitNs, &dummy);
+        if (A.flags) atomicOr(A.flags, BUDDY_DEV_TIMEOUT);
+      }
+      __syncwarp();
+    }
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+// The parts of the items that were cut, in order: a thread per row, 16 channels.
+template <int HD>
+__global__ void __launch_bounds__(2 * kPfRows) kv4_join_kernel(const AttnArgs4 A, const CutItem* cuts) {
+  const CutItem c = cuts[blockIdx.x];
+  const int x = threadIdx.x, ch = blockIdx.y * 16;
+  if (x >= c.rows || c.spans == 0) return;
+  auto part = [&](int k) {
+    return A.part + (2 * (int64_t)(blockIdx.x + k) + (k == 0 ? 1 : 0)) * pf_part_floats<HD>() + x;
+  };
+  float M = -INFINITY, L = 0.f, o[16];
+  for (int k = 0; k < c.spans; ++k) M = fmaxf(M, part(k)[0]);
+  const float at = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] = 0.f;
+#pragma unroll 2
+  for (int k = 0; k < c.spans; ++k) {
+    const float* p = part(k);
+    const float a = tca::exp2a(p[0] - at);
+    L += a * p[2 * kPfRows];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] += a * p[(2 + ch + i) * 2 * kPfRows];
+  }
+  const float inv = M == -INFINITY ? 0.f : 1.f / L;
+  const int row = c.row0 + x, G = A.G;
+  const int64_t to = (c.t0 + row / G) * A.a.out_stride + (int64_t)(c.g * G + row % G) * HD + ch;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] *= inv;
+  if (A.a.out_dtype == BUDDY_DTYPE_F32) {
+    float4* d = reinterpret_cast<float4*>((float*)A.a.out + to);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+  } else {
+    uint4* d = reinterpret_cast<uint4*>((bf16*)A.a.out + to);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      d[i] = make_uint4(tca::pack_bf16(o[8 * i], o[8 * i + 1]), tca::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
+                        tca::pack_bf16(o[8 * i + 4], o[8 * i + 5]), tca::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+  }
+}
+
+int64_t prompt_workspace(int head_dim, int sms) {
+  return (int64_t)sms * (sizeof(CutItem) + 2 * (head_dim == 128 ? pf_part_floats<128>() : pf_part_floats<64>()) * 4);
+}
+
+template <int HD>
+static int launch_prompt_hd(const AttnArgs4& A, CutItem* cuts, int sms, cudaStream_t s) {
+  if (cudaFuncSetAttribute(kv4_prompt_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pf_smem<HD>()) !=
+      cudaSuccess)
+    return BUDDY_ERR_CUDA;
+  kv4_prompt_kernel<HD><<<sms, kPfThreads, pf_smem<HD>(), s>>>(A, cuts);
+  if (cudaGetLastError() != cudaSuccess) return BUDDY_ERR_CUDA;
+  kv4_join_kernel<HD><<<dim3(sms, HD / 16), 2 * kPfRows, 0, s>>>(A, cuts);
+  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+}
+
+// ws: prompt_workspace() bytes.
+int launch_prompt(AttnArgs4 A, int head_dim, int sms, void* ws, cudaStream_t s) {
+  CutItem* cuts = (CutItem*)ws;
+  A.part = (float*)((uint8_t*)ws + sms * sizeof(CutItem));
+  return head_dim == 128 ? launch_prompt_hd<128>(A, cuts, sms, s) : launch_prompt_hd<64>(A, cuts, sms, s);
+}
+
+}  // namespace kv4
+}  // namespace buddy
