@@ -11,8 +11,8 @@
 //               TMEM as half over S's columns;
 //   O += P V    M = 128, N = HD, K = 128: P from TMEM, V from shared memory (MN-major),
 //               O in TMEM.
-// Two producer warps take the codes of a tile's positions from the pages (a position per
-// thread and half tile, in registers while the tile before is worked on) and write them
+// Four producer warps take the codes of a tile's positions from the pages (a position per
+// thread, in registers while the tile before is worked on) and write them
 // as halves into the 128-byte-swizzled layout, two buffers each for keys and values.
 // Positions past the end and pages that are not there become zeros and are masked.
 //
@@ -32,8 +32,11 @@ namespace buddy {
 namespace kv4 {
 
 constexpr int kPfRows = 128, kPfKeys = 128;
-constexpr int kPfSoftWarps = 8, kPfProducers = 64;
-constexpr int kPfThreads = 32 * kPfSoftWarps + 32 + kPfProducers;
+constexpr int kPfSoftWarps = 8, kPfProducers = 128;
+constexpr int kPfThreads = 512;          // four warpgroups: two of softmax, producers, the MMA warp's
+// Registers: 128 a thread at launch (65,536 in all), then by setmaxnreg 2 x 128 x 176 +
+// 128 x 104 + 128 x 56 = 65,536.
+constexpr int kPfRegsSoft = 176, kPfRegsProduce = 104, kPfRegsMma = 56;
 constexpr int kPfOpen = 3;               // what beginning and ending an item costs, in tiles
 constexpr int kPfWhole = 4;              // items of at most this many tiles are not cut
 constexpr uint32_t kPfRegion = 128u * 128u;   // 128 rows x 64 channels of half
@@ -131,6 +134,11 @@ __device__ __forceinline__ void pf_store_row32(const AttnArgs4& A, int64_t at, c
   }
 }
 
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 template <int HD>
 __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArgs4 A, CutItem* cuts) {
   extern __shared__ uint8_t smem_raw[];
@@ -155,7 +163,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   uint8_t* sQ = smem;                                   // [tile]
   uint8_t* sK = smem + 2 * TILE;                        // [2]
   uint8_t* sV = sK + 2 * TILE;                          // [2]
-  constexpr int kMmaWarp = kPfSoftWarps;
+  constexpr int kMmaWarp = kPfSoftWarps + kPfProducers / 32;
 
   // ---- this CTA's share of all items' openings and tiles
   const int per = (B + kPfSoftWarps - 1) / kPfSoftWarps;
@@ -234,45 +242,35 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   ptx::tc_fence_after();
   const uint32_t tmem = tmem_slot;
 
-  PfWalk walk{};                   // warp 0's
-  if (warp == 0) {
-    walk.q = {s_item.t0, s_item.m, s_item.n};
-    walk.i = s_item.seq, walk.g = s_item.g, walk.qp = s_item.row0 / (2 * kPfRows), walk.nt = s_item.nt;
-    walk.start = s_item.start;
-    const int64_t x = lo - walk.start;                  // tile of the item; below 0: its opening
-    walk.rem = min(share, total - lo) + min(x, (int64_t)0);
-    walk.j0 = (int)max(x, (int64_t)0);
-    bool go = walk.rem > 0;
-    if (go) {
-      if (x > 0 && walk.nt <= kPfWhole) {               // the CTA before has it all
-        walk.rem -= walk.nt - x;
-        go = walk.next(A, lane);
-      } else {
-        walk.j1 = walk.nt <= kPfWhole ? walk.nt : (int)min((int64_t)walk.nt, walk.j0 + walk.rem);
-        walk.rem -= walk.j1 - walk.j0;
-      }
-    }
-    __syncwarp();
-    if (lane == 0) s_go = go;
-  }
-
-  // counts of tiles and items so far, which give the barriers' phases: all tiles, items,
-  // and those with a second tile of rows
+  // Every role walks the items: between two barriers s_item is one item's, and the counts
+  // of tiles and items so far give the mbarriers' phases: of all tiles and items, and of
+  // those with a second tile of rows.
   uint32_t T = 0, I = 0, T1 = 0, I1 = 0;
-  while (true) {
-    if (warp == 0 && lane == 0)
-      s_item = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * 2 * kPfRows, walk.nt, walk.j0, walk.j1,
-                walk.start};
-    if (tid < GR) s_nan[tid] = INT32_MAX;
+  PfItem it;
+  int nq = 1, len = 0, kmax = 0;
+  auto next_item = [&]() {
     __syncthreads();
-    if (!s_go || abort_flag) break;
-    const PfItem it = s_item;
-    const int nq = it.R - it.row0 > kPfRows ? 2 : 1;    // tiles with rows
-    const int len = it.j1 - it.j0;
+    if (!s_go || abort_flag) return false;
+    it = s_item;
+    nq = it.R - it.row0 > kPfRows ? 2 : 1;              // tiles with rows
+    len = it.j1 - it.j0;
     const int last = min(it.R, it.row0 + 2 * kPfRows) - 1;
-    const int kmax = max(it.n - it.m + last / G + 1, 0);   // positions that the last row sees
+    kmax = max(it.n - it.m + last / G + 1, 0);          // positions that the last row sees
+    return true;
+  };
+  auto end_item = [&]() {
+    T += len, ++I;
+    if (nq == 2) T1 += len, ++I1;
+    __syncthreads();                                    // s_item, s_nan and the query buffers are free again
+  };
 
-    if (warp < kMmaWarp) {
+  // (a warpgroup takes or gives registers in one instruction; warps 13 to 15 read the first
+  // s_item before it is written anew)
+  if (warp >= kMmaWarp) regs_down<kPfRegsMma>();
+  if (warp < kPfSoftWarps) {
+    regs_up<kPfRegsSoft>();
+    __syncthreads();
+    while (next_item()) {
       const int q = warp >> 2;                          // this warp's tile
       if (q < nq) {
         // ----------------------------------------------------------- softmax
@@ -426,8 +424,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           }
         }
       }
-    } else if (warp == kMmaWarp) {
-      // ------------------------------------------------------------------ MMA
+      end_item();
+    }
+  } else if (warp == kMmaWarp) {
+    // -------------------------------------------------------------------- MMA
+    __syncthreads();
+    while (next_item()) {
       if (lane == 0) {
         const uint32_t id_s = (1u << 4) | ((uint32_t)(kPfKeys >> 3) << 17) | (8u << 24);   // half in, fp32 out, M 128
         const uint32_t id_o = (1u << 4) | ((uint32_t)(HD >> 3) << 17) | (8u << 24) | ptx::kIdescBMnMajor;
@@ -480,9 +482,54 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         }
       }
       __syncwarp();
-    } else {
-      // ------------------------------------------------------------ K, V tiles
-      const int lt = tid - 32 * (kMmaWarp + 1);
+      end_item();
+    }
+  } else if (warp > kMmaWarp) {
+    // ------------------------------------------------- the walk over the items
+    PfWalk walk{};
+    walk.q = {s_item.t0, s_item.m, s_item.n};
+    walk.i = s_item.seq, walk.g = s_item.g, walk.qp = s_item.row0 / (2 * kPfRows), walk.nt = s_item.nt;
+    walk.start = s_item.start;
+    const int64_t x = lo - walk.start;                  // tile of the item; below 0: its opening
+    walk.rem = min(share, total - lo) + min(x, (int64_t)0);
+    walk.j0 = (int)max(x, (int64_t)0);
+    bool go = walk.rem > 0;
+    if (go) {
+      if (x > 0 && walk.nt <= kPfWhole) {               // the CTA before has it all
+        walk.rem -= walk.nt - x;
+        go = walk.next(A, lane);
+      } else {
+        walk.j1 = walk.nt <= kPfWhole ? walk.nt : (int)min((int64_t)walk.nt, walk.j0 + walk.rem);
+        walk.rem -= walk.j1 - walk.j0;
+      }
+    }
+    const bool mine = warp == kMmaWarp + 1;             // (the other two warps follow)
+    __syncthreads();                                    // everyone has read the first s_item
+    while (true) {
+      if (mine) {
+        if (lane == 0) {
+          s_item = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * 2 * kPfRows, walk.nt, walk.j0,
+                    walk.j1, walk.start};
+          s_go = go;
+          if (go && walk.j0 == 0 && walk.j1 < walk.nt) {
+            CutItem* c = cuts + blockIdx.x;
+            c->t0 = walk.q.t0, c->g = walk.g, c->row0 = walk.qp * 2 * kPfRows;
+            c->rows = min(walk.q.m * G - c->row0, 2 * kPfRows);
+            c->spans = (int)((walk.start + walk.nt - 1) / share - blockIdx.x) + 1;
+          }
+        }
+        if (lane < GR) s_nan[lane] = INT32_MAX;
+      }
+      if (!next_item()) break;
+      if (mine) go = walk.next(A, lane);
+      end_item();
+    }
+  } else {
+    // -------------------------------------------------------------- K, V tiles
+    regs_down<kPfRegsProduce>();
+    const int lt = tid - 32 * kPfSoftWarps;             // this thread's position of a tile
+    __syncthreads();
+    while (next_item()) {
       const int end = min(it.n, kmax);                  // positions that any row sees
       const int in_page = (1 << A.p.shift) - 1;
       const int32_t* table = A.a.table + (int64_t)it.seq * A.a.max_pages;
@@ -491,100 +538,71 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         uint4 w[GR];
         __half s[GR];
       };
-      // pages of this thread's positions of a tile: -1 past the end, -2 not there
-      auto ids_of = [&](int j, int* id) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int p = j * kPfKeys + lt + 64 * u;
-          id[u] = -1;
-          if (p < end) {
-            id[u] = table[p >> A.p.shift];
-            if ((uint32_t)id[u] >= (uint32_t)A.p.n_pages) {
-              id[u] = -2;
-              if (A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
-            }
-          }
-        }
+      // page of this thread's position of a tile: -1 past the end, -2 not there
+      auto id_of = [&](int j) {
+        const int p = j * kPfKeys + lt;
+        if (p >= end) return -1;
+        const int id = table[p >> A.p.shift];
+        if ((uint32_t)id < (uint32_t)A.p.n_pages) return id;
+        if (A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+        return -2;
       };
-      auto load = [&](const uint8_t* pages, int j, const int* id, Entry* e) {
+      auto load = [&](const uint8_t* pages, int j, int id, Entry* e) {
+        const int r = (j * kPfKeys + lt) & in_page;
+        const uint8_t* b = pages + (id >= 0 ? block_at<HD>(A.p, id, it.g) : 0);
+        const uint8_t* sc = b + ((int64_t)code_bytes(HD) << A.p.shift) + r * scale_bytes(HD);
+        b += r * code_bytes(HD);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int r = (j * kPfKeys + lt + 64 * u) & in_page;
-          const uint8_t* b = pages + (id[u] >= 0 ? block_at<HD>(A.p, id[u], it.g) : 0);
-          const uint8_t* sc = b + ((int64_t)code_bytes(HD) << A.p.shift) + r * scale_bytes(HD);
-          b += r * code_bytes(HD);
-#pragma unroll
-          for (int x = 0; x < GR; ++x) {
-            e[u].w[x] = id[u] >= 0 ? __ldg(reinterpret_cast<const uint4*>(b) + x) : make_uint4(0, 0, 0, 0);
-            e[u].s[x] = id[u] >= 0 ? __ldg(reinterpret_cast<const __half*>(sc) + x) : __ushort_as_half(0);
-          }
+        for (int x = 0; x < GR; ++x) {
+          e->w[x] = id >= 0 ? __ldg(reinterpret_cast<const uint4*>(b) + x) : make_uint4(0, 0, 0, 0);
+          e->s[x] = id >= 0 ? __ldg(reinterpret_cast<const __half*>(sc) + x) : __ushort_as_half(0);
         }
       };
       auto put = [&](uint8_t* dst, const Entry* e, int j, bool values) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int r = lt + 64 * u;
+        for (int x = 0; x < GR; ++x) {
+          __half sc = e->s[x];
+          // A NaN must not meet the zero probabilities of rows that do not see its position:
+          // its values count as zeros, and the rows that see it become NaN at the end.
+          if (values && __hisnan(sc)) {
+            sc = __ushort_as_half(0);
+            atomicMin(s_nan + x, j * kPfKeys + lt);
+          }
+          const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
+          const uint32_t w[4] = {e->w[x].x, e->w[x].y, e->w[x].z, e->w[x].w};
 #pragma unroll
-          for (int x = 0; x < GR; ++x) {
-            __half sc = e[u].s[x];
-            // A NaN must not meet the zero probabilities of rows that do not see its position:
-            // its values count as zeros, and the rows that see it become NaN at the end.
-            if (values && __hisnan(sc)) {
-              sc = __ushort_as_half(0);
-              atomicMin(s_nan + x, j * kPfKeys + r);
-            }
-            const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
-            const uint32_t w[4] = {e[u].w[x].x, e[u].w[x].y, e[u].w[x].z, e[u].w[x].w};
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              uint32_t o[4];
-              dequant4(w[y], s2, s72, magic, o);
-              *reinterpret_cast<uint4*>(dst + pf_piece(r, 4 * x + y)) = make_uint4(o[0], o[1], o[2], o[3]);
-            }
+          for (int y = 0; y < 4; ++y) {
+            uint32_t o[4];
+            dequant4(w[y], s2, s72, magic, o);
+            *reinterpret_cast<uint4*>(dst + pf_piece(lt, 4 * x + y)) = make_uint4(o[0], o[1], o[2], o[3]);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       };
-      Entry ek[2], ev[2];
-      int id[2], id_next[2] = {-1, -1};
-      ids_of(it.j0, id);
-      load(A.p.k, it.j0, id, ek);
-      load(A.p.v, it.j0, id, ev);
+      Entry ek, ev;
+      int id = id_of(it.j0), id_next = -1;
+      load(A.p.k, it.j0, id, &ek);
+      load(A.p.v, it.j0, id, &ev);
       for (int jj = 0; jj < len; ++jj) {
         const int j = it.j0 + jj;
         const uint32_t u = T + jj;
         const bool more = jj + 1 < len;
-        if (more) ids_of(j + 1, id_next);
+        if (more) id_next = id_of(j + 1);
         if (!ptx::mbar_wait_bounded(&k_empty[u & 1], ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag)) break;
-        put(sK + (size_t)(u & 1) * TILE, ek, j, false);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint32_t bad = __ballot_sync(0xffffffffu, id[x] == -2);
-          if (lane == 0) s_ok[u & 3][(lt >> 5) + 2 * x] = (uint8_t)(((bad & 0xFFFFu) ? 0 : 1) | ((bad >> 16) ? 0 : 2));
-        }
+        put(sK + (size_t)(u & 1) * TILE, &ek, j, false);
+        const uint32_t bad = __ballot_sync(__activemask(), id == -2);
+        if (lane == 0) s_ok[u & 3][lt >> 5] = (uint8_t)(((bad & 0xFFFFu) ? 0 : 1) | ((bad >> 16) ? 0 : 2));
         ptx::mbar_arrive(&k_full[u & 1]);
-        if (more) load(A.p.k, j + 1, id_next, ek);
+        if (more) load(A.p.k, j + 1, id_next, &ek);
         if (!ptx::mbar_wait_bounded(&v_empty[u & 1], ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag)) break;
-        put(sV + (size_t)(u & 1) * TILE, ev, j, true);
+        put(sV + (size_t)(u & 1) * TILE, &ev, j, true);
         ptx::mbar_arrive(&v_full[u & 1]);
-        if (more) load(A.p.v, j + 1, id_next, ev);
-        id[0] = id_next[0], id[1] = id_next[1];
+        if (more) load(A.p.v, j + 1, id_next, &ev);
+        id = id_next;
       }
-    }
-
-    T += len, ++I;
-    if (nq == 2) T1 += len, ++I1;
-    if (warp == 0) {
-      if (lane == 0 && it.j0 == 0 && len < it.nt) {
-        CutItem* c = cuts + blockIdx.x;
-        c->t0 = it.t0, c->g = it.g, c->row0 = it.row0, c->rows = min(it.R - it.row0, 2 * kPfRows);
-        c->spans = (int)((it.start + it.nt - 1) / share - blockIdx.x) + 1;
-      }
-      const bool go = walk.next(A, lane);
       __syncwarp();
-      if (lane == 0) s_go = go;      // (read by the others behind the next barrier, and before the one after it)
+      end_item();
     }
-    __syncthreads();                 // s_item, s_nan and the query buffers are free again
   }
 
   // every issued MMA completes before TMEM is freed: normally all have (o_full), after a
