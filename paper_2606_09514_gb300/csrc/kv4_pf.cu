@@ -134,6 +134,24 @@ __device__ __forceinline__ void pf_store_row32(const AttnArgs4& A, int64_t at, c
   }
 }
 
+// Two fp32 at once.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 template <int N>
 __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -147,7 +165,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   // TMEM columns: S of tile q at 128 q (P over their first half), O of tile q at 256 + 128 q
   constexpr uint32_t kO = 256;
   __shared__ __align__(8) uint64_t q_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
-  __shared__ __align__(8) uint64_t s_full[2], p_ready[2], o_full[2], drained;
+  __shared__ __align__(8) uint64_t s_full[2], p_ready[2][2], o_full[2], drained;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   __shared__ int64_t s_sum[kPfSoftWarps];
@@ -183,7 +201,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       ptx::mbar_init(&k_empty[b], 1);
       ptx::mbar_init(&v_empty[b], 1);
       ptx::mbar_init(&s_full[b], 1);
-      ptx::mbar_init(&p_ready[b], 128);
+      ptx::mbar_init(&p_ready[b][0], 128);
+      ptx::mbar_init(&p_ready[b][1], 128);
       ptx::mbar_init(&o_full[b], 1);
     }
     ptx::mbar_init(&drained, 1);
@@ -282,29 +301,41 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           constexpr int LPR = HD / 8, RPL = 32 / LPR;   // lanes per row, rows per load
           const int64_t at = (it.t0 + t) * A.a.q_stride + (int64_t)h * HD;
           const int l8 = lane % LPR;
-#pragma unroll 1
-          for (int r0 = 0; r0 < 32; r0 += 4 * RPL) {
-            float v[4][8];
+          auto put_q = [&](int r, const float* v) {
+            float top = 0.f, down, fac;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int64_t src = __shfl_sync(0xffffffffu, (long long)at, r0 + u * RPL + lane / LPR) + l8 * 8;
-              if (A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + src, v[u]);
-              else load8((const bf16*)A.a.q + src, v[u]);
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+#pragma unroll
+            for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            row_scale(top, A.a.scale, HD, &down, &fac);
+            if (l8 == 0) s_fac[q * kPfRows + r] = fac;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = h2(__floats2half2_rn(v[2 * e] * down, v[2 * e + 1] * down));
+            *reinterpret_cast<uint4*>(qdst + pf_piece(r, l8)) = make_uint4(w[0], w[1], w[2], w[3]);
+          };
+          auto from = [&](int r) { return __shfl_sync(0xffffffffu, (long long)at, r + lane / LPR) + l8 * 8; };
+          const int w0 = (warp & 3) * 32 + lane / LPR;
+          if (A.a.q_dtype == BUDDY_DTYPE_BF16) {
+            uint4 raw[32 / RPL];                        // all 32 rows in flight
+#pragma unroll
+            for (int u = 0; u < 32 / RPL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)A.a.q + from(u * RPL)));
+#pragma unroll
+            for (int u = 0; u < 32 / RPL; ++u) {
+              const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+              float v[8];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+              put_q(w0 + u * RPL, v);
             }
+          } else {
+#pragma unroll 1
+            for (int r0 = 0; r0 < 32; r0 += 4 * RPL) {
+              float v[4][8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int r = (warp & 3) * 32 + r0 + u * RPL + lane / LPR;
-              float top = 0.f, down, fac;
+              for (int u = 0; u < 4; ++u) load8((const float*)A.a.q + from(r0 + u * RPL), v[u]);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[u][e]));
-#pragma unroll
-              for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-              row_scale(top, A.a.scale, HD, &down, &fac);
-              if (l8 == 0) s_fac[q * kPfRows + r] = fac;
-              uint32_t w[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) w[e] = h2(__floats2half2_rn(v[u][2 * e] * down, v[u][2 * e + 1] * down));
-              *reinterpret_cast<uint4*>(qdst + pf_piece(r, l8)) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int u = 0; u < 4; ++u) put_q(w0 + r0 + u * RPL, v[u]);
             }
           }
           __syncwarp();
@@ -360,23 +391,31 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-          float ls[4] = {0.f, 0.f, 0.f, 0.f};
+          // The first half of P is handed over while the second is worked out.
+          const uint64_t fac2 = pair(fac, fac), ref2 = pair(-ref, -ref);
+          uint64_t ls[4] = {0, 0, 0, 0};
 #pragma unroll
           for (int c = 0; c < kPfKeys; c += 32) {
             uint32_t p[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float p0 = tca::exp2a(fmaf(__uint_as_float(s[c + 2 * i]), fac, -ref));
-              const float p1 = tca::exp2a(fmaf(__uint_as_float(s[c + 2 * i + 1]), fac, -ref));
-              ls[i & 3] += p0 + p1;
+              float p0, p1;
+              unpair(fma2(pair(__uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1])), fac2, ref2), p0, p1);
+              p0 = tca::exp2a(p0);
+              p1 = tca::exp2a(p1);
+              ls[i & 3] = add2(ls[i & 3], pair(p0, p1));
               p[i] = h2(__floats2half2_rn(p0, p1));
             }
             ptx::tmem_st16(ts + c / 2, p);
+            if (c == kPfKeys / 2 - 32 || c == kPfKeys - 32) {
+              ptx::tmem_wait_st();
+              ptx::tc_fence_before();
+              ptx::mbar_arrive(&p_ready[q][c > kPfKeys / 2]);
+            }
           }
-          l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-          ptx::tmem_wait_st();
-          ptx::tc_fence_before();
-          ptx::mbar_arrive(&p_ready[q]);
+          float l0, l1;
+          unpair(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), l0, l1);
+          l += l0 + l1;
         }
         if (ok)
           ok = __all_sync(0xffffffffu,
@@ -447,13 +486,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           }
           ptx::mma_commit(&s_full[q]);
         };
-        auto pv = [&](int q, uint32_t tile, bool first) {   // O_q += P_q V
+        auto pv = [&](int q, uint32_t tile, int half, bool first) {   // O_q += P_q V, 64 positions
           const uint8_t* V = sV + (size_t)(tile & 1) * TILE;
 #pragma unroll
-          for (int k = 0; k < kPfKeys / 16; ++k) {
+          for (int x = 0; x < kPfKeys / 32; ++x) {
+            const int k = half * (kPfKeys / 32) + x;
             const uint64_t dv = ptx::smem_desc_sw128_mn(V + k * 2048, kPfRegion);   // 16 positions: two 1 KiB groups
             ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, tmem + (uint32_t)q * 128u + 8u * k, dv, id_o,
-                             (!first || k > 0) ? 1u : 0u);
+                             (!first || x > 0) ? 1u : 0u);
           }
         };
         bool ok = wait(&q_ready[0], I) && (nq == 1 || wait(&q_ready[1], I1)) && wait(&k_full[T & 1], T >> 1);
@@ -466,11 +506,15 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           const bool more = jj + 1 < len;
           const uint32_t u = T + jj;
           for (int q = 0; q < nq && ok; ++q) {
-            ok = wait(&p_ready[q], (q == 0 ? T : T1) + jj) && (q > 0 || wait(&v_full[u & 1], u >> 1)) &&
-                 (q > 0 || !more || wait(&k_full[(u + 1) & 1], (u + 1) >> 1));
+            const uint32_t c = (q == 0 ? T : T1) + jj;
+            ok = (q > 0 || wait(&v_full[u & 1], u >> 1)) && wait(&p_ready[q][0], c);
             if (!ok) break;
             ptx::tc_fence_after();
-            pv(q, u, jj == 0);
+            pv(q, u, 0, jj == 0);
+            ok = (q > 0 || !more || wait(&k_full[(u + 1) & 1], (u + 1) >> 1)) && wait(&p_ready[q][1], c);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            pv(q, u, 1, false);
             if (q == nq - 1) ptx::mma_commit(&v_empty[u & 1]);
             if (more) {
               qk(q, u + 1);   // in issue order after the P V that reads P from the same columns
