@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
   __shared__ int s_first, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
   const int B = A.a.batch, G = A.G;
+  pdl_trigger();   // (the prompts of the same call may start where there is room)
 
   // ---- this CTA's share: [lo, lo + share) of all streams' openings and chunks
   const int per = (B + kThreads - 1) / kThreads;

@@ -35,8 +35,8 @@ constexpr int kPfRows = 128, kPfKeys = 128;
 constexpr int kPfSoftWarps = 8, kPfProducers = 128;
 constexpr int kPfThreads = 512;          // four warpgroups: two of softmax, producers, the MMA warp's
 // Registers: 128 a thread at launch (65,536 in all), then by setmaxnreg 2 x 128 x 176 +
-// 128 x 104 + 128 x 56 = 65,536.
-constexpr int kPfRegsSoft = 176, kPfRegsProduce = 104, kPfRegsMma = 56;
+// 128 x 88 + 128 x 72 = 65,536.
+constexpr int kPfRegsSoft = 176, kPfRegsProduce = 88, kPfRegsMma = 72;
 constexpr int kPfOpen = 3;               // what beginning and ending an item costs, in tiles
 constexpr int kPfWhole = 4;              // items of at most this many tiles are not cut
 constexpr uint32_t kPfRegion = 128u * 128u;   // 128 rows x 64 channels of half
@@ -63,6 +63,10 @@ struct CutItem {
 struct PfItem {
   int seq, t0, m, n, g, R, row0, nt, j0, j1;
   int64_t start;                  // where the item's first tile is
+  int go;                         // 0: the share's end, no item
+
+  __device__ __forceinline__ int tiles() const { return R - row0 > kPfRows ? 2 : 1; }   // tiles of rows
+  __device__ __forceinline__ int len() const { return j1 - j0; }
 };
 
 __device__ __forceinline__ int pf_tiles(int n, int m, int G, int R, int qp) {
@@ -169,10 +173,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
   __shared__ int64_t s_sum[kPfSoftWarps];
-  __shared__ PfItem s_item;
-  __shared__ int s_go;
+  __shared__ __align__(8) uint64_t item_full[2], item_empty[2];
+  __shared__ PfItem s_first, s_item[2];                 // [item % 2]
   __shared__ float s_fac[2 * kPfRows];
-  __shared__ int s_nan[GR];
+  __shared__ int s_nan[2][GR];                          // [item % 2] first position whose values are NaN, by group
   __shared__ __align__(4) uint8_t s_ok[4][4];           // [tile % 4][32 positions]: two bits, pages that are there
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -204,10 +208,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       ptx::mbar_init(&p_ready[b][0], 128);
       ptx::mbar_init(&p_ready[b][1], 128);
       ptx::mbar_init(&o_full[b], 1);
+      ptx::mbar_init(&item_full[b], 1);
+      ptx::mbar_init(&item_empty[b], kPfSoftWarps + kPfProducers / 32 + 1);
     }
     ptx::mbar_init(&drained, 1);
     abort_flag = 0;
-    s_go = 0;
     cuts[blockIdx.x].spans = 0;
     ptx::fence_mbar_init();
   }
@@ -219,7 +224,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   }
   const int64_t share = max((int64_t)kPfWhole, (total + gridDim.x - 1) / gridDim.x);
   const int64_t lo = blockIdx.x * share;
-  if (lo >= total) return;
+  if (lo >= total) {
+    pdl_wait();
+    return;
+  }
   if (warp < kPfSoftWarps && before <= lo && lo < before + mine) {
     // the sequence, its head, the item of it and the tile where the share begins
     PfWalk w;
@@ -250,7 +258,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       at += __shfl_sync(0xffffffffu, upto, 31);
     }
     if (lane == 0)
-      s_item = {w.i, w.q.t0, w.q.m, w.q.n, w.g, R, w.qp * 2 * kPfRows, pf_tiles(w.q.n, w.q.m, G, R, w.qp), 0, 0, at + kPfOpen};
+      s_first = {w.i, w.q.t0, w.q.m, w.q.n, w.g, R, w.qp * 2 * kPfRows, pf_tiles(w.q.n, w.q.m, G, R, w.qp), 0, 0,
+                 at + kPfOpen, 1};
   }
   if (warp == kMmaWarp) {
     ptx::tmem_alloc(&tmem_slot, 512);
@@ -261,45 +270,66 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   ptx::tc_fence_after();
   const uint32_t tmem = tmem_slot;
 
-  // Every role walks the items: between two barriers s_item is one item's, and the counts
-  // of tiles and items so far give the mbarriers' phases: of all tiles and items, and of
-  // those with a second tile of rows.
+  // A warp walks the items and hands them to the roles, two at a time; a role gives an item
+  // back when it is done with it, so that the producers are at the next item's keys and the
+  // softmax warps have its queries on the way while this one's outputs are written.  The
+  // counts of tiles and items so far give the mbarriers' phases: of all tiles and items,
+  // and of those with a second tile of rows.
   uint32_t T = 0, I = 0, T1 = 0, I1 = 0;
-  PfItem it;
-  int nq = 1, len = 0, kmax = 0;
-  auto next_item = [&]() {
-    __syncthreads();
-    if (!s_go || abort_flag) return false;
-    it = s_item;
-    nq = it.R - it.row0 > kPfRows ? 2 : 1;              // tiles with rows
-    len = it.j1 - it.j0;
-    const int last = min(it.R, it.row0 + 2 * kPfRows) - 1;
-    kmax = max(it.n - it.m + last / G + 1, 0);          // positions that the last row sees
-    return true;
+  auto take = [&](uint32_t i) {    // whether there is an item i: s_item[i % 2] until it is given back
+    if (!__all_sync(0xffffffffu,
+                    ptx::mbar_wait_bounded(&item_full[i & 1], (i >> 1) & 1, kWaitLimitNs, &abort_flag)))
+      return false;
+    return s_item[i & 1].go != 0;
   };
-  auto end_item = [&]() {
+  auto give = [&]() {              // (whole warp)
+    const int len = s_item[I & 1].len(), two = s_item[I & 1].tiles() - 1;
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&item_empty[I & 1]);
     T += len, ++I;
-    if (nq == 2) T1 += len, ++I1;
-    __syncthreads();                                    // s_item, s_nan and the query buffers are free again
+    T1 += two * len, I1 += two;
   };
 
-  // (a warpgroup takes or gives registers in one instruction; warps 13 to 15 read the first
-  // s_item before it is written anew)
+  // (a warpgroup takes or gives registers in one instruction)
   if (warp >= kMmaWarp) regs_down<kPfRegsMma>();
   if (warp < kPfSoftWarps) {
     regs_up<kPfRegsSoft>();
-    __syncthreads();
-    while (next_item()) {
-      const int q = warp >> 2;                          // this warp's tile
-      if (q < nq) {
+    const int q = warp >> 2;                            // this warp's tile
+    constexpr int LPR = HD / 8, RPL = 32 / LPR;         // queries: lanes per row, rows per load
+    uint4 raw[32 / RPL];                                // an item's queries on their way (bf16), 32 rows of the warp
+    auto row_at = [&](const PfItem& x, int64_t stride) {   // this lane's row
+      const int rr = min(x.row0 + q * kPfRows + (warp & 3) * 32 + lane, x.R - 1), t = rr / G;
+      return (x.t0 + t) * stride + (int64_t)(x.g * G + rr - t * G) * HD;
+    };
+    // (always all of raw: what an item does not need must not live through its tiles)
+    auto fetch_q = [&](const PfItem& x, bool want) {
+      want = want && A.a.q_dtype == BUDDY_DTYPE_BF16 && q < x.tiles();
+      const int64_t at = want ? row_at(x, A.a.q_stride) : 0;
+#pragma unroll
+      for (int u = 0; u < 32 / RPL; ++u) {
+        const int64_t src = __shfl_sync(0xffffffffu, (long long)at, u * RPL + lane / LPR) + (lane % LPR) * 8;
+        raw[u] = want ? __ldg(reinterpret_cast<const uint4*>((const bf16*)A.a.q + src)) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    bool go = take(0);
+    fetch_q(s_item[0], go);
+    while (go) {
+      const PfItem& it = s_item[I & 1];
+      const int len = it.len();
+      bool ok = true;
+      if (q >= it.tiles()) {
+        go = take(I + 1);
+        fetch_q(s_item[(I + 1) & 1], go);
+      } else {
         // ----------------------------------------------------------- softmax
-        const int rt = (warp & 3) * 32 + lane;          // row of the tile
-        const int row = it.row0 + q * kPfRows + rt, rr = min(row, it.R - 1);
-        const int t = rr / G, h = it.g * G + rr - t * G;
+        // (what only the beginning or the end needs is worked out there: the tiles need the
+        // registers)
         uint8_t* const qdst = sQ + (size_t)q * TILE;
+        const int rt = (warp & 3) * 32 + lane;          // row of the tile
+        auto seen_by = [&]() {                          // positions this lane's row sees (may be <= 0)
+          return it.n - it.m + min(it.row0 + q * kPfRows + rt, it.R - 1) / G + 1;
+        };
         {
-          constexpr int LPR = HD / 8, RPL = 32 / LPR;   // lanes per row, rows per load
-          const int64_t at = (it.t0 + t) * A.a.q_stride + (int64_t)h * HD;
           const int l8 = lane % LPR;
           auto put_q = [&](int r, const float* v) {
             float top = 0.f, down, fac;
@@ -314,12 +344,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
             for (int e = 0; e < 4; ++e) w[e] = h2(__floats2half2_rn(v[2 * e] * down, v[2 * e + 1] * down));
             *reinterpret_cast<uint4*>(qdst + pf_piece(r, l8)) = make_uint4(w[0], w[1], w[2], w[3]);
           };
-          auto from = [&](int r) { return __shfl_sync(0xffffffffu, (long long)at, r + lane / LPR) + l8 * 8; };
           const int w0 = (warp & 3) * 32 + lane / LPR;
           if (A.a.q_dtype == BUDDY_DTYPE_BF16) {
-            uint4 raw[32 / RPL];                        // all 32 rows in flight
-#pragma unroll
-            for (int u = 0; u < 32 / RPL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)A.a.q + from(u * RPL)));
 #pragma unroll
             for (int u = 0; u < 32 / RPL; ++u) {
               const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
@@ -329,6 +355,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
               put_q(w0 + u * RPL, v);
             }
           } else {
+            const int64_t at = row_at(it, A.a.q_stride);
+            auto from = [&](int r) { return __shfl_sync(0xffffffffu, (long long)at, r + lane / LPR) + l8 * 8; };
 #pragma unroll 1
             for (int r0 = 0; r0 < 32; r0 += 4 * RPL) {
               float v[4][8];
@@ -345,10 +373,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         const float fac = s_fac[q * kPfRows + rt];
         const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t ts = tq + (uint32_t)q * 128u, to = tq + kO + (uint32_t)q * 128u;
-        const int seen = it.n - it.m + t + 1;           // positions this row sees (may be <= 0)
+        const int seen = seen_by();
         const uint32_t C = q == 0 ? T : T1;
         float m = -INFINITY, l = 0.f;
-        bool ok = true;
         for (int jj = 0; jj < len; ++jj) {
           ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(&s_full[q], (C + jj) & 1, kWaitLimitNs, &abort_flag));
           if (!ok) break;
@@ -393,7 +420,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           const float ref = m == -INFINITY ? 0.f : m;
           // The first half of P is handed over while the second is worked out.
           const uint64_t fac2 = pair(fac, fac), ref2 = pair(-ref, -ref);
-          uint64_t ls[4] = {0, 0, 0, 0};
+          uint64_t ls[2] = {0, 0};
 #pragma unroll
           for (int c = 0; c < kPfKeys; c += 32) {
             uint32_t p[16];
@@ -403,7 +430,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
               unpair(fma2(pair(__uint_as_float(s[c + 2 * i]), __uint_as_float(s[c + 2 * i + 1])), fac2, ref2), p0, p1);
               p0 = tca::exp2a(p0);
               p1 = tca::exp2a(p1);
-              ls[i & 3] = add2(ls[i & 3], pair(p0, p1));
+              ls[i & 1] = add2(ls[i & 1], pair(p0, p1));
               p[i] = h2(__floats2half2_rn(p0, p1));
             }
             ptx::tmem_st16(ts + c / 2, p);
@@ -414,26 +441,30 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
             }
           }
           float l0, l1;
-          unpair(add2(add2(ls[0], ls[1]), add2(ls[2], ls[3])), l0, l1);
+          unpair(add2(ls[0], ls[1]), l0, l1);
           l += l0 + l1;
         }
-        if (ok)
+        if (ok) {
+          go = take(I + 1);
+          fetch_q(s_item[(I + 1) & 1], go);
           ok = __all_sync(0xffffffffu,
                           ptx::mbar_wait_bounded(&o_full[q], (q == 0 ? I : I1) & 1, kWaitLimitNs, &abort_flag));
+        }
         if (ok) {
           ptx::tc_fence_after();
           const bool whole = len == it.nt;
           const float inv = !whole ? 1.f : m == -INFINITY ? 0.f : 1.f / l;
           float* part = A.part + (2 * (int64_t)blockIdx.x + (it.j0 == 0 ? 1 : 0)) * pf_part_floats<HD>() + q * kPfRows + rt;
           if (!whole) part[0] = m, part[2 * kPfRows] = l;
-          const int64_t out_at = (it.t0 + t) * A.a.out_stride + (int64_t)h * HD;
+          const int64_t out_at = row_at(it, A.a.out_stride);
+          const int sees = seen_by();
           const bool staged = whole && A.a.out_dtype == BUDDY_DTYPE_BF16;
 #pragma unroll 1
           for (int c = 0; c < HD; c += 32) {
             float o[32];
             ptx::tmem_ld32(to + c, reinterpret_cast<uint32_t*>(o));
             ptx::tmem_wait_ld();
-            const bool nan = *reinterpret_cast<const volatile int*>(s_nan + c / kGroup) < seen;
+            const bool nan = *reinterpret_cast<const volatile int*>(&s_nan[I & 1][c / kGroup]) < sees;
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] = nan ? __uint_as_float(0x7FC00000u) : o[i] * inv;
             if (!whole) {
@@ -445,7 +476,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
                 *reinterpret_cast<uint4*>(qdst + pf_piece(rt, (c + i) >> 3)) =
                     make_uint4(tca::pack_bf16(o[i], o[i + 1]), tca::pack_bf16(o[i + 2], o[i + 3]),
                                tca::pack_bf16(o[i + 4], o[i + 5]), tca::pack_bf16(o[i + 6], o[i + 7]));
-            } else if (row < it.R) {
+            } else if (it.row0 + q * kPfRows + rt < it.R) {
               pf_store_row32(A, out_at + c, o);
             }
           }
@@ -463,40 +494,41 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           }
         }
       }
-      end_item();
+      if (!ok) break;
+      give();
     }
   } else if (warp == kMmaWarp) {
     // -------------------------------------------------------------------- MMA
-    __syncthreads();
-    while (next_item()) {
-      if (lane == 0) {
+    while (take(I)) {
+      const int nq = s_item[I & 1].tiles(), len = s_item[I & 1].len();
+      bool ok = true;
+      if (ptx::elect_one()) {
         const uint32_t id_s = (1u << 4) | ((uint32_t)(kPfKeys >> 3) << 17) | (8u << 24);   // half in, fp32 out, M 128
         const uint32_t id_o = (1u << 4) | ((uint32_t)(HD >> 3) << 17) | (8u << 24) | ptx::kIdescBMnMajor;
         auto wait = [&](uint64_t* bar, uint32_t count) {
           return ptx::mbar_wait_bounded(bar, count & 1, kWaitLimitNs, &abort_flag);
         };
+        // (descriptors of the buffers once: what an MMA adds to one fits in its address field)
+        const uint64_t dQ = ptx::smem_desc_sw128(sQ), dK = ptx::smem_desc_sw128(sK);
+        const uint64_t dV = ptx::smem_desc_sw128_mn(sV, kPfRegion);
         auto qk = [&](int q, uint32_t tile) {           // S_q = Q_q K^T
-          const uint8_t* Q = sQ + (size_t)q * TILE;
-          const uint8_t* K = sK + (size_t)(tile & 1) * TILE;
+          const uint64_t a = dQ + (uint64_t)q * (TILE >> 4), b = dK + (uint64_t)(tile & 1) * (TILE >> 4);
 #pragma unroll
           for (int k = 0; k < HD / 16; ++k) {
-            const uint64_t dk = ptx::smem_desc_sw128(K + (k >> 2) * kPfRegion) + 2ull * (k & 3);
-            const uint64_t dq = ptx::smem_desc_sw128(Q + (k >> 2) * kPfRegion) + 2ull * (k & 3);
-            ptx::mma_bf16(tmem + (uint32_t)q * 128u, dq, dk, id_s, k > 0 ? 1u : 0u);
+            const uint64_t off = (k >> 2) * (kPfRegion >> 4) + 2 * (k & 3);
+            ptx::mma_bf16(tmem + (uint32_t)q * 128u, a + off, b + off, id_s, k > 0 ? 1u : 0u);
           }
           ptx::mma_commit(&s_full[q]);
         };
         auto pv = [&](int q, uint32_t tile, int half, bool first) {   // O_q += P_q V, 64 positions
-          const uint8_t* V = sV + (size_t)(tile & 1) * TILE;
+          const uint64_t v = dV + (uint64_t)(tile & 1) * (TILE >> 4) + half * (kPfKeys / 32) * (2048 >> 4);
+          const uint32_t p = tmem + (uint32_t)q * 128u + 8u * half * (kPfKeys / 32);
 #pragma unroll
-          for (int x = 0; x < kPfKeys / 32; ++x) {
-            const int k = half * (kPfKeys / 32) + x;
-            const uint64_t dv = ptx::smem_desc_sw128_mn(V + k * 2048, kPfRegion);   // 16 positions: two 1 KiB groups
-            ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, tmem + (uint32_t)q * 128u + 8u * k, dv, id_o,
+          for (int x = 0; x < kPfKeys / 32; ++x)        // 16 positions: two 1 KiB groups
+            ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, p + 8u * x, v + x * (2048 >> 4), id_o,
                              (!first || x > 0) ? 1u : 0u);
-          }
         };
-        bool ok = wait(&q_ready[0], I) && (nq == 1 || wait(&q_ready[1], I1)) && wait(&k_full[T & 1], T >> 1);
+        ok = wait(&q_ready[0], I) && (nq == 1 || wait(&q_ready[1], I1)) && wait(&k_full[T & 1], T >> 1);
         if (ok) {
           ptx::tc_fence_after();
           for (int q = 0; q < nq; ++q) qk(q, T);
@@ -525,15 +557,15 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           }
         }
       }
-      __syncwarp();
-      end_item();
+      if (!__all_sync(0xffffffffu, ok)) break;
+      give();
     }
-  } else if (warp > kMmaWarp) {
+  } else if (warp == kMmaWarp + 1) {
     // ------------------------------------------------- the walk over the items
     PfWalk walk{};
-    walk.q = {s_item.t0, s_item.m, s_item.n};
-    walk.i = s_item.seq, walk.g = s_item.g, walk.qp = s_item.row0 / (2 * kPfRows), walk.nt = s_item.nt;
-    walk.start = s_item.start;
+    walk.q = {s_first.t0, s_first.m, s_first.n};
+    walk.i = s_first.seq, walk.g = s_first.g, walk.qp = s_first.row0 / (2 * kPfRows), walk.nt = s_first.nt;
+    walk.start = s_first.start;
     const int64_t x = lo - walk.start;                  // tile of the item; below 0: its opening
     walk.rem = min(share, total - lo) + min(x, (int64_t)0);
     walk.j0 = (int)max(x, (int64_t)0);
@@ -547,34 +579,35 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         walk.rem -= walk.j1 - walk.j0;
       }
     }
-    const bool mine = warp == kMmaWarp + 1;             // (the other two warps follow)
-    __syncthreads();                                    // everyone has read the first s_item
-    while (true) {
-      if (mine) {
-        if (lane == 0) {
-          s_item = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * 2 * kPfRows, walk.nt, walk.j0,
-                    walk.j1, walk.start};
-          s_go = go;
-          if (go && walk.j0 == 0 && walk.j1 < walk.nt) {
-            CutItem* c = cuts + blockIdx.x;
-            c->t0 = walk.q.t0, c->g = walk.g, c->row0 = walk.qp * 2 * kPfRows;
-            c->rows = min(walk.q.m * G - c->row0, 2 * kPfRows);
-            c->spans = (int)((walk.start + walk.nt - 1) / share - blockIdx.x) + 1;
-          }
+    for (uint32_t i = 0;; ++i) {
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&item_empty[i & 1], ((i >> 1) & 1) ^ 1, kWaitLimitNs,
+                                                          &abort_flag)))
+        break;
+      if (lane < GR) s_nan[i & 1][lane] = INT32_MAX;
+      __syncwarp();
+      if (lane == 0) {
+        s_item[i & 1] = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * 2 * kPfRows, walk.nt,
+                         walk.j0, walk.j1, walk.start, go};
+        if (go && walk.j0 == 0 && walk.j1 < walk.nt) {
+          CutItem* c = cuts + blockIdx.x;
+          c->t0 = walk.q.t0, c->g = walk.g, c->row0 = walk.qp * 2 * kPfRows;
+          c->rows = min(walk.q.m * G - c->row0, 2 * kPfRows);
+          c->spans = (int)((walk.start + walk.nt - 1) / share - blockIdx.x) + 1;
         }
-        if (lane < GR) s_nan[lane] = INT32_MAX;
+        ptx::mbar_arrive(&item_full[i & 1]);
       }
-      if (!next_item()) break;
-      if (mine) go = walk.next(A, lane);
-      end_item();
+      if (!go) break;
+      go = walk.next(A, lane);
     }
-  } else {
+  } else if (warp < kMmaWarp) {
     // -------------------------------------------------------------- K, V tiles
     regs_down<kPfRegsProduce>();
     const int lt = tid - 32 * kPfSoftWarps;             // this thread's position of a tile
-    __syncthreads();
-    while (next_item()) {
-      const int end = min(it.n, kmax);                  // positions that any row sees
+    while (take(I)) {
+      const PfItem it = s_item[I & 1];
+      const int len = it.len();
+      const int last = min(it.R, it.row0 + 2 * kPfRows) - 1;
+      const int end = min(it.n, max(it.n - it.m + last / G + 1, 0));                  // positions that any row sees
       const int in_page = (1 << A.p.shift) - 1;
       const int32_t* table = A.a.table + (int64_t)it.seq * A.a.max_pages;
       const uint32_t magic = 0x54005400u;
@@ -610,7 +643,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           // its values count as zeros, and the rows that see it become NaN at the end.
           if (values && __hisnan(sc)) {
             sc = __ushort_as_half(0);
-            atomicMin(s_nan + x, j * kPfKeys + lt);
+            atomicMin(&s_nan[I & 1][x], j * kPfKeys + lt);
           }
           const __half2 s2 = __half2half2(sc), s72 = __hmul2(s2, __float2half2_rn(-72.f));
           const uint32_t w[4] = {e->w[x].x, e->w[x].y, e->w[x].z, e->w[x].w};
@@ -644,13 +677,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         if (more) load(A.p.v, j + 1, id_next, &ev);
         id = id_next;
       }
-      __syncwarp();
-      end_item();
+      if (__any_sync(0xffffffffu, abort_flag)) break;
+      give();
     }
   }
 
   // every issued MMA completes before TMEM is freed: normally all have (o_full), after a
   // wait that ran out the MMA warp waits for its own
+  pdl_trigger();
   __syncthreads();
   if (warp == kMmaWarp) {
     if (abort_flag) {
@@ -665,46 +699,56 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
+  pdl_wait();   // (started next to the few-row kernel: does not end before it)
 }
 
-// The parts of the items that were cut, in order: a thread per row, 16 channels.
+// The parts of the items that were cut, in order: a thread per row, four channels, eight
+// parts' loads at a time.
 template <int HD>
 __global__ void __launch_bounds__(2 * kPfRows) kv4_join_kernel(const AttnArgs4 A, const CutItem* cuts) {
+  pdl_wait();
   const CutItem c = cuts[blockIdx.x];
-  const int x = threadIdx.x, ch = blockIdx.y * 16;
+  const int x = threadIdx.x, ch = blockIdx.y * 4;
   if (x >= c.rows || c.spans == 0) return;
   auto part = [&](int k) {
     return A.part + (2 * (int64_t)(blockIdx.x + k) + (k == 0 ? 1 : 0)) * pf_part_floats<HD>() + x;
   };
-  float M = -INFINITY, L = 0.f, o[16];
-  for (int k = 0; k < c.spans; ++k) M = fmaxf(M, part(k)[0]);
-  const float at = M == -INFINITY ? 0.f : M;
+  float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int N = 8;
+  for (int k0 = 0; k0 < c.spans; k0 += N) {
+    float m[N], l[N], v[N][4], to = M;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) o[i] = 0.f;
-#pragma unroll 2
-  for (int k = 0; k < c.spans; ++k) {
-    const float* p = part(k);
-    const float a = tca::exp2a(p[0] - at);
-    L += a * p[2 * kPfRows];
+    for (int k = 0; k < N; ++k) {
+      const float* p = part(min(k0 + k, c.spans - 1));
+      m[k] = k0 + k < c.spans ? p[0] : -INFINITY;
+      l[k] = p[2 * kPfRows];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[i] += a * p[(2 + ch + i) * 2 * kPfRows];
+      for (int i = 0; i < 4; ++i) v[k][i] = p[(2 + ch + i) * 2 * kPfRows];
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) to = fmaxf(to, m[k]);
+    const float at = to == -INFINITY ? 0.f : to, a = tca::exp2a(M - at);
+    L *= a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] *= a;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (k0 + k >= c.spans) break;
+      const float b = tca::exp2a(m[k] - at);
+      L += b * l[k];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += b * v[k][i];
+    }
+    M = to;
   }
   const float inv = M == -INFINITY ? 0.f : 1.f / L;
   const int row = c.row0 + x, G = A.G;
   const int64_t to = (c.t0 + row / G) * A.a.out_stride + (int64_t)(c.g * G + row % G) * HD + ch;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) o[i] *= inv;
-  if (A.a.out_dtype == BUDDY_DTYPE_F32) {
-    float4* d = reinterpret_cast<float4*>((float*)A.a.out + to);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-  } else {
-    uint4* d = reinterpret_cast<uint4*>((bf16*)A.a.out + to);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      d[i] = make_uint4(tca::pack_bf16(o[8 * i], o[8 * i + 1]), tca::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
-                        tca::pack_bf16(o[8 * i + 4], o[8 * i + 5]), tca::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
-  }
+  if (A.a.out_dtype == BUDDY_DTYPE_F32)
+    *reinterpret_cast<float4*>((float*)A.a.out + to) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  else
+    *reinterpret_cast<uint2*>((bf16*)A.a.out + to) =
+        make_uint2(tca::pack_bf16(o[0] * inv, o[1] * inv), tca::pack_bf16(o[2] * inv, o[3] * inv));
 }
 
 int64_t prompt_workspace(int head_dim, int sms) {
@@ -716,10 +760,12 @@ static int launch_prompt_hd(const AttnArgs4& A, CutItem* cuts, int sms, cudaStre
   if (cudaFuncSetAttribute(kv4_prompt_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pf_smem<HD>()) !=
       cudaSuccess)
     return BUDDY_ERR_CUDA;
-  kv4_prompt_kernel<HD><<<sms, kPfThreads, pf_smem<HD>(), s>>>(A, cuts);
-  if (cudaGetLastError() != cudaSuccess) return BUDDY_ERR_CUDA;
-  kv4_join_kernel<HD><<<dim3(sms, HD / 16), 2 * kPfRows, 0, s>>>(A, cuts);
-  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  // the prompts start on the SMs that the few-row kernel leaves free, the join is launched
+  // as the prompts end
+  if (launch_k(kv4_prompt_kernel<HD>, sms, kPfThreads, pf_smem<HD>(), s, true, A, cuts) != cudaSuccess ||
+      launch_k(kv4_join_kernel<HD>, dim3(sms, HD / 4), 2 * kPfRows, 0, s, true, A, (const CutItem*)cuts) != cudaSuccess)
+    return BUDDY_ERR_CUDA;
+  return BUDDY_OK;
 }
 
 // ws: prompt_workspace() bytes.
