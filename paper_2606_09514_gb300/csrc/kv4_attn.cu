@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       float down, f;
-      row_scale(top, A.a.scale, HD, &down, &f);
+      row_scale(top, (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f, &down, &f);
 #pragma unroll
       for (int e = 0; e < HD / 4; e += 2)
         qf[b][e / 4][(e / 2) & 1] = h2(__floats2half2_rn(x[e] * down, x[e + 1] * down));

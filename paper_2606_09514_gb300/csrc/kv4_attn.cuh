@@ -36,12 +36,11 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs4& A, int i, bool* bad) {
 
 // Query rows enter the products as halves of 1 .. 2 times a power of two per row: the
 // exponent (of the row's largest magnitude), its inverse, and the factor that takes a
-// score of the halves to base 2.  (Above zero, so that it takes -inf to -inf.)
-__device__ __forceinline__ void row_scale(float top, float scale, int hd, float* down, float* fac) {
+// score of the halves to base 2 (base: log2(e) times the scores' scale).  (Above zero, so that it takes -inf to -inf.)
+__device__ __forceinline__ void row_scale(float top, float base, float* down, float* fac) {
   const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
   *down = __uint_as_float((uint32_t)(127 - ex) << 23);
-  const float up = __uint_as_float((uint32_t)(127 + ex) << 23);
-  *fac = fmaxf((scale != 0.f ? scale : rsqrtf((float)hd)) * 1.4426950408889634f * up, 1.2e-38f);
+  *fac = fmaxf(base * __uint_as_float((uint32_t)(127 + ex) << 23), 1.2e-38f);
 }
 
 __device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }

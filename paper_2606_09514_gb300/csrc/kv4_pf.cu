@@ -4,8 +4,8 @@
 // The rows of a (sequence, KV head) are (query token, head of the group) pairs, row
 // r = token r / G, head r % G; two tiles of 128 of them (an item) walk the same
 // key/value tiles of 128 positions.  On the 5th-generation tensor cores, in half:
-//   S = Q K^T   tcgen05.mma M = 128, N = 128, K = HD: queries (scaled by a power of two
-//               per row to 1 .. 2) and keys from shared memory, S in TMEM;
+//   S = Q K^T   tcgen05.mma M = 128, N = 128, K = HD: queries (of a warp's 32 rows, scaled by
+//               a power of two to 2 at most) and keys from shared memory, S in TMEM;
 //   softmax     four warps per tile, a row per thread, base 2: running reference m,
 //               which follows the maximum when that rises by more than 8; p back into
 //               TMEM as half over S's columns;
@@ -37,7 +37,7 @@ constexpr int kPfThreads = 512;          // four warpgroups: two of softmax, pro
 // Registers: 128 a thread at launch (65,536 in all), then by setmaxnreg 2 x 128 x 176 +
 // 128 x 88 + 128 x 72 = 65,536.
 constexpr int kPfRegsSoft = 176, kPfRegsProduce = 88, kPfRegsMma = 72;
-constexpr int kPfOpen = 3;               // what beginning and ending an item costs, in tiles
+constexpr int kPfOpen = 4;               // what beginning and ending an item costs, in tiles
 constexpr int kPfWhole = 4;              // items of at most this many tiles are not cut
 constexpr uint32_t kPfRegion = 128u * 128u;   // 128 rows x 64 channels of half
 
@@ -77,6 +77,7 @@ __device__ __forceinline__ int pf_tiles(int n, int m, int G, int R, int qp) {
 __device__ __forceinline__ int64_t pf_head_cost(int n, int m, int G, int R, int lane) {
   const int nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
   int64_t c = 0;
+#pragma unroll 1
   for (int qp = lane; qp < nqp; qp += 32) c += pf_tiles(n, m, G, R, qp) + kPfOpen;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
@@ -84,6 +85,7 @@ __device__ __forceinline__ int64_t pf_head_cost(int n, int m, int G, int R, int 
 }
 // First sequence from i on (below end) that is this kernel's; end if none (whole warp).
 __device__ __forceinline__ int pf_next_seq(const AttnArgs4& A, int i, int end, int lane, Rows* q) {
+#pragma unroll 1
   for (; i < end; i += 32) {
     Rows s{0, 0, 0};
     bool bad;
@@ -124,20 +126,6 @@ struct PfWalk {
   }
 };
 
-__device__ __forceinline__ void pf_store_row32(const AttnArgs4& A, int64_t at, const float* o) {
-  if (A.a.out_dtype == BUDDY_DTYPE_F32) {
-    float4* d = reinterpret_cast<float4*>((float*)A.a.out + at);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-  } else {
-    uint4* d = reinterpret_cast<uint4*>((bf16*)A.a.out + at);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      d[i] = make_uint4(tca::pack_bf16(o[8 * i], o[8 * i + 1]), tca::pack_bf16(o[8 * i + 2], o[8 * i + 3]),
-                        tca::pack_bf16(o[8 * i + 4], o[8 * i + 5]), tca::pack_bf16(o[8 * i + 6], o[8 * i + 7]));
-  }
-}
-
 // Two fp32 at once.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t r;
@@ -175,7 +163,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   __shared__ int64_t s_sum[kPfSoftWarps];
   __shared__ __align__(8) uint64_t item_full[2], item_empty[2];
   __shared__ PfItem s_first, s_item[2];                 // [item % 2]
-  __shared__ float s_fac[2 * kPfRows];
   __shared__ int s_nan[2][GR];                          // [item % 2] first position whose values are NaN, by group
   __shared__ __align__(4) uint8_t s_ok[4][4];           // [tile % 4][32 positions]: two bits, pages that are there
 
@@ -237,9 +224,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       if (lo < at + cost * A.p.nkv) break;
       at += cost * A.p.nkv;
     }
-    w.g = (int)((lo - at) / cost);
-    at += w.g * cost;
+    w.g = 0;
+#pragma unroll 1
+    for (; lo >= at + cost; at += cost) ++w.g;
     const int R = w.q.m * G, nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+#pragma unroll 1
     for (int q0 = 0;; q0 += 32) {
       const int64_t c = q0 + lane < nqp ? pf_tiles(w.q.n, w.q.m, G, R, q0 + lane) + kPfOpen : 0;
       int64_t upto = c;
@@ -296,81 +285,91 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     regs_up<kPfRegsSoft>();
     const int q = warp >> 2;                            // this warp's tile
     constexpr int LPR = HD / 8, RPL = 32 / LPR;         // queries: lanes per row, rows per load
-    uint4 raw[32 / RPL];                                // an item's queries on their way (bf16), 32 rows of the warp
     auto row_at = [&](const PfItem& x, int64_t stride) {   // this lane's row
       const int rr = min(x.row0 + q * kPfRows + (warp & 3) * 32 + lane, x.R - 1), t = rr / G;
       return (x.t0 + t) * stride + (int64_t)(x.g * G + rr - t * G) * HD;
     };
-    // (always all of raw: what an item does not need must not live through its tiles)
-    auto fetch_q = [&](const PfItem& x, bool want) {
-      want = want && A.a.q_dtype == BUDDY_DTYPE_BF16 && q < x.tiles();
-      const int64_t at = want ? row_at(x, A.a.q_stride) : 0;
+    auto fetch_q = [&](const PfItem& x) {               // an item's queries into L2
+      if (q >= x.tiles()) return;
+      const int esz = A.a.q_dtype == BUDDY_DTYPE_F32 ? 4 : 2;
+      const uint8_t* src = (const uint8_t*)A.a.q + row_at(x, A.a.q_stride) * esz;
+      for (int i = 0; i < HD * esz; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + i));
+    };
+    uint8_t* const qdst = sQ + (size_t)q * TILE;
+    const float base = (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f;
+    // The queries of this warp's 32 rows as halves of at most 2, scaled by one power of two;
+    // returns the factor of their scores.
+    auto put_q = [&](const PfItem& x) {
+      const int l8 = lane % LPR;
+      const int64_t at = row_at(x, A.a.q_stride);
+      auto from = [&](int u) { return __shfl_sync(0xffffffffu, (long long)at, u * RPL + lane / LPR) + l8 * 8; };
+      auto dst = [&](int u) { return qdst + pf_piece((warp & 3) * 32 + u * RPL + lane / LPR, l8); };
+      float down, fac;
+      if (A.a.q_dtype == BUDDY_DTYPE_BF16) {
+        const bf16* src = (const bf16*)A.a.q;
+        uint4 raw[32 / RPL];                            // all of them in flight
 #pragma unroll
-      for (int u = 0; u < 32 / RPL; ++u) {
-        const int64_t src = __shfl_sync(0xffffffffu, (long long)at, u * RPL + lane / LPR) + (lane % LPR) * 8;
-        raw[u] = want ? __ldg(reinterpret_cast<const uint4*>((const bf16*)A.a.q + src)) : make_uint4(0, 0, 0, 0);
+        for (int u = 0; u < 32 / RPL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>(src + from(u)));
+        __nv_bfloat162 top = __float2bfloat162_rn(0.f);
+        auto b2 = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+#pragma unroll
+        for (int u = 0; u < 32 / RPL; ++u) {
+          top = __hmax2(top, __hmax2(__habs2(b2(raw[u].x)), __habs2(b2(raw[u].y))));
+          top = __hmax2(top, __hmax2(__habs2(b2(raw[u].z)), __habs2(b2(raw[u].w))));
+        }
+        row_scale(warp_max(fmaxf(__low2float(top), __high2float(top))), base, &down, &fac);
+#pragma unroll
+        for (int u = 0; u < 32 / RPL; ++u) {
+          const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            h[e] = h2(__floats2half2_rn(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xFFFF0000u) * down));
+          *reinterpret_cast<uint4*>(dst(u)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+      } else {
+        const float* src = (const float*)A.a.q;
+        float top = 0.f;
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 2
+          for (int u = 0; u < 32 / RPL; ++u) {
+            float v[8];
+            load8(src + from(u), v);
+            if (pass == 0) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+            } else {
+              uint32_t h[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) h[e] = h2(__floats2half2_rn(v[2 * e] * down, v[2 * e + 1] * down));
+              *reinterpret_cast<uint4*>(dst(u)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+          }
+          if (pass == 0) row_scale(warp_max(top), base, &down, &fac);
+        }
       }
+      __syncwarp();
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      ptx::mbar_arrive(&q_ready[q]);
+      return fac;
     };
     bool go = take(0);
-    fetch_q(s_item[0], go);
     while (go) {
       const PfItem& it = s_item[I & 1];
       const int len = it.len();
       bool ok = true;
       if (q >= it.tiles()) {
         go = take(I + 1);
-        fetch_q(s_item[(I + 1) & 1], go);
+        if (go) fetch_q(s_item[(I + 1) & 1]);
       } else {
         // ----------------------------------------------------------- softmax
-        // (what only the beginning or the end needs is worked out there: the tiles need the
-        // registers)
-        uint8_t* const qdst = sQ + (size_t)q * TILE;
+        // (what only the end needs is worked out there: the tiles need the registers)
         const int rt = (warp & 3) * 32 + lane;          // row of the tile
         auto seen_by = [&]() {                          // positions this lane's row sees (may be <= 0)
           return it.n - it.m + min(it.row0 + q * kPfRows + rt, it.R - 1) / G + 1;
         };
-        {
-          const int l8 = lane % LPR;
-          auto put_q = [&](int r, const float* v) {
-            float top = 0.f, down, fac;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-#pragma unroll
-            for (int o = LPR / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            row_scale(top, A.a.scale, HD, &down, &fac);
-            if (l8 == 0) s_fac[q * kPfRows + r] = fac;
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = h2(__floats2half2_rn(v[2 * e] * down, v[2 * e + 1] * down));
-            *reinterpret_cast<uint4*>(qdst + pf_piece(r, l8)) = make_uint4(w[0], w[1], w[2], w[3]);
-          };
-          const int w0 = (warp & 3) * 32 + lane / LPR;
-          if (A.a.q_dtype == BUDDY_DTYPE_BF16) {
-#pragma unroll
-            for (int u = 0; u < 32 / RPL; ++u) {
-              const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-              float v[8];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-              put_q(w0 + u * RPL, v);
-            }
-          } else {
-            const int64_t at = row_at(it, A.a.q_stride);
-            auto from = [&](int r) { return __shfl_sync(0xffffffffu, (long long)at, r + lane / LPR) + l8 * 8; };
-#pragma unroll 1
-            for (int r0 = 0; r0 < 32; r0 += 4 * RPL) {
-              float v[4][8];
-#pragma unroll
-              for (int u = 0; u < 4; ++u) load8((const float*)A.a.q + from(r0 + u * RPL), v[u]);
-#pragma unroll
-              for (int u = 0; u < 4; ++u) put_q(w0 + r0 + u * RPL, v[u]);
-            }
-          }
-          __syncwarp();
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          ptx::mbar_arrive(&q_ready[q]);
-        }
-        const float fac = s_fac[q * kPfRows + rt];
+        const float fac = put_q(it);
         const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t ts = tq + (uint32_t)q * 128u, to = tq + kO + (uint32_t)q * 128u;
         const int seen = seen_by();
@@ -393,8 +392,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           }
           if (there != 0x03030303u) {
 #pragma unroll
-            for (int i = 0; i < kPfKeys; ++i)
-              if (!((there >> (8 * (i >> 5) + ((i >> 4) & 1))) & 1)) s[i] = 0xff800000u;
+            for (int i = 0; i < kPfKeys; i += 16)
+              if (!((there >> (8 * (i >> 5) + ((i >> 4) & 1))) & 1))
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[i + e] = 0xff800000u;
           }
           float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         }
         if (ok) {
           go = take(I + 1);
-          fetch_q(s_item[(I + 1) & 1], go);
+          if (go) fetch_q(s_item[(I + 1) & 1]);
           ok = __all_sync(0xffffffffu,
                           ptx::mbar_wait_bounded(&o_full[q], (q == 0 ? I : I1) & 1, kWaitLimitNs, &abort_flag));
         }
@@ -477,7 +478,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
                     make_uint4(tca::pack_bf16(o[i], o[i + 1]), tca::pack_bf16(o[i + 2], o[i + 3]),
                                tca::pack_bf16(o[i + 4], o[i + 5]), tca::pack_bf16(o[i + 6], o[i + 7]));
             } else if (it.row0 + q * kPfRows + rt < it.R) {
-              pf_store_row32(A, out_at + c, o);
+              float4* d = reinterpret_cast<float4*>((float*)A.a.out + out_at + c);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
           }
           if (staged) {
@@ -491,6 +494,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
                 *reinterpret_cast<uint4*>((bf16*)A.a.out + dst) =
                     *reinterpret_cast<const uint4*>(qdst + pf_piece((warp & 3) * 32 + r, c));
             }
+            __syncwarp();
           }
         }
       }
@@ -528,12 +532,14 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
             ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, p + 8u * x, v + x * (2048 >> 4), id_o,
                              (!first || x > 0) ? 1u : 0u);
         };
-        ok = wait(&q_ready[0], I) && (nq == 1 || wait(&q_ready[1], I1)) && wait(&k_full[T & 1], T >> 1);
-        if (ok) {
+        ok = wait(&k_full[T & 1], T >> 1);
+        for (int q = 0; q < nq && ok; ++q) {
+          ok = wait(&q_ready[q], q == 0 ? I : I1);
+          if (!ok) break;
           ptx::tc_fence_after();
-          for (int q = 0; q < nq; ++q) qk(q, T);
-          ptx::mma_commit(&k_empty[T & 1]);
+          qk(q, T);
         }
+        if (ok) ptx::mma_commit(&k_empty[T & 1]);
         for (int jj = 0; jj < len && ok; ++jj) {
           const bool more = jj + 1 < len;
           const uint32_t u = T + jj;
@@ -719,11 +725,12 @@ __global__ void __launch_bounds__(2 * kPfRows) kv4_join_kernel(const AttnArgs4 A
     float m[N], l[N], v[N][4], to = M;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const float* p = part(min(k0 + k, c.spans - 1));
-      m[k] = k0 + k < c.spans ? p[0] : -INFINITY;
-      l[k] = p[2 * kPfRows];
+      const bool in = k0 + k < c.spans;
+      const float* p = part(k0 + k);
+      m[k] = in ? p[0] : -INFINITY;
+      l[k] = in ? p[2 * kPfRows] : 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[k][i] = p[(2 + ch + i) * 2 * kPfRows];
+      for (int i = 0; i < 4; ++i) v[k][i] = in ? p[(2 + ch + i) * 2 * kPfRows] : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) to = fmaxf(to, m[k]);
