@@ -383,24 +383,34 @@ class Context:
 _DTYPES = {torch.float32: BUDDY_DTYPE_F32, torch.bfloat16: BUDDY_DTYPE_BF16, torch.float16: BUDDY_DTYPE_F16}
 
 
-def _at(t: Optional[torch.Tensor], dtype, n: int, what: str) -> Optional[int]:
-    """Address of a contiguous CUDA tensor of `n` elements or more."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
-        raise ValueError(f"{what}: a contiguous CUDA tensor of {n} or more {dtype} is wanted")
-    return t.data_ptr()
+def _vectors(*wanted):
+    """Checks (tensor, type, elements, name) of contiguous CUDA tensors; None is left out."""
+    for t, dtype, n, what in wanted:
+        if t is not None and (t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < n):
+            raise ValueError(f"{what}: a contiguous CUDA tensor of {n} or more {dtype} is wanted")
 
 
-def _heads(t: torch.Tensor, tokens: int, dim: int, what: str) -> int:
-    """Elements from token to token of a [tokens, heads, dim] view with whole heads."""
-    if not t.is_cuda or t.dim() != 3:
-        raise ValueError(f"{what}: a CUDA tensor [tokens, heads, head_dim] is wanted")
-    n, h, d = t.shape
+def _heads(t: torch.Tensor, dtype, shape, what: str) -> int:
+    """Elements from token to token of a [tokens, heads, head_dim] view with whole heads."""
     s = t.stride()
-    if n != tokens or d != dim or s[2] != 1 or (h > 1 and s[1] != d):
-        raise ValueError(f"{what}: [{tokens}, heads, {dim}] with whole heads one after the other is wanted")
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or s[2] != 1 or (s[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{what}: CUDA {dtype} {tuple(shape)} with whole heads one after the other is wanted")
     return s[0]
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(t: torch.Tensor, stream) -> int:
+    """The stream given, or the current one of t's device (asked for directly: the
+    Stream object takes longer to make than a launch)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(t.get_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+
+def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def buddy_rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None):
@@ -416,37 +426,41 @@ def buddy_page_plan(length: torch.Tensor, n_new: torch.Tensor, page_size: int, t
                     slot: torch.Tensor, pos: torch.Tensor, free_head_out: torch.Tensor,
                     flags: Optional[torch.Tensor] = None, stream=None):
     """Block tables, slots and positions of a call's new tokens from the lengths."""
-    B, i32 = length.numel(), torch.int32
-    if table.dim() != 2 or table.shape[0] != B:
+    B, T, i32 = length.numel(), slot.numel(), torch.int32
+    _vectors((length, i32, B, "length"), (n_new, i32, B, "n_new"), (table, i32, 0, "table"),
+             (free_pages, i32, 0, "free_pages"), (free_head, i32, 1, "free_head"), (kv_len, i32, B, "kv_len"),
+             (row_start, i32, B + 1, "row_start"), (slot, torch.int64, T, "slot"), (pos, i32, T, "pos"),
+             (free_head_out, i32, 1, "free_head_out"), (flags, i32, 1, "flags"))
+    rows = table.shape
+    if len(rows) != 2 or rows[0] != B:
         raise ValueError("table: [batch, max_pages] is wanted")
-    T = slot.numel()
-    a = buddy_page_plan_args(B, page_size, table.shape[1], free_pages.numel(), T, _at(length, i32, B, "length"),
-                             _at(n_new, i32, B, "n_new"), _at(table, i32, 0, "table"),
-                             _at(free_pages, i32, 0, "free_pages"), _at(free_head, i32, 1, "free_head"),
-                             _at(kv_len, i32, B, "kv_len"), _at(row_start, i32, B + 1, "row_start"),
-                             _at(slot, torch.int64, T, "slot"), _at(pos, i32, T, "pos"),
-                             _at(free_head_out, i32, 1, "free_head_out"))
-    _check(load_library().buddy_page_plan(a, _at(flags, i32, 1, "flags"), _stream(stream)), "buddy_page_plan")
+    a = buddy_page_plan_args(B, page_size, rows[1], free_pages.numel(), T, length.data_ptr(), n_new.data_ptr(),
+                             table.data_ptr(), free_pages.data_ptr(), free_head.data_ptr(), kv_len.data_ptr(),
+                             row_start.data_ptr(), slot.data_ptr(), pos.data_ptr(), free_head_out.data_ptr())
+    _check(load_library().buddy_page_plan(a, _addr(flags), _stream_of(length, stream)), "buddy_page_plan")
 
 
-def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps) -> buddy_qk_rows:
-    T, nkv, hd = k.shape
-    dt, f32 = k.dtype, torch.float32
-    nq = 0 if q is None else q.shape[1]
-    for t in (q, q_out, k_out):
-        if t is not None and t.dtype is not dt:
-            raise ValueError("queries, keys and outputs are of one type")
-    if nq and (q_out is None or q_out.shape[1] != nq) or k_out is not None and k_out.shape[1] != nkv:
-        raise ValueError("outputs have the heads of their inputs")
+def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags) -> buddy_qk_rows:
+    dt, shape, f32 = k.dtype, k.shape, torch.float32
+    if len(shape) != 3 or dt not in _DTYPES:
+        raise ValueError("k: [tokens, heads, head_dim] of fp32 or bf16 is wanted")
+    T, nkv, hd = shape
+    k_stride = _heads(k, dt, shape, "k")
+    k_out_stride = 0 if k_out is None else _heads(k_out, dt, shape, "k_out")
+    nq = q_stride = q_out_stride = 0
+    if q is not None:
+        nq = q.size(1)
+        q_stride = _heads(q, dt, (T, nq, hd), "q")
+        if q_out is None:
+            raise ValueError("q_out is wanted with q")
+        q_out_stride = _heads(q_out, dt, (T, nq, hd), "q_out")
     co, si = rope
-    rows = co.shape[0]
-    return buddy_qk_rows(T, nq, nkv, hd, _DTYPES.get(dt, -1), rows, eps, q.data_ptr() if nq else None, k.data_ptr(),
-                         _heads(q, T, hd, "q") if nq else 0, _heads(k, T, hd, "k"), _at(q_gain, f32, hd, "q_gain"),
-                         _at(k_gain, f32, hd, "k_gain"), _at(pos, torch.int32, T, "pos"),
-                         _at(co, f32, rows * hd // 2, "cos"), _at(si, f32, rows * hd // 2, "sin"),
-                         q_out.data_ptr() if nq else None, None if k_out is None else k_out.data_ptr(),
-                         _heads(q_out, T, hd, "q_out") if nq else 0,
-                         0 if k_out is None else _heads(k_out, T, hd, "k_out"))
+    rows = co.size(0)
+    _vectors((q_gain, f32, hd, "q_gain"), (k_gain, f32, hd, "k_gain"), (pos, torch.int32, T, "pos"),
+             (co, f32, rows * hd // 2, "cos"), (si, f32, rows * hd // 2, "sin"), (flags, torch.int32, 1, "flags"))
+    return buddy_qk_rows(T, nq, nkv, hd, _DTYPES[dt], rows, eps, _addr(q), k.data_ptr(), q_stride, k_stride,
+                         _addr(q_gain), _addr(k_gain), pos.data_ptr(), co.data_ptr(), si.data_ptr(),
+                         _addr(q_out) if nq else None, _addr(k_out), q_out_stride, k_out_stride)
 
 
 def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Tensor, rope, q_out, k_out,
@@ -454,9 +468,8 @@ def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Te
                        eps: float = 1e-6, flags: Optional[torch.Tensor] = None, stream=None):
     """Norm of each query and key head (with gains) and rotation, in one pass.
     q, k, q_out, k_out: [tokens, heads, head_dim], fp32 or bf16; rope: (cos, sin)."""
-    r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps)
-    _check(load_library().buddy_qk_norm_rope(r, _at(flags, torch.int32, 1, "flags"), _stream(stream)),
-           "buddy_qk_norm_rope")
+    r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags)
+    _check(load_library().buddy_qk_norm_rope(r, _addr(flags), _stream_of(k, stream)), "buddy_qk_norm_rope")
 
 
 class KV4Cache:
@@ -474,8 +487,8 @@ class KV4Cache:
         if not self.head_dim:
             raise ValueError("a block holds page_size * (hd / 2 + hd / 16) bytes, hd 64 or 128")
         self.k_pages, self.v_pages, self.page_size, self.n_kv = k_pages, v_pages, page_size, n_kv
-        self.state = buddy_kv4_cache(_at(k_pages, torch.uint8, 0, "k_pages"), _at(v_pages, torch.uint8, 0, "v_pages"),
-                                     n_pages, page_size, n_kv, self.head_dim)
+        _vectors((k_pages, torch.uint8, 0, "k_pages"), (v_pages, torch.uint8, 0, "v_pages"))
+        self.state = buddy_kv4_cache(k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size, n_kv, self.head_dim)
         self.lib = load_library()
         self.workspace = workspace
         self._made: List = []           # workspaces made here; calls under way may still use an older one
@@ -502,45 +515,47 @@ class KV4Cache:
                          eps: float = 1e-6, flags: Optional[torch.Tensor] = None,
                          k_out: Optional[torch.Tensor] = None, stream=None):
         """buddy_qk_norm_rope, with the keys and values v stored at `slot`."""
-        r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps)
-        T = k.shape[0]
-        if v.dtype is not k.dtype or v.shape != k.shape:
-            raise ValueError("v: type and shape of k are wanted")
-        _check(self.lib.buddy_kv4_append(self.state, r, _ptr(v), _heads(v, T, k.shape[2], "v"),
-                                         _at(slot, torch.int64, T, "slot"), _at(flags, torch.int32, 1, "flags"),
-                                         _stream(stream)), "buddy_kv4_append")
+        r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags)
+        _vectors((slot, torch.int64, r.n_tok, "slot"))
+        _check(self.lib.buddy_kv4_append(self.state, r, v.data_ptr(), _heads(v, k.dtype, k.shape, "v"), slot.data_ptr(),
+                                         _addr(flags), _stream_of(k, stream)), "buddy_kv4_append")
 
     def buddy_kv4_read(self, slot: torch.Tensor, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor],
                        flags: Optional[torch.Tensor] = None, stream=None):
         """The values stored at `slot`: [n, n_kv, head_dim] of fp32, fp16 or bf16."""
         n = slot.numel()
         out = k_out if k_out is not None else v_out
-        if out is None or out.dtype not in _DTYPES:
+        dt = None if out is None else out.dtype
+        if dt not in _DTYPES:
             raise ValueError("k_out, v_out: fp32, fp16 or bf16 is wanted")
         size = n * self.n_kv * self.head_dim
-        _check(self.lib.buddy_kv4_read(self.state, n, _at(slot, torch.int64, n, "slot"), _DTYPES[out.dtype],
-                                       _at(k_out, out.dtype, size, "k_out"), _at(v_out, out.dtype, size, "v_out"),
-                                       _at(flags, torch.int32, 1, "flags"), _stream(stream)), "buddy_kv4_read")
+        _vectors((slot, torch.int64, n, "slot"), (k_out, dt, size, "k_out"), (v_out, dt, size, "v_out"),
+                 (flags, torch.int32, 1, "flags"))
+        _check(self.lib.buddy_kv4_read(self.state, n, slot.data_ptr(), _DTYPES[dt], _addr(k_out), _addr(v_out),
+                                       _addr(flags), _stream_of(slot, stream)), "buddy_kv4_read")
 
     def buddy_kv4_attention(self, q: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, out: torch.Tensor,
                             row_start: Optional[torch.Tensor] = None, max_new: int = 1, scale: float = 0.0,
                             flags: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                             stream=None):
         """Causal attention of query tokens over the cache; q, out [tokens, n_q, head_dim]."""
-        T, nq, hd = q.shape
-        B, i32 = kv_len.numel(), torch.int32
-        if hd != self.head_dim or out.shape != q.shape or table.dim() != 2 or table.shape[0] != B:
-            raise ValueError("q, out: [tokens, heads, head_dim of the cache], table: [batch, max_pages] are wanted")
+        shape, B, i32 = q.shape, kv_len.numel(), torch.int32
+        if len(shape) != 3 or shape[2] != self.head_dim:
+            raise ValueError("q: [tokens, heads, head_dim of the cache] is wanted")
+        T, nq, _ = shape
+        q_stride, out_stride = _heads(q, q.dtype, shape, "q"), _heads(out, out.dtype, shape, "out")
         ws = workspace if workspace is not None else self.workspace
         if ws is None:
             need = self.workspace_bytes(nq, max_new)
             if not self._made or self._made[-1].numel() < need:
                 self._made.append(torch.zeros(need, dtype=torch.uint8, device=q.device))
             ws = self._made[-1]
-        a = buddy_kv4_attention_args(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1),
-                                     table.shape[1], scale, q.data_ptr(), out.data_ptr(), _heads(q, T, hd, "q"),
-                                     _heads(out, T, hd, "out"), _at(row_start, i32, B + 1, "row_start"),
-                                     _at(kv_len, i32, B, "kv_len"), _at(table, i32, 0, "table"), ws.data_ptr(),
-                                     ws.numel())
-        _check(self.lib.buddy_kv4_attention(self.state, a, _at(flags, i32, 1, "flags"), _stream(stream)),
-               "buddy_kv4_attention")
+        _vectors((row_start, i32, B + 1, "row_start"), (kv_len, i32, B, "kv_len"), (table, i32, 0, "table"),
+                 (ws, torch.uint8, 0, "workspace"), (flags, i32, 1, "flags"))
+        rows = table.shape
+        if len(rows) != 2 or rows[0] != B:
+            raise ValueError("table: [batch, max_pages] is wanted")
+        a = buddy_kv4_attention_args(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1), rows[1],
+                                     scale, q.data_ptr(), out.data_ptr(), q_stride, out_stride, _addr(row_start),
+                                     kv_len.data_ptr(), table.data_ptr(), ws.data_ptr(), ws.numel())
+        _check(self.lib.buddy_kv4_attention(self.state, a, _addr(flags), _stream_of(q, stream)), "buddy_kv4_attention")

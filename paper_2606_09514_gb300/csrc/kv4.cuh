@@ -45,17 +45,6 @@ __device__ __forceinline__ __half scale_of(uint32_t amax_bits) {
 // Nibble of the code word that holds channel e of eight.
 __host__ __device__ constexpr int nibble_of(int e) { return (e & 1) ? 4 + (e >> 1) : e >> 1; }
 
-// Code word of eight channels under scale s (0 and NaN: every code 8).
-__device__ __forceinline__ uint32_t encode8(const float* x, float s) {
-  uint32_t w = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float n = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x[e], s)), -7.f), 7.f) : 0.f;
-    w |= (uint32_t)((int)n + 8) << (4 * nibble_of(e));
-  }
-  return w;
-}
-
 __device__ __forceinline__ float decode(uint32_t w, int e, float s) {
   return (float)((int)((w >> (4 * nibble_of(e))) & 15u) - 8) * s;
 }

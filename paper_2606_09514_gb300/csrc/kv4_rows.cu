@@ -3,17 +3,18 @@
 // entries quantised into the paged 4-bit cache (buddy_kv4_append), and entries read
 // back (buddy_kv4_read).
 //
-// A team of HD / 8 lanes holds a head, eight channels per lane in one 16-byte load:
-// the channel that the rotation pairs with is in the lane HD / 16 further on, a
-// scale's 32 channels are four lanes, and a lane's eight codes are one word.  A team
-// takes kRowHeads consecutive heads of a token, all loaded before the first is used,
-// so that the token's position and rotation factors are read once for them.
+// A team of HD / 16 lanes holds a head: a lane has eight neighbours of the lower half and
+// the eight of the upper half that the rotation pairs them with, each in one 16-byte load
+// (bf16).  A scale's 32 channels are four lanes, a lane's eight codes are one word.  A
+// team takes consecutive heads of a token, one loaded while the one before is worked on, so
+// that the token's position, slot and rotation factors are read once for them.
 //
-// The sum of squares: within a lane halves of the eight onto each other, then
-// halves of the lanes; products and sums rounded one by one (no fused
-// multiply-adds), so that a plain program can follow it bit by bit, which the codes
-// need: where a value lies between two codes, one bit decides.
+// The sum of squares: within the eights halves onto each other, then halves of the
+// eights; products and sums rounded one by one (no fused multiply-adds), so that a plain program can follow it bit by bit, which the
+// codes need: where a value lies between two codes, one bit decides.
 #include <cuda_runtime.h>
+
+#include <algorithm>
 
 #include "common.cuh"
 #include "internal.h"
@@ -21,8 +22,7 @@
 
 namespace buddy {
 
-constexpr int kRowThreads = 256;
-constexpr int kRowHeads = 4;
+constexpr int kRowThreads = 128;
 
 struct RowArgs {
   buddy_qk_rows r;
@@ -31,6 +31,7 @@ struct RowArgs {
   kv4::Pages pages;
   const int64_t* slot;
   int32_t* flags;
+  int per, groups;             // heads of a team, teams of a token
 };
 
 __device__ __forceinline__ void store8(float* p, const float* x) {
@@ -50,119 +51,220 @@ __device__ __forceinline__ void store8(__half* p, const float* x) {
   *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
 }
 
-// Every lane's x of the head becomes x / sqrt(mean(x^2) + eps) * gain.
-template <int HD>
-__device__ __forceinline__ void norm_head(float* x, const float* gain, float eps) {
-  float q[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = __fmul_rn(x[e], x[e]);
-#pragma unroll
-  for (int n = 4; n > 0; n >>= 1)
-#pragma unroll
-    for (int e = 0; e < n; ++e) q[e] = __fadd_rn(q[e], q[e + n]);
-#pragma unroll
-  for (int o = HD / 16; o > 0; o >>= 1) q[0] = __fadd_rn(q[0], __shfl_xor_sync(0xffffffffu, q[0], o));
-  const float r = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fmul_rn(q[0], 1.f / HD), eps)));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = __fmul_rn(__fmul_rn(x[e], r), gain[e]);
+// Two fp32 at once, each rounded as alone.
+struct F2 {
+  uint64_t v;
+  __device__ __forceinline__ F2() {}
+  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+// Products that a sum takes, one by one: the assembler makes fused multiply-adds of a packed
+// product and a packed sum, rounding modifiers or not.
+__device__ __forceinline__ F2 products(F2 a, F2 b) {
+  float a0, a1, b0, b1;
+  a.get(a0, a1);
+  b.get(b0, b1);
+  return F2(__fmul_rn(a0, b0), __fmul_rn(a1, b1));
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 neg(F2 a) {
+  F2 r;
+  r.v = a.v ^ 0x8000000080000000ull;
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if one is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 
-template <int HD>
-__device__ __forceinline__ void turn_head(float* x, const float* co, const float* si, bool low) {
+// Eight consecutive elements as they lie in memory.
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const bf16* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void get(F2* o) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float y = __shfl_xor_sync(0xffffffffu, x[e], HD / 16);
-    const float a = __fmul_rn(x[e], co[e]), b = __fmul_rn(y, si[e]);
-    x[e] = low ? __fsub_rn(a, b) : __fadd_rn(a, b);
+    for (int i = 0; i < 4; ++i) o[i] = F2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
   }
+};
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldg(reinterpret_cast<const float4*>(p));
+    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void get(F2* o) const {
+    o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
+  }
+};
+__device__ __forceinline__ void load8(const float* p, F2* o) {
+  Raw8<float> r;
+  r.load(p);
+  r.get(o);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const F2* x) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i].get(y[2 * i], y[2 * i + 1]);
+  store8(p, y);
 }
 
-// The lane's eight channels into an entry at byte `at` of `pages`; whole teams call it.
-template <int HD>
-__device__ __forceinline__ void store_entry(uint8_t* pages, int64_t block, int row, int shift, int tl, const float* x,
-                                            bool real) {
-  uint32_t m = 0;
+// Sum of the squares of eight values, halves onto each other.
+__device__ __forceinline__ float squares8(const F2* x) {
+  const F2 a = products(x[0], x[0]) + products(x[2], x[2]), b = products(x[1], x[1]) + products(x[3], x[3]), c = a + b;
+  float u, v;
+  c.get(u, v);
+  return __fadd_rn(u, v);
+}
+
+// Eight channels of a group of 32 (four lanes, all of `mask`) into code word and scale.
+// The quotients are the correctly rounded ones: with y = 1 / s correctly rounded, q = x y
+// and r = x - q s, q + r y rounds to x / s (P. Markstein, IBM J. Res. Dev. 34 (1990), theorem
+// on the last step of a division by multiplications).  Adding 1.5 * 2^23 + 8 rounds one to an integer (ties
+// to even) and leaves its code in the low bits.
+__device__ __forceinline__ uint32_t encode8(const F2* x, uint32_t mask, __half* scale) {
+  float v[8], m = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-  const __half s = kv4::scale_of(m);
-  if (!real) return;
-  uint8_t* b = pages + block;
-  *reinterpret_cast<uint32_t*>(b + row * kv4::code_bytes(HD) + 4 * tl) = kv4::encode8(x, __half2float(s));
-  if ((tl & 3) == 0)
-    *reinterpret_cast<__half*>(b + ((int64_t)kv4::code_bytes(HD) << shift) + row * kv4::scale_bytes(HD) + (tl >> 1)) = s;
+  for (int i = 0; i < 4; ++i) {
+    x[i].get(v[2 * i], v[2 * i + 1]);
+    m = max_nan(m, max_nan(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));
+  }
+  m = max_nan(m, __shfl_xor_sync(mask, m, 1));
+  m = max_nan(m, __shfl_xor_sync(mask, m, 2));
+  *scale = kv4::scale_of(__float_as_uint(m));
+  const float s = __half2float(*scale);
+  if (!(s > 0.f)) return 0x88888888u;
+  const float y = __frcp_rn(s);
+  // a scale at its limit, or rounded among the smallest halves: larger quotients than 7 are there
+  const bool clamp = s >= kv4::kMaxScale || s < 7.62939453125e-6f;
+  const F2 s2(-s, -s), y2(y, y), magic(12582920.f, 12582920.f);
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    F2 z = x[i];
+    if (clamp) {
+      const float top = 7.f * s;
+      z = F2(fminf(fmaxf(v[2 * i], -top), top), fminf(fmaxf(v[2 * i + 1], -top), top));
+    }
+    const F2 q = z * y2, n = fma2(fma2(q, s2, z), y2, q) + magic;
+    float lo, hi;
+    n.get(lo, hi);
+    w |= (__byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410) & 0x000F000Fu) << (4 * i);
+  }
+  return w;
 }
 
 template <typename T, int HD, bool CACHE>
 __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A) {
-  constexpr int LPH = HD / 8, TEAMS = kRowThreads / LPH;
+  constexpr int LPH = HD / 16, HALF = HD / 2;
   const buddy_qk_rows& R = A.r;
-  const int heads = R.n_q_heads + R.n_kv_heads * (CACHE ? 2 : 1);
-  const int groups = (heads + kRowHeads - 1) / kRowHeads;
+  const int kq = R.n_q_heads, kk = kq + R.n_kv_heads, heads = kk + (CACHE ? R.n_kv_heads : 0);
   const int tl = threadIdx.x % LPH;
-  const int64_t u = (int64_t)blockIdx.x * TEAMS + threadIdx.x / LPH;
-  const int t = (int)min(u / groups, (int64_t)R.n_tok - 1);
-  const bool there = u < (int64_t)R.n_tok * groups;
-  const int h0 = (int)(u % groups) * kRowHeads;
+  const uint32_t team = ((1u << LPH) - 1) << (threadIdx.x % 32 / LPH * LPH);   // this team's lanes
+  const int64_t u = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / LPH;
+  const int64_t t = u / A.groups;
+  if (t >= R.n_tok) return;                     // (whole teams)
+  const int h0 = (int)(u - t * A.groups) * A.per, h1 = min(h0 + A.per, heads);
 
+  const int c = tl * 8;                         // this lane's channels: c .. c + 7 of both halves
+  auto row = [&](int h) -> const T* {
+    if (h < kq) return (const T*)R.q + t * R.q_stride + (int64_t)h * HD + c;
+    if (!CACHE || h < kk) return (const T*)R.k + t * R.k_stride + (int64_t)(h - kq) * HD + c;
+    return (const T*)A.v + t * A.v_stride + (int64_t)(h - kk) * HD + c;
+  };
+  Raw8<T> lo, hi;
+  const T* src = row(h0);
+  lo.load(src);
+  hi.load(src + HALF);
   const int p = R.pos[t];
-  const bool ok = there && p >= 0 && p < R.max_pos;
   int64_t slot = -1;
   if (CACHE) slot = A.slot[t];
+  const bool ok = p >= 0 && p < R.max_pos;
   const int64_t end = (int64_t)A.pages.n_pages << A.pages.shift;
-  if (there && tl == 0 && h0 == 0 && A.flags) {
-    const int bad = (p >= R.max_pos ? BUDDY_DEV_BAD_POSITION : 0) |
-                    (CACHE && p >= 0 && slot >= end ? BUDDY_DEV_BAD_PAGE : 0);
+  if (tl == 0 && h0 == 0 && A.flags) {
+    const int bad = (p >= R.max_pos ? BUDDY_DEV_BAD_POSITION : 0) | (CACHE && ok && slot >= end ? BUDDY_DEV_BAD_PAGE : 0);
     if (bad) atomicOr(A.flags, bad);
   }
-  const bool keep = CACHE && ok && slot >= 0 && slot < end;
-
-  float x[kRowHeads][8];
-#pragma unroll
-  for (int i = 0; i < kRowHeads; ++i) {
-    int h = min(h0 + i, heads - 1);
-    const T* src;
-    if (h < R.n_q_heads) src = (const T*)R.q + t * R.q_stride;
-    else if ((h -= R.n_q_heads) < R.n_kv_heads) src = (const T*)R.k + t * R.k_stride;
-    else h -= R.n_kv_heads, src = (const T*)A.v + t * A.v_stride;
-    load8(src + (int64_t)h * HD + tl * 8, x[i]);
+  if (!ok) return;
+  const bool keep = CACHE && slot >= 0 && slot < end;
+  F2 co[4], si[4];
+  if (h0 < kk) {
+    load8(R.rope_cos + (int64_t)p * HALF + c, co);
+    load8(R.rope_sin + (int64_t)p * HALF + c, si);
   }
-  float co[8], si[8];
-  const bool low = tl < LPH / 2;
-  {
-    const int64_t at = (int64_t)(ok ? p : 0) * (HD / 2) + (low ? tl : tl - LPH / 2) * 8;
-    load8(R.rope_cos + at, co);
-    load8(R.rope_sin + at, si);
-  }
-#pragma unroll
-  for (int i = 0; i < kRowHeads; ++i) {
-    const int h = h0 + i;
-    const bool is_q = h < R.n_q_heads, is_v = h >= R.n_q_heads + R.n_kv_heads;
-    const bool real = ok && h < heads;
-    const float* gains = is_q ? R.q_gain : R.k_gain;
-    // (a warp may hold teams of both kinds: all lanes take part in the shuffles)
-    float y[8], gain[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x[i][e], gain[e] = 1.f;
-    if (gains) load8(gains + tl * 8, gain);
-    norm_head<HD>(y, gain, R.eps);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = gains ? y[e] : x[i][e];
-    turn_head<HD>(y, co, si, low);
-    if (is_q) {
-      if (real) store8((T*)R.q_out + t * R.q_out_stride + (int64_t)h * HD + tl * 8, y);
-    } else if (!is_v) {
-      if (real && R.k_out) store8((T*)R.k_out + t * R.k_out_stride + (int64_t)(h - R.n_q_heads) * HD + tl * 8, y);
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    F2 a[4], b[4];                              // lower and upper half
+    lo.get(a);
+    hi.get(b);
+    if (h + 1 < h1) {
+      src = row(h + 1);
+      lo.load(src);
+      hi.load(src + HALF);
     }
-    if (CACHE) {
-      const int g = is_v ? h - R.n_q_heads - R.n_kv_heads : h - R.n_q_heads;
+    if (!CACHE || h < kk) {
+      const float* gains = h < kq ? R.q_gain : R.k_gain;
+      if (gains) {
+        float sum = __fadd_rn(squares8(a), squares8(b));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = is_v ? x[i][e] : y[e];
-      const bool put = keep && real && !is_q;
-      const int64_t block = put ? kv4::block_at<HD>(A.pages, slot >> A.pages.shift, g) : 0;
-      store_entry<HD>(is_v ? A.pages.v : A.pages.k, block, (int)(slot & ((1 << A.pages.shift) - 1)), A.pages.shift, tl,
-                      y, put);
+        for (int o = LPH / 2; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(team, sum, o));
+        const float r = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.f / HD), R.eps)));
+        const F2 r2(r, r);
+        F2 ga[4], gb[4];
+        load8(gains + c, ga);
+        load8(gains + HALF + c, gb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = a[i] * r2 * ga[i], b[i] = b[i] * r2 * gb[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const F2 ac = products(a[i], co[i]), bs = products(b[i], si[i]);
+        b[i] = products(b[i], co[i]) + products(a[i], si[i]);
+        a[i] = ac + neg(bs);
+      }
+      if (h < kq) {
+        T* d = (T*)R.q_out + t * R.q_out_stride + (int64_t)h * HD + c;
+        store8(d, a);
+        store8(d + HALF, b);
+        continue;
+      }
+      if (R.k_out) {
+        T* d = (T*)R.k_out + t * R.k_out_stride + (int64_t)(h - kq) * HD + c;
+        store8(d, a);
+        store8(d + HALF, b);
+      }
+    }
+    if (CACHE && keep) {
+      __half sa, sb;
+      const uint32_t wa = encode8(a, team, &sa), wb = encode8(b, team, &sb);
+      const int in_page = (int)(slot & ((1 << A.pages.shift) - 1));
+      uint8_t* blk = (h < kk ? A.pages.k : A.pages.v) + kv4::block_at<HD>(A.pages, slot >> A.pages.shift, h < kk ? h - kq : h - kk);
+      uint32_t* codes = reinterpret_cast<uint32_t*>(blk + in_page * kv4::code_bytes(HD)) + tl;
+      codes[0] = wa;
+      codes[HD / 16] = wb;
+      if (tl % 4 == 0) {
+        __half* sc = reinterpret_cast<__half*>(blk + ((int64_t)kv4::code_bytes(HD) << A.pages.shift) +
+                                               in_page * kv4::scale_bytes(HD)) + tl / 4;
+        sc[0] = sa;
+        sc[HD / 64] = sb;
+      }
     }
   }
 }
@@ -184,17 +286,24 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const kv4::Pages 
   }
   const int64_t block = kv4::block_at<HD>(P, slot >> P.shift, g);
   const int row = (int)(slot & ((1 << P.shift) - 1));
+  const int64_t code_at = block + row * kv4::code_bytes(HD) + 4 * tl;
+  const int64_t scale_at = block + ((int64_t)kv4::code_bytes(HD) << P.shift) + row * kv4::scale_bytes(HD) + (tl >> 2) * 2;
+  uint32_t w[2] = {0, 0};
+  float s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {   // both before the first is stored
+    if (!(i ? v_out : k_out)) continue;
+    const uint8_t* b = i ? P.v : P.k;
+    w[i] = *reinterpret_cast<const uint32_t*>(b + code_at);
+    s[i] = __half2float(*reinterpret_cast<const __half*>(b + scale_at));
+  }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     T* out = i ? v_out : k_out;
     if (!out) continue;
-    const uint8_t* b = (i ? P.v : P.k) + block;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(b + row * kv4::code_bytes(HD) + 4 * tl);
-    const float s = __half2float(*reinterpret_cast<const __half*>(b + ((int64_t)kv4::code_bytes(HD) << P.shift) +
-                                                                  row * kv4::scale_bytes(HD) + (tl >> 2) * 2));
     float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = kv4::decode(w, e, s);
+    for (int e = 0; e < 8; ++e) y[e] = kv4::decode(w[i], e, s[i]);
     store8(out + u * HD + tl * 8, y);
   }
 }
@@ -230,11 +339,15 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
   return {(uint8_t*)c->k_pages, (uint8_t*)c->v_pages, c->n_pages, shift, c->n_kv_heads};
 }
 
+// Heads of a team: one while there are few rows, for the shortest chain; more as they fill
+// the GPU (kRowTeams), up to eight, which share the reads of position and rotation.
+constexpr int64_t kRowTeams = 16384;
 template <typename T, int HD, bool CACHE>
-static int launch_rows(const RowArgs& A, cudaStream_t s) {
+static int launch_rows(RowArgs A, cudaStream_t s) {
   const int heads = A.r.n_q_heads + A.r.n_kv_heads * (CACHE ? 2 : 1);
-  const int64_t teams = (int64_t)A.r.n_tok * ((heads + kRowHeads - 1) / kRowHeads);
-  const int64_t ctas = (teams * (HD / 8) + kRowThreads - 1) / kRowThreads;
+  A.per = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)A.r.n_tok * heads / kRowTeams));
+  A.groups = (heads + A.per - 1) / A.per;
+  const int64_t ctas = ((int64_t)A.r.n_tok * A.groups * (HD / 16) + kRowThreads - 1) / kRowThreads;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   qk_rows_kernel<T, HD, CACHE><<<(unsigned)ctas, kRowThreads, 0, s>>>(A);
   return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
@@ -286,7 +399,7 @@ extern "C" int buddy_kv4_append(const buddy_kv4_cache* cache, const buddy_qk_row
     return BUDDY_ERR_ARG;
   if (rows->n_tok > 0 && (!slot || !aligned_rows(v, v_stride, rows->dtype == BUDDY_DTYPE_F32 ? 4 : 2)))
     return BUDDY_ERR_ARG;
-  const RowArgs A{*rows, v, v_stride, kv4_pages(cache), slot, flags};
+  const RowArgs A{*rows, v, v_stride, kv4_pages(cache), slot, flags, 0, 0};
   return dispatch_rows<true>(A, (cudaStream_t)stream);
 }
 
