@@ -166,7 +166,7 @@ __device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, int pag
   // at a sequence's end, and where a page is not there: zeros for what is not read
   const int64_t b0 = block_at<HD>(P, max(page0, 0), g), b1 = block_at<HD>(P, max(page1, 0), g);
   const int up = P.shift == 4 ? 0 : in_page + 16;   // where the upper 16 positions begin in their page
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < 2 * HALF; ++i) {
     const int r = i * (512 / CB) + lane / (CB / 16);
     const int64_t at = i < HALF ? b0 + in_page * CB + lane * 16 + 512 * i : b1 + up * CB + lane * 16 + 512 * (i - HALF);
@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
     put = put + 1 == kStages ? 0 : put + 1;
   };
   fetch_ids();
-#pragma unroll
+#pragma unroll 1
   for (int s = 0; s < kStages - 1; ++s) issue();
 
   // where a lane's codes and scales are in a stage: keys of row lg, values of rows 2 lc and 2 lc + 1
@@ -594,32 +594,50 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       if (s_last) {
         // first every row's M = max m and L = sum 2^(m - M) l over the spans, a warp per row;
         // then the outputs, eight spans' loads at a time
-        auto span = [&](int k) {
-          return A.part + (2 * (first_cta + k) + (k == 0 ? 1 : 0)) * partial_floats<HD, NB>();
-        };
+        constexpr int64_t PF = partial_floats<HD, NB>();
+        const float* p0 = A.part + (2 * first_cta + 1) * PF;      // the first span's partial, and the
+        const float* p1 = A.part + 2 * (first_cta + 1) * PF;      // second's; the others 2 PF apart
+        auto span = [&](int k) { return k == 0 ? p0 : p1 + (k - 1) * (2 * PF); };
+#pragma unroll 1
         for (int r = warp; r < rows; r += kWarps) {
           float M = -INFINITY, L = 0.f;
-          for (int k = lane; k < spans; k += 32) M = fmaxf(M, __ldcg(span(k) + r));
-          M = warp_max(M);
-          const float at = M == -INFINITY ? 0.f : M;
-          for (int k = lane; k < spans; k += 32)
-            L += __ldcg(span(k) + ROWS + r) * tca::exp2a(__ldcg(span(k) + r) - at);
-          L = warp_sum(L);
-          if (lane == 0) sM[r] = at, sL[r] = M == -INFINITY ? 0.f : 1.f / L;
+#pragma unroll 1
+          for (int k0 = 0; k0 < spans; k0 += 32) {
+            const float* p = span(min(k0 + lane, spans - 1)) + r;
+            const float m = __ldcg(p), l = __ldcg(p + ROWS);
+            const float to = fmaxf(M, m), a = to == -INFINITY ? 0.f : tca::exp2a(m - to);
+            L = L * (M == -INFINITY ? 0.f : tca::exp2a(M - to)) + (k0 + lane < spans ? l * a : 0.f);
+            M = to;
+          }
+          const float all = warp_max(M), at = all == -INFINITY ? 0.f : all;
+          L = warp_sum(M == -INFINITY ? 0.f : L * tca::exp2a(M - at));
+          if (lane == 0) sM[r] = at, sL[r] = all == -INFINITY ? 0.f : 1.f / L;
         }
         __syncthreads();
         const int items = rows * (HD / 4);
         // few rows: the spans go over as many groups of threads as there are
-        const int groups = max(1, kThreads / items), grp = tid / items;
-        for (int x = items >= kThreads ? tid : tid - grp * items; x < items; x += kThreads) {
-          if (items < kThreads && grp >= groups) break;
+        const int groups = items < kThreads ? kThreads / items : 1, grp = items < kThreads ? tid / items : 0;
+#pragma unroll 1
+        for (int x = tid - grp * items; x < items && grp < groups; x += kThreads) {
           const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
+          const float at = sM[r];
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-          for (int k = items < kThreads ? grp : 0; k < spans; k += groups) {
-            const float a = tca::exp2a(__ldcg(span(k) + r) - sM[r]);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(span(k) + 2 * ROWS + r * HD + ch));
-            v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
+#pragma unroll 1
+          for (int k0 = grp; k0 < spans; k0 += 8 * groups) {
+            float m[8];
+            float4 y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int k = k0 + i * groups;
+              const float* p = span(min(k, spans - 1));
+              m[i] = k < spans ? __ldcg(p + r) : -INFINITY;
+              y[i] = k < spans ? __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS + x * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float a = tca::exp2a(m[i] - at);
+              v.x += a * y[i].x, v.y += a * y[i].y, v.z += a * y[i].z, v.w += a * y[i].w;
+            }
           }
           if (groups == 1) {
             out4(r, ch, make_float4(v.x * sL[r], v.y * sL[r], v.z * sL[r], v.w * sL[r]));
