@@ -54,6 +54,7 @@ constexpr int kCtasPerSm = 3;
 constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
 constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
 constexpr int kMaxGrid = 1024;   // CTAs: three on each of at most 341 SMs
+constexpr int kJoin = 16;        // partials in flight when a cut stream is joined
 constexpr int kFewRows = 32;     // rows of a KV head up to which these kernels take a sequence
 
 template <int HD>
@@ -592,69 +593,68 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       }
       __syncthreads();
       if (s_last) {
-        // first every row's M = max m and L = sum 2^(m - M) l over the spans, a warp per row;
-        // then the outputs, eight spans' loads at a time
+        // kJoin spans' loads at a time into a running log-sum-exp
         constexpr int64_t PF = partial_floats<HD, NB>();
         const float* p0 = A.part + (2 * first_cta + 1) * PF;      // the first span's partial, and the
         const float* p1 = A.part + 2 * (first_cta + 1) * PF;      // second's; the others 2 PF apart
-        auto span = [&](int k) { return k == 0 ? p0 : p1 + (k - 1) * (2 * PF); };
-#pragma unroll 1
-        for (int r = warp; r < rows; r += kWarps) {
-          float M = -INFINITY, L = 0.f;
-#pragma unroll 1
-          for (int k0 = 0; k0 < spans; k0 += 32) {
-            const float* p = span(min(k0 + lane, spans - 1)) + r;
-            const float m = __ldcg(p), l = __ldcg(p + ROWS);
-            const float to = fmaxf(M, m), a = to == -INFINITY ? 0.f : tca::exp2a(m - to);
-            L = L * (M == -INFINITY ? 0.f : tca::exp2a(M - to)) + (k0 + lane < spans ? l * a : 0.f);
-            M = to;
-          }
-          const float all = warp_max(M), at = all == -INFINITY ? 0.f : all;
-          L = warp_sum(M == -INFINITY ? 0.f : L * tca::exp2a(M - at));
-          if (lane == 0) sM[r] = at, sL[r] = all == -INFINITY ? 0.f : 1.f / L;
-        }
-        __syncthreads();
         const int items = rows * (HD / 4);
         // few rows: the spans go over as many groups of threads as there are
         const int groups = items < kThreads ? kThreads / items : 1, grp = items < kThreads ? tid / items : 0;
 #pragma unroll 1
         for (int x = tid - grp * items; x < items && grp < groups; x += kThreads) {
           const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
-          const float at = sM[r];
+          float M = -INFINITY, L = 0.f;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-          for (int k0 = grp; k0 < spans; k0 += 8 * groups) {
-            float m[8];
-            float4 y[8];
+          for (int k0 = grp; k0 < spans; k0 += kJoin * groups) {
+            float m[kJoin], l[kJoin], to = M;
+            float4 y[kJoin];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kJoin; ++i) {
               const int k = k0 + i * groups;
-              const float* p = span(min(k, spans - 1));
-              m[i] = k < spans ? __ldcg(p + r) : -INFINITY;
-              y[i] = k < spans ? __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS + x * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+              const float* p = k == 0 ? p0 : p1 + (k - 1) * (2 * PF);
+              m[i] = -INFINITY, l[i] = 0.f, y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (k < spans) {
+                m[i] = __ldcg(p + r), l[i] = __ldcg(p + ROWS + r);
+                y[i] = __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS + x * 4));
+              }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float a = tca::exp2a(m[i] - at);
-              v.x += a * y[i].x, v.y += a * y[i].y, v.z += a * y[i].z, v.w += a * y[i].w;
+            for (int i = 0; i < kJoin; ++i) to = fmaxf(to, m[i]);
+            const float at = to == -INFINITY ? 0.f : to, a = tca::exp2a(M - at);
+            L *= a, v.x *= a, v.y *= a, v.z *= a, v.w *= a;
+#pragma unroll
+            for (int i = 0; i < kJoin; ++i) {
+              const float b = tca::exp2a(m[i] - at);
+              L += b * l[i];
+              v.x += b * y[i].x, v.y += b * y[i].y, v.z += b * y[i].z, v.w += b * y[i].w;
             }
+            M = to;
           }
           if (groups == 1) {
-            out4(r, ch, make_float4(v.x * sL[r], v.y * sL[r], v.z * sL[r], v.w * sL[r]));
+            const float inv = M == -INFINITY ? 0.f : 1.f / L;
+            out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
           } else {
             reinterpret_cast<float4*>(sO)[grp * items + x] = v;
+            if (ch == 0) sM[grp * rows + r] = M, sL[grp * rows + r] = L;
           }
         }
         if (groups > 1) {
           __syncthreads();
           if (tid < items) {
             const int r = tid / (HD / 4), ch = tid % (HD / 4) * 4;
-            float4 v = reinterpret_cast<float4*>(sO)[tid];
-            for (int k = 1; k < groups; ++k) {
+            float M = -INFINITY, L = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < groups; ++k) M = fmaxf(M, sM[k * rows + r]);
+            const float at = M == -INFINITY ? 0.f : M;
+            for (int k = 0; k < groups; ++k) {
+              const float a = tca::exp2a(sM[k * rows + r] - at);
               const float4 y = reinterpret_cast<float4*>(sO)[k * items + tid];
-              v.x += y.x, v.y += y.y, v.z += y.z, v.w += y.w;
+              L += a * sL[k * rows + r];
+              v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
             }
-            out4(r, ch, make_float4(v.x * sL[r], v.y * sL[r], v.z * sL[r], v.w * sL[r]));
+            const float inv = M == -INFINITY ? 0.f : 1.f / L;
+            out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
           }
         }
       }
