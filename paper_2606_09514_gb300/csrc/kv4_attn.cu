@@ -50,18 +50,26 @@ constexpr int kChunk = 32;
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 3;
-constexpr int kCtasPerSm = 3;
+// CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two).
+template <int NB>
+__host__ __device__ constexpr int ctas_per_sm() { return NB == 1 ? 4 : 3; }
 constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
 constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
-constexpr int kMaxGrid = 1024;   // CTAs: three on each of at most 341 SMs
+constexpr int kMaxGrid = 1024;   // CTAs: four on each of at most 256 SMs
 constexpr int kJoin = 16;        // partials in flight when a cut stream is joined
 constexpr int kFewRows = 32;     // rows of a KV head up to which these kernels take a sequence
 
 template <int HD>
 __host__ __device__ constexpr int stage_bytes() { return 2 * kChunk * entry_bytes(HD); }
+// A warp's outputs, maxima and sums when the warps are joined: with one block of rows in
+// the stage that it has used last, which is free until its next copy.
+template <int HD, int NB>
+__host__ __device__ constexpr int join_bytes() { return 8 * NB * (HD + 4 + 2) * 4; }
+template <int HD, int NB>
+__host__ __device__ constexpr bool join_in_stage() { return join_bytes<HD, NB>() <= stage_bytes<HD>(); }
 template <int HD, int NB>
 __host__ __device__ constexpr int smem_bytes() {
-  return kWarps * kStages * stage_bytes<HD>() + kWarps * 8 * NB * (HD + 4 + 2) * 4;
+  return kWarps * (kStages * stage_bytes<HD>() + (join_in_stage<HD, NB>() ? 0 : join_bytes<HD, NB>()));
 }
 // Arrival counters, then two partials per CTA: m and l of 8 NB rows, then their outputs.
 template <int HD, int NB>
@@ -185,12 +193,17 @@ __device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, int pag
 }
 
 template <int HD, int NB>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const AttnArgs4 A) {
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel(const AttnArgs4 A) {
   extern __shared__ __align__(16) uint8_t smem[];
   constexpr int ROWS = 8 * NB, KS = HD / 16, LDO = HD + 4;
-  float* sO = reinterpret_cast<float*>(smem + kWarps * kStages * stage_bytes<HD>());   // [warp][row][LDO]
-  float* sM = sO + kWarps * ROWS * LDO;                                                // [warp][row]
-  float* sL = sM + kWarps * ROWS;
+  __shared__ int s_stage[kWarps];
+  // where warp w's part is: [row][LDO] outputs, then maxima and sums
+  auto part_of = [&](int w) {
+    return reinterpret_cast<float*>(smem + (join_in_stage<HD, NB>()
+                                                ? (w * kStages + s_stage[w]) * stage_bytes<HD>()
+                                                : kWarps * kStages * stage_bytes<HD>() + w * join_bytes<HD, NB>()));
+  };
+  constexpr int PM = ROWS * LDO, PL = PM + ROWS;
   __shared__ int64_t s_sum[kWarps], s_at;
   __shared__ int s_first, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
@@ -535,7 +548,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       issue();
     }
 
-    // ---- join the warps: a lane has rows 2 lc, 2 lc + 1 of each block, HD / 8 channels from lg * HD / 8 on
+    // ---- join the warps (a stage is free: `put` of the last copy is one behind `take`): a lane has rows 2 lc, 2 lc + 1 of each block, HD / 8 channels from lg * HD / 8 on
+    if (lane == 0) s_stage[warp] = put;
+    __syncwarp();
+    float* const mine = part_of(warp);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -544,8 +560,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
         for (int x = 4; x < 32; x <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], x);
         const int r = 8 * b + 2 * lc + e;
         if (r < rows) {
-          if (lg == 0) sM[warp * ROWS + r] = m[b][e], sL[warp * ROWS + r] = l[b][e];
-          float4* d = reinterpret_cast<float4*>(sO + (warp * ROWS + r) * LDO + lg * (HD / 8));
+          if (lg == 0) mine[PM + r] = m[b][e], mine[PL + r] = l[b][e];
+          float4* d = reinterpret_cast<float4*>(mine + r * LDO + lg * (HD / 8));
 #pragma unroll
           for (int t = 0; t < HD / 16; t += 2)
             d[t / 2] = make_float4(o[b][t][e], o[b][t][e + 2], o[b][t + 1][e], o[b][t + 1][e + 2]);
@@ -568,12 +584,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
       float M = -INFINITY, L = 0.f;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sM[w * ROWS + r]);
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, part_of(w)[PM + r]);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float mw = sM[w * ROWS + r], a = mw == -INFINITY ? 0.f : tca::exp2a(mw - M);
-        const float4 y = *reinterpret_cast<const float4*>(sO + (w * ROWS + r) * LDO + ch);
-        L += a * sL[w * ROWS + r];
+        const float* const pw = part_of(w);
+        const float mw = pw[PM + r], a = mw == -INFINITY ? 0.f : tca::exp2a(mw - M);
+        const float4 y = *reinterpret_cast<const float4*>(pw + r * LDO + ch);
+        L += a * pw[PL + r];
         v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
       }
       if (whole) {
@@ -635,8 +652,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
             const float inv = M == -INFINITY ? 0.f : 1.f / L;
             out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
           } else {
-            reinterpret_cast<float4*>(sO)[grp * items + x] = v;
-            if (ch == 0) sM[grp * rows + r] = M, sL[grp * rows + r] = L;
+            reinterpret_cast<float4*>(part_of(0))[grp * items + x] = v;
+            if (ch == 0) part_of(0)[PM + grp * rows + r] = M, part_of(0)[PL + grp * rows + r] = L;
           }
         }
         if (groups > 1) {
@@ -645,12 +662,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
             const int r = tid / (HD / 4), ch = tid % (HD / 4) * 4;
             float M = -INFINITY, L = 0.f;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < groups; ++k) M = fmaxf(M, sM[k * rows + r]);
+            const float* const pw = part_of(0);
+            for (int k = 0; k < groups; ++k) M = fmaxf(M, pw[PM + k * rows + r]);
             const float at = M == -INFINITY ? 0.f : M;
             for (int k = 0; k < groups; ++k) {
-              const float a = tca::exp2a(sM[k * rows + r] - at);
-              const float4 y = reinterpret_cast<float4*>(sO)[k * items + tid];
-              L += a * sL[k * rows + r];
+              const float a = tca::exp2a(pw[PM + k * rows + r] - at);
+              const float4 y = reinterpret_cast<const float4*>(pw)[k * items + tid];
+              L += a * pw[PL + k * rows + r];
               v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
             }
             const float inv = M == -INFINITY ? 0.f : 1.f / L;
@@ -659,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv4_decode_kernel(const 
         }
       }
     }
-    __syncthreads();     // sM, sL, sO are free again
+    __syncthreads();     // the warps' parts are free again
     start += use.q.nc + kOpen;
     go = use.next(A);
   }
@@ -738,7 +756,7 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   const int64_t streams = cache->n_kv_heads * ((std::min<int64_t>(most_rows, kFewRows) + (two ? 15 : 7)) / (two ? 16 : 8));
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
   const int64_t most = streams > (1 << 20) || chunks > (1 << 20) ? INT32_MAX : a->batch * streams * chunks / kWarps + 1;
-  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, kCtasPerSm * sms));
+  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, (two ? ctas_per_sm<2>() : ctas_per_sm<1>()) * sms));
   cudaStream_t s = (cudaStream_t)stream;
   const int rc = cache->head_dim == 128 ? (two ? launch_decode<128, 2>(A, grid, s) : launch_decode<128, 1>(A, grid, s))
                                         : (two ? launch_decode<64, 2>(A, grid, s) : launch_decode<64, 1>(A, grid, s));
