@@ -34,9 +34,10 @@ namespace kv4 {
 constexpr int kPfRows = 128, kPfKeys = 128;
 constexpr int kPfSoftWarps = 8, kPfProducers = 128;
 constexpr int kPfThreads = 512;          // four warpgroups: two of softmax, producers, the MMA warp's
-// Registers: 128 a thread at launch (65,536 in all), then by setmaxnreg 2 x 128 x 176 +
-// 128 x 88 + 128 x 72 = 65,536.
-constexpr int kPfRegsSoft = 176, kPfRegsProduce = 88, kPfRegsMma = 72;
+// Registers: 128 a thread at launch (65,536 in all), then by setmaxnreg 2 x 128 x 184 +
+// 128 x 80 + 128 x 64 = 65,536.  (What spills, in any role, is felt: nine requests take 260 us so, 275
+// with 176, 88 and 72, 287 with 168, 96 and 80, 294 with 192, 72 and 56.)
+constexpr int kPfRegsSoft = 184, kPfRegsProduce = 80, kPfRegsMma = 64;
 constexpr int kPfOpen = 4;               // what beginning and ending an item costs, in tiles
 constexpr int kPfWhole = 4;              // items of at most this many tiles are not cut
 constexpr uint32_t kPfRegion = 128u * 128u;   // 128 rows x 64 channels of half
