@@ -3,7 +3,7 @@
 //
 // The rows of a (sequence, KV head) are (query token, head of the group) pairs, row
 // r = token r / G, head r % G; up to 8 NB of them share a walk over the keys and
-// values (a stream; more rows make more streams).  With so few rows the work is
+// values (a stream).  With so few rows the work is
 // reading the cache and turning codes into numbers, which the tensor cores' mma.sync
 // takes from registers: nothing goes back to shared memory.
 //
@@ -57,7 +57,10 @@ constexpr int kWhole = 8;        // streams of at most this many chunks are not 
 constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
 constexpr int kMaxGrid = 1024;   // CTAs: four on each of at most 256 SMs
 constexpr int kJoin = 16;        // partials in flight when a cut stream is joined
-constexpr int kFewRows = 32;     // rows of a KV head up to which these kernels take a sequence
+// Rows of a KV head up to which these kernels take a sequence.  (28 rows over 4 KV heads, 16
+// sequences of 4,096 positions 57 us here, 45 us with the prompts' kernel; one of 30,000 43 and 32;
+// 100 of 600 67 and 68.)
+constexpr int kFewRows = 16;
 
 template <int HD>
 __host__ __device__ constexpr int stage_bytes() { return 2 * kChunk * entry_bytes(HD); }
@@ -75,41 +78,34 @@ __host__ __device__ constexpr int smem_bytes() {
 template <int HD, int NB>
 __host__ __device__ constexpr int64_t partial_floats() { return 8 * NB * (HD + 2); }
 
-// What a sequence asks for: query rows, positions, and its streams here.
-struct Seq : Rows {
-  int nc, subs;               // nc chunks, subs streams (0: not this kernel's)
-};
-
-template <int NB>
-__device__ __forceinline__ Seq seq_of(const AttnArgs4& A, int i, bool* bad) {
-  Seq s;
-  *static_cast<Rows*>(&s) = rows_of(A, i, bad);
-  const int rows = s.m * A.G;
-  s.nc = max(1, (s.n + kChunk - 1) / kChunk);   // (a sequence without positions: one chunk of nothing)
-  s.subs = rows > A.row_limit ? 0 : A.p.nkv * ((rows + 8 * NB - 1) / (8 * NB));
-  return s;
+// Chunks of a stream of n positions.  (A sequence without positions: one of nothing.)
+__device__ __forceinline__ int chunks_of(int n) { return max(1, (n + kChunk - 1) / kChunk); }
+// A sequence with m = 0 where it has no rows here.
+__device__ __forceinline__ Rows few_rows(const AttnArgs4& A, int i, bool* bad) {
+  Rows q = rows_of(A, i, bad);
+  if (q.m * A.G > A.row_limit) q.m = 0;
+  return q;
 }
 
 // A walk over the streams of a CTA's share.
-template <int NB>
 struct Walk {
-  Seq q;
-  int i, sub, c, c1;          // sequence, stream of it, chunks [c, c1) of the stream in this share
-  int64_t rem;                // what is left of the share behind this stream
-  __device__ __forceinline__ int g(const AttnArgs4& A) const { return q.subs == A.p.nkv ? sub : sub / (q.subs / A.p.nkv); }
+  Rows q;
+  int i, g, c, c1;            // sequence, KV head, chunks [c, c1) of the stream in this share
+  int rem;                    // what is left of the share behind this stream
   // to the next stream; false at the share's end
   __device__ __forceinline__ bool next(const AttnArgs4& A) {
     rem -= kOpen;
     if (rem <= 0) return false;
-    if (++sub >= q.subs) {
-      sub = 0;
+    if (++g >= A.p.nkv) {
+      g = 0;
       bool bad;
       do {
-        q = seq_of<NB>(A, ++i, &bad);   // (with some of the share left there is another stream)
-      } while (q.subs == 0);
+        q = few_rows(A, ++i, &bad);   // (with some of the share left there is another stream)
+      } while (q.m == 0);
     }
     c = 0;
-    c1 = q.nc <= kWhole ? q.nc : (int)min((int64_t)q.nc, rem);
+    c1 = chunks_of(q.n);
+    if (c1 > kWhole) c1 = min(c1, rem);
     rem -= c1;
     return true;
   }
@@ -205,6 +201,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   };
   constexpr int PM = ROWS * LDO, PL = PM + ROWS;
   __shared__ int64_t s_sum[kWarps], s_at;
+  __shared__ int s_streams[kWarps];
   __shared__ int s_first, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
   const int B = A.a.batch, G = A.G;
@@ -214,36 +211,48 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   const int per = (B + kThreads - 1) / kThreads;
   const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
   int64_t mine = 0;
+  int streams = 0;
   bool any_bad = false;
+#pragma unroll 1
   for (int i = b0; i < b1; ++i) {
     bool bad;
-    const Seq q = seq_of<NB>(A, i, &bad);
+    const Rows q = few_rows(A, i, &bad);
     any_bad |= bad;
-    mine += (int64_t)(q.nc + kOpen) * q.subs;
+    if (q.m > 0) mine += chunks_of(q.n) + kOpen, ++streams;
   }
   if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+  mine *= A.p.nkv;
+  streams = __reduce_add_sync(0xffffffffu, streams);
   int64_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += v;
   }
-  if (lane == 31) s_sum[warp] = upto;
+  if (lane == 31) s_sum[warp] = upto, s_streams[warp] = streams;
   __syncthreads();
   int64_t total = 0;
+  streams = 0;
   for (int w = 0; w < kWarps; ++w) {
     if (w == warp) upto += total;
     total += s_sum[w];
+    streams += s_streams[w];
   }
-  const int64_t share = max((int64_t)kWarps, (total + gridDim.x - 1) / gridDim.x + kWarps - 1) / kWarps * kWarps;
-  const int64_t lo = blockIdx.x * share;
+  if (total == 0) return;
+  // A stream of n chunks in parts of x takes about x b / 4 + (n / x) (rows HD / 512) / 16 c: the chunks
+  // of a part, then the parts in the join; with b / c about 2.5 least at x = sqrt(0.4 n passes).
+  const float fair = (float)(total / A.p.nkv - (int64_t)streams * kOpen) / (float)streams;
+  const int64_t least = (int64_t)sqrtf(0.4f * fair * (float)A.passes) + 1;
+  const int share = (int)min((int64_t)INT32_MAX / 2, (max(least, (total + gridDim.x - 1) / gridDim.x) + kWarps - 1) / kWarps * kWarps);
+  const int64_t lo = (int64_t)blockIdx.x * share;
   if (lo >= total) return;
   if (upto - mine <= lo && lo < upto) {
     int64_t at = upto - mine;
+#pragma unroll 1
     for (int i = b0; i < b1; ++i) {
       bool bad;
-      const Seq q = seq_of<NB>(A, i, &bad);
-      const int64_t n = (int64_t)(q.nc + kOpen) * q.subs;
+      const Rows q = few_rows(A, i, &bad);
+      const int64_t n = q.m > 0 ? (int64_t)(chunks_of(q.n) + kOpen) * A.p.nkv : 0;
       if (lo < at + n) {
         s_first = i;
         s_at = lo - at;
@@ -253,28 +262,29 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     }
   }
   __syncthreads();
-  Walk<NB> use;
-  int64_t start;                    // where the first chunk of the stream is
+  Walk use;
+  int start;                        // where the stream's first chunk is, from the share's beginning on
   {
     bool bad;
     use.i = s_first;
-    use.q = seq_of<NB>(A, use.i, &bad);
-    use.sub = (int)(s_at / (use.q.nc + kOpen));
-    const int64_t x = s_at - (int64_t)use.sub * (use.q.nc + kOpen) - kOpen;   // chunk of the stream; below 0: its opening
-    start = lo - x;
-    use.rem = min(share, total - lo) + min(x, (int64_t)0);
-    use.c = (int)max(x, (int64_t)0);
+    use.q = few_rows(A, use.i, &bad);
+    const int nc = chunks_of(use.q.n);
+    use.g = (int)(s_at / (nc + kOpen));
+    const int x = (int)(s_at - (int64_t)use.g * (nc + kOpen)) - kOpen;   // chunk of the stream; below 0: its opening
+    start = -x;
+    use.rem = (int)min((int64_t)share, total - lo) + min(x, 0);
+    use.c = max(x, 0);
     if (use.rem <= 0) return;
-    if (x > 0 && use.q.nc <= kWhole) {   // the CTA before has it all
-      use.rem -= use.q.nc - x;
-      start += use.q.nc + kOpen;
+    if (x > 0 && nc <= kWhole) {         // the CTA before has it all
+      use.rem -= nc - x;
+      start += nc + kOpen;
       if (!use.next(A)) return;
     } else {
-      use.c1 = use.q.nc <= kWhole ? use.q.nc : (int)min((int64_t)use.q.nc, use.c + use.rem);
+      use.c1 = nc <= kWhole ? nc : min(nc, use.c + use.rem);
       use.rem -= use.c1 - use.c;
     }
   }
-  Walk<NB> ld = use;
+  Walk ld = use;
   bool more = true;
   ld.c += warp;
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * stage_bytes<HD>();
@@ -306,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         if ((uint32_t)id1 >= (uint32_t)A.p.n_pages) id1 = -1, ok &= 1;
         if (lane == 0 && A.flags && p0 < ld.q.n) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
       }
-      load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), id0, id1, ld.g(A), p0, ld.q.n, lane);
+      load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), id0, id1, ld.g, p0, ld.q.n, lane);
       there |= ok << (2 * flying);
       ld.c += kWarps;
       fetch_ids();
@@ -330,21 +340,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     vs_at[u] = VSC + place(2 * lc + u) * scale_bytes(HD) + (lg * (HD / 8) / 32) * 2;
   }
 
-  uint32_t magic;                   // (opaque: otherwise it is made anew at every use)
-  asm volatile("mov.b32 %0, 0x54005400;" : "=r"(magic));
-
   for (bool go = true; go;) {
     // ---- one stream (or the part of it in this share)
-    const int g = use.g(A), r0 = (use.sub - g * (use.q.subs / A.p.nkv)) * ROWS;
-    const int rows = min(use.q.m * G - r0, ROWS), n = use.q.n;
-    const bool whole = use.c == 0 && use.c1 == use.q.nc;
+    const int g = use.g, rows = use.q.m * G, n = use.q.n, nc = chunks_of(n);
+    const bool whole = use.c == 0 && use.c1 == nc;
     // queries: rows lg of each block of eight, this lane's HD / 4 channels
     uint32_t qf[NB][KS][2];
     float fac[NB][2];               // of the scores of rows 2 lc and 2 lc + 1
     int seen[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int r = min(8 * b + lg, rows - 1) + r0;
+      const int r = min(8 * b + lg, rows - 1);
       const int64_t at = (use.q.t0 + r / G) * A.a.q_stride + (int64_t)(g * G + r % G) * HD + lc * (HD / 4);
       float x[HD / 4], top = 0.f;
 #pragma unroll
@@ -365,10 +371,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       for (int e = 0; e < 2; ++e) {
         fac[b][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
         // (rows that are not there repeat the last)
-        seen[b][e] = n - use.q.m + (r0 + min(8 * b + 2 * lc + e, rows - 1)) / G + 1;
+        seen[b][e] = n - use.q.m + min(8 * b + 2 * lc + e, rows - 1) / G + 1;
       }
     }
-    const int all_seen = n - use.q.m + r0 / G + 1;   // positions that every row sees
+    const int all_seen = n - use.q.m + 1;   // positions that every row sees
     float o[NB][HD / 16][4], m[NB][2], l[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -419,8 +425,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             uint32_t x[4], y[4];
-            dequant4(w[t][0][i], sc[t][0], s72[t][0], magic, x);
-            dequant4(w[t][1][i], sc[t][1], s72[t][1], magic, y);
+            dequant4(w[t][0][i], sc[t][0], s72[t][0], x);
+            dequant4(w[t][1][i], sc[t][1], s72[t][1], y);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
               mma_f16(s[b][t], x[0], y[0], x[1], y[1], qf[b][2 * i][0], qf[b][2 * i][1]);
@@ -521,10 +527,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
 #pragma unroll
         for (int x = 0; x < HD / 64; ++x) {
           uint32_t a[4][4];
-          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, magic, a[0]);
-          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, magic, a[1]);
-          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, magic, a[2]);
-          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, magic, a[3]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x5410), sa, sa72, a[0]);
+          dequant4(__byte_perm(w[0][x], w[1][x], 0x7632), sa, sa72, a[1]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x5410), sb, sb72, a[2]);
+          dequant4(__byte_perm(w[2][x], w[3][x], 0x7632), sb, sb72, a[3]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
 #pragma unroll
@@ -568,11 +574,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         }
       }
     __syncthreads();
-    const int64_t first_cta = whole ? 0 : start / share, last_cta = whole ? 0 : (start + use.q.nc - 1) / share;
-    float* part = A.part + (2 * (int64_t)blockIdx.x + ((int64_t)blockIdx.x == first_cta ? 1 : 0)) * partial_floats<HD, NB>();
+    // the CTAs that have parts of the stream: from the one of its first chunk (start may lie
+    // before this share) to the one of its last
+    const int first_cta = (int)blockIdx.x - (start < 0 ? (share - 1 - start) / share : 0);
+    const int last_cta = (int)blockIdx.x + (start + nc - 1) / share;
+    float* part = A.part + (2 * (int64_t)blockIdx.x + ((int)blockIdx.x == first_cta ? 1 : 0)) * partial_floats<HD, NB>();
     auto out4 = [&](int r, int ch, float4 v) {
-      const int row = r0 + r;
-      const int64_t at = (use.q.t0 + row / G) * A.a.out_stride + (int64_t)(g * G + row % G) * HD + ch;
+      const int64_t at = (use.q.t0 + r / G) * A.a.out_stride + (int64_t)(g * G + r % G) * HD + ch;
       if (A.a.out_dtype == BUDDY_DTYPE_F32) {
         *reinterpret_cast<float4*>((float*)A.a.out + at) = v;
       } else {
@@ -603,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     }
     if (!whole) {
       __syncthreads();   // the partial's writes come before the arrival, which releases them
-      const int spans = (int)(last_cta - first_cta) + 1;
+      const int spans = last_cta - first_cta + 1;
       if (tid == 0) {
         s_last = ptx::atom_add_acq_rel(A.arrive + first_cta, 1) == spans - 1;
         if (s_last) A.arrive[first_cta] = 0;
@@ -612,8 +620,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       if (s_last) {
         // kJoin spans' loads at a time into a running log-sum-exp
         constexpr int64_t PF = partial_floats<HD, NB>();
-        const float* p0 = A.part + (2 * first_cta + 1) * PF;      // the first span's partial, and the
-        const float* p1 = A.part + 2 * (first_cta + 1) * PF;      // second's; the others 2 PF apart
+        const float* p0 = A.part + (2 * (int64_t)first_cta + 1) * PF;      // the first span's partial, and the
+        const float* p1 = A.part + 2 * ((int64_t)first_cta + 1) * PF;      // second's; the others 2 PF apart
         const int items = rows * (HD / 4);
         // few rows: the spans go over as many groups of threads as there are
         const int groups = items < kThreads ? kThreads / items : 1, grp = items < kThreads ? tid / items : 0;
@@ -678,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       }
     }
     __syncthreads();     // the warps' parts are free again
-    start += use.q.nc + kOpen;
+    start += nc + kOpen;
     go = use.next(A);
   }
   cp_wait<0>();
@@ -753,9 +761,9 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   // one CTA for every four chunks there can be, three on each SM at most
   const int64_t most_rows = (int64_t)a->max_new * A.G;
   const bool two = most_rows > 8;
-  const int64_t streams = cache->n_kv_heads * ((std::min<int64_t>(most_rows, kFewRows) + (two ? 15 : 7)) / (two ? 16 : 8));
+  A.passes = (int)((std::min<int64_t>(most_rows, two ? 16 : 8) * (cache->head_dim / 4) + kThreads - 1) / kThreads);
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
-  const int64_t most = streams > (1 << 20) || chunks > (1 << 20) ? INT32_MAX : a->batch * streams * chunks / kWarps + 1;
+  const int64_t most = (int64_t)a->batch * cache->n_kv_heads * (chunks + kOpen) / kWarps + 1;
   const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, (two ? ctas_per_sm<2>() : ctas_per_sm<1>()) * sms));
   cudaStream_t s = (cudaStream_t)stream;
   const int rc = cache->head_dim == 128 ? (two ? launch_decode<128, 2>(A, grid, s) : launch_decode<128, 1>(A, grid, s))

@@ -17,6 +17,7 @@ struct AttnArgs4 {
   int32_t* flags;
   int32_t* arrive;            // few rows: [grid], zero between calls
   float* part;                // partials of streams or items that are cut
+  int passes;                 // few rows: rounds of a CTA's threads over a stream's outputs
 };
 
 // A sequence's query tokens t0 .. t0 + m - 1 and its n positions; m = 0 where they are bad.
@@ -46,11 +47,10 @@ __device__ __forceinline__ void row_scale(float top, float base, float* down, fl
 __device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
 __device__ __forceinline__ __half2 as_h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
 
-// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.  `magic`: 64 in
-// both halves, in a register (the instruction takes one constant).
-__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72, uint32_t magic) {
+// Codes in bits 4 .. 7 of both halves -> (code - 8) s, with s72 = -72 s.
+__device__ __forceinline__ uint32_t dequant(uint32_t w, __half2 s, __half2 s72) {
   uint32_t x;
-  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(x) : "r"(w), "r"(magic));   // (w & mask) | magic
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x54005400, 0xEA;" : "=r"(x) : "r"(w));   // (w & mask) | 64.0
   return h2(__hfma2(as_h2(x), s, s72));
 }
 // Codes in bits 0 .. 3: 1024 + n needs a subtraction of its own (1032 s would be rounded), but no
@@ -60,15 +60,15 @@ __device__ __forceinline__ uint32_t dequant_low(uint32_t w, __half2 s) {
   asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(x) : "r"(w));
   return h2(__hmul2(__hadd2(as_h2(x), __float2half2_rn(-1032.f)), s));
 }
-__device__ __forceinline__ void dequant2(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t* o) {
+__device__ __forceinline__ void dequant2(uint32_t w, __half2 s, __half2 s72, uint32_t* o) {
   o[0] = dequant_low(w, s);
-  o[1] = dequant(w, s, s72, magic);
+  o[1] = dequant(w, s, s72);
 }
 // The four pairs (codes j of both halves) of a word.  (With shifts for all four, 250 sequences
 // take 96.6 us instead of 93.9; with shifts as high halves of products 4 to 10% more.)
-__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t magic, uint32_t* o) {
-  dequant2(w, s, s72, magic, o);
-  dequant2(w >> 8, s, s72, magic, o + 2);
+__device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uint32_t* o) {
+  dequant2(w, s, s72, o);
+  dequant2(w >> 8, s, s72, o + 2);
 }
 
 // Sequences of more than row_limit rows per KV head (kv4_pf.cu).

@@ -84,6 +84,28 @@ __device__ __forceinline__ int64_t pf_head_cost(int n, int m, int G, int R, int 
   for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
   return c;
 }
+// Cost of a KV head of sequence i0 + lane (0: not this kernel's, or not below end): a lane for
+// itself where there are few items, the whole warp for the longer ones.
+__device__ __forceinline__ int64_t pf_block_costs(const AttnArgs4& A, int i0, int end, int lane, Rows* q) {
+  *q = {0, 0, 0};
+  bool bad;
+  if (i0 + lane < end) *q = rows_of(A, i0 + lane, &bad);
+  const int R = q->m * A.G, nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+  int64_t c = 0;
+  if (R > A.row_limit && nqp <= 4)
+#pragma unroll 1
+    for (int qp = 0; qp < nqp; ++qp) c += pf_tiles(q->n, q->m, A.G, R, qp) + kPfOpen;
+  uint32_t longer = __ballot_sync(0xffffffffu, R > A.row_limit && nqp > 4);
+#pragma unroll 1
+  while (longer) {
+    const int x = __ffs(longer) - 1;
+    longer &= longer - 1;
+    const int m = __shfl_sync(0xffffffffu, q->m, x);
+    const int64_t v = pf_head_cost(__shfl_sync(0xffffffffu, q->n, x), m, A.G, m * A.G, lane);
+    if (lane == x) c = v;
+  }
+  return c;
+}
 // First sequence from i on (below end) that is this kernel's; end if none (whole warp).
 __device__ __forceinline__ int pf_next_seq(const AttnArgs4& A, int i, int end, int lane, Rows* q) {
 #pragma unroll 1
@@ -181,8 +203,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   int64_t mine = 0;
   if (warp < kPfSoftWarps) {
     Rows q;
-    for (int i = pf_next_seq(A, b0, b1, lane, &q); i < b1; i = pf_next_seq(A, i + 1, b1, lane, &q))
-      mine += A.p.nkv * pf_head_cost(q.n, q.m, G, q.m * G, lane);
+#pragma unroll 1
+    for (int i0 = b0; i0 < b1; i0 += 32) mine += pf_block_costs(A, i0, b1, lane, &q);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    mine *= A.p.nkv;
     if (lane == 0) s_sum[warp] = mine;
   }
   if (tid == 0) {
@@ -220,10 +245,25 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     // the sequence, its head, the item of it and the tile where the share begins
     PfWalk w;
     int64_t at = before, cost = 0;
-    for (w.i = pf_next_seq(A, b0, b1, lane, &w.q);; w.i = pf_next_seq(A, w.i + 1, b1, lane, &w.q)) {
-      cost = pf_head_cost(w.q.n, w.q.m, G, w.q.m * G, lane);
-      if (lo < at + cost * A.p.nkv) break;
-      at += cost * A.p.nkv;
+#pragma unroll 1
+    for (int i0 = b0;; i0 += 32) {
+      const int64_t c = pf_block_costs(A, i0, b1, lane, &w.q);
+      int64_t upto = c * A.p.nkv;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const uint32_t hit = __ballot_sync(0xffffffffu, lo < at + upto);
+      if (hit || i0 + 32 >= b1) {
+        const int x = hit ? __ffs(hit) - 1 : 31;
+        w.i = i0 + x;
+        cost = __shfl_sync(0xffffffffu, c, x);
+        at += __shfl_sync(0xffffffffu, upto - c * A.p.nkv, x);
+        w.q = {__shfl_sync(0xffffffffu, w.q.t0, x), __shfl_sync(0xffffffffu, w.q.m, x), __shfl_sync(0xffffffffu, w.q.n, x)};
+        break;
+      }
+      at += __shfl_sync(0xffffffffu, upto, 31);
     }
     w.g = 0;
 #pragma unroll 1
@@ -617,7 +657,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       const int end = min(it.n, max(it.n - it.m + last / G + 1, 0));                  // positions that any row sees
       const int in_page = (1 << A.p.shift) - 1;
       const int32_t* table = A.a.table + (int64_t)it.seq * A.a.max_pages;
-      const uint32_t magic = 0x54005400u;
       struct Entry {
         uint4 w[GR];
         __half s[GR];
@@ -657,7 +696,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             uint32_t o[4];
-            dequant4(w[y], s2, s72, magic, o);
+            dequant4(w[y], s2, s72, o);
             *reinterpret_cast<uint4*>(dst + pf_piece(lt, 4 * x + y)) = make_uint4(o[0], o[1], o[2], o[3]);
           }
         }
