@@ -508,9 +508,10 @@ BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int6
  *   sum_p softmax_p(scale * q . k_p) v_p   over positions 0 .. its own;
  * a token without any position (kv_len[i] = 0, or more query tokens than
  * positions) gets zeros.  Rows of q behind row_start[batch] are not written.
- * Queries enter the products with 11 significant bits (of their head's largest
- * element; a bf16 query whole), probabilities with 11, keys and values exactly;
- * sums and statistics are fp32.
+ * Query elements enter the products as halves: 11 significant bits (a bf16
+ * element whole), below 2^-14 rounded at 2^-25; a row with elements above 2^15 is
+ * scaled by a power of two.  Probabilities enter with 11 bits, keys and values
+ * exactly; sums and statistics are fp32.
  * Device-checked: 0 <= kv_len[i] <= max_pages * page_size and row_start
  * ascending from >= 0 to <= n_tok with at most max_new rows each
  * (BUDDY_DEV_BAD_POSITION: the sequence's rows are not written); page ids

@@ -4,8 +4,7 @@
 // The rows of a (sequence, KV head) are (query token, head of the group) pairs, row
 // r = token r / G, head r % G; two tiles of 128 of them (an item) walk the same
 // key/value tiles of 128 positions.  On the 5th-generation tensor cores, in half:
-//   S = Q K^T   tcgen05.mma M = 128, N = 128, K = HD: queries (of a warp's 32 rows, scaled by
-//               a power of two to 2 at most) and keys from shared memory, S in TMEM;
+//   S = Q K^T   tcgen05.mma M = 128, N = 128, K = HD: queries and keys from shared memory, S in TMEM;
 //   softmax     four warps per tile, a row per thread, base 2: running reference m,
 //               which follows the maximum when that rises by more than 8; p back into
 //               TMEM as half over S's columns;
@@ -338,59 +337,69 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     };
     uint8_t* const qdst = sQ + (size_t)q * TILE;
     const float base = (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f;
-    // The queries of this warp's 32 rows as halves of at most 2, scaled by one power of two;
-    // returns the factor of their scores.
+    // The queries of this warp's 32 rows as halves; returns the factor of this lane's row's
+    // scores.  Rows with elements above 2^15 (and those next to them) are taken once more,
+    // scaled by a power of two each.
     auto put_q = [&](const PfItem& x) {
       const int l8 = lane % LPR;
       const int64_t at = row_at(x, A.a.q_stride);
       auto from = [&](int u) { return __shfl_sync(0xffffffffu, (long long)at, u * RPL + lane / LPR) + l8 * 8; };
-      auto dst = [&](int u) { return qdst + pf_piece((warp & 3) * 32 + u * RPL + lane / LPR, l8); };
-      float down, fac;
-      if (A.a.q_dtype == BUDDY_DTYPE_BF16) {
+      auto put = [&](int u, const float* v) {
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = h2(__floats2half2_rn(v[2 * e], v[2 * e + 1]));
+        *reinterpret_cast<uint4*>(qdst + pf_piece((warp & 3) * 32 + u * RPL + lane / LPR, l8)) = make_uint4(h[0], h[1], h[2], h[3]);
+      };
+      const bool wide = A.a.q_dtype == BUDDY_DTYPE_F32;
+      float top = 0.f;
+      if (!wide) {
         const bf16* src = (const bf16*)A.a.q;
         uint4 raw[32 / RPL];                            // all of them in flight
 #pragma unroll
         for (int u = 0; u < 32 / RPL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>(src + from(u)));
-        __nv_bfloat162 top = __float2bfloat162_rn(0.f);
-        auto b2 = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+        auto b2 = [](uint32_t w) { return __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w)); };
+        __nv_bfloat162 most = __float2bfloat162_rn(0.f);
 #pragma unroll
         for (int u = 0; u < 32 / RPL; ++u) {
-          top = __hmax2(top, __hmax2(__habs2(b2(raw[u].x)), __habs2(b2(raw[u].y))));
-          top = __hmax2(top, __hmax2(__habs2(b2(raw[u].z)), __habs2(b2(raw[u].w))));
-        }
-        row_scale(warp_max(fmaxf(__low2float(top), __high2float(top))), base, &down, &fac);
-#pragma unroll
-        for (int u = 0; u < 32 / RPL; ++u) {
+          most = __hmax2(most, __hmax2(__hmax2(b2(raw[u].x), b2(raw[u].y)), __hmax2(b2(raw[u].z), b2(raw[u].w))));
           const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-          uint32_t h[4];
+          float v[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            h[e] = h2(__floats2half2_rn(__uint_as_float(w[e] << 16) * down, __uint_as_float(w[e] & 0xFFFF0000u) * down));
-          *reinterpret_cast<uint4*>(dst(u)) = make_uint4(h[0], h[1], h[2], h[3]);
+          for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+          put(u, v);
         }
+        top = fmaxf(__low2float(most), __high2float(most));
       } else {
-        const float* src = (const float*)A.a.q;
-        float top = 0.f;
-#pragma unroll 1
-        for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 2
-          for (int u = 0; u < 32 / RPL; ++u) {
-            float v[8];
-            load8(src + from(u), v);
-            if (pass == 0) {
+#pragma unroll 4
+        for (int u = 0; u < 32 / RPL; ++u) {
+          float v[8];
+          load8((const float*)A.a.q + from(u), v);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-            } else {
-              uint32_t h[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) h[e] = h2(__floats2half2_rn(v[2 * e] * down, v[2 * e + 1] * down));
-              *reinterpret_cast<uint4*>(dst(u)) = make_uint4(h[0], h[1], h[2], h[3]);
-            }
-          }
-          if (pass == 0) row_scale(warp_max(top), base, &down, &fac);
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+          put(u, v);
         }
       }
-      __syncwarp();
+      float fac = fmaxf(base, 1.2e-38f);
+      if (__any_sync(0xffffffffu, top > 32768.f)) {
+#pragma unroll 1
+        for (int u = 0; u < 32 / RPL; ++u) {
+          float v[8], row_top = 0.f, down, f;
+          const int64_t src = from(u);
+          if (wide) load8((const float*)A.a.q + src, v);
+          else load8((const bf16*)A.a.q + src, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) row_top = fmaxf(row_top, fabsf(v[e]));
+#pragma unroll
+          for (int o = LPR / 2; o > 0; o >>= 1) row_top = fmaxf(row_top, __shfl_xor_sync(0xffffffffu, row_top, o));
+          row_scale(row_top, base, &down, &f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= down;
+          put(u, v);
+          // to the lane of the row
+          const float mine = __shfl_sync(0xffffffffu, f, (lane % RPL) * LPR);
+          if (lane / RPL == u) fac = mine;
+        }
+      }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       ptx::mbar_arrive(&q_ready[q]);
       return fac;

@@ -481,6 +481,36 @@ def test_attention_nan_entries_reach_their_readers_only():
     assert torch.isnan(out[149]).all() and torch.isfinite(out[:149]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m", [1, 4, 150])
+def test_attention_huge_queries_reach_their_own_rows_only(m, dtype):
+    """Infinities, NaN and elements beyond a half's range, each in one (token, head).
+
+    A query with one element of 2^17 has scores that are single products, off by two
+    roundings of 2^-24 (the factor, the exponent); the other rows as everywhere.
+    """
+    hd, lens = 64, [210, 170]
+    cache, table, vals = make_cache(lens, 16, 1, hd, nan_tail=False)
+    q = torch.randn(2 * m, 4, hd, device="cuda").bfloat16().to(dtype)
+    q[0, 0], q[m, 1, 5], q[m, 2, 9] = 0.0, float("inf"), float("nan")
+    q[0, 0, 3] = 2.0 ** 17
+    out = torch.empty_like(q, dtype=torch.float32)
+    cache.buddy_kv4_attention(q, i32(lens), table, out, i32([0, m, 2 * m]), m)
+    got = f64(out)
+    assert not np.isfinite(got[m, 1]).any() and not np.isfinite(got[m, 2]).any()
+    for i in range(2):
+        k, v = vals[i]
+        qi = f64(q[i * m:(i + 1) * m])
+        bad = ~np.isfinite(qi).all(-1)
+        want = O.attention(np.where(bad[..., None], 0.0, qi), k, v, m, hd ** -0.5)
+        top = np.abs(v).max()
+        tol = np.full(bad.shape, top * (2.0 ** -11 + 2.0 ** -12))
+        if i == 0:
+            tol[0, 0] += top * 2 * np.expm1(2 * 2.0 ** -24 * 2.0 ** 17 * np.abs(k[0, :, 3]).max() * hd ** -0.5 * 2)
+        err = np.abs(got[i * m:(i + 1) * m] - want).max(-1)
+        assert np.all((err <= tol) | bad), (err / tol)[~bad].max()
+
+
 @pytest.mark.parametrize("n_new", [1, 40])
 def test_attention_reports_bad_lengths_and_pages(n_new):
     lens = [70, 70, 70, 70]
