@@ -36,6 +36,7 @@
 
 #include <algorithm>
 
+#include "gemm_common.cuh"
 #include "internal.h"
 #include "kv4_attn.cuh"
 
@@ -118,79 +119,45 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes) {   // the rest of 16: zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Position (of 16) of row r of S^T: odd and even neighbours, so that neither the key nor the
 // value loads meet in a bank more than they have to.
 __device__ __forceinline__ int place(int r) { return r ^ ((r >> 1) & 1); }
 
-// A warp's copies of one chunk into a stage: K codes, V codes, K scales, V scales.  A
-// position's codes are as many bytes in the stage as in the page, so a lane's pieces lie
-// 512 bytes apart on both sides.  page0, page1: pages of the lower and the upper 16
-// positions, negative where there is none.
+// Copies of one chunk into a stage, by one lane: K codes, V codes, K scales, V scales, in
+// whole halves of 16 positions (what lies behind the sequence's end is in the block too).
+// page0, page1: pages of the lower and the upper 16 positions; ok: two bits, which to copy.
 template <int HD>
-__device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, int page0, int page1, int g, int p0, int n,
-                                           int lane) {
+__device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, uint64_t* bar, int page0, int page1, uint32_t ok,
+                                           int g, int p0) {
   constexpr int CB = code_bytes(HD), SB = scale_bytes(HD);
-  constexpr int HALF = 16 * CB / 512;               // copies of 16 positions' codes
-  constexpr int PIECES = kChunk * SB / 16;          // 16-byte pieces of scales: 16 or 8, keys on the lower half-warp
-  const int in_page = p0 & ((1 << P.shift) - 1);
-  const int x = lane & 15;
-  const uint32_t sdst = dst + 2 * kChunk * CB + (lane < 16 ? 0 : kChunk * SB) + x * 16;
-  const uint8_t* const sbase = lane < 16 ? P.k : P.v;
-  dst += lane * 16;
-  if (page0 >= 0 && page1 >= 0 && p0 + kChunk <= n) {
-    const int64_t b0 = block_at<HD>(P, page0, g);
-    int64_t at = b0 + in_page * CB + lane * 16;
-    int64_t sat = b0 + (CB << P.shift) + in_page * SB + x * 16;
-    const uint8_t *k = P.k + at, *v = P.v + at;
-#pragma unroll
-    for (int i = 0; i < HALF; ++i) {
-      cp_async(dst + 512 * i, k + 512 * i, 16);
-      cp_async(dst + kChunk * CB + 512 * i, v + 512 * i, 16);
-    }
-    if (P.shift == 4) {
-      const int64_t b1 = block_at<HD>(P, page1, g);
-      at = b1 + lane * 16 - 512 * HALF;
-      k = P.k + at, v = P.v + at;
-      if (x >= PIECES / 2) sat = b1 + (CB << 4) + (x - PIECES / 2) * 16;
-    }
-#pragma unroll
-    for (int i = HALF; i < 2 * HALF; ++i) {
-      cp_async(dst + 512 * i, k + 512 * i, 16);
-      cp_async(dst + kChunk * CB + 512 * i, v + 512 * i, 16);
-    }
-    if (x < PIECES) cp_async(sdst, sbase + sat, 16);
-    return;
-  }
-  // at a sequence's end, and where a page is not there: zeros for what is not read
-  const int64_t b0 = block_at<HD>(P, max(page0, 0), g), b1 = block_at<HD>(P, max(page1, 0), g);
-  const int up = P.shift == 4 ? 0 : in_page + 16;   // where the upper 16 positions begin in their page
-#pragma unroll 1
-  for (int i = 0; i < 2 * HALF; ++i) {
-    const int r = i * (512 / CB) + lane / (CB / 16);
-    const int64_t at = i < HALF ? b0 + in_page * CB + lane * 16 + 512 * i : b1 + up * CB + lane * 16 + 512 * (i - HALF);
-    const int real = p0 + r < n && (i < HALF ? page0 : page1) >= 0 ? 16 : 0;
-    cp_async(dst + 512 * i, P.k + (real ? at : 0), real);
-    cp_async(dst + kChunk * CB + 512 * i, P.v + (real ? at : 0), real);
-  }
-  if (x < PIECES) {
-    constexpr int RPS = 16 / SB;                    // positions of a piece
-    const int r = x * RPS;
-    const int real = (r < 16 ? page0 : page1) >= 0 ? min(max(n - p0 - r, 0), RPS) * SB : 0;
-    const int64_t sat = r < 16 ? b0 + (CB << P.shift) + (in_page + r) * SB : b1 + (CB << P.shift) + (up + r - 16) * SB;
-    cp_async(sdst, sbase + (real ? sat : 0), real);
+  const uint32_t b = ptx::smem_u32(bar);
+  auto copies = [&](int64_t block, int in_page, int at, int n) {
+    const int64_t codes = block + in_page * CB, scales = block + ((int64_t)CB << P.shift) + in_page * SB;
+    bulk_load(dst + at * CB, P.k + codes, n * CB, b);
+    bulk_load(dst + (kChunk + at) * CB, P.v + codes, n * CB, b);
+    bulk_load(dst + 2 * kChunk * CB + at * SB, P.k + scales, n * SB, b);
+    bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, P.v + scales, n * SB, b);
+  };
+  ptx::mbar_arrive_expect_tx(bar, (uint32_t)__popc(ok) * 16 * 2 * entry_bytes(HD));
+  if (P.shift > 4) {
+    if (ok) copies(block_at<HD>(P, page0, g), p0 & ((1 << P.shift) - 1), 0, kChunk);
+  } else {
+    if (ok & 1) copies(block_at<HD>(P, page0, g), 0, 0, 16);
+    if (ok & 2) copies(block_at<HD>(P, page1, g), 0, 16, 16);
   }
 }
 
 template <int HD, int NB>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel(const AttnArgs4 A) {
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t full[kWarps * kStages];
+  __shared__ volatile int abort_flag;
   constexpr int ROWS = 8 * NB, KS = HD / 16, LDO = HD + 4;
   __shared__ int s_stage[kWarps];
   // where warp w's part is: [row][LDO] outputs, then maxima and sums
@@ -206,6 +173,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
   const int B = A.a.batch, G = A.G;
   pdl_trigger();   // (the prompts of the same call may start where there is room)
+  if (tid < kWarps * kStages) ptx::mbar_init(&full[tid], 1);
+  if (tid == 0) abort_flag = 0;
+  ptx::fence_mbar_init();
 
   // ---- this CTA's share: [lo, lo + share) of all streams' openings and chunks
   const int per = (B + kThreads - 1) / kThreads;
@@ -306,22 +276,25 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     }
   };
   uint32_t there = 0;               // two bits per chunk in flight, the oldest lowest: 16 positions whose page is there
-  int flying = 0, put = 0, take = 0;
+  int flying = 0, put = 0, take = 0, issued = 0;
+  uint32_t phase = 0;               // of the stage to take
   auto issue = [&]() {
     if (more) {
       const int p0 = ld.c * kChunk;
       uint32_t ok = 3;
       if ((uint32_t)id0 >= (uint32_t)A.p.n_pages || (uint32_t)id1 >= (uint32_t)A.p.n_pages) {
-        if ((uint32_t)id0 >= (uint32_t)A.p.n_pages) id0 = -1, ok &= 2;
-        if ((uint32_t)id1 >= (uint32_t)A.p.n_pages) id1 = -1, ok &= 1;
+        if ((uint32_t)id0 >= (uint32_t)A.p.n_pages) ok &= 2;
+        if ((uint32_t)id1 >= (uint32_t)A.p.n_pages) ok &= 1;
         if (lane == 0 && A.flags && p0 < ld.q.n) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
       }
-      load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), id0, id1, ld.g, p0, ld.q.n, lane);
+      __syncwarp();
+      if (ptx::elect_one())
+        load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), &full[warp * kStages + put], id0, id1, ok, ld.g, p0);
       there |= ok << (2 * flying);
       ld.c += kWarps;
+      ++issued;
       fetch_ids();
     }
-    cp_commit();
     ++flying;
     put = put + 1 == kStages ? 0 : put + 1;
   };
@@ -387,13 +360,14 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     }
 
     for (int c = use.c + warp; c < use.c1; c += kWarps) {
-      cp_wait<kStages - 2>();
-      __syncwarp();
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp * kStages + take], phase, kWaitLimitNs, &abort_flag)))
+        more = false;
       const uint8_t* st = smem + (warp * kStages + take) * stage_bytes<HD>();
       const uint32_t ok = there & 3u;
       there >>= 2;
       --flying;
       take = take + 1 == kStages ? 0 : take + 1;
+      phase ^= take == 0;
       const int p0 = c * kChunk;
 
       // ---- S^T
@@ -490,6 +464,18 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         for (int u = 0; u < 2; ++u)
           vsc[t][u] = __halves2half2(*reinterpret_cast<const __half*>(st + vs_at[0] + (16 * t + 8 * u) * scale_bytes(HD)),
                                      *reinterpret_cast<const __half*>(st + vs_at[1] + (16 * t + 8 * u) * scale_bytes(HD)));
+      // What lies behind the sequence's end, or was not copied, counts as zeros.
+      if (p0 + kChunk > n || ok != 3u) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int p = p0 + 16 * t + 8 * u;
+            const __half z = __float2half_rn(0.f);
+            const bool lo = p + place(2 * lc) < n && ((ok >> t) & 1), hi = p + place(2 * lc + 1) < n && ((ok >> t) & 1);
+            vsc[t][u] = __halves2half2(lo ? __low2half(vsc[t][u]) : z, hi ? __high2half(vsc[t][u]) : z);
+          }
+      }
       // A NaN must not meet the zero probabilities of rows that do not see its position:
       // its values count as zeros, and the rows that do see it become NaN below.
       int nan_at = INT32_MAX;                         // first position whose values here are NaN
@@ -685,11 +671,18 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         }
       }
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();     // the warps' parts are free again
     start += nc + kOpen;
     go = use.next(A);
   }
-  cp_wait<0>();
+  if (abort_flag) {      // a copy did not come: the results are not whole; the others' writes are waited for
+    volatile int ignored = 0;
+    for (int s = 0; s < kStages; ++s)
+      if (issued > s)
+        ptx::mbar_wait_bounded(&full[warp * kStages + s], ((issued - s - 1) / kStages) & 1, kWaitLimitNs, &ignored);
+    if (lane == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_TIMEOUT);
+  }
 }
 
 }  // namespace kv4
