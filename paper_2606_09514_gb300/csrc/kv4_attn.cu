@@ -137,19 +137,24 @@ __device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, uint64_
                                            int g, int p0) {
   constexpr int CB = code_bytes(HD), SB = scale_bytes(HD);
   const uint32_t b = ptx::smem_u32(bar);
-  auto copies = [&](int64_t block, int in_page, int at, int n) {
-    const int64_t codes = block + in_page * CB, scales = block + ((int64_t)CB << P.shift) + in_page * SB;
-    bulk_load(dst + at * CB, P.k + codes, n * CB, b);
-    bulk_load(dst + (kChunk + at) * CB, P.v + codes, n * CB, b);
-    bulk_load(dst + 2 * kChunk * CB + at * SB, P.k + scales, n * SB, b);
-    bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, P.v + scales, n * SB, b);
+  auto copies = [&](int page, int in_page, int at, int n) {
+    // (the blocks' count fits in 32 bits: one has 576 bytes at least)
+    const uint32_t block = (uint32_t)page * (uint32_t)P.nkv + (uint32_t)g;
+    const uint8_t* const k = P.k + (uint64_t)block * (uint32_t)(entry_bytes(HD) << P.shift) + (uint32_t)(in_page * CB);
+    const uint32_t to_scales = (uint32_t)((CB << P.shift) - in_page * (CB - SB));
+    const uint8_t* const v = k + (P.v - P.k);
+    bulk_load(dst + at * CB, k, n * CB, b);
+    bulk_load(dst + (kChunk + at) * CB, v, n * CB, b);
+    bulk_load(dst + 2 * kChunk * CB + at * SB, k + to_scales, n * SB, b);
+    bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, v + to_scales, n * SB, b);
   };
-  ptx::mbar_arrive_expect_tx(bar, (uint32_t)__popc(ok) * 16 * 2 * entry_bytes(HD));
   if (P.shift > 4) {
-    if (ok) copies(block_at<HD>(P, page0, g), p0 & ((1 << P.shift) - 1), 0, kChunk);
+    ptx::mbar_arrive_expect_tx(bar, ok ? 2 * kChunk * entry_bytes(HD) : 0);
+    if (ok) copies(page0, p0 & ((1 << P.shift) - 1), 0, kChunk);
   } else {
-    if (ok & 1) copies(block_at<HD>(P, page0, g), 0, 0, 16);
-    if (ok & 2) copies(block_at<HD>(P, page1, g), 0, 16, 16);
+    ptx::mbar_arrive_expect_tx(bar, (uint32_t)__popc(ok) * 16 * 2 * entry_bytes(HD));
+    if (ok & 1) copies(page0, 0, 0, 16);
+    if (ok & 2) copies(page1, 0, 16, 16);
   }
 }
 
@@ -276,31 +281,28 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     }
   };
   uint32_t there = 0;               // two bits per chunk in flight, the oldest lowest: 16 positions whose page is there
-  int flying = 0, put = 0, take = 0, issued = 0;
-  uint32_t phase = 0;               // of the stage to take
-  auto issue = [&]() {
+  int take = 0, issued = 0;         // the stage to take, and its phase
+  uint32_t phase = 0;
+  auto issue = [&](int stage, int ahead) {
     if (more) {
       const int p0 = ld.c * kChunk;
       uint32_t ok = 3;
-      if ((uint32_t)id0 >= (uint32_t)A.p.n_pages || (uint32_t)id1 >= (uint32_t)A.p.n_pages) {
-        if ((uint32_t)id0 >= (uint32_t)A.p.n_pages) ok &= 2;
-        if ((uint32_t)id1 >= (uint32_t)A.p.n_pages) ok &= 1;
+      if (max((uint32_t)id0, (uint32_t)id1) >= (uint32_t)A.p.n_pages) {
+        ok = ((uint32_t)id0 < (uint32_t)A.p.n_pages ? 1 : 0) + ((uint32_t)id1 < (uint32_t)A.p.n_pages ? 2 : 0);
         if (lane == 0 && A.flags && p0 < ld.q.n) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
       }
       __syncwarp();
       if (ptx::elect_one())
-        load_chunk<HD>(A.p, ring + put * stage_bytes<HD>(), &full[warp * kStages + put], id0, id1, ok, ld.g, p0);
-      there |= ok << (2 * flying);
+        load_chunk<HD>(A.p, ring + stage * stage_bytes<HD>(), &full[warp * kStages + stage], id0, id1, ok, ld.g, p0);
+      there |= ok << (2 * ahead);
       ld.c += kWarps;
       ++issued;
       fetch_ids();
     }
-    ++flying;
-    put = put + 1 == kStages ? 0 : put + 1;
   };
   fetch_ids();
 #pragma unroll 1
-  for (int s = 0; s < kStages - 1; ++s) issue();
+  for (int s = 0; s < kStages - 1; ++s) issue(s, s);
 
   // where a lane's codes and scales are in a stage: keys of row lg, values of rows 2 lc and 2 lc + 1
   constexpr int VC = kChunk * code_bytes(HD), KSC = 2 * VC, VSC = KSC + kChunk * scale_bytes(HD);
@@ -365,9 +367,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       const uint8_t* st = smem + (warp * kStages + take) * stage_bytes<HD>();
       const uint32_t ok = there & 3u;
       there >>= 2;
-      --flying;
-      take = take + 1 == kStages ? 0 : take + 1;
-      phase ^= take == 0;
+      issue(take == 0 ? kStages - 1 : take - 1, kStages - 2);   // to the stage that the chunk before this one has left
       const int p0 = c * kChunk;
 
       // ---- S^T
@@ -464,34 +464,27 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         for (int u = 0; u < 2; ++u)
           vsc[t][u] = __halves2half2(*reinterpret_cast<const __half*>(st + vs_at[0] + (16 * t + 8 * u) * scale_bytes(HD)),
                                      *reinterpret_cast<const __half*>(st + vs_at[1] + (16 * t + 8 * u) * scale_bytes(HD)));
-      // What lies behind the sequence's end, or was not copied, counts as zeros.
-      if (p0 + kChunk > n || ok != 3u) {
+      int nan_at = INT32_MAX;                         // first position whose values here are NaN
+      bool has_nan = false;
+      if (cut) {
+        // What lies behind the sequence's end, or was not copied, counts as zeros.  And a NaN
+        // must not meet the zero probabilities of rows that do not see its position: its
+        // values count as zeros, and the rows that do see it become NaN below.
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const int p = p0 + 16 * t + 8 * u;
-            const __half z = __float2half_rn(0.f);
-            const bool lo = p + place(2 * lc) < n && ((ok >> t) & 1), hi = p + place(2 * lc + 1) < n && ((ok >> t) & 1);
-            vsc[t][u] = __halves2half2(lo ? __low2half(vsc[t][u]) : z, hi ? __high2half(vsc[t][u]) : z);
-          }
-      }
-      // A NaN must not meet the zero probabilities of rows that do not see its position:
-      // its values count as zeros, and the rows that do see it become NaN below.
-      int nan_at = INT32_MAX;                         // first position whose values here are NaN
-      const __half2 probe = __hadd2(__hadd2(vsc[0][0], vsc[0][1]), __hadd2(vsc[1][0], vsc[1][1]));
-      const bool has_nan = __any_sync(0xffffffffu, !__hbeq2(probe, probe));   // (NaN spreads through sums)
-      if (has_nan) {
+            __half x[2] = {__low2half(vsc[t][u]), __high2half(vsc[t][u])};
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            __half x = (u & 1) ? __high2half(vsc[t][u >> 1]) : __low2half(vsc[t][u >> 1]);
-            if (!__hisnan(x)) continue;
-            nan_at = min(nan_at, p0 + 16 * t + place(2 * lc + (u & 1)) + 8 * (u >> 1));
-            const __half2 z = vsc[t][u >> 1], o2 = __float2half2_rn(0.f);
-            vsc[t][u >> 1] = (u & 1) ? __lows2half2(z, o2) : __highs2half2(o2, z);
+            for (int e = 0; e < 2; ++e) {
+              const int pos = p0 + 16 * t + place(2 * lc + e) + 8 * u;
+              const bool real = pos < n && ((ok >> t) & 1), nan = __hisnan(x[e]);
+              if (real && nan) nan_at = min(nan_at, pos);
+              if (!real || nan) x[e] = __float2half_rn(0.f);
+            }
+            vsc[t][u] = __halves2half2(x[0], x[1]);
           }
+        has_nan = __any_sync(0xffffffffu, nan_at != INT32_MAX);
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -536,12 +529,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
             for (int e = 0; e < 4; ++e)
               if (nan_at < seen[b][e & 1]) o[b][t][e] = __uint_as_float(0x7FC00000u);
       }
-      __syncwarp();
-      issue();
+      take = take + 1 == kStages ? 0 : take + 1;
+      phase ^= take == 0;
     }
 
-    // ---- join the warps (a stage is free: `put` of the last copy is one behind `take`): a lane has rows 2 lc, 2 lc + 1 of each block, HD / 8 channels from lg * HD / 8 on
-    if (lane == 0) s_stage[warp] = put;
+    // ---- join the warps, in the stages taken last: a lane has rows 2 lc, 2 lc + 1 of each block,
+    // HD / 8 channels from lg * HD / 8 on
+    if (lane == 0) s_stage[warp] = take == 0 ? kStages - 1 : take - 1;
     __syncwarp();
     float* const mine = part_of(warp);
 #pragma unroll
