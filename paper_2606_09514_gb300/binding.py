@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -87,6 +88,17 @@ class buddy_kv4_attention_args(ctypes.Structure):
                 ("table", c_p), ("workspace", c_p), ("workspace_bytes", ctypes.c_int64)]
 
 
+def _packer(cls):
+    """A Structure's values to its bytes: a third of the time that making one takes."""
+    codes = {c_i32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", c_p: "P"}
+    s = struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0q")
+    assert s.size == ctypes.sizeof(cls)
+    return s.pack
+
+
+_pack_plan, _pack_rows, _pack_attention = map(_packer, (buddy_page_plan_args, buddy_qk_rows, buddy_kv4_attention_args))
+
+
 class BuddyError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: libbuddy error {code}")
@@ -155,6 +167,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                  "buddy_decode_step_host", "buddy_set_options", "buddy_device_status", "buddy_set_profiling",
                  "buddy_profile_read"):
         getattr(lib, name).restype = ctypes.c_int
+    # The same entries for calls with packed arguments
+    for name, args in (("buddy_page_plan", [c_p] * 3), ("buddy_qk_norm_rope", [c_p] * 3),
+                       ("buddy_kv4_append", [c_p, c_p, c_p, ctypes.c_int64, c_p, c_p, c_p]),
+                       ("buddy_kv4_read", [c_p, c_i32, c_p, c_i32, c_p, c_p, c_p, c_p]),
+                       ("buddy_kv4_attention", [c_p] * 4)):
+        f = lib[name]
+        f.argtypes, f.restype = args, ctypes.c_int
+        setattr(lib, "packed_" + name, f)
     if path is None:
         _lib = lib
     return lib
@@ -251,6 +271,7 @@ class Context:
     def __init__(self, *, n_layers, d_model, n_q_heads, n_kv_heads, head_dim, ffn_dim, dm_hidden, dtype,
                  max_batch, max_pos, qkv_bias, rms_eps, rope_theta, feature="v", ctx_layer=0, skip_kv="zero",
                  max_prefill_tokens=0):
+        self._state = ctypes.addressof(self.state)
         self.lib = load_library()
         cfg = buddy_config(n_layers, d_model, n_q_heads, n_kv_heads, head_dim, ffn_dim, dm_hidden,
                            BUDDY_DTYPE_BF16 if dtype == "bf16" else BUDDY_DTYPE_F32, max_batch, max_pos,
@@ -409,8 +430,8 @@ def _stream_of(t: torch.Tensor, stream) -> int:
     return _raw_stream(t.get_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
 
 
-def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _addr(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
 
 
 def buddy_rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None):
@@ -434,13 +455,13 @@ def buddy_page_plan(length: torch.Tensor, n_new: torch.Tensor, page_size: int, t
     rows = table.shape
     if len(rows) != 2 or rows[0] != B:
         raise ValueError("table: [batch, max_pages] is wanted")
-    a = buddy_page_plan_args(B, page_size, rows[1], free_pages.numel(), T, length.data_ptr(), n_new.data_ptr(),
-                             table.data_ptr(), free_pages.data_ptr(), free_head.data_ptr(), kv_len.data_ptr(),
-                             row_start.data_ptr(), slot.data_ptr(), pos.data_ptr(), free_head_out.data_ptr())
-    _check(load_library().buddy_page_plan(a, _addr(flags), _stream_of(length, stream)), "buddy_page_plan")
+    a = _pack_plan(B, page_size, rows[1], free_pages.numel(), T, length.data_ptr(), n_new.data_ptr(),
+                   table.data_ptr(), free_pages.data_ptr(), free_head.data_ptr(), kv_len.data_ptr(),
+                   row_start.data_ptr(), slot.data_ptr(), pos.data_ptr(), free_head_out.data_ptr())
+    _check(load_library().packed_buddy_page_plan(a, _addr(flags), _stream_of(length, stream)), "buddy_page_plan")
 
 
-def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags) -> buddy_qk_rows:
+def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags) -> bytes:
     dt, shape, f32 = k.dtype, k.shape, torch.float32
     if len(shape) != 3 or dt not in _DTYPES:
         raise ValueError("k: [tokens, heads, head_dim] of fp32 or bf16 is wanted")
@@ -458,9 +479,9 @@ def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags) -> buddy
     rows = co.size(0)
     _vectors((q_gain, f32, hd, "q_gain"), (k_gain, f32, hd, "k_gain"), (pos, torch.int32, T, "pos"),
              (co, f32, rows * hd // 2, "cos"), (si, f32, rows * hd // 2, "sin"), (flags, torch.int32, 1, "flags"))
-    return buddy_qk_rows(T, nq, nkv, hd, _DTYPES[dt], rows, eps, _addr(q), k.data_ptr(), q_stride, k_stride,
-                         _addr(q_gain), _addr(k_gain), pos.data_ptr(), co.data_ptr(), si.data_ptr(),
-                         _addr(q_out) if nq else None, _addr(k_out), q_out_stride, k_out_stride)
+    return _pack_rows(T, nq, nkv, hd, _DTYPES[dt], rows, eps, _addr(q), k.data_ptr(), q_stride, k_stride,
+                      _addr(q_gain), _addr(k_gain), pos.data_ptr(), co.data_ptr(), si.data_ptr(),
+                      _addr(q_out) if nq else 0, _addr(k_out), q_out_stride, k_out_stride)
 
 
 def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Tensor, rope, q_out, k_out,
@@ -469,7 +490,7 @@ def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Te
     """Norm of each query and key head (with gains) and rotation, in one pass.
     q, k, q_out, k_out: [tokens, heads, head_dim], fp32 or bf16; rope: (cos, sin)."""
     r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags)
-    _check(load_library().buddy_qk_norm_rope(r, _addr(flags), _stream_of(k, stream)), "buddy_qk_norm_rope")
+    _check(load_library().packed_buddy_qk_norm_rope(r, _addr(flags), _stream_of(k, stream)), "buddy_qk_norm_rope")
 
 
 class KV4Cache:
@@ -489,6 +510,7 @@ class KV4Cache:
         self.k_pages, self.v_pages, self.page_size, self.n_kv = k_pages, v_pages, page_size, n_kv
         _vectors((k_pages, torch.uint8, 0, "k_pages"), (v_pages, torch.uint8, 0, "v_pages"))
         self.state = buddy_kv4_cache(k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size, n_kv, self.head_dim)
+        self._state = ctypes.addressof(self.state)
         self.lib = load_library()
         self.workspace = workspace
         self._made: List = []           # workspaces made here; calls under way may still use an older one
@@ -516,9 +538,10 @@ class KV4Cache:
                          k_out: Optional[torch.Tensor] = None, stream=None):
         """buddy_qk_norm_rope, with the keys and values v stored at `slot`."""
         r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags)
-        _vectors((slot, torch.int64, r.n_tok, "slot"))
-        _check(self.lib.buddy_kv4_append(self.state, r, v.data_ptr(), _heads(v, k.dtype, k.shape, "v"), slot.data_ptr(),
-                                         _addr(flags), _stream_of(k, stream)), "buddy_kv4_append")
+        _vectors((slot, torch.int64, k.shape[0], "slot"))
+        _check(self.lib.packed_buddy_kv4_append(self._state, r, v.data_ptr(), _heads(v, k.dtype, k.shape, "v"),
+                                                slot.data_ptr(), _addr(flags), _stream_of(k, stream)),
+               "buddy_kv4_append")
 
     def buddy_kv4_read(self, slot: torch.Tensor, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor],
                        flags: Optional[torch.Tensor] = None, stream=None):
@@ -531,8 +554,8 @@ class KV4Cache:
         size = n * self.n_kv * self.head_dim
         _vectors((slot, torch.int64, n, "slot"), (k_out, dt, size, "k_out"), (v_out, dt, size, "v_out"),
                  (flags, torch.int32, 1, "flags"))
-        _check(self.lib.buddy_kv4_read(self.state, n, slot.data_ptr(), _DTYPES[dt], _addr(k_out), _addr(v_out),
-                                       _addr(flags), _stream_of(slot, stream)), "buddy_kv4_read")
+        _check(self.lib.packed_buddy_kv4_read(self._state, n, slot.data_ptr(), _DTYPES[dt], _addr(k_out), _addr(v_out),
+                                              _addr(flags), _stream_of(slot, stream)), "buddy_kv4_read")
 
     def buddy_kv4_attention(self, q: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, out: torch.Tensor,
                             row_start: Optional[torch.Tensor] = None, max_new: int = 1, scale: float = 0.0,
@@ -555,7 +578,8 @@ class KV4Cache:
         rows = table.shape
         if len(rows) != 2 or rows[0] != B:
             raise ValueError("table: [batch, max_pages] is wanted")
-        a = buddy_kv4_attention_args(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1), rows[1],
-                                     scale, q.data_ptr(), out.data_ptr(), q_stride, out_stride, _addr(row_start),
-                                     kv_len.data_ptr(), table.data_ptr(), ws.data_ptr(), ws.numel())
-        _check(self.lib.buddy_kv4_attention(self.state, a, _addr(flags), _stream_of(q, stream)), "buddy_kv4_attention")
+        a = _pack_attention(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1), rows[1], scale,
+                            q.data_ptr(), out.data_ptr(), q_stride, out_stride, _addr(row_start), kv_len.data_ptr(),
+                            table.data_ptr(), ws.data_ptr(), ws.numel())
+        _check(self.lib.packed_buddy_kv4_attention(self._state, a, _addr(flags), _stream_of(q, stream)),
+               "buddy_kv4_attention")
