@@ -1,11 +1,12 @@
-"""ctypes binding of libbuddy (include/buddy.h).  Argument marshalling only:
+"""Binding of libbuddy (include/buddy.h), by ctypes; the 4-bit cache's entries, some of
+them called for a single token, by the compiled _calls.  Argument marshalling only:
 every step of the decode path runs in the library's CUDA kernels; PyTorch
 provides device memory and streams.  Raises if the library is missing."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
-import struct
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -88,17 +89,6 @@ class buddy_kv4_attention_args(ctypes.Structure):
                 ("table", c_p), ("workspace", c_p), ("workspace_bytes", ctypes.c_int64)]
 
 
-def _packer(cls):
-    """A Structure's values to its bytes: a third of the time that making one takes."""
-    codes = {c_i32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", c_p: "P"}
-    s = struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0q")
-    assert s.size == ctypes.sizeof(cls)
-    return s.pack
-
-
-_pack_plan, _pack_rows, _pack_attention = map(_packer, (buddy_page_plan_args, buddy_qk_rows, buddy_kv4_attention_args))
-
-
 class BuddyError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: libbuddy error {code}")
@@ -167,14 +157,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                  "buddy_decode_step_host", "buddy_set_options", "buddy_device_status", "buddy_set_profiling",
                  "buddy_profile_read"):
         getattr(lib, name).restype = ctypes.c_int
-    # The same entries for calls with packed arguments
-    for name, args in (("buddy_page_plan", [c_p] * 3), ("buddy_qk_norm_rope", [c_p] * 3),
-                       ("buddy_kv4_append", [c_p, c_p, c_p, ctypes.c_int64, c_p, c_p, c_p]),
-                       ("buddy_kv4_read", [c_p, c_i32, c_p, c_i32, c_p, c_p, c_p, c_p]),
-                       ("buddy_kv4_attention", [c_p] * 4)):
-        f = lib[name]
-        f.argtypes, f.restype = args, ctypes.c_int
-        setattr(lib, "packed_" + name, f)
+    try:
+        from . import _calls
+    except ImportError as e:
+        raise RuntimeError(f"_calls.so does not load ({e}): run __graft_entry__.build() first") from e
+    for name in ("page_plan", "qk_norm_rope", "kv4_append", "kv4_read", "kv4_attention"):
+        entry = ctypes.cast(getattr(lib, "buddy_" + name), c_p).value
+        setattr(lib, "call_" + name, functools.partial(getattr(_calls, name), entry))
     if path is None:
         _lib = lib
     return lib
@@ -271,7 +260,6 @@ class Context:
     def __init__(self, *, n_layers, d_model, n_q_heads, n_kv_heads, head_dim, ffn_dim, dm_hidden, dtype,
                  max_batch, max_pos, qkv_bias, rms_eps, rope_theta, feature="v", ctx_layer=0, skip_kv="zero",
                  max_prefill_tokens=0):
-        self._state = ctypes.addressof(self.state)
         self.lib = load_library()
         cfg = buddy_config(n_layers, d_model, n_q_heads, n_kv_heads, head_dim, ffn_dim, dm_hidden,
                            BUDDY_DTYPE_BF16 if dtype == "bf16" else BUDDY_DTYPE_F32, max_batch, max_pos,
@@ -401,7 +389,6 @@ class Context:
 # Paged 4-bit KV cache (see include/buddy.h).  The library sees addresses only:
 # what a tensor can say about itself (type, device, shape, strides) is checked here.
 # ---------------------------------------------------------------------------
-_DTYPES = {torch.float32: BUDDY_DTYPE_F32, torch.bfloat16: BUDDY_DTYPE_BF16, torch.float16: BUDDY_DTYPE_F16}
 
 
 def _vectors(*wanted):
@@ -409,29 +396,6 @@ def _vectors(*wanted):
     for t, dtype, n, what in wanted:
         if t is not None and (t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() < n):
             raise ValueError(f"{what}: a contiguous CUDA tensor of {n} or more {dtype} is wanted")
-
-
-def _heads(t: torch.Tensor, dtype, shape, what: str) -> int:
-    """Elements from token to token of a [tokens, heads, head_dim] view with whole heads."""
-    s = t.stride()
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or s[2] != 1 or (s[1] != shape[2] and shape[1] > 1):
-        raise ValueError(f"{what}: CUDA {dtype} {tuple(shape)} with whole heads one after the other is wanted")
-    return s[0]
-
-
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
-def _stream_of(t: torch.Tensor, stream) -> int:
-    """The stream given, or the current one of t's device (asked for directly: the
-    Stream object takes longer to make than a launch)."""
-    if stream is not None:
-        return stream.cuda_stream
-    return _raw_stream(t.get_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
-
-
-def _addr(t: Optional[torch.Tensor]) -> int:
-    return 0 if t is None else t.data_ptr()
 
 
 def buddy_rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None):
@@ -447,41 +411,8 @@ def buddy_page_plan(length: torch.Tensor, n_new: torch.Tensor, page_size: int, t
                     slot: torch.Tensor, pos: torch.Tensor, free_head_out: torch.Tensor,
                     flags: Optional[torch.Tensor] = None, stream=None):
     """Block tables, slots and positions of a call's new tokens from the lengths."""
-    B, T, i32 = length.numel(), slot.numel(), torch.int32
-    _vectors((length, i32, B, "length"), (n_new, i32, B, "n_new"), (table, i32, 0, "table"),
-             (free_pages, i32, 0, "free_pages"), (free_head, i32, 1, "free_head"), (kv_len, i32, B, "kv_len"),
-             (row_start, i32, B + 1, "row_start"), (slot, torch.int64, T, "slot"), (pos, i32, T, "pos"),
-             (free_head_out, i32, 1, "free_head_out"), (flags, i32, 1, "flags"))
-    rows = table.shape
-    if len(rows) != 2 or rows[0] != B:
-        raise ValueError("table: [batch, max_pages] is wanted")
-    a = _pack_plan(B, page_size, rows[1], free_pages.numel(), T, length.data_ptr(), n_new.data_ptr(),
-                   table.data_ptr(), free_pages.data_ptr(), free_head.data_ptr(), kv_len.data_ptr(),
-                   row_start.data_ptr(), slot.data_ptr(), pos.data_ptr(), free_head_out.data_ptr())
-    _check(load_library().packed_buddy_page_plan(a, _addr(flags), _stream_of(length, stream)), "buddy_page_plan")
-
-
-def _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags) -> bytes:
-    dt, shape, f32 = k.dtype, k.shape, torch.float32
-    if len(shape) != 3 or dt not in _DTYPES:
-        raise ValueError("k: [tokens, heads, head_dim] of fp32 or bf16 is wanted")
-    T, nkv, hd = shape
-    k_stride = _heads(k, dt, shape, "k")
-    k_out_stride = 0 if k_out is None else _heads(k_out, dt, shape, "k_out")
-    nq = q_stride = q_out_stride = 0
-    if q is not None:
-        nq = q.size(1)
-        q_stride = _heads(q, dt, (T, nq, hd), "q")
-        if q_out is None:
-            raise ValueError("q_out is wanted with q")
-        q_out_stride = _heads(q_out, dt, (T, nq, hd), "q_out")
-    co, si = rope
-    rows = co.size(0)
-    _vectors((q_gain, f32, hd, "q_gain"), (k_gain, f32, hd, "k_gain"), (pos, torch.int32, T, "pos"),
-             (co, f32, rows * hd // 2, "cos"), (si, f32, rows * hd // 2, "sin"), (flags, torch.int32, 1, "flags"))
-    return _pack_rows(T, nq, nkv, hd, _DTYPES[dt], rows, eps, _addr(q), k.data_ptr(), q_stride, k_stride,
-                      _addr(q_gain), _addr(k_gain), pos.data_ptr(), co.data_ptr(), si.data_ptr(),
-                      _addr(q_out) if nq else 0, _addr(k_out), q_out_stride, k_out_stride)
+    _check(load_library().call_page_plan(length, n_new, page_size, table, free_pages, free_head, kv_len, row_start,
+                                         slot, pos, free_head_out, flags, stream), "buddy_page_plan")
 
 
 def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Tensor, rope, q_out, k_out,
@@ -489,8 +420,9 @@ def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Te
                        eps: float = 1e-6, flags: Optional[torch.Tensor] = None, stream=None):
     """Norm of each query and key head (with gains) and rotation, in one pass.
     q, k, q_out, k_out: [tokens, heads, head_dim], fp32 or bf16; rope: (cos, sin)."""
-    r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags)
-    _check(load_library().packed_buddy_qk_norm_rope(r, _addr(flags), _stream_of(k, stream)), "buddy_qk_norm_rope")
+    co, si = rope
+    _check(load_library().call_qk_norm_rope(q, k, pos, co, si, q_out, k_out, q_gain, k_gain, eps, flags, stream),
+           "buddy_qk_norm_rope")
 
 
 class KV4Cache:
@@ -510,7 +442,7 @@ class KV4Cache:
         self.k_pages, self.v_pages, self.page_size, self.n_kv = k_pages, v_pages, page_size, n_kv
         _vectors((k_pages, torch.uint8, 0, "k_pages"), (v_pages, torch.uint8, 0, "v_pages"))
         self.state = buddy_kv4_cache(k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size, n_kv, self.head_dim)
-        self._state = ctypes.addressof(self.state)
+        self.address = ctypes.addressof(self.state)
         self.lib = load_library()
         self.workspace = workspace
         self._made: List = []           # workspaces made here; calls under way may still use an older one
@@ -537,49 +469,27 @@ class KV4Cache:
                          eps: float = 1e-6, flags: Optional[torch.Tensor] = None,
                          k_out: Optional[torch.Tensor] = None, stream=None):
         """buddy_qk_norm_rope, with the keys and values v stored at `slot`."""
-        r = _qk_rows(q, k, pos, rope, q_out, k_out, q_gain, k_gain, eps, flags)
-        _vectors((slot, torch.int64, k.shape[0], "slot"))
-        _check(self.lib.packed_buddy_kv4_append(self._state, r, v.data_ptr(), _heads(v, k.dtype, k.shape, "v"),
-                                                slot.data_ptr(), _addr(flags), _stream_of(k, stream)),
-               "buddy_kv4_append")
+        co, si = rope
+        _check(self.lib.call_kv4_append(self.address, q, k, pos, co, si, q_out, k_out, q_gain, k_gain, eps, v, slot,
+                                        flags, stream), "buddy_kv4_append")
 
     def buddy_kv4_read(self, slot: torch.Tensor, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor],
                        flags: Optional[torch.Tensor] = None, stream=None):
         """The values stored at `slot`: [n, n_kv, head_dim] of fp32, fp16 or bf16."""
-        n = slot.numel()
-        out = k_out if k_out is not None else v_out
-        dt = None if out is None else out.dtype
-        if dt not in _DTYPES:
-            raise ValueError("k_out, v_out: fp32, fp16 or bf16 is wanted")
-        size = n * self.n_kv * self.head_dim
-        _vectors((slot, torch.int64, n, "slot"), (k_out, dt, size, "k_out"), (v_out, dt, size, "v_out"),
-                 (flags, torch.int32, 1, "flags"))
-        _check(self.lib.packed_buddy_kv4_read(self._state, n, slot.data_ptr(), _DTYPES[dt], _addr(k_out), _addr(v_out),
-                                              _addr(flags), _stream_of(slot, stream)), "buddy_kv4_read")
+        _check(self.lib.call_kv4_read(self.address, slot, k_out, v_out, flags, stream), "buddy_kv4_read")
 
     def buddy_kv4_attention(self, q: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, out: torch.Tensor,
                             row_start: Optional[torch.Tensor] = None, max_new: int = 1, scale: float = 0.0,
                             flags: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                             stream=None):
         """Causal attention of query tokens over the cache; q, out [tokens, n_q, head_dim]."""
-        shape, B, i32 = q.shape, kv_len.numel(), torch.int32
-        if len(shape) != 3 or shape[2] != self.head_dim:
-            raise ValueError("q: [tokens, heads, head_dim of the cache] is wanted")
-        T, nq, _ = shape
-        q_stride, out_stride = _heads(q, q.dtype, shape, "q"), _heads(out, out.dtype, shape, "out")
         ws = workspace if workspace is not None else self.workspace
         if ws is None:
-            need = self.workspace_bytes(nq, max_new)
+            if q.dim() != 3:
+                raise ValueError("q: [tokens, heads, head_dim of the cache] is wanted")
+            need = self.workspace_bytes(q.shape[1], max_new)
             if not self._made or self._made[-1].numel() < need:
                 self._made.append(torch.zeros(need, dtype=torch.uint8, device=q.device))
             ws = self._made[-1]
-        _vectors((row_start, i32, B + 1, "row_start"), (kv_len, i32, B, "kv_len"), (table, i32, 0, "table"),
-                 (ws, torch.uint8, 0, "workspace"), (flags, i32, 1, "flags"))
-        rows = table.shape
-        if len(rows) != 2 or rows[0] != B:
-            raise ValueError("table: [batch, max_pages] is wanted")
-        a = _pack_attention(B, T, max_new, nq, _DTYPES.get(q.dtype, -1), _DTYPES.get(out.dtype, -1), rows[1], scale,
-                            q.data_ptr(), out.data_ptr(), q_stride, out_stride, _addr(row_start), kv_len.data_ptr(),
-                            table.data_ptr(), ws.data_ptr(), ws.numel())
-        _check(self.lib.packed_buddy_kv4_attention(self._state, a, _addr(flags), _stream_of(q, stream)),
-               "buddy_kv4_attention")
+        _check(self.lib.call_kv4_attention(self.address, q, kv_len, table, out, row_start, max_new, scale, flags, ws,
+                                           stream), "buddy_kv4_attention")

@@ -1,4 +1,5 @@
-"""Builds libbuddy.so in-tree with nvcc for sm_103a (no cmake, no torch)."""
+"""Builds libbuddy.so in-tree with nvcc for sm_103a (no cmake, no torch), and _calls.so,
+which turns tensors into its arguments, with the host compiler and torch's headers."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -6,6 +7,8 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
+from importlib.util import find_spec
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -13,6 +16,7 @@ OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbuddy.so")
 SOURCES = ["api.cu", "kernels.cu", "attention.cu", "gemm_simt.cu", "gemm_tc.cu", "noalloc.cu", "gemm_pf.cu",
            "attn_pf.cu", "prefill.cu", "attn_cl.cu", "pages.cu", "kv4_rows.cu", "kv4_attn.cu", "kv4_pf.cu"]
+CALLS = os.path.join(HERE, "_calls.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-Xptxas", "-warn-spills"]
@@ -34,6 +38,15 @@ def _stale(obj: str, src: str) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _calls_command(nvcc: str) -> list:
+    torch = os.path.dirname(find_spec("torch").origin)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc))), "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            "-I" + sysconfig.get_paths()["include"], "-isystem", os.path.join(torch, "include"), "-isystem", cuda,
+            os.path.join(CSRC, "calls.cpp"), "-o", CALLS + ".tmp", "-L" + os.path.join(torch, "lib"),
+            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+
+
 def build(verbose: bool = False, force: bool = False) -> str:
     nvcc = _nvcc()
     os.makedirs(OUT_DIR, exist_ok=True)
@@ -45,14 +58,20 @@ def build(verbose: bool = False, force: bool = False) -> str:
         objs.append(obj)
         if force or _stale(obj, src):
             jobs.append([nvcc, *ARCH, *FLAGS, "-c", src, "-o", obj])
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    kernels = bool(jobs)
+    calls = force or _stale(CALLS, os.path.join(CSRC, "calls.cpp"))
+    if calls:
+        jobs.append(_calls_command(nvcc))
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         results = list(ex.map(lambda cmd: subprocess.run(cmd, capture_output=True, text=True), jobs))
     for cmd, r in zip(jobs, results):
         if verbose or r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
         if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed: {' '.join(cmd)}")
-    if jobs or not os.path.exists(LIB):
+            raise RuntimeError(f"failed: {' '.join(cmd)}")
+    if calls:
+        os.replace(CALLS + ".tmp", CALLS)
+    if kernels or not os.path.exists(LIB):
         link = [nvcc, *ARCH, "-shared", "-o", LIB + ".tmp", *objs]
         r = subprocess.run(link, capture_output=True, text=True)
         if r.returncode != 0:
