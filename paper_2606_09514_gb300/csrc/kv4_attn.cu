@@ -177,10 +177,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   __shared__ int s_first, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
   const int B = A.a.batch, G = A.G;
-  pdl_trigger();   // (the prompts of the same call may start where there is room)
   if (tid < kWarps * kStages) ptx::mbar_init(&full[tid], 1);
   if (tid == 0) abort_flag = 0;
   ptx::fence_mbar_init();
+  pdl_wait();
+  pdl_trigger();   // (the prompts of the same call may start where there is room)
 
   // ---- this CTA's share: [lo, lo + share) of all streams' openings and chunks
   const int per = (B + kThreads - 1) / kThreads;
@@ -695,8 +696,7 @@ static int launch_decode(const AttnArgs4& A, int grid, cudaStream_t s) {
   constexpr int smem = smem_bytes<HD, NB>();
   if (cudaFuncSetAttribute(kv4_decode_kernel<HD, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
-  kv4_decode_kernel<HD, NB><<<grid, kThreads, smem, s>>>(A);
-  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  return launch_k(kv4_decode_kernel<HD, NB>, grid, kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 
 }  // namespace buddy

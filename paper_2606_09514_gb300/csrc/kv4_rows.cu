@@ -179,6 +179,8 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A) {
   const int tl = threadIdx.x % LPH;
   const uint32_t team = ((1u << LPH) - 1) << (threadIdx.x % 32 / LPH * LPH);   // this team's lanes
   const int64_t u = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / LPH;
+  pdl_wait();
+  pdl_trigger();
   // (the teams of a warp take the same heads of neighbouring tokens: queries, keys and
   // values go different ways)
   const int64_t grp = u / R.n_tok;
@@ -278,6 +280,8 @@ __global__ void __launch_bounds__(kRowThreads) kv4_read_kernel(const kv4::Pages 
   constexpr int LPH = HD / 8;
   const int64_t u = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / LPH;   // (entry, head)
   const int tl = threadIdx.x % LPH;
+  pdl_wait();
+  pdl_trigger();
   if (u >= (int64_t)n * P.nkv) return;
   const int64_t j = u / P.nkv;
   const int g = (int)(u - j * P.nkv);
@@ -354,8 +358,8 @@ static int launch_rows(RowArgs A, cudaStream_t s) {
   A.groups = (heads + A.per - 1) / A.per;
   const int64_t ctas = ((int64_t)A.r.n_tok * A.groups * (HD / 16) + kRowThreads - 1) / kRowThreads;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  qk_rows_kernel<T, HD, CACHE><<<(unsigned)ctas, kRowThreads, 0, s>>>(A);
-  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  return launch_k(qk_rows_kernel<T, HD, CACHE>, (unsigned)ctas, kRowThreads, 0, s, true, A) == cudaSuccess
+             ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 template <bool CACHE>
 static int dispatch_rows(const RowArgs& A, cudaStream_t s) {
@@ -370,11 +374,9 @@ static int launch_read(const buddy_kv4_cache* c, int n, const int64_t* slot, voi
                        cudaStream_t s) {
   const int64_t ctas = ((int64_t)n * c->n_kv_heads * (c->head_dim / 8) + kRowThreads - 1) / kRowThreads;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  if (c->head_dim == 128)
-    kv4_read_kernel<T, 128><<<(unsigned)ctas, kRowThreads, 0, s>>>(kv4_pages(c), n, slot, (T*)k, (T*)v, flags);
-  else
-    kv4_read_kernel<T, 64><<<(unsigned)ctas, kRowThreads, 0, s>>>(kv4_pages(c), n, slot, (T*)k, (T*)v, flags);
-  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  auto* const kern = c->head_dim == 128 ? kv4_read_kernel<T, 128> : kv4_read_kernel<T, 64>;
+  return launch_k(kern, (unsigned)ctas, kRowThreads, 0, s, true, kv4_pages(c), n, slot, (T*)k, (T*)v, flags) == cudaSuccess
+             ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 
 }  // namespace buddy

@@ -35,6 +35,8 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const buddy_pag
   __shared__ int64_t warp_tok[kPlanThreads / 32], warp_page[kPlanThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t mask = ((int64_t)1 << shift) - 1, room = (int64_t)A.max_pages << shift;
+  pdl_wait();
+  pdl_trigger();
 
   // consecutive sequences per thread: their sums, then a scan over the threads
   const int per = (A.batch + kPlanThreads - 1) / kPlanThreads;
@@ -133,6 +135,6 @@ extern "C" int buddy_page_plan(const buddy_page_plan_args* a, int32_t* flags, vo
       cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   const int grid = min(max(1, a->n_tok / kPlanPerCta + (a->n_tok % kPlanPerCta != 0)), 152);
-  page_plan_kernel<<<grid, kPlanThreads, smem, (cudaStream_t)stream>>>(*a, shift, flags);
-  return cudaGetLastError() == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  return launch_k(page_plan_kernel, grid, kPlanThreads, smem, (cudaStream_t)stream, true, *a, shift, flags) == cudaSuccess
+             ? BUDDY_OK : BUDDY_ERR_CUDA;
 }

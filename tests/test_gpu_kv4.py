@@ -570,6 +570,51 @@ def test_attention_shares_a_workspace_between_shapes_and_streams():
         side.synchronize()
 
 
+@pytest.mark.parametrize("m", [1, 3, 40])
+def test_calls_in_a_row_wait_for_each_other(m):
+    """Launches may overlap their predecessors' ends: a chain of calls with ordinary kernels
+    between them, enqueued at once, gives what it gives with the host waiting after each."""
+    nq, nkv, hd, page, B = 8, 2, 64, 16, 6
+    rope = pkg().buddy_rope_table(4096, hd, THETA)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    src = torch.randn(12, B * m, nq + 2 * nkv, hd, generator=g, device="cuda").bfloat16()
+    big = torch.randn(2048, 2048, device="cuda", generator=g)
+
+    def chain(wait):
+        cache = pkg().KV4Cache.empty(B * 64, page, nkv, hd)
+        table = torch.full((B, 64), -1, dtype=torch.int32, device="cuda")
+        free, head = torch.randperm(B * 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).int(), i32([0])
+        length, n_new, kv, rows, head2 = i32([0] * B), i32([m] * B), i32([0] * B), i32([0] * (B + 1)), i32([0])
+        slot, pos = torch.zeros(B * m, dtype=torch.int64, device="cuda"), i32([0] * (B * m))
+        x, q, k, fl, got = torch.empty_like(src[0]), torch.empty_like(src[0][:, :nq]), None, flags(), []
+        out = torch.empty_like(q)
+        kr = torch.empty(B * m, nkv, hd, dtype=torch.float32, device="cuda")
+        for i in range(len(src)):
+            (big @ big).sum()                       # something that takes a while
+            steps = [
+                lambda: x.copy_(src[i]),
+                lambda: pkg().buddy_page_plan(length, n_new, page, table, free, head, kv, rows, slot, pos, head2, fl),
+                lambda: cache.buddy_kv4_append(x[:, :nq], x[:, nq:nq + nkv], x[:, nq + nkv:], pos, slot, rope, q, flags=fl),
+                lambda: x.zero_(),
+                lambda: cache.buddy_kv4_attention(q, kv, table, out, rows, m, flags=fl),
+                lambda: cache.buddy_kv4_read(slot, kr, None, fl),
+                lambda: pkg().buddy_qk_norm_rope(None, kr, pos, rope, None, kr, flags=fl),
+                lambda: q.zero_(),
+                lambda: (got.append(out.clone()), got.append(kr.clone())),
+                lambda: (length.copy_(kv), head.copy_(head2), slot.fill_(-1), out.zero_()),
+            ]
+            for step in steps:
+                step()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert fl.item() == 0
+        return got
+
+    for a, b in zip(chain(False), chain(True)):
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
 def test_step_in_a_graph():
     """Plan, append and attention captured once, replayed as the sequences grow."""
     nq, nkv, hd, page, B = 6, 2, 64, 16, 5
