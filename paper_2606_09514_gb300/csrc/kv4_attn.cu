@@ -57,7 +57,9 @@ __host__ __device__ constexpr int ctas_per_sm() { return NB == 1 ? 4 : 3; }
 constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
 constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
 constexpr int kMaxGrid = 1024;   // CTAs: four on each of at most 256 SMs
-constexpr int kJoin = 16;        // partials in flight when a cut stream is joined
+constexpr int kJoin = 8;        // partials in flight when a cut stream is joined
+constexpr int kOneTeam = 24;     // spans up to which one CTA joins them all
+constexpr int kTeam = 4;         // spans of a team: a multiple of this
 // Rows of a KV head up to which these kernels take a sequence.  (28 rows over 4 KV heads, 16
 // sequences of 4,096 positions 57 us here, 45 us with the prompts' kernel; one of 30,000 43 and 32;
 // 100 of 600 67 and 68.)
@@ -173,7 +175,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   };
   constexpr int PM = ROWS * LDO, PL = PM + ROWS;
   __shared__ int64_t s_sum[kWarps], s_at;
-  __shared__ int s_streams[kWarps];
   __shared__ int s_first, s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lc = lane & 3;
   const int B = A.a.batch, G = A.G;
@@ -187,39 +188,31 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   const int per = (B + kThreads - 1) / kThreads;
   const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
   int64_t mine = 0;
-  int streams = 0;
   bool any_bad = false;
 #pragma unroll 1
   for (int i = b0; i < b1; ++i) {
     bool bad;
     const Rows q = few_rows(A, i, &bad);
     any_bad |= bad;
-    if (q.m > 0) mine += chunks_of(q.n) + kOpen, ++streams;
+    if (q.m > 0) mine += chunks_of(q.n) + kOpen;
   }
   if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
   mine *= A.p.nkv;
-  streams = __reduce_add_sync(0xffffffffu, streams);
   int64_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += v;
   }
-  if (lane == 31) s_sum[warp] = upto, s_streams[warp] = streams;
+  if (lane == 31) s_sum[warp] = upto;
   __syncthreads();
   int64_t total = 0;
-  streams = 0;
   for (int w = 0; w < kWarps; ++w) {
     if (w == warp) upto += total;
     total += s_sum[w];
-    streams += s_streams[w];
   }
   if (total == 0) return;
-  // A stream of n chunks in parts of x takes about x b / 4 + (n / x) (rows HD / 512) / 16 c: the chunks
-  // of a part, then the parts in the join; with b / c about 2.5 least at x = sqrt(0.4 n passes).
-  const float fair = (float)(total / A.p.nkv - (int64_t)streams * kOpen) / (float)streams;
-  const int64_t least = (int64_t)sqrtf(0.4f * fair * (float)A.passes) + 1;
-  const int share = (int)min((int64_t)INT32_MAX / 2, (max(least, (total + gridDim.x - 1) / gridDim.x) + kWarps - 1) / kWarps * kWarps);
+  const int share = (int)min((int64_t)INT32_MAX / 2, ((total + gridDim.x - 1) / gridDim.x + kWarps - 1) / kWarps * kWarps);
   const int64_t lo = (int64_t)blockIdx.x * share;
   if (lo >= total) return;
   if (upto - mine <= lo && lo < upto) {
@@ -591,36 +584,29 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       }
     }
     if (!whole) {
-      __syncthreads();   // the partial's writes come before the arrival, which releases them
-      const int spans = last_cta - first_cta + 1;
-      if (tid == 0) {
-        s_last = ptx::atom_add_acq_rel(A.arrive + first_cta, 1) == spans - 1;
-        if (s_last) A.arrive[first_cta] = 0;
-      }
-      __syncthreads();
-      if (s_last) {
-        // kJoin spans' loads at a time into a running log-sum-exp
-        constexpr int64_t PF = partial_floats<HD, NB>();
-        const float* p0 = A.part + (2 * (int64_t)first_cta + 1) * PF;      // the first span's partial, and the
-        const float* p1 = A.part + 2 * ((int64_t)first_cta + 1) * PF;      // second's; the others 2 PF apart
-        const int items = rows * (HD / 4);
-        // few rows: the spans go over as many groups of threads as there are
-        const int groups = items < kThreads ? kThreads / items : 1, grp = items < kThreads ? tid / items : 0;
+      constexpr int64_t PF = partial_floats<HD, NB>();
+      const int spans = last_cta - first_cta + 1, span = (int)blockIdx.x - first_cta;
+      const int items = rows * (HD / 4);
+      // few rows: the spans go over as many groups of threads as there are
+      const int groups = items < kThreads ? kThreads / items : 1, grp = items < kThreads ? tid / items : 0;
+      auto slot = [&](int cta, int which) { return A.part + (2 * (int64_t)cta + which) * PF; };
+      // `count` partials, partial k at from(k), kJoin at a time into a running log-sum-exp
+      auto join = [&](int count, auto from, auto emit) {
 #pragma unroll 1
         for (int x = tid - grp * items; x < items && grp < groups; x += kThreads) {
           const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
           float M = -INFINITY, L = 0.f;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-          for (int k0 = grp; k0 < spans; k0 += kJoin * groups) {
+          for (int k0 = grp; k0 < count; k0 += kJoin * groups) {
             float m[kJoin], l[kJoin], to = M;
             float4 y[kJoin];
 #pragma unroll
             for (int i = 0; i < kJoin; ++i) {
               const int k = k0 + i * groups;
-              const float* p = k == 0 ? p0 : p1 + (k - 1) * (2 * PF);
               m[i] = -INFINITY, l[i] = 0.f, y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (k < spans) {
+              if (k < count) {
+                const float* p = from(k);
                 m[i] = __ldcg(p + r), l[i] = __ldcg(p + ROWS + r);
                 y[i] = __ldcg(reinterpret_cast<const float4*>(p + 2 * ROWS + x * 4));
               }
@@ -638,8 +624,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
             M = to;
           }
           if (groups == 1) {
-            const float inv = M == -INFINITY ? 0.f : 1.f / L;
-            out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            emit(r, ch, M, L, v);
           } else {
             reinterpret_cast<float4*>(part_of(0))[grp * items + x] = v;
             if (ch == 0) part_of(0)[PM + grp * rows + r] = M, part_of(0)[PL + grp * rows + r] = L;
@@ -660,10 +645,51 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
               L += a * pw[PL + k * rows + r];
               v.x += a * y.x, v.y += a * y.y, v.z += a * y.z, v.w += a * y.w;
             }
-            const float inv = M == -INFINITY ? 0.f : 1.f / L;
-            out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            emit(r, ch, M, L, v);
           }
         }
+      };
+      auto finish = [&](int r, int ch, float M, float L, float4 v) {
+        const float inv = M == -INFINITY ? 0.f : 1.f / L;
+        out4(r, ch, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+      };
+      // True in the last of `count` CTAs that come here with this counter.
+      auto last_of = [&](int counter, int count) {
+        __syncthreads();   // the partial's writes come before the arrival, which releases them
+        if (tid == 0) {
+          s_last = ptx::atom_add_acq_rel(A.arrive + counter, 1) == count - 1;
+          if (s_last) A.arrive[counter] = 0;
+        }
+        __syncthreads();
+        return s_last != 0;
+      };
+      // The first span's partial is its CTA's second one, the others are their CTAs' first.
+      auto span_at = [&](int k) { return slot(first_cta + k, k == 0 ? 1 : 0); };
+      if (spans <= kOneTeam) {
+        if (last_of(first_cta, spans)) join(spans, span_at, finish);
+      } else {
+        // Many spans: in about as many teams as a team has spans, then the teams.  What a team
+        // has joined goes to the second partial of a CTA that begins no stream, its first one
+        // (of the first team: its second), whose counter is the team's.
+        int team = kTeam;
+        while (team * team < spans) team += kTeam;
+        const int teams = (spans + team - 1) / team, mine_k = span / team;
+        auto host = [&](int t) { return first_cta + (t == 0 ? 1 : t * team); };
+        const int in_team = min(team, spans - mine_k * team);
+        bool go_on = true;
+        if (in_team > 1) {
+          go_on = last_of(host(mine_k), in_team);
+          if (go_on) {
+            float* const to = slot(host(mine_k), 1);
+            join(in_team, [&](int k) { return span_at(mine_k * team + k); },
+                 [&](int r, int ch, float M, float L, float4 v) {
+                   if (ch == 0) to[r] = M, to[ROWS + r] = L;
+                   *reinterpret_cast<float4*>(to + 2 * ROWS + r * HD + ch) = v;
+                 });
+          }
+        }
+        if (go_on && last_of(first_cta, teams))
+          join(teams, [&](int t) { return t * team + 1 == spans ? span_at(t * team) : slot(host(t), 1); }, finish);
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -748,7 +774,6 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   // one CTA for every four chunks there can be, three on each SM at most
   const int64_t most_rows = (int64_t)a->max_new * A.G;
   const bool two = most_rows > 8;
-  A.passes = (int)((std::min<int64_t>(most_rows, two ? 16 : 8) * (cache->head_dim / 4) + kThreads - 1) / kThreads);
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
   const int64_t most = (int64_t)a->batch * cache->n_kv_heads * (chunks + kOpen) / kWarps + 1;
   const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, (two ? ctas_per_sm<2>() : ctas_per_sm<1>()) * sms));

@@ -17,7 +17,6 @@ struct AttnArgs4 {
   int32_t* flags;
   int32_t* arrive;            // few rows: [grid], zero between calls
   float* part;                // partials of streams or items that are cut
-  int passes;                 // few rows: rounds of a CTA's threads over a stream's outputs
 };
 
 // A sequence's query tokens t0 .. t0 + m - 1 and its n positions; m = 0 where they are bad.
