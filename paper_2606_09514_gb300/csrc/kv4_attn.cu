@@ -16,22 +16,30 @@
 //                 four positions, whose code words are put side by side by halves; P^T
 //                 is S^T's accumulator transposed in registers (movmatrix).
 //
-// Codes become halves in one logical and one fused multiply-add instruction per pair
-// (kv4.cuh), exactly.  Queries are scaled by a power of two per row to 1 .. 2 and
-// rounded to half (11 bits; bf16 queries lose nothing), the power goes into the
-// softmax's factor.  Probabilities are rounded to half for the product only (their
-// sum is taken before): 2^-12 of the largest value at most.
+// Codes become halves in one logical and one or two arithmetic instructions per pair
+// (kv4_attn.cuh), exactly.  Queries are scaled by a power of two per row to 1 .. 2 and
+// rounded to half (11 bits, below 2^-14 of the row's largest 2^-25 of it), the power goes
+// into the softmax's factor.  Probabilities are rounded to half for the product only (their sum is taken
+// before): 2^-12 of the largest value at most.
 //
 // Work: all streams end to end, each as its chunks of 32 positions and kOpen chunks'
-// worth for its beginning and end, in equal shares per CTA (31 sequences of 100 to
-// 4,096 positions, 40 KV heads: 174 us with shares of chunks alone, 93, 70, 72 and 77 us
-// with 4, 8, 16 and 24 for an opening; 250 sequences of 512 to 8,192, 4 KV heads: 121, then
-// 110, 104, 106, 113; a short stream belongs to the share where it begins: what a CTA saves by passing on
-// a part of it, the partials cost again); in a share, four warps take the chunks of a stream in turn, each with its own ring of
-// cp.async buffers that runs on across streams; rows past the sequence's end and
-// pages that are not there are filled with zeros and masked.  A stream within a share
-// is written out; the CTAs of one that is cut write partials, and the last of them
-// (an arrival counter) joins them in order.
+// worth for its beginning and end, in equal shares per CTA.  (With kOpen 4, 8, 10 and 12:
+// 250 sequences of 512 to 8,192 positions and 4 KV heads 98.9, 93.0, 89.5 and 90.5 us; 31
+// of 100 to 4,096 with up to five new tokens and 40 KV heads 76, 60, 60 and 61.)  A short
+// stream belongs to the share where it begins: what a CTA saves by passing on a part of it,
+// the partials cost again.  In a share, four warps take the chunks of a stream in turn,
+// each with its own ring of stages, which runs on across streams: one lane copies a chunk
+// in four bulk copies, in whole halves of 16 positions, and what lies behind the sequence's
+// end, or has no page, is masked.  A stream within a share is written out; the CTAs of one
+// that is cut write partials, which are joined in order by the last of them to arrive or,
+// where they are many, by teams first (one sequence of 120,001 positions, 4 KV heads, 152
+// CTAs each: 49 us with one join, 32 with teams).
+//
+// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 119 us,
+// their copies alone 91 us (94% of HBM's rate), the arithmetic alone 100; a chunk is about
+// 700 instructions of a warp, 350 of them codes to halves.  One token over 2,048 positions
+// takes 8.5 us: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
+// for two chunks, 4 for partials, arrival and join.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -55,14 +63,14 @@ constexpr int kStages = 3;
 template <int NB>
 __host__ __device__ constexpr int ctas_per_sm() { return NB == 1 ? 4 : 3; }
 constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
-constexpr int kOpen = 8;         // what beginning and ending a stream costs, in chunks
+constexpr int kOpen = 10;        // what beginning and ending a stream costs, in chunks
 constexpr int kMaxGrid = 1024;   // CTAs: four on each of at most 256 SMs
-constexpr int kJoin = 8;        // partials in flight when a cut stream is joined
+constexpr int kJoin = 8;         // partials in flight when a cut stream is joined
 constexpr int kOneTeam = 24;     // spans up to which one CTA joins them all
 constexpr int kTeam = 4;         // spans of a team: a multiple of this
-// Rows of a KV head up to which these kernels take a sequence.  (28 rows over 4 KV heads, 16
-// sequences of 4,096 positions 57 us here, 45 us with the prompts' kernel; one of 30,000 43 and 32;
-// 100 of 600 67 and 68.)
+// Rows of a KV head up to which these kernels take a sequence.  (With a limit of 32, 28 rows
+// over 4 KV heads took, 16 sequences of 4,096 positions, 57 us here and 45 us with the
+// prompts' kernel; one of 30,000 43 and 32; 100 of 600 67 and 68.)
 constexpr int kFewRows = 16;
 
 template <int HD>
@@ -131,33 +139,21 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 // value loads meet in a bank more than they have to.
 __device__ __forceinline__ int place(int r) { return r ^ ((r >> 1) & 1); }
 
-// Copies of one chunk into a stage, by one lane: K codes, V codes, K scales, V scales, in
-// whole halves of 16 positions (what lies behind the sequence's end is in the block too).
-// page0, page1: pages of the lower and the upper 16 positions; ok: two bits, which to copy.
-template <int HD>
-__device__ __forceinline__ void load_chunk(const Pages& P, uint32_t dst, uint64_t* bar, int page0, int page1, uint32_t ok,
-                                           int g, int p0) {
+// Copies of a chunk's 16 or 32 positions from in_page on into a stage from position `at`
+// on, by one lane: K codes, V codes, K scales, V scales (what lies behind the sequence's
+// end is in the block too).
+template <int HD, int N>
+__device__ __forceinline__ void load_piece(const Pages& P, uint32_t dst, uint32_t bar, int page, int g, int in_page, int at) {
   constexpr int CB = code_bytes(HD), SB = scale_bytes(HD);
-  const uint32_t b = ptx::smem_u32(bar);
-  auto copies = [&](int page, int in_page, int at, int n) {
-    // (the blocks' count fits in 32 bits: one has 576 bytes at least)
-    const uint32_t block = (uint32_t)page * (uint32_t)P.nkv + (uint32_t)g;
-    const uint8_t* const k = P.k + (uint64_t)block * (uint32_t)(entry_bytes(HD) << P.shift) + (uint32_t)(in_page * CB);
-    const uint32_t to_scales = (uint32_t)((CB << P.shift) - in_page * (CB - SB));
-    const uint8_t* const v = k + (P.v - P.k);
-    bulk_load(dst + at * CB, k, n * CB, b);
-    bulk_load(dst + (kChunk + at) * CB, v, n * CB, b);
-    bulk_load(dst + 2 * kChunk * CB + at * SB, k + to_scales, n * SB, b);
-    bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, v + to_scales, n * SB, b);
-  };
-  if (P.shift > 4) {
-    ptx::mbar_arrive_expect_tx(bar, ok ? 2 * kChunk * entry_bytes(HD) : 0);
-    if (ok) copies(page0, p0 & ((1 << P.shift) - 1), 0, kChunk);
-  } else {
-    ptx::mbar_arrive_expect_tx(bar, (uint32_t)__popc(ok) * 16 * 2 * entry_bytes(HD));
-    if (ok & 1) copies(page0, 0, 0, 16);
-    if (ok & 2) copies(page1, 0, 16, 16);
-  }
+  // (the blocks' count fits in 32 bits: one has 576 bytes at least)
+  const uint32_t block = (uint32_t)page * (uint32_t)P.nkv + (uint32_t)g;
+  const uint8_t* const k = P.k + (uint64_t)block * (uint32_t)(entry_bytes(HD) << P.shift) + (uint32_t)(in_page * CB);
+  const uint8_t* const v = k + (P.v - P.k);
+  const uint32_t to_scales = (uint32_t)((CB << P.shift) - in_page * (CB - SB));
+  bulk_load(dst + at * CB, k, N * CB, bar);
+  bulk_load(dst + (kChunk + at) * CB, v, N * CB, bar);
+  bulk_load(dst + 2 * kChunk * CB + at * SB, k + to_scales, N * SB, bar);
+  bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, v + to_scales, N * SB, bar);
 }
 
 template <int HD, int NB>
@@ -254,45 +250,53 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     }
   }
   Walk ld = use;
-  bool more = true;
+  bool more = true;                 // (the walk's, until a copy does not come)
   ld.c += warp;
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * stage_bytes<HD>();
 
-  // The load walk stands on the chunk to copy next; its page ids are read a chunk early.
+  // The load walk stands on the chunk to copy next; its page ids, of the lower and the upper
+  // 16 positions, are read a chunk early.  (A chunk of nothing reads the row's first.)
   int id0 = -1, id1 = -1;
   auto fetch_ids = [&]() {
-    while (more && ld.c >= ld.c1) {
-      more = ld.next(A);
-      ld.c += warp;
+    if (ld.c >= ld.c1) {
+      do {
+        more = ld.next(A);
+        ld.c += warp;
+      } while (more && ld.c >= ld.c1);
+      if (!more) return;
     }
-    if (!more) return;
     const int p0 = ld.c * kChunk;
-    id0 = id1 = -1;
-    if (p0 < ld.q.n) {              // (a chunk of nothing has no page)
-      const int32_t* row = A.a.table + (int64_t)ld.i * A.a.max_pages;
-      id0 = id1 = row[p0 >> A.p.shift];
-      if (A.p.shift == 4 && p0 + 16 < ld.q.n) id1 = row[(p0 >> 4) + 1];
-    }
+    const int32_t* row = A.a.table + (int64_t)ld.i * A.a.max_pages;
+    id0 = id1 = row[p0 >> A.p.shift];
+    if (A.p.shift == 4 && p0 + 16 < ld.q.n) id1 = row[(p0 >> 4) + 1];
   };
-  uint32_t there = 0;               // two bits per chunk in flight, the oldest lowest: 16 positions whose page is there
+  uint32_t gone = 0;                // two bits per chunk in flight, the oldest lowest: 16 positions without a page
   int take = 0, issued = 0;         // the stage to take, and its phase
   uint32_t phase = 0;
   auto issue = [&](int stage, int ahead) {
-    if (more) {
-      const int p0 = ld.c * kChunk;
-      uint32_t ok = 3;
-      if (max((uint32_t)id0, (uint32_t)id1) >= (uint32_t)A.p.n_pages) {
-        ok = ((uint32_t)id0 < (uint32_t)A.p.n_pages ? 1 : 0) + ((uint32_t)id1 < (uint32_t)A.p.n_pages ? 2 : 0);
-        if (lane == 0 && A.flags && p0 < ld.q.n) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
-      }
-      __syncwarp();
-      if (ptx::elect_one())
-        load_chunk<HD>(A.p, ring + stage * stage_bytes<HD>(), &full[warp * kStages + stage], id0, id1, ok, ld.g, p0);
-      there |= ok << (2 * ahead);
-      ld.c += kWarps;
-      ++issued;
-      fetch_ids();
+    if (!more) return;
+    const int p0 = ld.c * kChunk;
+    uint32_t lost = 0;
+    if (max((uint32_t)id0, (uint32_t)id1) >= (uint32_t)A.p.n_pages) {
+      lost = ((uint32_t)id0 < (uint32_t)A.p.n_pages ? 0 : 1) + ((uint32_t)id1 < (uint32_t)A.p.n_pages ? 0 : 2);
+      if (lane == 0 && A.flags && p0 < ld.q.n) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+      gone |= lost << (2 * ahead);
     }
+    __syncwarp();
+    if (ptx::elect_one()) {
+      uint64_t* const bar = &full[warp * kStages + stage];
+      const uint32_t dst = ring + stage * stage_bytes<HD>(), b = ptx::smem_u32(bar);
+      ptx::mbar_arrive_expect_tx(bar, (2 - __popc(lost)) * 16 * 2 * entry_bytes(HD));
+      if (A.p.shift > 4) {
+        if (lost == 0) load_piece<HD, kChunk>(A.p, dst, b, id0, ld.g, p0 & ((1 << A.p.shift) - 1), 0);
+      } else {
+        if (!(lost & 1)) load_piece<HD, 16>(A.p, dst, b, id0, ld.g, 0, 0);
+        if (!(lost & 2)) load_piece<HD, 16>(A.p, dst, b, id1, ld.g, 0, 16);
+      }
+    }
+    ld.c += kWarps;
+    ++issued;
+    fetch_ids();
   };
   fetch_ids();
 #pragma unroll 1
@@ -359,8 +363,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp * kStages + take], phase, kWaitLimitNs, &abort_flag)))
         more = false;
       const uint8_t* st = smem + (warp * kStages + take) * stage_bytes<HD>();
-      const uint32_t ok = there & 3u;
-      there >>= 2;
+      const uint32_t lost = gone & 3u;
+      gone >>= 2;
       issue(take == 0 ? kStages - 1 : take - 1, kStages - 2);   // to the stage that the chunk before this one has left
       const int p0 = c * kChunk;
 
@@ -404,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       }
       // ---- mask and softmax
       uint32_t pt[NB][2][2];
-      const bool cut = p0 + kChunk > all_seen || ok != 3u;
+      const bool cut = p0 + kChunk > all_seen || lost != 0;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         if (cut) {
@@ -413,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int p = p0 + 16 * t + place(lg) + 8 * (e >> 1);
-              if (p >= seen[b][e & 1] || !((ok >> t) & 1)) s[b][t][e] = -INFINITY;
+              if (p >= seen[b][e & 1] || ((lost >> t) & 1)) s[b][t][e] = -INFINITY;
             }
         }
         float mx[2];
@@ -472,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const int pos = p0 + 16 * t + place(2 * lc + e) + 8 * u;
-              const bool real = pos < n && ((ok >> t) & 1), nan = __hisnan(x[e]);
+              const bool real = pos < n && !((lost >> t) & 1), nan = __hisnan(x[e]);
               if (real && nan) nan_at = min(nan_at, pos);
               if (!real || nan) x[e] = __float2half_rn(0.f);
             }
@@ -771,7 +775,7 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
     return BUDDY_ERR_ARG;
   AttnArgs4 A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, kFewRows, flags, (int32_t*)a->workspace,
               (float*)((uint8_t*)a->workspace + kWsCounters)};
-  // one CTA for every four chunks there can be, three on each SM at most
+  // one CTA for every four chunks there can be, as many as run at once at most
   const int64_t most_rows = (int64_t)a->max_new * A.G;
   const bool two = most_rows > 8;
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;

@@ -34,9 +34,9 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs4& A, int i, bool* bad) {
   return s;
 }
 
-// Query rows enter the products as halves of 1 .. 2 times a power of two per row: the
-// exponent (of the row's largest magnitude), its inverse, and the factor that takes a
-// score of the halves to base 2 (base: log2(e) times the scores' scale).  (Above zero, so that it takes -inf to -inf.)
+// For query rows that enter the products as halves of 1 .. 2: the power of two that takes
+// the row's largest magnitude there, and the factor that takes a score of the halves to
+// base 2 (base: log2(e) times the scores' scale; above zero, so that it takes -inf to -inf).
 __device__ __forceinline__ void row_scale(float top, float base, float* down, float* fac) {
   const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
   *down = __uint_as_float((uint32_t)(127 - ex) << 23);

