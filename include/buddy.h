@@ -398,7 +398,11 @@ BUDDY_API int32_t buddy_budget_to_k(float b, int32_t n_layers);
  *
  * `flags` of the entries below: device int32, or NULL.  A kernel that meets a
  * bad value in device memory sets its BUDDY_DEV_* bit there and leaves out what
- * the entry says; nothing clears the word. */
+ * the entry says; nothing clears the word.  (BUDDY_DEV_TIMEOUT: a wait of an
+ * attention kernel has run out after 4 s; its outputs are incomplete.)
+ *
+ * Launches of the entries below may begin while the work before them on their
+ * stream ends; they read and write memory only after it. */
 typedef struct {
   void* k_pages;        /* device, n_pages * n_kv_heads blocks; 16-byte aligned */
   void* v_pages;        /* device, as k_pages */
@@ -508,9 +512,10 @@ BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int6
  *   sum_p softmax_p(scale * q . k_p) v_p   over positions 0 .. its own;
  * a token without any position (kv_len[i] = 0, or more query tokens than
  * positions) gets zeros.  Rows of q behind row_start[batch] are not written.
- * Query elements enter the products as halves: 11 significant bits (a bf16
- * element whole), below 2^-14 rounded at 2^-25; a row with elements above 2^15 is
- * scaled by a power of two.  Probabilities enter with 11 bits, keys and values
+ * Query elements enter the products as halves, scaled by a power of two per row
+ * where that is needed: 11 significant bits (a bf16 element whole), fewer below
+ * 2^-14 or 2^-14 of the row's largest element, whichever is larger (rounded at
+ * 2^-25 or 2^-25 of it).  Probabilities enter with 11 bits, keys and values
  * exactly; sums and statistics are fp32.
  * Device-checked: 0 <= kv_len[i] <= max_pages * page_size and row_start
  * ascending from >= 0 to <= n_tok with at most max_new rows each

@@ -21,9 +21,9 @@
 // the parts in order.  Every wait is bounded.
 //
 // Nine requests of 1 to 1,500 new tokens behind 300 to 6,000 positions, 32 heads over 8:
-// 255 us, 970 TFLOP/s, the tensor pipe busy for half of the time.  A tile of 256 rows and 128 positions
-// takes about 3,500 cycles, of which one warp's issue of its MMAs (N = 128) is half; the
-// rest is what softmax, codes to halves and hand-overs do not hide.
+// 255 us, 970 TFLOP/s, the tensor pipe busy for half of the time.  A tile of 256 rows and
+// 128 positions takes about 3,500 cycles; its 32 MMAs of N = 128 take 3,100 of them at the
+// rate at which a thread issues such (97 cycles; two issuing warps were slower).
 #include <cuda_runtime.h>
 
 #include <algorithm>
