@@ -39,6 +39,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const buddy_pag
   const int64_t mask = ((int64_t)1 << shift) - 1, room = (int64_t)A.max_pages << shift;
   pdl_wait();
   pdl_trigger();
+  const int64_t head = *A.free_head;
 
   // consecutive sequences per thread: their sums, then a scan over the threads
   const int per = (A.batch + kPlanThreads - 1) / kPlanThreads;
@@ -65,7 +66,6 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const buddy_pag
     all_tok += warp_tok[w];
     all_page += warp_page[w];
   }
-  const int64_t head = *A.free_head;
   int bad = 0;   // (with bad lengths the counts say nothing)
   if (off || all_tok > A.n_tok) bad = BUDDY_DEV_BAD_POSITION;
   else if (head < 0 || head + all_page > A.n_free) bad = BUDDY_DEV_NO_PAGES;
