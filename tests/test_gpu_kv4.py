@@ -570,6 +570,62 @@ def test_attention_shares_a_workspace_between_shapes_and_streams():
         side.synchronize()
 
 
+def test_calls_refuse_wrong_tensors():
+    """A wrong type, device, shape, stride or size of any tensor: an error that names it, and
+    nothing written."""
+    P, T, nq, nkv, hd, page = pkg(), 6, 4, 2, 64, 16
+    cache = P.KV4Cache.empty(4, page, nkv, hd)
+    co, si = P.buddy_rope_table(8, hd, THETA)
+    x = torch.randn(T, nq + nkv, hd, device="cuda").bfloat16()
+    q, k, v, q_out = x[:, :nq], x[:, nq:], x[:, nq:], torch.full((T, nq, hd), 7.0, device="cuda").bfloat16()
+    pos, slot = i32([0] * T), torch.arange(T, device="cuda")
+    gain = torch.ones(hd, device="cuda")
+    good = dict(q=q, k=k, v=v, pos=pos, slot=slot, rope=(co, si), q_out=q_out, q_gain=gain, k_gain=gain, flags=flags())
+
+    def check(call, good, bad, untouched):
+        for name, value in bad:
+            before = [t.clone() for t in untouched]
+            with pytest.raises((ValueError, TypeError)) as e:
+                call(**{**good, name: value})
+            assert any(w in str(e.value) for w in (name, "cos", "sin")), (name, e.value)
+            assert all(torch.equal(a, b) for a, b in zip(before, untouched)), name
+
+    pages = [cache.k_pages, cache.v_pages, q_out]
+    check(cache.buddy_kv4_append, good, [
+        ("q", q.float()), ("q", q.cpu()), ("q", q[:-1]), ("q", q[0]), ("q", q.transpose(1, 2).contiguous().transpose(1, 2)),
+        ("k", k.half()[0]), ("k", x[:, ::3]), ("k", None), ("v", v[:, :1]), ("v", v.float()), ("v", 3), ("pos", pos.long()),
+        ("pos", pos[:-1]), ("pos", torch.zeros(2 * T, device="cuda", dtype=torch.int32)[::2]), ("slot", slot.int()),
+        ("slot", slot[:-1]), ("rope", (co.double(), si)), ("rope", (co, si[:-1])), ("q_out", None), ("q_out", q_out[:, :-1]),
+        ("q_gain", gain[:-1]), ("k_gain", gain.bfloat16()), ("flags", flags().cpu())], pages)
+    out = torch.empty(T, nkv, hd, device="cuda")
+    check(cache.buddy_kv4_read, dict(slot=slot, k_out=out, v_out=out, flags=None), [
+        ("slot", slot.int()), ("k_out", out.double()), ("k_out", out[:-1]), ("v_out", out.half()), ("flags", 1)], [out])
+    att = dict(q=q, kv_len=i32([3] * T), table=i32([[0]] * T), out=q_out, row_start=i32(range(T + 1)), flags=None)
+    check(cache.buddy_kv4_attention, att, [
+        ("q", q[:, :, :32]), ("q", q[0]), ("kv_len", i32([3] * T).long()), ("table", i32([0] * T)), ("table", i32([[0]] * 2)),
+        ("out", q_out[:-1]), ("out", q_out.cpu()), ("row_start", i32(range(T))), ("workspace", flags())], [q_out])
+    t, _ = make_plan([15, 3], [2, 30], page)
+    plan = dict(length=t["length"], n_new=t["n_new"], page_size=page, table=t["table"], free_pages=t["free"],
+                free_head=t["head"], kv_len=t["kv_len"], row_start=t["row_start"], slot=t["slot"], pos=t["pos"],
+                free_head_out=t["head_out"], flags=t["flags"])
+    check(P.buddy_page_plan, plan, [
+        ("length", t["length"].long()), ("length", [1, 2]), ("n_new", t["n_new"][:1]), ("table", t["table"][0]),
+        ("table", t["table"][:, ::2]), ("free_pages", t["free"].long()), ("free_head", t["head"].cpu()),
+        ("kv_len", t["kv_len"][:1]), ("row_start", t["kv_len"]), ("slot", t["pos"]), ("pos", t["pos"][:-1]),
+        ("free_head_out", t["head_out"].float())], [t["table"], t["slot"], t["pos"], t["kv_len"]])
+    with pytest.raises(OverflowError):
+        P.buddy_page_plan(**{**plan, "page_size": 2 ** 40})
+    with pytest.raises(P.BuddyError):
+        P.buddy_page_plan(**{**plan, "page_size": 48})
+    with pytest.raises(P.BuddyError):          # a workspace that is too small
+        cache.buddy_kv4_attention(**{**att, "workspace": torch.zeros(4096, dtype=torch.uint8, device="cuda")})
+    side = torch.cuda.Stream()
+    cache.buddy_kv4_append(**good, stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert good["flags"].item() == 0 and torch.isfinite(q_out).all()
+
+
 @pytest.mark.parametrize("m", [1, 3, 40])
 def test_calls_in_a_row_wait_for_each_other(m):
     """Launches may overlap their predecessors' ends: a chain of calls with ordinary kernels
