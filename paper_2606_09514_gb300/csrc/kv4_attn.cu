@@ -38,7 +38,7 @@
 // Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 119 us,
 // their copies alone 91 us (94% of HBM's rate), the arithmetic alone 100; a chunk is about
 // 700 instructions of a warp, 350 of them codes to halves.  One token over 2,048 positions
-// takes 8.5 us: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
+// takes 8.2 us: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
 // for two chunks, 4 for partials, arrival and join.
 #include <cuda_runtime.h>
 
@@ -177,65 +177,91 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   if (tid < kWarps * kStages) ptx::mbar_init(&full[tid], 1);
   if (tid == 0) abort_flag = 0;
   ptx::fence_mbar_init();
+  __syncthreads();
   pdl_wait();
   pdl_trigger();   // (the prompts of the same call may start where there is room)
 
-  // ---- this CTA's share: [lo, lo + share) of all streams' openings and chunks
-  const int per = (B + kThreads - 1) / kThreads;
-  const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
-  int64_t mine = 0;
-  bool any_bad = false;
-#pragma unroll 1
-  for (int i = b0; i < b1; ++i) {
-    bool bad;
-    const Rows q = few_rows(A, i, &bad);
-    any_bad |= bad;
-    if (q.m > 0) mine += chunks_of(q.n) + kOpen;
-  }
-  if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
-  mine *= A.p.nkv;
-  int64_t upto = mine;
+  // ---- this CTA's share: [lo, lo + share) of all streams' openings and chunks.  Where it
+  // begins: sequence use.i and how far into that one's streams
+  auto cost = [&](const Rows& q) { return q.m > 0 ? (int64_t)(chunks_of(q.n) + kOpen) * A.p.nkv : 0; };
+  auto scan = [&](int64_t x) {      // over the warp
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += v;
-  }
-  if (lane == 31) s_sum[warp] = upto;
-  __syncthreads();
-  int64_t total = 0;
-  for (int w = 0; w < kWarps; ++w) {
-    if (w == warp) upto += total;
-    total += s_sum[w];
-  }
-  if (total == 0) return;
-  const int share = (int)min((int64_t)INT32_MAX / 2, ((total + gridDim.x - 1) / gridDim.x + kWarps - 1) / kWarps * kWarps);
-  const int64_t lo = (int64_t)blockIdx.x * share;
-  if (lo >= total) return;
-  if (upto - mine <= lo && lo < upto) {
-    int64_t at = upto - mine;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += v;
+    }
+    return x;
+  };
+  auto share_of = [&](int64_t total) {
+    return (int)min((int64_t)INT32_MAX / 2, ((total + gridDim.x - 1) / gridDim.x + kWarps - 1) / kWarps * kWarps);
+  };
+  Walk use;
+  int64_t total = 0, lo, at;
+  int share;
+  if (B <= 32) {                    // every warp by itself
+    Rows q{0, 0, 0};
+    bool bad = false;
+    if (lane < B) q = few_rows(A, lane, &bad);
+    if (__any_sync(0xffffffffu, bad) && blockIdx.x == 0 && tid == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+    const int64_t mine = cost(q), upto = scan(mine);
+    total = __shfl_sync(0xffffffffu, upto, 31);
+    if (total == 0) return;
+    share = share_of(total);
+    lo = (int64_t)blockIdx.x * share;
+    if (lo >= total) return;
+    use.i = __ffs(__ballot_sync(0xffffffffu, lo < upto)) - 1;
+    at = lo - __shfl_sync(0xffffffffu, upto - mine, use.i);
+    use.q.t0 = __shfl_sync(0xffffffffu, q.t0, use.i);
+    use.q.m = __shfl_sync(0xffffffffu, q.m, use.i);
+    use.q.n = __shfl_sync(0xffffffffu, q.n, use.i);
+  } else {
+    const int per = (B + kThreads - 1) / kThreads;
+    const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    int64_t mine = 0;
+    bool any_bad = false;
 #pragma unroll 1
     for (int i = b0; i < b1; ++i) {
       bool bad;
-      const Rows q = few_rows(A, i, &bad);
-      const int64_t n = q.m > 0 ? (int64_t)(chunks_of(q.n) + kOpen) * A.p.nkv : 0;
-      if (lo < at + n) {
-        s_first = i;
-        s_at = lo - at;
-        break;
-      }
-      at += n;
+      mine += cost(few_rows(A, i, &bad));
+      any_bad |= bad;
     }
-  }
-  __syncthreads();
-  Walk use;
-  int start;                        // where the stream's first chunk is, from the share's beginning on
-  {
+    if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+    int64_t upto = scan(mine);
+    if (lane == 31) s_sum[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) {
+      if (w == warp) upto += total;
+      total += s_sum[w];
+    }
+    if (total == 0) return;
+    share = share_of(total);
+    lo = (int64_t)blockIdx.x * share;
+    if (lo >= total) return;
+    if (upto - mine <= lo && lo < upto) {
+      int64_t x = upto - mine;
+#pragma unroll 1
+      for (int i = b0; i < b1; ++i) {
+        bool bad;
+        const int64_t n = cost(few_rows(A, i, &bad));
+        if (lo < x + n) {
+          s_first = i;
+          s_at = lo - x;
+          break;
+        }
+        x += n;
+      }
+    }
+    __syncthreads();
     bool bad;
     use.i = s_first;
+    at = s_at;
     use.q = few_rows(A, use.i, &bad);
+  }
+  int start;                        // where the stream's first chunk is, from the share's beginning on
+  {
     const int nc = chunks_of(use.q.n);
-    use.g = (int)(s_at / (nc + kOpen));
-    const int x = (int)(s_at - (int64_t)use.g * (nc + kOpen)) - kOpen;   // chunk of the stream; below 0: its opening
+    use.g = (int)(at / (nc + kOpen));
+    const int x = (int)(at - (int64_t)use.g * (nc + kOpen)) - kOpen;   // chunk of the stream; below 0: its opening
     start = -x;
     use.rem = (int)min((int64_t)share, total - lo) + min(x, 0);
     use.c = max(x, 0);
