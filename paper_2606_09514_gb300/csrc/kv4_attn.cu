@@ -27,15 +27,18 @@
 // 250 sequences of 512 to 8,192 positions and 4 KV heads 98.9, 93.0, 89.5 and 90.5 us; 31
 // of 100 to 4,096 with up to five new tokens and 40 KV heads 76, 60, 60 and 61.)  A short
 // stream belongs to the share where it begins: what a CTA saves by passing on a part of it,
-// the partials cost again.  In a share, four warps take the chunks of a stream in turn,
-// each with its own ring of stages, which runs on across streams: one lane copies a chunk
-// in four bulk copies, in whole halves of 16 positions, and what lies behind the sequence's
+// the partials cost again.  In a share, four warps take the chunks of a stream in turn or,
+// where there are several short streams, a warp the whole of every fourth, without barriers
+// and joins (250 sequences of 50 to 200 positions, 8 KV heads: 19.0 us, 25.5 with their
+// chunks in turn; 1,000 of 20 to 250: 54 and 76; up to 16 chunks instead of 12 costs 250 of
+// 30 to 1,000 a sixth).  Each warp has its own ring of stages, which runs on across streams:
+// one lane copies a chunk in four bulk copies, in whole halves of 16 positions, and what lies behind the sequence's
 // end, or has no page, is masked.  A stream within a share is written out; the CTAs of one
 // that is cut write partials, which are joined in order by the last of them to arrive or,
 // where they are many, by teams first (one sequence of 120,001 positions, 4 KV heads, 152
 // CTAs each: 49 us with one join, 32 with teams).
 //
-// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 119 us,
+// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 120 us,
 // their copies alone 91 us (94% of HBM's rate), the arithmetic alone 100; a chunk is about
 // 700 instructions of a warp, 350 of them codes to halves.  One token over 2,048 positions
 // takes 8.2 us: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
@@ -62,8 +65,9 @@ constexpr int kStages = 3;
 // CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two).
 template <int NB>
 __host__ __device__ constexpr int ctas_per_sm() { return NB == 1 ? 4 : 3; }
-constexpr int kWhole = 8;        // streams of at most this many chunks are not cut
+constexpr int kWhole = 12;       // streams of at most this many chunks are not cut
 constexpr int kOpen = 10;        // what beginning and ending a stream costs, in chunks
+constexpr int kMany = 2 * kOpen; // shares from this on hold several short streams
 constexpr int kMaxGrid = 1024;   // CTAs: four on each of at most 256 SMs
 constexpr int kJoin = 8;         // partials in flight when a cut stream is joined
 constexpr int kOneTeam = 24;     // spans up to which one CTA joins them all
@@ -102,11 +106,13 @@ __device__ __forceinline__ Rows few_rows(const AttnArgs4& A, int i, bool* bad) {
 struct Walk {
   Rows q;
   int i, g, c, c1;            // sequence, KV head, chunks [c, c1) of the stream in this share
+  int k;                      // streams of the share before this one
   int rem;                    // what is left of the share behind this stream
   // to the next stream; false at the share's end
   __device__ __forceinline__ bool next(const AttnArgs4& A) {
     rem -= kOpen;
     if (rem <= 0) return false;
+    ++k;
     if (++g >= A.p.nkv) {
       g = 0;
       bool bad;
@@ -257,6 +263,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     at = s_at;
     use.q = few_rows(A, use.i, &bad);
   }
+  use.k = 0;
   int start;                        // where the stream's first chunk is, from the share's beginning on
   {
     const int nc = chunks_of(use.q.n);
@@ -277,7 +284,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   }
   Walk ld = use;
   bool more = true;                 // (the walk's, until a copy does not come)
-  ld.c += warp;
+  // Where a share holds several short streams, a warp takes the whole of every fourth.
+  const bool many = share >= kMany;
+  auto owned = [&](const Walk& w) { return NB == 1 && many && w.q.n <= kWhole * kChunk; };
+  auto enter = [&](const Walk& w) { return owned(w) ? (w.k % kWarps == warp ? 0 : w.c1) : w.c + warp; };
+  ld.c = enter(ld);
+  int ld_step = owned(ld) ? 1 : kWarps;
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * stage_bytes<HD>();
 
   // The load walk stands on the chunk to copy next; its page ids, of the lower and the upper
@@ -287,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     if (ld.c >= ld.c1) {
       do {
         more = ld.next(A);
-        ld.c += warp;
+        ld.c = enter(ld);
+        ld_step = owned(ld) ? 1 : kWarps;
       } while (more && ld.c >= ld.c1);
       if (!more) return;
     }
@@ -320,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         if (!(lost & 2)) load_piece<HD, 16>(A.p, dst, b, id1, ld.g, 0, 16);
       }
     }
-    ld.c += kWarps;
+    ld.c += ld_step;
     ++issued;
     fetch_ids();
   };
@@ -342,7 +355,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
   for (bool go = true; go;) {
     // ---- one stream (or the part of it in this share)
     const int g = use.g, rows = use.q.m * G, n = use.q.n, nc = chunks_of(n);
-    const bool whole = use.c == 0 && use.c1 == nc;
+    const bool whole = use.c == 0 && use.c1 == nc, own = owned(use);
+    const int c0 = enter(use), step = own ? 1 : kWarps;
+    if (own && c0 == use.c1) {      // another warp's
+      start += nc + kOpen;
+      go = use.next(A);
+      continue;
+    }
     // queries: rows lg of each block of eight, this lane's HD / 4 channels
     uint32_t qf[NB][KS][2];
     float fac[NB][2];               // of the scores of rows 2 lc and 2 lc + 1
@@ -385,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
         for (int e = 0; e < 4; ++e) o[b][t][e] = 0.f;
     }
 
-    for (int c = use.c + warp; c < use.c1; c += kWarps) {
+    for (int c = c0; c < use.c1; c += step) {
       if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp * kStages + take], phase, kWaitLimitNs, &abort_flag)))
         more = false;
       const uint8_t* st = smem + (warp * kStages + take) * stage_bytes<HD>();
@@ -557,6 +576,34 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       phase ^= take == 0;
     }
 
+    auto out4 = [&](int r, int ch, float4 v) {
+      const int64_t at = (use.q.t0 + r / G) * A.a.out_stride + (int64_t)(g * G + r % G) * HD + ch;
+      if (A.a.out_dtype == BUDDY_DTYPE_F32) {
+        *reinterpret_cast<float4*>((float*)A.a.out + at) = v;
+      } else {
+        *reinterpret_cast<uint2*>((bf16*)A.a.out + at) = make_uint2(tca::pack_bf16(v.x, v.y), tca::pack_bf16(v.z, v.w));
+      }
+    };
+    if (own) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], x);
+          const int r = 8 * b + 2 * lc + e;
+          if (r < rows) {
+            const float inv = m[b][e] == -INFINITY ? 0.f : 1.f / l[b][e];
+#pragma unroll
+            for (int t = 0; t < HD / 16; t += 2)
+              out4(r, lg * (HD / 8) + 2 * t, make_float4(o[b][t][e] * inv, o[b][t][e + 2] * inv, o[b][t + 1][e] * inv,
+                                                         o[b][t + 1][e + 2] * inv));
+          }
+        }
+      start += nc + kOpen;
+      go = use.next(A);
+      continue;
+    }
     // ---- join the warps, in the stages taken last: a lane has rows 2 lc, 2 lc + 1 of each block,
     // HD / 8 channels from lg * HD / 8 on
     if (lane == 0) s_stage[warp] = take == 0 ? kStages - 1 : take - 1;
@@ -583,14 +630,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
     const int first_cta = (int)blockIdx.x - (start < 0 ? (share - 1 - start) / share : 0);
     const int last_cta = (int)blockIdx.x + (start + nc - 1) / share;
     float* part = A.part + (2 * (int64_t)blockIdx.x + ((int)blockIdx.x == first_cta ? 1 : 0)) * partial_floats<HD, NB>();
-    auto out4 = [&](int r, int ch, float4 v) {
-      const int64_t at = (use.q.t0 + r / G) * A.a.out_stride + (int64_t)(g * G + r % G) * HD + ch;
-      if (A.a.out_dtype == BUDDY_DTYPE_F32) {
-        *reinterpret_cast<float4*>((float*)A.a.out + at) = v;
-      } else {
-        *reinterpret_cast<uint2*>((bf16*)A.a.out + at) = make_uint2(tca::pack_bf16(v.x, v.y), tca::pack_bf16(v.z, v.w));
-      }
-    };
     for (int x = tid; x < rows * (HD / 4); x += kThreads) {
       const int r = x / (HD / 4), ch = x % (HD / 4) * 4;
       float M = -INFINITY, L = 0.f;
