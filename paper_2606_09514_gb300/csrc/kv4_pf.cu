@@ -763,53 +763,58 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
 }
 
 // The parts of the items that were cut, in order: a thread per row, four channels, eight
-// parts' loads at a time.
+// parts' loads at a time.  A CTA's threads take 8 channels (nine requests as above 254 us,
+// with 4 channels, and so twice the CTAs, most of them without work, 257, with 16 256).
+constexpr int kJoinChannels = 8;
 template <int HD>
 __global__ void __launch_bounds__(2 * kPfRows) kv4_join_kernel(const AttnArgs4 A, const CutItem* cuts) {
   pdl_wait();
   const CutItem c = cuts[blockIdx.x];
-  const int x = threadIdx.x, ch = blockIdx.y * 4;
+  const int x = threadIdx.x;
   if (x >= c.rows || c.spans == 0) return;
-  auto part = [&](int k) {
-    return A.part + (2 * (int64_t)(blockIdx.x + k) + (k == 0 ? 1 : 0)) * pf_part_floats<HD>() + x;
-  };
-  float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  constexpr int N = 8;
-  for (int k0 = 0; k0 < c.spans; k0 += N) {
-    float m[N], l[N], v[N][4], to = M;
+#pragma unroll 1
+  for (int ch = blockIdx.y * 4; ch < HD; ch += gridDim.y * 4) {
+    auto part = [&](int k) {
+      return A.part + (2 * (int64_t)(blockIdx.x + k) + (k == 0 ? 1 : 0)) * pf_part_floats<HD>() + x;
+    };
+    float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int N = 8;
+    for (int k0 = 0; k0 < c.spans; k0 += N) {
+      float m[N], l[N], v[N][4], to = M;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const bool in = k0 + k < c.spans;
-      const float* p = part(k0 + k);
-      m[k] = in ? p[0] : -INFINITY;
-      l[k] = in ? p[2 * kPfRows] : 0.f;
+      for (int k = 0; k < N; ++k) {
+        const bool in = k0 + k < c.spans;
+        const float* p = part(k0 + k);
+        m[k] = in ? p[0] : -INFINITY;
+        l[k] = in ? p[2 * kPfRows] : 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[k][i] = in ? p[(2 + ch + i) * 2 * kPfRows] : 0.f;
+        for (int i = 0; i < 4; ++i) v[k][i] = in ? p[(2 + ch + i) * 2 * kPfRows] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) to = fmaxf(to, m[k]);
+      const float at = to == -INFINITY ? 0.f : to, a = tca::exp2a(M - at);
+      L *= a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= a;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (k0 + k >= c.spans) break;
+        const float b = tca::exp2a(m[k] - at);
+        L += b * l[k];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += b * v[k][i];
+      }
+      M = to;
     }
-#pragma unroll
-    for (int k = 0; k < N; ++k) to = fmaxf(to, m[k]);
-    const float at = to == -INFINITY ? 0.f : to, a = tca::exp2a(M - at);
-    L *= a;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] *= a;
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (k0 + k >= c.spans) break;
-      const float b = tca::exp2a(m[k] - at);
-      L += b * l[k];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] += b * v[k][i];
-    }
-    M = to;
+    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+    const int row = c.row0 + x, G = A.G;
+    const int64_t to = (c.t0 + row / G) * A.a.out_stride + (int64_t)(c.g * G + row % G) * HD + ch;
+    if (A.a.out_dtype == BUDDY_DTYPE_F32)
+      *reinterpret_cast<float4*>((float*)A.a.out + to) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    else
+      *reinterpret_cast<uint2*>((bf16*)A.a.out + to) =
+          make_uint2(tca::pack_bf16(o[0] * inv, o[1] * inv), tca::pack_bf16(o[2] * inv, o[3] * inv));
   }
-  const float inv = M == -INFINITY ? 0.f : 1.f / L;
-  const int row = c.row0 + x, G = A.G;
-  const int64_t to = (c.t0 + row / G) * A.a.out_stride + (int64_t)(c.g * G + row % G) * HD + ch;
-  if (A.a.out_dtype == BUDDY_DTYPE_F32)
-    *reinterpret_cast<float4*>((float*)A.a.out + to) = make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  else
-    *reinterpret_cast<uint2*>((bf16*)A.a.out + to) =
-        make_uint2(tca::pack_bf16(o[0] * inv, o[1] * inv), tca::pack_bf16(o[2] * inv, o[3] * inv));
 }
 
 int64_t prompt_workspace(int head_dim, int sms) {
@@ -824,7 +829,7 @@ static int launch_prompt_hd(const AttnArgs4& A, CutItem* cuts, int sms, cudaStre
   // the prompts start on the SMs that the few-row kernel leaves free, the join is launched
   // as the prompts end
   if (launch_k(kv4_prompt_kernel<HD>, sms, kPfThreads, pf_smem<HD>(), s, true, A, cuts) != cudaSuccess ||
-      launch_k(kv4_join_kernel<HD>, dim3(sms, HD / 4), 2 * kPfRows, 0, s, true, A, (const CutItem*)cuts) != cudaSuccess)
+      launch_k(kv4_join_kernel<HD>, dim3(sms, HD / kJoinChannels), 2 * kPfRows, 0, s, true, A, (const CutItem*)cuts) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   return BUDDY_OK;
 }
