@@ -425,6 +425,17 @@ def test_attention_one_long_sequence():
     check_attention(cache, table, vals, [n], [50], 8)
 
 
+@pytest.mark.parametrize("heads", [(2, 2, 128), (3, 1, 64), (8, 1, 128), (7, 7, 64)])
+@pytest.mark.parametrize("lens", [[40001], [9000, 13000], [3000, 20, 6000, 17, 5000]])
+def test_attention_streams_of_many_shares(heads, lens):
+    """Streams that tens of CTAs share, next to streams that begin and end in the same CTAs:
+    few and many rows per join."""
+    nq, nkv, hd = heads
+    cache, table, vals = make_cache(lens, 64, nkv, hd, seed=len(lens))
+    check_attention(cache, table, vals, lens, [1] * len(lens), nq, ragged=False)
+    check_attention(cache, table, vals, lens, [2] * len(lens), nq, out_dtype=torch.float32)
+
+
 def test_attention_many_sequences():
     rng = np.random.default_rng(5)
     lens = [int(x) for x in rng.integers(0, 90, 700)]
@@ -540,6 +551,35 @@ def test_attention_reports_bad_lengths_and_pages(n_new):
             want = O.attention(f64(q[2:3]), k, v, 1, 0.125)
             assert np.abs(f64(out[2:3]) - want).max() <= np.abs(v).max() * 2.0 ** -10 + np.abs(want).max() * 2.0 ** -8
         assert torch.equal(out[:2 * n_new], ok[:2 * n_new]) and torch.equal(out[3 * n_new:], ok[3 * n_new:])
+
+
+@pytest.mark.parametrize("page", [16, 32, 128])
+@pytest.mark.parametrize("copies", [1, 40, 700])
+def test_attention_without_some_pages(page, copies):
+    """Pages that are not there, in every place of a chunk and of a sequence: their positions
+    do not count, whoever walks the sequence (one warp, a CTA, many CTAs).  What was in the
+    buffers before is NaN in the pages that are there behind the sequences' ends."""
+    lens = [5, 33, 250, 300, 47, 1200] * copies if copies < 700 else [5, 33, 250, 40] * copies
+    cache, table, vals = make_cache(lens, page, 1, 64, seed=11)
+    rng = np.random.default_rng(page)
+    lost = []
+    t2 = table.clone()
+    for i, n in enumerate(lens):
+        held = -(-n // page)
+        which = {0: [0], 1: [held - 1], 2: range(held)}.get(i % 5, rng.permutation(held)[:rng.integers(0, held + 1)])
+        for w in which:
+            t2[i, int(w)] = -1 if w % 2 else cache.k_pages.shape[0] + 5
+        lost.append(np.isin(np.arange(n) // page, np.asarray(list(which), int)))
+    q = torch.randn(len(lens), 3, 64, device="cuda").bfloat16()
+    out, fl = torch.full((len(lens), 3, 64), 77.0, device="cuda"), flags()
+    cache.buddy_kv4_attention(q, i32(lens), t2, out, flags=fl)
+    assert fl.item() == BAD_PAGE
+    got = f64(out)
+    for i, gone in enumerate(lost[:200]):
+        k, v = (x[:, ~gone] for x in vals[i])
+        want = O.attention(f64(q[i:i + 1]), k, v, 1, 0.125) if (~gone).any() else np.zeros((1, 3, 64))
+        tol = np.abs(v).max(initial=0.0) * (2.0 ** -11 + 2.0 ** -12) + 2.0 ** -22 * np.abs(want)
+        assert np.all(np.abs(got[i:i + 1] - want) <= tol), (i, lens[i])
 
 
 @pytest.mark.parametrize("rows", [[0, 1, 3, 2, 4], [-1, 1, 2, 3, 4], [0, 1, 2, 3, 9], [0, 1, 4, 4, 4]])
