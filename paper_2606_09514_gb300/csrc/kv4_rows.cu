@@ -184,15 +184,14 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A) {
   const int kq = R.n_q_heads, kk = kq + R.n_kv_heads, heads = kk + (CACHE ? R.n_kv_heads : 0);
   const int tl = threadIdx.x % LPH;
   const uint32_t team = ((1u << LPH) - 1) << (threadIdx.x % 32 / LPH * LPH);   // this team's lanes
-  const int64_t u = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / LPH;
   pdl_wait();
   pdl_trigger();
   // (the teams of a warp take the same heads of neighbouring tokens: queries, keys and
   // values go different ways)
-  const int64_t grp = u / R.n_tok;
-  if (grp >= A.groups) return;                  // (whole teams)
-  const int64_t t = u - grp * R.n_tok;
-  const int h0 = (int)grp * A.per, h1 = min(h0 + A.per, heads);
+  const int grp = (int)(blockIdx.x % (unsigned)A.groups);
+  const int64_t t = (int64_t)(blockIdx.x / (unsigned)A.groups) * (kRowThreads / LPH) + threadIdx.x / LPH;
+  if (t >= R.n_tok) return;                     // (whole teams)
+  const int h0 = grp * A.per, h1 = min(h0 + A.per, heads);
 
   const int c = tl * 8;                         // this lane's channels: c .. c + 7 of both halves
   auto row = [&](int h) -> const T* {
@@ -353,16 +352,16 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
 }
 
 // Heads of a team: one while there are few rows, for the shortest chain; more as they fill
-// the GPU (kRowTeams), up to four, which share the reads of position and rotation
-// (8,297 tokens of 40 heads 32.8 us, 33.1 with eight; append of 4,999 tokens of 36 heads and
-// their read 25.1 and 25.5).
+// the GPU (kRowTeams), up to eight, which share the reads of position and rotation
+// (8,297 tokens of 40 heads 32.3 us, 32.4 with four, 37.7 with two; append of 4,999 tokens of
+// 36 heads and their read 23.8, 24.6 and 26.0).
 constexpr int64_t kRowTeams = 16384;
 template <typename T, int HD, bool CACHE>
 static int launch_rows(RowArgs A, cudaStream_t s) {
   const int heads = A.r.n_q_heads + A.r.n_kv_heads * (CACHE ? 2 : 1);
-  A.per = (int)std::min<int64_t>(4, std::max<int64_t>(1, (int64_t)A.r.n_tok * heads / kRowTeams));
+  A.per = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)A.r.n_tok * heads / kRowTeams));
   A.groups = (heads + A.per - 1) / A.per;
-  const int64_t ctas = ((int64_t)A.r.n_tok * A.groups * (HD / 16) + kRowThreads - 1) / kRowThreads;
+  const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   return launch_k(qk_rows_kernel<T, HD, CACHE>, (unsigned)ctas, kRowThreads, 0, s, true, A) == cudaSuccess
              ? BUDDY_OK : BUDDY_ERR_CUDA;
