@@ -164,6 +164,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     for name in ("page_plan", "qk_norm_rope", "kv4_append", "kv4_read", "kv4_attention"):
         entry = ctypes.cast(getattr(lib, "buddy_" + name), c_p).value
         setattr(lib, "call_" + name, functools.partial(getattr(_calls, name), entry))
+    lib.call_stream_for_workspace = _calls.stream_for_workspace
     if path is None:
         _lib = lib
     return lib
@@ -427,9 +428,12 @@ def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Te
 
 class KV4Cache:
     """One layer's paged 4-bit KV cache: pages of keys and of values, uint8
-    [n_pages, n_kv, page_size * (hd / 2 + hd / 16)], and the workspace of its
-    attention calls.  Layers whose calls do not overlap on the GPU may share one
-    workspace: pass it, a zeroed uint8 tensor of workspace_bytes()."""
+    [n_pages, n_kv, page_size * (hd / 2 + hd / 16)], and the workspaces of its
+    attention calls.  Without `workspace` it makes one for every stream that they go
+    to, so that calls on different streams may overlap.  One that is passed, a zeroed
+    uint8 tensor of workspace_bytes(), serves every call of the cache, and those of
+    other layers that it is passed to: none of them may overlap on the GPU.  Calls that
+    are captured in a graph want one, which the graph's replays then use."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_size: int,
                  workspace: Optional[torch.Tensor] = None):
@@ -445,7 +449,7 @@ class KV4Cache:
         self.address = ctypes.addressof(self.state)
         self.lib = load_library()
         self.workspace = workspace
-        self._made: List = []           # workspaces made here; calls under way may still use an older one
+        self._made: Dict = {}           # workspaces made here: (device, stream) -> tensor
         self._need: Dict = {}
 
     @classmethod
@@ -462,6 +466,19 @@ class KV4Cache:
                 raise BuddyError(BUDDY_ERR_ARG, "buddy_kv4_attention_workspace")
             self._need[n_q_heads, max_new] = n
         return n
+
+    def _own_workspace(self, q: torch.Tensor, max_new: int, stream) -> torch.Tensor:
+        """The workspace of the calls that go where this one goes, made and zeroed there:
+        in order with them, as is the next use of the memory of one that has become too small."""
+        if q.dim() != 3:
+            raise ValueError("q: [tokens, heads, head_dim of the cache] is wanted")
+        key = q.device, self.lib.call_stream_for_workspace(q, stream)
+        need = self.workspace_bytes(q.shape[1], max_new)
+        ws = self._made.get(key)
+        if ws is None or ws.numel() < need:
+            with torch.cuda.stream(stream):          # (None: the current one)
+                ws = self._made[key] = torch.zeros(need, dtype=torch.uint8, device=q.device)
+        return ws
 
     def buddy_kv4_append(self, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
                          slot: torch.Tensor, rope, q_out: Optional[torch.Tensor],
@@ -485,11 +502,6 @@ class KV4Cache:
         """Causal attention of query tokens over the cache; q, out [tokens, n_q, head_dim]."""
         ws = workspace if workspace is not None else self.workspace
         if ws is None:
-            if q.dim() != 3:
-                raise ValueError("q: [tokens, heads, head_dim of the cache] is wanted")
-            need = self.workspace_bytes(q.shape[1], max_new)
-            if not self._made or self._made[-1].numel() < need:
-                self._made.append(torch.zeros(need, dtype=torch.uint8, device=q.device))
-            ws = self._made[-1]
+            ws = self._own_workspace(q, max_new, stream)
         _check(self.lib.call_kv4_attention(self.address, q, kv_len, table, out, row_start, max_new, scale, flags, ws,
                                            stream), "buddy_kv4_attention")

@@ -7,6 +7,7 @@
 // entry's code.  Faulty tensors raise ValueError, what is not a tensor TypeError.
 #include <Python.h>
 
+#include <c10/cuda/CUDAException.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -120,6 +121,17 @@ void* stream_of(const at::Tensor& t, PyObject* stream) {
   Py_DECREF(s);
   if (!p && PyErr_Occurred()) throw Failed{};
   return p;
+}
+
+// tensor, stream: the handle of the stream that a call with that tensor goes to.  For a cache
+// that keeps a workspace for every stream: under a capture there is none to keep, since a
+// replay may run next to calls that share the stream's.
+PyObject* stream_for_workspace(PyObject* const* a) {
+  const auto s = static_cast<cudaStream_t>(stream_of(tensor(a[0], "q"), a[1]));
+  cudaStreamCaptureStatus status;
+  C10_CUDA_CHECK(cudaStreamIsCapturing(s, &status));
+  if (status != cudaStreamCaptureStatusNone) wrong("workspace", "a call that is captured in a graph wants one given");
+  return PyLong_FromVoidPtr(s);
 }
 
 template <class F>
@@ -306,7 +318,8 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<14, page_plan>("page_plan"),         method<13, qk_norm_rope>("qk_norm_rope"),
                          method<16, kv4_append>("kv4_append"),       method<7, kv4_read>("kv4_read"),
-                         method<12, kv4_attention>("kv4_attention"), {nullptr, nullptr, 0, nullptr}};
+                         method<12, kv4_attention>("kv4_attention"), method<2, stream_for_workspace>("stream_for_workspace"),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
