@@ -515,8 +515,9 @@ BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int6
  * Query elements enter the products as halves, scaled by a power of two per row
  * where that is needed: 11 significant bits (a bf16 element whole), fewer below
  * 2^-14 or 2^-14 of the row's largest element, whichever is larger (rounded at
- * 2^-25 or 2^-25 of it).  Probabilities enter with 11 bits, keys and values
- * exactly; sums and statistics are fp32.
+ * 2^-25 or 2^-25 of it).  Probabilities enter with 11 bits, below 2^-21 of the
+ * row's largest rounded at 2^-32 of that; keys and values exactly; sums and
+ * statistics are fp32.
  * Device-checked: 0 <= kv_len[i] <= max_pages * page_size and row_start
  * ascending from >= 0 to <= n_tok with at most max_new rows each
  * (BUDDY_DEV_BAD_POSITION: the sequence's rows are not written); page ids

@@ -11,7 +11,8 @@
 //                 in the contraction is free, so a lane takes HD / 4 consecutive
 //                 ones: one wide load of codes is its A operand of all K steps.
 //   softmax       base 2, per row (a column here): running reference m, which follows
-//                 the maximum when that rises by more than 8 (p < 2^8 in half).
+//                 the maximum when that rises by more than 8 (p is 2^7 times that of the
+//                 reference, 2^15 at most in half).
 //   O^T += V^T P^T  16 channels x 8 rows; a lane takes HD / 8 consecutive channels of
 //                 four positions, whose code words are put side by side by halves; P^T
 //                 is S^T's accumulator transposed in registers (movmatrix).
@@ -20,7 +21,7 @@
 // (kv4_attn.cuh), exactly.  Queries are scaled by a power of two per row to 1 .. 2 and
 // rounded to half (11 bits, below 2^-14 of the row's largest 2^-25 of it), the power goes
 // into the softmax's factor.  Probabilities are rounded to half for the product only (their sum is taken
-// before): 2^-12 of the largest value at most.
+// before): each by 2^-11 of it at most, or 2^-32 of the row's largest where that is more.
 //
 // Work: all streams end to end, each as its chunks of 32 positions and kOpen chunks'
 // worth for its beginning and end, in equal shares per CTA.  (With kOpen 4, 8, 10 and 12:
@@ -485,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[b][t][e] *= al[e & 1];
         }
-        const float ref[2] = {m[b][0] == -INFINITY ? 0.f : m[b][0], m[b][1] == -INFINITY ? 0.f : m[b][1]};
+        const float ref[2] = {m[b][0] == -INFINITY ? 0.f : m[b][0] - kHigh, m[b][1] == -INFINITY ? 0.f : m[b][1] - kHigh};
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           float p[4];

@@ -34,6 +34,14 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs4& A, int i, bool* bad) {
   return s;
 }
 
+// Probabilities enter the products as halves, 2^kHigh times what the running reference makes
+// them: a row's largest is 2^7 at least, and 2^15 at most, since the reference follows the
+// maximum when that is more than 8 above.  With eleven bits down to 2^-21 of the largest, and
+// below that steps of 2^-31 of it, a million small ones behind a few large ones still add up.  (At
+// 1 to 2^8 they would be rounded to steps of 2^-24 of the largest, or to nothing: 4,092
+// positions with 2^-23.4 of it each came out a third too small.)
+constexpr float kHigh = 7.f;
+
 // For query rows that enter the products as halves of 1 .. 2: the power of two that takes
 // the row's largest magnitude there, and the factor that takes a score of the halves to
 // base 2 (base: log2(e) times the scores' scale; above zero, so that it takes -inf to -inf).

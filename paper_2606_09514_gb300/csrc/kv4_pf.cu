@@ -6,8 +6,8 @@
 // key/value tiles of 128 positions.  On the 5th-generation tensor cores, in half:
 //   S = Q K^T   tcgen05.mma M = 128, N = 128, K = HD: queries and keys from shared memory, S in TMEM;
 //   softmax     four warps per tile, a row per thread, base 2: running reference m,
-//               which follows the maximum when that rises by more than 8; p back into
-//               TMEM as half over S's columns;
+//               which follows the maximum when that rises by more than 8; p, 2^7 times
+//               that of the reference, back into TMEM as half over S's columns;
 //   O += P V    M = 128, N = HD, K = 128: P from TMEM, V from shared memory (MN-major),
 //               O in TMEM.
 // Four producer warps take the codes of a tile's positions from the pages (a position per
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
               }
             }
           }
-          const float ref = m == -INFINITY ? 0.f : m;
+          const float ref = m == -INFINITY ? 0.f : m - kHigh;
           // The first half of P is handed over while the second is worked out.
           const uint64_t fac2 = pair(fac, fac), ref2 = pair(-ref, -ref);
           uint64_t ls[2] = {0, 0};
