@@ -716,6 +716,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       };
+      // (the whole warp goes on or leaves: its lanes say together which pages are there)
+      auto emptied = [&](uint64_t* bar, uint32_t u) {
+        return __all_sync(0xffffffffu, ptx::mbar_wait_bounded(bar, ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag));
+      };
       Entry ek, ev;
       int id = id_of(it.j0), id_next = -1;
       load(A.p.k, it.j0, id, &ek);
@@ -725,13 +729,13 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         const uint32_t u = T + jj;
         const bool more = jj + 1 < len;
         if (more) id_next = id_of(j + 1);
-        if (!ptx::mbar_wait_bounded(&k_empty[u & 1], ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag)) break;
+        if (!emptied(&k_empty[u & 1], u)) break;
         put(sK + (size_t)(u & 1) * TILE, &ek, j, false);
-        const uint32_t bad = __ballot_sync(__activemask(), id == -2);
+        const uint32_t bad = __ballot_sync(0xffffffffu, id == -2);
         if (lane == 0) s_ok[u & 3][lt >> 5] = (uint8_t)(((bad & 0xFFFFu) ? 0 : 1) | ((bad >> 16) ? 0 : 2));
         ptx::mbar_arrive(&k_full[u & 1]);
         if (more) load(A.p.k, j + 1, id_next, &ek);
-        if (!ptx::mbar_wait_bounded(&v_empty[u & 1], ((u >> 1) & 1) ^ 1, kWaitLimitNs, &abort_flag)) break;
+        if (!emptied(&v_empty[u & 1], u)) break;
         put(sV + (size_t)(u & 1) * TILE, &ev, j, true);
         ptx::mbar_arrive(&v_full[u & 1]);
         if (more) load(A.p.v, j + 1, id_next, &ev);

@@ -49,3 +49,10 @@ def test_no_state_kept_in_functions():
     found = [f"{f.name}: {line.strip()}" for f in sorted(CSRC.glob("*.cu*")) + sorted(CSRC.glob("*.h"))
              for line in code(f).splitlines() if re.match(r"\s+static\s+(?!const\b|constexpr\b)", line)]
     assert not found
+
+
+# The active mask says which lanes happen to be together, not which have to take part: after
+# waits that lanes end one by one it may hold some of them.
+def test_no_warp_intrinsic_goes_by_the_active_mask():
+    found = [f.name for f in sorted(CSRC.glob("*.cu*")) if "__activemask" in code(f)]
+    assert not found
