@@ -752,7 +752,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   __syncthreads();
   if (warp == kMmaWarp) {
     if (abort_flag) {
-      if (lane == 0) {
+      if (ptx::elect_one()) {   // the thread that has issued them
         ptx::mma_commit(&drained);
         volatile int dummy = 0;
         ptx::mbar_wait_bounded(&drained, 0, kWaitLimitNs, &dummy);

@@ -56,3 +56,14 @@ def test_no_state_kept_in_functions():
 def test_no_warp_intrinsic_goes_by_the_active_mask():
     found = [f.name for f in sorted(CSRC.glob("*.cu*")) if "__activemask" in code(f)]
     assert not found
+
+
+# A commit follows the MMAs of the thread that makes it: where an elected thread issues
+# them, lane 0 need not be that thread.
+@pytest.mark.parametrize("path", [pytest.param(f, id=f.name) for f in sorted(CSRC.glob("*.cu"))
+                                  if "mma_commit" in f.read_text() and "elect_one()" in f.read_text()])
+def test_commits_are_made_by_the_thread_that_issues(path):
+    text = code(path)
+    for m in re.finditer(r"mma_commit", text):
+        before = text[:m.start()]
+        assert before.rfind("elect_one()") > before.rfind("lane == 0"), text[m.start() - 80:m.end() + 20]
