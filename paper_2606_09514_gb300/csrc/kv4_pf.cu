@@ -41,7 +41,9 @@ constexpr int kPfThreads = 512;          // four warpgroups: two of softmax, pro
 // Registers: 128 a thread at launch (65,536 in all), then by setmaxnreg 2 x 128 x 184 +
 // 128 x 80 + 128 x 64 = 65,536.  (What spills, in any role, is felt: nine requests take 260 us so, 275
 // with 176, 88 and 72, 287 with 168, 96 and 80, 294 with 192, 72 and 56.)
-constexpr int kPfRegsSoft = 184, kPfRegsProduce = 80, kPfRegsMma = 64;
+constexpr int kPfRegsSoft = 184, kPfRegsProduce = 80, kPfRegsMma = 64, kPfRegs = 128;
+static_assert(256 * kPfRegsSoft + kPfProducers * kPfRegsProduce + 128 * kPfRegsMma <= kPfThreads * kPfRegs,
+              "the roles' registers come out of the launch's");
 constexpr int kPfOpen = 4;               // what beginning and ending an item costs, in tiles
 constexpr int kPfWhole = 4;              // items of at most this many tiles are not cut
 constexpr uint32_t kPfRegion = 128u * 128u;   // 128 rows x 64 channels of half
@@ -827,8 +829,11 @@ int64_t prompt_workspace(int head_dim, int sms) {
 
 template <int HD>
 static int launch_prompt_hd(const AttnArgs4& A, CutItem* cuts, int sms, cudaStream_t s) {
-  if (cudaFuncSetAttribute(kv4_prompt_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pf_smem<HD>()) !=
-      cudaSuccess)
+  // (built with fewer registers, the roles would wait for ever for theirs)
+  cudaFuncAttributes at;
+  if (cudaFuncGetAttributes(&at, kv4_prompt_kernel<HD>) != cudaSuccess || at.numRegs != kPfRegs ||
+      cudaFuncSetAttribute(kv4_prompt_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pf_smem<HD>()) !=
+          cudaSuccess)
     return BUDDY_ERR_CUDA;
   // the prompts start on the SMs that the few-row kernel leaves free, the join is launched
   // as the prompts end

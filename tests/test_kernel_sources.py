@@ -67,3 +67,12 @@ def test_commits_are_made_by_the_thread_that_issues(path):
     for m in re.finditer(r"mma_commit", text):
         before = text[:m.start()]
         assert before.rfind("elect_one()") > before.rfind("lane == 0"), text[m.start() - 80:m.end() + 20]
+
+
+# setmaxnreg.inc takes from what the block was launched with and waits for ever for more: the
+# host compares the kernel's registers with what its roles ask for before it launches it.
+def test_register_splits_are_checked_before_the_launch():
+    for f in sorted(CSRC.glob("*.cu")):
+        text = code(f)
+        if "setmaxnreg.inc" in text:
+            assert "numRegs" in text and "static_assert" in text, f.name
