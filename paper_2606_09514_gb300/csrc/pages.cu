@@ -97,19 +97,20 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const buddy_pag
   }
   __syncthreads();
 
+  // (counted in 64 bits: both ends may be next to 2^31)
   const int stride = gridDim.x * kPlanThreads, first = blockIdx.x * kPlanThreads + tid;
-  for (int x = first; x < NP; x += stride) {
-    const int i = last_at_most(page, A.batch, x);
+  for (int64_t x = first; x < NP; x += stride) {
+    const int i = last_at_most(page, A.batch, (int)x);
     const int64_t held = ((int64_t)A.len[i] + mask) >> shift;
     A.table[(int64_t)i * A.max_pages + held + (x - page[i])] = A.free_pages[head + x];
   }
-  for (int t = first; t < A.n_tok; t += stride) {
+  for (int64_t t = first; t < A.n_tok; t += stride) {
     int64_t slot = -1;
     int p = -1;
     if (t < T) {
-      const int i = last_at_most(tok, A.batch, t);
+      const int i = last_at_most(tok, A.batch, (int)t);
       const int n = A.len[i];
-      p = n + (t - tok[i]);
+      p = n + ((int)t - tok[i]);
       const int64_t at = p >> shift, held = ((int64_t)n + mask) >> shift;
       const int32_t id = at < held ? A.table[(int64_t)i * A.max_pages + at] : A.free_pages[head + page[i] + (at - held)];
       slot = ((int64_t)id << shift) + (p & mask);
