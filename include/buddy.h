@@ -421,7 +421,8 @@ typedef struct {
  * + n_new[i]; row_start[i] = new tokens before sequence i, row_start[batch] =
  * their number; for token t of the call its slot and its position; -1 for both
  * behind the last token, up to n_tok; *free_head_out = the index after the last
- * page taken.  No output may overlap an input other than `table`.
+ * page taken.  What is written (`table` among it) overlaps neither an input nor
+ * anything else that is written (else BUDDY_ERR_ARG).
  * Device-checked: lengths >= 0, len[i] + n_new[i] <= max_pages * page_size, at
  * most n_tok new tokens (BUDDY_DEV_BAD_POSITION); 0 <= *free_head and as many free
  * pages left as the call needs (BUDDY_DEV_NO_PAGES); on failure nothing is

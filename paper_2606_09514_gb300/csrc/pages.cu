@@ -120,6 +120,15 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const buddy_pag
   }
 }
 
+struct Range {
+  const void* p;
+  int64_t bytes;
+};
+static bool overlap(const Range& a, const Range& b) {
+  const auto x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+
 }  // namespace buddy
 
 using namespace buddy;
@@ -130,8 +139,18 @@ extern "C" int buddy_page_plan(const buddy_page_plan_args* a, int32_t* flags, vo
       !a->n_new || !a->table || !a->free_head || !a->kv_len || !a->row_start || !a->free_head_out ||
       (a->n_free > 0 && !a->free_pages) || (a->n_tok > 0 && (!a->slot || !a->pos)))
     return BUDDY_ERR_ARG;
-  // every CTA reads the inputs: none may be written by another meanwhile
-  if (a->kv_len == a->len || a->kv_len == a->n_new || a->free_head_out == a->free_head) return BUDDY_ERR_ARG;
+  // every CTA reads the inputs while others write: nothing that is written may overlap anything else
+  const auto batch = (int64_t)a->batch;
+  const Range written[] = {{a->table, batch * a->max_pages * 4}, {a->kv_len, batch * 4},
+                           {a->row_start, (batch + 1) * 4},      {a->slot, (int64_t)a->n_tok * 8},
+                           {a->pos, (int64_t)a->n_tok * 4},      {a->free_head_out, 4}};
+  const Range read[] = {{a->len, batch * 4}, {a->n_new, batch * 4}, {a->free_pages, (int64_t)a->n_free * 4}, {a->free_head, 4}};
+  for (const Range& w : written) {
+    for (const Range& r : read)
+      if (overlap(w, r)) return BUDDY_ERR_ARG;
+    for (const Range& o : written)
+      if (&o != &w && overlap(w, o)) return BUDDY_ERR_ARG;
+  }
   int shift = 0;
   while ((1 << shift) < a->page_size) ++shift;
   const size_t smem = 2 * ((size_t)a->batch + 1) * sizeof(int32_t);

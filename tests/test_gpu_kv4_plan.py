@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_kv4 import flags, i32, pkg
+from test_gpu_kv4 import flags, i32, make_plan, pkg, run_plan
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,29 @@ def test_plan_of_nearly_2_to_the_31_tokens(n_new, page):
         assert torch.equal(slot[t0:t1], want) and torch.equal(pos[t0:t1], want.int()), t0
     del slot, pos, table, free, want
     torch.cuda.empty_cache()
+
+
+def test_plan_takes_buffers_that_touch():
+    """Every buffer of a call out of one allocation, one right behind the other."""
+    length, n_new, page = [15, 0, 33], [3, 20, 1], 16
+    want, _ = make_plan(length, n_new, page)
+    run_plan(want, page)
+    t, _ = make_plan(length, n_new, page)
+    names = ["slot", "kv_len", "length", "table", "n_new", "row_start", "free", "pos", "head", "head_out"]
+    words = [t[n].numel() * t[n].element_size() // 4 for n in names]
+    buf, at = torch.zeros(sum(words), dtype=torch.int32, device="cuda"), 0
+    for name, w in zip(names, words):
+        x = buf[at:at + w].view(t[name].dtype).view(t[name].shape)
+        x.copy_(t[name])
+        t[name], at = x, at + w
+    run_plan(t, page)
+    assert all(torch.equal(t[n], want[n]) for n in names) and t["flags"].item() == 0
+
+
+def test_plan_without_new_tokens_or_free_pages():
+    t, _ = make_plan([15, 16], [0, 0], 16, n_tok=0)
+    t["free"] = t["free"][:0]
+    t["head"].zero_()
+    got = run_plan(t, 16)
+    assert got["flags"][0] == 0 and got["kv_len"].tolist() == [15, 16] and got["row_start"].tolist() == [0, 0, 0]
+    assert got["head_out"][0] == 0
