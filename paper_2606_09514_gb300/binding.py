@@ -98,6 +98,10 @@ class BuddyError(RuntimeError):
 _lib = None
 
 
+def _without_calls(why: str, *args):
+    raise RuntimeError(f"_calls.so does not load ({why}): run __graft_entry__.build() first")
+
+
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Loads libbuddy.so (built by __graft_entry__.build()); raises if absent."""
     global _lib
@@ -159,12 +163,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         getattr(lib, name).restype = ctypes.c_int
     try:
         from . import _calls
-    except ImportError as e:
-        raise RuntimeError(f"_calls.so does not load ({e}): run __graft_entry__.build() first") from e
+    except ImportError as e:          # (the rest of the library does without)
+        missing = functools.partial(_without_calls, str(e))
+        _calls = None
     for name in ("page_plan", "qk_norm_rope", "kv4_append", "kv4_read", "kv4_attention"):
         entry = ctypes.cast(getattr(lib, "buddy_" + name), c_p).value
-        setattr(lib, "call_" + name, functools.partial(getattr(_calls, name), entry))
-    lib.call_stream_for_workspace = _calls.stream_for_workspace
+        setattr(lib, "call_" + name, functools.partial(getattr(_calls, name), entry) if _calls else missing)
+    lib.call_stream_for_workspace = _calls.stream_for_workspace if _calls else missing
     if path is None:
         _lib = lib
     return lib

@@ -1,0 +1,36 @@
+"""How the binding and the build get along with the compiled calls of the 4-bit cache."""
+import importlib.metadata
+import shutil
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from paper_2606_09514_gb300 import binding, build
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    build.build()
+
+
+@pytest.fixture
+def without_calls(monkeypatch):
+    import paper_2606_09514_gb300 as pkg
+    monkeypatch.setitem(sys.modules, "paper_2606_09514_gb300._calls", None)     # an import raises ImportError
+    monkeypatch.delattr(pkg, "_calls", raising=False)
+
+
+def test_the_library_loads_without_the_compiled_calls(without_calls):
+    lib = binding.load_library(binding.LIB_PATH)
+    assert lib.buddy_budget_to_k(0.5, 32) > 0
+
+
+def test_the_cache_names_what_is_missing(without_calls, monkeypatch):
+    monkeypatch.setattr(binding, "_lib", binding.load_library(binding.LIB_PATH))
+    z = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(RuntimeError, match="_calls"):
+        binding.buddy_page_plan(z, z, 16, z.view(4, 1), z, z, z, z, z.long(), z, z)
+    with pytest.raises(RuntimeError, match="_calls"):
+        binding.buddy_qk_norm_rope(None, z, z, (z, z), None, z)
