@@ -3,6 +3,7 @@ which turns tensors into its arguments, with the host compiler and torch's heade
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.metadata
 import os
 import shutil
 import subprocess
@@ -17,6 +18,7 @@ LIB = os.path.join(HERE, "libbuddy.so")
 SOURCES = ["api.cu", "kernels.cu", "attention.cu", "gemm_simt.cu", "gemm_tc.cu", "noalloc.cu", "gemm_pf.cu",
            "attn_pf.cu", "prefill.cu", "attn_cl.cu", "pages.cu", "kv4_rows.cu", "kv4_attn.cu", "kv4_pf.cu"]
 CALLS = os.path.join(HERE, "_calls.so")
+CALLS_FOR = os.path.join(OUT_DIR, "calls_for.txt")   # the torch and the command that it was built with
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr", "-Xptxas", "-warn-spills"]
@@ -47,6 +49,20 @@ def _calls_command(nvcc: str) -> list:
             "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
 
 
+def _torch_version() -> str:
+    try:
+        return importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        return ""
+
+
+def _calls_built_for() -> str:
+    try:
+        return open(CALLS_FOR).read()
+    except FileNotFoundError:
+        return ""
+
+
 def build(verbose: bool = False, force: bool = False) -> str:
     nvcc = _nvcc()
     os.makedirs(OUT_DIR, exist_ok=True)
@@ -59,9 +75,11 @@ def build(verbose: bool = False, force: bool = False) -> str:
         if force or _stale(obj, src):
             jobs.append([nvcc, *ARCH, *FLAGS, "-c", src, "-o", obj])
     kernels = bool(jobs)
-    calls = force or _stale(CALLS, os.path.join(CSRC, "calls.cpp"))
+    calls_command = _calls_command(nvcc)
+    calls_for = _torch_version() + "\n" + " ".join(calls_command)
+    calls = force or _stale(CALLS, os.path.join(CSRC, "calls.cpp")) or _calls_built_for() != calls_for
     if calls:
-        jobs.append(_calls_command(nvcc))
+        jobs.append(calls_command)
     with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         results = list(ex.map(lambda cmd: subprocess.run(cmd, capture_output=True, text=True), jobs))
     for cmd, r in zip(jobs, results):
@@ -71,6 +89,8 @@ def build(verbose: bool = False, force: bool = False) -> str:
             raise RuntimeError(f"failed: {' '.join(cmd)}")
     if calls:
         os.replace(CALLS + ".tmp", CALLS)
+        with open(CALLS_FOR, "w") as f:
+            f.write(calls_for)
     if kernels or not os.path.exists(LIB):
         link = [nvcc, *ARCH, "-shared", "-o", LIB + ".tmp", *objs]
         r = subprocess.run(link, capture_output=True, text=True)

@@ -34,3 +34,24 @@ def test_the_cache_names_what_is_missing(without_calls, monkeypatch):
         binding.buddy_page_plan(z, z, 16, z.view(4, 1), z, z, z, z, z.long(), z, z)
     with pytest.raises(RuntimeError, match="_calls"):
         binding.buddy_qk_norm_rope(None, z, z, (z, z), None, z)
+
+
+def test_the_compiled_calls_are_built_for_the_torch_that_is_there(monkeypatch, tmp_path):
+    """Another version of torch builds them anew, the same one does not."""
+    real_run, real_version, version, built = subprocess.run, importlib.metadata.version, [None], []
+
+    def run(cmd, *a, **kw):
+        if build.CALLS + ".tmp" not in cmd:
+            return real_run(cmd, *a, **kw)
+        built.append(version[0])
+        shutil.copy(build.CALLS, build.CALLS + ".tmp")
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+
+    monkeypatch.setattr(build.subprocess, "run", run)
+    monkeypatch.setattr(importlib.metadata, "version",
+                        lambda name: version[0] if name == "torch" and version[0] else real_version(name))
+    monkeypatch.setattr(build, "CALLS_FOR", str(tmp_path / "for"), raising=False)
+    for v in (None, None, "9.9.9", "9.9.9", None):
+        version[0] = v
+        build.build()
+    assert built == [None, "9.9.9", None]
