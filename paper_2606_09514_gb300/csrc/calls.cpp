@@ -106,6 +106,14 @@ int64_t heads(const at::Tensor& t, ScalarType type, int64_t tokens, int64_t n, i
   return t.stride(0);
 }
 
+// A rotary table: [positions, head_dim / 2].
+const float* table(PyObject* o, int64_t hd, const char* what, int32_t* positions) {
+  const at::Tensor& t = vec(o, ScalarType::Float, 0, what);
+  if (t.dim() != 2 || 2 * t.size(1) != hd) wrong(what, "[positions, head_dim / 2] is wanted");
+  *positions = int32(t.size(0), what);
+  return static_cast<const float*>(t.data_ptr());
+}
+
 int32_t dtype_of(ScalarType t) {
   return t == ScalarType::Float ? BUDDY_DTYPE_F32
          : t == ScalarType::BFloat16 ? BUDDY_DTYPE_BF16
@@ -222,14 +230,13 @@ buddy_qk_rows rows_of(PyObject* const* a) {
     r.q_out_stride = heads(t, type, T, r.n_q_heads, hd, "q_out");
     r.q_out = r.n_q_heads ? t.data_ptr() : nullptr;
   }
-  const at::Tensor& co = tensor(a[3], "cos");
-  if (co.dim() < 1) wrong("cos", "[positions, head_dim / 2] is wanted");
-  r.max_pos = int32(co.size(0), "cos");
+  r.rope_cos = table(a[3], hd, "cos", &r.max_pos);
+  int32_t rows;
+  r.rope_sin = table(a[4], hd, "sin", &rows);
+  if (rows != r.max_pos) wrong("sin", "as many positions as in cos are wanted");
   r.q_gain = data_or_null<float>(a[7], F, hd, "q_gain");
   r.k_gain = data_or_null<float>(a[8], F, hd, "k_gain");
   r.pos = data<int32_t>(a[2], ScalarType::Int, T, "pos");
-  r.rope_cos = data<float>(a[3], F, r.max_pos * hd / 2, "cos");
-  r.rope_sin = data<float>(a[4], F, r.max_pos * hd / 2, "sin");
   return r;
 }
 
