@@ -406,9 +406,12 @@ def _vectors(*wanted):
 
 def buddy_rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None):
     """(cos, sin) rotary tables, [max_pos, head_dim / 2] fp32 each."""
-    co, si = (torch.empty(max_pos, head_dim // 2, dtype=torch.float32, device=device) for _ in range(2))
-    _check(load_library().buddy_rope_table(_ptr(co), _ptr(si), max_pos, head_dim, theta, _stream(stream)),
-           "buddy_rope_table")
+    if torch.device(device).type != "cuda":
+        raise ValueError("device: a CUDA device is wanted")
+    with torch.cuda.device(device), torch.cuda.stream(stream):      # (the memory is the stream's that fills it)
+        co, si = (torch.empty(max_pos, head_dim // 2, dtype=torch.float32, device=device) for _ in range(2))
+        _check(load_library().buddy_rope_table(_ptr(co), _ptr(si), max_pos, head_dim, theta, _stream(stream)),
+               "buddy_rope_table")
     return co, si
 
 

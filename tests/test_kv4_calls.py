@@ -115,3 +115,49 @@ def test_a_given_workspace_is_used(cache):
     attend(c)
     attend(c, stream=Stream(3))
     assert len(made) == n and all(ws is c.workspace for _, ws in lib.calls)
+
+
+# ------------------------------------------------------------------ rotary tables
+def test_rotary_tables_are_filled_on_the_stream_that_they_are_made_on(monkeypatch):
+    """Memory of another stream's pool may still be in use there."""
+    now, made, filled = [Stream(0)], {}, []
+
+    @contextlib.contextmanager
+    def on(stream):
+        now.append(stream or now[-1])
+        yield
+        now.pop()
+
+    real = torch.empty
+
+    def empty(*size, device, **kw):
+        t = real(*size, **kw)
+        made[t.data_ptr()] = (now[-1].cuda_stream, device)
+        return t
+
+    class Lib:
+        def buddy_rope_table(self, co, si, max_pos, hd, theta, stream):
+            filled.append((made[co.value], made[si.value], stream.value or 0))
+            return b.BUDDY_OK
+
+    monkeypatch.setattr(b.torch.cuda, "stream", on)
+    monkeypatch.setattr(b.torch.cuda, "device", lambda d: contextlib.nullcontext())
+    monkeypatch.setattr(b.torch.cuda, "current_stream", lambda *a: now[-1])
+    monkeypatch.setattr(b.torch, "empty", empty)
+    monkeypatch.setattr(b, "load_library", lambda *a: Lib())
+    for stream, want in ((None, 0), (Stream(7), 7)):
+        co, si = b.buddy_rope_table(9, 64, 1e4, stream=stream)
+        assert co.shape == si.shape == (9, 32)
+        (co_on, _), (si_on, _), launched = filled[-1]
+        assert co_on == si_on == launched == want
+
+
+@pytest.mark.parametrize("device", ["cpu", "meta", torch.device("cpu")])
+def test_rotary_tables_are_on_a_gpu(monkeypatch, device):
+    class Lib:
+        def buddy_rope_table(self, *args):
+            raise AssertionError("called with host memory")
+
+    monkeypatch.setattr(b, "load_library", lambda *a: Lib())
+    with pytest.raises(ValueError, match="device"):
+        b.buddy_rope_table(9, 64, 1e4, device)
