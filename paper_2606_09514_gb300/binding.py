@@ -68,6 +68,11 @@ class buddy_kv4_cache(ctypes.Structure):
                 ("n_kv_heads", c_i32), ("head_dim", c_i32)]
 
 
+class _CacheOnDevice(ctypes.Structure):
+    """What the compiled calls take for a cache."""
+    _fields_ = [("cache", buddy_kv4_cache), ("device", c_i32)]
+
+
 class buddy_page_plan_args(ctypes.Structure):
     _fields_ = [("batch", c_i32), ("page_size", c_i32), ("max_pages", c_i32), ("n_free", c_i32), ("n_tok", c_i32),
                 ("len", c_p), ("n_new", c_p), ("table", c_p), ("free_pages", c_p), ("free_head", c_p),
@@ -454,7 +459,10 @@ class KV4Cache:
         self.k_pages, self.v_pages, self.page_size, self.n_kv = k_pages, v_pages, page_size, n_kv
         _vectors((k_pages, torch.uint8, 0, "k_pages"), (v_pages, torch.uint8, 0, "v_pages"))
         self.state = buddy_kv4_cache(k_pages.data_ptr(), v_pages.data_ptr(), n_pages, page_size, n_kv, self.head_dim)
-        self.address = ctypes.addressof(self.state)
+        if v_pages.device != k_pages.device:
+            raise ValueError("v_pages: a tensor on the device of k_pages is wanted")
+        self._on_device = _CacheOnDevice(self.state, k_pages.get_device())
+        self.address = ctypes.addressof(self._on_device)
         self.lib = load_library()
         self.workspace = workspace
         self._made: Dict = {}           # workspaces made here: (device, stream) -> tensor
@@ -469,7 +477,8 @@ class KV4Cache:
     def workspace_bytes(self, n_q_heads: int, max_new: int = 1) -> int:
         n = self._need.get((n_q_heads, max_new))
         if n is None:
-            n = self.lib.buddy_kv4_attention_workspace(n_q_heads, self.n_kv, self.head_dim, max_new)
+            with torch.cuda.device(self.k_pages.get_device()):
+                n = self.lib.buddy_kv4_attention_workspace(n_q_heads, self.n_kv, self.head_dim, max_new)
             if n < 0:
                 raise BuddyError(BUDDY_ERR_ARG, "buddy_kv4_attention_workspace")
             self._need[n_q_heads, max_new] = n

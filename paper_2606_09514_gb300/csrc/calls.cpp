@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <c10/cuda/CUDAException.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -66,6 +67,12 @@ float real(PyObject* o) {
   if (v == -1.0 && PyErr_Occurred()) throw Failed{};
   return (float)v;
 }
+// What a cache's address stands for: its argument, and the device of its pages.
+struct Cache {
+  buddy_kv4_cache c;
+  int32_t device;
+};
+
 template <class F>
 F entry(PyObject* o) {
   void* p = PyLong_AsVoidPtr(o);
@@ -76,39 +83,57 @@ F entry(PyObject* o) {
   return reinterpret_cast<F>(p);
 }
 
+// The device of a call: that of its first tensor.  The others are on it too.
+struct Device {
+  int index = -1;
+  void take(const at::Tensor& t, const char* what) {
+    if (index < 0) index = t.get_device();
+    if (t.get_device() != index) wrong(what, "a tensor on the device of the others is wanted");
+  }
+};
+
+const Cache* pages(Device& d, PyObject* address) {
+  const Cache* const c = entry<const Cache*>(address);
+  if (d.index < 0) d.index = c->device;
+  if (d.index != c->device) wrong("pages", "a cache on the device of the tensors is wanted");
+  return c;
+}
+
 // A contiguous CUDA tensor of n or more elements of a type.
-const at::Tensor& vec(PyObject* o, ScalarType type, int64_t n, const char* what) {
+const at::Tensor& vec(Device& d, PyObject* o, ScalarType type, int64_t n, const char* what) {
   const at::Tensor& t = tensor(o, what);
   if (t.scalar_type() != type || !t.is_cuda() || !t.is_contiguous() || t.numel() < n) {
     PyErr_Format(PyExc_ValueError, "%s: a contiguous CUDA tensor of %lld or more %s is wanted", what, (long long)n,
                  name_of(type));
     throw Failed{};
   }
+  d.take(t, what);
   return t;
 }
 template <class T>
-T* data(PyObject* o, ScalarType type, int64_t n, const char* what) {
-  return static_cast<T*>(vec(o, type, n, what).data_ptr());
+T* data(Device& d, PyObject* o, ScalarType type, int64_t n, const char* what) {
+  return static_cast<T*>(vec(d, o, type, n, what).data_ptr());
 }
 template <class T>
-T* data_or_null(PyObject* o, ScalarType type, int64_t n, const char* what) {
-  return o == Py_None ? nullptr : data<T>(o, type, n, what);
+T* data_or_null(Device& d, PyObject* o, ScalarType type, int64_t n, const char* what) {
+  return o == Py_None ? nullptr : data<T>(d, o, type, n, what);
 }
 
 // [tokens, heads, head_dim] with whole heads one after the other: elements from token to token.
-int64_t heads(const at::Tensor& t, ScalarType type, int64_t tokens, int64_t n, int64_t hd, const char* what) {
+int64_t heads(Device& d, const at::Tensor& t, ScalarType type, int64_t tokens, int64_t n, int64_t hd, const char* what) {
   if (t.scalar_type() != type || !t.is_cuda() || t.dim() != 3 || t.size(0) != tokens || t.size(1) != n ||
       t.size(2) != hd || t.stride(2) != 1 || (t.stride(1) != hd && n > 1)) {
     PyErr_Format(PyExc_ValueError, "%s: CUDA %s (%lld, %lld, %lld) with whole heads one after the other is wanted", what,
                  name_of(type), (long long)tokens, (long long)n, (long long)hd);
     throw Failed{};
   }
+  d.take(t, what);
   return t.stride(0);
 }
 
 // A rotary table: [positions, head_dim / 2].
-const float* table(PyObject* o, int64_t hd, const char* what, int32_t* positions) {
-  const at::Tensor& t = vec(o, ScalarType::Float, 0, what);
+const float* table(Device& d, PyObject* o, int64_t hd, const char* what, int32_t* positions) {
+  const at::Tensor& t = vec(d, o, ScalarType::Float, 0, what);
   if (t.dim() != 2 || 2 * t.size(1) != hd) wrong(what, "[positions, head_dim / 2] is wanted");
   *positions = int32(t.size(0), what);
   return static_cast<const float*>(t.data_ptr());
@@ -142,8 +167,11 @@ PyObject* stream_for_workspace(PyObject* const* a) {
   return PyLong_FromVoidPtr(s);
 }
 
+// The call, with its device as the current one.
 template <class F>
-PyObject* called(F&& f) {
+PyObject* called(const Device& d, F&& f) {
+  c10::cuda::OptionalCUDAGuard guard;
+  if (c10::cuda::current_device() != d.index) guard.set_index((c10::DeviceIndex)d.index);
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = f();
@@ -170,37 +198,38 @@ PyObject* guarded(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // entry, length, n_new, page_size, table, free_pages, free_head, kv_len, row_start, slot, pos,
 // free_head_out, flags, stream
 PyObject* page_plan(PyObject* const* a) {
+  Device d;
   const at::Tensor& length = tensor(a[1], "length");
   const int64_t B = length.numel();
   const auto I = ScalarType::Int, L = ScalarType::Long;
-  const at::Tensor& slot = vec(a[9], L, 0, "slot");
-  const at::Tensor& table = vec(a[4], I, 0, "table");
-  const at::Tensor& free = vec(a[5], I, 0, "free_pages");
+  const at::Tensor& slot = vec(d, a[9], L, 0, "slot");
+  const at::Tensor& table = vec(d, a[4], I, 0, "table");
+  const at::Tensor& free = vec(d, a[5], I, 0, "free_pages");
   buddy_page_plan_args p{};
   p.batch = int32(B, "length");
   p.page_size = int32(a[3]);
   p.n_free = int32(free.numel(), "free_pages");
   p.n_tok = int32(slot.numel(), "slot");
-  p.len = data<int32_t>(a[1], I, B, "length");
-  p.n_new = data<int32_t>(a[2], I, B, "n_new");
+  p.len = data<int32_t>(d, a[1], I, B, "length");
+  p.n_new = data<int32_t>(d, a[2], I, B, "n_new");
   p.table = static_cast<int32_t*>(table.data_ptr());
   p.free_pages = static_cast<int32_t*>(free.data_ptr());
-  p.free_head = data<int32_t>(a[6], I, 1, "free_head");
-  p.kv_len = data<int32_t>(a[7], I, B, "kv_len");
-  p.row_start = data<int32_t>(a[8], I, B + 1, "row_start");
+  p.free_head = data<int32_t>(d, a[6], I, 1, "free_head");
+  p.kv_len = data<int32_t>(d, a[7], I, B, "kv_len");
+  p.row_start = data<int32_t>(d, a[8], I, B + 1, "row_start");
   p.slot = static_cast<int64_t*>(slot.data_ptr());
-  p.pos = data<int32_t>(a[10], I, p.n_tok, "pos");
-  p.free_head_out = data<int32_t>(a[11], I, 1, "free_head_out");
-  int32_t* flags = data_or_null<int32_t>(a[12], I, 1, "flags");
+  p.pos = data<int32_t>(d, a[10], I, p.n_tok, "pos");
+  p.free_head_out = data<int32_t>(d, a[11], I, 1, "free_head_out");
+  int32_t* flags = data_or_null<int32_t>(d, a[12], I, 1, "flags");
   if (table.dim() != 2 || table.size(0) != B) wrong("table", "[batch, max_pages] is wanted");
   p.max_pages = int32(table.size(1), "table");
   void* s = stream_of(length, a[13]);
   auto f = entry<decltype(&buddy_page_plan)>(a[0]);
-  return called([&] { return f(&p, flags, s); });
+  return called(d, [&] { return f(&p, flags, s); });
 }
 
 // q, k, pos, cos, sin, q_out, k_out, q_gain, k_gain, eps
-buddy_qk_rows rows_of(PyObject* const* a) {
+buddy_qk_rows rows_of(Device& d, PyObject* const* a) {
   const at::Tensor& k = tensor(a[1], "k");
   const ScalarType type = k.scalar_type();
   const auto F = ScalarType::Float;
@@ -213,79 +242,83 @@ buddy_qk_rows rows_of(PyObject* const* a) {
   r.dtype = dtype_of(type);
   r.eps = real(a[9]);
   r.k = k.data_ptr();
-  r.k_stride = heads(k, type, T, nkv, hd, "k");
+  r.k_stride = heads(d, k, type, T, nkv, hd, "k");
   if (a[6] != Py_None) {
     const at::Tensor& t = tensor(a[6], "k_out");
-    r.k_out_stride = heads(t, type, T, nkv, hd, "k_out");
+    r.k_out_stride = heads(d, t, type, T, nkv, hd, "k_out");
     r.k_out = t.data_ptr();
   }
   if (a[0] != Py_None) {
     const at::Tensor& q = tensor(a[0], "q");
     if (q.dim() != 3) wrong("q", "[tokens, heads, head_dim] is wanted");
     r.n_q_heads = int32(q.size(1), "q");
-    r.q_stride = heads(q, type, T, r.n_q_heads, hd, "q");
+    r.q_stride = heads(d, q, type, T, r.n_q_heads, hd, "q");
     r.q = q.data_ptr();
     if (a[5] == Py_None) wrong("q_out", "is wanted with q");
     const at::Tensor& t = tensor(a[5], "q_out");
-    r.q_out_stride = heads(t, type, T, r.n_q_heads, hd, "q_out");
+    r.q_out_stride = heads(d, t, type, T, r.n_q_heads, hd, "q_out");
     r.q_out = r.n_q_heads ? t.data_ptr() : nullptr;
   }
-  r.rope_cos = table(a[3], hd, "cos", &r.max_pos);
+  r.rope_cos = table(d, a[3], hd, "cos", &r.max_pos);
   int32_t rows;
-  r.rope_sin = table(a[4], hd, "sin", &rows);
+  r.rope_sin = table(d, a[4], hd, "sin", &rows);
   if (rows != r.max_pos) wrong("sin", "as many positions as in cos are wanted");
-  r.q_gain = data_or_null<float>(a[7], F, hd, "q_gain");
-  r.k_gain = data_or_null<float>(a[8], F, hd, "k_gain");
-  r.pos = data<int32_t>(a[2], ScalarType::Int, T, "pos");
+  r.q_gain = data_or_null<float>(d, a[7], F, hd, "q_gain");
+  r.k_gain = data_or_null<float>(d, a[8], F, hd, "k_gain");
+  r.pos = data<int32_t>(d, a[2], ScalarType::Int, T, "pos");
   return r;
 }
 
 // entry, the ten of rows_of, flags, stream
 PyObject* qk_norm_rope(PyObject* const* a) {
-  const buddy_qk_rows r = rows_of(a + 1);
-  int32_t* flags = data_or_null<int32_t>(a[11], ScalarType::Int, 1, "flags");
+  Device d;
+  const buddy_qk_rows r = rows_of(d, a + 1);
+  int32_t* flags = data_or_null<int32_t>(d, a[11], ScalarType::Int, 1, "flags");
   void* s = stream_of(tensor(a[2], "k"), a[12]);
   auto f = entry<decltype(&buddy_qk_norm_rope)>(a[0]);
-  return called([&] { return f(&r, flags, s); });
+  return called(d, [&] { return f(&r, flags, s); });
 }
 
 // entry, cache's address, the ten of rows_of, v, slot, flags, stream
 PyObject* kv4_append(PyObject* const* a) {
-  const buddy_qk_rows r = rows_of(a + 2);
+  Device d;
+  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
+  const buddy_qk_rows r = rows_of(d, a + 2);
   const at::Tensor& k = tensor(a[3], "k");
   const at::Tensor& v = tensor(a[12], "v");
-  const int64_t stride = heads(v, k.scalar_type(), r.n_tok, r.n_kv_heads, r.head_dim, "v");
-  const int64_t* slot = data<int64_t>(a[13], ScalarType::Long, r.n_tok, "slot");
-  int32_t* flags = data_or_null<int32_t>(a[14], ScalarType::Int, 1, "flags");
+  const int64_t stride = heads(d, v, k.scalar_type(), r.n_tok, r.n_kv_heads, r.head_dim, "v");
+  const int64_t* slot = data<int64_t>(d, a[13], ScalarType::Long, r.n_tok, "slot");
+  int32_t* flags = data_or_null<int32_t>(d, a[14], ScalarType::Int, 1, "flags");
   void* s = stream_of(k, a[15]);
-  auto c = entry<const buddy_kv4_cache*>(a[1]);
   auto f = entry<decltype(&buddy_kv4_append)>(a[0]);
   const void* pv = v.data_ptr();
-  return called([&] { return f(c, &r, pv, stride, slot, flags, s); });
+  return called(d, [&] { return f(c, &r, pv, stride, slot, flags, s); });
 }
 
 // entry, cache's address, slot, k_out, v_out, flags, stream
 PyObject* kv4_read(PyObject* const* a) {
-  auto c = entry<const buddy_kv4_cache*>(a[1]);
-  const at::Tensor& slot = vec(a[2], ScalarType::Long, 0, "slot");
+  Device d;
+  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
+  const at::Tensor& slot = vec(d, a[2], ScalarType::Long, 0, "slot");
   PyObject* const out = a[3] != Py_None ? a[3] : a[4];
   const ScalarType type = out == Py_None ? ScalarType::Undefined : tensor(out, "k_out, v_out").scalar_type();
   const int32_t dtype = dtype_of(type), n = int32(slot.numel(), "slot");
   if (dtype < 0) wrong("k_out, v_out", "fp32, fp16 or bf16 is wanted");
   const int64_t size = (int64_t)n * c->n_kv_heads * c->head_dim;
-  void* k = data_or_null<void>(a[3], type, size, "k_out");
-  void* v = data_or_null<void>(a[4], type, size, "v_out");
-  int32_t* flags = data_or_null<int32_t>(a[5], ScalarType::Int, 1, "flags");
+  void* k = data_or_null<void>(d, a[3], type, size, "k_out");
+  void* v = data_or_null<void>(d, a[4], type, size, "v_out");
+  int32_t* flags = data_or_null<int32_t>(d, a[5], ScalarType::Int, 1, "flags");
   void* s = stream_of(slot, a[6]);
   const int64_t* at = static_cast<int64_t*>(slot.data_ptr());
   auto f = entry<decltype(&buddy_kv4_read)>(a[0]);
-  return called([&] { return f(c, n, at, dtype, k, v, flags, s); });
+  return called(d, [&] { return f(c, n, at, dtype, k, v, flags, s); });
 }
 
 // entry, cache's address, q, kv_len, table, out, row_start, max_new, scale, flags, workspace, stream
 PyObject* kv4_attention(PyObject* const* a) {
+  Device d;
   const auto I = ScalarType::Int;
-  auto c = entry<const buddy_kv4_cache*>(a[1]);
+  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
   const at::Tensor& q = tensor(a[2], "q");
   const at::Tensor& out = tensor(a[5], "out");
   const at::Tensor& kv_len = tensor(a[3], "kv_len");
@@ -299,23 +332,23 @@ PyObject* kv4_attention(PyObject* const* a) {
   p.scale = real(a[8]);
   p.q_dtype = dtype_of(q.scalar_type());
   p.out_dtype = dtype_of(out.scalar_type());
-  p.q_stride = heads(q, q.scalar_type(), p.n_tok, p.n_q_heads, c->head_dim, "q");
-  p.out_stride = heads(out, out.scalar_type(), p.n_tok, p.n_q_heads, c->head_dim, "out");
+  p.q_stride = heads(d, q, q.scalar_type(), p.n_tok, p.n_q_heads, c->head_dim, "q");
+  p.out_stride = heads(d, out, out.scalar_type(), p.n_tok, p.n_q_heads, c->head_dim, "out");
   p.q = q.data_ptr();
   p.out = out.data_ptr();
-  p.row_start = data_or_null<int32_t>(a[6], I, B + 1, "row_start");
-  p.kv_len = data<int32_t>(a[3], I, B, "kv_len");
-  const at::Tensor& table = vec(a[4], I, 0, "table");
+  p.row_start = data_or_null<int32_t>(d, a[6], I, B + 1, "row_start");
+  p.kv_len = data<int32_t>(d, a[3], I, B, "kv_len");
+  const at::Tensor& table = vec(d, a[4], I, 0, "table");
   if (table.dim() != 2 || table.size(0) != B) wrong("table", "[batch, max_pages] is wanted");
   p.max_pages = int32(table.size(1), "table");
   p.table = static_cast<int32_t*>(table.data_ptr());
-  const at::Tensor& ws = vec(a[10], ScalarType::Byte, 0, "workspace");
+  const at::Tensor& ws = vec(d, a[10], ScalarType::Byte, 0, "workspace");
   p.workspace = ws.data_ptr();
   p.workspace_bytes = ws.numel();
-  int32_t* flags = data_or_null<int32_t>(a[9], I, 1, "flags");
+  int32_t* flags = data_or_null<int32_t>(d, a[9], I, 1, "flags");
   void* s = stream_of(q, a[11]);
   auto f = entry<decltype(&buddy_kv4_attention)>(a[0]);
-  return called([&] { return f(c, &p, flags, s); });
+  return called(d, [&] { return f(c, &p, flags, s); });
 }
 
 template <int N, PyObject* (*F)(PyObject* const*)>
