@@ -98,11 +98,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if one is
   return r;
 }
 
-// Eight consecutive elements as they lie in memory.
+// Eight consecutive elements of a row as they lie in memory.  (Ordinary loads: in place, the
+// kernel writes what it has read, which the path of read-only data does not allow.)
 template <typename T> struct Raw8;
 template <> struct Raw8<bf16> {
   uint4 a;
-  __device__ __forceinline__ void load(const bf16* p) { a = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load(const bf16* p) { a = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void get(F2* o) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -112,17 +113,17 @@ template <> struct Raw8<bf16> {
 template <> struct Raw8<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) {
-    a = __ldg(reinterpret_cast<const float4*>(p));
-    b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
   }
   __device__ __forceinline__ void get(F2* o) const {
     o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
   }
 };
+// Eight values that no kernel of the call writes (gains, rotation factors).
 __device__ __forceinline__ void load8(const float* p, F2* o) {
-  Raw8<float> r;
-  r.load(p);
-  r.get(o);
+  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const F2* x) {

@@ -76,3 +76,11 @@ def test_register_splits_are_checked_before_the_launch():
         text = code(f)
         if "setmaxnreg.inc" in text:
             assert "numRegs" in text and "static_assert" in text, f.name
+
+
+# Queries and keys may be turned in place: their rows are not read through the path of data
+# that no one writes while the kernel runs.
+def test_rows_that_may_be_written_are_read_by_ordinary_loads():
+    text = code(CSRC / "kv4_rows.cu")
+    loaders = re.findall(r"struct Raw8<\w+> \{.*?\n\};", text, flags=re.S)
+    assert len(loaders) == 2 and not any(re.search(r"__ldg|\.nc\b", x) for x in loaders)
