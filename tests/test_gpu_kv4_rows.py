@@ -60,3 +60,29 @@ def test_append_of_many_tokens(heads, T, dtype):
     q0[3], q0[T - 2], k0[3], k0[T - 2] = q[3], q[T - 2], k[3], k[T - 2]           # (tokens that are left out)
     assert torch.equal(q0, q) and torch.equal(k0, k) and torch.equal(v, left) and fl.item() == 0
     assert torch.equal(a.k_pages, c.k_pages) and torch.equal(a.v_pages, c.v_pages)
+
+
+def test_special_keys():
+    """At position 0 the rotation multiplies by one and zero: keys are stored as values are, but
+    for NaN and infinities, which make NaN of the channel that they are turned with."""
+    hd, page = 64, 16
+    x = torch.zeros(7, 1, hd, device="cuda")
+    x[1, 0, 3] = float("nan")
+    x[2, 0, 5], x[2, 0, 6] = float("inf"), 3.0
+    x[3] = 2.0 ** -30
+    x[4, 0, 0], x[4, 0, 1] = 7 * 2.0 ** -24, -3 * 2.0 ** -24
+    x[5, 0, 0] = 1e30
+    x[6, 0, 0], x[6, 0, 33], x[6, 0, 40] = 7.0, -2.5, 1.25
+    cache = pkg().KV4Cache.empty(2, page, 1, hd)
+    slot = torch.arange(3, 10, device="cuda")
+    cache.buddy_kv4_append(None, x, x, torch.zeros(7, dtype=torch.int32, device="cuda"), slot,
+                           pkg().buddy_rope_table(8, hd, 1e4), None)
+    k, v = (torch.empty(7, 1, hd, device="cuda") for _ in range(2))
+    cache.buddy_kv4_read(slot, k, v)
+    k, v = k[:, 0].cpu(), v[:, 0].cpu()
+    same = [0, 3, 4, 5, 6]
+    assert torch.equal(k[same], v[same]) and torch.isfinite(v[same]).all() and v[6].any() and v[5, 0] == 6272
+    assert torch.isnan(k[1]).all()
+    assert torch.isnan(v[1, :32]).all() and torch.all(v[1, 32:] == 0)
+    assert k[2, 5] == v[2, 5] == 6272 and k[2, :32].count_nonzero() == 1 and v[2].count_nonzero() == 1
+    assert torch.isnan(k[2, 32:]).all()
