@@ -518,7 +518,9 @@ BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int6
  * 2^-14 or 2^-14 of the row's largest element, whichever is larger (rounded at
  * 2^-25 or 2^-25 of it).  Probabilities enter with 11 bits, below 2^-21 of the
  * row's largest rounded at 2^-32 of that; keys and values exactly; sums and
- * statistics are fp32.
+ * statistics are fp32.  With fp32 queries or fp32 outputs both enter as the sum of
+ * two halves, with 22 bits (queries rounded at 2^-39 of the row's largest element
+ * or less).
  * Device-checked: 0 <= kv_len[i] <= max_pages * page_size and row_start
  * ascending from >= 0 to <= n_tok with at most max_new rows each
  * (BUDDY_DEV_BAD_POSITION: the sequence's rows are not written); page ids

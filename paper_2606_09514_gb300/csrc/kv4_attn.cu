@@ -21,7 +21,9 @@
 // (kv4_attn.cuh), exactly.  Queries are scaled by a power of two per row to 1 .. 2 and
 // rounded to half (11 bits, below 2^-14 of the row's largest 2^-25 of it), the power goes
 // into the softmax's factor.  Probabilities are rounded to half for the product only (their sum is taken
-// before): each by 2^-11 of it at most, or 2^-32 of the row's largest where that is more.
+// before): each by 2^-11 of it at most, or 2^-32 of the row's largest where that is more.  With fp32
+// queries or outputs (WIDE) both are sums of two halves: twice the MMAs and a CTA less per SM
+// (64 sequences of 8,192 positions 154 us instead of 126; errors of 2^-12 become 2^-20).
 //
 // Work: all streams end to end, each as its chunks of 32 positions and kOpen chunks'
 // worth for its beginning and end, in equal shares per CTA.  (With kOpen 4, 8, 10 and 12:
@@ -63,9 +65,10 @@ constexpr int kChunk = 32;
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 3;
-// CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two).
-template <int NB>
-__host__ __device__ constexpr int ctas_per_sm() { return NB == 1 ? 4 : 3; }
+// CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two; WIDE
+// 168 and 255).
+template <int NB, bool WIDE>
+__host__ __device__ constexpr int ctas_per_sm() { return (NB == 1 ? 4 : 3) - (WIDE ? 1 : 0); }
 constexpr int kWhole = 12;       // streams of at most this many chunks are not cut
 constexpr int kOpen = 10;        // what beginning and ending a stream costs, in chunks
 constexpr int kMany = 2 * kOpen; // shares from this on hold several short streams
@@ -163,8 +166,8 @@ __device__ __forceinline__ void load_piece(const Pages& P, uint32_t dst, uint32_
   bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, v + to_scales, N * SB, bar);
 }
 
-template <int HD, int NB>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel(const AttnArgs4 A) {
+template <int HD, int NB, bool WIDE>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_kernel(const AttnArgs4 A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t full[kWarps * kStages];
   __shared__ volatile int abort_flag;
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       continue;
     }
     // queries: rows lg of each block of eight, this lane's HD / 4 channels
-    uint32_t qf[NB][KS][2];
+    uint32_t qf[NB][KS][2], ql[WIDE ? NB : 1][KS][2];
     float fac[NB][2];               // of the scores of rows 2 lc and 2 lc + 1
     int seen[NB][2];
 #pragma unroll
@@ -382,10 +385,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       float down, f;
-      row_scale(top, (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f, &down, &f);
+      row_scale<WIDE>(top, (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f, &down, &f);
 #pragma unroll
-      for (int e = 0; e < HD / 4; e += 2)
-        qf[b][e / 4][(e / 2) & 1] = h2(__floats2half2_rn(x[e] * down, x[e + 1] * down));
+      for (int e = 0; e < HD / 4; e += 2) {
+        const Halves<WIDE> y(x[e] * down, x[e + 1] * down);
+        qf[b][e / 4][(e / 2) & 1] = y.hi;
+        if constexpr (WIDE) ql[b][e / 4][(e / 2) & 1] = y.lo;
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         fac[b][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
@@ -449,11 +455,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
             for (int b = 0; b < NB; ++b) {
               mma_f16(s[b][t], x[0], y[0], x[1], y[1], qf[b][2 * i][0], qf[b][2 * i][1]);
               mma_f16(s[b][t], x[2], y[2], x[3], y[3], qf[b][2 * i + 1][0], qf[b][2 * i + 1][1]);
+              if constexpr (WIDE) {
+                mma_f16(s[b][t], x[0], y[0], x[1], y[1], ql[b][2 * i][0], ql[b][2 * i][1]);
+                mma_f16(s[b][t], x[2], y[2], x[3], y[3], ql[b][2 * i + 1][0], ql[b][2 * i + 1][1]);
+              }
             }
           }
       }
       // ---- mask and softmax
-      uint32_t pt[NB][2][2];
+      uint32_t pt[NB][2][2], pl[WIDE ? NB : 1][2][2];
       const bool cut = p0 + kChunk > all_seen || lost != 0;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
@@ -495,8 +505,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
             p[e] = tca::exp2a(fmaf(s[b][t][e], fac[b][e & 1], -ref[e & 1]));
             l[b][e & 1] += p[e];
           }
-          pt[b][t][0] = tca::movt(h2(__floats2half2_rn(p[0], p[1])));
-          pt[b][t][1] = tca::movt(h2(__floats2half2_rn(p[2], p[3])));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const Halves<WIDE> y(p[2 * e], p[2 * e + 1]);
+            pt[b][t][e] = tca::movt(y.hi);
+            if constexpr (WIDE) pl[b][t][e] = tca::movt(y.lo);
+          }
         }
       }
       // ---- O^T: this lane's four positions of each 16, channels lg * HD / 8 on
@@ -557,8 +571,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB>()) kv4_decode_kernel
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b) {
               mma_f16(o[b][4 * x + j], a[0][j], a[1][j], a[2][j], a[3][j], pt[b][t][0], pt[b][t][1]);
+              if constexpr (WIDE) mma_f16(o[b][4 * x + j], a[0][j], a[1][j], a[2][j], a[3][j], pl[b][t][0], pl[b][t][1]);
+            }
           }
         }
       }
@@ -787,12 +803,17 @@ static int sm_count() {
   return n;
 }
 
-template <int HD, int NB>
-static int launch_decode(const AttnArgs4& A, int grid, cudaStream_t s) {
+template <int HD, int NB, bool WIDE>
+static int launch_decode(const AttnArgs4& A, int64_t most, int sms, cudaStream_t s) {
   constexpr int smem = smem_bytes<HD, NB>();
-  if (cudaFuncSetAttribute(kv4_decode_kernel<HD, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, ctas_per_sm<NB, WIDE>() * sms));
+  if (cudaFuncSetAttribute(kv4_decode_kernel<HD, NB, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
-  return launch_k(kv4_decode_kernel<HD, NB>, grid, kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  return launch_k(kv4_decode_kernel<HD, NB, WIDE>, grid, kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+}
+template <int HD, bool WIDE>
+static int launch_few(const AttnArgs4& A, bool two, int64_t most, int sms, cudaStream_t s) {
+  return two ? launch_decode<HD, 2, WIDE>(A, most, sms, s) : launch_decode<HD, 1, WIDE>(A, most, sms, s);
 }
 
 }  // namespace buddy
@@ -846,10 +867,11 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   const bool two = most_rows > 8;
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
   const int64_t most = (int64_t)a->batch * cache->n_kv_heads * (chunks + kOpen) / kWarps + 1;
-  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, (two ? ctas_per_sm<2>() : ctas_per_sm<1>()) * sms));
+  const bool wide = a->q_dtype == BUDDY_DTYPE_F32 || a->out_dtype == BUDDY_DTYPE_F32;
   cudaStream_t s = (cudaStream_t)stream;
-  const int rc = cache->head_dim == 128 ? (two ? launch_decode<128, 2>(A, grid, s) : launch_decode<128, 1>(A, grid, s))
-                                        : (two ? launch_decode<64, 2>(A, grid, s) : launch_decode<64, 1>(A, grid, s));
+  const int rc = cache->head_dim == 128
+                     ? (wide ? launch_few<128, true>(A, two, most, sms, s) : launch_few<128, false>(A, two, most, sms, s))
+                     : (wide ? launch_few<64, true>(A, two, most, sms, s) : launch_few<64, false>(A, two, most, sms, s));
   if (rc != BUDDY_OK || most_rows <= kFewRows) return rc;
-  return launch_prompt(A, cache->head_dim, sms, (uint8_t*)a->workspace + few_bytes(cache->head_dim), s);
+  return launch_prompt(A, cache->head_dim, wide, sms, (uint8_t*)a->workspace + few_bytes(cache->head_dim), s);
 }

@@ -42,13 +42,33 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs4& A, int i, bool* bad) {
 // positions with 2^-23.4 of it each came out a third too small.)
 constexpr float kHigh = 7.f;
 
-// For query rows that enter the products as halves of 1 .. 2: the power of two that takes
-// the row's largest magnitude there, and the factor that takes a score of the halves to
-// base 2 (base: log2(e) times the scores' scale; above zero, so that it takes -inf to -inf).
+// Numbers of the products.  A product takes halves, eleven bits of a query's element or of a
+// probability, which is what bf16 queries have and bf16 outputs can hold.  Where the queries or
+// the outputs are fp32 (WIDE), each is the sum of two halves, the second one what the first
+// leaves: 22 bits, for twice as many MMAs.
+template <bool WIDE>
+struct Halves {
+  uint32_t hi, lo;
+  __device__ __forceinline__ Halves(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    if constexpr (WIDE) {
+      const __half2 l = __floats2half2_rn(a - __low2float(h), b - __high2float(h));
+      lo = *reinterpret_cast<const uint32_t*>(&l);
+    }
+  }
+};
+
+// For query rows that enter the products as halves of 1 .. 2 (WIDE: 2^14 .. 2^15, so that the
+// second halves are not among the smallest): the power of two that takes the row's largest
+// magnitude there, and the factor that takes a score of the halves to base 2 (base: log2(e)
+// times the scores' scale; above zero, so that it takes -inf to -inf).
+template <bool WIDE>
 __device__ __forceinline__ void row_scale(float top, float base, float* down, float* fac) {
-  const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
-  *down = __uint_as_float((uint32_t)(127 - ex) << 23);
-  *fac = fmaxf(base * __uint_as_float((uint32_t)(127 + ex) << 23), 1.2e-38f);
+  constexpr int UP = WIDE ? 14 : 0;
+  const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, UP - 126), 126);
+  *down = __uint_as_float((uint32_t)(127 + UP - ex) << 23);
+  *fac = fmaxf(base * __uint_as_float((uint32_t)(127 - UP + ex) << 23), 1.2e-38f);
 }
 
 __device__ __forceinline__ uint32_t h2(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
@@ -80,7 +100,7 @@ __device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uin
 
 // Sequences of more than row_limit rows per KV head (kv4_pf.cu).
 int64_t prompt_workspace(int head_dim, int sms);
-int launch_prompt(AttnArgs4 A, int head_dim, int sms, void* ws, cudaStream_t s);
+int launch_prompt(AttnArgs4 A, int head_dim, bool wide, int sms, void* ws, cudaStream_t s);
 
 }  // namespace kv4
 }  // namespace buddy

@@ -14,6 +14,9 @@
 // thread, in registers while the tile before is worked on) and write them
 // as halves into the 128-byte-swizzled layout, two buffers each for keys and values.
 // Positions past the end and pages that are not there become zeros and are masked.
+// With fp32 queries or outputs (WIDE) queries and P are sums of two halves: an item is one tile
+// of 128 rows, whose second halves take the second tile's place (eight pieces of 1,024 tokens
+// behind 3,072 positions, 32 heads over 8: 1,090 us instead of 395).
 //
 // Work: the items' tiles end to end, each item with kPfOpen tiles' worth for its
 // beginning and end, in equal shares for one CTA per SM.  What an item that is cut
@@ -72,42 +75,46 @@ struct PfItem {
   int64_t start;                  // where the item's first tile is
   int go;                         // 0: the share's end, no item
 
-  __device__ __forceinline__ int tiles() const { return R - row0 > kPfRows ? 2 : 1; }   // tiles of rows
+  template <int IR>
+  __device__ __forceinline__ int tiles() const { return IR > kPfRows && R - row0 > kPfRows ? 2 : 1; }   // tiles of rows
   __device__ __forceinline__ int len() const { return j1 - j0; }
 };
 
+template <int IR>
 __device__ __forceinline__ int pf_tiles(int n, int m, int G, int R, int qp) {
-  const int last = min(R, (qp + 1) * 2 * kPfRows) - 1;
+  const int last = min(R, (qp + 1) * IR) - 1;
   return max(1, (max(n - m + last / G + 1, 0) + kPfKeys - 1) / kPfKeys);
 }
 // Cost of one KV head of a sequence (whole warp).
+template <int IR>
 __device__ __forceinline__ int64_t pf_head_cost(int n, int m, int G, int R, int lane) {
-  const int nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+  const int nqp = (R + IR - 1) / IR;
   int64_t c = 0;
 #pragma unroll 1
-  for (int qp = lane; qp < nqp; qp += 32) c += pf_tiles(n, m, G, R, qp) + kPfOpen;
+  for (int qp = lane; qp < nqp; qp += 32) c += pf_tiles<IR>(n, m, G, R, qp) + kPfOpen;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
   return c;
 }
 // Cost of a KV head of sequence i0 + lane (0: not this kernel's, or not below end): a lane for
 // itself where there are few items, the whole warp for the longer ones.
+template <int IR>
 __device__ __forceinline__ int64_t pf_block_costs(const AttnArgs4& A, int i0, int end, int lane, Rows* q) {
   *q = {0, 0, 0};
   bool bad;
   if (i0 + lane < end) *q = rows_of(A, i0 + lane, &bad);
-  const int R = q->m * A.G, nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+  const int R = q->m * A.G, nqp = (R + IR - 1) / IR;
   int64_t c = 0;
   if (R > A.row_limit && nqp <= 4)
 #pragma unroll 1
-    for (int qp = 0; qp < nqp; ++qp) c += pf_tiles(q->n, q->m, A.G, R, qp) + kPfOpen;
+    for (int qp = 0; qp < nqp; ++qp) c += pf_tiles<IR>(q->n, q->m, A.G, R, qp) + kPfOpen;
   uint32_t longer = __ballot_sync(0xffffffffu, R > A.row_limit && nqp > 4);
 #pragma unroll 1
   while (longer) {
     const int x = __ffs(longer) - 1;
     longer &= longer - 1;
     const int m = __shfl_sync(0xffffffffu, q->m, x);
-    const int64_t v = pf_head_cost(__shfl_sync(0xffffffffu, q->n, x), m, A.G, m * A.G, lane);
+    const int64_t v = pf_head_cost<IR>(__shfl_sync(0xffffffffu, q->n, x), m, A.G, m * A.G, lane);
     if (lane == x) c = v;
   }
   return c;
@@ -132,6 +139,7 @@ __device__ __forceinline__ int pf_next_seq(const AttnArgs4& A, int i, int end, i
 }
 
 // The walk over a CTA's items, by one warp.
+template <int IR>
 struct PfWalk {
   Rows q;
   int i, g, qp, nt, j0, j1;
@@ -140,14 +148,14 @@ struct PfWalk {
     start += nt + kPfOpen;
     rem -= kPfOpen;
     if (rem <= 0) return false;
-    if (++qp * 2 * kPfRows >= q.m * A.G) {
+    if (++qp * IR >= q.m * A.G) {
       qp = 0;
       if (++g == A.p.nkv) {
         g = 0;
         i = pf_next_seq(A, i + 1, A.a.batch, lane, &q);   // (with some of the share left there is another)
       }
     }
-    nt = pf_tiles(q.n, q.m, A.G, q.m * A.G, qp);
+    nt = pf_tiles<IR>(q.n, q.m, A.G, q.m * A.G, qp);
     j0 = 0;
     j1 = nt <= kPfWhole ? nt : (int)min((int64_t)nt, rem);
     rem -= j1;
@@ -178,11 +186,14 @@ __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.al
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-template <int HD>
+template <int HD, bool WIDE>
 __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArgs4 A, CutItem* cuts) {
   extern __shared__ uint8_t smem_raw[];
   constexpr uint32_t TILE = (HD / 64) * kPfRegion;      // bytes of a 128-row tile
   constexpr int GR = HD / kGroup;                       // scale groups of a head
+  // Rows of an item.  WIDE: one tile, the second buffer of queries holds their second halves, and
+  // the second halves of P lie behind the first ones over S's columns.
+  constexpr int IR = WIDE ? kPfRows : 2 * kPfRows;
   // TMEM columns: S of tile q at 128 q (P over their first half), O of tile q at 256 + 128 q
   constexpr uint32_t kO = 256;
   __shared__ __align__(8) uint64_t q_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2];
@@ -210,7 +221,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   if (warp < kPfSoftWarps) {
     Rows q;
 #pragma unroll 1
-    for (int i0 = b0; i0 < b1; i0 += 32) mine += pf_block_costs(A, i0, b1, lane, &q);
+    for (int i0 = b0; i0 < b1; i0 += 32) mine += pf_block_costs<IR>(A, i0, b1, lane, &q);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     mine *= A.p.nkv;
@@ -249,11 +260,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   }
   if (warp < kPfSoftWarps && before <= lo && lo < before + mine) {
     // the sequence, its head, the item of it and the tile where the share begins
-    PfWalk w;
+    PfWalk<IR> w;
     int64_t at = before, cost = 0;
 #pragma unroll 1
     for (int i0 = b0;; i0 += 32) {
-      const int64_t c = pf_block_costs(A, i0, b1, lane, &w.q);
+      const int64_t c = pf_block_costs<IR>(A, i0, b1, lane, &w.q);
       int64_t upto = c * A.p.nkv;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -274,10 +285,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     w.g = 0;
 #pragma unroll 1
     for (; lo >= at + cost; at += cost) ++w.g;
-    const int R = w.q.m * G, nqp = (R + 2 * kPfRows - 1) / (2 * kPfRows);
+    const int R = w.q.m * G, nqp = (R + IR - 1) / IR;
 #pragma unroll 1
     for (int q0 = 0;; q0 += 32) {
-      const int64_t c = q0 + lane < nqp ? pf_tiles(w.q.n, w.q.m, G, R, q0 + lane) + kPfOpen : 0;
+      const int64_t c = q0 + lane < nqp ? pf_tiles<IR>(w.q.n, w.q.m, G, R, q0 + lane) + kPfOpen : 0;
       int64_t upto = c;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -294,7 +305,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       at += __shfl_sync(0xffffffffu, upto, 31);
     }
     if (lane == 0)
-      s_first = {w.i, w.q.t0, w.q.m, w.q.n, w.g, R, w.qp * 2 * kPfRows, pf_tiles(w.q.n, w.q.m, G, R, w.qp), 0, 0,
+      s_first = {w.i, w.q.t0, w.q.m, w.q.n, w.g, R, w.qp * IR, pf_tiles<IR>(w.q.n, w.q.m, G, R, w.qp), 0, 0,
                  at + kPfOpen, 1};
   }
   if (warp == kMmaWarp) {
@@ -319,7 +330,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     return s_item[i & 1].go != 0;
   };
   auto give = [&]() {              // (whole warp)
-    const int len = s_item[I & 1].len(), two = s_item[I & 1].tiles() - 1;
+    const int len = s_item[I & 1].len(), two = s_item[I & 1].template tiles<IR>() - 1;
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(&item_empty[I & 1]);
     T += len, ++I;
@@ -337,7 +348,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       return (x.t0 + t) * stride + (int64_t)(x.g * G + rr - t * G) * HD;
     };
     auto fetch_q = [&](const PfItem& x) {               // an item's queries into L2
-      if (q >= x.tiles()) return;
+      if (q >= x.template tiles<IR>()) return;
       const int esz = A.a.q_dtype == BUDDY_DTYPE_F32 ? 4 : 2;
       const uint8_t* src = (const uint8_t*)A.a.q + row_at(x, A.a.q_stride) * esz;
       for (int i = 0; i < HD * esz; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + i));
@@ -352,14 +363,36 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       const int64_t at = row_at(x, A.a.q_stride);
       auto from = [&](int u) { return __shfl_sync(0xffffffffu, (long long)at, u * RPL + lane / LPR) + l8 * 8; };
       auto put = [&](int u, const float* v) {
-        uint32_t h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = h2(__floats2half2_rn(v[2 * e], v[2 * e + 1]));
-        *reinterpret_cast<uint4*>(qdst + pf_piece((warp & 3) * 32 + u * RPL + lane / LPR, l8)) = make_uint4(h[0], h[1], h[2], h[3]);
+        const Halves<WIDE> a(v[0], v[1]), b(v[2], v[3]), c(v[4], v[5]), d(v[6], v[7]);
+        uint8_t* const dst = qdst + pf_piece((warp & 3) * 32 + u * RPL + lane / LPR, l8);
+        *reinterpret_cast<uint4*>(dst) = make_uint4(a.hi, b.hi, c.hi, d.hi);
+        if constexpr (WIDE) *reinterpret_cast<uint4*>(dst + TILE) = make_uint4(a.lo, b.lo, c.lo, d.lo);
       };
-      const bool wide = A.a.q_dtype == BUDDY_DTYPE_F32;
-      float top = 0.f;
-      if (!wide) {
+      const bool f32 = A.a.q_dtype == BUDDY_DTYPE_F32;
+      float fac = fmaxf(base, 1.2e-38f), top = 0.f;
+      // row by row, scaled by a power of two each
+      auto scaled = [&](int u) {
+        float v[8], row_top = 0.f, down, f;
+        const int64_t src = from(u);
+        if (f32) load8((const float*)A.a.q + src, v);
+        else load8((const bf16*)A.a.q + src, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) row_top = fmaxf(row_top, fabsf(v[e]));
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) row_top = fmaxf(row_top, __shfl_xor_sync(0xffffffffu, row_top, o));
+        row_scale<WIDE>(row_top, base, &down, &f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= down;
+        put(u, v);
+        // to the lane of the row
+        const float mine = __shfl_sync(0xffffffffu, f, (lane % RPL) * LPR);
+        if (lane / RPL == u) fac = mine;
+      };
+      if constexpr (WIDE) {
+#pragma unroll 2
+        for (int u = 0; u < 32 / RPL; ++u) scaled(u);
+      } else {
+      if (!f32) {
         const bf16* src = (const bf16*)A.a.q;
         uint4 raw[32 / RPL];                            // all of them in flight
 #pragma unroll
@@ -386,26 +419,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           put(u, v);
         }
       }
-      float fac = fmaxf(base, 1.2e-38f);
       if (__any_sync(0xffffffffu, top > 32768.f)) {
 #pragma unroll 1
-        for (int u = 0; u < 32 / RPL; ++u) {
-          float v[8], row_top = 0.f, down, f;
-          const int64_t src = from(u);
-          if (wide) load8((const float*)A.a.q + src, v);
-          else load8((const bf16*)A.a.q + src, v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) row_top = fmaxf(row_top, fabsf(v[e]));
-#pragma unroll
-          for (int o = LPR / 2; o > 0; o >>= 1) row_top = fmaxf(row_top, __shfl_xor_sync(0xffffffffu, row_top, o));
-          row_scale(row_top, base, &down, &f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= down;
-          put(u, v);
-          // to the lane of the row
-          const float mine = __shfl_sync(0xffffffffu, f, (lane % RPL) * LPR);
-          if (lane / RPL == u) fac = mine;
-        }
+        for (int u = 0; u < 32 / RPL; ++u) scaled(u);
+      }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       ptx::mbar_arrive(&q_ready[q]);
@@ -416,7 +433,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       const PfItem& it = s_item[I & 1];
       const int len = it.len();
       bool ok = true;
-      if (q >= it.tiles()) {
+      if (q >= it.template tiles<IR>()) {
         go = take(I + 1);
         if (go) fetch_q(s_item[(I + 1) & 1]);
       } else {
@@ -481,7 +498,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           uint64_t ls[2] = {0, 0};
 #pragma unroll
           for (int c = 0; c < kPfKeys; c += 32) {
-            uint32_t p[16];
+            uint32_t p[16], pl[WIDE ? 16 : 1];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               float p0, p1;
@@ -489,9 +506,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
               p0 = tca::exp2a(p0);
               p1 = tca::exp2a(p1);
               ls[i & 1] = add2(ls[i & 1], pair(p0, p1));
-              p[i] = h2(__floats2half2_rn(p0, p1));
+              const Halves<WIDE> y(p0, p1);
+              p[i] = y.hi;
+              if constexpr (WIDE) pl[i] = y.lo;
             }
             ptx::tmem_st16(ts + c / 2, p);
+            if constexpr (WIDE) ptx::tmem_st16(ts + kPfKeys / 2 + c / 2, pl);
             if (c == kPfKeys / 2 - 32 || c == kPfKeys - 32) {
               ptx::tmem_wait_st();
               ptx::tc_fence_before();
@@ -561,7 +581,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
   } else if (warp == kMmaWarp) {
     // -------------------------------------------------------------------- MMA
     while (take(I)) {
-      const int nq = s_item[I & 1].tiles(), len = s_item[I & 1].len();
+      const int nq = s_item[I & 1].template tiles<IR>(), len = s_item[I & 1].len();
       bool ok = true;
       if (ptx::elect_one()) {
         const uint32_t id_s = (1u << 4) | ((uint32_t)(kPfKeys >> 3) << 17) | (8u << 24);   // half in, fp32 out, M 128
@@ -575,19 +595,24 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         auto qk = [&](int q, uint32_t tile) {           // S_q = Q_q K^T
           const uint64_t a = dQ + (uint64_t)q * (TILE >> 4), b = dK + (uint64_t)(tile & 1) * (TILE >> 4);
 #pragma unroll
-          for (int k = 0; k < HD / 16; ++k) {
-            const uint64_t off = (k >> 2) * (kPfRegion >> 4) + 2 * (k & 3);
-            ptx::mma_bf16(tmem + (uint32_t)q * 128u, a + off, b + off, id_s, k > 0 ? 1u : 0u);
-          }
+          for (int x = 0; x < (WIDE ? 2 : 1); ++x)
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k) {
+              const uint64_t off = (k >> 2) * (kPfRegion >> 4) + 2 * (k & 3);
+              ptx::mma_bf16(tmem + (uint32_t)q * 128u, a + x * (TILE >> 4) + off, b + off, id_s, x + k > 0 ? 1u : 0u);
+            }
           ptx::mma_commit(&s_full[q]);
         };
         auto pv = [&](int q, uint32_t tile, int half, bool first) {   // O_q += P_q V, 64 positions
           const uint64_t v = dV + (uint64_t)(tile & 1) * (TILE >> 4) + half * (kPfKeys / 32) * (2048 >> 4);
           const uint32_t p = tmem + (uint32_t)q * 128u + 8u * half * (kPfKeys / 32);
 #pragma unroll
-          for (int x = 0; x < kPfKeys / 32; ++x)        // 16 positions: two 1 KiB groups
+          for (int x = 0; x < kPfKeys / 32; ++x) {      // 16 positions: two 1 KiB groups
             ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, p + 8u * x, v + x * (2048 >> 4), id_o,
                              (!first || x > 0) ? 1u : 0u);
+            if constexpr (WIDE)
+              ptx::mma_bf16_ts(tmem + kO + (uint32_t)q * 128u, p + kPfKeys / 2 + 8u * x, v + x * (2048 >> 4), id_o, 1u);
+          }
         };
         ok = wait(&k_full[T & 1], T >> 1);
         for (int q = 0; q < nq && ok; ++q) {
@@ -625,9 +650,9 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     }
   } else if (warp == kMmaWarp + 1) {
     // ------------------------------------------------- the walk over the items
-    PfWalk walk{};
+    PfWalk<IR> walk{};
     walk.q = {s_first.t0, s_first.m, s_first.n};
-    walk.i = s_first.seq, walk.g = s_first.g, walk.qp = s_first.row0 / (2 * kPfRows), walk.nt = s_first.nt;
+    walk.i = s_first.seq, walk.g = s_first.g, walk.qp = s_first.row0 / IR, walk.nt = s_first.nt;
     walk.start = s_first.start;
     const int64_t x = lo - walk.start;                  // tile of the item; below 0: its opening
     walk.rem = min(share, total - lo) + min(x, (int64_t)0);
@@ -649,12 +674,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       if (lane < GR) s_nan[i & 1][lane] = INT32_MAX;
       __syncwarp();
       if (lane == 0) {
-        s_item[i & 1] = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * 2 * kPfRows, walk.nt,
+        s_item[i & 1] = {walk.i, walk.q.t0, walk.q.m, walk.q.n, walk.g, walk.q.m * G, walk.qp * IR, walk.nt,
                          walk.j0, walk.j1, walk.start, go};
         if (go && walk.j0 == 0 && walk.j1 < walk.nt) {
           CutItem* c = cuts + blockIdx.x;
-          c->t0 = walk.q.t0, c->g = walk.g, c->row0 = walk.qp * 2 * kPfRows;
-          c->rows = min(walk.q.m * G - c->row0, 2 * kPfRows);
+          c->t0 = walk.q.t0, c->g = walk.g, c->row0 = walk.qp * IR;
+          c->rows = min(walk.q.m * G - c->row0, IR);
           c->spans = (int)((walk.start + walk.nt - 1) / share - blockIdx.x) + 1;
         }
         ptx::mbar_arrive(&item_full[i & 1]);
@@ -669,7 +694,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     while (take(I)) {
       const PfItem it = s_item[I & 1];
       const int len = it.len();
-      const int last = min(it.R, it.row0 + 2 * kPfRows) - 1;
+      const int last = min(it.R, it.row0 + IR) - 1;
       const int end = min(it.n, max(it.n - it.m + last / G + 1, 0));                  // positions that any row sees
       const int in_page = (1 << A.p.shift) - 1;
       const int32_t* table = A.a.table + (int64_t)it.seq * A.a.max_pages;
@@ -827,27 +852,28 @@ int64_t prompt_workspace(int head_dim, int sms) {
   return (int64_t)sms * (sizeof(CutItem) + 2 * (head_dim == 128 ? pf_part_floats<128>() : pf_part_floats<64>()) * 4);
 }
 
-template <int HD>
+template <int HD, bool WIDE>
 static int launch_prompt_hd(const AttnArgs4& A, CutItem* cuts, int sms, cudaStream_t s) {
   // (built with fewer registers, the roles would wait for ever for theirs)
   cudaFuncAttributes at;
-  if (cudaFuncGetAttributes(&at, kv4_prompt_kernel<HD>) != cudaSuccess || at.numRegs != kPfRegs ||
-      cudaFuncSetAttribute(kv4_prompt_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pf_smem<HD>()) !=
+  if (cudaFuncGetAttributes(&at, kv4_prompt_kernel<HD, WIDE>) != cudaSuccess || at.numRegs != kPfRegs ||
+      cudaFuncSetAttribute(kv4_prompt_kernel<HD, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pf_smem<HD>()) !=
           cudaSuccess)
     return BUDDY_ERR_CUDA;
   // the prompts start on the SMs that the few-row kernel leaves free, the join is launched
   // as the prompts end
-  if (launch_k(kv4_prompt_kernel<HD>, sms, kPfThreads, pf_smem<HD>(), s, true, A, cuts) != cudaSuccess ||
+  if (launch_k(kv4_prompt_kernel<HD, WIDE>, sms, kPfThreads, pf_smem<HD>(), s, true, A, cuts) != cudaSuccess ||
       launch_k(kv4_join_kernel<HD>, dim3(sms, HD / kJoinChannels), 2 * kPfRows, 0, s, true, A, (const CutItem*)cuts) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   return BUDDY_OK;
 }
 
 // ws: prompt_workspace() bytes.
-int launch_prompt(AttnArgs4 A, int head_dim, int sms, void* ws, cudaStream_t s) {
+int launch_prompt(AttnArgs4 A, int head_dim, bool wide, int sms, void* ws, cudaStream_t s) {
   CutItem* cuts = (CutItem*)ws;
   A.part = (float*)((uint8_t*)ws + sms * sizeof(CutItem));
-  return head_dim == 128 ? launch_prompt_hd<128>(A, cuts, sms, s) : launch_prompt_hd<64>(A, cuts, sms, s);
+  if (wide) return head_dim == 128 ? launch_prompt_hd<128, true>(A, cuts, sms, s) : launch_prompt_hd<64, true>(A, cuts, sms, s);
+  return head_dim == 128 ? launch_prompt_hd<128, false>(A, cuts, sms, s) : launch_prompt_hd<64, false>(A, cuts, sms, s);
 }
 
 }  // namespace kv4
