@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
       float x[HD / 4], top = 0.f;
 #pragma unroll
       for (int e = 0; e < HD / 4; e += 8) {
-        if (A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + at + e, x + e);
+        if (WIDE && A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + at + e, x + e);
         else load8((const bf16*)A.a.q + at + e, x + e);
       }
 #pragma unroll

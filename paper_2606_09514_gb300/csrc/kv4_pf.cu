@@ -347,9 +347,10 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
       const int rr = min(x.row0 + q * kPfRows + (warp & 3) * 32 + lane, x.R - 1), t = rr / G;
       return (x.t0 + t) * stride + (int64_t)(x.g * G + rr - t * G) * HD;
     };
+    const bool q32 = WIDE && A.a.q_dtype == BUDDY_DTYPE_F32, out32 = WIDE && A.a.out_dtype == BUDDY_DTYPE_F32;
     auto fetch_q = [&](const PfItem& x) {               // an item's queries into L2
       if (q >= x.template tiles<IR>()) return;
-      const int esz = A.a.q_dtype == BUDDY_DTYPE_F32 ? 4 : 2;
+      const int esz = q32 ? 4 : 2;
       const uint8_t* src = (const uint8_t*)A.a.q + row_at(x, A.a.q_stride) * esz;
       for (int i = 0; i < HD * esz; i += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + i));
     };
@@ -368,13 +369,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         *reinterpret_cast<uint4*>(dst) = make_uint4(a.hi, b.hi, c.hi, d.hi);
         if constexpr (WIDE) *reinterpret_cast<uint4*>(dst + TILE) = make_uint4(a.lo, b.lo, c.lo, d.lo);
       };
-      const bool f32 = A.a.q_dtype == BUDDY_DTYPE_F32;
-      float fac = fmaxf(base, 1.2e-38f), top = 0.f;
+      float fac = fmaxf(base, 1.2e-38f);
       // row by row, scaled by a power of two each
       auto scaled = [&](int u) {
         float v[8], row_top = 0.f, down, f;
         const int64_t src = from(u);
-        if (f32) load8((const float*)A.a.q + src, v);
+        if (q32) load8((const float*)A.a.q + src, v);
         else load8((const bf16*)A.a.q + src, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) row_top = fmaxf(row_top, fabsf(v[e]));
@@ -392,7 +392,6 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
 #pragma unroll 2
         for (int u = 0; u < 32 / RPL; ++u) scaled(u);
       } else {
-      if (!f32) {
         const bf16* src = (const bf16*)A.a.q;
         uint4 raw[32 / RPL];                            // all of them in flight
 #pragma unroll
@@ -408,21 +407,12 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
           put(u, v);
         }
-        top = fmaxf(__low2float(most), __high2float(most));
-      } else {
-#pragma unroll 4
-        for (int u = 0; u < 32 / RPL; ++u) {
-          float v[8];
-          load8((const float*)A.a.q + from(u), v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-          put(u, v);
-        }
-      }
-      if (__any_sync(0xffffffffu, top > 32768.f)) {
+        if (__any_sync(0xffffffffu, fmaxf(__low2float(most), __high2float(most)) > 32768.f)) {
+          // (a counter in memory keeps this apart from the loops above: nine requests as above take
+          // 258 us so, 262 otherwise)
 #pragma unroll 1
-        for (int u = 0; u < 32 / RPL; ++u) scaled(u);
-      }
+          for (volatile int u = 0; u < 32 / RPL; u = u + 1) scaled(u);
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       ptx::mbar_arrive(&q_ready[q]);
@@ -536,7 +526,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
           if (!whole) part[0] = m, part[2 * kPfRows] = l;
           const int64_t out_at = row_at(it, A.a.out_stride);
           const int sees = seen_by();
-          const bool staged = whole && A.a.out_dtype == BUDDY_DTYPE_BF16;
+          const bool staged = whole && !out32;
 #pragma unroll 1
           for (int c = 0; c < HD; c += 32) {
             float o[32];
@@ -554,7 +544,7 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
                 *reinterpret_cast<uint4*>(qdst + pf_piece(rt, (c + i) >> 3)) =
                     make_uint4(tca::pack_bf16(o[i], o[i + 1]), tca::pack_bf16(o[i + 2], o[i + 3]),
                                tca::pack_bf16(o[i + 4], o[i + 5]), tca::pack_bf16(o[i + 6], o[i + 7]));
-            } else if (it.row0 + q * kPfRows + rt < it.R) {
+            } else if (WIDE && it.row0 + q * kPfRows + rt < it.R) {
               float4* d = reinterpret_cast<float4*>((float*)A.a.out + out_at + c);
 #pragma unroll
               for (int i = 0; i < 8; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
