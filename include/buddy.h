@@ -514,9 +514,9 @@ BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int6
  * a token without any position (kv_len[i] = 0, or more query tokens than
  * positions) gets zeros.  Rows of q behind row_start[batch] are not written.
  * Query elements enter the products as halves, scaled by a power of two per row
- * where that is needed: 11 significant bits (a bf16 element whole), fewer below
- * 2^-14 or 2^-14 of the row's largest element, whichever is larger (rounded at
- * 2^-25 or 2^-25 of it).  Probabilities enter with 11 bits, below 2^-21 of the
+ * where that is needed: 11 significant bits (a bf16 element whole), fewer for the
+ * smallest of a row, which are rounded at 2^-25 of its largest element, or at 2^-25
+ * where that is in 2^-14 .. 2^15.  Probabilities enter with 11 bits, below 2^-21 of the
  * row's largest rounded at 2^-32 of that; keys and values exactly; sums and
  * statistics are fp32.  With fp32 queries or fp32 outputs both enter as the sum of
  * two halves, with 22 bits (queries rounded at 2^-39 of the row's largest element

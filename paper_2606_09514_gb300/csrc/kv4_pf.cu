@@ -357,8 +357,8 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     uint8_t* const qdst = sQ + (size_t)q * TILE;
     const float base = (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f;
     // The queries of this warp's 32 rows as halves; returns the factor of this lane's row's
-    // scores.  Rows with elements above 2^15 (and those next to them) are taken once more,
-    // scaled by a power of two each.
+    // scores.  Where a row has elements above 2^15, or none of 2^-14, the warp's rows are taken
+    // once more, scaled by a power of two each.
     auto put_q = [&](const PfItem& x) {
       const int l8 = lane % LPR;
       const int64_t at = row_at(x, A.a.q_stride);
@@ -396,18 +396,27 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
         uint4 raw[32 / RPL];                            // all of them in flight
 #pragma unroll
         for (int u = 0; u < 32 / RPL; ++u) raw[u] = __ldg(reinterpret_cast<const uint4*>(src + from(u)));
-        auto b2 = [](uint32_t w) { return __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w)); };
-        __nv_bfloat162 most = __float2bfloat162_rn(0.f);
+        // magnitudes as integers, which order alike: the largest of all, and by rows whether any is
+        // above zero, and any 2^-14 or more
+        uint32_t top = 0, some = 0, enough = 0;
 #pragma unroll
         for (int u = 0; u < 32 / RPL; ++u) {
-          most = __hmax2(most, __hmax2(__hmax2(b2(raw[u].x), b2(raw[u].y)), __hmax2(b2(raw[u].z), b2(raw[u].w))));
           const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+          uint32_t m2 = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m2 = __vmaxu2(m2, w[e] & 0x7FFF7FFFu);
+          const uint32_t most = max(m2 >> 16, m2 & 0xFFFFu);
+          top = max(top, most);
+          some |= (most != 0 ? 1u : 0u) << u;
+          enough |= (most >= 0x3880u ? 1u : 0u) << u;    // 2^-14
           float v[8];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[2 * e] = __uint_as_float(w[e] << 16), v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
           put(u, v);
         }
-        if (__any_sync(0xffffffffu, fmaxf(__low2float(most), __high2float(most)) > 32768.f)) {
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) some |= __shfl_xor_sync(0xffffffffu, some, o), enough |= __shfl_xor_sync(0xffffffffu, enough, o);
+        if (__any_sync(0xffffffffu, top > 0x4700u || some != enough)) {   // (above 2^15)
           // (a counter in memory keeps this apart from the loops above: nine requests as above take
           // 258 us so, 262 otherwise)
 #pragma unroll 1

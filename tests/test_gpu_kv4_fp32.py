@@ -64,3 +64,35 @@ def test_attention_in_fp32_of_large_and_small_queries(up, m):
 def test_attention_in_fp32_behind_a_long_prefix(m):
     check((8, 2, 128), 64, [20011, 300], [m, m], F, F)
     check((4, 4, 64), 64, [16384], [m], F, F)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 40, 2.0 ** -12, 2.0 ** -20, 2.0 ** -40, 2.0 ** -110])
+@pytest.mark.parametrize("m", [1, 4, 60])
+def test_attention_in_bf16_of_large_and_small_queries(up, m):
+    """A power of two in all queries, taken back by the scale, changes no bit; in every other head's, it
+    leaves both kinds of rows within what bf16 calls are held to (2^-11 + 2^-12 of the largest value, and the
+    output's rounding of 2^-8).  Rows of zeros and of one element are among them."""
+    lens, n_new = [300, 64, 1000], [m, m, 1]
+    cache, table, vals = make_cache(lens, 16, 2, 64)
+    starts = np.concatenate([[0], np.cumsum(n_new)])
+    g = torch.Generator(device="cuda").manual_seed(m)
+    # two bits per element: whole as halves whatever the row's power of two is
+    q = torch.randint(-3, 4, (starts[-1], 8, 64), generator=g, device="cuda").to(B) / 2
+    q[0, 0], q[-1, 3] = 0.0, 0.0
+    q[-1, 3, 9] = 1.5
+
+    def call(x, scale):
+        out = torch.full_like(q, 77.0)
+        cache.buddy_kv4_attention(x, i32(lens), table, out, i32(starts), m, scale)
+        return out
+
+    assert torch.equal(call((q.float() * up).to(B), 0.125 / up), call(q, 0.125))
+    some = torch.arange(8, device="cuda")[:, None] % 2 == 0
+    x = (q.float() * torch.where(some, up, 1.0)).to(B)
+    for heads, scale in ((slice(0, None, 2), 0.125 / up), (slice(1, None, 2), 0.125)):
+        got = f64(call(x, scale))
+        for i, (n, mi) in enumerate(zip(lens, n_new)):
+            rows = slice(starts[i], starts[i + 1])
+            want = O.attention(f64(q[rows]), *vals[i], mi, 0.125)
+            tol = np.abs(vals[i][1]).max() * (2.0 ** -11 + 2.0 ** -12) + np.abs(want) * 2.0 ** -8
+            assert np.all((np.abs(got[rows] - want) <= tol)[:, heads]), (i, heads)
