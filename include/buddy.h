@@ -533,7 +533,7 @@ typedef struct {
   int32_t q_dtype;            /* BUDDY_DTYPE_F32 or _BF16 */
   int32_t out_dtype;          /* BUDDY_DTYPE_F32 or _BF16 */
   int32_t max_pages;          /* entries of a table row, max_pages * page_size < 2^31 */
-  float scale;                /* of the scores; 0: 1 / sqrt(head_dim) */
+  float scale;                /* of the scores, 0 .. 2.3e38; 0: 1 / sqrt(head_dim) */
   const void* q;              /* device [n_tok, n_q_heads, head_dim], tokens q_stride elements apart */
   void* out;                  /* device, as q with out_stride; must not overlap q */
   int64_t q_stride;           /* rows 16-byte aligned */

@@ -841,7 +841,7 @@ extern "C" int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv
 extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags,
                                    void* stream) {
   if (!kv4_cache_ok(cache) || !a || a->batch < 1 || a->batch > 16384 || a->n_tok < 0 || a->max_pages < 1 ||
-      (int64_t)a->max_pages * cache->page_size > INT32_MAX || !(a->scale >= 0.f) || a->scale > 3e38f)
+      (int64_t)a->max_pages * cache->page_size > INT32_MAX || !(a->scale >= 0.f) || a->scale > 2.3e38f)   // (times log2(e) it is finite)
     return BUDDY_ERR_ARG;
   if (!sizes_ok(a->n_q_heads, cache->n_kv_heads, cache->head_dim, a->max_new) ||
       (a->q_dtype != BUDDY_DTYPE_F32 && a->q_dtype != BUDDY_DTYPE_BF16) ||
