@@ -527,7 +527,7 @@ BUDDY_API int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int6
  * (BUDDY_DEV_BAD_PAGE: the page's positions count as not there). */
 typedef struct {
   int32_t batch;              /* 1 .. 16384 */
-  int32_t n_tok;              /* rows of q and out; n_tok * n_q_heads < 2^31 (else BUDDY_ERR_RANGE) */
+  int32_t n_tok;              /* rows of q and out; n_tok * n_q_heads < 2^31 - 512 (else BUDDY_ERR_RANGE) */
   int32_t max_new;            /* >= 1: most query tokens of one sequence */
   int32_t n_q_heads;          /* a multiple of n_kv_heads, at most 8 times */
   int32_t q_dtype;            /* BUDDY_DTYPE_F32 or _BF16 */

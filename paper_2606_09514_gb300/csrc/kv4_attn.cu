@@ -852,7 +852,8 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
       (reinterpret_cast<uintptr_t>(a->workspace) & 255))
     return BUDDY_ERR_ARG;
   if (a->n_tok == 0) return BUDDY_OK;
-  if ((int64_t)a->n_tok * a->n_q_heads > INT32_MAX) return BUDDY_ERR_RANGE;   // rows are counted in 32 bits
+  // rows are counted in 32 bits, up to the end of their last tile
+  if ((int64_t)a->n_tok * a->n_q_heads >= (int64_t)INT32_MAX - 511) return BUDDY_ERR_RANGE;
   if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->out) ||
       a->q_stride * (a->q_dtype == BUDDY_DTYPE_F32 ? 4 : 2) % 16 || a->out_stride * (a->out_dtype == BUDDY_DTYPE_F32 ? 4 : 2) % 16)
     return BUDDY_ERR_ARG;
