@@ -23,7 +23,7 @@
 // into the softmax's factor.  Probabilities are rounded to half for the product only (their sum is taken
 // before): each by 2^-11 of it at most, or 2^-32 of the row's largest where that is more.  With fp32
 // queries or outputs (WIDE) both are sums of two halves: twice the MMAs and a CTA less per SM
-// (64 sequences of 8,192 positions 154 us instead of 126; errors of 2^-12 become 2^-20).
+// (64 sequences of 8,192 positions 148 us instead of 121; errors of 2^-12 become 2^-21).
 //
 // Work: all streams end to end, each as its chunks of 32 positions and kOpen chunks'
 // worth for its beginning and end, in equal shares per CTA.  (With kOpen 4, 8, 10 and 12:
@@ -41,10 +41,10 @@
 // where they are many, by teams first (one sequence of 120,001 positions, 4 KV heads, 152
 // CTAs each: 49 us with one join, 32 with teams).
 //
-// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 120 us,
+// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 121 us,
 // their copies alone 91 us (94% of HBM's rate), the arithmetic alone 100; a chunk is about
 // 700 instructions of a warp, 350 of them codes to halves.  One token over 2,048 positions
-// takes 8.2 us: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
+// takes 9.0 us a call: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
 // for two chunks, 4 for partials, arrival and join.
 #include <cuda_runtime.h>
 

@@ -15,8 +15,8 @@
 // as halves into the 128-byte-swizzled layout, two buffers each for keys and values.
 // Positions past the end and pages that are not there become zeros and are masked.
 // With fp32 queries or outputs (WIDE) queries and P are sums of two halves: an item is one tile
-// of 128 rows, whose second halves take the second tile's place (eight pieces of 1,024 tokens
-// behind 3,072 positions, 32 heads over 8: 1,090 us instead of 395).
+// of 128 rows, whose second halves take the second tile's place (the nine requests below 634 us
+// instead of 257).
 //
 // Work: the items' tiles end to end, each item with kPfOpen tiles' worth for its
 // beginning and end, in equal shares for one CTA per SM.  What an item that is cut
@@ -24,9 +24,11 @@
 // the parts in order.  Every wait is bounded.
 //
 // Nine requests of 1 to 1,500 new tokens behind 300 to 6,000 positions, 32 heads over 8:
-// 255 us, 970 TFLOP/s, the tensor pipe busy for half of the time.  A tile of 256 rows and
-// 128 positions takes about 3,500 cycles; its 32 MMAs of N = 128 take 3,100 of them at the
-// rate at which a thread issues such (97 cycles; two issuing warps were slower).
+// 257 us, 960 TFLOP/s, the tensor pipe busy for half of the time.  A tile of 256 rows and
+// 128 positions takes about 3,500 cycles, 3,100 of them in its 32 MMAs of N = 128, 97 cycles each
+// where the pipe alone would need 64.  What they wait for was not told apart: their issue (two
+// issuing warps were slower), or shared memory, whose whole rate the operands of 64 cycles
+// take, with 64 KB of producers' writes per tile next to them.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -789,7 +791,11 @@ __global__ void __launch_bounds__(kPfThreads, 1) kv4_prompt_kernel(const AttnArg
     ptx::tc_fence_after();
     ptx::tmem_dealloc(tmem, 512);
   }
-  pdl_wait();   // (started next to the few-row kernel: does not end before it)
+  // Started next to the few-row kernel of the call, which lets it start once each of its CTAs has
+  // waited for all work before the call: queries, entries and lengths are there from the
+  // beginning, and the workspace is free.  It does not end before that kernel, so that what
+  // waits for this one has waited for both.
+  pdl_wait();
 }
 
 // The parts of the items that were cut, in order: a thread per row, four channels, eight

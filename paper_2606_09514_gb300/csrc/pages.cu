@@ -4,8 +4,8 @@
 // the running counts of new tokens and new pages in its shared memory, so that no
 // CTA waits for another; then it writes its part of the table entries and slots,
 // each found by bisection in those counts.  The checks come out of the same scan,
-// before anything is written.  Latency only: 250 sequences of a token each 3.3 us a call,
-// 61 prompts of 128 to 1,024 tokens 2.9; two launches, counts first, would cost another
+// before anything is written.  Latency only: 250 sequences of a token each 3.4 us a call,
+// 61 prompts of 128 to 1,024 tokens 3.1; two launches, counts first, would cost another
 // 2 us.
 #include <cuda_runtime.h>
 
@@ -14,7 +14,7 @@
 
 namespace buddy {
 
-// A thread has a token, up to the largest grid.  (61 prompts 2.9 us, with four tokens each 4.5,
+// A thread has a token, up to the largest grid.  (When it was chosen, 61 prompts took 2.9 us, with four tokens each 4.5,
 // with CTAs of 128 threads 3.3; 16,000 sequences 34 us, with CTAs of 1,024 threads 51.)
 constexpr int kPlanThreads = 256;
 constexpr int kPlanMaxBatch = 16384;    // two counts per sequence in shared memory
