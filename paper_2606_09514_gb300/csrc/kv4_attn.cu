@@ -33,8 +33,8 @@
 // the partials cost again.  In a share, four warps take the chunks of a stream in turn or,
 // where there are several short streams, a warp the whole of every fourth, without barriers
 // and joins (250 sequences of 50 to 200 positions, 8 KV heads: 19.0 us, 25.5 with their
-// chunks in turn; 1,000 of 20 to 250: 54 and 76; up to 16 chunks instead of 12 costs 250 of
-// 30 to 1,000 a sixth).  Each warp has its own ring of stages, which runs on across streams:
+// chunks in turn; 1,000 of 20 to 250: 54 and 76; with long streams among them it loses, 250 of
+// 30 to 1,000 take 40 us instead of 37, and a sixth more with up to 16 chunks instead of 12).  Each warp has its own ring of stages, which runs on across streams:
 // one lane copies a chunk in four bulk copies, in whole halves of 16 positions, and what lies behind the sequence's
 // end, or has no page, is masked.  A stream within a share is written out; the CTAs of one
 // that is cut write partials, which are joined in order by the last of them to arrive or,
@@ -863,7 +863,9 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
     return BUDDY_ERR_ARG;
   AttnArgs4 A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, kFewRows, flags, (int32_t*)a->workspace,
               (float*)((uint8_t*)a->workspace + kWsCounters)};
-  // one CTA for every four chunks there can be, as many as run at once at most
+  // The form by the most rows that a sequence may have here: a prompt in the call, too, sends
+  // its single tokens through the form for 16 rows (not measured next to many of them).  One CTA
+  // for every four chunks there can be, as many as run at once at most.
   const int64_t most_rows = (int64_t)a->max_new * A.G;
   const bool two = most_rows > 8;
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
