@@ -34,9 +34,10 @@
 // where there are several short streams, a warp the whole of every fourth, without barriers
 // and joins (250 sequences of 50 to 200 positions, 8 KV heads: 19.0 us, 25.5 with their
 // chunks in turn; 1,000 of 20 to 250: 54 and 76; with long streams among them it loses, 250 of
-// 30 to 1,000 take 40 us instead of 37, and a sixth more with up to 16 chunks instead of 12).  Each warp has its own ring of stages, which runs on across streams:
-// one lane copies a chunk in four bulk copies, in whole halves of 16 positions, and what lies behind the sequence's
-// end, or has no page, is masked.  A stream within a share is written out; the CTAs of one
+// 30 to 1,000 take 40 us instead of 37, and a sixth more with up to 16 chunks instead of 12).
+// Each warp has its own ring of stages, which runs on across streams: one lane copies a
+// chunk in four bulk copies, in whole halves of 16 positions, and what lies behind the
+// sequence's end, or has no page, is masked.  A stream within a share is written out; the CTAs of one
 // that is cut write partials, which are joined in order by the last of them to arrive or,
 // where they are many, by teams first (one sequence of 120,001 positions, 4 KV heads, 152
 // CTAs each: 49 us with one join, 32 with teams).
