@@ -498,6 +498,23 @@ BUDDY_API int buddy_qk_norm_rope(const buddy_qk_rows* rows, int32_t* flags, void
 BUDDY_API int buddy_kv4_append(const buddy_kv4_cache* cache, const buddy_qk_rows* rows, const void* v,
                                int64_t v_stride, const int64_t* slot, int32_t* flags, void* stream);
 
+/* Both with several position axes (time, height and width of a video's patches; text
+ * has the same position on every axis).  Frequency j, the pair of channels j and
+ * j + hd/2, turns by the tables' row of axis axis[j]'s position: row pos[a] for a =
+ * axis[j], where axis a's positions are rows->pos[a * pos_stride + t], t < n_tok.
+ * Everything else is as above; a token that is negative on any axis is left out, one
+ * with a position >= max_pos on any axis too (BUDDY_DEV_BAD_POSITION). */
+typedef struct {
+  int32_t n_axes;        /* 1 .. 4 */
+  uint8_t axis[64];      /* of frequency j < head_dim / 2; each < n_axes */
+  int64_t pos_stride;    /* elements from axis to axis of rows->pos, >= 0 */
+} buddy_rope_axes;
+BUDDY_API int buddy_qk_norm_rope_axes(const buddy_qk_rows* rows, const buddy_rope_axes* axes, int32_t* flags,
+                                      void* stream);
+BUDDY_API int buddy_kv4_append_axes(const buddy_kv4_cache* cache, const buddy_qk_rows* rows,
+                                    const buddy_rope_axes* axes, const void* v, int64_t v_stride,
+                                    const int64_t* slot, int32_t* flags, void* stream);
+
 /* The values that the cache holds at n slots: k_out, v_out device [n,
  * n_kv_heads, head_dim] of dtype BUDDY_DTYPE_F32 or _F16 (both exact) or _BF16
  * (rounded), 16-byte aligned; either may be NULL.  Rows of negative slots are

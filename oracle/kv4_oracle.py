@@ -34,6 +34,17 @@ def norm_rope(x, gain, pos, theta, eps):
     return np.concatenate([lo * np.cos(a) - hi * np.sin(a), hi * np.cos(a) + lo * np.sin(a)], -1)
 
 
+def norm_rope_axes(x, gain, pos, axis, theta, eps):
+    """The same with several position axes: pos [axes, tokens], axis[j] that of frequency j."""
+    out, h = np.empty(np.shape(x)), np.shape(x)[-1] // 2
+    for a, p in enumerate(np.asarray(pos)):
+        turned = norm_rope(x, gain, p, theta, eps)
+        for j in range(h):
+            if axis[j] == a:
+                out[..., [j, j + h]] = turned[..., [j, j + h]]
+    return out
+
+
 def scale_of(amax):
     """The stored scale of a group with this largest magnitude."""
     if np.isnan(amax):

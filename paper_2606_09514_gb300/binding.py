@@ -27,7 +27,8 @@ EXPORTED = ["buddy_create", "buddy_destroy", "buddy_set_weights", "buddy_kv_appe
             "buddy_set_profiling", "buddy_profile_read", "buddy_profile_class_name",
             "buddy_route_noalloc", "buddy_set_budget_predictor", "buddy_get_paths", "buddy_prefill",
             "buddy_set_wait_limit", "buddy_page_plan", "buddy_rope_table", "buddy_qk_norm_rope",
-            "buddy_kv4_append", "buddy_kv4_read", "buddy_kv4_attention", "buddy_kv4_attention_workspace"]
+            "buddy_kv4_append", "buddy_kv4_read", "buddy_kv4_attention", "buddy_kv4_attention_workspace",
+            "buddy_qk_norm_rope_axes", "buddy_kv4_append_axes"]
 PROF_CLASSES = ["check", "rmsnorm", "gemm_qkv", "qkv_finalize", "attention", "gemm_o", "gemm_gate_up",
                 "gemm_down", "route", "compact", "other", "gemm_fixup",
                 "pf_gemm", "pf_attention", "pf_other"]
@@ -85,6 +86,12 @@ class buddy_qk_rows(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_gain", c_p), ("k_gain", c_p),
                 ("pos", c_p), ("rope_cos", c_p), ("rope_sin", c_p), ("q_out", c_p), ("k_out", c_p),
                 ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
+
+
+class RopeAxes(ctypes.Structure):
+    """Which of several position axes turns each frequency of a head (buddy_rope_axes makes
+    one): the C ABI's argument, and the head dimension that it is of."""
+    _fields_ = [("n_axes", c_i32), ("axis", ctypes.c_uint8 * 64), ("pos_stride", ctypes.c_int64), ("head_dim", c_i32)]
 
 
 class buddy_kv4_attention_args(ctypes.Structure):
@@ -158,8 +165,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.buddy_kv4_read.argtypes = [P(buddy_kv4_cache), c_i32, c_p, c_i32, c_p, c_p, c_p, c_p]
     lib.buddy_kv4_attention.argtypes = [P(buddy_kv4_cache), P(buddy_kv4_attention_args), c_p, c_p]
     lib.buddy_kv4_attention_workspace.argtypes = [c_i32, c_i32, c_i32, c_i32]
+    lib.buddy_qk_norm_rope_axes.argtypes = [P(buddy_qk_rows), P(RopeAxes), c_p, c_p]
+    lib.buddy_kv4_append_axes.argtypes = [P(buddy_kv4_cache), P(buddy_qk_rows), P(RopeAxes), c_p, ctypes.c_int64, c_p,
+                                          c_p, c_p]
     for name in ("buddy_page_plan", "buddy_rope_table", "buddy_qk_norm_rope", "buddy_kv4_append", "buddy_kv4_read",
-                 "buddy_kv4_attention"):
+                 "buddy_kv4_attention", "buddy_qk_norm_rope_axes", "buddy_kv4_append_axes"):
         getattr(lib, name).restype = ctypes.c_int
     lib.buddy_kv4_attention_workspace.restype = ctypes.c_int64
     for name in ("buddy_create", "buddy_set_weights", "buddy_kv_append", "buddy_route", "buddy_decode_step",
@@ -171,7 +181,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     except ImportError as e:          # (the rest of the library does without)
         missing = functools.partial(_without_calls, str(e))
         _calls = None
-    for name in ("page_plan", "qk_norm_rope", "kv4_append", "kv4_read", "kv4_attention"):
+    for name in ("page_plan", "qk_norm_rope", "kv4_append", "kv4_read", "kv4_attention", "qk_norm_rope_axes",
+                 "kv4_append_axes"):
         entry = ctypes.cast(getattr(lib, "buddy_" + name), c_p).value
         setattr(lib, "call_" + name, functools.partial(getattr(_calls, name), entry) if _calls else missing)
     lib.call_stream_for_workspace = _calls.stream_for_workspace if _calls else missing
@@ -429,12 +440,41 @@ def buddy_page_plan(length: torch.Tensor, n_new: torch.Tensor, page_size: int, t
                                          slot, pos, free_head_out, flags, stream), "buddy_page_plan")
 
 
+def buddy_rope_axes(head_dim: int, sections: Sequence[int], interleaved: bool = False) -> RopeAxes:
+    """Position axes (time, height, width, ...: up to four) of the head_dim / 2 frequencies of a
+    head, for buddy_qk_norm_rope and buddy_kv4_append, whose positions are then [axes, tokens].
+    sections: how many frequencies each axis has.  They lie in runs, axis after axis, or, when
+    interleaved, go round the axes as long as an axis has some left."""
+    counts = [int(n) for n in sections]
+    if head_dim not in (64, 128):
+        raise ValueError("head_dim: 64 or 128 is wanted")
+    if not 1 <= len(counts) <= 4 or min(counts) < 0 or sum(counts) != head_dim // 2:
+        raise ValueError("sections: one to four counts of frequencies, head_dim / 2 in all, are wanted")
+    if interleaved:
+        axis = [a for turn in range(max(counts)) for a, n in enumerate(counts) if n > turn]
+    else:
+        axis = [a for a, n in enumerate(counts) for _ in range(n)]
+    return RopeAxes(len(counts), (ctypes.c_uint8 * 64)(*axis), 0, head_dim)
+
+
+def _axes_address(axes) -> int:
+    if not isinstance(axes, RopeAxes):
+        raise TypeError("axes: what buddy_rope_axes makes is wanted")
+    return ctypes.addressof(axes)
+
+
 def buddy_qk_norm_rope(q: Optional[torch.Tensor], k: torch.Tensor, pos: torch.Tensor, rope, q_out, k_out,
                        q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
-                       eps: float = 1e-6, flags: Optional[torch.Tensor] = None, stream=None):
+                       eps: float = 1e-6, flags: Optional[torch.Tensor] = None, stream=None,
+                       axes: Optional[RopeAxes] = None):
     """Norm of each query and key head (with gains) and rotation, in one pass.
-    q, k, q_out, k_out: [tokens, heads, head_dim], fp32 or bf16; rope: (cos, sin)."""
+    q, k, q_out, k_out: [tokens, heads, head_dim], fp32 or bf16; rope: (cos, sin);
+    pos: [tokens], or, with axes (buddy_rope_axes), [axes, tokens]."""
     co, si = rope
+    if axes is not None:
+        _check(load_library().call_qk_norm_rope_axes(q, k, pos, co, si, q_out, k_out, q_gain, k_gain, eps, flags, stream,
+                                                     _axes_address(axes)), "buddy_qk_norm_rope_axes")
+        return
     _check(load_library().call_qk_norm_rope(q, k, pos, co, si, q_out, k_out, q_gain, k_gain, eps, flags, stream),
            "buddy_qk_norm_rope")
 
@@ -501,9 +541,13 @@ class KV4Cache:
                          slot: torch.Tensor, rope, q_out: Optional[torch.Tensor],
                          q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
                          eps: float = 1e-6, flags: Optional[torch.Tensor] = None,
-                         k_out: Optional[torch.Tensor] = None, stream=None):
+                         k_out: Optional[torch.Tensor] = None, stream=None, axes: Optional[RopeAxes] = None):
         """buddy_qk_norm_rope, with the keys and values v stored at `slot`."""
         co, si = rope
+        if axes is not None:
+            _check(self.lib.call_kv4_append_axes(self.address, q, k, pos, co, si, q_out, k_out, q_gain, k_gain, eps, v,
+                                                 slot, flags, stream, _axes_address(axes)), "buddy_kv4_append_axes")
+            return
         _check(self.lib.call_kv4_append(self.address, q, k, pos, co, si, q_out, k_out, q_gain, k_gain, eps, v, slot,
                                         flags, stream), "buddy_kv4_append")
 

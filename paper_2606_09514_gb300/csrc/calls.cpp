@@ -228,8 +228,8 @@ PyObject* page_plan(PyObject* const* a) {
   return called(d, [&] { return f(&p, flags, s); });
 }
 
-// q, k, pos, cos, sin, q_out, k_out, q_gain, k_gain, eps
-buddy_qk_rows rows_of(Device& d, PyObject* const* a) {
+// q, k, pos, cos, sin, q_out, k_out, q_gain, k_gain, eps; with `axes`, pos [axes, tokens]
+buddy_qk_rows rows_of(Device& d, PyObject* const* a, buddy_rope_axes* axes = nullptr) {
   const at::Tensor& k = tensor(a[1], "k");
   const ScalarType type = k.scalar_type();
   const auto F = ScalarType::Float;
@@ -265,7 +265,33 @@ buddy_qk_rows rows_of(Device& d, PyObject* const* a) {
   if (rows != r.max_pos) wrong("sin", "as many positions as in cos are wanted");
   r.q_gain = data_or_null<float>(d, a[7], F, hd, "q_gain");
   r.k_gain = data_or_null<float>(d, a[8], F, hd, "k_gain");
-  r.pos = data<int32_t>(d, a[2], ScalarType::Int, T, "pos");
+  if (!axes) {
+    r.pos = data<int32_t>(d, a[2], ScalarType::Int, T, "pos");
+    return r;
+  }
+  const at::Tensor& pos = tensor(a[2], "pos");
+  if (pos.scalar_type() != ScalarType::Int || !pos.is_cuda() || pos.dim() != 2 || pos.size(0) != axes->n_axes ||
+      pos.size(1) != T || (pos.stride(1) != 1 && T > 1)) {
+    PyErr_Format(PyExc_ValueError, "pos: CUDA int32 (%d, %lld) with the tokens of an axis one after the other is wanted",
+                 (int)axes->n_axes, (long long)T);
+    throw Failed{};
+  }
+  d.take(pos, "pos");
+  r.pos = static_cast<const int32_t*>(pos.data_ptr());
+  axes->pos_stride = pos.stride(0);
+  return r;
+}
+
+// What a RopeAxes' address stands for: the axes, and the head dimension that they are of.
+struct AxesOf {
+  buddy_rope_axes axes;
+  int32_t head_dim;
+};
+buddy_qk_rows rows_with_axes(Device& d, PyObject* const* a, PyObject* address, buddy_rope_axes* axes) {
+  const AxesOf* const given = entry<const AxesOf*>(address);
+  *axes = given->axes;
+  const buddy_qk_rows r = rows_of(d, a, axes);
+  if (r.head_dim != given->head_dim) wrong("axes", "axes of the head dimension of k are wanted");
   return r;
 }
 
@@ -279,20 +305,56 @@ PyObject* qk_norm_rope(PyObject* const* a) {
   return called(d, [&] { return f(&r, flags, s); });
 }
 
-// entry, cache's address, the ten of rows_of, v, slot, flags, stream
+// entry, the ten of rows_of, flags, stream, axes
+PyObject* qk_norm_rope_axes(PyObject* const* a) {
+  Device d;
+  buddy_rope_axes axes;
+  const buddy_qk_rows r = rows_with_axes(d, a + 1, a[13], &axes);
+  int32_t* flags = data_or_null<int32_t>(d, a[11], ScalarType::Int, 1, "flags");
+  void* s = stream_of(tensor(a[2], "k"), a[12]);
+  auto f = entry<decltype(&buddy_qk_norm_rope_axes)>(a[0]);
+  return called(d, [&] { return f(&r, &axes, flags, s); });
+}
+
+// The cache's address, the ten of rows_of, v, slot, flags, stream
+struct Append {
+  const buddy_kv4_cache* c;
+  buddy_qk_rows r;
+  const void* v;
+  int64_t v_stride;
+  const int64_t* slot;
+  int32_t* flags;
+  void* stream;
+};
+Append append_of(Device& d, PyObject* const* a, PyObject* address = nullptr, buddy_rope_axes* axes = nullptr) {
+  Append x;
+  x.c = &pages(d, a[0])->c;
+  x.r = axes ? rows_with_axes(d, a + 1, address, axes) : rows_of(d, a + 1);
+  const at::Tensor& k = tensor(a[2], "k");
+  const at::Tensor& v = tensor(a[11], "v");
+  x.v_stride = heads(d, v, k.scalar_type(), x.r.n_tok, x.r.n_kv_heads, x.r.head_dim, "v");
+  x.slot = data<int64_t>(d, a[12], ScalarType::Long, x.r.n_tok, "slot");
+  x.flags = data_or_null<int32_t>(d, a[13], ScalarType::Int, 1, "flags");
+  x.stream = stream_of(k, a[14]);
+  x.v = v.data_ptr();
+  return x;
+}
+
+// entry, those of append_of
 PyObject* kv4_append(PyObject* const* a) {
   Device d;
-  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
-  const buddy_qk_rows r = rows_of(d, a + 2);
-  const at::Tensor& k = tensor(a[3], "k");
-  const at::Tensor& v = tensor(a[12], "v");
-  const int64_t stride = heads(d, v, k.scalar_type(), r.n_tok, r.n_kv_heads, r.head_dim, "v");
-  const int64_t* slot = data<int64_t>(d, a[13], ScalarType::Long, r.n_tok, "slot");
-  int32_t* flags = data_or_null<int32_t>(d, a[14], ScalarType::Int, 1, "flags");
-  void* s = stream_of(k, a[15]);
+  const Append x = append_of(d, a + 1);
   auto f = entry<decltype(&buddy_kv4_append)>(a[0]);
-  const void* pv = v.data_ptr();
-  return called(d, [&] { return f(c, &r, pv, stride, slot, flags, s); });
+  return called(d, [&] { return f(x.c, &x.r, x.v, x.v_stride, x.slot, x.flags, x.stream); });
+}
+
+// entry, those of append_of, axes
+PyObject* kv4_append_axes(PyObject* const* a) {
+  Device d;
+  buddy_rope_axes axes;
+  const Append x = append_of(d, a + 1, a[16], &axes);
+  auto f = entry<decltype(&buddy_kv4_append_axes)>(a[0]);
+  return called(d, [&] { return f(x.c, &x.r, &axes, x.v, x.v_stride, x.slot, x.flags, x.stream); });
 }
 
 // entry, cache's address, slot, k_out, v_out, flags, stream
@@ -359,6 +421,8 @@ PyMethodDef method(const char* name) {
 PyMethodDef methods[] = {method<14, page_plan>("page_plan"),         method<13, qk_norm_rope>("qk_norm_rope"),
                          method<16, kv4_append>("kv4_append"),       method<7, kv4_read>("kv4_read"),
                          method<12, kv4_attention>("kv4_attention"), method<2, stream_for_workspace>("stream_for_workspace"),
+                         method<14, qk_norm_rope_axes>("qk_norm_rope_axes"),
+                         method<17, kv4_append_axes>("kv4_append_axes"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

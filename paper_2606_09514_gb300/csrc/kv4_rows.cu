@@ -1,7 +1,7 @@
 // Rows of queries, keys and values between a block's QKV projection and its
 // attention: norm of each head and rotation (buddy_qk_norm_rope), the same with the
-// entries quantised into the paged 4-bit cache (buddy_kv4_append), and entries read
-// back (buddy_kv4_read).
+// entries quantised into the paged 4-bit cache (buddy_kv4_append), both with one position
+// or with several axes of them (.._axes), and entries read back (buddy_kv4_read).
 //
 // A team of HD / 16 lanes holds a head: a lane has eight neighbours of the lower half and
 // the eight of the upper half that the rotation pairs them with, each in one 16-byte load
@@ -21,6 +21,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -39,6 +40,14 @@ struct RowArgs {
   int32_t* flags;
   int per, groups;             // heads of a team, teams of a token
 };
+
+// Which position turns a frequency: two bits each, the first of a word lowest.
+struct Axes {
+  uint32_t of[4];
+  int n;
+  int64_t stride;              // from axis to axis of the positions
+};
+struct OneAxis {};
 
 __device__ __forceinline__ void store8(float* p, const float* x) {
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -125,6 +134,16 @@ __device__ __forceinline__ void load8(const float* p, F2* o) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
   o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
 }
+// Where two bits of the lowest sixteen are those of axis a (a 0x5555 all along): the values of `y`.
+__device__ __forceinline__ void take8(F2* o, const F2* y, uint32_t w, uint32_t a) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float o0, o1, y0, y1;
+    o[i].get(o0, o1);
+    y[i].get(y0, y1);
+    o[i] = F2(((w >> (4 * i)) & 3u) == a ? y0 : o0, ((w >> (4 * i + 2)) & 3u) == a ? y1 : o1);
+  }
+}
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const F2* x) {
   float y[8];
@@ -178,8 +197,12 @@ __device__ __forceinline__ uint32_t encode8(const F2* x, uint32_t mask, __half* 
   return w;
 }
 
-template <typename T, int HD, bool CACHE>
-__global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A) {
+// AX: OneAxis, or Axes.  With several axes a lane's eight frequencies mostly have the same (runs
+// of a multiple of eight frequencies per axis): two rows of the tables as with one; where
+// they have not, two more rows for each further axis, and a choice between them.
+template <typename T, int HD, bool CACHE, typename AX>
+__global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, const AX ax) {
+  constexpr bool AXES = std::is_same<AX, Axes>::value;
   constexpr int LPH = HD / 16, HALF = HD / 2;
   const buddy_qk_rows& R = A.r;
   const int kq = R.n_q_heads, kk = kq + R.n_kv_heads, heads = kk + (CACHE ? R.n_kv_heads : 0);
@@ -204,13 +227,25 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A) {
   const T* src = row(h0);
   lo.load(src);
   hi.load(src + HALF);
-  const int p = R.pos[t];
+  int p = R.pos[t], most = p, least = p;        // (of all axes)
+  uint32_t mix = 0, axis = 0;                   // two bits of each of the lane's frequencies, the first one's axis
+  if constexpr (AXES) {
+    int q[4] = {p, p, p, p};
+#pragma unroll
+    for (int a = 1; a < 4; ++a)
+      if (a < ax.n) q[a] = R.pos[a * ax.stride + t];
+    mix = (ax.of[tl / 2] >> (tl % 2 * 16)) & 0xFFFFu;
+    axis = mix & 3u;
+    most = max(max(q[0], q[1]), max(q[2], q[3]));
+    least = min(min(q[0], q[1]), min(q[2], q[3]));
+    p = axis & 2 ? (axis & 1 ? q[3] : q[2]) : (axis & 1 ? q[1] : q[0]);
+  }
   int64_t slot = -1;
   if (CACHE) slot = A.slot[t];
-  const bool ok = p >= 0 && p < R.max_pos;
+  const bool ok = least >= 0 && most < R.max_pos;
   const int64_t end = (int64_t)A.pages.n_pages << A.pages.shift;
   if (tl == 0 && h0 == 0 && A.flags) {
-    const int bad = (p >= R.max_pos ? BUDDY_DEV_BAD_POSITION : 0) | (CACHE && ok && slot >= end ? BUDDY_DEV_BAD_PAGE : 0);
+    const int bad = (most >= R.max_pos ? BUDDY_DEV_BAD_POSITION : 0) | (CACHE && ok && slot >= end ? BUDDY_DEV_BAD_PAGE : 0);
     if (bad) atomicOr(A.flags, bad);
   }
   if (!ok) return;
@@ -219,6 +254,19 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A) {
   if (h0 < kk) {
     load8(R.rope_cos + (int64_t)p * HALF + c, co);
     load8(R.rope_sin + (int64_t)p * HALF + c, si);
+    if constexpr (AXES) {
+      if (mix != axis * 0x5555u) {
+        for (uint32_t a = 0; a < (uint32_t)ax.n; ++a) {
+          if (a == axis) continue;
+          const int64_t at = (int64_t)R.pos[a * ax.stride + t] * HALF + c;
+          F2 y[4], z[4];
+          load8(R.rope_cos + at, y);
+          load8(R.rope_sin + at, z);
+          take8(co, y, mix, a);
+          take8(si, z, mix, a);
+        }
+      }
+    }
   }
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
@@ -357,22 +405,33 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
 // (8,297 tokens of 40 heads 32.3 us, 32.4 with four, 37.7 with two; append of 4,999 tokens of
 // 36 heads and their read 23.8, 24.6 and 26.0).
 constexpr int64_t kRowTeams = 16384;
-template <typename T, int HD, bool CACHE>
-static int launch_rows(RowArgs A, cudaStream_t s) {
+template <typename T, int HD, bool CACHE, typename AX>
+static int launch_rows(RowArgs A, const AX& ax, cudaStream_t s) {
   const int heads = A.r.n_q_heads + A.r.n_kv_heads * (CACHE ? 2 : 1);
   A.per = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)A.r.n_tok * heads / kRowTeams));
   A.groups = (heads + A.per - 1) / A.per;
   const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  return launch_k(qk_rows_kernel<T, HD, CACHE>, (unsigned)ctas, kRowThreads, 0, s, true, A) == cudaSuccess
+  return launch_k(qk_rows_kernel<T, HD, CACHE, AX>, (unsigned)ctas, kRowThreads, 0, s, true, A, ax) == cudaSuccess
              ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
-template <bool CACHE>
-static int dispatch_rows(const RowArgs& A, cudaStream_t s) {
+template <bool CACHE, typename AX>
+static int dispatch_rows(const RowArgs& A, const AX& ax, cudaStream_t s) {
   if (A.r.n_tok == 0) return BUDDY_OK;
   if (A.r.dtype == BUDDY_DTYPE_F32)
-    return A.r.head_dim == 128 ? launch_rows<float, 128, CACHE>(A, s) : launch_rows<float, 64, CACHE>(A, s);
-  return A.r.head_dim == 128 ? launch_rows<bf16, 128, CACHE>(A, s) : launch_rows<bf16, 64, CACHE>(A, s);
+    return A.r.head_dim == 128 ? launch_rows<float, 128, CACHE>(A, ax, s) : launch_rows<float, 64, CACHE>(A, ax, s);
+  return A.r.head_dim == 128 ? launch_rows<bf16, 128, CACHE>(A, ax, s) : launch_rows<bf16, 64, CACHE>(A, ax, s);
+}
+
+// The axes of a call's frequencies; false where they are not those of head_dim / 2 frequencies.
+static bool axes_ok(const buddy_rope_axes* a, int head_dim, Axes* out) {
+  if (!a || a->n_axes < 1 || a->n_axes > 4 || a->pos_stride < 0) return false;
+  *out = Axes{{0, 0, 0, 0}, a->n_axes, a->pos_stride};
+  for (int j = 0; j < head_dim / 2; ++j) {
+    if (a->axis[j] >= a->n_axes) return false;
+    out->of[j / 16] |= (uint32_t)a->axis[j] << (j % 16 * 2);
+  }
+  return true;
 }
 
 template <typename T>
@@ -402,18 +461,40 @@ extern "C" int buddy_qk_norm_rope(const buddy_qk_rows* rows, int32_t* flags, voi
   RowArgs A{};
   A.r = *rows;
   A.flags = flags;
-  return dispatch_rows<false>(A, (cudaStream_t)stream);
+  return dispatch_rows<false>(A, OneAxis{}, (cudaStream_t)stream);
+}
+
+extern "C" int buddy_qk_norm_rope_axes(const buddy_qk_rows* rows, const buddy_rope_axes* axes, int32_t* flags,
+                                       void* stream) {
+  Axes ax;
+  if (!rows_ok(rows, true) || !axes_ok(axes, rows->head_dim, &ax)) return BUDDY_ERR_ARG;
+  RowArgs A{};
+  A.r = *rows;
+  A.flags = flags;
+  return dispatch_rows<false>(A, ax, (cudaStream_t)stream);
+}
+
+static bool append_ok(const buddy_kv4_cache* cache, const buddy_qk_rows* rows, const void* v, int64_t v_stride,
+                      const int64_t* slot) {
+  if (!kv4_cache_ok(cache) || !rows_ok(rows, false) || rows->n_kv_heads != cache->n_kv_heads ||
+      rows->head_dim != cache->head_dim)
+    return false;
+  return rows->n_tok == 0 || (slot && aligned_rows(v, v_stride, rows->dtype == BUDDY_DTYPE_F32 ? 4 : 2));
 }
 
 extern "C" int buddy_kv4_append(const buddy_kv4_cache* cache, const buddy_qk_rows* rows, const void* v,
                                 int64_t v_stride, const int64_t* slot, int32_t* flags, void* stream) {
-  if (!kv4_cache_ok(cache) || !rows_ok(rows, false) || rows->n_kv_heads != cache->n_kv_heads ||
-      rows->head_dim != cache->head_dim)
-    return BUDDY_ERR_ARG;
-  if (rows->n_tok > 0 && (!slot || !aligned_rows(v, v_stride, rows->dtype == BUDDY_DTYPE_F32 ? 4 : 2)))
-    return BUDDY_ERR_ARG;
+  if (!append_ok(cache, rows, v, v_stride, slot)) return BUDDY_ERR_ARG;
   const RowArgs A{*rows, v, v_stride, kv4_pages(cache), slot, flags, 0, 0};
-  return dispatch_rows<true>(A, (cudaStream_t)stream);
+  return dispatch_rows<true>(A, OneAxis{}, (cudaStream_t)stream);
+}
+
+extern "C" int buddy_kv4_append_axes(const buddy_kv4_cache* cache, const buddy_qk_rows* rows, const buddy_rope_axes* axes,
+                                     const void* v, int64_t v_stride, const int64_t* slot, int32_t* flags, void* stream) {
+  Axes ax;
+  if (!append_ok(cache, rows, v, v_stride, slot) || !axes_ok(axes, rows->head_dim, &ax)) return BUDDY_ERR_ARG;
+  const RowArgs A{*rows, v, v_stride, kv4_pages(cache), slot, flags, 0, 0};
+  return dispatch_rows<true>(A, ax, (cudaStream_t)stream);
 }
 
 extern "C" int buddy_kv4_read(const buddy_kv4_cache* cache, int32_t n, const int64_t* slot, int32_t dtype, void* k_out,
