@@ -571,6 +571,80 @@ BUDDY_API int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_
 BUDDY_API int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                                 int32_t max_new);
 
+/* ---------------------------------------------------------------------------
+ * Attention over the pages that a score selects for each query: for contexts so
+ * long that reading all of them for every token costs too much.  After an append,
+ *   buddy_kv4_bounds            bounds of the keys of the pages that it wrote to,
+ *   buddy_kv4_select            each query's best pages by those bounds,
+ *   buddy_kv4_attention_pages   attention over them.
+ *
+ * Sequences of a call, as in buddy_kv4_attention: tokens row_start[i] ..
+ * row_start[i + 1] - 1 are the last positions of sequence i's kv_len[i]. */
+typedef struct {
+  int32_t batch;              /* 1 .. 16384 */
+  int32_t n_tok;              /* rows of the call */
+  int32_t max_new;            /* >= 1: most tokens of one sequence */
+  int32_t max_pages;          /* entries of a table row, max_pages * page_size < 2^31 */
+  const int32_t* row_start;   /* device [batch + 1]; NULL: one token per sequence (n_tok == batch) */
+  const int32_t* kv_len;      /* device [batch], the call's tokens among them */
+  const int32_t* table;       /* device [batch, max_pages] */
+} buddy_kv4_seqs;
+
+/* Bounds of the keys: device half [n_pages, n_kv_heads, 2, head_dim], 16-byte
+ * aligned: of each page, KV head and channel the smallest of the stored keys, then
+ * the largest; exact, and NaN where one of them is.  Written are those of the pages
+ * that the call's tokens lie in, from everything these pages hold up to kv_len[i]
+ * (so the bounds of a sequence with as many tokens as positions are made anew; a
+ * call may be repeated); others are left as they were.
+ * Device-checked: lengths and row starts as in buddy_kv4_attention
+ * (BUDDY_DEV_BAD_POSITION: the sequence is left out); page ids (BUDDY_DEV_BAD_PAGE:
+ * the page is). */
+BUDDY_API int buddy_kv4_bounds(const buddy_kv4_cache* cache, const buddy_kv4_seqs* seqs, void* bounds,
+                               int32_t* flags, void* stream);
+
+/* Of each query token and KV head at most `budget` pages.  A token at position p has
+ * pages 0 .. p / page_size.  Where they are `budget` or fewer, all are selected;
+ * else the `first` first ones, the `last` last ones (its own the last of them), and
+ * of the others those with the highest scores, ties to the lower position:
+ *   score = sum_c a_c hi_c + sum_c b_c lo_c,
+ *   a_c = sum_h max(q_hc, 0), b_c = sum_h min(q_hc, 0),
+ * over the query heads h of the KV head and the page's bounds: the sum over these
+ * heads of a bound of q . k over the page.  A NaN counts as the highest score, a page
+ * that is not there (BUDDY_DEV_BAD_PAGE) as the lowest.  fp32, every product and sum
+ * rounded by itself, in this order: over h from the first head on; the products over
+ * c halves onto each other inside eight neighbours, then so over the eights; then the
+ * sum over hi plus that over lo.
+ * Written for each token t: to pages[t][g] the page ids, in the order of their
+ * positions, -1 behind them; to visible[t] how many positions they hold up to the
+ * token (all pages but the last are whole), the same for every KV head: 0 for a
+ * token without any position, -1, with its pages left as they were, for one that is
+ * in no sequence, or in one whose length or row starts are bad
+ * (BUDDY_DEV_BAD_POSITION). */
+typedef struct {
+  buddy_kv4_seqs s;           /* max_pages <= 49152 (else BUDDY_ERR_RANGE) */
+  int32_t n_q_heads;          /* a multiple of n_kv_heads, at most 8 times */
+  int32_t q_dtype;            /* BUDDY_DTYPE_F32 or _BF16 */
+  int32_t budget;             /* >= first + last */
+  int32_t first;              /* >= 0 */
+  int32_t last;               /* >= 1 */
+  const void* q;              /* device [n_tok, n_q_heads, head_dim], tokens q_stride elements apart */
+  int64_t q_stride;           /* rows 16-byte aligned */
+  const void* bounds;         /* device, of buddy_kv4_bounds */
+  int32_t* pages;             /* device [n_tok, n_kv_heads, budget] */
+  int32_t* visible;           /* device [n_tok] */
+} buddy_kv4_select_args;
+BUDDY_API int buddy_kv4_select(const buddy_kv4_cache* cache, const buddy_kv4_select_args* args, int32_t* flags,
+                               void* stream);
+
+/* buddy_kv4_attention of single tokens, each KV head over pages of its own: batch ==
+ * n_tok, 0 .. 16384 tokens, max_new 1, row_start NULL; table is device [n_tok,
+ * n_kv_heads, max_pages], kv_len[t] the positions of token t's lists that it sees
+ * (the first kv_len[t] in the order of the lists).  A token with none gets zeros, one
+ * with a negative number is left as it was.  Numerics, workspace
+ * (buddy_kv4_attention_workspace with max_new 1) and device checks as above. */
+BUDDY_API int buddy_kv4_attention_pages(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* args,
+                                        int32_t* flags, void* stream);
+
 BUDDY_API const char* buddy_error_string(int32_t code);
 BUDDY_API int32_t buddy_version(void);
 

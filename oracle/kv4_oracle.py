@@ -123,3 +123,49 @@ def attention(q, k, v, n_new, scale):
             p = np.exp(s - s.max())
             out[j, h] = p @ v[h // group, :seen] / p.sum()
     return out
+
+
+def page_bounds(keys, page, n):
+    """keys [pages, heads, page, hd] of one sequence of n positions: [pages, heads, 2, hd]."""
+    out = np.empty(keys.shape[:2] + (2, keys.shape[-1]))
+    for j, blk in enumerate(keys):
+        held = blk[:, :n - j * page]
+        out[j, :, 0], out[j, :, 1] = held.min(1), held.max(1)
+    return out
+
+
+def _eights(x):
+    """fp32 sum over the last axis: halves onto each other inside eight neighbours, then so over the eights."""
+    x = x.reshape(*x.shape[:-1], -1, 8)
+    for _ in range(2):
+        while x.shape[-1] > 1:
+            h = x.shape[-1] // 2
+            x = x[..., :h] + x[..., h:]
+        x = x[..., 0]
+    return x
+
+
+def page_scores(q, bounds):
+    """q [nq, hd] and bounds [pages, heads, 2, hd], fp32: [heads, pages], every product and sum rounded."""
+    q, bounds = np.asarray(q, np.float32), np.asarray(bounds, np.float32)
+    out = np.empty((bounds.shape[1], bounds.shape[0]), np.float32)
+    group = len(q) // bounds.shape[1]
+    with np.errstate(all="ignore"):
+        for g in range(bounds.shape[1]):
+            mine = q[g * group:(g + 1) * group]
+            a, b = np.maximum(mine[0], 0), np.minimum(mine[0], 0)
+            for x in mine[1:]:
+                a, b = a + np.maximum(x, 0), b + np.minimum(x, 0)
+            out[g] = _eights(a * bounds[:, g, 1]) + _eights(b * bounds[:, g, 0])
+    return out
+
+
+def select(score, budget, first, last):
+    """Positions of the selected pages of score [pages], ascending; None for a page that is not there."""
+    n = len(score)
+    if n <= budget:
+        return list(range(n))
+    always = list(range(first)) + list(range(n - last, n))
+    rank = {j: (0, 0) if score[j] is None else (2, 0) if np.isnan(score[j]) else (1, score[j]) for j in range(first, n - last)}
+    best = sorted(rank, key=lambda j: (-rank[j][0], -rank[j][1], j))[:budget - first - last]
+    return sorted(always + best)

@@ -28,7 +28,8 @@ EXPORTED = ["buddy_create", "buddy_destroy", "buddy_set_weights", "buddy_kv_appe
             "buddy_route_noalloc", "buddy_set_budget_predictor", "buddy_get_paths", "buddy_prefill",
             "buddy_set_wait_limit", "buddy_page_plan", "buddy_rope_table", "buddy_qk_norm_rope",
             "buddy_kv4_append", "buddy_kv4_read", "buddy_kv4_attention", "buddy_kv4_attention_workspace",
-            "buddy_qk_norm_rope_axes", "buddy_kv4_append_axes"]
+            "buddy_qk_norm_rope_axes", "buddy_kv4_append_axes", "buddy_kv4_bounds", "buddy_kv4_select",
+            "buddy_kv4_attention_pages"]
 PROF_CLASSES = ["check", "rmsnorm", "gemm_qkv", "qkv_finalize", "attention", "gemm_o", "gemm_gate_up",
                 "gemm_down", "route", "compact", "other", "gemm_fixup",
                 "pf_gemm", "pf_attention", "pf_other"]
@@ -101,6 +102,17 @@ class buddy_kv4_attention_args(ctypes.Structure):
                 ("table", c_p), ("workspace", c_p), ("workspace_bytes", ctypes.c_int64)]
 
 
+class buddy_kv4_seqs(ctypes.Structure):
+    _fields_ = [("batch", c_i32), ("n_tok", c_i32), ("max_new", c_i32), ("max_pages", c_i32), ("row_start", c_p),
+                ("kv_len", c_p), ("table", c_p)]
+
+
+class buddy_kv4_select_args(ctypes.Structure):
+    _fields_ = [("s", buddy_kv4_seqs), ("n_q_heads", c_i32), ("q_dtype", c_i32), ("budget", c_i32), ("first", c_i32),
+                ("last", c_i32), ("q", c_p), ("q_stride", ctypes.c_int64), ("bounds", c_p), ("pages", c_p),
+                ("visible", c_p)]
+
+
 class BuddyError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: libbuddy error {code}")
@@ -168,8 +180,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.buddy_qk_norm_rope_axes.argtypes = [P(buddy_qk_rows), P(RopeAxes), c_p, c_p]
     lib.buddy_kv4_append_axes.argtypes = [P(buddy_kv4_cache), P(buddy_qk_rows), P(RopeAxes), c_p, ctypes.c_int64, c_p,
                                           c_p, c_p]
+    lib.buddy_kv4_bounds.argtypes = [P(buddy_kv4_cache), P(buddy_kv4_seqs), c_p, c_p, c_p]
+    lib.buddy_kv4_select.argtypes = [P(buddy_kv4_cache), P(buddy_kv4_select_args), c_p, c_p]
+    lib.buddy_kv4_attention_pages.argtypes = [P(buddy_kv4_cache), P(buddy_kv4_attention_args), c_p, c_p]
     for name in ("buddy_page_plan", "buddy_rope_table", "buddy_qk_norm_rope", "buddy_kv4_append", "buddy_kv4_read",
-                 "buddy_kv4_attention", "buddy_qk_norm_rope_axes", "buddy_kv4_append_axes"):
+                 "buddy_kv4_attention", "buddy_qk_norm_rope_axes", "buddy_kv4_append_axes", "buddy_kv4_bounds",
+                 "buddy_kv4_select", "buddy_kv4_attention_pages"):
         getattr(lib, name).restype = ctypes.c_int
     lib.buddy_kv4_attention_workspace.restype = ctypes.c_int64
     for name in ("buddy_create", "buddy_set_weights", "buddy_kv_append", "buddy_route", "buddy_decode_step",
@@ -182,7 +198,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         missing = functools.partial(_without_calls, str(e))
         _calls = None
     for name in ("page_plan", "qk_norm_rope", "kv4_append", "kv4_read", "kv4_attention", "qk_norm_rope_axes",
-                 "kv4_append_axes"):
+                 "kv4_append_axes", "kv4_bounds", "kv4_select", "kv4_attention_pages"):
         entry = ctypes.cast(getattr(lib, "buddy_" + name), c_p).value
         setattr(lib, "call_" + name, functools.partial(getattr(_calls, name), entry) if _calls else missing)
     lib.call_stream_for_workspace = _calls.stream_for_workspace if _calls else missing
@@ -566,3 +582,35 @@ class KV4Cache:
             ws = self._own_workspace(q, max_new, stream)
         _check(self.lib.call_kv4_attention(self.address, q, kv_len, table, out, row_start, max_new, scale, flags, ws,
                                            stream), "buddy_kv4_attention")
+
+    def empty_bounds(self) -> torch.Tensor:
+        """Room for the bounds of the cache's keys: fp16 [n_pages, n_kv, 2, head_dim], zeros."""
+        shape = (self.k_pages.shape[0], self.n_kv, 2, self.head_dim)
+        return torch.zeros(shape, dtype=torch.float16, device=self.k_pages.device)
+
+    def buddy_kv4_bounds(self, bounds: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor,
+                         row_start: Optional[torch.Tensor] = None, max_new: int = 1,
+                         flags: Optional[torch.Tensor] = None, stream=None):
+        """After an append: smallest and largest key of each channel in the pages that it wrote to."""
+        _check(self.lib.call_kv4_bounds(self.address, bounds, kv_len, table, row_start, max_new, flags, stream),
+               "buddy_kv4_bounds")
+
+    def buddy_kv4_select(self, q: torch.Tensor, bounds: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor,
+                         pages: torch.Tensor, visible: torch.Tensor, row_start: Optional[torch.Tensor] = None,
+                         max_new: int = 1, first: int = 1, last: int = 1, flags: Optional[torch.Tensor] = None,
+                         stream=None):
+        """The pages of each query token and KV head that may matter most by the keys' bounds: to
+        pages [tokens, n_kv, budget], the first and the last ones always among them, and to visible
+        [tokens] the positions that they hold up to the token."""
+        _check(self.lib.call_kv4_select(self.address, q, bounds, kv_len, table, row_start, max_new, pages, visible, first,
+                                        last, flags, stream), "buddy_kv4_select")
+
+    def buddy_kv4_attention_pages(self, q: torch.Tensor, visible: torch.Tensor, pages: torch.Tensor, out: torch.Tensor,
+                                  scale: float = 0.0, flags: Optional[torch.Tensor] = None,
+                                  workspace: Optional[torch.Tensor] = None, stream=None):
+        """Attention of each query token over lists of pages, one for each KV head (buddy_kv4_select)."""
+        ws = workspace if workspace is not None else self.workspace
+        if ws is None:
+            ws = self._own_workspace(q, 1, stream)
+        _check(self.lib.call_kv4_attention_pages(self.address, q, visible, pages, out, scale, flags, ws, stream),
+               "buddy_kv4_attention_pages")

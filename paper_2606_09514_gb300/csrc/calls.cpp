@@ -413,6 +413,104 @@ PyObject* kv4_attention(PyObject* const* a) {
   return called(d, [&] { return f(c, &p, flags, s); });
 }
 
+// kv_len, table, row_start, max_new of a call with `tokens` rows (-1: as many as row_start says)
+buddy_kv4_seqs seqs_of(Device& d, PyObject* const* a, int64_t tokens) {
+  const auto I = ScalarType::Int;
+  const int64_t B = tensor(a[0], "kv_len").numel();
+  buddy_kv4_seqs s{};
+  s.batch = int32(B, "kv_len");
+  s.kv_len = data<int32_t>(d, a[0], I, B, "kv_len");
+  const at::Tensor& table = vec(d, a[1], I, 0, "table");
+  if (table.dim() != 2 || table.size(0) != B) wrong("table", "[batch, max_pages] is wanted");
+  s.max_pages = int32(table.size(1), "table");
+  s.table = static_cast<int32_t*>(table.data_ptr());
+  s.row_start = data_or_null<int32_t>(d, a[2], I, B + 1, "row_start");
+  s.max_new = int32(a[3]);
+  s.n_tok = tokens >= 0 ? int32(tokens, "q") : s.row_start ? INT32_MAX : s.batch;
+  return s;
+}
+
+// The keys' bounds of a cache: half [n_pages, n_kv_heads, 2, head_dim].
+void* bounds_of(Device& d, PyObject* o, const buddy_kv4_cache* c) {
+  const at::Tensor& t = vec(d, o, ScalarType::Half, 0, "bounds");
+  if (t.dim() != 4 || t.size(0) != c->n_pages || t.size(1) != c->n_kv_heads || t.size(2) != 2 || t.size(3) != c->head_dim)
+    wrong("bounds", "[n_pages, n_kv, 2, head_dim] of the cache is wanted");
+  return t.data_ptr();
+}
+
+// entry, cache's address, bounds, kv_len, table, row_start, max_new, flags, stream
+PyObject* kv4_bounds(PyObject* const* a) {
+  Device d;
+  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
+  void* const bounds = bounds_of(d, a[2], c);
+  const buddy_kv4_seqs s = seqs_of(d, a + 3, -1);
+  int32_t* flags = data_or_null<int32_t>(d, a[7], ScalarType::Int, 1, "flags");
+  void* stream = stream_of(tensor(a[2], "bounds"), a[8]);
+  auto f = entry<decltype(&buddy_kv4_bounds)>(a[0]);
+  return called(d, [&] { return f(c, &s, bounds, flags, stream); });
+}
+
+// The lists of pages of a call's tokens, [tokens, n_kv_heads, pages]: entries of one.
+int32_t* lists_of(Device& d, PyObject* o, const buddy_kv4_cache* c, int64_t tokens, int32_t* entries) {
+  const at::Tensor& t = vec(d, o, ScalarType::Int, 0, "pages");
+  if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != c->n_kv_heads) wrong("pages", "[tokens, n_kv, budget] is wanted");
+  *entries = int32(t.size(2), "pages");
+  return static_cast<int32_t*>(t.data_ptr());
+}
+
+// entry, cache's address, q, bounds, kv_len, table, row_start, max_new, pages, visible, first, last, flags, stream
+PyObject* kv4_select(PyObject* const* a) {
+  Device d;
+  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
+  const at::Tensor& q = tensor(a[2], "q");
+  if (q.dim() != 3 || q.size(2) != c->head_dim) wrong("q", "[tokens, heads, head_dim of the cache] is wanted");
+  buddy_kv4_select_args p{};
+  p.n_q_heads = int32(q.size(1), "q");
+  p.q_dtype = dtype_of(q.scalar_type());
+  p.q_stride = heads(d, q, q.scalar_type(), q.size(0), p.n_q_heads, c->head_dim, "q");
+  p.q = q.data_ptr();
+  p.bounds = bounds_of(d, a[3], c);
+  p.s = seqs_of(d, a + 4, q.size(0));
+  p.pages = lists_of(d, a[8], c, q.size(0), &p.budget);
+  p.visible = data<int32_t>(d, a[9], ScalarType::Int, q.size(0), "visible");
+  p.first = int32(a[10]);
+  p.last = int32(a[11]);
+  int32_t* flags = data_or_null<int32_t>(d, a[12], ScalarType::Int, 1, "flags");
+  void* s = stream_of(q, a[13]);
+  auto f = entry<decltype(&buddy_kv4_select)>(a[0]);
+  return called(d, [&] { return f(c, &p, flags, s); });
+}
+
+// entry, cache's address, q, visible, pages, out, scale, flags, workspace, stream
+PyObject* kv4_attention_pages(PyObject* const* a) {
+  Device d;
+  const auto I = ScalarType::Int;
+  const buddy_kv4_cache* const c = &pages(d, a[1])->c;
+  const at::Tensor& q = tensor(a[2], "q");
+  const at::Tensor& out = tensor(a[5], "out");
+  if (q.dim() != 3 || q.size(2) != c->head_dim) wrong("q", "[tokens, heads, head_dim of the cache] is wanted");
+  buddy_kv4_attention_args p{};
+  p.batch = p.n_tok = int32(q.size(0), "q");
+  p.n_q_heads = int32(q.size(1), "q");
+  p.max_new = 1;
+  p.scale = real(a[6]);
+  p.q_dtype = dtype_of(q.scalar_type());
+  p.out_dtype = dtype_of(out.scalar_type());
+  p.q_stride = heads(d, q, q.scalar_type(), p.n_tok, p.n_q_heads, c->head_dim, "q");
+  p.out_stride = heads(d, out, out.scalar_type(), p.n_tok, p.n_q_heads, c->head_dim, "out");
+  p.q = q.data_ptr();
+  p.out = out.data_ptr();
+  p.kv_len = data<int32_t>(d, a[3], I, p.n_tok, "visible");
+  p.table = lists_of(d, a[4], c, p.n_tok, &p.max_pages);
+  const at::Tensor& ws = vec(d, a[8], ScalarType::Byte, 0, "workspace");
+  p.workspace = ws.data_ptr();
+  p.workspace_bytes = ws.numel();
+  int32_t* flags = data_or_null<int32_t>(d, a[7], I, 1, "flags");
+  void* s = stream_of(q, a[9]);
+  auto f = entry<decltype(&buddy_kv4_attention_pages)>(a[0]);
+  return called(d, [&] { return f(c, &p, flags, s); });
+}
+
 template <int N, PyObject* (*F)(PyObject* const*)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<N, F>)), METH_FASTCALL, nullptr};
@@ -423,6 +521,9 @@ PyMethodDef methods[] = {method<14, page_plan>("page_plan"),         method<13, 
                          method<12, kv4_attention>("kv4_attention"), method<2, stream_for_workspace>("stream_for_workspace"),
                          method<14, qk_norm_rope_axes>("qk_norm_rope_axes"),
                          method<17, kv4_append_axes>("kv4_append_axes"),
+                         method<9, kv4_bounds>("kv4_bounds"),
+                         method<14, kv4_select>("kv4_select"),
+                         method<10, kv4_attention_pages>("kv4_attention_pages"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -100,14 +100,22 @@ __host__ __device__ constexpr int64_t partial_floats() { return 8 * NB * (HD + 2
 
 // Chunks of a stream of n positions.  (A sequence without positions: one of nothing.)
 __device__ __forceinline__ int chunks_of(int n) { return max(1, (n + kChunk - 1) / kChunk); }
-// A sequence with m = 0 where it has no rows here.
+// A sequence with m = 0 where it has no rows here.  LISTS: a token that has a list of pages for
+// each KV head; without rows where its positions are negative.
+template <bool LISTS>
 __device__ __forceinline__ Rows few_rows(const AttnArgs4& A, int i, bool* bad) {
+  if constexpr (LISTS) {
+    const int n = A.a.kv_len[i];
+    *bad = n > (int64_t)A.a.max_pages << A.p.shift;
+    return Rows{i, *bad || n < 0 ? 0 : 1, n};
+  }
   Rows q = rows_of(A, i, bad);
   if (q.m * A.G > A.row_limit) q.m = 0;
   return q;
 }
 
 // A walk over the streams of a CTA's share.
+template <bool LISTS>
 struct Walk {
   Rows q;
   int i, g, c, c1;            // sequence, KV head, chunks [c, c1) of the stream in this share
@@ -122,7 +130,7 @@ struct Walk {
       g = 0;
       bool bad;
       do {
-        q = few_rows(A, ++i, &bad);   // (with some of the share left there is another stream)
+        q = few_rows<LISTS>(A, ++i, &bad);   // (with some of the share left there is another stream)
       } while (q.m == 0);
     }
     c = 0;
@@ -167,7 +175,8 @@ __device__ __forceinline__ void load_piece(const Pages& P, uint32_t dst, uint32_
   bulk_load(dst + 2 * kChunk * CB + (kChunk + at) * SB, v + to_scales, N * SB, bar);
 }
 
-template <int HD, int NB, bool WIDE>
+// LISTS: each (token, KV head) has pages of its own, in a table [tokens, KV heads, max_pages].
+template <int HD, int NB, bool WIDE, bool LISTS>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_kernel(const AttnArgs4 A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t full[kWarps * kStages];
@@ -206,13 +215,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
   auto share_of = [&](int64_t total) {
     return (int)min((int64_t)INT32_MAX / 2, ((total + gridDim.x - 1) / gridDim.x + kWarps - 1) / kWarps * kWarps);
   };
-  Walk use;
+  Walk<LISTS> use;
   int64_t total = 0, lo, at;
   int share;
   if (B <= 32) {                    // every warp by itself
     Rows q{0, 0, 0};
     bool bad = false;
-    if (lane < B) q = few_rows(A, lane, &bad);
+    if (lane < B) q = few_rows<LISTS>(A, lane, &bad);
     if (__any_sync(0xffffffffu, bad) && blockIdx.x == 0 && tid == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
     const int64_t mine = cost(q), upto = scan(mine);
     total = __shfl_sync(0xffffffffu, upto, 31);
@@ -233,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
 #pragma unroll 1
     for (int i = b0; i < b1; ++i) {
       bool bad;
-      mine += cost(few_rows(A, i, &bad));
+      mine += cost(few_rows<LISTS>(A, i, &bad));
       any_bad |= bad;
     }
     if (any_bad && blockIdx.x == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
@@ -253,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
 #pragma unroll 1
       for (int i = b0; i < b1; ++i) {
         bool bad;
-        const int64_t n = cost(few_rows(A, i, &bad));
+        const int64_t n = cost(few_rows<LISTS>(A, i, &bad));
         if (lo < x + n) {
           s_first = i;
           s_at = lo - x;
@@ -266,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
     bool bad;
     use.i = s_first;
     at = s_at;
-    use.q = few_rows(A, use.i, &bad);
+    use.q = few_rows<LISTS>(A, use.i, &bad);
   }
   use.k = 0;
   int start;                        // where the stream's first chunk is, from the share's beginning on
@@ -287,12 +296,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
       use.rem -= use.c1 - use.c;
     }
   }
-  Walk ld = use;
+  Walk<LISTS> ld = use;
   bool more = true;                 // (the walk's, until a copy does not come)
   // Where a share holds several short streams, a warp takes the whole of every fourth.
   const bool many = share >= kMany;
-  auto owned = [&](const Walk& w) { return NB == 1 && many && w.q.n <= kWhole * kChunk; };
-  auto enter = [&](const Walk& w) { return owned(w) ? (w.k % kWarps == warp ? 0 : w.c1) : w.c + warp; };
+  auto owned = [&](const Walk<LISTS>& w) { return NB == 1 && many && w.q.n <= kWhole * kChunk; };
+  auto enter = [&](const Walk<LISTS>& w) { return owned(w) ? (w.k % kWarps == warp ? 0 : w.c1) : w.c + warp; };
   ld.c = enter(ld);
   int ld_step = owned(ld) ? 1 : kWarps;
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * stage_bytes<HD>();
@@ -310,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
       if (!more) return;
     }
     const int p0 = ld.c * kChunk;
-    const int32_t* row = A.a.table + (int64_t)ld.i * A.a.max_pages;
+    const int32_t* row = A.a.table + (LISTS ? (int64_t)ld.i * A.p.nkv + ld.g : (int64_t)ld.i) * A.a.max_pages;
     id0 = id1 = row[p0 >> A.p.shift];
     if (A.p.shift == 4 && p0 + 16 < ld.q.n) id1 = row[(p0 >> 4) + 1];
   };
@@ -804,17 +813,26 @@ static int sm_count() {
   return n;
 }
 
-template <int HD, int NB, bool WIDE>
+template <int HD, int NB, bool WIDE, bool LISTS>
 static int launch_decode(const AttnArgs4& A, int64_t most, int sms, cudaStream_t s) {
   constexpr int smem = smem_bytes<HD, NB>();
+  auto* const kern = kv4_decode_kernel<HD, NB, WIDE, LISTS>;
   const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, ctas_per_sm<NB, WIDE>() * sms));
-  if (cudaFuncSetAttribute(kv4_decode_kernel<HD, NB, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-    return BUDDY_ERR_CUDA;
-  return launch_k(kv4_decode_kernel<HD, NB, WIDE>, grid, kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return BUDDY_ERR_CUDA;
+  return launch_k(kern, grid, kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
-template <int HD, bool WIDE>
-static int launch_few(const AttnArgs4& A, bool two, int64_t most, int sms, cudaStream_t s) {
-  return two ? launch_decode<HD, 2, WIDE>(A, most, sms, s) : launch_decode<HD, 1, WIDE>(A, most, sms, s);
+template <bool LISTS>
+static int launch_few(const AttnArgs4& A, int head_dim, bool two, bool wide, int64_t most, int sms, cudaStream_t s) {
+  if constexpr (!LISTS) {
+    if (two) {
+      if (head_dim == 128)
+        return wide ? launch_decode<128, 2, true, false>(A, most, sms, s) : launch_decode<128, 2, false, false>(A, most, sms, s);
+      return wide ? launch_decode<64, 2, true, false>(A, most, sms, s) : launch_decode<64, 2, false, false>(A, most, sms, s);
+    }
+  }
+  if (head_dim == 128)
+    return wide ? launch_decode<128, 1, true, LISTS>(A, most, sms, s) : launch_decode<128, 1, false, LISTS>(A, most, sms, s);
+  return wide ? launch_decode<64, 1, true, LISTS>(A, most, sms, s) : launch_decode<64, 1, false, LISTS>(A, most, sms, s);
 }
 
 }  // namespace buddy
@@ -839,15 +857,18 @@ extern "C" int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv
   return sms > 0 ? workspace_bytes(n_q_heads / n_kv_heads, head_dim, max_new, sms) : -1;
 }
 
-extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags,
-                                   void* stream) {
-  if (!kv4_cache_ok(cache) || !a || a->batch < 1 || a->batch > 16384 || a->n_tok < 0 || a->max_pages < 1 ||
+// Both forms; LISTS: a list of pages for each token and KV head.
+template <bool LISTS>
+static int attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags, void* stream) {
+  if (!kv4_cache_ok(cache) || !a || a->batch < (LISTS ? 0 : 1) || a->batch > 16384 || a->n_tok < 0 || a->max_pages < 1 ||
       (int64_t)a->max_pages * cache->page_size > INT32_MAX || !(a->scale >= 0.f) || a->scale > 2.3e38f)   // (times log2(e) it is finite)
     return BUDDY_ERR_ARG;
   if (!sizes_ok(a->n_q_heads, cache->n_kv_heads, cache->head_dim, a->max_new) ||
       (a->q_dtype != BUDDY_DTYPE_F32 && a->q_dtype != BUDDY_DTYPE_BF16) ||
-      (a->out_dtype != BUDDY_DTYPE_F32 && a->out_dtype != BUDDY_DTYPE_BF16) || !a->kv_len || !a->table)
+      (a->out_dtype != BUDDY_DTYPE_F32 && a->out_dtype != BUDDY_DTYPE_BF16) ||
+      ((!a->kv_len || !a->table) && !(LISTS && a->n_tok == 0)))   // (empty tensors have no address)
     return BUDDY_ERR_ARG;
+  if (LISTS && a->row_start) return BUDDY_ERR_ARG;
   if (!a->row_start && (a->n_tok != a->batch || a->max_new != 1)) return BUDDY_ERR_ARG;
   if (!a->workspace || a->workspace_bytes < few_bytes(cache->head_dim) ||
       (reinterpret_cast<uintptr_t>(a->workspace) & 255))
@@ -868,14 +889,21 @@ extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4
   // its single tokens through the form for 16 rows (not measured next to many of them).  One CTA
   // for every four chunks there can be, as many as run at once at most.
   const int64_t most_rows = (int64_t)a->max_new * A.G;
-  const bool two = most_rows > 8;
   const int64_t chunks = ((int64_t)a->max_pages * cache->page_size + kv4::kChunk - 1) / kv4::kChunk;
   const int64_t most = (int64_t)a->batch * cache->n_kv_heads * (chunks + kOpen) / kWarps + 1;
   const bool wide = a->q_dtype == BUDDY_DTYPE_F32 || a->out_dtype == BUDDY_DTYPE_F32;
   cudaStream_t s = (cudaStream_t)stream;
-  const int rc = cache->head_dim == 128
-                     ? (wide ? launch_few<128, true>(A, two, most, sms, s) : launch_few<128, false>(A, two, most, sms, s))
-                     : (wide ? launch_few<64, true>(A, two, most, sms, s) : launch_few<64, false>(A, two, most, sms, s));
+  const int rc = launch_few<LISTS>(A, cache->head_dim, most_rows > 8, wide, most, sms, s);
   if (rc != BUDDY_OK || most_rows <= kFewRows) return rc;
   return launch_prompt(A, cache->head_dim, wide, sms, (uint8_t*)a->workspace + few_bytes(cache->head_dim), s);
+}
+
+extern "C" int buddy_kv4_attention(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags,
+                                   void* stream) {
+  return attention<false>(cache, a, flags, stream);
+}
+
+extern "C" int buddy_kv4_attention_pages(const buddy_kv4_cache* cache, const buddy_kv4_attention_args* a, int32_t* flags,
+                                         void* stream) {
+  return attention<true>(cache, a, flags, stream);
 }
