@@ -226,6 +226,29 @@ def test_select_many_pages():
             check_select(*made, lens, [1, 1], budget)
 
 
+@pytest.mark.parametrize("heads", [(4, 2, 128), (2, 1, 64), (24, 8, 128)])
+@pytest.mark.parametrize("n_pages", [127, 128, 129, 255, 256, 257, 700, 1100, 2100])
+def test_select_by_clusters(heads, n_pages):
+    """One token, or few: the pages of a head shared by 1 to 16 CTAs, of which the last may have none."""
+    for lens in ([n_pages * 16 - 1], [n_pages * 16 - 15, 16 * 90 + 4, 3], [n_pages * 16] * 20):
+        made = make_select(lens, [1] * len(lens), 16, heads, torch.bfloat16, seed=n_pages, max_pages=n_pages)
+        check_select(*made, lens, [1] * len(lens), 40, rows=len(lens) == 3)
+
+
+def test_select_of_scores_near_and_far():
+    """Scores in one binade, in many, and alike but for a few bits."""
+    lens = [16 * 1500]
+    cache, table, bounds, q = make_select(lens, [1], 16, (2, 2, 64), torch.float32, seed=1)
+    for scale in (1e-30, 1e-3, 1e4):
+        q[0] = 0
+        q[0, :, 5] = scale
+        wide = torch.randn(bounds.shape[:2], device="cuda")
+        for spread in (1.0, 1e-3, 30.0):
+            bounds[:, :, 1, 5] = (1000 + spread * wide if spread != 30.0 else 10 ** (4 * torch.rand_like(wide))).half()
+            for budget in (3, 65, 1400):
+                check_select(cache, table, bounds, q, lens, [1], budget)
+
+
 @pytest.mark.parametrize("batch", [31, 33, 1025, 3000])
 def test_select_finds_each_tokens_sequence(batch):
     rng = np.random.default_rng(batch)

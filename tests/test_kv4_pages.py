@@ -184,3 +184,14 @@ class TestFakes:
             for arg in ("first", "last", "max_new"):
                 with pytest.raises(OverflowError):
                     fake_cache().buddy_kv4_select(**{**good, arg: 2 ** 31})
+
+
+def test_first_memory_is_reached_after_a_cluster_barrier():
+    """The kernels that write to the first CTA of their cluster: it has started, and waits for them."""
+    from test_kernel_sources import CSRC, code, kernels
+    found = [body for name, body in kernels(code(CSRC / "kv4_pages.cu")) if "put_first" in body]
+    assert len(found) == 1
+    for body in found:
+        first, last = body.index("put_first"), body.rindex("put_first")
+        assert body.index("cluster_arrive_started") < body.index("cluster_wait_started") < first
+        assert "cluster_sync" in body[last:]
