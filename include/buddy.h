@@ -621,7 +621,7 @@ BUDDY_API int buddy_kv4_bounds(const buddy_kv4_cache* cache, const buddy_kv4_seq
  * in no sequence, or in one whose length or row starts are bad
  * (BUDDY_DEV_BAD_POSITION). */
 typedef struct {
-  buddy_kv4_seqs s;           /* max_pages <= 49152 (else BUDDY_ERR_RANGE) */
+  buddy_kv4_seqs s;           /* max_pages <= 40000 (else BUDDY_ERR_RANGE) */
   int32_t n_q_heads;          /* a multiple of n_kv_heads, at most 8 times */
   int32_t q_dtype;            /* BUDDY_DTYPE_F32 or _BF16 */
   int32_t budget;             /* >= first + last */

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const Boun
 // ------------------------------------------------------------------ selection
 constexpr int kSelWarps = 8;
 constexpr int kSelThreads = 32 * kSelWarps;
-constexpr int kSelMaxPages = 49152;     // a score each in shared memory
+constexpr int kSelMaxPages = 40000;     // a score each in shared memory, next to the copies in flight
 constexpr int kSelCluster = 16;         // most CTAs of a (token, KV head)
 constexpr int kSelBins = 256;
 
@@ -188,23 +188,57 @@ __device__ __forceinline__ void sum_lanes(float (&v)[V], int lane, int* base) {
   *base = at;
 }
 
-// Where the best r of M keys end: just r of them are above *at, or these and the first of those
-// equal to it. By counts of the keys in 256 parts of the range [lo, hi] that holds the r-th, from the
-// top, until a part is one value or its keys are all wanted. bins: two sets, zeros.
-__device__ __forceinline__ uint32_t threshold(const uint32_t* keys, int M, int r, uint32_t lo, uint32_t hi,
-                                              int (*bins)[kSelBins], int tid, int lane) {
+// What a thread has of M keys: warp w those from w * run on, 32 at a time. Up to kSelKept of them
+// stay in registers, more in shared memory.
+constexpr int kSelKept = 8;
+struct Keys {
+  const uint32_t* all;
+  int first, end;                                  // of the warp
+  bool few;
+  uint32_t kept[kSelKept];
+  __device__ __forceinline__ Keys(const uint32_t* keys, int M, int warp, int lane) : all(keys) {
+    const int run = (M + kSelThreads - 1) / kSelThreads * 32;
+    first = warp * run;
+    end = min(M, first + run);
+    few = run <= kSelKept * 32;
+    if (few) {
+#pragma unroll
+      for (int k = 0; k < kSelKept; ++k) kept[k] = first + 32 * k + lane < end ? keys[first + 32 * k + lane] : 0u;
+    }
+  }
+  // f(key, index, true where there is one), a warp together
+  template <typename F>
+  __device__ __forceinline__ void each(int lane, F&& f) const {
+    if (few) {
+#pragma unroll
+      for (int k = 0; k < kSelKept; ++k)
+        if (first + 32 * k < end) f(kept[k], first + 32 * k + lane, first + 32 * k + lane < end);
+    } else {
+#pragma unroll 4
+      for (int j = first + lane; j - lane < end; j += 32) f(j < end ? all[j] : 0u, j, j < end);
+    }
+  }
+};
+
+// Where the best r of the keys end: just r of them are above what is returned, or these and the first
+// of those equal to it. By counts of the keys in 256 parts of the range [lo, hi] that holds the r-th,
+// from the top, until a part is one value or its keys are all wanted. bins: two sets, zeros.
+__device__ __forceinline__ uint32_t threshold(const Keys& keys, int r, uint32_t lo, uint32_t hi, int (*bins)[kSelBins],
+                                              int tid, int lane) {
   for (int set = 0;; set ^= 1) {
     const int shift = max(0, 32 - __clz(hi - lo) - 8);       // ((hi - lo) >> shift) < 256
-    for (int j = tid; j < M; j += kSelThreads) {
-      const uint32_t k = keys[j];
-      if (k >= lo && k <= hi) atomicAdd(&bins[set][(k - lo) >> shift], 1);
-    }
+    keys.each(lane, [&](uint32_t k, int, bool there) {
+      if (there && k >= lo && k <= hi) atomicAdd(&bins[set][(k - lo) >> shift], 1);
+    });
     __syncthreads();
     bins[set ^ 1][tid] = 0;
-    // every warp: lane x has the parts 255 - 8 x and below
-    int c[8], sum = 0;
+    // every warp: lane x has the parts from 255 - 8 x down
+    const int4* const mine = reinterpret_cast<const int4*>(bins[set] + 248 - 8 * lane);
+    const int4 y0 = mine[1], y1 = mine[0];
+    const int c[8] = {y0.w, y0.z, y0.y, y0.x, y1.w, y1.z, y1.y, y1.x};
+    int sum = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += c[e] = bins[set][255 - 8 * lane - e];
+    for (int e = 0; e < 8; ++e) sum += c[e];
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -224,24 +258,40 @@ __device__ __forceinline__ uint32_t threshold(const uint32_t* keys, int M, int r
     hi = lo + min(hi - lo, (1u << shift) - 1);
     __syncthreads();                               // (the other set is zero, this one has been read)
     if (shift == 0) return lo;
-    if (in == r) return lo - 1;                    // (lo > 0: no score lies below the parts' range)
+    if (in == r) return lo - 1;                    // (lo > 0: not all of the keys are wanted)
   }
 }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {   // zeros where there is nothing
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+// Pages of a warp's turn, as loads of 16 bytes per lane; turns in flight.
+constexpr int kSelLoads = 4;
+template <int TT, bool CL>
+__host__ __device__ constexpr int sel_turns() { return TT == 1 && !CL ? 2 : 4; }
+template <int TT, bool CL>
+__host__ __device__ constexpr int sel_ring() { return kSelWarps * sel_turns<TT, CL>() * kSelLoads * 512; }   // bytes
+template <int TT>
+__host__ __device__ constexpr int sel_ctas() { return TT == 1 ? 4 : 2; }                                      // per SM
+
 // Up to TT tokens of a sequence share a walk over its pages' bounds; the CTA of the first of
 // them does the work of all. CL: a cluster has one token, its CTAs the pages in turn, and the first
-// one the scores. A page's bounds are HD / 4 loads of 16 bytes, one per lane: the smallest
-// of eight channels, by b, or the largest, by a.
+// one the scores. A page's bounds are HD / 4 copies of 16 bytes, one per lane: the smallest
+// of eight channels, by b, or the largest, by a. Every lane reads what it has copied itself, so
+// that the turns in flight need neither registers nor barriers.
 template <typename T, int HD, int TT, bool CL>
-__global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kernel(const SelectArgs A) {
-  extern __shared__ uint32_t keys[];               // [TT][slots]
-  __shared__ int bins[2][kSelBins];
+__global__ void __launch_bounds__(kSelThreads, sel_ctas<TT>()) kv4_select_kernel(const SelectArgs A) {
+  extern __shared__ __align__(128) uint8_t sel_smem[];
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + sel_ring<TT, CL>());   // [TT][slots]
+  __shared__ __align__(16) int bins[2][kSelBins];
   __shared__ uint32_t s_lo[TT][kSelCluster * kSelWarps], s_hi[TT][kSelCluster * kSelWarps];
   __shared__ int s_above[kSelWarps], s_equal[kSelWarps];
+  __shared__ __align__(16) float s_q[TT][2][HD];   // a token's b, then its a
   static_assert(!CL || TT == 1, "");
   constexpr int LPP = HD / 4, PPW = 32 / LPP;      // lanes of a page, pages of a warp's load
-  constexpr int LOADS = TT == 1 ? 8 : 4;           // in flight
-  constexpr int V = LOADS * TT;
+  constexpr int LOADS = kSelLoads, V = LOADS * TT; // of a turn, and their scores
+  constexpr int TURNS = sel_turns<TT, CL>(), PAGES = LOADS * PPW, IDS = 32 / PAGES;   // turns whose ids a warp reads at once
   const buddy_kv4_select_args& a = A.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = CL ? ptx::cluster_rank() : 0, C = CL ? ptx::cluster_size() : 1;
@@ -250,7 +300,27 @@ __global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kerne
   bins[0][tid] = bins[1][tid] = 0;
   pdl_wait();
   pdl_trigger();
+  // (the queries are on their way while the token's sequence is looked for)
+  constexpr int PER = (TT * HD + kSelThreads - 1) / kSelThreads;
+  T x[PER][8];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const int u = (tid + e * kSelThreads) / HD, c = tid % HD;
+    const T* const q = (const T*)a.q + min(t + u, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + c;
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+      if (u < TT && h < A.G) x[e][h] = q[h * HD];
+  }
   const int i = seq_of(a.s, t, lane);
+  // turn n of the warp has the pages from (n C kSelWarps + rank kSelWarps + warp) PAGES on; their ids,
+  // of IDS turns at once, by lanes (what lies behind the sequence's pages may be anything)
+  const int32_t* const row = a.s.table + (int64_t)max(i, 0) * a.s.max_pages;
+  const int turn = (int)C * kSelWarps * PAGES, j_first = ((int)rank * kSelWarps + warp) * PAGES;
+  auto ids_of = [&](int n) {
+    const int64_t j = (int64_t)(n + lane / PAGES) * turn + j_first + lane % PAGES;
+    return j < A.slots && a.first + j < a.s.max_pages ? row[a.first + j] : -1;
+  };
+  int ids = ids_of(0), ids_next = ids_of(IDS);
   Rows s{};
   bool ok = i >= 0;
   if (ok) {
@@ -270,11 +340,12 @@ __global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kerne
   }
   if (TT > 1 && (t - s.t0) % TT != 0) return;
   const int tokens = min(TT, s.t0 + s.m - t);
-  const int32_t* const row = a.s.table + (int64_t)i * a.s.max_pages;
   auto list_of = [&](int u) { return a.pages + ((int64_t)(t + u) * A.p.nkv + g) * a.budget; };
-  // what is in without a score
   const int r = a.budget - a.first - a.last;
-  if (rank == 0) {
+  auto scored = [&](int u) { const int N = pages_of(p0 + u); return u < tokens && N > a.budget ? N - a.first - a.last : 0; };
+  const int M = scored(tokens - 1);                // of the last token: the most
+  // what is in without a score
+  auto always = [&]() {
     for (int u = 0; u < tokens; ++u) {
       const int N = pages_of(p0 + u);
       int32_t* const out = list_of(u);
@@ -285,72 +356,95 @@ __global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kerne
         for (int j = tid; j < a.last; j += kSelThreads) out[a.budget - a.last + j] = row[N - a.last + j];
       }
     }
+  };
+  if (M == 0 || r == 0) {                          // (the same in the whole cluster)
+    if (rank == 0) always();
+    return;
   }
-  auto scored = [&](int u) { const int N = pages_of(p0 + u); return u < tokens && N > a.budget ? N - a.first - a.last : 0; };
-  const int M = scored(tokens - 1);                // of the last token: the most
-  if (M == 0 || r == 0) return;                    // (the same in the whole cluster)
   if (CL) ptx::cluster_arrive_started();
 
   // ---- scores
-  float f[TT][8];
-#pragma unroll
-  for (int u = 0; u < TT; ++u) {
-    const bool high = lane % LPP >= LPP / 2;
-    const T* q = (const T*)a.q + (t + min(u, tokens - 1)) * a.q_stride + (int64_t)g * A.G * HD + lane % (LPP / 2) * 8;
-    for (int h = 0; h < A.G; ++h) {
-      float x[8];
-      load8(q + h * HD, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float y = isnan(x[e]) ? x[e] : high ? fmaxf(x[e], 0.f) : fminf(x[e], 0.f);
-        f[u][e] = h == 0 ? y : __fadd_rn(f[u][e], y);
-      }
-    }
-  }
+  const int turns = M > j_first ? (M - j_first + turn - 1) / turn : 0;
+  const uint32_t ring = ptx::smem_u32(sel_smem) + (uint32_t)(warp * TURNS * LOADS * 512 + lane * 16);
   const __half* const bounds = (const __half*)a.bounds + (int64_t)g * 2 * HD + lane % LPP * 8;
   const int64_t per_page = (int64_t)A.p.nkv * 2 * HD;
+  uint32_t gone = 0;                               // of the loads in flight and the one at hand, LOADS bits a turn, the newest lowest
+  auto issue = [&](int n, int at) {                // (a turn that is not there copies nothing: the counts of groups go on)
+    gone <<= LOADS;
+    if (n < turns) {
+      if (n > 0 && n % IDS == 0) ids = ids_next, ids_next = ids_of(n + IDS);
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) {
+        const int id = __shfl_sync(0xffffffffu, ids, n % IDS * PAGES + k * PPW + lane / LPP);
+        const bool there = (uint32_t)id < (uint32_t)A.p.n_pages;
+        gone |= there ? 0u : 1u << k;
+        copy16(ring + (at * LOADS + k) * 512, bounds + (there ? id : 0) * per_page, there);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int n = 0; n < TURNS; ++n) issue(n, n);
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const int u = (tid + e * kSelThreads) / HD, c = tid % HD;
+    if (u >= TT) continue;
+    float up = 0.f, down = 0.f;
+#pragma unroll
+    for (int h = 0; h < 8; ++h) {
+      if (h >= A.G) continue;
+      const float y = to_f(x[e][h]), y0 = isnan(y) ? y : fminf(y, 0.f), y1 = isnan(y) ? y : fmaxf(y, 0.f);
+      down = h == 0 ? y0 : __fadd_rn(down, y0);
+      up = h == 0 ? y1 : __fadd_rn(up, y1);
+    }
+    s_q[u][0][c] = down;
+    s_q[u][1][c] = up;
+  }
+  __syncthreads();
+  float f[TT][8];                                  // this lane's eight channels, of lo or of hi
+#pragma unroll
+  for (int u = 0; u < TT; ++u) {
+    const float4* const y = reinterpret_cast<const float4*>(&s_q[u][0][0] + lane % LPP * 8);
+    const float4 y0 = y[0], y1 = y[1];
+    f[u][0] = y0.x, f[u][1] = y0.y, f[u][2] = y0.z, f[u][3] = y0.w;
+    f[u][4] = y1.x, f[u][5] = y1.y, f[u][6] = y1.z, f[u][7] = y1.w;
+  }
   bool lost = false;
   uint32_t low[TT], top[TT];
 #pragma unroll
   for (int u = 0; u < TT; ++u) low[u] = 0xFFFFFFFFu, top[u] = 0u;
   if (CL) ptx::cluster_wait_started();
-  for (int j0 = ((int)rank * kSelWarps + warp) * LOADS * PPW; j0 < M; j0 += (int)C * kSelWarps * LOADS * PPW) {
-    uint4 w[LOADS];
-    uint32_t gone = 0;                             // loads whose page is not there
-#pragma unroll
-    for (int k = 0; k < LOADS; ++k) {
-      const int j = j0 + k * PPW + lane / LPP;
-      const int id = j < M ? row[a.first + j] : 0;
-      const bool there = (uint32_t)id < (uint32_t)A.p.n_pages;
-      gone |= there ? 0u : 1u << k;
-      w[k] = there ? __ldg(reinterpret_cast<const uint4*>(bounds + id * per_page)) : make_uint4(0, 0, 0, 0);
-    }
+  for (int n = 0, at = 0; n < turns; ++n, at = at + 1 == TURNS ? 0 : at + 1) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");
     float v[V];
 #pragma unroll
     for (int k = 0; k < LOADS; ++k) {
-      const float2 y[4] = {__half22float2(as_h2(w[k].x)), __half22float2(as_h2(w[k].y)), __half22float2(as_h2(w[k].z)),
-                           __half22float2(as_h2(w[k].w))};
+      const uint4 w = *reinterpret_cast<const uint4*>(sel_smem + ((warp * TURNS + at) * LOADS + k) * 512 + lane * 16);
+      const float2 y[4] = {__half22float2(as_h2(w.x)), __half22float2(as_h2(w.y)), __half22float2(as_h2(w.z)),
+                           __half22float2(as_h2(w.w))};
 #pragma unroll
       for (int u = 0; u < TT; ++u) {
-        float x[8];
+        float z[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[2 * e] = __fmul_rn(f[u][2 * e], y[e].x), x[2 * e + 1] = __fmul_rn(f[u][2 * e + 1], y[e].y);
+        for (int e = 0; e < 4; ++e) z[2 * e] = __fmul_rn(f[u][2 * e], y[e].x), z[2 * e + 1] = __fmul_rn(f[u][2 * e + 1], y[e].y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __fadd_rn(x[e], x[e + 4]);
-        v[k * TT + u] = __fadd_rn(__fadd_rn(x[0], x[2]), __fadd_rn(x[1], x[3]));
+        for (int e = 0; e < 4; ++e) z[e] = __fadd_rn(z[e], z[e + 4]);
+        v[k * TT + u] = __fadd_rn(__fadd_rn(z[0], z[2]), __fadd_rn(z[1], z[3]));
       }
     }
     int base;
     sum_lanes<HD, V>(v, lane, &base);
+    const uint32_t missing = gone >> ((TURNS - 1) * LOADS);
+    issue(n + TURNS, at);                          // (what this turn has read has been used)
     constexpr int LEFT = V > LPP ? V / LPP : 1;    // values that a lane is left with
     // lanes that differ in these bits only are left with the same
     constexpr int TWINS = V >= LPP ? 0 : V == LPP / 2 ? LPP / 2 : LPP / 2 + LPP / (2 * V) - 1;
 #pragma unroll
-    for (int x = 0; x < LEFT; ++x) {
-      const int k = (base + x) / TT, u = (base + x) % TT, j = j0 + k * PPW + lane / LPP;
+    for (int e = 0; e < LEFT; ++e) {
+      const int k = (base + e) / TT, u = (base + e) % TT, j = n * turn + j_first + k * PPW + lane / LPP;
       if (j >= scored(u) || (lane & TWINS)) continue;
-      const bool there = !(gone >> k & 1);
-      const uint32_t key = there ? key_of(v[x]) : 0u;
+      const bool there = !(missing >> k & 1);
+      const uint32_t key = there ? key_of(v[e]) : 0u;
       lost |= !there;
       if (CL) put_first(&keys[j], key);
       else keys[u * A.slots + j] = key;
@@ -370,6 +464,7 @@ __global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kerne
       else s_lo[u][at] = low[u], s_hi[u][at] = top[u];
     }
   }
+  if (rank == 0) always();
   if (CL) {
     ptx::cluster_sync();
     if (rank != 0) return;
@@ -381,19 +476,17 @@ __global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kerne
   for (int u = 0; u < tokens; ++u) {
     const int m = scored(u);
     if (m == 0) continue;
-    const uint32_t* const mine = keys + u * A.slots;
+    const Keys mine(keys + u * A.slots, m, warp, lane);
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
-    for (int x = lane; x < (int)C * kSelWarps; x += 32) lo = min(lo, s_lo[u][x]), hi = max(hi, s_hi[u][x]);
+    for (int y = lane; y < (int)C * kSelWarps; y += 32) lo = min(lo, s_lo[u][y]), hi = max(hi, s_hi[u][y]);
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t at = threshold(mine, m, r, lo, hi, bins, tid, lane);
-    const int run = (m + kSelThreads - 1) / kSelThreads * 32, end = min(m, (warp + 1) * run);   // of a warp
+    const uint32_t at = threshold(mine, r, lo, hi, bins, tid, lane);
     int above = 0, equal = 0;
-    for (int j = warp * run + lane; j - lane < end; j += 32) {
-      const uint32_t k = j < end ? mine[j] : 0u;
-      above += __popc(__ballot_sync(0xffffffffu, j < end && k > at));
-      equal += __popc(__ballot_sync(0xffffffffu, j < end && k == at));
-    }
+    mine.each(lane, [&](uint32_t k, int, bool there) {
+      above += __popc(__ballot_sync(0xffffffffu, there && k > at));
+      equal += __popc(__ballot_sync(0xffffffffu, there && k == at));
+    });
     if (lane == 0) s_above[warp] = above, s_equal[warp] = equal;
     bins[0][tid] = bins[1][tid] = 0;               // for the next token
     __syncthreads();
@@ -407,14 +500,13 @@ __global__ void __launch_bounds__(kSelThreads, TT == 1 ? 4 : 2) kv4_select_kerne
     const int left = r - all_above;                // of those with the r-th score
     const uint32_t below = (1u << lane) - 1;
     int32_t* const out = list_of(u) + a.first;
-    for (int j = warp * run + lane; j - lane < end; j += 32) {
-      const uint32_t k = j < end ? mine[j] : 0u;
-      const uint32_t up = __ballot_sync(0xffffffffu, j < end && k > at), eq = __ballot_sync(0xffffffffu, j < end && k == at);
+    mine.each(lane, [&](uint32_t k, int j, bool there) {
+      const uint32_t up = __ballot_sync(0xffffffffu, there && k > at), eq = __ballot_sync(0xffffffffu, there && k == at);
       const int ups = n_above + __popc(up & below), eqs = n_equal + __popc(eq & below);
       if ((up >> lane & 1) || ((eq >> lane & 1) && eqs < left)) out[ups + min(eqs, left)] = row[a.first + j];
       n_above += __popc(up);
       n_equal += __popc(eq);
-    }
+    });
     if (TT > 1) __syncthreads();                   // (the warps' counts have been read)
   }
 }
@@ -434,8 +526,8 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
   const int64_t ctas = (int64_t)A.a.s.n_tok * A.p.nkv * C;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = kv4_select_kernel<T, HD, TT, CL>;
-  const size_t smem = sizeof(uint32_t) * (size_t)TT * A.slots;
-  if (smem > 32 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+  const size_t smem = sel_ring<TT, CL>() + sizeof(uint32_t) * (size_t)TT * A.slots;
+  if (smem > 24 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   if (!CL) return launch_k(kern, (unsigned)ctas, kSelThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
   if (C > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return BUDDY_ERR_CUDA;
@@ -462,10 +554,10 @@ constexpr int kSelTokens = 4;
 template <typename T, int HD>
 static int dispatch_select(SelectArgs A, cudaStream_t s) {
   A.slots = std::max(1, A.a.s.max_pages - A.a.first - A.a.last);
-  if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= kSelMaxPages) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
+  if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
   const int64_t units = (int64_t)A.a.s.n_tok * A.p.nkv;
   int C = 1;
-  while (C < kSelCluster && 2 * C * kSelWarps * 8 * (128 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
+  while (C < kSelCluster && 2 * C * kSelWarps * kSelLoads * (128 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
   return C > 1 ? launch_select<T, HD, 1, true>(A, C, s) : launch_select<T, HD, 1, false>(A, 1, s);
 }
 

@@ -219,7 +219,7 @@ def test_select_ties_go_to_the_lower_position(levels):
 
 def test_select_many_pages():
     """Up to the largest table there may be."""
-    for n_pages in (255, 256, 257, 4095, 10001, 49152):
+    for n_pages in (255, 256, 257, 4095, 10001, 40000):
         lens = [n_pages * 16 - 5, 16 * 40]
         made = make_select(lens, [1, 1], 16, (2, 1, 64), torch.bfloat16, seed=n_pages, max_pages=n_pages)
         for budget in (3, 64, 3000 if n_pages > 3000 else 100, n_pages - 1):

@@ -113,11 +113,11 @@ def test_bounds_refuse(lib, bad):
 @pytest.mark.parametrize("bad", [dict(s=seqs(**b)) for b in BAD_SEQS] + [
     dict(n_q_heads=1), dict(n_q_heads=5), dict(n_q_heads=18), dict(q_dtype=2), dict(budget=1), dict(first=-1), dict(last=0),
     dict(first=2 ** 31 - 1, last=2), dict(q=None), dict(q=P + 8), dict(q_stride=257), dict(bounds=None), dict(bounds=P + 8),
-    dict(pages=None), dict(visible=None), dict(s=seqs(max_pages=49153))])
+    dict(pages=None), dict(visible=None), dict(s=seqs(max_pages=40001))])
 def test_select_refuses(lib, bad):
     good = dict(s=seqs(), n_q_heads=4, q_dtype=1, budget=4, first=1, last=1, q=P, q_stride=256, bounds=P, pages=P, visible=P)
     a = B.buddy_kv4_select_args(**{**good, **bad})
-    want = B.BUDDY_ERR_RANGE if a.s.max_pages == 49153 else B.BUDDY_ERR_ARG
+    want = B.BUDDY_ERR_RANGE if a.s.max_pages == 40001 else B.BUDDY_ERR_ARG
     assert lib.buddy_kv4_select(ctypes.byref(cache()), ctypes.byref(a), None, None) == want
     assert lib.buddy_kv4_select(ctypes.byref(cache()), None, None, None) == B.BUDDY_ERR_ARG
 
