@@ -120,8 +120,7 @@ __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const Boun
 }
 
 // ------------------------------------------------------------------ selection
-constexpr int kSelWarps = 8;
-constexpr int kSelThreads = 32 * kSelWarps;
+constexpr int kSelWarps = 8;            // of a CTA at most
 constexpr int kSelMaxPages = 40000;     // a score each in shared memory, next to the copies in flight
 constexpr int kSelCluster = 16;         // most CTAs of a (token, KV head)
 constexpr int kSelBins = 256;
@@ -188,52 +187,90 @@ __device__ __forceinline__ void sum_lanes(float (&v)[V], int lane, int* base) {
   *base = at;
 }
 
-// What a thread has of M keys: warp w those from w * run on, 32 at a time. Up to kSelKept of them
-// stay in registers, more in shared memory.
+// The warps that look for a token's best pages: WARPS of a CTA's, the bar-th such group.
+template <int WARPS>
+struct Group {
+  int tid, lane, warp, bar;
+  __device__ __forceinline__ void sync() const {
+    asm volatile("bar.sync %0, %1;" ::"r"(bar + 1), "n"(32 * WARPS) : "memory");
+  }
+};
+
+// What a thread has of M keys, and the ids of their pages: a warp those from `first` on, 32 at a
+// time. Up to kSelKept of them stay in registers, more in shared memory.
 constexpr int kSelKept = 8;
+template <int WARPS>
 struct Keys {
   const uint32_t* all;
+  const int32_t* ids;
   int first, end;                                  // of the warp
   bool few;
   uint32_t kept[kSelKept];
-  __device__ __forceinline__ Keys(const uint32_t* keys, int M, int warp, int lane) : all(keys) {
-    const int run = (M + kSelThreads - 1) / kSelThreads * 32;
-    first = warp * run;
+  int32_t page[kSelKept];
+  __device__ __forceinline__ Keys(const uint32_t* keys, const int32_t* row, int M, const Group<WARPS>& G) : all(keys), ids(row) {
+    const int run = (M + 32 * WARPS - 1) / (32 * WARPS) * 32;
+    first = G.warp * run;
     end = min(M, first + run);
     few = run <= kSelKept * 32;
     if (few) {
 #pragma unroll
-      for (int k = 0; k < kSelKept; ++k) kept[k] = first + 32 * k + lane < end ? keys[first + 32 * k + lane] : 0u;
+      for (int k = 0; k < kSelKept; ++k) {
+        const int j = first + 32 * k + G.lane;
+        kept[k] = j < end ? keys[j] : 0u;
+        page[k] = j < end ? row[j] : 0;
+      }
     }
   }
-  // f(key, index, true where there is one), a warp together
+  // f(key, index, true where there is one, id()), a warp together
   template <typename F>
   __device__ __forceinline__ void each(int lane, F&& f) const {
     if (few) {
 #pragma unroll
       for (int k = 0; k < kSelKept; ++k)
-        if (first + 32 * k < end) f(kept[k], first + 32 * k + lane, first + 32 * k + lane < end);
+        if (first + 32 * k < end) f(kept[k], first + 32 * k + lane < end, [&] { return page[k]; });
     } else {
 #pragma unroll 4
-      for (int j = first + lane; j - lane < end; j += 32) f(j < end ? all[j] : 0u, j, j < end);
+      for (int j = first + lane; j - lane < end; j += 32) f(j < end ? all[j] : 0u, j < end, [&] { return ids[j]; });
     }
   }
 };
 
+// A group's scratch.
+constexpr int kSelFew = 64;
+struct Search {
+  __align__(16) int bins[kSelBins];                // zeros before and after
+  uint32_t few[kSelFew];
+  int n_few;                                       // as bins
+  int above[kSelWarps], equal[kSelWarps];          // of each warp
+};
+
+// The r-th largest of n <= kSelFew keys, by every warp.
+__device__ __forceinline__ uint32_t rank_few(const uint32_t* few, int n, int r, int lane) {
+  const uint32_t k0 = lane < n ? few[lane] : 0u, k1 = lane + 32 < n ? few[lane + 32] : 0u;
+  int g0 = 0, g1 = 0, e0 = 0, e1 = 0;              // larger ones, equal ones
+  for (int x = 0; x < n; ++x) {
+    const uint32_t k = few[x];
+    g0 += k > k0, e0 += k == k0, g1 += k > k1, e1 += k == k1;
+  }
+  const uint32_t h0 = __ballot_sync(0xffffffffu, lane < n && g0 < r && g0 + e0 >= r);
+  const uint32_t h1 = __ballot_sync(0xffffffffu, lane + 32 < n && g1 < r && g1 + e1 >= r);
+  return h0 ? __shfl_sync(0xffffffffu, k0, __ffs(h0) - 1) : __shfl_sync(0xffffffffu, k1, __ffs(h1) - 1);
+}
+
 // Where the best r of the keys end: just r of them are above what is returned, or these and the first
 // of those equal to it. By counts of the keys in 256 parts of the range [lo, hi] that holds the r-th,
-// from the top, until a part is one value or its keys are all wanted. bins: two sets, zeros.
-__device__ __forceinline__ uint32_t threshold(const Keys& keys, int r, uint32_t lo, uint32_t hi, int (*bins)[kSelBins],
-                                              int tid, int lane) {
-  for (int set = 0;; set ^= 1) {
+// from the top, until a part's keys are all wanted, are few, or are one value.
+template <int WARPS>
+__device__ __forceinline__ uint32_t threshold(const Keys<WARPS>& keys, int r, uint32_t lo, uint32_t hi, Search& S,
+                                              const Group<WARPS>& G) {
+  for (;;) {
     const int shift = max(0, 32 - __clz(hi - lo) - 8);       // ((hi - lo) >> shift) < 256
-    keys.each(lane, [&](uint32_t k, int, bool there) {
-      if (there && k >= lo && k <= hi) atomicAdd(&bins[set][(k - lo) >> shift], 1);
+    keys.each(G.lane, [&](uint32_t k, bool there, auto) {
+      if (there && k >= lo && k <= hi) atomicAdd(&S.bins[(k - lo) >> shift], 1);
     });
-    __syncthreads();
-    bins[set ^ 1][tid] = 0;
+    G.sync();
     // every warp: lane x has the parts from 255 - 8 x down
-    const int4* const mine = reinterpret_cast<const int4*>(bins[set] + 248 - 8 * lane);
+    const int4* const mine = reinterpret_cast<const int4*>(S.bins + 248 - 8 * G.lane);
     const int4 y0 = mine[1], y1 = mine[0];
     const int c[8] = {y0.w, y0.z, y0.y, y0.x, y1.w, y1.z, y1.y, y1.x};
     int sum = 0;
@@ -243,22 +280,32 @@ __device__ __forceinline__ uint32_t threshold(const Keys& keys, int r, uint32_t 
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
+      if (G.lane >= o) upto += y;
     }
     const int src = __ffs(__ballot_sync(0xffffffffu, upto >= r)) - 1;
-    int before = upto - sum, part = 255 - 8 * lane, in = c[0];
+    int before = upto - sum, part = 255 - 8 * G.lane, in = c[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e)
-      if (before + in < r) before += in, in = c[e], part = 255 - 8 * lane - e;
+      if (before + in < r) before += in, in = c[e], part = 255 - 8 * G.lane - e;
     before = __shfl_sync(0xffffffffu, before, src);
     part = __shfl_sync(0xffffffffu, part, src);
     in = __shfl_sync(0xffffffffu, in, src);
     r -= before;
     lo += (uint32_t)part << shift;
     hi = lo + min(hi - lo, (1u << shift) - 1);
-    __syncthreads();                               // (the other set is zero, this one has been read)
+    G.sync();                                      // (the counts have been read)
+    for (int b = G.tid; b < kSelBins; b += 32 * WARPS) S.bins[b] = 0;
     if (shift == 0) return lo;
     if (in == r) return lo - 1;                    // (lo > 0: not all of the keys are wanted)
+    if (in <= kSelFew) {
+      keys.each(G.lane, [&](uint32_t k, bool there, auto) {
+        if (there && k >= lo && k <= hi) S.few[atomicAdd(&S.n_few, 1)] = k;
+      });
+      G.sync();
+      if (G.tid == 0) S.n_few = 0;
+      return rank_few(S.few, in, r, G.lane);
+    }
+    G.sync();
   }
 }
 
@@ -266,14 +313,15 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// Pages of a warp's turn, as loads of 16 bytes per lane; turns in flight.
-constexpr int kSelLoads = 4;
+// The forms of the kernel: one token by a CTA, one by a cluster, four of a sequence by a CTA.
+// Loads of 16 bytes per lane in a turn of a warp, turns in flight, warps, and those that look for
+// the pages of one token.
 template <int TT, bool CL>
-__host__ __device__ constexpr int sel_turns() { return TT == 1 && !CL ? 2 : 4; }
-template <int TT, bool CL>
-__host__ __device__ constexpr int sel_ring() { return kSelWarps * sel_turns<TT, CL>() * kSelLoads * 512; }   // bytes
-template <int TT>
-__host__ __device__ constexpr int sel_ctas() { return TT == 1 ? 4 : 2; }                                      // per SM
+struct Form {
+  static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 8 : 4,
+                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kCtas = TT == 1 && !CL ? 7 : 2;
+  static constexpr int kRing = kWarps * kTurns * kLoads * 512;   // bytes
+};
 
 // Up to TT tokens of a sequence share a walk over its pages' bounds; the CTA of the first of
 // them does the work of all. CL: a cluster has one token, its CTAs the pages in turn, and the first
@@ -281,41 +329,43 @@ __host__ __device__ constexpr int sel_ctas() { return TT == 1 ? 4 : 2; }        
 // of eight channels, by b, or the largest, by a. Every lane reads what it has copied itself, so
 // that the turns in flight need neither registers nor barriers.
 template <typename T, int HD, int TT, bool CL>
-__global__ void __launch_bounds__(kSelThreads, sel_ctas<TT>()) kv4_select_kernel(const SelectArgs A) {
+__global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
+  using F = Form<TT, CL>;
   extern __shared__ __align__(128) uint8_t sel_smem[];
-  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + sel_ring<TT, CL>());   // [TT][slots]
-  __shared__ __align__(16) int bins[2][kSelBins];
-  __shared__ uint32_t s_lo[TT][kSelCluster * kSelWarps], s_hi[TT][kSelCluster * kSelWarps];
-  __shared__ int s_above[kSelWarps], s_equal[kSelWarps];
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots]
+  constexpr int WARPS = F::kWarps, THREADS = F::kThreads, MOST = CL ? kSelCluster * WARPS : WARPS;
+  __shared__ Search search[TT];
+  __shared__ uint32_t s_lo[TT][MOST], s_hi[TT][MOST];
   __shared__ __align__(16) float s_q[TT][2][HD];   // a token's b, then its a
   static_assert(!CL || TT == 1, "");
   constexpr int LPP = HD / 4, PPW = 32 / LPP;      // lanes of a page, pages of a warp's load
-  constexpr int LOADS = kSelLoads, V = LOADS * TT; // of a turn, and their scores
-  constexpr int TURNS = sel_turns<TT, CL>(), PAGES = LOADS * PPW, IDS = 32 / PAGES;   // turns whose ids a warp reads at once
+  constexpr int LOADS = F::kLoads, V = LOADS * TT; // of a turn, and their scores
+  constexpr int TURNS = F::kTurns, PAGES = LOADS * PPW, IDS = 32 / PAGES;   // turns whose ids a warp reads at once
   const buddy_kv4_select_args& a = A.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = CL ? ptx::cluster_rank() : 0, C = CL ? ptx::cluster_size() : 1;
   const unsigned unit = blockIdx.x / C;
   const int g = (int)(unit % (unsigned)A.p.nkv), t = (int)(unit / (unsigned)A.p.nkv);
-  bins[0][tid] = bins[1][tid] = 0;
+  for (int b = tid; b < TT * kSelBins; b += THREADS) search[b / kSelBins].bins[b % kSelBins] = 0;
+  if (tid < TT) search[tid].n_few = 0;
   pdl_wait();
   pdl_trigger();
   // (the queries are on their way while the token's sequence is looked for)
-  constexpr int PER = (TT * HD + kSelThreads - 1) / kSelThreads;
+  constexpr int PER = (TT * HD + THREADS - 1) / THREADS;
   T x[PER][8];
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
-    const int u = (tid + e * kSelThreads) / HD, c = tid % HD;
+    const int u = (tid + e * THREADS) / HD, c = tid % HD;
     const T* const q = (const T*)a.q + min(t + u, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + c;
 #pragma unroll
     for (int h = 0; h < 8; ++h)
       if (u < TT && h < A.G) x[e][h] = q[h * HD];
   }
   const int i = seq_of(a.s, t, lane);
-  // turn n of the warp has the pages from (n C kSelWarps + rank kSelWarps + warp) PAGES on; their ids,
+  // turn n of the warp has the pages from (n C WARPS + rank WARPS + warp) PAGES on; their ids,
   // of IDS turns at once, by lanes (what lies behind the sequence's pages may be anything)
   const int32_t* const row = a.s.table + (int64_t)max(i, 0) * a.s.max_pages;
-  const int turn = (int)C * kSelWarps * PAGES, j_first = ((int)rank * kSelWarps + warp) * PAGES;
+  const int turn = (int)C * WARPS * PAGES, j_first = ((int)rank * WARPS + warp) * PAGES;
   auto ids_of = [&](int n) {
     const int64_t j = (int64_t)(n + lane / PAGES) * turn + j_first + lane % PAGES;
     return j < A.slots && a.first + j < a.s.max_pages ? row[a.first + j] : -1;
@@ -350,10 +400,10 @@ __global__ void __launch_bounds__(kSelThreads, sel_ctas<TT>()) kv4_select_kernel
       const int N = pages_of(p0 + u);
       int32_t* const out = list_of(u);
       if (N <= a.budget) {
-        for (int j = tid; j < a.budget; j += kSelThreads) out[j] = j < N ? row[j] : -1;
+        for (int j = tid; j < a.budget; j += THREADS) out[j] = j < N ? row[j] : -1;
       } else {
-        for (int j = tid; j < a.first; j += kSelThreads) out[j] = row[j];
-        for (int j = tid; j < a.last; j += kSelThreads) out[a.budget - a.last + j] = row[N - a.last + j];
+        for (int j = tid; j < a.first; j += THREADS) out[j] = row[j];
+        for (int j = tid; j < a.last; j += THREADS) out[a.budget - a.last + j] = row[N - a.last + j];
       }
     }
   };
@@ -385,9 +435,10 @@ __global__ void __launch_bounds__(kSelThreads, sel_ctas<TT>()) kv4_select_kernel
   };
 #pragma unroll
   for (int n = 0; n < TURNS; ++n) issue(n, n);
+  if (rank == 0) always();
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
-    const int u = (tid + e * kSelThreads) / HD, c = tid % HD;
+    const int u = (tid + e * THREADS) / HD, c = tid % HD;
     if (u >= TT) continue;
     float up = 0.f, down = 0.f;
 #pragma unroll
@@ -459,12 +510,11 @@ __global__ void __launch_bounds__(kSelThreads, sel_ctas<TT>()) kv4_select_kernel
     low[u] = __reduce_min_sync(0xffffffffu, low[u]);
     top[u] = __reduce_max_sync(0xffffffffu, top[u]);
     if (lane == 0) {
-      const int at = (int)rank * kSelWarps + warp;
+      const int at = (int)rank * WARPS + warp;
       if (CL) put_first(&s_lo[u][at], low[u]), put_first(&s_hi[u][at], top[u]);
       else s_lo[u][at] = low[u], s_hi[u][at] = top[u];
     }
   }
-  if (rank == 0) always();
   if (CL) {
     ptx::cluster_sync();
     if (rank != 0) return;
@@ -472,43 +522,41 @@ __global__ void __launch_bounds__(kSelThreads, sel_ctas<TT>()) kv4_select_kernel
     __syncthreads();
   }
 
-  // ---- the best r, in their order
-  for (int u = 0; u < tokens; ++u) {
-    const int m = scored(u);
-    if (m == 0) continue;
-    const Keys mine(keys + u * A.slots, m, warp, lane);
-    uint32_t lo = 0xFFFFFFFFu, hi = 0;
-    for (int y = lane; y < (int)C * kSelWarps; y += 32) lo = min(lo, s_lo[u][y]), hi = max(hi, s_hi[u][y]);
-    lo = __reduce_min_sync(0xffffffffu, lo);
-    hi = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t at = threshold(mine, r, lo, hi, bins, tid, lane);
-    int above = 0, equal = 0;
-    mine.each(lane, [&](uint32_t k, int, bool there) {
-      above += __popc(__ballot_sync(0xffffffffu, there && k > at));
-      equal += __popc(__ballot_sync(0xffffffffu, there && k == at));
-    });
-    if (lane == 0) s_above[warp] = above, s_equal[warp] = equal;
-    bins[0][tid] = bins[1][tid] = 0;               // for the next token
-    __syncthreads();
-    int n_above = 0, n_equal = 0, all_above = 0;
+  // ---- the best r, in their order: each token by a group of warps
+  const int u = warp / F::kGroup, m = scored(u);
+  if (m == 0) return;
+  const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, u};
+  Search& S = search[u];
+  const Keys<F::kGroup> mine(keys + u * A.slots, row + a.first, m, G);
+  uint32_t lo = 0xFFFFFFFFu, hi = 0;
+  for (int y = lane; y < (int)C * WARPS; y += 32) lo = min(lo, s_lo[u][y]), hi = max(hi, s_hi[u][y]);
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  const uint32_t at = m <= kSelFew ? rank_few(mine.all, m, r, lane) : threshold(mine, r, lo, hi, S, G);
+  int above = 0, equal = 0;
+  mine.each(lane, [&](uint32_t k, bool there, auto) {
+    above += __popc(__ballot_sync(0xffffffffu, there && k > at));
+    equal += __popc(__ballot_sync(0xffffffffu, there && k == at));
+  });
+  if (lane == 0) S.above[G.warp] = above, S.equal[G.warp] = equal;
+  G.sync();
+  int n_above = 0, n_equal = 0, all_above = 0;
 #pragma unroll
-    for (int w = 0; w < kSelWarps; ++w) {
-      if (w == warp) n_above = all_above;
-      if (w < warp) n_equal += s_equal[w];
-      all_above += s_above[w];
-    }
-    const int left = r - all_above;                // of those with the r-th score
-    const uint32_t below = (1u << lane) - 1;
-    int32_t* const out = list_of(u) + a.first;
-    mine.each(lane, [&](uint32_t k, int j, bool there) {
-      const uint32_t up = __ballot_sync(0xffffffffu, there && k > at), eq = __ballot_sync(0xffffffffu, there && k == at);
-      const int ups = n_above + __popc(up & below), eqs = n_equal + __popc(eq & below);
-      if ((up >> lane & 1) || ((eq >> lane & 1) && eqs < left)) out[ups + min(eqs, left)] = row[a.first + j];
-      n_above += __popc(up);
-      n_equal += __popc(eq);
-    });
-    if (TT > 1) __syncthreads();                   // (the warps' counts have been read)
+  for (int w = 0; w < F::kGroup; ++w) {
+    if (w == G.warp) n_above = all_above;
+    if (w < G.warp) n_equal += S.equal[w];
+    all_above += S.above[w];
   }
+  const int left = r - all_above;                  // of those with the r-th score
+  const uint32_t below = (1u << lane) - 1;
+  int32_t* const out = list_of(u) + a.first;
+  mine.each(lane, [&](uint32_t k, bool there, auto id) {
+    const uint32_t up = __ballot_sync(0xffffffffu, there && k > at), eq = __ballot_sync(0xffffffffu, there && k == at);
+    const int ups = n_above + __popc(up & below), eqs = n_equal + __popc(eq & below);
+    if ((up >> lane & 1) || ((eq >> lane & 1) && eqs < left)) out[ups + min(eqs, left)] = id();
+    n_above += __popc(up);
+    n_equal += __popc(eq);
+  });
 }
 
 }  // namespace kv4
@@ -526,14 +574,15 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
   const int64_t ctas = (int64_t)A.a.s.n_tok * A.p.nkv * C;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = kv4_select_kernel<T, HD, TT, CL>;
-  const size_t smem = sel_ring<TT, CL>() + sizeof(uint32_t) * (size_t)TT * A.slots;
+  using F = Form<TT, CL>;
+  const size_t smem = F::kRing + sizeof(uint32_t) * (size_t)TT * A.slots;
   if (smem > 24 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
-  if (!CL) return launch_k(kern, (unsigned)ctas, kSelThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  if (!CL) return launch_k(kern, (unsigned)ctas, F::kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
   if (C > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return BUDDY_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = (unsigned)ctas;
-  cfg.blockDim = kSelThreads;
+  cfg.blockDim = F::kThreads;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute at[2];
@@ -557,7 +606,7 @@ static int dispatch_select(SelectArgs A, cudaStream_t s) {
   if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
   const int64_t units = (int64_t)A.a.s.n_tok * A.p.nkv;
   int C = 1;
-  while (C < kSelCluster && 2 * C * kSelWarps * kSelLoads * (128 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
+  while (C < kSelCluster && 2 * C * Form<1, true>::kWarps * Form<1, true>::kLoads * (128 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
   return C > 1 ? launch_select<T, HD, 1, true>(A, C, s) : launch_select<T, HD, 1, false>(A, 1, s);
 }
 
