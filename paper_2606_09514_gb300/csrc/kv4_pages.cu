@@ -197,40 +197,41 @@ struct Group {
 };
 
 // What a thread has of M keys, and the ids of their pages: a warp those from `first` on, 32 at a
-// time. Up to kSelKept of them stay in registers, more in shared memory.
-constexpr int kSelKept = 8;
-template <int WARPS>
+// time. Up to KEPT of them stay in registers, more in shared memory.
+template <int WARPS, int KEPT>
 struct Keys {
   const uint32_t* all;
   const int32_t* ids;
   int first, end;                                  // of the warp
   bool few;
-  uint32_t kept[kSelKept];
-  int32_t page[kSelKept];
+  uint32_t kept[KEPT];
+  int32_t page[KEPT];
   __device__ __forceinline__ Keys(const uint32_t* keys, const int32_t* row, int M, const Group<WARPS>& G) : all(keys), ids(row) {
     const int run = (M + 32 * WARPS - 1) / (32 * WARPS) * 32;
     first = G.warp * run;
     end = min(M, first + run);
-    few = run <= kSelKept * 32;
+    few = run <= KEPT * 32;
     if (few) {
 #pragma unroll
-      for (int k = 0; k < kSelKept; ++k) {
-        const int j = first + 32 * k + G.lane;
-        kept[k] = j < end ? keys[j] : 0u;
-        page[k] = j < end ? row[j] : 0;
-      }
+      for (int k = 0; k < KEPT; ++k) page[k] = there(k, G.lane) ? row[first + 32 * k + G.lane] : 0;
+#pragma unroll
+      for (int k = 0; k < KEPT; ++k) kept[k] = there(k, G.lane) ? keys[first + 32 * k + G.lane] : 0u;
     }
   }
-  // f(key, index, true where there is one, id()), a warp together
+  __device__ __forceinline__ bool there(int k, int lane) const { return first + 32 * k + lane < end; }
+  // f(key) of those in [lo, hi]
   template <typename F>
-  __device__ __forceinline__ void each(int lane, F&& f) const {
+  __device__ __forceinline__ void within(uint32_t lo, uint32_t hi, int lane, F&& f) const {
     if (few) {
 #pragma unroll
-      for (int k = 0; k < kSelKept; ++k)
-        if (first + 32 * k < end) f(kept[k], first + 32 * k + lane < end, [&] { return page[k]; });
+      for (int k = 0; k < KEPT; ++k)
+        if (there(k, lane) && kept[k] - lo <= hi - lo) f(kept[k]);
     } else {
 #pragma unroll 4
-      for (int j = first + lane; j - lane < end; j += 32) f(j < end ? all[j] : 0u, j < end, [&] { return ids[j]; });
+      for (int j = first + lane; j < end; j += 32) {
+        const uint32_t k = all[j];
+        if (k - lo <= hi - lo) f(k);
+      }
     }
   }
 };
@@ -239,18 +240,23 @@ struct Keys {
 constexpr int kSelFew = 64;
 struct Search {
   __align__(16) int bins[kSelBins];                // zeros before and after
-  uint32_t few[kSelFew];
+  __align__(16) uint32_t few[kSelFew];
   int n_few;                                       // as bins
   int above[kSelWarps], equal[kSelWarps];          // of each warp
 };
 
-// The r-th largest of n <= kSelFew keys, by every warp.
+// The r-th largest of n <= kSelFew keys (16-byte aligned, readable to a multiple of four), by every warp.
 __device__ __forceinline__ uint32_t rank_few(const uint32_t* few, int n, int r, int lane) {
   const uint32_t k0 = lane < n ? few[lane] : 0u, k1 = lane + 32 < n ? few[lane + 32] : 0u;
   int g0 = 0, g1 = 0, e0 = 0, e1 = 0;              // larger ones, equal ones
-  for (int x = 0; x < n; ++x) {
-    const uint32_t k = few[x];
-    g0 += k > k0, e0 += k == k0, g1 += k > k1, e1 += k == k1;
+  auto count = [&](uint32_t k) { g0 += k > k0, e0 += k == k0, g1 += k > k1, e1 += k == k1; };
+#pragma unroll 2
+  for (int x = 0; x < n; x += 4) {
+    const uint4 k = *reinterpret_cast<const uint4*>(few + x);
+    count(k.x);
+    if (x + 1 < n) count(k.y);
+    if (x + 2 < n) count(k.z);
+    if (x + 3 < n) count(k.w);
   }
   const uint32_t h0 = __ballot_sync(0xffffffffu, lane < n && g0 < r && g0 + e0 >= r);
   const uint32_t h1 = __ballot_sync(0xffffffffu, lane + 32 < n && g1 < r && g1 + e1 >= r);
@@ -260,14 +266,12 @@ __device__ __forceinline__ uint32_t rank_few(const uint32_t* few, int n, int r, 
 // Where the best r of the keys end: just r of them are above what is returned, or these and the first
 // of those equal to it. By counts of the keys in 256 parts of the range [lo, hi] that holds the r-th,
 // from the top, until a part's keys are all wanted, are few, or are one value.
-template <int WARPS>
-__device__ __forceinline__ uint32_t threshold(const Keys<WARPS>& keys, int r, uint32_t lo, uint32_t hi, Search& S,
+template <int WARPS, int KEPT>
+__device__ __forceinline__ uint32_t threshold(const Keys<WARPS, KEPT>& keys, int r, uint32_t lo, uint32_t hi, Search& S,
                                               const Group<WARPS>& G) {
   for (;;) {
     const int shift = max(0, 32 - __clz(hi - lo) - 8);       // ((hi - lo) >> shift) < 256
-    keys.each(G.lane, [&](uint32_t k, bool there, auto) {
-      if (there && k >= lo && k <= hi) atomicAdd(&S.bins[(k - lo) >> shift], 1);
-    });
+    keys.within(lo, hi, G.lane, [&](uint32_t k) { atomicAdd(&S.bins[(k - lo) >> shift], 1); });
     G.sync();
     // every warp: lane x has the parts from 255 - 8 x down
     const int4* const mine = reinterpret_cast<const int4*>(S.bins + 248 - 8 * G.lane);
@@ -298,9 +302,12 @@ __device__ __forceinline__ uint32_t threshold(const Keys<WARPS>& keys, int r, ui
     if (shift == 0) return lo;
     if (in == r) return lo - 1;                    // (lo > 0: not all of the keys are wanted)
     if (in <= kSelFew) {
-      keys.each(G.lane, [&](uint32_t k, bool there, auto) {
-        if (there && k >= lo && k <= hi) S.few[atomicAdd(&S.n_few, 1)] = k;
-      });
+      int n = 0;
+      keys.within(lo, hi, G.lane, [&](uint32_t) { ++n; });
+      if (n > 0) {
+        uint32_t* to = S.few + atomicAdd(&S.n_few, n);
+        keys.within(lo, hi, G.lane, [&](uint32_t k) { *to++ = k; });
+      }
       G.sync();
       if (G.tid == 0) S.n_few = 0;
       return rank_few(S.few, in, r, G.lane);
@@ -319,7 +326,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
 template <int TT, bool CL>
 struct Form {
   static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 8 : 4,
-                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kCtas = TT == 1 && !CL ? 7 : 2;
+                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kKept = TT == 1 && !CL ? 4 : 8, kCtas = TT == 1 && !CL ? 7 : 2;
   static constexpr int kRing = kWarps * kTurns * kLoads * 512;   // bytes
 };
 
@@ -332,7 +339,7 @@ template <typename T, int HD, int TT, bool CL>
 __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
   using F = Form<TT, CL>;
   extern __shared__ __align__(128) uint8_t sel_smem[];
-  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots]
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots, a multiple of four]
   constexpr int WARPS = F::kWarps, THREADS = F::kThreads, MOST = CL ? kSelCluster * WARPS : WARPS;
   __shared__ Search search[TT];
   __shared__ uint32_t s_lo[TT][MOST], s_hi[TT][MOST];
@@ -348,19 +355,20 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   const int g = (int)(unit % (unsigned)A.p.nkv), t = (int)(unit / (unsigned)A.p.nkv);
   for (int b = tid; b < TT * kSelBins; b += THREADS) search[b / kSelBins].bins[b % kSelBins] = 0;
   if (tid < TT) search[tid].n_few = 0;
+  constexpr int PER = (TT * HD + THREADS - 1) / THREADS;
+  const T* q[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e)
+    q[e] = (const T*)a.q + min(t + (tid + e * THREADS) / HD, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + tid % HD;
   pdl_wait();
   pdl_trigger();
   // (the queries are on their way while the token's sequence is looked for)
-  constexpr int PER = (TT * HD + THREADS - 1) / THREADS;
   T x[PER][8];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) {
-    const int u = (tid + e * THREADS) / HD, c = tid % HD;
-    const T* const q = (const T*)a.q + min(t + u, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + c;
+  for (int e = 0; e < PER; ++e)
 #pragma unroll
     for (int h = 0; h < 8; ++h)
-      if (u < TT && h < A.G) x[e][h] = q[h * HD];
-  }
+      if ((tid + e * THREADS) / HD < TT && h < A.G) x[e][h] = q[e][h * HD];
   const int i = seq_of(a.s, t, lane);
   // turn n of the warp has the pages from (n C WARPS + rank WARPS + warp) PAGES on; their ids,
   // of IDS turns at once, by lanes (what lies behind the sequence's pages may be anything)
@@ -423,12 +431,14 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     gone <<= LOADS;
     if (n < turns) {
       if (n > 0 && n % IDS == 0) ids = ids_next, ids_next = ids_of(n + IDS);
+      int id[LOADS];
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) id[k] = __shfl_sync(0xffffffffu, ids, n % IDS * PAGES + k * PPW + lane / LPP);
 #pragma unroll
       for (int k = 0; k < LOADS; ++k) {
-        const int id = __shfl_sync(0xffffffffu, ids, n % IDS * PAGES + k * PPW + lane / LPP);
-        const bool there = (uint32_t)id < (uint32_t)A.p.n_pages;
+        const bool there = (uint32_t)id[k] < (uint32_t)A.p.n_pages;
         gone |= there ? 0u : 1u << k;
-        copy16(ring + (at * LOADS + k) * 512, bounds + (there ? id : 0) * per_page, there);
+        copy16(ring + (at * LOADS + k) * 512, bounds + (there ? id[k] : 0) * per_page, there);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -527,17 +537,33 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   if (m == 0) return;
   const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, u};
   Search& S = search[u];
-  const Keys<F::kGroup> mine(keys + u * A.slots, row + a.first, m, G);
+  const Keys<F::kGroup, F::kKept> mine(keys + u * A.slots, row + a.first, m, G);
   uint32_t lo = 0xFFFFFFFFu, hi = 0;
   for (int y = lane; y < (int)C * WARPS; y += 32) lo = min(lo, s_lo[u][y]), hi = max(hi, s_hi[u][y]);
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   const uint32_t at = m <= kSelFew ? rank_few(mine.all, m, r, lane) : threshold(mine, r, lo, hi, S, G);
+  // pages above it in each 32, pages with it; then where these of the warp begin
+  const uint32_t below = (1u << lane) - 1;
+  int32_t* const out = list_of(u) + a.first;
   int above = 0, equal = 0;
-  mine.each(lane, [&](uint32_t k, bool there, auto) {
-    above += __popc(__ballot_sync(0xffffffffu, there && k > at));
-    equal += __popc(__ballot_sync(0xffffffffu, there && k == at));
-  });
+  uint32_t up[F::kKept], eq[F::kKept];
+  if (mine.few) {
+#pragma unroll
+    for (int k = 0; k < F::kKept; ++k) {
+      up[k] = __ballot_sync(0xffffffffu, mine.there(k, lane) && mine.kept[k] > at);
+      eq[k] = __ballot_sync(0xffffffffu, mine.there(k, lane) && mine.kept[k] == at);
+    }
+#pragma unroll
+    for (int k = 0; k < F::kKept; ++k) above += __popc(up[k]), equal += __popc(eq[k]);
+  } else {
+#pragma unroll 4
+    for (int j = mine.first + lane; j - lane < mine.end; j += 32) {
+      const uint32_t k = j < mine.end ? mine.all[j] : 0u;
+      above += __popc(__ballot_sync(0xffffffffu, j < mine.end && k > at));
+      equal += __popc(__ballot_sync(0xffffffffu, j < mine.end && k == at));
+    }
+  }
   if (lane == 0) S.above[G.warp] = above, S.equal[G.warp] = equal;
   G.sync();
   int n_above = 0, n_equal = 0, all_above = 0;
@@ -548,15 +574,22 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     all_above += S.above[w];
   }
   const int left = r - all_above;                  // of those with the r-th score
-  const uint32_t below = (1u << lane) - 1;
-  int32_t* const out = list_of(u) + a.first;
-  mine.each(lane, [&](uint32_t k, bool there, auto id) {
-    const uint32_t up = __ballot_sync(0xffffffffu, there && k > at), eq = __ballot_sync(0xffffffffu, there && k == at);
-    const int ups = n_above + __popc(up & below), eqs = n_equal + __popc(eq & below);
-    if ((up >> lane & 1) || ((eq >> lane & 1) && eqs < left)) out[ups + min(eqs, left)] = id();
-    n_above += __popc(up);
-    n_equal += __popc(eq);
-  });
+  auto put = [&](uint32_t ups, uint32_t eqs, int32_t id) {
+    const int n = n_above + __popc(ups & below), e = n_equal + __popc(eqs & below);
+    if ((ups >> lane & 1) || ((eqs >> lane & 1) && e < left)) out[n + min(e, left)] = id;
+    n_above += __popc(ups);
+    n_equal += __popc(eqs);
+  };
+  if (mine.few) {
+#pragma unroll
+    for (int k = 0; k < F::kKept; ++k) put(up[k], eq[k], mine.page[k]);
+  } else {
+    for (int j = mine.first + lane; j - lane < mine.end; j += 32) {
+      const uint32_t k = j < mine.end ? mine.all[j] : 0u;
+      put(__ballot_sync(0xffffffffu, j < mine.end && k > at), __ballot_sync(0xffffffffu, j < mine.end && k == at),
+          j < mine.end ? mine.ids[j] : 0);
+    }
+  }
 }
 
 }  // namespace kv4
@@ -602,7 +635,7 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
 constexpr int kSelTokens = 4;
 template <typename T, int HD>
 static int dispatch_select(SelectArgs A, cudaStream_t s) {
-  A.slots = std::max(1, A.a.s.max_pages - A.a.first - A.a.last);
+  A.slots = (std::max(1, A.a.s.max_pages - A.a.first - A.a.last) + 3) / 4 * 4;
   if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
   const int64_t units = (int64_t)A.a.s.n_tok * A.p.nkv;
   int C = 1;
