@@ -130,6 +130,7 @@ struct SelectArgs {
   Pages p;
   int G;
   int slots;                            // scores of a token: entries of a table row that may be among them
+  float minus_zero;
   int32_t* flags;
 };
 
@@ -159,16 +160,50 @@ __device__ __forceinline__ void put_first(uint32_t* at, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ptx::dsmem_addr(at, 0)), "r"(v) : "memory");
 }
 
+// Two fp32 at once, each rounded as alone.  A product is a fused multiply-add with a -0 that the
+// compiler does not know: of a packed product and a packed sum it would make one operation with
+// one rounding.
+using F2 = uint64_t;
+__device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 product2(F2 a, F2 b, F2 minus_zero) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(minus_zero));
+  return r;
+}
+__device__ __forceinline__ F2 sum2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Sums over the lanes of a page, in the order of the scores: the eights of lo and of hi by
 // halves, then both. Of V values a lane gives half away at each step, as long as it has two, so
-// that there is about one exchange per sum; it is left with those from *base on.
+// that there is about one exchange per sum; it is left with those from first_sum() on, in the
+// first places.
+template <int HD>
+__device__ __forceinline__ constexpr int sum_steps() { return HD == 128 ? 4 : 3; }
+template <int HD>
+__device__ __forceinline__ constexpr int sum_bit(int step) {   // 4 2 1 8, or 2 1 4
+  return step < sum_steps<HD>() - 1 ? HD / 32 >> step : HD / 16;
+}
 template <int HD, int V>
-__device__ __forceinline__ void sum_lanes(float (&v)[V], int lane, int* base) {
-  constexpr int EIGHTS = HD / 8;
-  int n = V, at = 0;
+__device__ __forceinline__ int first_sum(int lane) {
+  int at = 0, n = V;
 #pragma unroll
-  for (int o = EIGHTS / 2; o >= 0; o = o > 1 ? o / 2 : o - 1) {
-    const int bit = o > 0 ? o : EIGHTS;            // (last: lo and hi)
+  for (int step = 0; step < sum_steps<HD>(); ++step)
+    if (n > 1) n /= 2, at += lane & sum_bit<HD>(step) ? n : 0;
+  return at;
+}
+template <int HD, int V>
+__device__ __forceinline__ void sum_lanes(float (&v)[V], int lane) {
+  int n = V;
+#pragma unroll
+  for (int step = 0; step < sum_steps<HD>(); ++step) {
+    const int bit = sum_bit<HD>(step);
     if (n > 1) {
       n /= 2;
       const bool up = lane & bit;
@@ -179,12 +214,10 @@ __device__ __forceinline__ void sum_lanes(float (&v)[V], int lane, int* base) {
           v[i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, give, bit));
         }
       }
-      at += up ? n : 0;
     } else {
       v[0] = __fadd_rn(v[0], __shfl_xor_sync(0xffffffffu, v[0], bit));
     }
   }
-  *base = at;
 }
 
 // The warps that look for a token's best pages: WARPS of a CTA's, the bar-th such group.
@@ -219,6 +252,20 @@ struct Keys {
     }
   }
   __device__ __forceinline__ bool there(int k, int lane) const { return first + 32 * k + lane < end; }
+  // smallest and largest of the warp's
+  __device__ __forceinline__ void range(int lane, uint32_t* lo, uint32_t* hi) const {
+    uint32_t a = 0xFFFFFFFFu, b = 0u;
+    if (few) {
+#pragma unroll
+      for (int k = 0; k < KEPT; ++k)
+        if (there(k, lane)) a = min(a, kept[k]), b = max(b, kept[k]);
+    } else {
+#pragma unroll 4
+      for (int j = first + lane; j < end; j += 32) a = min(a, all[j]), b = max(b, all[j]);
+    }
+    *lo = __reduce_min_sync(0xffffffffu, a);
+    *hi = __reduce_max_sync(0xffffffffu, b);
+  }
   // f(key) of those in [lo, hi]
   template <typename F>
   __device__ __forceinline__ void within(uint32_t lo, uint32_t hi, int lane, F&& f) const {
@@ -243,6 +290,7 @@ struct Search {
   __align__(16) uint32_t few[kSelFew];
   int n_few;                                       // as bins
   int above[kSelWarps], equal[kSelWarps];          // of each warp
+  uint32_t lo[kSelWarps], hi[kSelWarps];
 };
 
 // The r-th largest of n <= kSelFew keys (16-byte aligned, readable to a multiple of four), by every warp.
@@ -267,8 +315,15 @@ __device__ __forceinline__ uint32_t rank_few(const uint32_t* few, int n, int r, 
 // of those equal to it. By counts of the keys in 256 parts of the range [lo, hi] that holds the r-th,
 // from the top, until a part's keys are all wanted, are few, or are one value.
 template <int WARPS, int KEPT>
-__device__ __forceinline__ uint32_t threshold(const Keys<WARPS, KEPT>& keys, int r, uint32_t lo, uint32_t hi, Search& S,
-                                              const Group<WARPS>& G) {
+__device__ __forceinline__ uint32_t threshold(const Keys<WARPS, KEPT>& keys, int r, Search& S, const Group<WARPS>& G) {
+  uint32_t lo, hi;
+  keys.range(G.lane, &lo, &hi);
+  if (WARPS > 1) {
+    if (G.lane == 0) S.lo[G.warp] = lo, S.hi[G.warp] = hi;
+    G.sync();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) lo = min(lo, S.lo[w]), hi = max(hi, S.hi[w]);
+  }
   for (;;) {
     const int shift = max(0, 32 - __clz(hi - lo) - 8);       // ((hi - lo) >> shift) < 256
     keys.within(lo, hi, G.lane, [&](uint32_t k) { atomicAdd(&S.bins[(k - lo) >> shift], 1); });
@@ -321,31 +376,31 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
 }
 
 // The forms of the kernel: one token by a CTA, one by a cluster, four of a sequence by a CTA.
-// Loads of 16 bytes per lane in a turn of a warp, turns in flight, warps, and those that look for
-// the pages of one token.
+// Warps and those that look for the pages of one token; loads of a turn of a warp (two copies of
+// 16 bytes per lane each) and turns in flight.
 template <int TT, bool CL>
 struct Form {
-  static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 8 : 4,
-                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kKept = TT == 1 && !CL ? 4 : 8, kCtas = TT == 1 && !CL ? 7 : 2;
-  static constexpr int kRing = kWarps * kTurns * kLoads * 512;   // bytes
+  static constexpr int kWarps = CL ? 8 : 4, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2,
+                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = CL ? 2 : TT == 1 ? 7 : 4;
+  static constexpr int kRing = kWarps * kTurns * kLoads * 1024;   // bytes
 };
 
 // Up to TT tokens of a sequence share a walk over its pages' bounds; the CTA of the first of
 // them does the work of all. CL: a cluster has one token, its CTAs the pages in turn, and the first
-// one the scores. A page's bounds are HD / 4 copies of 16 bytes, one per lane: the smallest
-// of eight channels, by b, or the largest, by a. Every lane reads what it has copied itself, so
-// that the turns in flight need neither registers nor barriers.
+// one the scores. A page has HD / 8 lanes: the lower ones two eights each of the smallest of its
+// channels, by b, the upper ones of the largest, by a; the two eights are those that the
+// score's sum takes first, and go side by side through packed instructions. Every lane reads what
+// it has copied itself, so that the turns in flight need neither registers nor barriers.
 template <typename T, int HD, int TT, bool CL>
 __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
   using F = Form<TT, CL>;
   extern __shared__ __align__(128) uint8_t sel_smem[];
   uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots, a multiple of four]
-  constexpr int WARPS = F::kWarps, THREADS = F::kThreads, MOST = CL ? kSelCluster * WARPS : WARPS;
+  constexpr int WARPS = F::kWarps, THREADS = F::kThreads;
   __shared__ Search search[TT];
-  __shared__ uint32_t s_lo[TT][MOST], s_hi[TT][MOST];
   __shared__ __align__(16) float s_q[TT][2][HD];   // a token's b, then its a
   static_assert(!CL || TT == 1, "");
-  constexpr int LPP = HD / 4, PPW = 32 / LPP;      // lanes of a page, pages of a warp's load
+  constexpr int LPP = HD / 8, PPW = 32 / LPP;      // lanes of a page, pages of a warp's load
   constexpr int LOADS = F::kLoads, V = LOADS * TT; // of a turn, and their scores
   constexpr int TURNS = F::kTurns, PAGES = LOADS * PPW, IDS = 32 / PAGES;   // turns whose ids a warp reads at once
   const buddy_kv4_select_args& a = A.a;
@@ -404,15 +459,14 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   const int M = scored(tokens - 1);                // of the last token: the most
   // what is in without a score
   auto always = [&]() {
-    for (int u = 0; u < tokens; ++u) {
+    const int ends = a.first + a.last;
+    for (int x = tid; x < tokens * ends; x += THREADS) {
+      const int u = TT == 1 ? 0 : x / ends, j = x - u * ends, N = pages_of(p0 + u);
+      if (N > a.budget) list_of(u)[j < a.first ? j : a.budget - ends + j] = row[j < a.first ? j : N - ends + j];
+    }
+    for (int u = 0; u < tokens && pages_of(p0 + u) <= a.budget; ++u) {
       const int N = pages_of(p0 + u);
-      int32_t* const out = list_of(u);
-      if (N <= a.budget) {
-        for (int j = tid; j < a.budget; j += THREADS) out[j] = j < N ? row[j] : -1;
-      } else {
-        for (int j = tid; j < a.first; j += THREADS) out[j] = row[j];
-        for (int j = tid; j < a.last; j += THREADS) out[a.budget - a.last + j] = row[N - a.last + j];
-      }
+      for (int j = tid; j < a.budget; j += THREADS) list_of(u)[j] = j < N ? row[j] : -1;
     }
   };
   if (M == 0 || r == 0) {                          // (the same in the whole cluster)
@@ -423,8 +477,9 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
 
   // ---- scores
   const int turns = M > j_first ? (M - j_first + turn - 1) / turn : 0;
-  const uint32_t ring = ptx::smem_u32(sel_smem) + (uint32_t)(warp * TURNS * LOADS * 512 + lane * 16);
-  const __half* const bounds = (const __half*)a.bounds + (int64_t)g * 2 * HD + lane % LPP * 8;
+  const uint32_t ring = ptx::smem_u32(sel_smem) + (uint32_t)(warp * TURNS * LOADS * 1024 + lane * 16);
+  const int eight = lane % (LPP / 2), high = lane / (LPP / 2) % 2;   // the lane's first of two; of lo or of hi
+  const __half* const bounds = (const __half*)a.bounds + ((int64_t)g * 2 + high) * HD + eight * 8;
   const int64_t per_page = (int64_t)A.p.nkv * 2 * HD;
   uint32_t gone = 0;                               // of the loads in flight and the one at hand, LOADS bits a turn, the newest lowest
   auto issue = [&](int n, int at) {                // (a turn that is not there copies nothing: the counts of groups go on)
@@ -438,7 +493,9 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
       for (int k = 0; k < LOADS; ++k) {
         const bool there = (uint32_t)id[k] < (uint32_t)A.p.n_pages;
         gone |= there ? 0u : 1u << k;
-        copy16(ring + (at * LOADS + k) * 512, bounds + (there ? id[k] : 0) * per_page, there);
+        const __half* const src = bounds + (there ? id[k] : 0) * per_page;
+        copy16(ring + (at * LOADS + k) * 1024, src, there);
+        copy16(ring + (at * LOADS + k) * 1024 + 512, src + HD / 2, there);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -462,69 +519,73 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     s_q[u][1][c] = up;
   }
   __syncthreads();
-  float f[TT][8];                                  // this lane's eight channels, of lo or of hi
+  F2 f[TT][8];                                     // this lane's channels of both eights
 #pragma unroll
   for (int u = 0; u < TT; ++u) {
-    const float4* const y = reinterpret_cast<const float4*>(&s_q[u][0][0] + lane % LPP * 8);
-    const float4 y0 = y[0], y1 = y[1];
-    f[u][0] = y0.x, f[u][1] = y0.y, f[u][2] = y0.z, f[u][3] = y0.w;
-    f[u][4] = y1.x, f[u][5] = y1.y, f[u][6] = y1.z, f[u][7] = y1.w;
+    const float4* const y = reinterpret_cast<const float4*>(&s_q[u][high][eight * 8]);
+    const float4 a0 = y[0], a1 = y[1], b0 = y[HD / 8], b1 = y[HD / 8 + 1];
+    f[u][0] = pair(a0.x, b0.x), f[u][1] = pair(a0.y, b0.y), f[u][2] = pair(a0.z, b0.z), f[u][3] = pair(a0.w, b0.w);
+    f[u][4] = pair(a1.x, b1.x), f[u][5] = pair(a1.y, b1.y), f[u][6] = pair(a1.z, b1.z), f[u][7] = pair(a1.w, b1.w);
   }
+  const F2 minus_zero = pair(A.minus_zero, A.minus_zero);
   bool lost = false;
-  uint32_t low[TT], top[TT];
+  constexpr int LEFT = V > LPP ? V / LPP : 1;      // values of a turn that a lane is left with
+  // lanes that differ in these bits only are left with the same
+  constexpr int TWINS = V >= LPP ? 0 : V == LPP / 2 ? LPP / 2 : LPP / 2 + LPP / (2 * V) - 1;
+  const int mine_at = first_sum<HD, V>(lane);
+  int j_mine[LEFT], j_end[LEFT], u_mine[LEFT];     // their pages in the first turn, where their token's end, and the token
 #pragma unroll
-  for (int u = 0; u < TT; ++u) low[u] = 0xFFFFFFFFu, top[u] = 0u;
+  for (int e = 0; e < LEFT; ++e) {
+    u_mine[e] = (mine_at + e) % TT;
+    j_mine[e] = j_first + (mine_at + e) / TT * PPW + lane / LPP;
+    j_end[e] = lane & TWINS ? 0 : scored(u_mine[e]);
+  }
   if (CL) ptx::cluster_wait_started();
   for (int n = 0, at = 0; n < turns; ++n, at = at + 1 == TURNS ? 0 : at + 1) {
     asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");
     float v[V];
 #pragma unroll
     for (int k = 0; k < LOADS; ++k) {
-      const uint4 w = *reinterpret_cast<const uint4*>(sel_smem + ((warp * TURNS + at) * LOADS + k) * 512 + lane * 16);
-      const float2 y[4] = {__half22float2(as_h2(w.x)), __half22float2(as_h2(w.y)), __half22float2(as_h2(w.z)),
-                           __half22float2(as_h2(w.w))};
+      const uint8_t* const src = sel_smem + ((warp * TURNS + at) * LOADS + k) * 1024 + lane * 16;
+      const uint4 w0 = *reinterpret_cast<const uint4*>(src), w1 = *reinterpret_cast<const uint4*>(src + 512);
+      const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+      F2 y[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 y0 = __half22float2(as_h2(x0[e])), y1 = __half22float2(as_h2(x1[e]));
+        y[2 * e] = pair(y0.x, y1.x), y[2 * e + 1] = pair(y0.y, y1.y);
+      }
 #pragma unroll
       for (int u = 0; u < TT; ++u) {
-        float z[8];
+        v[k * TT + u] = 0.f;
+        if (TT > 1 && u >= tokens) continue;
+        F2 z[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[2 * e] = __fmul_rn(f[u][2 * e], y[e].x), z[2 * e + 1] = __fmul_rn(f[u][2 * e + 1], y[e].y);
+        for (int e = 0; e < 8; ++e) z[e] = product2(f[u][e], y[e], minus_zero);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = __fadd_rn(z[e], z[e + 4]);
-        v[k * TT + u] = __fadd_rn(__fadd_rn(z[0], z[2]), __fadd_rn(z[1], z[3]));
+        for (int h = 4; h > 0; h /= 2)
+#pragma unroll
+          for (int e = 0; e < h; ++e) z[e] = sum2(z[e], z[e + h]);
+        float s0, s1;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(z[0]));
+        v[k * TT + u] = __fadd_rn(s0, s1);
       }
     }
-    int base;
-    sum_lanes<HD, V>(v, lane, &base);
+    sum_lanes<HD, V>(v, lane);
     const uint32_t missing = gone >> ((TURNS - 1) * LOADS);
     issue(n + TURNS, at);                          // (what this turn has read has been used)
-    constexpr int LEFT = V > LPP ? V / LPP : 1;    // values that a lane is left with
-    // lanes that differ in these bits only are left with the same
-    constexpr int TWINS = V >= LPP ? 0 : V == LPP / 2 ? LPP / 2 : LPP / 2 + LPP / (2 * V) - 1;
 #pragma unroll
     for (int e = 0; e < LEFT; ++e) {
-      const int k = (base + e) / TT, u = (base + e) % TT, j = n * turn + j_first + k * PPW + lane / LPP;
-      if (j >= scored(u) || (lane & TWINS)) continue;
-      const bool there = !(missing >> k & 1);
+      const int j = j_mine[e] + n * turn;
+      if (j >= j_end[e]) continue;
+      const bool there = !(missing >> ((mine_at + e) / TT) & 1);
       const uint32_t key = there ? key_of(v[e]) : 0u;
       lost |= !there;
       if (CL) put_first(&keys[j], key);
-      else keys[u * A.slots + j] = key;
-#pragma unroll
-      for (int y = 0; y < TT; ++y)
-        if (y == u) low[y] = min(low[y], key), top[y] = max(top[y], key);
+      else keys[u_mine[e] * A.slots + j] = key;
     }
   }
   if (lost && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
-#pragma unroll
-  for (int u = 0; u < TT; ++u) {
-    low[u] = __reduce_min_sync(0xffffffffu, low[u]);
-    top[u] = __reduce_max_sync(0xffffffffu, top[u]);
-    if (lane == 0) {
-      const int at = (int)rank * WARPS + warp;
-      if (CL) put_first(&s_lo[u][at], low[u]), put_first(&s_hi[u][at], top[u]);
-      else s_lo[u][at] = low[u], s_hi[u][at] = top[u];
-    }
-  }
   if (CL) {
     ptx::cluster_sync();
     if (rank != 0) return;
@@ -538,11 +599,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, u};
   Search& S = search[u];
   const Keys<F::kGroup, F::kKept> mine(keys + u * A.slots, row + a.first, m, G);
-  uint32_t lo = 0xFFFFFFFFu, hi = 0;
-  for (int y = lane; y < (int)C * WARPS; y += 32) lo = min(lo, s_lo[u][y]), hi = max(hi, s_hi[u][y]);
-  lo = __reduce_min_sync(0xffffffffu, lo);
-  hi = __reduce_max_sync(0xffffffffu, hi);
-  const uint32_t at = m <= kSelFew ? rank_few(mine.all, m, r, lane) : threshold(mine, r, lo, hi, S, G);
+  const uint32_t at = m <= kSelFew ? rank_few(mine.all, m, r, lane) : threshold(mine, r, S, G);
   // pages above it in each 32, pages with it; then where these of the warp begin
   const uint32_t below = (1u << lane) - 1;
   int32_t* const out = list_of(u) + a.first;
@@ -639,7 +696,7 @@ static int dispatch_select(SelectArgs A, cudaStream_t s) {
   if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
   const int64_t units = (int64_t)A.a.s.n_tok * A.p.nkv;
   int C = 1;
-  while (C < kSelCluster && 2 * C * Form<1, true>::kWarps * Form<1, true>::kLoads * (128 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
+  while (C < kSelCluster && 2 * C * Form<1, true>::kWarps * Form<1, true>::kLoads * (256 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
   return C > 1 ? launch_select<T, HD, 1, true>(A, C, s) : launch_select<T, HD, 1, false>(A, 1, s);
 }
 
@@ -672,7 +729,7 @@ extern "C" int buddy_kv4_select(const buddy_kv4_cache* cache, const buddy_kv4_se
   if (!a->q || !aligned16(a->q) || a->q_stride * (a->q_dtype == BUDDY_DTYPE_F32 ? 4 : 2) % 16 || !a->bounds ||
       !aligned16(a->bounds) || !a->pages || !a->visible)
     return BUDDY_ERR_ARG;
-  const SelectArgs A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, 0, flags};
+  const SelectArgs A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, 0, -0.f, flags};
   cudaStream_t s = (cudaStream_t)stream;
   if (a->q_dtype == BUDDY_DTYPE_F32)
     return cache->head_dim == 128 ? dispatch_select<float, 128>(A, s) : dispatch_select<float, 64>(A, s);
