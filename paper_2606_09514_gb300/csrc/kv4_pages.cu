@@ -12,6 +12,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -130,6 +131,7 @@ struct SelectArgs {
   Pages p;
   int G;
   int slots;                            // scores of a token: entries of a table row that may be among them
+  int chunks;                           // CTAs per head of a sequence, TT tokens each; 0: a CTA for each token
   float minus_zero;
   int32_t* flags;
 };
@@ -151,6 +153,17 @@ __device__ __forceinline__ int seq_of(const buddy_kv4_seqs& S, int t, int lane) 
     if (c == 0) return -1;
     lo += (c - 1) * step;
     hi = min(hi, lo + step);
+  }
+  return lo < S.batch ? lo : -1;
+}
+
+// The same by one thread.
+__device__ __forceinline__ int seq_of(const buddy_kv4_seqs& S, int t) {
+  int lo = -1, hi = S.batch + 1;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (S.row_start[mid] <= t) lo = mid;
+    else hi = mid;
   }
   return lo < S.batch ? lo : -1;
 }
@@ -380,8 +393,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
 // 16 bytes per lane each) and turns in flight.
 template <int TT, bool CL>
 struct Form {
-  static constexpr int kWarps = CL ? 8 : 4, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2,
-                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = CL ? 2 : TT == 1 ? 7 : 4;
+  static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2,
+                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = TT == 1 && !CL ? 7 : 2;
   static constexpr int kRing = kWarps * kTurns * kLoads * 1024;   // bytes
 };
 
@@ -401,30 +414,65 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   __shared__ __align__(16) float s_q[TT][2][HD];   // a token's b, then its a
   static_assert(!CL || TT == 1, "");
   constexpr int LPP = HD / 8, PPW = 32 / LPP;      // lanes of a page, pages of a warp's load
-  constexpr int LOADS = F::kLoads, V = LOADS * TT; // of a turn, and their scores
+  constexpr int LOADS = F::kLoads;
   constexpr int TURNS = F::kTurns, PAGES = LOADS * PPW, IDS = 32 / PAGES;   // turns whose ids a warp reads at once
   const buddy_kv4_select_args& a = A.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = CL ? ptx::cluster_rank() : 0, C = CL ? ptx::cluster_size() : 1;
   const unsigned unit = blockIdx.x / C;
-  const int g = (int)(unit % (unsigned)A.p.nkv), t = (int)(unit / (unsigned)A.p.nkv);
+  const int g = (int)(unit % (unsigned)A.p.nkv);
+  int t = (int)(unit / (unsigned)A.p.nkv), i = 0, chunk = 0;
+  const bool by_seq = TT > 1 && A.chunks > 0;
+  if (by_seq) {
+    i = t / A.chunks, chunk = t % A.chunks;
+    if (i >= a.s.batch) {                          // behind the sequences' CTAs: the tokens that are in none
+      const int64_t x = ((int64_t)unit - (int64_t)a.s.batch * A.chunks * A.p.nkv) * THREADS + tid;
+      pdl_wait();
+      pdl_trigger();
+      if (x >= a.s.n_tok) return;
+      t = (int)x, i = seq_of(a.s, t);
+      Rows s{};
+      const bool ok = i >= 0 && rows_of(a.s, A.p.shift, i, &s) && t >= s.t0 && t < s.t0 + s.m;
+      if (!ok) a.visible[t] = -1;
+      if (!ok && i >= 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+      return;
+    }
+  }
   for (int b = tid; b < TT * kSelBins; b += THREADS) search[b / kSelBins].bins[b % kSelBins] = 0;
   if (tid < TT) search[tid].n_few = 0;
   constexpr int PER = (TT * HD + THREADS - 1) / THREADS;
-  const T* q[PER];
-#pragma unroll
-  for (int e = 0; e < PER; ++e)
-    q[e] = (const T*)a.q + min(t + (tid + e * THREADS) / HD, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + tid % HD;
-  pdl_wait();
-  pdl_trigger();
-  // (the queries are on their way while the token's sequence is looked for)
+  auto query = [&](int t, int e) {
+    return (const T*)a.q + min(t + (tid + e * THREADS) / HD, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + tid % HD;
+  };
   T x[PER][8];
+  auto read_queries = [&](const T* const (&q)[PER]) {
 #pragma unroll
-  for (int e = 0; e < PER; ++e)
+    for (int e = 0; e < PER; ++e)
 #pragma unroll
-    for (int h = 0; h < 8; ++h)
-      if ((tid + e * THREADS) / HD < TT && h < A.G) x[e][h] = q[e][h * HD];
-  const int i = seq_of(a.s, t, lane);
+      for (int h = 0; h < 8; ++h)
+        if ((tid + e * THREADS) / HD < TT && h < A.G) x[e][h] = q[e][h * HD];
+  };
+  Rows s{};
+  bool ok = true;
+  if (by_seq) {
+    pdl_wait();
+    pdl_trigger();
+    ok = rows_of(a.s, A.p.shift, i, &s) && chunk * TT < s.m;
+    t = s.t0 + chunk * TT;
+    if (!ok) return;                               // (the CTAs behind see to the tokens)
+    const T* q[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) q[e] = query(t, e);
+    read_queries(q);
+  } else {
+    const T* q[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) q[e] = query(t, e);
+    pdl_wait();
+    pdl_trigger();
+    read_queries(q);                               // (on their way while the token's sequence is looked for)
+    i = seq_of(a.s, t, lane);
+  }
   // turn n of the warp has the pages from (n C WARPS + rank WARPS + warp) PAGES on; their ids,
   // of IDS turns at once, by lanes (what lies behind the sequence's pages may be anything)
   const int32_t* const row = a.s.table + (int64_t)max(i, 0) * a.s.max_pages;
@@ -434,25 +482,26 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     return j < A.slots && a.first + j < a.s.max_pages ? row[a.first + j] : -1;
   };
   int ids = ids_of(0), ids_next = ids_of(IDS);
-  Rows s{};
-  bool ok = i >= 0;
-  if (ok) {
-    ok = rows_of(a.s, A.p.shift, i, &s) && t >= s.t0 && t < s.t0 + s.m;
-    if (!ok && g == 0 && tid == 0 && rank == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
-  }
-  if (!ok) {
-    if (g == 0 && tid == 0 && rank == 0) a.visible[t] = -1;
-    return;
+  if (!by_seq) {
+    ok = i >= 0;
+    if (ok) {
+      ok = rows_of(a.s, A.p.shift, i, &s) && t >= s.t0 && t < s.t0 + s.m;
+      if (!ok && g == 0 && tid == 0 && rank == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+    }
+    if (!ok) {
+      if (g == 0 && tid == 0 && rank == 0) a.visible[t] = -1;
+      return;
+    }
+    if (TT > 1 && (t - s.t0) % TT != 0) return;    // (the CTA of another token sees to this one)
   }
   const int p0 = s.n - s.m + (t - s.t0);           // of token t; the next ones follow
   const int in_page = (1 << A.p.shift) - 1;
   auto pages_of = [&](int p) { return p < 0 ? 0 : (p >> A.p.shift) + 1; };
-  if (g == 0 && tid == 0 && rank == 0) {
-    const int N = pages_of(p0);
-    a.visible[t] = N == 0 ? 0 : ((min(N, a.budget) - 1) << A.p.shift) + (p0 & in_page) + 1;
-  }
-  if (TT > 1 && (t - s.t0) % TT != 0) return;
   const int tokens = min(TT, s.t0 + s.m - t);
+  if (g == 0 && tid < tokens && rank == 0) {
+    const int p = p0 + tid, N = pages_of(p);
+    a.visible[t + tid] = N == 0 ? 0 : ((min(N, a.budget) - 1) << A.p.shift) + (p & in_page) + 1;
+  }
   auto list_of = [&](int u) { return a.pages + ((int64_t)(t + u) * A.p.nkv + g) * a.budget; };
   const int r = a.budget - a.first - a.last;
   auto scored = [&](int u) { const int N = pages_of(p0 + u); return u < tokens && N > a.budget ? N - a.first - a.last : 0; };
@@ -519,72 +568,82 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     s_q[u][1][c] = up;
   }
   __syncthreads();
-  F2 f[TT][8];                                     // this lane's channels of both eights
-#pragma unroll
-  for (int u = 0; u < TT; ++u) {
-    const float4* const y = reinterpret_cast<const float4*>(&s_q[u][high][eight * 8]);
-    const float4 a0 = y[0], a1 = y[1], b0 = y[HD / 8], b1 = y[HD / 8 + 1];
-    f[u][0] = pair(a0.x, b0.x), f[u][1] = pair(a0.y, b0.y), f[u][2] = pair(a0.z, b0.z), f[u][3] = pair(a0.w, b0.w);
-    f[u][4] = pair(a1.x, b1.x), f[u][5] = pair(a1.y, b1.y), f[u][6] = pair(a1.z, b1.z), f[u][7] = pair(a1.w, b1.w);
-  }
   const F2 minus_zero = pair(A.minus_zero, A.minus_zero);
   bool lost = false;
-  constexpr int LEFT = V > LPP ? V / LPP : 1;      // values of a turn that a lane is left with
-  // lanes that differ in these bits only are left with the same
-  constexpr int TWINS = V >= LPP ? 0 : V == LPP / 2 ? LPP / 2 : LPP / 2 + LPP / (2 * V) - 1;
-  const int mine_at = first_sum<HD, V>(lane);
-  int j_mine[LEFT], j_end[LEFT], u_mine[LEFT];     // their pages in the first turn, where their token's end, and the token
-#pragma unroll
-  for (int e = 0; e < LEFT; ++e) {
-    u_mine[e] = (mine_at + e) % TT;
-    j_mine[e] = j_first + (mine_at + e) / TT * PPW + lane / LPP;
-    j_end[e] = lane & TWINS ? 0 : scored(u_mine[e]);
-  }
   if (CL) ptx::cluster_wait_started();
-  for (int n = 0, at = 0; n < turns; ++n, at = at + 1 == TURNS ? 0 : at + 1) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");
-    float v[V];
+  auto score = [&](auto number) {
+    constexpr int NT = decltype(number)::value, NP = NT == 3 ? 4 : NT, V = LOADS * NP;   // tokens; scores of a turn
+    F2 f[NT][8];                                   // this lane's channels of both eights
 #pragma unroll
-    for (int k = 0; k < LOADS; ++k) {
-      const uint8_t* const src = sel_smem + ((warp * TURNS + at) * LOADS + k) * 1024 + lane * 16;
-      const uint4 w0 = *reinterpret_cast<const uint4*>(src), w1 = *reinterpret_cast<const uint4*>(src + 512);
-      const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
-      F2 y[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 y0 = __half22float2(as_h2(x0[e])), y1 = __half22float2(as_h2(x1[e]));
-        y[2 * e] = pair(y0.x, y1.x), y[2 * e + 1] = pair(y0.y, y1.y);
-      }
-#pragma unroll
-      for (int u = 0; u < TT; ++u) {
-        v[k * TT + u] = 0.f;
-        if (TT > 1 && u >= tokens) continue;
-        F2 z[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = product2(f[u][e], y[e], minus_zero);
-#pragma unroll
-        for (int h = 4; h > 0; h /= 2)
-#pragma unroll
-          for (int e = 0; e < h; ++e) z[e] = sum2(z[e], z[e + h]);
-        float s0, s1;
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(z[0]));
-        v[k * TT + u] = __fadd_rn(s0, s1);
-      }
+    for (int u = 0; u < NT; ++u) {
+      const float4* const y = reinterpret_cast<const float4*>(&s_q[u][high][eight * 8]);
+      const float4 a0 = y[0], a1 = y[1], b0 = y[HD / 8], b1 = y[HD / 8 + 1];
+      f[u][0] = pair(a0.x, b0.x), f[u][1] = pair(a0.y, b0.y), f[u][2] = pair(a0.z, b0.z), f[u][3] = pair(a0.w, b0.w);
+      f[u][4] = pair(a1.x, b1.x), f[u][5] = pair(a1.y, b1.y), f[u][6] = pair(a1.z, b1.z), f[u][7] = pair(a1.w, b1.w);
     }
-    sum_lanes<HD, V>(v, lane);
-    const uint32_t missing = gone >> ((TURNS - 1) * LOADS);
-    issue(n + TURNS, at);                          // (what this turn has read has been used)
+    // what a lane is left with of a turn: its page in the first turn, where its token's pages end, and the token
+    constexpr int LEFT = V > LPP ? V / LPP : 1;
+    // (lanes that differ in these bits only are left with the same)
+    constexpr int TWINS = V >= LPP ? 0 : V == LPP / 2 ? LPP / 2 : LPP / 2 + LPP / (2 * V) - 1;
+    const int mine_at = first_sum<HD, V>(lane);
+    int j_mine[LEFT], j_end[LEFT], u_mine[LEFT];
 #pragma unroll
     for (int e = 0; e < LEFT; ++e) {
-      const int j = j_mine[e] + n * turn;
-      if (j >= j_end[e]) continue;
-      const bool there = !(missing >> ((mine_at + e) / TT) & 1);
-      const uint32_t key = there ? key_of(v[e]) : 0u;
-      lost |= !there;
-      if (CL) put_first(&keys[j], key);
-      else keys[u_mine[e] * A.slots + j] = key;
+      u_mine[e] = (mine_at + e) % NP;
+      j_mine[e] = j_first + (mine_at + e) / NP * PPW + lane / LPP;
+      j_end[e] = lane & TWINS ? 0 : scored(u_mine[e]);
     }
-  }
+    for (int n = 0, at = 0; n < turns; ++n, at = at + 1 == TURNS ? 0 : at + 1) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");
+      float v[V];
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) {
+        const uint8_t* const src = sel_smem + ((warp * TURNS + at) * LOADS + k) * 1024 + lane * 16;
+        const uint4 w0 = *reinterpret_cast<const uint4*>(src), w1 = *reinterpret_cast<const uint4*>(src + 512);
+        const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+        F2 y[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 y0 = __half22float2(as_h2(x0[e])), y1 = __half22float2(as_h2(x1[e]));
+          y[2 * e] = pair(y0.x, y1.x), y[2 * e + 1] = pair(y0.y, y1.y);
+        }
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          if (u >= NT) {
+            v[k * NP + u] = 0.f;
+            continue;
+          }
+          F2 z[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[e] = product2(f[min(u, NT - 1)][e], y[e], minus_zero);
+#pragma unroll
+          for (int h = 4; h > 0; h /= 2)
+#pragma unroll
+            for (int e = 0; e < h; ++e) z[e] = sum2(z[e], z[e + h]);
+          float s0, s1;
+          asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(z[0]));
+          v[k * NP + u] = __fadd_rn(s0, s1);
+        }
+      }
+      sum_lanes<HD, V>(v, lane);
+      const uint32_t missing = gone >> ((TURNS - 1) * LOADS);
+      issue(n + TURNS, at);                        // (what this turn has read has been used)
+#pragma unroll
+      for (int e = 0; e < LEFT; ++e) {
+        const int j = j_mine[e] + n * turn;
+        if (j >= j_end[e]) continue;
+        const bool there = !(missing >> ((mine_at + e) / NP) & 1);
+        const uint32_t key = there ? key_of(v[e]) : 0u;
+        lost |= !there;
+        if (CL) put_first(&keys[j], key);
+        else keys[u_mine[e] * A.slots + j] = key;
+      }
+    }
+  };
+  if (TT == 1 || tokens == 1) score(std::integral_constant<int, 1>());
+  else if (TT > 1 && tokens == 2) score(std::integral_constant<int, TT == 1 ? 1 : 2>());
+  else if (TT > 1 && tokens == 3) score(std::integral_constant<int, TT == 1 ? 1 : 3>());
+  else if (TT > 1) score(std::integral_constant<int, TT>());
   if (lost && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
   if (CL) {
     ptx::cluster_sync();
@@ -661,10 +720,17 @@ static bool seqs_ok(const buddy_kv4_cache* c, const buddy_kv4_seqs& s) {
 
 template <typename T, int HD, int TT, bool CL>
 static int launch_select(SelectArgs A, int C, cudaStream_t s) {
-  const int64_t ctas = (int64_t)A.a.s.n_tok * A.p.nkv * C;
+  using F = Form<TT, CL>;
+  int64_t ctas = (int64_t)A.a.s.n_tok * A.p.nkv * C;
+  if (TT > 1) {                                    // by sequences, unless few of them have as many tokens as the longest
+    const int64_t chunks = (A.a.s.max_new + TT - 1) / TT;
+    if (A.a.s.batch * chunks <= A.a.s.n_tok) {
+      A.chunks = (int)chunks;
+      ctas = A.a.s.batch * chunks * A.p.nkv + (A.a.s.n_tok + F::kThreads - 1) / F::kThreads;
+    }
+  }
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = kv4_select_kernel<T, HD, TT, CL>;
-  using F = Form<TT, CL>;
   const size_t smem = F::kRing + sizeof(uint32_t) * (size_t)TT * A.slots;
   if (smem > 24 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
@@ -729,7 +795,7 @@ extern "C" int buddy_kv4_select(const buddy_kv4_cache* cache, const buddy_kv4_se
   if (!a->q || !aligned16(a->q) || a->q_stride * (a->q_dtype == BUDDY_DTYPE_F32 ? 4 : 2) % 16 || !a->bounds ||
       !aligned16(a->bounds) || !a->pages || !a->visible)
     return BUDDY_ERR_ARG;
-  const SelectArgs A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, 0, -0.f, flags};
+  const SelectArgs A{*a, kv4_pages(cache), a->n_q_heads / cache->n_kv_heads, 0, 0, -0.f, flags};
   cudaStream_t s = (cudaStream_t)stream;
   if (a->q_dtype == BUDDY_DTYPE_F32)
     return cache->head_dim == 128 ? dispatch_select<float, 128>(A, s) : dispatch_select<float, 64>(A, s);
