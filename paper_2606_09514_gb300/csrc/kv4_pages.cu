@@ -85,28 +85,42 @@ __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const Boun
   __half2 lo[8], hi[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) lo[e] = __half2half2(__ushort_as_half(0x7C00)), hi[e] = __half2half2(__ushort_as_half(0xFC00));
-#pragma unroll 1
-  for (int r0 = row; r0 < end; r0 += kBoundLoads * RPL) {
-    uint2 w[kBoundLoads];
-    __half sc[kBoundLoads];
+  // N positions of the lane's, the first of them r0; CHECK: up to the sequence's end
+  auto take = [&](auto number, auto check, int r0) {
+    constexpr int N = decltype(number)::value;
+    constexpr bool CHECK = decltype(check)::value;
+    const uint8_t* const c = codes + r0 * code_bytes(HD);
+    const __half* const sc = scales + r0 * (scale_bytes(HD) / 2);
+    uint2 w[N];
+    __half s0[N];
 #pragma unroll
-    for (int j = 0; j < kBoundLoads; ++j) {
-      const int r = r0 + j * RPL;
-      if (r < end) {
-        w[j] = *reinterpret_cast<const uint2*>(codes + r * code_bytes(HD));
-        sc[j] = scales[r * (scale_bytes(HD) / 2)];
-      }
+    for (int j = 0; j < N; ++j) {
+      if (CHECK && r0 + j * RPL >= end) continue;
+      w[j] = *reinterpret_cast<const uint2*>(c + j * RPL * code_bytes(HD));
+      s0[j] = sc[j * RPL * (scale_bytes(HD) / 2)];
     }
 #pragma unroll
-    for (int j = 0; j < kBoundLoads; ++j) {
-      if (r0 + j * RPL >= end) break;
-      const __half2 s1 = __half2half2(sc[j]), s72 = __hmul2(s1, __float2half2_rn(-72.f));
+    for (int j = 0; j < N; ++j) {
+      if (CHECK && r0 + j * RPL >= end) continue;
+      const __half2 s1 = __half2half2(s0[j]), s72 = __hmul2(s1, __float2half2_rn(-72.f));
       uint32_t v[8];
       dequant4(w[j].x, s1, s72, v);
       dequant4(w[j].y, s1, s72, v + 4);
 #pragma unroll
       for (int e = 0; e < 8; ++e) lo[e] = __hmin2_nan(lo[e], as_h2(v[e])), hi[e] = __hmax2_nan(hi[e], as_h2(v[e]));
     }
+  };
+  using Few = std::integral_constant<int, 16 / RPL>;       // 16 positions of the warp
+  using Many = std::integral_constant<int, kBoundLoads>;
+  if (end < 1 << A.p.shift) {
+#pragma unroll 1
+    for (int r0 = row; r0 < end; r0 += Few::value * RPL) take(Few(), std::true_type(), r0);
+  } else if (kBoundLoads * RPL > end) {
+#pragma unroll 1
+    for (int r0 = row; r0 < end; r0 += Few::value * RPL) take(Few(), std::false_type(), r0);
+  } else {
+#pragma unroll 1
+    for (int r0 = row; r0 < end; r0 += kBoundLoads * RPL) take(Many(), std::false_type(), r0);
   }
 #pragma unroll
   for (int o = LPR; o < 32; o <<= 1)
@@ -114,9 +128,11 @@ __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const Boun
     for (int e = 0; e < 8; ++e) lo[e] = __hmin2_nan(lo[e], shfl_xor(lo[e], o)), hi[e] = __hmax2_nan(hi[e], shfl_xor(hi[e], o));
   if (row < 2) {
     uint4* const d = reinterpret_cast<uint4*>(A.bounds + (((int64_t)id * A.p.nkv + g) * 2 + row) * HD + 16 * tl);
-    const __half2* const y = row ? hi : lo;
-    d[0] = make_uint4(h2(y[0]), h2(y[1]), h2(y[2]), h2(y[3]));
-    d[1] = make_uint4(h2(y[4]), h2(y[5]), h2(y[6]), h2(y[7]));
+    uint32_t y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = row ? h2(hi[e]) : h2(lo[e]);
+    d[0] = make_uint4(y[0], y[1], y[2], y[3]);
+    d[1] = make_uint4(y[4], y[5], y[6], y[7]);
   }
 }
 

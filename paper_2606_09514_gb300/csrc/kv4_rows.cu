@@ -26,6 +26,7 @@
 #include "common.cuh"
 #include "internal.h"
 #include "kv4.cuh"
+#include "ptx.cuh"
 
 namespace buddy {
 
@@ -48,6 +49,15 @@ struct Axes {
   int64_t stride;              // from axis to axis of the positions
 };
 struct OneAxis {};
+
+// Heads of a team on their way at once (copied to shared memory, which takes no registers: a lane
+// reads what it has copied itself).
+constexpr int kRowAhead = 4;
+template <typename T>
+__host__ __device__ constexpr int row_ring() { return kRowAhead * kRowThreads * 16 * (int)sizeof(T); }   // bytes
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 
 __device__ __forceinline__ void store8(float* p, const float* x) {
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -113,6 +123,7 @@ template <typename T> struct Raw8;
 template <> struct Raw8<bf16> {
   uint4 a;
   __device__ __forceinline__ void load(const bf16* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void load(const uint8_t* p, int) { a = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void get(F2* o) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -124,6 +135,10 @@ template <> struct Raw8<float> {
   __device__ __forceinline__ void load(const float* p) {
     a = reinterpret_cast<const float4*>(p)[0];
     b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void load(const uint8_t* p, int step) {     // pieces of 16 bytes
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + step);
   }
   __device__ __forceinline__ void get(F2* o) const {
     o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
@@ -224,9 +239,27 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     return (const T*)A.v + t * A.v_stride + (int64_t)(h - kk) * HD + c;
   };
   Raw8<T> lo, hi;
-  const T* src = row(h0);
-  lo.load(src);
-  hi.load(src + HALF);
+  // a lane's pieces of 16 bytes of a head, those of the other threads between them
+  extern __shared__ __align__(16) uint8_t rows_smem[];
+  constexpr int PIECES = (int)sizeof(T);        // eight channels of both halves: 16 sizeof(T) bytes
+  const uint32_t ring = ptx::smem_u32(rows_smem) + threadIdx.x * 16;
+  auto ahead = [&](int h) {
+    if (h < h1) {
+      const T* src = row(h);
+#pragma unroll
+      for (int x = 0; x < PIECES; ++x)
+        copy16(ring + ((h - h0) % kRowAhead * PIECES + x) * (kRowThreads * 16),
+               src + x % (PIECES / 2) * (16 / (int)sizeof(T)) + (x < PIECES / 2 ? 0 : HALF));
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  const bool one = A.per == 1;
+  if (one) {
+    lo.load(row(h0));
+    hi.load(row(h0) + HALF);
+  } else {
+    for (int h = h0; h < h0 + kRowAhead - 1; ++h) ahead(h);
+  }
   int p = R.pos[t], most = p, least = p;        // (of all axes)
   uint32_t mix = 0, axis = 0;                   // two bits of each of the lane's frequencies, the first one's axis
   if constexpr (AXES) {
@@ -248,7 +281,10 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     const int bad = (most >= R.max_pos ? BUDDY_DEV_BAD_POSITION : 0) | (CACHE && ok && slot >= end ? BUDDY_DEV_BAD_PAGE : 0);
     if (bad) atomicOr(A.flags, bad);
   }
-  if (!ok) return;
+  if (!ok) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return;
+  }
   const bool keep = CACHE && slot >= 0 && slot < end;
   F2 co[4], si[4];
   if (h0 < kk) {
@@ -271,13 +307,15 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
     F2 a[4], b[4];                              // lower and upper half
+    if (!one) {
+      ahead(h + kRowAhead - 1);                 // to where the head before this one was
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRowAhead - 1) : "memory");
+      const uint8_t* const at = rows_smem + (h - h0) % kRowAhead * PIECES * (kRowThreads * 16) + threadIdx.x * 16;
+      lo.load(at, kRowThreads * 16);
+      hi.load(at + PIECES / 2 * (kRowThreads * 16), kRowThreads * 16);
+    }
     lo.get(a);
     hi.get(b);
-    if (h + 1 < h1) {
-      src = row(h + 1);
-      lo.load(src);
-      hi.load(src + HALF);
-    }
     if (!CACHE || h < kk) {
       const float* gains = h < kq ? R.q_gain : R.k_gain;
       if (gains) {
@@ -412,7 +450,7 @@ static int launch_rows(RowArgs A, const AX& ax, cudaStream_t s) {
   A.groups = (heads + A.per - 1) / A.per;
   const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  return launch_k(qk_rows_kernel<T, HD, CACHE, AX>, (unsigned)ctas, kRowThreads, 0, s, true, A, ax) == cudaSuccess
+  return launch_k(qk_rows_kernel<T, HD, CACHE, AX>, (unsigned)ctas, kRowThreads, A.per > 1 ? row_ring<T>() : 0, s, true, A, ax) == cudaSuccess
              ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 template <bool CACHE, typename AX>
