@@ -52,7 +52,7 @@ struct OneAxis {};
 
 // Heads of a team on their way at once (copied to shared memory, which takes no registers: a lane
 // reads what it has copied itself).
-constexpr int kRowAhead = 4;
+constexpr int kRowAhead = 3;
 template <typename T>
 __host__ __device__ constexpr int row_ring() { return kRowAhead * kRowThreads * 16 * (int)sizeof(T); }   // bytes
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
