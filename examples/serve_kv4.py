@@ -16,7 +16,17 @@ back, and what the stack has added to the last tokens with the same stack withou
 everything that the sequences were fed: with keys and values rounded to 4 bits as the cache
 rounds them (the rest is bf16's roundings), and with exact ones (what the 4 bits cost).
 
-    python examples/serve_kv4.py [--layers 4] [--batch 8] [--prompt 600] [--piece 128] [--steps 32]
+With --pages N a single token attends, per KV head, to N pages of its sequence only:
+
+    buddy_kv4_bounds           per layer, after the append: bounds of the keys of each page
+    buddy_kv4_select           the first and the last page and those whose bounds promise most
+    buddy_kv4_attention_pages  the queries over these pages
+
+The 64-bit comparison is then over the selected pages. The one with the whole stack shows what
+the other positions would have added: of random keys, which are all alike, more than of a
+model's.
+
+    python examples/serve_kv4.py [--layers 4] [--batch 8] [--prompt 600] [--piece 128] [--steps 32] [--pages 0]
 """
 from __future__ import annotations
 
@@ -35,8 +45,8 @@ D, NQ, NKV, HD, PAGE, EPS, THETA = 1024, 16, 4, 64, 64, 1e-6, 1e6
 
 
 class Server:
-    def __init__(self, layers: int, batch: int, max_len: int, device="cuda"):
-        self.batch, self.device = batch, device
+    def __init__(self, layers: int, batch: int, max_len: int, device="cuda", pages: int = 0):
+        self.batch, self.device, self.pages = batch, device, pages
         self.max_pages = -(-max_len // PAGE)
         i32 = dict(dtype=torch.int32, device=device)
         n_pages = batch * self.max_pages
@@ -57,6 +67,7 @@ class Server:
         ws = torch.zeros(self.caches[0].workspace_bytes(NQ, max_len), dtype=torch.uint8, device=device)
         for c in self.caches:
             c.workspace = ws
+        self.bounds = [c.empty_bounds() if pages else None for c in self.caches]
 
     def forward(self, x: torch.Tensor, n_new: torch.Tensor, max_new: int) -> torch.Tensor:
         """x [tokens, D]: the new tokens of every sequence, sequence by sequence."""
@@ -65,32 +76,44 @@ class Server:
         pos = torch.empty(T, dtype=torch.int32, device=self.device)
         buddy.buddy_page_plan(self.length, n_new, PAGE, self.table, self.free, self.head, self.kv_len, self.row_start,
                               slot, pos, self.head_out, self.flags)
-        for w_qkv, w_o, (q_gain, k_gain), cache in zip(self.w_qkv, self.w_o, self.gains, self.caches):
+        few = self.pages > 0 and max_new == 1
+        pages, visible = (torch.empty(*n, dtype=torch.int32, device=self.device) for n in ((T, NKV, max(1, self.pages)), (T,)))
+        for w_qkv, w_o, (q_gain, k_gain), cache, bounds in zip(self.w_qkv, self.w_o, self.gains, self.caches, self.bounds):
             h = x.float()
             h = (h * torch.rsqrt(h.square().mean(-1, keepdim=True) + EPS)).to(x.dtype)
             q, k, v = (h @ w_qkv).unflatten(1, (NQ + 2 * NKV, HD)).split((NQ, NKV, NKV), 1)
             q_out, out = torch.empty(2, T, NQ, HD, dtype=x.dtype, device=self.device)
             cache.buddy_kv4_append(q, k, v, pos, slot, self.rope, q_out, q_gain, k_gain, EPS, self.flags)
-            cache.buddy_kv4_attention(q_out, self.kv_len, self.table, out, self.row_start, max_new, flags=self.flags)
+            if self.pages:
+                cache.buddy_kv4_bounds(bounds, self.kv_len, self.table, self.row_start, max_new, self.flags)
+            if few:
+                cache.buddy_kv4_select(q_out, bounds, self.kv_len, self.table, pages, visible, self.row_start, max_new,
+                                       flags=self.flags)
+                cache.buddy_kv4_attention_pages(q_out, visible, pages, out, flags=self.flags)
+            else:
+                cache.buddy_kv4_attention(q_out, self.kv_len, self.table, out, self.row_start, max_new, flags=self.flags)
             x = x + out.flatten(1) @ w_o
-            self.last = (q_out, out)
+            self.last = (q_out, out, pages if few else None)
         self.length.copy_(self.kv_len)
         self.head.copy_(self.head_out)
         return x
 
     def check(self) -> float:
         """Largest deviation of the last layer's last single-token outputs from 64 bits."""
-        q, out = self.last
+        q, out, pages = self.last
         worst = 0.0
         for i in range(self.batch):
             n = int(self.kv_len[i])
             p = torch.arange(n, device=self.device)
-            slot = self.table[i].long()[p // PAGE] * PAGE + p % PAGE
+            ids = self.table[i].long()[p // PAGE]
             k, v = torch.empty(2, n, NKV, HD, device=self.device)
-            self.caches[-1].buddy_kv4_read(slot, k, v)
+            self.caches[-1].buddy_kv4_read(ids * PAGE + p % PAGE, k, v)
             k, v = (x.double().repeat_interleave(NQ // NKV, 1) for x in (k, v))
-            s = torch.softmax(torch.einsum("hd,phd->hp", q[i].double(), k) / math.sqrt(HD), -1)
-            want = torch.einsum("hp,phd->hd", s, v)
+            s = torch.einsum("hd,phd->hp", q[i].double(), k) / math.sqrt(HD)
+            if pages is not None:        # (a page of the sequence is there or not, whole)
+                there = (pages[i][:, None] == ids[None, :, None]).any(-1)
+                s = s.masked_fill(~there.repeat_interleave(NQ // NKV, 0), -math.inf)
+            want = torch.einsum("hp,phd->hd", torch.softmax(s, -1), v)
             worst = max(worst, float((out[i].double() - want).abs().max() / want.abs().max()))
         return worst
 
@@ -134,10 +157,11 @@ def serve(argv=None) -> dict:
     ap.add_argument("--prompt", type=int, default=600, help="longest prompt")
     ap.add_argument("--piece", type=int, default=128, help="tokens of a prompt per call")
     ap.add_argument("--steps", type=int, default=32, help="single tokens after the longest prompt")
+    ap.add_argument("--pages", type=int, default=0, help="pages that a single token attends to (0: all)")
     a = ap.parse_args(argv)
     torch.manual_seed(0)
     # (a sequence gets a token in every call from its prompt's end on)
-    s = Server(a.layers, a.batch, a.prompt + -(-a.prompt // a.piece) + a.steps + 8)
+    s = Server(a.layers, a.batch, a.prompt + -(-a.prompt // a.piece) + a.steps + 8, pages=a.pages)
     bf16 = dict(dtype=torch.bfloat16, device="cuda")
     left = [max(1, a.prompt * (i + 1) // a.batch) for i in range(a.batch)]
     fed = [[] for _ in left]
