@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbuddy.so")
 SOURCES = ["api.cu", "kernels.cu", "attention.cu", "gemm_simt.cu", "gemm_tc.cu", "noalloc.cu", "gemm_pf.cu",
-           "attn_pf.cu", "prefill.cu", "attn_cl.cu", "pages.cu", "kv4_rows.cu", "kv4_attn.cu", "kv4_pf.cu", "kv4_pages.cu"]
+           "attn_pf.cu", "prefill.cu", "attn_cl.cu", "pages.cu", "kv4_rows.cu", "kv4_attn.cu", "kv4_pf.cu", "kv4_pages.cu", "kv4_lists.cu"]
 CALLS = os.path.join(HERE, "_calls.so")
 CALLS_FOR = os.path.join(OUT_DIR, "calls_for.txt")   # the torch and the command that it was built with
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -102,5 +102,8 @@ __device__ __forceinline__ void dequant4(uint32_t w, __half2 s, __half2 s72, uin
 int64_t prompt_workspace(int head_dim, int sms);
 int launch_prompt(AttnArgs4 A, int head_dim, bool wide, int sms, void* ws, cudaStream_t s);
 
+// Lists of pages of so many (token, KV head) streams that a warp takes them alone (kv4_lists.cu).
+int launch_lists(const AttnArgs4& A, int head_dim, bool wide, int sms, cudaStream_t s);
+
 }  // namespace kv4
 }  // namespace buddy
