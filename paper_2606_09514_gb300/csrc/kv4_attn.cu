@@ -328,11 +328,50 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
       go = use.next(A);
       continue;
     }
-    Stream<HD, NB, WIDE> rows_of_warp;
-    rows_of_warp.open(A, use.q.t0, use.q.m, g, n, lane);
-    auto& o = rows_of_warp.o;
-    auto& m = rows_of_warp.m;
-    auto& l = rows_of_warp.l;
+    // queries: rows lg of each block of eight, this lane's HD / 4 channels
+    uint32_t qf[NB][KS][2], ql[WIDE ? NB : 1][KS][2];
+    float fac[NB][2];               // of the scores of rows 2 lc and 2 lc + 1
+    int seen[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int r = min(8 * b + lg, rows - 1);
+      const int64_t at = (use.q.t0 + r / G) * A.a.q_stride + (int64_t)(g * G + r % G) * HD + lc * (HD / 4);
+      float x[HD / 4], top = 0.f;
+#pragma unroll
+      for (int e = 0; e < HD / 4; e += 8) {
+        if (WIDE && A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + at + e, x + e);
+        else load8((const bf16*)A.a.q + at + e, x + e);
+      }
+#pragma unroll
+      for (int e = 0; e < HD / 4; ++e) top = fmaxf(top, fabsf(x[e]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      float down, f;
+      row_scale<WIDE>(top, (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f, &down, &f);
+#pragma unroll
+      for (int e = 0; e < HD / 4; e += 2) {
+        const Halves<WIDE> y(x[e] * down, x[e + 1] * down);
+        qf[b][e / 4][(e / 2) & 1] = y.hi;
+        if constexpr (WIDE) ql[b][e / 4][(e / 2) & 1] = y.lo;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        fac[b][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
+        // (rows that are not there repeat the last)
+        seen[b][e] = n - use.q.m + min(8 * b + 2 * lc + e, rows - 1) / G + 1;
+      }
+    }
+    const int all_seen = n - use.q.m + 1;   // positions that every row sees
+    float o[NB][HD / 16][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      m[b][0] = m[b][1] = -INFINITY;
+      l[b][0] = l[b][1] = 0.f;
+#pragma unroll
+      for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[b][t][e] = 0.f;
+    }
 
     for (int c = c0; c < use.c1; c += step) {
       if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp * kStages + take], phase, kWaitLimitNs, &abort_flag)))
@@ -343,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_
       issue(take == 0 ? kStages - 1 : take - 1, kStages - 2);   // to the stage that the chunk before this one has left
       const int p0 = c * kChunk;
 
-      rows_of_warp.chunk(st, places, p0, n, lost, lane);
+      take_chunk<HD, NB, WIDE>(st, places, p0, n, all_seen, lost, lg, lc, qf, ql, fac, seen, o, m, l);
       take = take + 1 == kStages ? 0 : take + 1;
       phase ^= take == 0;
     }
@@ -602,8 +641,9 @@ extern "C" int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv
   return sms > 0 ? workspace_bytes(n_q_heads / n_kv_heads, head_dim, max_new, sms) : -1;
 }
 
-// Lists from which on warps take them alone.
-constexpr int64_t kManyLists = 256;
+// Lists from which on warps take them alone. (Lists of 32 pages of 64 positions, 8 KV heads, 32 query heads, in
+// CTAs' turns and by warps alone: 128 lists 17.5 and 24.8 us, 256 27.0 and 28.8, 512 42.2 and 41.4, 1,024 72.4 and 68.2.)
+constexpr int64_t kManyLists = 512;
 
 // Both forms; LISTS: a list of pages for each token and KV head.
 template <bool LISTS>

@@ -22,7 +22,7 @@ namespace kv4 {
 constexpr int kListWarps = 4;
 constexpr int kListThreads = 32 * kListWarps;
 constexpr int kListStages = 4;
-constexpr int kListOpen = 3;     // what beginning and ending a stream costs, in chunks
+constexpr int kListOpen = 2;     // what beginning and ending a stream costs, in chunks
 constexpr int kListWhole = 4;    // streams of at most this many chunks are not cut
 constexpr int kListMaxGrid = 512;   // two partials of eight rows and an arrival counter per warp in the workspace
 template <bool WIDE>
@@ -204,8 +204,40 @@ __global__ void __launch_bounds__(kListThreads, list_ctas<WIDE>()) kv4_lists_ker
   for (bool go = true; go;) {
     // ---- one stream (or the part of it in this share)
     const int n = use.n, nc = chunks_of(n);
-    Stream<HD, 1, WIDE> S;
-    S.open(A, use.i, 1, use.g, n, lane);
+    // queries: row lg, this lane's HD / 4 channels (rows that are not there repeat the last)
+    uint32_t qf[1][HD / 16][2], ql[1][HD / 16][2];
+    float fac[1][2], o[1][HD / 16][4], m[1][2], l[1][2];
+    const int seen[1][2] = {{n, n}};
+    {
+      const int64_t at = use.i * A.a.q_stride + (int64_t)(use.g * G + min(lg, G - 1)) * HD + lc * (HD / 4);
+      float x[HD / 4], top = 0.f;
+#pragma unroll
+      for (int e = 0; e < HD / 4; e += 8) {
+        if (WIDE && A.a.q_dtype == BUDDY_DTYPE_F32) load8((const float*)A.a.q + at + e, x + e);
+        else load8((const bf16*)A.a.q + at + e, x + e);
+      }
+#pragma unroll
+      for (int e = 0; e < HD / 4; ++e) top = fmaxf(top, fabsf(x[e]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      float down, f;
+      row_scale<WIDE>(top, (A.a.scale != 0.f ? A.a.scale : rsqrtf((float)HD)) * 1.4426950408889634f, &down, &f);
+#pragma unroll
+      for (int e = 0; e < HD / 4; e += 2) {
+        const Halves<WIDE> y(x[e] * down, x[e + 1] * down);
+        qf[0][e / 4][(e / 2) & 1] = y.hi;
+        if constexpr (WIDE) ql[0][e / 4][(e / 2) & 1] = y.lo;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        fac[0][e] = __shfl_sync(0xffffffffu, f, (2 * lc + e) * 4);
+        m[0][e] = -INFINITY, l[0][e] = 0.f;
+      }
+#pragma unroll
+      for (int t = 0; t < HD / 16; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[0][t][e] = 0.f;
+    }
     for (int c = use.c; c < use.c1; ++c) {
       if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&full[warp * kListStages + take], phase, kWaitLimitNs, &abort_flag)))
         more = false;
@@ -213,14 +245,14 @@ __global__ void __launch_bounds__(kListThreads, list_ctas<WIDE>()) kv4_lists_ker
       const uint32_t lost = gone & 3u;
       gone >>= 2;
       issue(take == 0 ? kListStages - 1 : take - 1, kListStages - 2);   // to the stage that the chunk before this one has left
-      S.chunk(st, places, c * kChunk, n, lost, lane);
+      take_chunk<HD, 1, WIDE>(st, places, c * kChunk, n, n, lost, lg, lc, qf, ql, fac, seen, o, m, l);
       take = take + 1 == kListStages ? 0 : take + 1;
       phase ^= take == 0;
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
-      for (int x = 4; x < 32; x <<= 1) S.l[0][e] += __shfl_xor_sync(0xffffffffu, S.l[0][e], x);
+      for (int x = 4; x < 32; x <<= 1) l[0][e] += __shfl_xor_sync(0xffffffffu, l[0][e], x);
     const bool whole = use.c == 0 && use.c1 == nc;
     const int64_t at = (int64_t)use.i * A.a.out_stride + (int64_t)use.g * G * HD;
     const int first = W - (start < 0 ? (share - 1 - start) / share : 0), last = W + (start + nc - 1) / share;   // warps of the stream
@@ -231,12 +263,12 @@ __global__ void __launch_bounds__(kListThreads, list_ctas<WIDE>()) kv4_lists_ker
     for (int e = 0; e < 2; ++e) {
       const int r = 2 * lc + e;
       if (r >= G) continue;
-      const float inv = !whole ? 1.f : S.m[0][e] == -INFINITY ? 0.f : 1.f / S.l[0][e];
-      if (!whole && lg == 0) part[r] = S.m[0][e], part[8 + r] = S.l[0][e];
+      const float inv = !whole ? 1.f : m[0][e] == -INFINITY ? 0.f : 1.f / l[0][e];
+      if (!whole && lg == 0) part[r] = m[0][e], part[8 + r] = l[0][e];
 #pragma unroll
       for (int t = 0; t < HD / 16; t += 2) {
         const int ch = lg * (HD / 8) + 2 * t;
-        const float4 v = make_float4(S.o[0][t][e] * inv, S.o[0][t][e + 2] * inv, S.o[0][t + 1][e] * inv, S.o[0][t + 1][e + 2] * inv);
+        const float4 v = make_float4(o[0][t][e] * inv, o[0][t][e + 2] * inv, o[0][t + 1][e] * inv, o[0][t + 1][e + 2] * inv);
         if (!whole) *reinterpret_cast<float4*>(part + 16 + r * HD + ch) = v;
         else if (A.a.out_dtype == BUDDY_DTYPE_F32) *reinterpret_cast<float4*>((float*)A.a.out + at + r * HD + ch) = v;
         else *reinterpret_cast<uint2*>((bf16*)A.a.out + at + r * HD + ch) = make_uint2(tca::pack_bf16(v.x, v.y), tca::pack_bf16(v.z, v.w));
@@ -263,14 +295,14 @@ __global__ void __launch_bounds__(kListThreads, list_ctas<WIDE>()) kv4_lists_ker
 #pragma unroll 2
         for (int w = first; w <= last; ++w) {
           const float* const p = slot(w);
-          float m[8], l[8], y[8][CH];
+          float pm[8], pl[8], y[8][CH];
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            m[r] = -INFINITY, l[r] = 0.f;
+            pm[r] = -INFINITY, pl[r] = 0.f;
 #pragma unroll
             for (int x = 0; x < CH; ++x) y[r][x] = 0.f;
             if (r < G) {
-              m[r] = __ldcg(p + r), l[r] = __ldcg(p + 8 + r);
+              pm[r] = __ldcg(p + r), pl[r] = __ldcg(p + 8 + r);
               if constexpr (CH == 4) {
                 const float4 z = __ldcg(reinterpret_cast<const float4*>(p + 16 + r * HD) + lane);
                 y[r][0] = z.x, y[r][1] = z.y, y[r][CH - 2] = z.z, y[r][CH - 1] = z.w;
@@ -282,9 +314,9 @@ __global__ void __launch_bounds__(kListThreads, list_ctas<WIDE>()) kv4_lists_ker
           }
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            const float to = fmaxf(M[r], m[r]), ref = to == -INFINITY ? 0.f : to;
-            const float a = tca::exp2a(M[r] - ref), b = tca::exp2a(m[r] - ref);
-            L[r] = a * L[r] + b * l[r];
+            const float to = fmaxf(M[r], pm[r]), ref = to == -INFINITY ? 0.f : to;
+            const float a = tca::exp2a(M[r] - ref), b = tca::exp2a(pm[r] - ref);
+            L[r] = a * L[r] + b * pl[r];
 #pragma unroll
             for (int x = 0; x < CH; ++x) v[r][x] = a * v[r][x] + b * y[r][x];
             M[r] = to;

@@ -412,8 +412,8 @@ def many(n, seed=0):
     return [LENGTHS[i % len(LENGTHS)] for i in np.random.default_rng(seed).permutation(n)]
 
 
-@pytest.mark.parametrize("heads,n", [((4, 2, 64), 150), ((5, 1, 64), 257), ((8, 1, 128), 400), ((7, 7, 128), 60),
-                                     ((14, 2, 128), 130), ((9, 3, 64), 90), ((3, 1, 128), 1000)])
+@pytest.mark.parametrize("heads,n", [((4, 2, 64), 300), ((5, 1, 64), 600), ((8, 1, 128), 520), ((7, 7, 128), 80),
+                                     ((14, 2, 128), 260), ((9, 3, 64), 180), ((3, 1, 128), 1000)])
 @pytest.mark.parametrize("page", [16, 32, 128])
 def test_attention_of_many_lists(heads, n, page):
     """So many lists that warps take them alone; some are cut between warps."""
@@ -428,7 +428,7 @@ def test_attention_of_many_lists(heads, n, page):
 @pytest.mark.parametrize("out_dtype", DTYPES)
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_of_many_lists_types(dtype, out_dtype, hd):
-    lens = many(140)
+    lens = many(260)
     cache, table, vals = make_cache(lens, 16, 2, hd)
     lists = lists_for(lens, table, 16, 2, 20)
     check_pages(cache, lens, vals, *lists, 10, dtype, out_dtype, 0.3, strided=True)
@@ -438,8 +438,8 @@ def test_attention_of_many_lists_types(dtype, out_dtype, hd):
 @pytest.mark.parametrize("long", [30011, 6000])
 def test_attention_of_long_lists_among_many(long):
     """A list that a hundred warps share, next to short ones and to tokens that are left out."""
-    lens = many(150)
-    lens[3], lens[70], lens[149] = long, long - 16, 17
+    lens = many(270)
+    lens[3], lens[70], lens[269] = long, long - 16, 17
     cache, table, vals = make_cache(lens, 16, 2, 64)
     pages, visible, at = lists_for(lens, table, 16, 2, long // 16 + 1)
     visible[5], visible[80], visible[71] = -1, -1, 0
@@ -447,15 +447,15 @@ def test_attention_of_long_lists_among_many(long):
 
 
 def test_many_lists_without_some_pages():
-    lens = many(200)
+    lens = many(260)
     cache, table, vals = make_cache(lens, 16, 2, 64)
     pages, visible, at = lists_for(lens, table, 16, 2, 12)
     rng = np.random.default_rng(4)
-    drop = [(t, h, e) for t in range(200) for h in range(2) for e in range(12) if e * 16 < visible[t] and rng.random() < 0.3]
+    drop = [(t, h, e) for t in range(260) for h in range(2) for e in range(12) if e * 16 < visible[t] and rng.random() < 0.3]
     for x, d in enumerate(drop):
         pages[d] = (-1, cache.k_pages.shape[0], 2 ** 31 - 1, -2 ** 31)[x % 4]
     check_pages(cache, lens, vals, pages, visible, at, 4, drop=set(drop), flag=BAD_PAGE)
-    q, out, fl = torch.randn(200, 4, 64, device="cuda"), torch.full((200, 4, 64), 77.0, device="cuda"), flags()
+    q, out, fl = torch.randn(260, 4, 64, device="cuda"), torch.full((260, 4, 64), 77.0, device="cuda"), flags()
     visible[150] = 12 * 16 + 1
     cache.buddy_kv4_attention_pages(q, visible, pages, out, flags=fl)
     assert fl.item() == BAD_PAGE | BAD_POSITION and torch.all(out[150] == 77) and not torch.any(out[149] == 77)
@@ -463,21 +463,21 @@ def test_many_lists_without_some_pages():
 
 def test_no_list_at_all():
     """Every token left out: nothing is written, and the workspace stays as it is."""
-    cache, table, vals = make_cache([50] * 300, 16, 1, 64)
-    pages, visible, at = lists_for([50] * 300, table, 16, 1, 2)
+    cache, table, vals = make_cache([50] * 600, 16, 1, 64)
+    pages, visible, at = lists_for([50] * 600, table, 16, 1, 2)
     cache.workspace = torch.zeros(cache.workspace_bytes(4), dtype=torch.uint8, device="cuda")
-    out = torch.full((300, 4, 64), 77.0, device="cuda")
-    cache.buddy_kv4_attention_pages(torch.randn(300, 4, 64, device="cuda"), torch.full_like(visible, -1), pages, out)
+    out = torch.full((600, 4, 64), 77.0, device="cuda")
+    cache.buddy_kv4_attention_pages(torch.randn(600, 4, 64, device="cuda"), torch.full_like(visible, -1), pages, out)
     assert torch.all(out == 77) and not cache.workspace.any()
-    check_pages(cache, [50] * 300, vals, pages, visible, at, 4)
+    check_pages(cache, [50] * 600, vals, pages, visible, at, 4)
 
 
 def test_workspace_counters_are_left_ready():
     """Both forms over one workspace in turn: what one leaves in it the other finds."""
-    lens = [900] * 200
+    lens = [900] * 300
     cache, table, vals = make_cache(lens, 16, 2, 64)
     cache.workspace = torch.zeros(cache.workspace_bytes(4), dtype=torch.uint8, device="cuda")
-    for n in (200, 3, 200, 60, 128):
+    for n in (300, 3, 260, 60, 256, 255):
         pages, visible, at = lists_for(lens[:n], table, 16, 2, 40)
         check_pages(cache, lens[:n], vals, pages, visible, at, 4)
         assert not cache.workspace[:8192].any()
