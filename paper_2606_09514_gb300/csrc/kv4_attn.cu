@@ -66,9 +66,10 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 3;
 // CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two; WIDE
-// 168 and 255).
-template <int NB, bool WIDE>
-__host__ __device__ constexpr int ctas_per_sm() { return (NB == 1 ? 4 : 3) - (WIDE ? 1 : 0); }
+// 168 and 255).  Lists are few and short here, so that latency counts: three CTAs, which spill nothing (one token,
+// lists of 64 pages, 8 KV heads: 9.9 us, with four 10.7; 128 lists of 32 pages 15.6 and 17.4).
+template <int NB, bool WIDE, bool LISTS>
+__host__ __device__ constexpr int ctas_per_sm() { return (NB == 1 && !LISTS ? 4 : 3) - (WIDE ? 1 : 0); }
 constexpr int kWhole = 12;       // streams of at most this many chunks are not cut
 constexpr int kOpen = 10;        // what beginning and ending a stream costs, in chunks
 constexpr int kMany = 2 * kOpen; // shares from this on hold several short streams
@@ -138,7 +139,7 @@ struct Walk {
 
 // LISTS: each (token, KV head) has pages of its own, in a table [tokens, KV heads, max_pages].
 template <int HD, int NB, bool WIDE, bool LISTS>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE>()) kv4_decode_kernel(const AttnArgs4 A) {
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<NB, WIDE, LISTS>()) kv4_decode_kernel(const AttnArgs4 A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t full[kWarps * kStages];
   __shared__ volatile int abort_flag;
@@ -601,7 +602,7 @@ template <int HD, int NB, bool WIDE, bool LISTS>
 static int launch_decode(const AttnArgs4& A, int64_t most, int sms, cudaStream_t s) {
   constexpr int smem = smem_bytes<HD, NB>();
   auto* const kern = kv4_decode_kernel<HD, NB, WIDE, LISTS>;
-  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, ctas_per_sm<NB, WIDE>() * sms));
+  const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, ctas_per_sm<NB, WIDE, LISTS>() * sms));
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return BUDDY_ERR_CUDA;
   return launch_k(kern, grid, kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
 }

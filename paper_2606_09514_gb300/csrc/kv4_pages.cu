@@ -340,6 +340,26 @@ __device__ __forceinline__ uint32_t rank_few(const uint32_t* few, int n, int r, 
   return h0 ? __shfl_sync(0xffffffffu, k0, __ffs(h0) - 1) : __shfl_sync(0xffffffffu, k1, __ffs(h1) - 1);
 }
 
+// How many of m keys (16-byte aligned, zeros behind them up to a multiple of 32) come before that of
+// index j0 + lane: larger ones, and of the equal ones those with a lower index.
+constexpr int kSelRanked = 32;       // per warp of the group: keys up to which each is ranked by itself
+__device__ __forceinline__ int rank_of(const uint32_t* keys, int m, uint32_t mine, int j0, int lane) {
+  int n = 0;
+  auto block = [&](int b, auto before) {
+#pragma unroll
+    for (int x = 0; x < 32; x += 4) {
+      const uint4 k = *reinterpret_cast<const uint4*>(keys + b + x);
+      n += before(k.x, x) + before(k.y, x + 1) + before(k.z, x + 2) + before(k.w, x + 3);
+    }
+  };
+#pragma unroll 1
+  for (int b = 0; b < j0; b += 32) block(b, [&](uint32_t k, int) { return (int)(k >= mine); });
+  block(j0, [&](uint32_t k, int x) { return (int)(k > mine || (k == mine && x < lane)); });
+#pragma unroll 1
+  for (int b = j0 + 32; b < m; b += 32) block(b, [&](uint32_t k, int) { return (int)(k > mine); });
+  return n;
+}
+
 // Where the best r of the keys end: just r of them are above what is returned, or these and the first
 // of those equal to it. By counts of the keys in 256 parts of the range [lo, hi] that holds the r-th,
 // from the top, until a part's keys are all wanted, are few, or are one value.
@@ -424,7 +444,7 @@ template <typename T, int HD, int TT, bool CL>
 __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
   using F = Form<TT, CL>;
   extern __shared__ __align__(128) uint8_t sel_smem[];
-  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots, a multiple of four]
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots, a multiple of 32]
   constexpr int WARPS = F::kWarps, THREADS = F::kThreads;
   __shared__ Search search[TT];
   __shared__ __align__(16) float s_q[TT][2][HD];   // a token's b, then its a
@@ -484,6 +504,8 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     const T* q[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) q[e] = query(t, e);
+    // (the arguments that are wanted first come from memory while the work before this kernel ends)
+    asm volatile("" ::"l"(a.s.kv_len), "l"(a.s.table), "l"(a.bounds), "l"(A.flags), "r"(A.G), "r"(A.slots));
     pdl_wait();
     pdl_trigger();
     read_queries(q);                               // (on their way while the token's sequence is looked for)
@@ -661,6 +683,11 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   else if (TT > 1 && tokens == 3) score(std::integral_constant<int, TT == 1 ? 1 : 3>());
   else if (TT > 1) score(std::integral_constant<int, TT>());
   if (lost && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+  if (rank == 0)                                   // (behind the keys zeros, up to a multiple of 32)
+    for (int x = tid; x < tokens * 32; x += THREADS) {
+      const int j = scored(x / 32) + x % 32;
+      if (j < (scored(x / 32) + 31) / 32 * 32) keys[x / 32 * A.slots + j] = 0u;
+    }
   if (CL) {
     ptx::cluster_sync();
     if (rank != 0) return;
@@ -674,13 +701,22 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, u};
   Search& S = search[u];
   const Keys<F::kGroup, F::kKept> mine(keys + u * A.slots, row + a.first, m, G);
-  const uint32_t at = m <= kSelFew ? rank_few(mine.all, m, r, lane) : threshold(mine, r, S, G);
+  const bool ranked = m <= kSelRanked * F::kGroup;
+  const uint32_t at = ranked ? 0u : threshold(mine, r, S, G);
   // pages above it in each 32, pages with it; then where these of the warp begin
   const uint32_t below = (1u << lane) - 1;
   int32_t* const out = list_of(u) + a.first;
   int above = 0, equal = 0;
   uint32_t up[F::kKept], eq[F::kKept];
-  if (mine.few) {
+  if (ranked) {
+#pragma unroll
+    for (int k = 0; k < F::kKept; ++k) {
+      up[k] = eq[k] = 0u;
+      if (k < kSelRanked / 32 && mine.first + 32 * k < mine.end)
+        up[k] = __ballot_sync(0xffffffffu, mine.there(k, lane) && rank_of(mine.all, m, mine.kept[k], mine.first + 32 * k, lane) < r);
+      above += __popc(up[k]);
+    }
+  } else if (mine.few) {
 #pragma unroll
     for (int k = 0; k < F::kKept; ++k) {
       up[k] = __ballot_sync(0xffffffffu, mine.there(k, lane) && mine.kept[k] > at);
@@ -774,7 +810,7 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
 constexpr int kSelTokens = 4;
 template <typename T, int HD>
 static int dispatch_select(SelectArgs A, cudaStream_t s) {
-  A.slots = (std::max(1, A.a.s.max_pages - A.a.first - A.a.last) + 3) / 4 * 4;
+  A.slots = (std::max(1, A.a.s.max_pages - A.a.first - A.a.last) + 31) / 32 * 32;
   if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
   const int64_t units = (int64_t)A.a.s.n_tok * A.p.nkv;
   int C = 1;
