@@ -149,16 +149,6 @@ __device__ __forceinline__ void load8(const float* p, F2* o) {
   const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
   o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
 }
-// Where two bits of the lowest sixteen are those of axis a (a 0x5555 all along): the values of `y`.
-__device__ __forceinline__ void take8(F2* o, const F2* y, uint32_t w, uint32_t a) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float o0, o1, y0, y1;
-    o[i].get(o0, o1);
-    y[i].get(y0, y1);
-    o[i] = F2(((w >> (4 * i)) & 3u) == a ? y0 : o0, ((w >> (4 * i + 2)) & 3u) == a ? y1 : o1);
-  }
-}
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const F2* x) {
   float y[8];
@@ -213,8 +203,9 @@ __device__ __forceinline__ uint32_t encode8(const F2* x, uint32_t mask, __half* 
 }
 
 // AX: OneAxis, or Axes.  With several axes a lane's eight frequencies mostly have the same (runs
-// of a multiple of eight frequencies per axis): two rows of the tables as with one; where
-// they have not, two more rows for each further axis, and a choice between them.
+// of a multiple of eight frequencies per axis): rows of the tables in wide loads, as with one
+// axis. Where they have not, each value is loaded by itself.  (In wide loads of every axis, and a
+// choice between them, 64 tokens whose frequencies go round three axes took 3.8 us instead of 3.4.)
 template <typename T, int HD, bool CACHE, typename AX>
 __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, const AX ax) {
   constexpr bool AXES = std::is_same<AX, Axes>::value;
@@ -261,9 +252,10 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     for (int h = h0; h < h0 + kRowAhead - 1; ++h) ahead(h);
   }
   int p = R.pos[t], most = p, least = p;        // (of all axes)
+  int q[4] = {p, p, p, p};                      // positions on the axes
+  auto place_of = [&](uint32_t a) { return a & 2 ? (a & 1 ? q[3] : q[2]) : (a & 1 ? q[1] : q[0]); };
   uint32_t mix = 0, axis = 0;                   // two bits of each of the lane's frequencies, the first one's axis
   if constexpr (AXES) {
-    int q[4] = {p, p, p, p};
 #pragma unroll
     for (int a = 1; a < 4; ++a)
       if (a < ax.n) q[a] = R.pos[a * ax.stride + t];
@@ -271,7 +263,7 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     axis = mix & 3u;
     most = max(max(q[0], q[1]), max(q[2], q[3]));
     least = min(min(q[0], q[1]), min(q[2], q[3]));
-    p = axis & 2 ? (axis & 1 ? q[3] : q[2]) : (axis & 1 ? q[1] : q[0]);
+    p = place_of(axis);
   }
   int64_t slot = -1;
   if (CACHE) slot = A.slot[t];
@@ -288,19 +280,16 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
   const bool keep = CACHE && slot >= 0 && slot < end;
   F2 co[4], si[4];
   if (h0 < kk) {
-    load8(R.rope_cos + (int64_t)p * HALF + c, co);
-    load8(R.rope_sin + (int64_t)p * HALF + c, si);
-    if constexpr (AXES) {
-      if (mix != axis * 0x5555u) {
-        for (uint32_t a = 0; a < (uint32_t)ax.n; ++a) {
-          if (a == axis) continue;
-          const int64_t at = (int64_t)R.pos[a * ax.stride + t] * HALF + c;
-          F2 y[4], z[4];
-          load8(R.rope_cos + at, y);
-          load8(R.rope_sin + at, z);
-          take8(co, y, mix, a);
-          take8(si, z, mix, a);
-        }
+    if (!AXES || mix == axis * 0x5555u) {
+      load8(R.rope_cos + (int64_t)p * HALF + c, co);
+      load8(R.rope_sin + (int64_t)p * HALF + c, si);
+    } else {                                    // value by value, all on their way at once
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t u = (int64_t)place_of(mix >> (4 * e)) * HALF + c + 2 * e;
+        const int64_t v = (int64_t)place_of(mix >> (4 * e + 2)) * HALF + c + 2 * e + 1;
+        co[e] = F2(__ldg(R.rope_cos + u), __ldg(R.rope_cos + v));
+        si[e] = F2(__ldg(R.rope_sin + u), __ldg(R.rope_sin + v));
       }
     }
   }
@@ -442,11 +431,23 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
 // the GPU (kRowTeams), up to eight, which share the reads of position and rotation
 // (8,297 tokens of 40 heads 32.3 us, 32.4 with four, 37.7 with two; append of 4,999 tokens of
 // 36 heads and their read 23.8, 24.6 and 26.0).
+// Where the axes change within a lane's frequencies the reads are many and narrow, and shared from fewer rows
+// on: 250 tokens of 40 heads 4.6 us instead of 5.3, 1,000 7.7 instead of 9.4 (an append does more with what it
+// has read: 250 tokens of fp32 7.4 instead of 6.9, so it does not).
 constexpr int64_t kRowTeams = 16384;
+// Whether a lane's eight frequencies have different axes somewhere.
+static bool mixed(const OneAxis&) { return false; }
+static bool mixed(const Axes& a) {
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t w = a.of[j / 2] >> (j % 2 * 16) & 0xFFFFu;
+    if (w != (w & 3u) * 0x5555u) return true;
+  }
+  return false;
+}
 template <typename T, int HD, bool CACHE, typename AX>
 static int launch_rows(RowArgs A, const AX& ax, cudaStream_t s) {
   const int heads = A.r.n_q_heads + A.r.n_kv_heads * (CACHE ? 2 : 1);
-  A.per = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)A.r.n_tok * heads / kRowTeams));
+  A.per = (int)std::min<int64_t>(8, std::max<int64_t>(1, (int64_t)A.r.n_tok * heads / (!CACHE && mixed(ax) ? kRowTeams / 4 : kRowTeams)));
   A.groups = (heads + A.per - 1) / A.per;
   const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
