@@ -784,7 +784,7 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = kv4_select_kernel<T, HD, TT, CL>;
   const size_t smem = F::kRing + sizeof(uint32_t) * (size_t)TT * A.slots;
-  if (smem > 24 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+  if (smem > 40 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   if (!CL) return launch_k(kern, (unsigned)ctas, F::kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
   if (C > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return BUDDY_ERR_CUDA;

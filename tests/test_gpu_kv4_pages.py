@@ -209,6 +209,50 @@ def test_select_several_tokens(dtype):
         check_select(*made, lens, n_new, budget)
 
 
+@pytest.mark.parametrize("lens,n_new", [([16 * 3000 - 3, 16 * 700, 16 * 8000], [3, 1, 6]), ([16 * 9001 - 1, 16 * 30], [2, 3]),
+                                        ([16 * 500, 16 * 130 + 2, 16 * 90, 16 * 260], [4, 9, 2, 5])])
+def test_select_several_tokens_of_many_pages(lens, n_new):
+    """Tokens that share a walk over thousands of pages, and tables too long for that."""
+    for heads, dtype in (((2, 1, 64), torch.bfloat16), ((3, 1, 128), torch.float32)):
+        made = make_select(lens, n_new, 16, heads, dtype, seed=len(lens))
+        for budget in (3, 80, 500):
+            check_select(*made, lens, n_new, budget)
+
+
+def test_select_several_tokens_special_scores():
+    """Ties, NaN, and pages that are not there, for tokens that share a walk."""
+    lens, n_new = [16 * 90, 16 * 300 + 5, 16 * 40], [3, 6, 2]
+    cache, table, bounds, q = make_select(lens, n_new, 16, (4, 2, 64), torch.bfloat16, seed=2, levels=3)
+    for budget in (5, 31, 85):
+        check_select(cache, table, bounds, q, lens, n_new, budget)
+    bounds[table[1, 7].long(), 0, 0, 3] = float("nan")
+    q[1] = float("nan")
+    table[0, 5], table[1, 100], table[2, 3] = -1, 10 ** 7, -9
+    for budget in (5, 30):
+        check_select(cache, table, bounds, q, lens, n_new, budget, flag=BAD_PAGE)
+
+
+def test_select_by_clusters_in_a_graph():
+    lens = [16 * 1000 - 2]
+    cache, table, bounds, q = make_select(lens, [1], 16, (4, 2, 128), torch.bfloat16)
+    pages, visible = torch.empty(1, 2, 30, dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    kv_len = i32(lens)
+    graph = torch.cuda.CUDAGraph()
+    cache.buddy_kv4_select(q, bounds, kv_len, table, pages, visible)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            cache.buddy_kv4_select(q, bounds, kv_len, table, pages, visible)
+    for n in (16 * 1000 - 2, 16 * 31, 16 * 500 + 1, 5):
+        q.copy_(torch.randn_like(q))
+        kv_len.fill_(n)
+        pages.fill_(55)
+        graph.replay()
+        wp, wv = want_pages(q, bounds, table, [n], [1], 16, 30, 1, 1, 1)
+        np.testing.assert_array_equal(pages.cpu().numpy(), wp)
+        assert visible.item() == wv[0]
+
+
 @pytest.mark.parametrize("levels", [1, 2, 5])
 def test_select_ties_go_to_the_lower_position(levels):
     lens = [16 * 50, 16 * 300 + 1, 16 * 1000]
