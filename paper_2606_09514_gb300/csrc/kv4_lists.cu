@@ -21,7 +21,7 @@ namespace kv4 {
 
 constexpr int kListWarps = 4;
 constexpr int kListThreads = 32 * kListWarps;
-constexpr int kListStages = 4;
+constexpr int kListStages = 2;
 constexpr int kListOpen = 2;     // what beginning and ending a stream costs, in chunks
 constexpr int kListWhole = 4;    // streams of at most this many chunks are not cut
 constexpr int kListMaxGrid = 512;   // two partials of eight rows and an arrival counter per warp in the workspace
