@@ -254,7 +254,8 @@ template <int WARPS>
 struct Group {
   int tid, lane, warp, bar;
   __device__ __forceinline__ void sync() const {
-    asm volatile("bar.sync %0, %1;" ::"r"(bar + 1), "n"(32 * WARPS) : "memory");
+    if constexpr (WARPS == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(bar + 1), "n"(32 * WARPS) : "memory");
   }
 };
 
@@ -424,13 +425,13 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// The forms of the kernel: one token by a CTA, one by a cluster, four of a sequence by a CTA.
-// Warps and those that look for the pages of one token; loads of a turn of a warp (two copies of
-// 16 bytes per lane each) and turns in flight.
-template <int TT, bool CL>
+// The forms of the kernel: one token by a CTA, one by a cluster (CL), up to TT = 4 of a sequence by a
+// CTA, for one KV head or two (HG). Warps and those that look for the pages of one token and head;
+// loads of a turn of a warp (two copies of 16 bytes per lane each) and turns in flight.
+template <int TT, int HG, bool CL>
 struct Form {
-  static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2,
-                       kTurns = TT == 1 ? 2 : 4, kGroup = kWarps / TT, kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = TT == 1 && !CL ? 7 : 2;
+  static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2, kTurns = TT == 1 ? 2 : 4;
+  static constexpr int kGroup = kWarps / (TT * HG), kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = TT == 1 && !CL ? 7 : 2;
   static constexpr int kRing = kWarps * kTurns * kLoads * 1024;   // bytes
 };
 
@@ -439,30 +440,33 @@ struct Form {
 // one the scores. A page has HD / 8 lanes: the lower ones two eights each of the smallest of its
 // channels, by b, the upper ones of the largest, by a; the two eights are those that the
 // score's sum takes first, and go side by side through packed instructions. Every lane reads what
-// it has copied itself, so that the turns in flight need neither registers nor barriers.
-template <typename T, int HD, int TT, bool CL>
-__global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
-  using F = Form<TT, CL>;
+// it has copied itself, so that the turns in flight need neither registers nor barriers. Two heads'
+// bounds of a page lie next to each other and go to neighbouring lanes.
+template <typename T, int HD, int TT, int HG, bool CL>
+__global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
+  using F = Form<TT, HG, CL>;
   extern __shared__ __align__(128) uint8_t sel_smem[];
-  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [TT][slots, a multiple of 32]
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(sel_smem + F::kRing);   // [HG][TT][slots, a multiple of 32]
   constexpr int WARPS = F::kWarps, THREADS = F::kThreads;
-  __shared__ Search search[TT];
-  __shared__ __align__(16) float s_q[TT][2][HD];   // a token's b, then its a
-  static_assert(!CL || TT == 1, "");
-  constexpr int LPP = HD / 8, PPW = 32 / LPP;      // lanes of a page, pages of a warp's load
+  __shared__ Search search[HG * TT];
+  __shared__ __align__(16) float s_q[HG * TT][2][HD];   // a token's b, then its a
+  __shared__ __align__(16) int s_len[TT > 1 ? THREADS : 4];
+  __shared__ int4 s_seq;
+  static_assert((!CL || TT == 1) && (HG == 1 || TT > 1), "");
+  constexpr int LPP = HD / 8, PPW = 32 / LPP / HG; // lanes of a head's page, pages of a warp's load
   constexpr int LOADS = F::kLoads;
   constexpr int TURNS = F::kTurns, PAGES = LOADS * PPW, IDS = 32 / PAGES;   // turns whose ids a warp reads at once
   const buddy_kv4_select_args& a = A.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = CL ? ptx::cluster_rank() : 0, C = CL ? ptx::cluster_size() : 1;
   const unsigned unit = blockIdx.x / C;
-  const int g = (int)(unit % (unsigned)A.p.nkv);
-  int t = (int)(unit / (unsigned)A.p.nkv), i = 0, chunk = 0;
+  const int gs = A.p.nkv / HG, g = (int)(unit % (unsigned)gs) * HG;   // (the first of HG heads)
+  int t = (int)(unit / (unsigned)gs), i = 0, chunk = 0;
   const bool by_seq = TT > 1 && A.chunks > 0;
   if (by_seq) {
     i = t / A.chunks, chunk = t % A.chunks;
     if (i >= a.s.batch) {                          // behind the sequences' CTAs: the tokens that are in none
-      const int64_t x = ((int64_t)unit - (int64_t)a.s.batch * A.chunks * A.p.nkv) * THREADS + tid;
+      const int64_t x = ((int64_t)unit - (int64_t)a.s.batch * A.chunks * gs) * THREADS + tid;
       pdl_wait();
       pdl_trigger();
       if (x >= a.s.n_tok) return;
@@ -474,11 +478,12 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
       return;
     }
   }
-  for (int b = tid; b < TT * kSelBins; b += THREADS) search[b / kSelBins].bins[b % kSelBins] = 0;
-  if (tid < TT) search[tid].n_few = 0;
-  constexpr int PER = (TT * HD + THREADS - 1) / THREADS;
-  auto query = [&](int t, int e) {
-    return (const T*)a.q + min(t + (tid + e * THREADS) / HD, a.s.n_tok - 1) * a.q_stride + (int64_t)g * A.G * HD + tid % HD;
+  for (int b = tid; b < HG * TT * kSelBins; b += THREADS) search[b / kSelBins].bins[b % kSelBins] = 0;
+  if (tid < HG * TT) search[tid].n_few = 0;
+  constexpr int PER = (HG * TT * HD + THREADS - 1) / THREADS;
+  auto query = [&](int t, int e) {                 // of a head and token
+    const int hu = (tid + e * THREADS) / HD;
+    return (const T*)a.q + min(t + hu % TT, a.s.n_tok - 1) * a.q_stride + (int64_t)(g + hu / TT) * A.G * HD + tid % HD;
   };
   T x[PER][8];
   auto read_queries = [&](const T* const (&q)[PER]) {
@@ -486,16 +491,36 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     for (int e = 0; e < PER; ++e)
 #pragma unroll
       for (int h = 0; h < 8; ++h)
-        if ((tid + e * THREADS) / HD < TT && h < A.G) x[e][h] = q[e][h * HD];
+        if ((tid + e * THREADS) / HD < HG * TT && h < A.G) x[e][h] = q[e][h * HD];
   };
   Rows s{};
   bool ok = true;
   if (by_seq) {
     pdl_wait();
     pdl_trigger();
-    ok = rows_of(a.s, A.p.shift, i, &s) && chunk * TT < s.m;
+    if (a.s.batch <= THREADS) {                    // the longest sequences first: theirs would be waited for at the end
+      ok = tid < a.s.batch && rows_of(a.s, A.p.shift, tid, &s);
+      s_len[tid] = tid < a.s.batch ? s.n : INT32_MIN;
+      __syncthreads();
+      if (tid < a.s.batch) {
+        int rank = 0;
+        for (int j = 0; j < a.s.batch; j += 4) {
+          const int4 y = *reinterpret_cast<const int4*>(s_len + j);
+          rank += (y.x > s.n || (y.x == s.n && j < tid)) + (y.y > s.n || (y.y == s.n && j + 1 < tid)) +
+                  (y.z > s.n || (y.z == s.n && j + 2 < tid)) + (y.w > s.n || (y.w == s.n && j + 3 < tid));
+        }
+        if (rank == i) s_seq = make_int4(ok ? tid : -1, s.t0, s.m, s.n);
+      }
+      __syncthreads();
+      const int4 y = s_seq;
+      i = y.x;
+      s = Rows{y.y, y.z, y.w};
+      ok = i >= 0;
+    } else {
+      ok = rows_of(a.s, A.p.shift, i, &s);
+    }
     t = s.t0 + chunk * TT;
-    if (!ok) return;                               // (the CTAs behind see to the tokens)
+    if (!ok || chunk * TT >= s.m) return;          // (the CTAs behind see to the tokens)
     const T* q[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) q[e] = query(t, e);
@@ -540,7 +565,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     const int p = p0 + tid, N = pages_of(p);
     a.visible[t + tid] = N == 0 ? 0 : ((min(N, a.budget) - 1) << A.p.shift) + (p & in_page) + 1;
   }
-  auto list_of = [&](int u) { return a.pages + ((int64_t)(t + u) * A.p.nkv + g) * a.budget; };
+  auto list_of = [&](int u, int hl) { return a.pages + ((int64_t)(t + u) * A.p.nkv + g + hl) * a.budget; };
   const int r = a.budget - a.first - a.last;
   auto scored = [&](int u) { const int N = pages_of(p0 + u); return u < tokens && N > a.budget ? N - a.first - a.last : 0; };
   const int M = scored(tokens - 1);                // of the last token: the most
@@ -549,11 +574,18 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     const int ends = a.first + a.last;
     for (int x = tid; x < tokens * ends; x += THREADS) {
       const int u = TT == 1 ? 0 : x / ends, j = x - u * ends, N = pages_of(p0 + u);
-      if (N > a.budget) list_of(u)[j < a.first ? j : a.budget - ends + j] = row[j < a.first ? j : N - ends + j];
+      if (N <= a.budget) continue;
+      const int32_t id = row[j < a.first ? j : N - ends + j];
+#pragma unroll
+      for (int hl = 0; hl < HG; ++hl) list_of(u, hl)[j < a.first ? j : a.budget - ends + j] = id;
     }
     for (int u = 0; u < tokens && pages_of(p0 + u) <= a.budget; ++u) {
       const int N = pages_of(p0 + u);
-      for (int j = tid; j < a.budget; j += THREADS) list_of(u)[j] = j < N ? row[j] : -1;
+      for (int j = tid; j < a.budget; j += THREADS) {
+        const int32_t id = j < N ? row[j] : -1;
+#pragma unroll
+        for (int hl = 0; hl < HG; ++hl) list_of(u, hl)[j] = id;
+      }
     }
   };
   if (M == 0 || r == 0) {                          // (the same in the whole cluster)
@@ -566,7 +598,8 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   const int turns = M > j_first ? (M - j_first + turn - 1) / turn : 0;
   const uint32_t ring = ptx::smem_u32(sel_smem) + (uint32_t)(warp * TURNS * LOADS * 1024 + lane * 16);
   const int eight = lane % (LPP / 2), high = lane / (LPP / 2) % 2;   // the lane's first of two; of lo or of hi
-  const __half* const bounds = (const __half*)a.bounds + ((int64_t)g * 2 + high) * HD + eight * 8;
+  const int hl = lane / LPP % HG, pl = lane / LPP / HG;              // its head, and its page of a load's
+  const __half* const bounds = (const __half*)a.bounds + ((int64_t)(g + hl) * 2 + high) * HD + eight * 8;
   const int64_t per_page = (int64_t)A.p.nkv * 2 * HD;
   uint32_t gone = 0;                               // of the loads in flight and the one at hand, LOADS bits a turn, the newest lowest
   auto issue = [&](int n, int at) {                // (a turn that is not there copies nothing: the counts of groups go on)
@@ -575,7 +608,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
       if (n > 0 && n % IDS == 0) ids = ids_next, ids_next = ids_of(n + IDS);
       int id[LOADS];
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k) id[k] = __shfl_sync(0xffffffffu, ids, n % IDS * PAGES + k * PPW + lane / LPP);
+      for (int k = 0; k < LOADS; ++k) id[k] = __shfl_sync(0xffffffffu, ids, n % IDS * PAGES + k * PPW + pl);
 #pragma unroll
       for (int k = 0; k < LOADS; ++k) {
         const bool there = (uint32_t)id[k] < (uint32_t)A.p.n_pages;
@@ -593,7 +626,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
     const int u = (tid + e * THREADS) / HD, c = tid % HD;
-    if (u >= TT) continue;
+    if (u >= HG * TT) continue;
     float up = 0.f, down = 0.f;
 #pragma unroll
     for (int h = 0; h < 8; ++h) {
@@ -614,7 +647,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
     F2 f[NT][8];                                   // this lane's channels of both eights
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-      const float4* const y = reinterpret_cast<const float4*>(&s_q[u][high][eight * 8]);
+      const float4* const y = reinterpret_cast<const float4*>(&s_q[hl * TT + u][high][eight * 8]);
       const float4 a0 = y[0], a1 = y[1], b0 = y[HD / 8], b1 = y[HD / 8 + 1];
       f[u][0] = pair(a0.x, b0.x), f[u][1] = pair(a0.y, b0.y), f[u][2] = pair(a0.z, b0.z), f[u][3] = pair(a0.w, b0.w);
       f[u][4] = pair(a1.x, b1.x), f[u][5] = pair(a1.y, b1.y), f[u][6] = pair(a1.z, b1.z), f[u][7] = pair(a1.w, b1.w);
@@ -628,7 +661,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
 #pragma unroll
     for (int e = 0; e < LEFT; ++e) {
       u_mine[e] = (mine_at + e) % NP;
-      j_mine[e] = j_first + (mine_at + e) / NP * PPW + lane / LPP;
+      j_mine[e] = j_first + (mine_at + e) / NP * PPW + pl;
       j_end[e] = lane & TWINS ? 0 : scored(u_mine[e]);
     }
     for (int n = 0, at = 0; n < turns; ++n, at = at + 1 == TURNS ? 0 : at + 1) {
@@ -674,7 +707,7 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
         const uint32_t key = there ? key_of(v[e]) : 0u;
         lost |= !there;
         if (CL) put_first(&keys[j], key);
-        else keys[u_mine[e] * A.slots + j] = key;
+        else keys[(hl * TT + u_mine[e]) * A.slots + j] = key;
       }
     }
   };
@@ -684,9 +717,9 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   else if (TT > 1) score(std::integral_constant<int, TT>());
   if (lost && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
   if (rank == 0)                                   // (behind the keys zeros, up to a multiple of 32)
-    for (int x = tid; x < tokens * 32; x += THREADS) {
-      const int j = scored(x / 32) + x % 32;
-      if (j < (scored(x / 32) + 31) / 32 * 32) keys[x / 32 * A.slots + j] = 0u;
+    for (int x = tid; x < HG * TT * 32; x += THREADS) {
+      const int end = scored(x / 32 % TT), j = end + x % 32;
+      if (j < (end + 31) / 32 * 32) keys[x / 32 * A.slots + j] = 0u;
     }
   if (CL) {
     ptx::cluster_sync();
@@ -696,16 +729,16 @@ __global__ void __launch_bounds__(Form<TT, CL>::kThreads, Form<TT, CL>::kCtas) k
   }
 
   // ---- the best r, in their order: each token by a group of warps
-  const int u = warp / F::kGroup, m = scored(u);
+  const int hu = warp / F::kGroup, u = hu % TT, m = scored(u);
   if (m == 0) return;
-  const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, u};
-  Search& S = search[u];
-  const Keys<F::kGroup, F::kKept> mine(keys + u * A.slots, row + a.first, m, G);
+  const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, hu};
+  Search& S = search[hu];
+  const Keys<F::kGroup, F::kKept> mine(keys + hu * A.slots, row + a.first, m, G);
   const bool ranked = m <= kSelRanked * F::kGroup;
   const uint32_t at = ranked ? 0u : threshold(mine, r, S, G);
   // pages above it in each 32, pages with it; then where these of the warp begin
   const uint32_t below = (1u << lane) - 1;
-  int32_t* const out = list_of(u) + a.first;
+  int32_t* const out = list_of(u, hu / TT) + a.first;
   int above = 0, equal = 0;
   uint32_t up[F::kKept], eq[F::kKept];
   if (ranked) {
@@ -770,20 +803,20 @@ static bool seqs_ok(const buddy_kv4_cache* c, const buddy_kv4_seqs& s) {
          (s.row_start || (s.n_tok == s.batch && s.max_new == 1));
 }
 
-template <typename T, int HD, int TT, bool CL>
+template <typename T, int HD, int TT, int HG, bool CL>
 static int launch_select(SelectArgs A, int C, cudaStream_t s) {
-  using F = Form<TT, CL>;
-  int64_t ctas = (int64_t)A.a.s.n_tok * A.p.nkv * C;
+  using F = Form<TT, HG, CL>;
+  int64_t ctas = (int64_t)A.a.s.n_tok * (A.p.nkv / HG) * C;
   if (TT > 1) {                                    // by sequences, unless few of them have as many tokens as the longest
     const int64_t chunks = (A.a.s.max_new + TT - 1) / TT;
     if (A.a.s.batch * chunks <= A.a.s.n_tok) {
       A.chunks = (int)chunks;
-      ctas = A.a.s.batch * chunks * A.p.nkv + (A.a.s.n_tok + F::kThreads - 1) / F::kThreads;
+      ctas = A.a.s.batch * chunks * (A.p.nkv / HG) + (A.a.s.n_tok + F::kThreads - 1) / F::kThreads;
     }
   }
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  auto* const kern = kv4_select_kernel<T, HD, TT, CL>;
-  const size_t smem = F::kRing + sizeof(uint32_t) * (size_t)TT * A.slots;
+  auto* const kern = kv4_select_kernel<T, HD, TT, HG, CL>;
+  const size_t smem = F::kRing + sizeof(uint32_t) * (size_t)(HG * TT) * A.slots;
   if (smem > 40 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   if (!CL) return launch_k(kern, (unsigned)ctas, F::kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
@@ -804,18 +837,25 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kern, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 
-// Several tokens of a sequence share a walk where there may be such; clusters, where a table has more pages than a
-// CTA's warps take at once, as large as leaves every warp a turn and the GPU (four CTAs
-// an SM) room for all.
+// Several tokens of a sequence share a walk where there may be such, over two heads' bounds where the table
+// is short, so that what a CTA does before and after its walk counts (31 sequences of up to five tokens, 40 KV
+// heads, 256 pages: 47.5 us, one head each 57.7; 9 prompts of up to 1,500 tokens, 8 KV heads, 60 pages: 142 and
+// 246; 750 pages, 25 to 750 in use: 54.8 and 45.4, the longest walk being the last to end). Clusters, where a
+// table has more pages than a CTA's warps take at once, as large as leaves every warp a turn and the
+// GPU (four CTAs an SM) room for all (one token of 8 KV heads over 1,876 pages: 64 us with a CTA for each head).
 constexpr int kSelTokens = 4;
+constexpr int kSelPairs = 512;          // scores of a token
 template <typename T, int HD>
 static int dispatch_select(SelectArgs A, cudaStream_t s) {
   A.slots = (std::max(1, A.a.s.max_pages - A.a.first - A.a.last) + 31) / 32 * 32;
-  if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) return launch_select<T, HD, kSelTokens, false>(A, 1, s);
+  if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) {
+    if (A.p.nkv % 2 == 0 && A.slots <= kSelPairs) return launch_select<T, HD, kSelTokens, 2, false>(A, 1, s);
+    return launch_select<T, HD, kSelTokens, 1, false>(A, 1, s);
+  }
   const int64_t units = (int64_t)A.a.s.n_tok * A.p.nkv;
   int C = 1;
-  while (C < kSelCluster && 2 * C * Form<1, true>::kWarps * Form<1, true>::kLoads * (256 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
-  return C > 1 ? launch_select<T, HD, 1, true>(A, C, s) : launch_select<T, HD, 1, false>(A, 1, s);
+  while (C < kSelCluster && 2 * C * Form<1, 1, true>::kWarps * Form<1, 1, true>::kLoads * (256 / HD) <= A.slots && units * 2 * C <= 4 * 152) C *= 2;
+  return C > 1 ? launch_select<T, HD, 1, 1, true>(A, C, s) : launch_select<T, HD, 1, 1, false>(A, 1, s);
 }
 
 }  // namespace buddy
