@@ -37,7 +37,6 @@ __device__ __forceinline__ bool rows_of(const buddy_kv4_seqs& S, int shift, int 
 
 // ------------------------------------------------------------------ bounds
 constexpr int kBoundWarps = 4;
-constexpr int kBoundLoads = 8;          // rows of codes in flight per lane
 
 struct BoundArgs {
   buddy_kv4_seqs s;
@@ -53,7 +52,13 @@ __device__ __forceinline__ __half2 shfl_xor(__half2 v, int o) {
 
 // A warp has a page's keys of one head: HD / 16 lanes a position, 16 channels a lane, smallest
 // and largest of them in registers, then over the lanes.  The values are exact in half
-// (kv4.cuh), and so are the bounds.
+// (kv4.cuh), and so are the bounds. What is recomputed is the page as it stands, not what the
+// call has added to it: no order of writes and no earlier bounds show in the result.
+//
+// Bound by instructions: 120,001 positions of 8 KV heads (77 MB) take 19.4 us, 4.0 TB/s, of which a word of
+// eight channels costs thirteen logical or comparing instructions and six of the products'. (Up to 16
+// positions per lane on their way; with 8 20.0 us. Comparisons of three fp32 values at once: 29.8 us.)
+// The last pages of 250 sequences take 3.7 us, the chain of length, page id and keys.
 template <int HD>
 __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const BoundArgs A) {
   constexpr int LPR = HD / 16, RPL = 32 / LPR;     // lanes per position, positions per load
@@ -110,17 +115,24 @@ __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const Boun
       for (int e = 0; e < 8; ++e) lo[e] = __hmin2_nan(lo[e], as_h2(v[e])), hi[e] = __hmax2_nan(hi[e], as_h2(v[e]));
     }
   };
-  using Few = std::integral_constant<int, 16 / RPL>;       // 16 positions of the warp
-  using Many = std::integral_constant<int, kBoundLoads>;
+  auto whole = [&](auto number) {                  // a page in one go, or in several
+    constexpr int N = decltype(number)::value;
+#pragma unroll 1
+    for (int r0 = row; r0 < end; r0 += N * RPL) take(number, std::false_type(), r0);
+  };
+  constexpr int FEW = 16 / RPL;                    // 16 positions of the warp
+  const int loads = (1 << A.p.shift) / RPL;
   if (end < 1 << A.p.shift) {
 #pragma unroll 1
-    for (int r0 = row; r0 < end; r0 += Few::value * RPL) take(Few(), std::true_type(), r0);
-  } else if (kBoundLoads * RPL > end) {
-#pragma unroll 1
-    for (int r0 = row; r0 < end; r0 += Few::value * RPL) take(Few(), std::false_type(), r0);
+    for (int r0 = row; r0 < end; r0 += FEW * RPL) take(std::integral_constant<int, FEW>(), std::true_type(), r0);
+  } else if (loads >= 16) {
+    whole(std::integral_constant<int, 16>());
+  } else if (loads == 8) {
+    whole(std::integral_constant<int, 8>());
+  } else if (loads == 4) {
+    whole(std::integral_constant<int, 4>());
   } else {
-#pragma unroll 1
-    for (int r0 = row; r0 < end; r0 += kBoundLoads * RPL) take(Many(), std::false_type(), r0);
+    whole(std::integral_constant<int, 2>());
   }
 #pragma unroll
   for (int o = LPR; o < 32; o <<= 1)
@@ -442,6 +454,14 @@ struct Form {
 // score's sum takes first, and go side by side through packed instructions. Every lane reads what
 // it has copied itself, so that the turns in flight need neither registers nor barriers. Two heads'
 // bounds of a page lie next to each other and go to neighbouring lanes.
+//
+// Bound by latencies where tokens are few: one token of 32 heads over 8 takes 7.9 us over 1,876 pages
+// (7.7 MB): 0.7 for the length, 0.5 for the page ids, 1.2 for the bounds, 0.7 for the cluster's barrier, 2 for the
+// search and the output, the launch; 250 sequences of 8 to 128 pages, 28 heads over 4 (18 MB), 9.1. By
+// instructions where several tokens share a walk: 31 sequences of up to 750 pages and five tokens, 40 KV
+// heads (115 MB), 45 us, 2.5 TB/s. What it gained: copies that need no registers instead of loads 11.8 -> 9.5 us (one token), a search by
+// counts and small ranks 64.8 -> 11.8 with the clusters, packed instructions over pairs of eights and code for
+// each number of tokens 62 -> 55 us (31 sequences), the longest sequences first 55 -> 45.
 template <typename T, int HD, int TT, int HG, bool CL>
 __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
   using F = Form<TT, HG, CL>;
