@@ -206,7 +206,9 @@ __device__ __forceinline__ uint32_t encode8(const F2* x, uint32_t mask, __half* 
 // of a multiple of eight frequencies per axis): rows of the tables in wide loads, as with one
 // axis. Where they have not, each value is loaded by itself.  (In wide loads of every axis, and a
 // choice between them, 64 tokens whose frequencies go round three axes took 3.8 us instead of 3.4.)
-template <typename T, int HD, bool CACHE, typename AX>
+// ONE: a team has one head, which it loads itself (with the copies' code 64 tokens appended and read took 5.0 us
+// instead of 4.8).
+template <typename T, int HD, bool CACHE, typename AX, bool ONE>
 __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, const AX ax) {
   constexpr bool AXES = std::is_same<AX, Axes>::value;
   constexpr int LPH = HD / 16, HALF = HD / 2;
@@ -221,7 +223,7 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
   const int grp = (int)(blockIdx.x % (unsigned)A.groups);
   const int64_t t = (int64_t)(blockIdx.x / (unsigned)A.groups) * (kRowThreads / LPH) + threadIdx.x / LPH;
   if (t >= R.n_tok) return;                     // (whole teams)
-  const int h0 = grp * A.per, h1 = min(h0 + A.per, heads);
+  const int h0 = ONE ? grp : grp * A.per, h1 = ONE ? h0 + 1 : min(h0 + A.per, heads);
 
   const int c = tl * 8;                         // this lane's channels: c .. c + 7 of both halves
   auto row = [&](int h) -> const T* {
@@ -244,8 +246,7 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  const bool one = A.per == 1;
-  if (one) {
+  if constexpr (ONE) {
     lo.load(row(h0));
     hi.load(row(h0) + HALF);
   } else {
@@ -274,7 +275,7 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     if (bad) atomicOr(A.flags, bad);
   }
   if (!ok) {
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    if constexpr (!ONE) asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
   const bool keep = CACHE && slot >= 0 && slot < end;
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
     F2 a[4], b[4];                              // lower and upper half
-    if (!one) {
+    if constexpr (!ONE) {
       ahead(h + kRowAhead - 1);                 // to where the head before this one was
       asm volatile("cp.async.wait_group %0;" ::"n"(kRowAhead - 1) : "memory");
       const uint8_t* const at = rows_smem + (h - h0) % kRowAhead * PIECES * (kRowThreads * 16) + threadIdx.x * 16;
@@ -451,7 +452,8 @@ static int launch_rows(RowArgs A, const AX& ax, cudaStream_t s) {
   A.groups = (heads + A.per - 1) / A.per;
   const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  return launch_k(qk_rows_kernel<T, HD, CACHE, AX>, (unsigned)ctas, kRowThreads, A.per > 1 ? row_ring<T>() : 0, s, true, A, ax) == cudaSuccess
+  auto* const kern = A.per == 1 ? qk_rows_kernel<T, HD, CACHE, AX, true> : qk_rows_kernel<T, HD, CACHE, AX, false>;
+  return launch_k(kern, (unsigned)ctas, kRowThreads, A.per > 1 ? row_ring<T>() : 0, s, true, A, ax) == cudaSuccess
              ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 template <bool CACHE, typename AX>
