@@ -14,10 +14,10 @@
 // program can follow it bit by bit, which the codes need: where a value lies between two
 // codes, one bit decides.
 //
-// Bound by HBM from thousands of tokens on (8,297 of 40 heads, 174 MB: 32.5 us a call, 5.3
-// TB/s, with instructions issued in 55% of the cycles; in fp32, 348 MB, 54.0 us, 6.4 TB/s); below by the latency of position,
-// rotation factors and rows, one after the other: one token 2.6 us, an append of 64 and
-// their read 4.8.
+// Bound by HBM from thousands of tokens on (8,297 of 40 heads, 174 MB: 29.8 us a call, 5.9
+// TB/s, with instructions issued in 59% of the cycles; in fp32, 348 MB, 53.9 us, 6.4 TB/s); below by the latency of position,
+// rotation factors and rows, one after the other: one token 2.5 us, an append of 64 and
+// their read 4.8.  With three axes in runs of frequencies 7,901 tokens take 30.8 us, in turn 34.5.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -50,11 +50,12 @@ struct Axes {
 };
 struct OneAxis {};
 
-// Heads of a team on their way at once (copied to shared memory, which takes no registers: a lane
-// reads what it has copied itself).
+// bf16: heads of a team on their way at once (copied to shared memory, which takes no registers: a lane
+// reads what it has copied itself).  Of fp32 a lane's eight channels are two pieces of 16 bytes, which its
+// neighbours' lie between: their sectors would be fetched twice (8,297 tokens 79 us, with loads of
+// the head after this one 54).
 constexpr int kRowAhead = 3;
-template <typename T>
-__host__ __device__ constexpr int row_ring() { return kRowAhead * kRowThreads * 16 * (int)sizeof(T); }   // bytes
+constexpr int kRowRing = kRowAhead * kRowThreads * 32;   // bytes
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -123,7 +124,6 @@ template <typename T> struct Raw8;
 template <> struct Raw8<bf16> {
   uint4 a;
   __device__ __forceinline__ void load(const bf16* p) { a = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void load(const uint8_t* p, int) { a = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void get(F2* o) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -135,10 +135,6 @@ template <> struct Raw8<float> {
   __device__ __forceinline__ void load(const float* p) {
     a = reinterpret_cast<const float4*>(p)[0];
     b = reinterpret_cast<const float4*>(p)[1];
-  }
-  __device__ __forceinline__ void load(const uint8_t* p, int step) {     // pieces of 16 bytes
-    a = *reinterpret_cast<const float4*>(p);
-    b = *reinterpret_cast<const float4*>(p + step);
   }
   __device__ __forceinline__ void get(F2* o) const {
     o[0] = F2(a.x, a.y), o[1] = F2(a.z, a.w), o[2] = F2(b.x, b.y), o[3] = F2(b.z, b.w);
@@ -232,21 +228,20 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     return (const T*)A.v + t * A.v_stride + (int64_t)(h - kk) * HD + c;
   };
   Raw8<T> lo, hi;
-  // a lane's pieces of 16 bytes of a head, those of the other threads between them
+  // a lane's pieces of 16 bytes of a head's halves, those of the other threads between them
   extern __shared__ __align__(16) uint8_t rows_smem[];
-  constexpr int PIECES = (int)sizeof(T);        // eight channels of both halves: 16 sizeof(T) bytes
   const uint32_t ring = ptx::smem_u32(rows_smem) + threadIdx.x * 16;
   auto ahead = [&](int h) {
     if (h < h1) {
       const T* src = row(h);
-#pragma unroll
-      for (int x = 0; x < PIECES; ++x)
-        copy16(ring + ((h - h0) % kRowAhead * PIECES + x) * (kRowThreads * 16),
-               src + x % (PIECES / 2) * (16 / (int)sizeof(T)) + (x < PIECES / 2 ? 0 : HALF));
+      const uint32_t to = ring + (h - h0) % kRowAhead * (kRowThreads * 32);
+      copy16(to, src);
+      copy16(to + kRowThreads * 16, src + HALF);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if constexpr (ONE) {
+  constexpr bool RING = !ONE && sizeof(T) == 2;
+  if constexpr (!RING) {
     lo.load(row(h0));
     hi.load(row(h0) + HALF);
   } else {
@@ -275,7 +270,7 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
     if (bad) atomicOr(A.flags, bad);
   }
   if (!ok) {
-    if constexpr (!ONE) asm volatile("cp.async.wait_all;" ::: "memory");
+    if constexpr (RING) asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
   const bool keep = CACHE && slot >= 0 && slot < end;
@@ -297,15 +292,19 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
 #pragma unroll 1
   for (int h = h0; h < h1; ++h) {
     F2 a[4], b[4];                              // lower and upper half
-    if constexpr (!ONE) {
+    if constexpr (RING) {
       ahead(h + kRowAhead - 1);                 // to where the head before this one was
       asm volatile("cp.async.wait_group %0;" ::"n"(kRowAhead - 1) : "memory");
-      const uint8_t* const at = rows_smem + (h - h0) % kRowAhead * PIECES * (kRowThreads * 16) + threadIdx.x * 16;
-      lo.load(at, kRowThreads * 16);
-      hi.load(at + PIECES / 2 * (kRowThreads * 16), kRowThreads * 16);
+      const uint8_t* const at = rows_smem + (h - h0) % kRowAhead * (kRowThreads * 32) + threadIdx.x * 16;
+      lo.load(reinterpret_cast<const T*>(at));
+      hi.load(reinterpret_cast<const T*>(at + kRowThreads * 16));
     }
     lo.get(a);
     hi.get(b);
+    if (!RING && h + 1 < h1) {
+      lo.load(row(h + 1));
+      hi.load(row(h + 1) + HALF);
+    }
     if (!CACHE || h < kk) {
       const float* gains = h < kq ? R.q_gain : R.k_gain;
       if (gains) {
@@ -430,8 +429,8 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
 
 // Heads of a team: one while there are few rows, for the shortest chain; more as they fill
 // the GPU (kRowTeams), up to eight, which share the reads of position and rotation
-// (8,297 tokens of 40 heads 32.3 us, 32.4 with four, 37.7 with two; append of 4,999 tokens of
-// 36 heads and their read 23.8, 24.6 and 26.0).
+// (8,297 tokens of 40 heads 29.8 us, a fifth more with four; append of 4,999 tokens of
+// 36 heads and their read 22.4, 12% more with four).
 // Where the axes change within a lane's frequencies the reads are many and narrow, and shared from fewer rows
 // on: 250 tokens of 40 heads 4.6 us instead of 5.3, 1,000 7.7 instead of 9.4 (an append does more with what it
 // has read: 250 tokens of fp32 7.4 instead of 6.9, so it does not).
@@ -453,7 +452,7 @@ static int launch_rows(RowArgs A, const AX& ax, cudaStream_t s) {
   const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = A.per == 1 ? qk_rows_kernel<T, HD, CACHE, AX, true> : qk_rows_kernel<T, HD, CACHE, AX, false>;
-  return launch_k(kern, (unsigned)ctas, kRowThreads, A.per > 1 ? row_ring<T>() : 0, s, true, A, ax) == cudaSuccess
+  return launch_k(kern, (unsigned)ctas, kRowThreads, A.per > 1 && sizeof(T) == 2 ? kRowRing : 0, s, true, A, ax) == cudaSuccess
              ? BUDDY_OK : BUDDY_ERR_CUDA;
 }
 template <bool CACHE, typename AX>
