@@ -42,10 +42,10 @@
 // where they are many, by teams first (one sequence of 120,001 positions, 4 KV heads, 152
 // CTAs each: 49 us with one join, 32 with teams).
 //
-// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 121 us,
+// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 120 us,
 // their copies alone 91 us (94% of HBM's rate), the arithmetic alone 100; a chunk is about
 // 700 instructions of a warp, 350 of them codes to halves.  One token over 2,048 positions
-// takes 9.0 us a call: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
+// takes 8.4 us a call: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
 // for two chunks, 4 for partials, arrival and join.
 #include <cuda_runtime.h>
 
@@ -65,7 +65,8 @@ namespace kv4 {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 // A chunk on its way while one is worked on.  (With two on their way: one token over 120,001 positions 40.4 us instead
-// of 38.9, over 2,048 9.0 instead of 8.4, 250 sequences 91.2 instead of 90.1.)
+// of 38.9, over 2,048 9.0 instead of 8.4, 250 sequences 91.2 instead of 90.1; with two blocks of rows they leave room for
+// fewer CTAs: 64 sequences of 4,096 positions, four tokens, 8 KV heads 147 us instead of 102.)
 constexpr int kStages = 2;
 // CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two; WIDE
 // 168 and 255).  Lists are few and short here, so that latency counts: three CTAs, which spill nothing (one token,
