@@ -516,6 +516,55 @@ def test_no_list_at_all():
     check_pages(cache, [50] * 600, vals, pages, visible, at, 4)
 
 
+def test_many_lists_in_a_graph_and_on_two_streams():
+    """Replays as the lists change, and two calls at once with workspaces of their own: bit by bit what
+    the same call gives by itself."""
+    lens = [700] * 280
+    cache, table, vals = make_cache(lens, 16, 2, 64)
+    q, out = torch.randn(280, 8, 64, device="cuda").bfloat16(), torch.empty(280, 8, 64, dtype=torch.bfloat16, device="cuda")
+    lists = [lists_for([n] * 280, table, 16, 2, 30, seed=n)[:2] for n in (700, 33, 470, 1)]
+    want = []
+    for pages, visible in lists:
+        want.append(torch.empty_like(out))
+        cache.buddy_kv4_attention_pages(q, visible, pages, want[-1])
+    torch.cuda.synchronize()
+    ws = torch.zeros(cache.workspace_bytes(8), dtype=torch.uint8, device="cuda")
+    pages, visible = (t.clone() for t in lists[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.buddy_kv4_attention_pages(q, visible, pages, out, workspace=ws)
+    for (p, v), w in zip(lists, want):
+        pages.copy_(p)
+        visible.copy_(v)
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, w)
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [[torch.zeros_like(out) for _ in lists] for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k, ((p, v), _) in enumerate(zip(lists, want)):
+            for s, o in zip(streams, outs):
+                cache.buddy_kv4_attention_pages(q, v, p, o[k], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for row in outs for o, w in zip(row, want))
+
+
+def test_many_lists_with_nan_keys_and_values():
+    """A NaN that a list's tokens see makes its outputs NaN, one behind the end does not."""
+    lens = [60] * 600
+    cache, table, vals = make_cache(lens, 16, 1, 64, nan_tail=False)
+    pages, visible, at = lists_for(lens, table, 16, 1, 3)
+    scales = [x[:, :, 16 * 32:].view(torch.float16) for x in (cache.k_pages, cache.v_pages)]
+    scales[0][int(pages[3, 0, 0]), 0, 5] = float("nan")      # a key that token 3 sees
+    scales[1][int(pages[8, 0, 1]), 0, 7] = float("nan")      # a value that token 8 sees
+    for k in range(2):
+        scales[k][int(pages[20, 0, 2]), 0, 2 * 12:] = float("nan")      # positions 60 .. 63: behind the end
+    q, out = torch.randn(600, 4, 64, device="cuda"), torch.empty(600, 4, 64, device="cuda")
+    cache.buddy_kv4_attention_pages(q, visible, pages, out)
+    bad = torch.isnan(out).flatten(1).any(1).nonzero().flatten().tolist()
+    assert bad == [3, 8] and torch.isnan(out[3]).all() and torch.isnan(out[8]).any(1).all()
+
+
 def test_workspace_counters_are_left_ready():
     """Both forms over one workspace in turn: what one leaves in it the other finds."""
     lens = [900] * 300
