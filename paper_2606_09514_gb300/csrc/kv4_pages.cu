@@ -355,7 +355,7 @@ __device__ __forceinline__ uint32_t rank_few(const uint32_t* few, int n, int r, 
 
 // How many of m keys (16-byte aligned, zeros behind them up to a multiple of 32) come before that of
 // index j0 + lane: larger ones, and of the equal ones those with a lower index.
-constexpr int kSelRanked = 32;       // per warp of the group: keys up to which each is ranked by itself
+constexpr int kSelRanked = 64;       // keys up to which each is ranked by itself
 __device__ __forceinline__ int rank_of(const uint32_t* keys, int m, uint32_t mine, int j0, int lane) {
   int n = 0;
   auto block = [&](int b, auto before) {
@@ -754,7 +754,9 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
   const Group<F::kGroup> G{tid % (32 * F::kGroup), lane, warp % F::kGroup, hu};
   Search& S = search[hu];
   const Keys<F::kGroup, F::kKept> mine(keys + hu * A.slots, row + a.first, m, G);
-  const bool ranked = m <= kSelRanked * F::kGroup;
+  // (A key of each lane's; where the groups are many the counts' round trips cost less than all these comparisons: 250
+  // tokens of 16 pages 7.3 us, 7.9 by ranks; of 64 pages 9.7 and 10.9; 100 sequences of three tokens, 16 pages, 8.8 and 8.0.)
+  const bool ranked = TT > 1 && m <= min(kSelRanked, 32 * F::kGroup);
   const uint32_t at = ranked ? 0u : threshold(mine, r, S, G);
   // pages above it in each 32, pages with it; then where these of the warp begin
   const uint32_t below = (1u << lane) - 1;
@@ -765,8 +767,8 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
 #pragma unroll
     for (int k = 0; k < F::kKept; ++k) {
       up[k] = eq[k] = 0u;
-      if (k < kSelRanked / 32 && mine.first + 32 * k < mine.end)
-        up[k] = __ballot_sync(0xffffffffu, mine.there(k, lane) && rank_of(mine.all, m, mine.kept[k], mine.first + 32 * k, lane) < r);
+      if (k == 0 && mine.first < mine.end)
+        up[k] = __ballot_sync(0xffffffffu, mine.there(k, lane) && rank_of(mine.all, m, mine.kept[k], mine.first, lane) < r);
       above += __popc(up[k]);
     }
   } else if (mine.few) {
