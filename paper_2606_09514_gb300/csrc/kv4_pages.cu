@@ -455,12 +455,12 @@ struct Form {
 // it has copied itself, so that the turns in flight need neither registers nor barriers. Two heads'
 // bounds of a page lie next to each other and go to neighbouring lanes.
 //
-// Bound by latencies where tokens are few: one token of 32 heads over 8 takes 7.9 us over 1,876 pages
+// Bound by latencies where tokens are few: one token of 32 heads over 8 takes 7.7 us over 1,876 pages
 // (7.7 MB): 0.7 for the length, 0.5 for the page ids, 1.2 for the bounds, 0.7 for the cluster's barrier, 2 for the
-// search and the output, the launch; 250 sequences of 8 to 128 pages, 28 heads over 4 (18 MB), 9.1. By
+// search and the output, the launch; 250 sequences of 8 to 128 pages, 28 heads over 4 (18 MB), 8.0. By
 // instructions where several tokens share a walk: 31 sequences of up to 750 pages and five tokens, 40 KV
-// heads (115 MB), 45 us, 2.5 TB/s. What it gained: copies that need no registers instead of loads 11.8 -> 9.5 us (one token), a search by
-// counts and small ranks 64.8 -> 11.8 with the clusters, packed instructions over pairs of eights and code for
+// heads (115 MB), 45 us, 2.5 TB/s. What it gained: a search by counts 64.8 -> 11.8 with the clusters (one token), copies
+// that need no registers instead of loads 11.8 -> 9.5, packed instructions over pairs of eights and code for
 // each number of tokens 62 -> 55 us (31 sequences), the longest sequences first 55 -> 45.
 template <typename T, int HD, int TT, int HG, bool CL>
 __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::kCtas) kv4_select_kernel(const SelectArgs A) {
@@ -589,13 +589,18 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
   const int r = a.budget - a.first - a.last;
   auto scored = [&](int u) { const int N = pages_of(p0 + u); return u < tokens && N > a.budget ? N - a.first - a.last : 0; };
   const int M = scored(tokens - 1);                // of the last token: the most
-  // what is in without a score
+  // what is in without a score: the ends of long lists, of which a thread reads its first one early, and all of short ones
+  const int ends = a.first + a.last;
+  auto end_of = [&](int x) {                       // the x-th of all tokens' ends
+    const int u = TT == 1 ? 0 : x / ends, j = x - u * ends, N = pages_of(p0 + u);
+    return N > a.budget ? row[j < a.first ? j : N - ends + j] : 0;
+  };
+  const int32_t early = (TT > 1 || CL) && tid < tokens * ends && rank == 0 ? end_of(tid) : 0;
   auto always = [&]() {
-    const int ends = a.first + a.last;
     for (int x = tid; x < tokens * ends; x += THREADS) {
-      const int u = TT == 1 ? 0 : x / ends, j = x - u * ends, N = pages_of(p0 + u);
-      if (N <= a.budget) continue;
-      const int32_t id = row[j < a.first ? j : N - ends + j];
+      const int u = TT == 1 ? 0 : x / ends, j = x - u * ends;
+      if (pages_of(p0 + u) <= a.budget) continue;
+      const int32_t id = (TT > 1 || CL) && x == tid ? early : end_of(x);
 #pragma unroll
       for (int hl = 0; hl < HG; ++hl) list_of(u, hl)[j < a.first ? j : a.budget - ends + j] = id;
     }
@@ -642,7 +647,10 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
   };
 #pragma unroll
   for (int n = 0; n < TURNS; ++n) issue(n, n);
-  if (rank == 0) always();
+  // (Written out here, the first warp waits for the ids: one token over 1,876 pages 7.9 us instead of 7.7. With many CTAs that
+  // wait is filled, and what is kept until later costs: 250 sequences 8.3 instead of 8.0.)
+  constexpr bool LATE = TT > 1 || CL;
+  if (!LATE) always();
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
     const int u = (tid + e * THREADS) / HD, c = tid % HD;
@@ -736,6 +744,7 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
   else if (TT > 1 && tokens == 3) score(std::integral_constant<int, TT == 1 ? 1 : 3>());
   else if (TT > 1) score(std::integral_constant<int, TT>());
   if (lost && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_PAGE);
+  if (LATE && rank == 0) always();
   if (rank == 0)                                   // (behind the keys zeros, up to a multiple of 32)
     for (int x = tid; x < HG * TT * 32; x += THREADS) {
       const int end = scored(x / 32 % TT), j = end + x % 32;
