@@ -1,6 +1,6 @@
 // The pages of a 4-bit cache that a query is likely to need: each page's bounds of the keys
 // (buddy_kv4_bounds) and each query's best pages by them (buddy_kv4_select).  Attention
-// over those lists is a form of the few-row kernel (kv4_attn.cu).
+// over those lists is a form of the few-row kernel (kv4_attn.cu), or a kernel of its own (kv4_lists.cu).
 //
 // For a channel c of a page's keys let lo_c <= k_pc <= hi_c.  Then for any position p
 //   q . k_p <= sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c,
