@@ -18,6 +18,7 @@ namespace buddy {
 // with CTAs of 128 threads 3.3; 16,000 sequences 34 us, with CTAs of 1,024 threads 51.)
 constexpr int kPlanThreads = 256;
 constexpr int kPlanMaxBatch = 16384;    // two counts per sequence in shared memory
+constexpr size_t plan_smem_bytes(int batch) { return 2 * ((size_t)batch + 1) * sizeof(int32_t); }
 
 // Largest i < n with a[i] <= x, for ascending a with a[0] <= x.
 __device__ __forceinline__ int last_at_most(const int32_t* a, int n, int x) {
@@ -153,9 +154,11 @@ extern "C" int buddy_page_plan(const buddy_page_plan_args* a, int32_t* flags, vo
   }
   int shift = 0;
   while ((1 << shift) < a->page_size) ++shift;
-  const size_t smem = 2 * ((size_t)a->batch + 1) * sizeof(int32_t);
-  if (smem > 40 * 1024 &&
-      cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+  const size_t smem = plan_smem_bytes(a->batch);
+  // the largest size any call uses: the attribute belongs to the function on the device, and a call's
+  // own would take it from another host thread's launch
+  if (smem > 40 * 1024 && cudaFuncSetAttribute(page_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)plan_smem_bytes(kPlanMaxBatch)) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   const int grid = min(max(1, a->n_tok / kPlanThreads + (a->n_tok % kPlanThreads != 0)), 152);
   return launch_k(page_plan_kernel, grid, kPlanThreads, smem, (cudaStream_t)stream, true, *a, shift, flags) == cudaSuccess

@@ -11,6 +11,9 @@ Tolerances, before any run:
       query in fp32 enters with 11 bits: its scores are off by at most 2^-11 of the
       largest sum of |q k|, and so the probabilities, relatively, by twice that.
 """
+import functools
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -129,6 +132,43 @@ def test_plan_failure_writes_nothing(what, flag):
     for k in got:
         if k != "flags":
             np.testing.assert_array_equal(got[k], before[k])
+
+
+def at_once(*calls, times=20000):
+    """Each call by a host thread of its own, over and over; what they raise is raised here."""
+    raised, start = [], threading.Barrier(len(calls))
+
+    def work(call):
+        start.wait()
+        try:
+            for _ in range(times):
+                call()
+        except Exception as e:
+            raised.append(e)
+
+    threads = [threading.Thread(target=work, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    if raised:
+        raise raised[0]
+
+
+def test_plans_of_two_batches_by_two_threads():
+    """Neither call's shared memory is taken from the other's."""
+    made, calls = [], []
+    for batch in (6000, 16384):
+        t, ref = make_plan([15, 3] * (batch // 2), [2, 1] * (batch // 2), 16, seed=batch)
+        calls.append(functools.partial(pkg().buddy_page_plan, t["length"], t["n_new"], 16, t["table"], t["free"], t["head"],
+                                       t["kv_len"], t["row_start"], t["slot"], t["pos"], t["head_out"], t["flags"],
+                                       stream=torch.cuda.Stream()))
+        made.append((t, ref))
+    torch.cuda.synchronize()
+    at_once(*calls)
+    for t, ref in made:
+        check_plan({k: v.cpu().numpy() for k, v in t.items()}, ref, 16)
 
 
 # ------------------------------------------------------------------ norm and rotation
