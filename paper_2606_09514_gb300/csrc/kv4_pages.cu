@@ -150,8 +150,11 @@ __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const Boun
 
 // ------------------------------------------------------------------ selection
 constexpr int kSelWarps = 8;            // of a CTA at most
-constexpr int kSelMaxPages = 40000;     // a score each in shared memory, next to the copies in flight
+constexpr int kSelMaxPages = 40000;     // a score each in shared memory, next to the copies in flight (a multiple of 32)
 constexpr int kSelCluster = 16;         // most CTAs of a (token, KV head)
+constexpr int kSelTokens = 4;           // most tokens of a sequence that share a walk
+constexpr int kSelShared = 8192;        // scores of a token up to which they do
+constexpr int kSelPairs = 512;          // up to which they do so over two heads' bounds
 constexpr int kSelBins = 256;
 
 struct SelectArgs {
@@ -445,6 +448,9 @@ struct Form {
   static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2, kTurns = TT == 1 ? 2 : 4;
   static constexpr int kGroup = kWarps / (TT * HG), kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = TT == 1 && !CL ? 7 : 2;
   static constexpr int kRing = kWarps * kTurns * kLoads * 1024;   // bytes
+  // shared memory of a call with so many scores per token, and of any call
+  static constexpr int smem(int slots) { return kRing + (int)sizeof(uint32_t) * HG * TT * slots; }
+  static constexpr int kMostSmem = smem(TT == 1 ? kSelMaxPages : HG == 1 ? kSelShared : kSelPairs);
 };
 
 // Up to TT tokens of a sequence share a walk over its pages' bounds; the CTA of the first of
@@ -847,8 +853,11 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
   }
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = kv4_select_kernel<T, HD, TT, HG, CL>;
-  const size_t smem = F::kRing + sizeof(uint32_t) * (size_t)(HG * TT) * A.slots;
-  if (smem > 40 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+  const int smem = F::smem(A.slots);
+  // the largest size any call uses: the attribute belongs to the function on the device, and a call's
+  // own would take it from another host thread's launch
+  if (smem > 40 * 1024 &&
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kMostSmem) != cudaSuccess)
     return BUDDY_ERR_CUDA;
   if (!CL) return launch_k(kern, (unsigned)ctas, F::kThreads, smem, s, true, A) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
   if (C > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return BUDDY_ERR_CUDA;
@@ -874,12 +883,10 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
 // 246; 750 pages, 25 to 750 in use: 54.8 and 45.4, the longest walk being the last to end). Clusters, where a
 // table has more pages than a CTA's warps take at once, as large as leaves every warp a turn and the
 // GPU (four CTAs an SM) room for all (one token of 8 KV heads over 1,876 pages: 64 us with a CTA for each head).
-constexpr int kSelTokens = 4;
-constexpr int kSelPairs = 512;          // scores of a token
 template <typename T, int HD>
 static int dispatch_select(SelectArgs A, cudaStream_t s) {
   A.slots = (std::max(1, A.a.s.max_pages - A.a.first - A.a.last) + 31) / 32 * 32;
-  if (A.a.s.max_new > 1 && (int64_t)A.slots * kSelTokens <= 32768) {
+  if (A.a.s.max_new > 1 && A.slots <= kSelShared) {
     if (A.p.nkv % 2 == 0 && A.slots <= kSelPairs) return launch_select<T, HD, kSelTokens, 2, false>(A, 1, s);
     return launch_select<T, HD, kSelTokens, 1, false>(A, 1, s);
   }

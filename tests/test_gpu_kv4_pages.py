@@ -3,12 +3,14 @@
 Bounds are values that the cache holds: they equal the oracle's.  Selections follow from sums
 in a stated order: they equal those of the same sums in numpy's fp32.  Attention has the
 tolerances of buddy_kv4_attention (test_gpu_kv4.py)."""
+import functools
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import kv4_oracle as O
-from test_gpu_kv4 import BAD_PAGE, BAD_POSITION, f64, flags, i32, make_cache, pkg
+from test_gpu_kv4 import BAD_PAGE, BAD_POSITION, at_once, f64, flags, i32, make_cache, pkg
 
 pytestmark = pytest.mark.gpu
 DTYPES = [torch.bfloat16, torch.float32]
@@ -788,3 +790,22 @@ def test_nothing_to_do():
     bounds = cache.empty_bounds()
     cache.buddy_kv4_bounds(bounds, i32([50]), table, i32([0, 0]), 5)
     assert not bounds.any()
+
+
+# ------------------------------------------------------------------ two callers
+@pytest.mark.parametrize("tokens,max_new,widths", [(1, 1, (300, 20000)), (400, 1, (3000, 40000)), (12, 3, (600, 8000))])
+def test_selections_over_tables_of_two_widths_by_two_threads(tokens, max_new, widths):
+    """Neither call's shared memory is taken from the other's: clusters, CTAs of a token, of four."""
+    lens = [16 * 20 - 3] * (tokens // max_new)
+    calls, checks = [], []
+    for n in widths:
+        cache, table, bounds, q = make_select(lens, [max_new] * len(lens), 16, (2, 1, 64), torch.bfloat16, seed=n, max_pages=n)
+        pages = torch.full((tokens, 1, 7), 55, dtype=torch.int32, device="cuda")
+        visible, kv_len, rows = torch.empty(tokens, dtype=torch.int32, device="cuda"), i32(lens), i32(starts_of([max_new] * len(lens)))
+        torch.cuda.synchronize()
+        calls.append(functools.partial(cache.buddy_kv4_select, q, bounds, kv_len, table, pages, visible, rows, max_new,
+                                       stream=torch.cuda.Stream()))
+        checks.append((pages, want_pages(q, bounds, table, lens, [max_new] * len(lens), 16, 7, 1, 1, tokens)[0]))
+    at_once(*calls)
+    for pages, want in checks:
+        np.testing.assert_array_equal(pages.cpu().numpy(), want)
