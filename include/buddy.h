@@ -619,7 +619,8 @@ BUDDY_API int buddy_kv4_bounds(const buddy_kv4_cache* cache, const buddy_kv4_seq
  * token (all pages but the last are whole), the same for every KV head: 0 for a
  * token without any position, -1, with its pages left as they were, for one that is
  * in no sequence, or in one whose length or row starts are bad
- * (BUDDY_DEV_BAD_POSITION). What is written overlaps no input. */
+ * (BUDDY_DEV_BAD_POSITION, also for a sequence without tokens). What is written
+ * overlaps no input. */
 typedef struct {
   buddy_kv4_seqs s;           /* max_pages <= 40000 (else BUDDY_ERR_RANGE) */
   int32_t n_q_heads;          /* a multiple of n_kv_heads, at most 8 times */

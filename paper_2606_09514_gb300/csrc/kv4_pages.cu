@@ -504,6 +504,14 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
       return;
     }
   }
+  if (!by_seq && t >= a.s.n_tok) {                 // behind the tokens' CTAs: the sequences, of which some have no token
+    const int64_t j = (int64_t)(unit - (unsigned)a.s.n_tok * (unsigned)gs) * THREADS + tid;
+    pdl_wait();
+    pdl_trigger();
+    Rows s{};
+    if (rank == 0 && j < a.s.batch && !rows_of(a.s, A.p.shift, (int)j, &s) && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
+    return;
+  }
   for (int b = tid; b < HG * TT * kSelBins; b += THREADS) search[b / kSelBins].bins[b % kSelBins] = 0;
   if (tid < HG * TT) search[tid].n_few = 0;
   constexpr int PER = (HG * TT * HD + THREADS - 1) / THREADS;
@@ -546,6 +554,7 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
       ok = rows_of(a.s, A.p.shift, i, &s);
     }
     t = s.t0 + chunk * TT;
+    if (!ok && chunk == 0 && g == 0 && tid == 0 && A.flags) atomicOr(A.flags, BUDDY_DEV_BAD_POSITION);
     if (!ok || chunk * TT >= s.m) return;          // (the CTAs behind see to the tokens)
     const T* q[PER];
 #pragma unroll
@@ -851,6 +860,7 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
       ctas = A.a.s.batch * chunks * (A.p.nkv / HG) + (A.a.s.n_tok + F::kThreads - 1) / F::kThreads;
     }
   }
+  if (A.chunks == 0 && A.a.s.row_start) ctas += (int64_t)(A.a.s.batch + F::kThreads - 1) / F::kThreads * C;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
   auto* const kern = kv4_select_kernel<T, HD, TT, HG, CL>;
   const int smem = F::smem(A.slots);

@@ -809,3 +809,37 @@ def test_selections_over_tables_of_two_widths_by_two_threads(tokens, max_new, wi
     at_once(*calls)
     for pages, want in checks:
         np.testing.assert_array_equal(pages.cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------ bad sequences without tokens
+@pytest.mark.parametrize("n_new,where", [([1] * 9, 4), ([1] * 400, 399), ([3, 4, 2, 4, 1], 2), ([1, 4, 0, 0, 1], 3),
+                                         ([2] * 300, 299), ([2] * 300, 0), ([4] + [0] * 700, 700), ([1], 0), ([1], 1)])
+@pytest.mark.parametrize("row", [10, 700])
+def test_select_tells_of_bad_sequences_without_tokens(n_new, where, row):
+    """They raise the flag as they do in the attention and the bounds; the others' lists are whole."""
+    n_new = n_new[:where] + [0] + n_new[where:]
+    lens, max_new = [16 * 9 - 1] * len(n_new), max(n_new)
+    cache, table, bounds, q = make_select(lens, n_new, 16, (4, 2, 64), torch.bfloat16, seed=where, max_pages=row)
+    wp, wv = want_pages(q, bounds, table, lens, n_new, 16, 3, 1, 1, len(q))
+    for n, flag in ((-1, BAD_POSITION), (16 * row + 1, BAD_POSITION), (2 ** 31 - 1, BAD_POSITION), (16 * row, 0), (0, 0)):
+        lens[where] = n
+        pages, visible = (torch.full(s, 55, dtype=torch.int32, device="cuda") for s in ((len(q), 2, 3), (len(q),)))
+        fl = flags()
+        cache.buddy_kv4_select(q, bounds, i32(lens), table, pages, visible, i32(starts_of(n_new)), max_new, flags=fl)
+        np.testing.assert_array_equal(pages.cpu().numpy(), wp)
+        np.testing.assert_array_equal(visible.cpu().numpy(), wv)
+        assert fl.item() == flag
+        if flag:
+            fl.zero_()
+            cache.buddy_kv4_bounds(cache.empty_bounds(), i32(lens), table, i32(starts_of(n_new)), max_new, fl)
+            assert fl.item() == BAD_POSITION
+
+
+def test_select_tells_of_row_starts_that_do_not_ascend():
+    lens = [16 * 9] * 4
+    cache, table, bounds, q = make_select(lens, [1] * 4, 16, (4, 2, 64), torch.bfloat16, max_pages=10)
+    for rows, max_new in (([0, 4, 1, 3, 4], 4), ([0, 1, 0, 1, 4], 3), ([0, 2, 1, 2, 3], 2), ([0, 1, 2, 4, 3], 2)):
+        pages, visible = (torch.full(s, 55, dtype=torch.int32, device="cuda") for s in ((4, 2, 3), (4,)))
+        fl = flags()
+        cache.buddy_kv4_select(q, bounds, i32(lens), table, pages, visible, i32(rows), max_new, flags=fl)
+        assert fl.item() == BAD_POSITION
