@@ -605,7 +605,8 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
   auto scored = [&](int u) { const int N = pages_of(p0 + u); return u < tokens && N > a.budget ? N - a.first - a.last : 0; };
   const int M = scored(tokens - 1);                // of the last token: the most
   // what is in without a score: the ends of long lists, of which a thread reads its first one early, and all of short ones
-  const int ends = a.first + a.last;
+  // (a list that is too short for a sequence's pages has fewer entries than a table may have: no count passes 32 bits)
+  const int ends = min(a.first + a.last, kSelMaxPages);
   auto end_of = [&](int x) {                       // the x-th of all tokens' ends
     const int u = TT == 1 ? 0 : x / ends, j = x - u * ends, N = pages_of(p0 + u);
     return N > a.budget ? row[j < a.first ? j : N - ends + j] : 0;
@@ -621,8 +622,8 @@ __global__ void __launch_bounds__(Form<TT, HG, CL>::kThreads, Form<TT, HG, CL>::
     }
     for (int u = 0; u < tokens && pages_of(p0 + u) <= a.budget; ++u) {
       const int N = pages_of(p0 + u);
-      for (int j = tid; j < a.budget; j += THREADS) {
-        const int32_t id = j < N ? row[j] : -1;
+      for (unsigned j = tid; j < (unsigned)a.budget; j += THREADS) {   // (a step may pass 2^31)
+        const int32_t id = j < (unsigned)N ? row[j] : -1;
 #pragma unroll
         for (int hl = 0; hl < HG; ++hl) list_of(u, hl)[j] = id;
       }

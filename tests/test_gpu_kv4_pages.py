@@ -843,3 +843,18 @@ def test_select_tells_of_row_starts_that_do_not_ascend():
         fl = flags()
         cache.buddy_kv4_select(q, bounds, i32(lens), table, pages, visible, i32(rows), max_new, flags=fl)
         assert fl.item() == BAD_POSITION
+
+
+@pytest.mark.parametrize("row", [12, 600])
+@pytest.mark.parametrize("max_new", [1, 2])
+@pytest.mark.parametrize("first,last", [(1, 1), (2 ** 31 - 2, 1), (2 ** 29, 1), (2 ** 29, 2 ** 30)])
+def test_select_into_the_longest_lists_there_may_be(row, max_new, first, last):
+    """Counts over their entries stay right next to 2^31: single tokens, clusters, tokens that share a walk."""
+    lens, budget = [16 * 9 - 3], 2 ** 31 - 1
+    cache, table, bounds, q = make_select(lens, [1], 16, (2, 1, 64), torch.bfloat16, max_pages=row)
+    pages = torch.full((1, 1, budget), 55, dtype=torch.int32, device="cuda")
+    visible, fl = torch.empty(1, dtype=torch.int32, device="cuda"), flags()
+    cache.buddy_kv4_select(q, bounds, i32(lens), table, pages, visible, i32([0, 1]), max_new, first, last, fl)
+    assert pages[0, 0, :9].tolist() == table[0, :9].tolist() and visible.item() == lens[0] and fl.item() == 0
+    for part in pages[0, 0, 9:].split(2 ** 28):
+        assert torch.all(part == -1)

@@ -2,6 +2,7 @@
 entries refuse."""
 import ctypes
 import os
+import re
 import subprocess
 
 import numpy as np
@@ -195,3 +196,17 @@ def test_first_memory_is_reached_after_a_cluster_barrier():
         first, last = body.index("put_first"), body.rindex("put_first")
         assert body.index("cluster_arrive_started") < body.index("cluster_wait_started") < first
         assert "cluster_sync" in body[last:]
+
+
+def test_no_count_over_a_lists_entries_passes_32_bits():
+    """A list may have 2^31 - 1 entries, and as many first and last pages: a signed counter that goes up to
+    them in steps, or a product with the tokens, would pass 2^31, and the loop not end."""
+    from test_kernel_sources import CSRC, code
+    text = code(CSRC / "kv4_pages.cu")
+    loops = re.findall(r"for \((\w+) (\w+) = [^;]*; \2 < ([^;]*); \2 \+= THREADS\)", text)
+    assert any("budget" in end for _, _, end in loops) and any("ends" in end for _, _, end in loops)
+    for kind, _, end in loops:
+        if re.search(r"budget|first|last", end):
+            assert kind in ("unsigned", "int64_t"), end
+    assert re.search(r"int ends = min\(a\.first \+ a\.last, kSelMaxPages\);", text)
+    assert int(re.search(r"kSelMaxPages = (\d+);", text).group(1)) * 4 + 256 < 2 ** 31
