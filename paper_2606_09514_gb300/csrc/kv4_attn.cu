@@ -76,7 +76,6 @@ __host__ __device__ constexpr int ctas_per_sm() { return (NB == 1 && !LISTS ? 4 
 constexpr int kWhole = 12;       // streams of at most this many chunks are not cut
 constexpr int kOpen = 10;        // what beginning and ending a stream costs, in chunks
 constexpr int kMany = 2 * kOpen; // shares from this on hold several short streams
-constexpr int kMaxGrid = 1024;   // CTAs: four on each of at most 256 SMs
 constexpr int kJoin = 8;         // partials in flight when a cut stream is joined
 constexpr int kOneTeam = 24;     // spans up to which one CTA joins them all
 constexpr int kTeam = 4;         // spans of a team: a multiple of this
@@ -604,6 +603,8 @@ static int sm_count() {
 template <int HD, int NB, bool WIDE, bool LISTS>
 static int launch_decode(const AttnArgs4& A, int64_t most, int sms, cudaStream_t s) {
   constexpr int smem = smem_bytes<HD, NB>();
+  static_assert(kMaxGrid * sizeof(int32_t) <= kWsCounters, "");
+  static_assert(2 * kMaxGrid * partial_floats<HD, NB>() * sizeof(float) <= few_bytes(HD) - kWsCounters, "");
   auto* const kern = kv4_decode_kernel<HD, NB, WIDE, LISTS>;
   const int grid = (int)std::min<int64_t>(most, std::min(kMaxGrid, ctas_per_sm<NB, WIDE, LISTS>() * sms));
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return BUDDY_ERR_CUDA;
@@ -626,9 +627,6 @@ static int launch_few(const AttnArgs4& A, int head_dim, bool two, bool wide, int
 }  // namespace buddy
 
 using namespace buddy;
-
-constexpr int64_t kWsCounters = 8192;   // bytes of arrival counters in front of a workspace
-static int64_t few_bytes(int head_dim) { return kWsCounters + (int64_t)kMaxGrid * 2 * 16 * (head_dim + 2) * 4; }
 
 static bool sizes_ok(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_new) {
   return n_kv_heads >= 1 && n_kv_heads <= 1024 && n_q_heads >= n_kv_heads && n_q_heads % n_kv_heads == 0 &&

@@ -8,6 +8,10 @@ namespace buddy {
 namespace kv4 {
 
 constexpr int kChunk = 32;
+// The workspace of these kernels: arrival counters, then partials.
+constexpr int kMaxGrid = 1024;          // CTAs that have two partials of sixteen rows each: four on each of at most 256 SMs
+constexpr int64_t kWsCounters = 8192;   // bytes of counters
+constexpr int64_t few_bytes(int head_dim) { return kWsCounters + (int64_t)kMaxGrid * 2 * 16 * (head_dim + 2) * 4; }
 template <int HD>
 __host__ __device__ constexpr int stage_bytes() { return 2 * kChunk * entry_bytes(HD); }
 // Chunks of a stream of n positions.  (A sequence without positions: one of nothing.)

@@ -360,6 +360,9 @@ __global__ void __launch_bounds__(kListThreads, list_ctas<WIDE>()) kv4_lists_ker
 
 template <int HD, bool WIDE>
 static int launch(const AttnArgs4& A, int sms, cudaStream_t s) {
+  constexpr int64_t warps = (int64_t)kListMaxGrid * kListWarps;
+  static_assert(warps * sizeof(int32_t) <= kWsCounters, "");
+  static_assert(2 * warps * list_part<HD>() * sizeof(float) <= few_bytes(HD) - kWsCounters, "");
   auto* const kern = kv4_lists_kernel<HD, WIDE>;
   constexpr int smem = list_smem<HD>();
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return BUDDY_ERR_CUDA;
