@@ -858,3 +858,36 @@ def test_select_into_the_longest_lists_there_may_be(row, max_new, first, last):
     assert pages[0, 0, :9].tolist() == table[0, :9].tolist() and visible.item() == lens[0] and fl.item() == 0
     for part in pages[0, 0, 9:].split(2 ** 28):
         assert torch.all(part == -1)
+
+
+# ------------------------------------------------------------------ CTAs by sequences
+@pytest.mark.parametrize("batch", [31, 255, 256, 257, 700])
+@pytest.mark.parametrize("heads,row", [((4, 2, 64), 30), ((3, 1, 128), 30), ((2, 2, 64), 600)])
+def test_select_proposed_tokens_of_many_sequences(batch, heads, row):
+    """As many sequences as a CTA has threads, fewer and more; of equal lengths, empty and bad ones among
+    them, and rows behind the last: over two heads at once, over one, over tables too wide for two."""
+    rng = np.random.default_rng(batch)
+    lens = [int(n) for n in rng.integers(0, 16 * 25, batch)]
+    for i in range(0, batch, 3):
+        lens[i] = 16 * 20 + 7
+    for i in range(5, batch, 11):
+        lens[i] = 0
+    n_new = [int(m) for m in rng.integers(2, 6, batch)]       # (more than four: two chunks)
+    n_new[batch - 1], pad = 4, 4 * batch                       # (so that most have as many as the longest)
+    for most in (4, 5):
+        new = [min(m, most) for m in n_new]
+        cache, table, bounds, q = make_select(lens, new, 16, heads, torch.bfloat16, seed=batch, pad=pad, max_pages=row)
+        check_select(cache, table, bounds, q, lens, new, 6)
+        kv, at, T = list(lens), starts_of(new), len(q)
+        for i, n in zip((0, 7, batch // 2, batch - 1), (-1, 16 * row + 1, 2 ** 31 - 1, -2 ** 31)):
+            kv[i] = n
+        wp, wv = want_pages(q, bounds, table, lens, new, 16, 6, 1, 1, T)
+        wp[at[-1]:] = 55
+        for i in (0, 7, batch // 2, batch - 1):
+            wp[at[i]:at[i + 1]], wv[at[i]:at[i + 1]] = 55, -1
+        pages, visible = (torch.full(s, 55, dtype=torch.int32, device="cuda") for s in ((T, heads[1], 6), (T,)))
+        fl = flags()
+        cache.buddy_kv4_select(q, bounds, i32(kv), table, pages, visible, i32(at), most, flags=fl)
+        np.testing.assert_array_equal(pages.cpu().numpy(), wp)
+        np.testing.assert_array_equal(visible.cpu().numpy(), wv)
+        assert fl.item() == BAD_POSITION
