@@ -55,7 +55,7 @@ struct OneAxis {};
 // neighbours' lie between: their sectors would be fetched twice (8,297 tokens 79 us, with loads of
 // the head after this one 54).
 constexpr int kRowAhead = 3;
-constexpr int kRowRing = kRowAhead * kRowThreads * 32;   // bytes
+constexpr int kRowHead = kRowThreads * 32, kRowRing = kRowAhead * kRowHead;   // bytes of a CTA
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -202,11 +202,14 @@ __device__ __forceinline__ uint32_t encode8(const F2* x, uint32_t mask, __half* 
 // of a multiple of eight frequencies per axis): rows of the tables in wide loads, as with one
 // axis. Where they have not, each value is loaded by itself.  (In wide loads of every axis, and a
 // choice between them, 64 tokens whose frequencies go round three axes took 3.8 us instead of 3.4.)
-// ONE: a team has one head, which it loads itself (with the copies' code 64 tokens appended and read took 5.0 us
-// instead of 4.8).
-template <typename T, int HD, bool CACHE, typename AX, bool ONE>
+enum class Team {
+  One,        // one head, which the team loads itself (with the copies' code 64 tokens appended and read took 5.0 us instead of 4.8)
+  Next,       // several, the next one in registers while one is worked on
+  Ring        // several, kRowAhead of them in shared memory
+};
+template <typename T, int HD, bool CACHE, typename AX, Team TEAM>
 __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, const AX ax) {
-  constexpr bool AXES = std::is_same<AX, Axes>::value;
+  constexpr bool AXES = std::is_same<AX, Axes>::value, ONE = TEAM == Team::One, RING = TEAM == Team::Ring;
   constexpr int LPH = HD / 16, HALF = HD / 2;
   const buddy_qk_rows& R = A.r;
   const int kq = R.n_q_heads, kk = kq + R.n_kv_heads, heads = kk + (CACHE ? R.n_kv_heads : 0);
@@ -231,21 +234,22 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
   // a lane's pieces of 16 bytes of a head's halves, those of the other threads between them
   extern __shared__ __align__(16) uint8_t rows_smem[];
   const uint32_t ring = ptx::smem_u32(rows_smem) + threadIdx.x * 16;
-  auto ahead = [&](int h) {
+  uint32_t held = 0;                            // where in the ring the head at hand is
+  auto ahead = [&](int h, uint32_t at) {
     if (h < h1) {
       const T* src = row(h);
-      const uint32_t to = ring + (h - h0) % kRowAhead * (kRowThreads * 32);
+      const uint32_t to = ring + at;
       copy16(to, src);
       copy16(to + kRowThreads * 16, src + HALF);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  constexpr bool RING = !ONE && sizeof(T) == 2;
+  static_assert(!RING || sizeof(T) == 2, "");
   if constexpr (!RING) {
     lo.load(row(h0));
     hi.load(row(h0) + HALF);
   } else {
-    for (int h = h0; h < h0 + kRowAhead - 1; ++h) ahead(h);
+    for (int j = 0; j < kRowAhead - 1; ++j) ahead(h0 + j, j * kRowHead);
   }
   int p = R.pos[t], most = p, least = p;        // (of all axes)
   int q[4] = {p, p, p, p};                      // positions on the axes
@@ -293,9 +297,10 @@ __global__ void __launch_bounds__(kRowThreads) qk_rows_kernel(const RowArgs A, c
   for (int h = h0; h < h1; ++h) {
     F2 a[4], b[4];                              // lower and upper half
     if constexpr (RING) {
-      ahead(h + kRowAhead - 1);                 // to where the head before this one was
+      ahead(h + kRowAhead - 1, held == 0 ? kRowRing - kRowHead : held - kRowHead);   // to where the head before this one was
       asm volatile("cp.async.wait_group %0;" ::"n"(kRowAhead - 1) : "memory");
-      const uint8_t* const at = rows_smem + (h - h0) % kRowAhead * (kRowThreads * 32) + threadIdx.x * 16;
+      const uint8_t* const at = rows_smem + held + threadIdx.x * 16;
+      held = held == kRowRing - kRowHead ? 0 : held + kRowHead;
       lo.load(reinterpret_cast<const T*>(at));
       hi.load(reinterpret_cast<const T*>(at + kRowThreads * 16));
     }
@@ -435,6 +440,12 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
 // on: 250 tokens of 40 heads 4.6 us instead of 5.3, 1,000 7.7 instead of 9.4 (an append does more with what it
 // has read: 250 tokens of fp32 7.4 instead of 6.9, so it does not).
 constexpr int64_t kRowTeams = 16384;
+// Heads of a call from which on bf16 appends with one axis take the ring. Below, with rows that a projection has left
+// in L2, its turns cost more than the registers that it saves (32 + 16 heads, in registers and by the ring: 3,000 tokens
+// with norms 19.9 and 21.5 us, 8,297 44.0 and 42.8; without norms 2,200 12.5 and 13.8, 6,000 31.2 and 28.5). Rows from HBM
+// gain by the ring earlier: 3,000 tokens without norms 20.4 and 19.9, with norms 23.0 and 23.6. With several axes it is the
+// ring throughout (3,000 tokens with norms, three axes in runs: 20.7 and 22.1 us, from HBM 25.8 and 24.6).
+constexpr int64_t kRingNorms = 17 * kRowTeams, kRingPlain = 9 * kRowTeams;
 // Whether a lane's eight frequencies have different axes somewhere.
 static bool mixed(const OneAxis&) { return false; }
 static bool mixed(const Axes& a) {
@@ -451,9 +462,19 @@ static int launch_rows(RowArgs A, const AX& ax, cudaStream_t s) {
   A.groups = (heads + A.per - 1) / A.per;
   const int64_t ctas = ((int64_t)A.r.n_tok * (HD / 16) + kRowThreads - 1) / kRowThreads * A.groups;
   if (ctas > INT32_MAX) return BUDDY_ERR_RANGE;
-  auto* const kern = A.per == 1 ? qk_rows_kernel<T, HD, CACHE, AX, true> : qk_rows_kernel<T, HD, CACHE, AX, false>;
-  return launch_k(kern, (unsigned)ctas, kRowThreads, A.per > 1 && sizeof(T) == 2 ? kRowRing : 0, s, true, A, ax) == cudaSuccess
-             ? BUDDY_OK : BUDDY_ERR_CUDA;
+  auto launch = [&](auto* kern, int smem) {
+    return launch_k(kern, (unsigned)ctas, kRowThreads, smem, s, true, A, ax) == cudaSuccess ? BUDDY_OK : BUDDY_ERR_CUDA;
+  };
+  if (A.per == 1) return launch(qk_rows_kernel<T, HD, CACHE, AX, Team::One>, 0);
+  if constexpr (sizeof(T) == 4) {
+    return launch(qk_rows_kernel<T, HD, CACHE, AX, Team::Next>, 0);
+  } else {
+    if constexpr (CACHE && std::is_same<AX, OneAxis>::value) {
+      if ((int64_t)A.r.n_tok * heads < (A.r.q_gain || A.r.k_gain ? kRingNorms : kRingPlain))
+        return launch(qk_rows_kernel<T, HD, CACHE, AX, Team::Next>, 0);
+    }
+    return launch(qk_rows_kernel<T, HD, CACHE, AX, Team::Ring>, kRowRing);
+  }
 }
 template <bool CACHE, typename AX>
 static int dispatch_rows(const RowArgs& A, const AX& ax, cudaStream_t s) {

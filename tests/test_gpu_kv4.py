@@ -345,6 +345,27 @@ def test_append_and_read_leave_bad_slots_out():
         assert torch.all(x[1] == 7) and torch.all(x[3] == 7) and not torch.any(x[0] == 7)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gains", [True, False])
+@pytest.mark.parametrize("heads", [(9, 3, 64), (6, 5, 128)])
+def test_append_stores_the_same_in_calls_of_any_size(heads, gains, dtype):
+    """Few tokens, some thousands, many: a team's heads are loaded in three ways."""
+    nq, nkv, hd = heads
+    T, page = 20001, 32
+    q, k, v, pos, rope, gain = make_rows(T, heads, dtype, seed=1, gains=gains)
+    slot = torch.randperm(20032, device="cuda")[:T].contiguous()
+    whole, pieces = (pkg().KV4Cache.empty(20032 // page, page, nkv, hd) for _ in range(2))
+    want, got = (torch.empty(T, nq, hd, dtype=dtype, device="cuda") for _ in range(2))
+    whole.buddy_kv4_append(q, k, v, pos, slot, rope, want, *gain, EPS)
+    at = 0
+    for n in (1, 500, 3001, 2000, 7, 7500, 6992):
+        cut = slice(at, at + n)
+        pieces.buddy_kv4_append(q[cut], k[cut], v[cut], pos[cut], slot[cut], rope, got[cut], *gain, EPS)
+        at += n
+    assert at == T and torch.equal(got, want)
+    assert torch.equal(whole.k_pages, pieces.k_pages) and torch.equal(whole.v_pages, pieces.v_pages)
+
+
 # ------------------------------------------------------------------ attention
 def make_cache(kv_len, page, nkv, hd, seed=0, nan_tail=True, first_page=0, n_pages=None):
     """Random pages, a table over them, and each sequence's values in float64."""
