@@ -23,18 +23,19 @@
 // into the softmax's factor.  Probabilities are rounded to half for the product only (their sum is taken
 // before): each by 2^-11 of it at most, or 2^-32 of the row's largest where that is more.  With fp32
 // queries or outputs (WIDE) both are sums of two halves: twice the MMAs and a CTA less per SM
-// (64 sequences of 8,192 positions 148 us instead of 121; errors of 2^-12 become 2^-21).
+// (64 sequences of 8,192 positions 150 us instead of 125; errors of 2^-12 become 2^-21).
 //
 // Work: all streams end to end, each as its chunks of 32 positions and kOpen chunks'
 // worth for its beginning and end, in equal shares per CTA.  (With kOpen 4, 8, 10 and 12:
-// 250 sequences of 512 to 8,192 positions and 4 KV heads 98.9, 93.0, 89.5 and 90.5 us; 31
-// of 100 to 4,096 with up to five new tokens and 40 KV heads 76, 60, 60 and 61.)  A short
+// 250 sequences of 512 to 8,192 positions and 4 KV heads 95.8, 92.0, 90.1 and 90.9 us; 31
+// of 100 to 4,096 with up to five new tokens and 40 KV heads 61.3, 59.8, 60.0 and 60.9.)  A short
 // stream belongs to the share where it begins: what a CTA saves by passing on a part of it,
 // the partials cost again.  In a share, four warps take the chunks of a stream in turn or,
 // where there are several short streams, a warp the whole of every fourth, without barriers
-// and joins (250 sequences of 50 to 200 positions, 8 KV heads: 19.0 us, 25.5 with their
-// chunks in turn; 1,000 of 20 to 250: 54 and 76; with long streams among them it loses, 250 of
-// 30 to 1,000 take 40 us instead of 37, and a sixth more with up to 16 chunks instead of 12).
+// and joins (with three stages, 250 sequences of 50 to 200 positions, 8 KV heads: 19.0 us, 25.5 with
+// their chunks in turn; 1,000 of 20 to 250: 54 and 76; with long streams among them it loses, 250 of
+// 30 to 1,000 took 40 us instead of 37.  Streams of up to 8, 12 and 16 chunks, with two stages: 250 of
+// 30 to 1,000 positions 53, 58 and 59 us, 250 of 50 to 200 and 1,000 of 20 to 250 alike).
 // Each warp has its own ring of stages, which runs on across streams: one lane copies a
 // chunk in four bulk copies, in whole halves of 16 positions, and what lies behind the
 // sequence's end, or has no page, is masked.  A stream within a share is written out; the CTAs of one
@@ -42,8 +43,8 @@
 // where they are many, by teams first (one sequence of 120,001 positions, 4 KV heads, 152
 // CTAs each: 49 us with one join, 32 with teams).
 //
-// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (567 MB) take 120 us,
-// their copies alone 91 us (94% of HBM's rate), the arithmetic alone 100; a chunk is about
+// Bound by instructions: 64 sequences of 8,192 positions and 8 KV heads (604 MB) take 125 us,
+// their copies alone 99 us (90% of HBM's measured rate), with instructions issued in 65% of the cycles; a chunk is about
 // 700 instructions of a warp, 350 of them codes to halves.  One token over 2,048 positions
 // takes 8.4 us a call: 1 for the lengths and shares, 2 for the page ids and the first chunk, 1.5
 // for two chunks, 4 for partials, arrival and join.
@@ -66,7 +67,9 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 // A chunk on its way while one is worked on.  (With two on their way: one token over 120,001 positions 40.4 us instead
 // of 38.9, over 2,048 9.0 instead of 8.4, 250 sequences 91.2 instead of 90.1; with two blocks of rows they leave room for
-// fewer CTAs: 64 sequences of 4,096 positions, four tokens, 8 KV heads 147 us instead of 102.)
+// fewer CTAs: 64 sequences of 4,096 positions, four tokens, 8 KV heads 148 us instead of 97.  What it costs: with two blocks
+// of rows, and two chunks per warp, the second is asked for when the first has come, 1 us: four tokens over 4,096 positions
+// 17.7 us instead of 16.5, of four sequences of 2,048 16.7 instead of 15.5; over 16,384 21.8 instead of 28.5.)
 constexpr int kStages = 2;
 // CTAs per SM: by registers (128 a thread with one block of eight rows, 168 with two; WIDE
 // 168 and 255).  Lists are few and short here, so that latency counts: three CTAs, which spill nothing (one token,
@@ -81,7 +84,7 @@ constexpr int kOneTeam = 24;     // spans up to which one CTA joins them all
 constexpr int kTeam = 4;         // spans of a team: a multiple of this
 // Rows of a KV head up to which these kernels take a sequence.  (With a limit of 32, 28 rows
 // over 4 KV heads took, 16 sequences of 4,096 positions, 57 us here and 45 us with the
-// prompts' kernel; one of 30,000 43 and 32; 100 of 600 67 and 68.)
+// prompts' kernel; one of 30,000 43 and 32; 100 of 600 67 and 68; with three stages.)
 constexpr int kFewRows = 16;
 
 // A warp's outputs, maxima and sums when the warps are joined: with one block of rows in
@@ -644,7 +647,8 @@ extern "C" int64_t buddy_kv4_attention_workspace(int32_t n_q_heads, int32_t n_kv
 }
 
 // Lists from which on warps take them alone. (Lists of 32 pages of 64 positions, 8 KV heads, 32 query heads, in
-// CTAs' turns and by warps alone: 128 lists 17.5 and 24.8 us, 256 27.0 and 28.8, 512 42.2 and 41.4, 1,024 72.4 and 68.2.)
+// CTAs' turns and by warps alone: 128 lists 17.5 and 24.8 us, 256 27.0 and 28.8, 512 42.2 and 41.4, 1,024 72.4 and 68.2;
+// other layouts were not measured at the switch.)
 constexpr int64_t kManyLists = 512;
 
 // Both forms; LISTS: a list of pages for each token and KV head.

@@ -58,7 +58,9 @@ __device__ __forceinline__ __half2 shfl_xor(__half2 v, int o) {
 // Bound by instructions: 120,001 positions of 8 KV heads (77 MB) take 19.4 us, 4.0 TB/s, of which a word of
 // eight channels costs thirteen logical or comparing instructions and six of the products'. (Up to 16
 // positions per lane on their way; with 8 20.0 us. Comparisons of three fp32 values at once: 29.8 us.)
-// The last pages of 250 sequences take 3.7 us, the chain of length, page id and keys.
+// The last pages of 250 sequences take 3.7 us, the chain of length, page id and keys.  There are CTAs for as many pages of every
+// sequence as the longest piece of the call may have, which find that they have none: 249 single tokens next to a prompt of
+// 2,000 take 19 us, of 100,000 800 (the prompt alone: 15).
 template <int HD>
 __global__ void __launch_bounds__(32 * kBoundWarps) kv4_bounds_kernel(const BoundArgs A) {
   constexpr int LPR = HD / 16, RPL = 32 / LPR;     // lanes per position, positions per load
@@ -446,6 +448,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
 template <int TT, int HG, bool CL>
 struct Form {
   static constexpr int kWarps = TT == 1 && !CL ? 4 : 8, kThreads = 32 * kWarps, kLoads = TT == 1 ? 4 : 2, kTurns = TT == 1 ? 2 : 4;
+  // (kCtas by registers: with the ring's shared memory a CTA of one token is there six times an SM at most)
   static constexpr int kGroup = kWarps / (TT * HG), kKept = TT == 1 ? (CL ? 8 : 4) : 16, kCtas = TT == 1 && !CL ? 7 : 2;
   static constexpr int kRing = kWarps * kTurns * kLoads * 1024;   // bytes
   // shared memory of a call with so many scores per token, and of any call
@@ -462,10 +465,11 @@ struct Form {
 // bounds of a page lie next to each other and go to neighbouring lanes.
 //
 // Bound by latencies where tokens are few: one token of 32 heads over 8 takes 7.7 us over 1,876 pages
-// (7.7 MB): 0.7 for the length, 0.5 for the page ids, 1.2 for the bounds, 0.7 for the cluster's barrier, 2 for the
-// search and the output, the launch; 250 sequences of 8 to 128 pages, 28 heads over 4 (18 MB), 8.0. By
-// instructions where several tokens share a walk: 31 sequences of up to 750 pages and five tokens, 40 KV
-// heads (115 MB), 45 us, 2.5 TB/s. What it gained: a search by counts 64.8 -> 11.8 with the clusters (one token), copies
+// (7.7 MB); time stamps of the clusters' first CTAs (medians, after the wait for the work before): lengths and page ids 0.7,
+// copies on their way 1.3, scores 3.2, the cluster's barrier 3.8, search 5.9, output 6.7. 250 sequences of 8 to 128
+// pages, 28 heads over 4 (18 MB), 8.1. By instructions where several tokens share a walk: 31 sequences of up to 750 pages and
+// five tokens, 40 KV heads (115 MB), 45 us, 2.5 TB/s; of a CTA's 13.8 us (median) the walk is 8.4, what comes before it 2.1,
+// search and output 3.3. What it gained: a search by counts 64.8 -> 11.8 with the clusters (one token), copies
 // that need no registers instead of loads 11.8 -> 9.5, packed instructions over pairs of eights and code for
 // each number of tokens 62 -> 55 us (31 sequences), the longest sequences first 55 -> 45.
 template <typename T, int HD, int TT, int HG, bool CL>
@@ -891,9 +895,16 @@ static int launch_select(SelectArgs A, int C, cudaStream_t s) {
 // Several tokens of a sequence share a walk where there may be such, over two heads' bounds where the table
 // is short, so that what a CTA does before and after its walk counts (31 sequences of up to five tokens, 40 KV
 // heads, 256 pages: 47.5 us, one head each 57.7; 9 prompts of up to 1,500 tokens, 8 KV heads, 60 pages: 142 and
-// 246; 750 pages, 25 to 750 in use: 54.8 and 45.4, the longest walk being the last to end). Clusters, where a
-// table has more pages than a CTA's warps take at once, as large as leaves every warp a turn and the
-// GPU (four CTAs an SM) room for all (one token of 8 KV heads over 1,876 pages: 64 us with a CTA for each head).
+// 246; 750 pages, 25 to 750 in use: 54.8 and 45.4, the longest walk being the last to end; widths between 256 and 750
+// were not measured). Clusters, where a table has more pages than a CTA's warps take at once, as large as leaves every warp
+// a turn, and up to 608 CTAs: twice as many as are resident at once by registers (two an SM; one by shared memory, from some
+// 12,000 pages on), a number that was not measured against smaller ones (one token of 8 KV heads over 1,876 pages 7.6 us,
+// 64 with a CTA for each head; four such sequences 14.5).
+//
+// Form and shared memory go by the table's width, not by what is in use: 250 sequences of 8 to 128 pages take 8.2 us
+// under tables of 129 to 2,048 entries, 9.8 of 8,192, 19 of 40,000; 31 sequences of several tokens and up to 750 pages 45 under
+// 751 to 2,048, 71 under 8,000. And tokens that share a walk have no clusters: one sequence over 1,876 pages, 8 KV heads,
+// takes 37 us with two tokens and 47 with four to eight, over 7,500 pages 128 and 172 (one token: 7.6 and 20).
 template <typename T, int HD>
 static int dispatch_select(SelectArgs A, cudaStream_t s) {
   A.slots = (std::max(1, A.a.s.max_pages - A.a.first - A.a.last) + 31) / 32 * 32;

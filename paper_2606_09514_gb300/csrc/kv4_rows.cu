@@ -15,9 +15,9 @@
 // codes, one bit decides.
 //
 // Bound by HBM from thousands of tokens on (8,297 of 40 heads, 174 MB: 29.8 us a call, 5.9
-// TB/s, with instructions issued in 59% of the cycles; in fp32, 348 MB, 53.9 us, 6.4 TB/s); below by the latency of position,
+// TB/s, with instructions issued in 63% of the cycles; in fp32, 348 MB, 53.9 us, 6.4 TB/s); below by the latency of position,
 // rotation factors and rows, one after the other: one token 2.5 us, an append of 64 and
-// their read 4.8.  With three axes in runs of frequencies 7,901 tokens take 30.8 us, in turn 34.5.
+// their read 4.8.  With three axes in runs of frequencies 7,901 tokens take 31.0 us, in turn 34.0.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -437,7 +437,7 @@ kv4::Pages kv4_pages(const buddy_kv4_cache* c) {
 // (8,297 tokens of 40 heads 29.8 us, a fifth more with four; append of 4,999 tokens of
 // 36 heads and their read 22.4, 12% more with four).
 // Where the axes change within a lane's frequencies the reads are many and narrow, and shared from fewer rows
-// on: 250 tokens of 40 heads 4.6 us instead of 5.3, 1,000 7.7 instead of 9.4 (an append does more with what it
+// on: 250 tokens of 40 heads 4.6 us instead of 5.3, 1,000 8.5 instead of 9.4 (an append does more with what it
 // has read: 250 tokens of fp32 7.4 instead of 6.9, so it does not).
 constexpr int64_t kRowTeams = 16384;
 // Heads of a call from which on bf16 appends with one axis take the ring. Below, with rows that a projection has left
